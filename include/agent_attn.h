@@ -305,6 +305,125 @@ int agent_attn_aggregate_static(agent_attn_handle* h, const void* A, const void*
 /* Size in bytes of the fixed scratch array used by agent_attn_aggregate_static. */
 size_t agent_attn_static_scratch_bytes(void);
 
+/* ------------------------------------------------------------------------------------------------
+ * Queries and keys before the attention: an RMS norm of each head and rotary positions.
+ *
+ * Per head row x of d channels of a token at position p (one coordinate for each of up to three axes, e.g.
+ * time, height and width):
+ *     y = gain * x / sqrt(mean(x^2) + eps)            (without a norm: y = x)
+ *     (y_u, y_v) -> (y_u cos t - y_v sin t, y_u sin t + y_v cos t),  t = p[axis] * freq[pair]
+ * for every pair (u, v) of channels.  Axis a turns the next channels[a] channels of the head, beginning
+ * at channel 0; what is left of the head keeps y.  Sums and angles are fp32 (an angle with the rounding
+ * error of its product, so that large positions keep their accuracy); one rounding to the element type. */
+typedef enum {
+    AA_PAIRS_HALVES = 0,      /* channel i of an axis's segment with i + channels[a] / 2           */
+    AA_PAIRS_NEIGHBOURS = 1   /* channel 2i with 2i + 1                                            */
+} aa_pairs;
+
+typedef struct {
+    int axes;                 /* 0 (no rotation) .. 3                                              */
+    int extent[3];            /* grid of the tokens, row-major over extent[0 .. axes - 1], whose product
+                                 is the token count; not read where `positions` is given          */
+    int channels[3];          /* channels of a head that each axis turns: even, sum <= head_dim    */
+    int pairs;                /* aa_pairs                                                          */
+    const float* freq;        /* device fp32 [sum(channels) / 2]: radians per unit, axis after axis */
+    const float* positions;   /* device fp32 [B or 1][N][axes], or NULL: coordinates in the grid   */
+    long long positions_batch;/* elements between the batch entries of `positions`; 0: shared      */
+} agent_attn_rotary;
+
+typedef struct {
+    const void* q_gain;       /* device [head_dim], element type, or NULL (1): gain of the queries */
+    const void* k_gain;       /* the same for the keys                                             */
+    float eps;                /* >= 0                                                              */
+} agent_attn_norm;
+
+/* Norm and rotation of queries and keys in one pass.
+ *   Q, K         device; element (b, head, token, c) at base + b * in_strides[0] + head * in_strides[1]
+ *                + token * in_strides[2] + c.  Either may be NULL (its result is then not written)
+ *   in_strides   host, 3 values in ELEMENTS shared by Q and K (multiples of 16 bytes, token stride
+ *                >= head_dim), or NULL: dense [B][heads][N][d]
+ *   rotary       NULL: norm alone.  Its freq and positions need 4-byte alignment only
+ *   norm         NULL: rotation alone
+ *   Q_out, K_out device, strides out_strides (NULL: dense).  Either may be its own input where both have the
+ *                same strides (in place: a fused projection's output is prepared where
+ *                agent_attn_forward_strided reads it); no other overlap
+ * Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED (N > max_tokens), AA_ERR_CUDA.  No host synchronisation,
+ * no allocation. */
+int agent_attn_rotate(agent_attn_handle* h, const void* Q, const void* K, const long long in_strides[3], int n_tokens,
+                      const agent_attn_rotary* rotary, const agent_attn_norm* norm,
+                      void* Q_out, void* K_out, const long long out_strides[3], void* stream);
+
+/* Bytes of device workspace for agent_attn_rotate_backward with a norm (shares of the gains' gradients).  0 for a
+ * NULL handle. */
+size_t agent_attn_rotate_workspace_bytes(const agent_attn_handle* h);
+
+/* Gradient of agent_attn_rotate.
+ *   dQ_out, dK_out device fp32, strides grad_strides (NULL: dense): gradients of its results, as
+ *                  agent_attn_backward writes them.  Either may be NULL with everything of its side
+ *   Q, K           device, strides in_strides (NULL: dense): the forward call's inputs.  Not read without a norm
+ *   rotary, norm   as in the forward call
+ *   dQ, dK         device fp32, strides out_strides (NULL: dense): gradients of Q and K; each may be dQ_out or
+ *                  dK_out itself where the strides are the same
+ *   dq_gain, dk_gain  device fp32 [head_dim], or NULL: gradients of the gains, summed over batch, heads and tokens
+ *   workspace      device, >= agent_attn_rotate_workspace_bytes; not read without a norm
+ * Sums are taken in a fixed order.  Errors as in agent_attn_rotate, and AA_ERR_WORKSPACE. */
+int agent_attn_rotate_backward(agent_attn_handle* h, const float* dQ_out, const float* dK_out, const long long grad_strides[3],
+                               const void* Q, const void* K, const long long in_strides[3], int n_tokens,
+                               const agent_attn_rotary* rotary, const agent_attn_norm* norm,
+                               float* dQ, float* dK, const long long out_strides[3], float* dq_gain, float* dk_gain,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Gated feed-forward product: the two projections of a block's feed-forward part, the activation of one and
+ * their product, in one kernel:
+ *     H = act(X Wg^T + bg) * (X Wu^T + bu)
+ * The projection back to the channels is a plain product of H and stays with the caller, like the attention's
+ * projections.  Of the handle it uses device and element type.  Sums, biases, activation and product are
+ * fp32, H is rounded once.  fp32 tensors enter the tensor cores as sums of three bf16 terms (fp32 accuracy; an
+ * infinite input makes its row, or its hidden unit, NaN). */
+typedef enum {
+    AA_ACT_SILU = 0,          /* g / (1 + exp(-g))                                                 */
+    AA_ACT_GELU = 1,          /* g (1 + erf(g / sqrt(2))) / 2                                      */
+    AA_ACT_GELU_TANH = 2      /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2                 */
+} aa_activation;
+
+typedef struct {
+    const void* x;            /* device [rows][channels]                                           */
+    const void* w_gate;       /* device [hidden][channels]                                         */
+    const void* w_up;         /* device [hidden][channels]: the halves of one fused weight will do */
+    const void* b_gate;       /* device [hidden], or NULL                                          */
+    const void* b_up;         /* device [hidden], or NULL                                          */
+    int rows;                 /* tokens of all batch entries: 1 .. 2^24                            */
+    int channels, hidden;     /* multiples of 8 (16-byte rows of 16-bit operands), at most 65536   */
+    int activation;           /* aa_activation                                                     */
+} agent_attn_gate;
+
+/* Bytes of device workspace of agent_attn_gated (backward == 0; none for 16-bit types) or
+ * agent_attn_gated_backward.  0 on invalid arguments, too. */
+size_t agent_attn_gated_workspace_bytes(const agent_attn_handle* h, int rows, int channels, int hidden, int backward);
+
+/* out device [rows][hidden].  Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED (limits above), AA_ERR_WORKSPACE,
+ * AA_ERR_CUDA.  No host synchronisation, no allocation. */
+int agent_attn_gated(agent_attn_handle* h, const agent_attn_gate* gate, void* out, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/* Gradients in the element type, overwritten; owned by the caller.  Every one may be NULL, the weights' and the
+ * biases' only in pairs. */
+typedef struct {
+    void* dx;                 /* [rows][channels]                                                  */
+    void* dw_gate;            /* [hidden][channels]                                                */
+    void* dw_up;              /* [hidden][channels]                                                */
+    void* db_gate;            /* [hidden]                                                          */
+    void* db_up;              /* [hidden]                                                          */
+} agent_attn_gate_grads;
+
+/* Gradients of agent_attn_gated for d_out = dL/dH (device [rows][hidden], element type).  Both projections are
+ * recomputed; nothing has to be saved.  The gradients of the two projections are rounded to the element type, as
+ * operands of the products that follow, which is why the results have that type and not fp32; sums are fp32, in a
+ * fixed order.  Errors as above. */
+int agent_attn_gated_backward(agent_attn_handle* h, const agent_attn_gate* gate, const void* d_out,
+                              const agent_attn_gate_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,7 @@ AA_F32, AA_BF16, AA_F16 = 0, 1, 2
 AA_PATH_AUTO, AA_PATH_SIMT, AA_PATH_UNFUSED, AA_PATH_QUEUE = 0, 1, 2, 3
 STATUS_NAMES = {0: "AA_OK", 1: "AA_ERR_INVALID_ARG", 2: "AA_ERR_UNSUPPORTED", 3: "AA_ERR_WORKSPACE",
                 4: "AA_ERR_CUDA", 5: "AA_ERR_TIMEOUT"}
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 _DTYPES = {torch.float32: AA_F32, torch.bfloat16: AA_BF16, torch.float16: AA_F16}
 
 EXPORTS = [
@@ -27,7 +28,8 @@ EXPORTS = [
     "agent_attn_last_launch_count", "agent_attn_aggregate_static", "agent_attn_static_scratch_bytes",
     "agent_attn_compose_bias", "agent_attn_forward_strided",
     "agent_attn_backward_workspace_bytes", "agent_attn_backward", "agent_attn_test_set_poll_limit",
-    "agent_attn_test_set_stage_mask",
+    "agent_attn_test_set_stage_mask", "agent_attn_rotate", "agent_attn_rotate_backward", "agent_attn_rotate_workspace_bytes",
+    "agent_attn_gated", "agent_attn_gated_backward", "agent_attn_gated_workspace_bytes",
 ]
 
 
@@ -45,6 +47,26 @@ class AgentAttnBias(ctypes.Structure):
 class AgentAttnGrads(ctypes.Structure):
     _fields_ = [("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p),
                 ("db1", ctypes.c_void_p), ("db2", ctypes.c_void_p), ("dwd", ctypes.c_void_p)]
+
+
+class AgentAttnRotary(ctypes.Structure):
+    _fields_ = [("axes", ctypes.c_int), ("extent", ctypes.c_int * 3), ("channels", ctypes.c_int * 3), ("pairs", ctypes.c_int),
+                ("freq", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_batch", ctypes.c_longlong)]
+
+
+class AgentAttnNorm(ctypes.Structure):
+    _fields_ = [("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
+class AgentAttnGate(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("w_gate", ctypes.c_void_p), ("w_up", ctypes.c_void_p), ("b_gate", ctypes.c_void_p),
+                ("b_up", ctypes.c_void_p), ("rows", ctypes.c_int), ("channels", ctypes.c_int), ("hidden", ctypes.c_int),
+                ("activation", ctypes.c_int)]
+
+
+class AgentAttnGateGrads(ctypes.Structure):
+    _fields_ = [("dx", ctypes.c_void_p), ("dw_gate", ctypes.c_void_p), ("dw_up", ctypes.c_void_p), ("db_gate", ctypes.c_void_p),
+                ("db_up", ctypes.c_void_p)]
 
 
 class AgentAttnError(RuntimeError):
@@ -114,6 +136,20 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.agent_attn_test_set_stage_mask.restype = ci
     lib.agent_attn_test_set_poll_limit.argtypes = [vp, ctypes.c_uint]
     lib.agent_attn_test_set_poll_limit.restype = ci
+    rot, nrm = ctypes.POINTER(AgentAttnRotary), ctypes.POINTER(AgentAttnNorm)
+    lib.agent_attn_rotate.argtypes = [vp, vp, vp, ll3, ci, rot, nrm, vp, vp, ll3, vp]
+    lib.agent_attn_rotate.restype = ci
+    lib.agent_attn_rotate_workspace_bytes.argtypes = [vp]
+    lib.agent_attn_rotate_workspace_bytes.restype = sz
+    lib.agent_attn_rotate_backward.argtypes = [vp, vp, vp, ll3, vp, vp, ll3, ci, rot, nrm, vp, vp, ll3, vp, vp, vp, sz, vp]
+    lib.agent_attn_rotate_backward.restype = ci
+    gate, ggrads = ctypes.POINTER(AgentAttnGate), ctypes.POINTER(AgentAttnGateGrads)
+    lib.agent_attn_gated_workspace_bytes.argtypes = [vp, ci, ci, ci, ci]
+    lib.agent_attn_gated_workspace_bytes.restype = sz
+    lib.agent_attn_gated.argtypes = [vp, gate, vp, vp, sz, vp]
+    lib.agent_attn_gated.restype = ci
+    lib.agent_attn_gated_backward.argtypes = [vp, gate, vp, ggrads, vp, sz, vp]
+    lib.agent_attn_gated_backward.restype = ci
     lib.agent_attn_static_scratch_bytes.argtypes = []
     lib.agent_attn_static_scratch_bytes.restype = sz
     _lib = lib
@@ -139,6 +175,42 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]):
 
 def _bias(b1: Optional[torch.Tensor], b2: Optional[torch.Tensor]):
     return None if b1 is None and b2 is None else ctypes.byref(AgentAttnBias(_ptr(b1), _ptr(b2)))
+
+
+class Rotary:
+    """Rotary positions of a network's tokens (`agent_attn_rotary`): what `AgentAttention.rotate` turns queries and keys by.
+
+    `channels` gives each axis (one to three: e.g. time, height, width) its number of channels of a head, an even one; `freq` the radians per
+    unit of position of every pair, axis after axis, as an fp32 CUDA tensor of sum(channels) / 2 (`Rotary.frequencies` makes the usual ones).
+    Positions are the tokens' places in the row-major grid `extent`, or `positions`, fp32 [B or 1, N, axes].  `pairs`: neighbouring channels
+    form a pair; else channel i of an axis's segment and channel i + channels / 2.
+    """
+
+    def __init__(self, freq: torch.Tensor, channels, extent=None, positions: Optional[torch.Tensor] = None, pairs: bool = False):
+        channels, axes = tuple(int(c) for c in channels), len(channels)
+        if not 1 <= axes <= 3 or any(c < 0 or c % 2 for c in channels):
+            raise ValueError(f"channels: expected one to three even numbers, got {channels}")
+        if freq.shape != (sum(channels) // 2,) or freq.dtype is not torch.float32 or not freq.is_cuda or not freq.is_contiguous():
+            raise ValueError(f"freq: expected a contiguous cuda float32 tensor of {sum(channels) // 2} values, got {tuple(freq.shape)} {freq.dtype} on {freq.device}")
+        if positions is not None:
+            if positions.dim() != 3 or positions.shape[2] != axes or positions.dtype is not torch.float32 or not positions.is_cuda or not positions.is_contiguous():
+                raise ValueError(f"positions: expected a contiguous cuda float32 tensor [B or 1, N, {axes}], got {tuple(positions.shape)} {positions.dtype} on {positions.device}")
+        elif extent is None or len(extent) != axes:
+            raise ValueError(f"extent: expected {axes} values, got {extent}")
+        self.freq, self.positions, self.channels, self.axes = freq, positions, channels, axes
+        self.extent = (1,) * axes if extent is None else tuple(int(e) for e in extent)
+        self._batch = 0 if positions is None else positions.shape[0]
+        self._c = AgentAttnRotary(axes, (ctypes.c_int * 3)(*self.extent), (ctypes.c_int * 3)(*channels), int(pairs), freq.data_ptr(), _ptr(positions),
+                                  positions.shape[1] * axes if self._batch > 1 else 0)
+
+    @staticmethod
+    def frequencies(channels, theta: float = 100.0, device: int = 0) -> torch.Tensor:
+        """theta ** (-i / pairs) for pair i of each axis."""
+        return torch.tensor([theta ** (-i / (c // 2)) for c in channels for i in range(c // 2)], dtype=torch.float32, device=torch.device("cuda", device))
+
+    def _check(self, batch: int, n_tokens: int):
+        if self.positions is not None and (self.positions.shape[1] != n_tokens or self._batch not in (1, batch)):
+            raise ValueError(f"positions: expected [{batch} or 1, {n_tokens}, {self.axes}], got {tuple(self.positions.shape)}")
 
 
 class AgentAttention:
@@ -430,3 +502,168 @@ class AgentAttention:
         if synchronize:
             s.synchronize()
         return out
+
+    # ------------------------------------------------------------------ queries and keys before the attention
+    def _chk_views(self, named, n_tokens: int, dtype: torch.dtype):
+        """Views of shape [B, heads, N, d] that share their strides, or None; the strides as the library takes them."""
+        strides = None
+        for name, t in named:
+            if t is None:
+                continue
+            if t.shape != (self.batch, self.heads, n_tokens, self.head_dim) or t.dtype is not dtype or not t.is_cuda or t.stride(3) != 1:
+                raise ValueError(f"{name}: expected a cuda {dtype} view of shape {(self.batch, self.heads, n_tokens, self.head_dim)} with contiguous "
+                                 f"channels, got {tuple(t.shape)} {t.dtype} on {t.device}")
+            st = tuple(s if n > 1 else self.head_dim for n, s in zip(t.shape, t.stride()[:3]))     # (of a single entry no stride is used)
+            if strides is not None and st != strides:
+                raise ValueError(f"{name}: expected the strides {strides} of the other tensor, got {st}")
+            strides = st
+        return None if strides is None else (ctypes.c_longlong * 3)(*strides)
+
+    def _norm(self, q_gain, k_gain, eps):
+        self._chk_tensor(q_gain, (self.head_dim,), "q_gain")
+        self._chk_tensor(k_gain, (self.head_dim,), "k_gain")
+        if eps is None:
+            if q_gain is not None or k_gain is not None:
+                raise ValueError("a gain belongs to a norm: give eps")
+            return None
+        return ctypes.byref(AgentAttnNorm(_ptr(q_gain), _ptr(k_gain), eps))
+
+    def rotate(self, q, k, rotary: Optional[Rotary] = None, q_gain=None, k_gain=None, eps: Optional[float] = None, out=None, stream=None):
+        """`agent_attn_rotate`: queries and keys as the attention takes them, with an RMS norm of each head (where `eps` is given) and rotary
+        positions.
+
+        `q` and `k` are views of shape [B, heads, N, d] with contiguous channels and the same strides (either may be None); `out` is a pair of
+        such views, by default new dense tensors.  `out=(q, k)` works in place: `qkv[:, :, i].permute(0, 2, 1, 3)` of a fused projection can be
+        prepared where `forward_strided` reads it.  Returns (q_out, k_out).
+        """
+        some = q if q is not None else k
+        if some is None:
+            raise ValueError("q or k is required")
+        N = some.shape[2] if some.dim() == 4 else 0
+        sin = self._chk_views((("q", q), ("k", k)), N, self.dtype)
+        if rotary is not None:
+            rotary._check(self.batch, N)
+        norm = self._norm(q_gain, k_gain, eps)
+        if out is None:
+            shape = (self.batch, self.heads, N, self.head_dim)
+            out = tuple(None if t is None else torch.empty(shape, dtype=self.dtype, device=self.device) for t in (q, k))
+            sout = None
+        else:
+            if any((t is None) != (o is None) for t, o in zip((q, k), out)):
+                raise ValueError("out: expected a tensor for each of q and k that is given")
+            sout = self._chk_views((("out[0]", out[0]), ("out[1]", out[1])), N, self.dtype)
+        self._check(self.lib.agent_attn_rotate(self._h, _ptr(q), _ptr(k), sin, N, None if rotary is None else ctypes.byref(rotary._c), norm,
+                                               _ptr(out[0]), _ptr(out[1]), sout, _stream_ptr(stream)))
+        return out[0], out[1]
+
+    def rotate_backward(self, dq_out, dk_out, rotary: Optional[Rotary] = None, q=None, k=None, q_gain=None, k_gain=None,
+                        eps: Optional[float] = None, out=None, workspace=None, stream=None) -> dict:
+        """`agent_attn_rotate_backward`: from the fp32 gradients of `rotate`'s results (what `backward` returns as `dq`, `dk`), those of its inputs.
+
+        `q`, `k` (the inputs of the forward call) are needed with a norm only.  Returns a dict with fp32 `dq`, `dk` ([B, heads, N, d]; `out`, a pair
+        of views, which may be the gradients given) and, for the gains that were given, `dq_gain`, `dk_gain` ([d]).
+        """
+        some = dq_out if dq_out is not None else dk_out
+        if some is None:
+            raise ValueError("dq_out or dk_out is required")
+        N = some.shape[2] if some.dim() == 4 else 0
+        f32 = torch.float32
+        sgrad = self._chk_views((("dq_out", dq_out), ("dk_out", dk_out)), N, f32)
+        if rotary is not None:
+            rotary._check(self.batch, N)
+        norm = self._norm(q_gain, k_gain, eps)
+        sin = None
+        if norm is not None:
+            if (dq_out is not None and q is None) or (dk_out is not None and k is None):
+                raise ValueError("the gradient of a norm needs q and k")
+            sin = self._chk_views((("q", q), ("k", k)), N, self.dtype)
+        if out is None:
+            shape = (self.batch, self.heads, N, self.head_dim)
+            out = tuple(None if t is None else torch.empty(shape, dtype=f32, device=self.device) for t in (dq_out, dk_out))
+            sout = None
+        else:
+            if any((t is None) != (o is None) for t, o in zip((dq_out, dk_out), out)):
+                raise ValueError("out: expected a tensor for each gradient that is given")
+            sout = self._chk_views((("out[0]", out[0]), ("out[1]", out[1])), N, f32)
+        got = {name: t for name, t in zip(("dq", "dk"), out) if t is not None}
+        for name, gain, grad in (("dq_gain", q_gain, dq_out), ("dk_gain", k_gain, dk_out)):
+            if gain is not None and grad is not None:
+                got[name] = torch.empty(self.head_dim, dtype=f32, device=self.device)
+        if norm is not None and workspace is None:
+            workspace = self._scratch(int(self.lib.agent_attn_rotate_workspace_bytes(self._h)), stream)
+        self._check(self.lib.agent_attn_rotate_backward(
+            self._h, _ptr(dq_out), _ptr(dk_out), sgrad, _ptr(q), _ptr(k), sin, N, None if rotary is None else ctypes.byref(rotary._c), norm,
+            _ptr(out[0]), _ptr(out[1]), sout, _ptr(got.get("dq_gain")), _ptr(got.get("dk_gain")),
+            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+        return got
+
+    # ------------------------------------------------------------------ gated feed-forward product
+    def _gate(self, x, w_gate, w_up, b_gate, b_up, activation):
+        if activation not in _ACTIVATIONS:
+            raise ValueError(f"activation: expected one of {sorted(_ACTIVATIONS)}, got {activation!r}")
+        if x.dim() < 1 or w_gate.dim() != 2:
+            raise ValueError(f"expected x [..., channels] and weights [hidden, channels], got {tuple(x.shape)} and {tuple(w_gate.shape)}")
+        F, C = w_gate.shape
+        self._chk_tensor(x, x.shape[:-1] + (C,), "x")
+        self._chk_tensor(w_gate, (F, C), "w_gate")
+        self._chk_tensor(w_up, (F, C), "w_up")
+        self._chk_tensor(b_gate, (F,), "b_gate")
+        self._chk_tensor(b_up, (F,), "b_up")
+        rows = x.numel() // C if C else 0
+        return AgentAttnGate(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(b_gate), _ptr(b_up), rows, C, F, _ACTIVATIONS[activation])
+
+    def _gate_workspace(self, gate, backward: int, workspace, stream):
+        """The workspace of a call: the caller's, or a new one where one is needed."""
+        if workspace is not None:
+            return workspace
+        key = ("gated", gate.rows, gate.channels, gate.hidden, backward)
+        need = self._bytes.get(key)
+        if need is None:
+            if len(self._bytes) >= 64:
+                self._bytes.clear()
+            need = self._bytes[key] = int(self.lib.agent_attn_gated_workspace_bytes(self._h, gate.rows, gate.channels, gate.hidden, backward))
+        return self._scratch(need, stream)
+
+    def _scratch(self, nbytes: int, stream) -> Optional[torch.Tensor]:
+        """Memory of one call: kept from reuse until `stream` is done with it where that is not the current stream."""
+        if nbytes == 0:
+            return None
+        t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        if stream is not None:
+            t.record_stream(stream)
+        return t
+
+    def gated(self, x, w_gate, w_up, b_gate=None, b_up=None, activation: str = "silu", out=None, workspace=None, stream=None) -> torch.Tensor:
+        """`agent_attn_gated`: act(x w_gate^T + b_gate) * (x w_up^T + b_up) for x [..., channels] and weights [hidden, channels].
+
+        `activation`: "silu", "gelu" (erf) or "gelu_tanh".  The halves of one fused weight [2 hidden, channels] are `weight.chunk(2)`.
+        """
+        gate = self._gate(x, w_gate, w_up, b_gate, b_up, activation)
+        shape = x.shape[:-1] + (gate.hidden,)
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        self._chk_tensor(out, shape, "out")
+        ws = self._gate_workspace(gate, 0, workspace, stream)
+        self._check(self.lib.agent_attn_gated(self._h, ctypes.byref(gate), _ptr(out), _ptr(ws), 0 if ws is None else ws.numel(), _stream_ptr(stream)))
+        return out
+
+    def gated_backward(self, x, w_gate, w_up, d_out, b_gate=None, b_up=None, activation: str = "silu", need_input_grad: bool = True,
+                       need_weight_grads: bool = True, workspace=None, stream=None) -> dict:
+        """`agent_attn_gated_backward`: gradients of `gated` for the upstream gradient `d_out`, in the element type.
+
+        Returns a dict with `dx`, `dw_gate`, `dw_up` and, where both biases are given, `db_gate`, `db_up`.
+        """
+        gate = self._gate(x, w_gate, w_up, b_gate, b_up, activation)
+        self._chk_tensor(d_out, x.shape[:-1] + (gate.hidden,), "d_out")
+        g = {}
+        if need_input_grad:
+            g["dx"] = torch.empty_like(x)
+        if need_weight_grads:
+            g["dw_gate"], g["dw_up"] = torch.empty_like(w_gate), torch.empty_like(w_up)
+            if b_gate is not None and b_up is not None:
+                g["db_gate"], g["db_up"] = torch.empty_like(b_gate), torch.empty_like(b_up)
+        grads = AgentAttnGateGrads(_ptr(g.get("dx")), _ptr(g.get("dw_gate")), _ptr(g.get("dw_up")), _ptr(g.get("db_gate")), _ptr(g.get("db_up")))
+        ws = self._gate_workspace(gate, 1, workspace, stream)
+        self._check(self.lib.agent_attn_gated_backward(self._h, ctypes.byref(gate), _ptr(d_out), ctypes.byref(grads), _ptr(ws),
+                                                       0 if ws is None else ws.numel(), _stream_ptr(stream)))
+        return g

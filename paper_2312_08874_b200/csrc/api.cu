@@ -660,6 +660,211 @@ int agent_attn_compose_bias(agent_attn_handle* h, const void* col, const void* r
     return AA_OK;
 }
 
+// ------------------------------------------------------------- queries and keys before the attention
+
+// Strides of a call's tensor, or the dense layout; `unit`: bytes of an element
+static int read_strides(agent_attn_handle* h, const long long* strides, int n_tokens, int unit, TokLayout* l) {
+    *l = dense_layout(h->cfg.heads, n_tokens, h->cfg.head_dim);
+    if (!strides) return AA_OK;
+    l->sb = strides[0]; l->sh = strides[1]; l->st = strides[2];
+    if (l->sb <= 0 || l->sh <= 0 || l->st < h->cfg.head_dim)
+        return fail(h, AA_ERR_INVALID_ARG, "strides must be positive and the token stride at least head_dim");
+    if ((l->sb * unit) % 16 || (l->sh * unit) % 16 || (l->st * unit) % 16)
+        return fail(h, AA_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
+    return AA_OK;
+}
+static bool same_layout(const TokLayout& a, const TokLayout& b) { return a.sb == b.sb && a.sh == b.sh && a.st == b.st; }
+
+// What both directions share: the shape, the rotation and the norm
+static int rotate_args(agent_attn_handle* h, int n_tokens, const agent_attn_rotary* rotary, const agent_attn_norm* norm, RotateArgs* a) {
+    memset(a, 0, sizeof(*a));
+    if (n_tokens <= 0) return fail(h, AA_ERR_INVALID_ARG, "token count must be positive (N=%d)", n_tokens);
+    if (n_tokens > h->cfg.max_tokens) return fail(h, AA_ERR_UNSUPPORTED, "N=%d exceeds the handle's max_tokens=%d", n_tokens, h->cfg.max_tokens);
+    a->slabs = h->cfg.batch * h->cfg.heads; a->heads = h->cfg.heads; a->N = n_tokens; a->d = h->cfg.head_dim;
+    if (rotary) {
+        if (rotary->axes < 0 || rotary->axes > 3) return fail(h, AA_ERR_INVALID_ARG, "0 to 3 axes, not %d", rotary->axes);
+        if (rotary->pairs != AA_PAIRS_HALVES && rotary->pairs != AA_PAIRS_NEIGHBOURS) return fail(h, AA_ERR_INVALID_ARG, "unknown kind of pairs %d", rotary->pairs);
+        long long sum = 0, tokens = 1;
+        for (int i = 0; i < rotary->axes; ++i) {
+            const int c = rotary->channels[i];
+            if (c < 0 || c % 2 || (sum += c) > h->cfg.head_dim)
+                return fail(h, AA_ERR_INVALID_ARG, "channels of the axes must be even and add up to at most head_dim=%d", h->cfg.head_dim);
+            if (!rotary->positions && (rotary->extent[i] <= 0 || (tokens *= rotary->extent[i]) > n_tokens))
+                return fail(h, AA_ERR_INVALID_ARG, "the grid does not have N=%d tokens", n_tokens);
+            a->channels[i] = c;
+            a->extent[i] = rotary->positions ? 1 : rotary->extent[i];
+        }
+        if (rotary->axes && !rotary->positions && tokens != n_tokens) return fail(h, AA_ERR_INVALID_ARG, "the grid does not have N=%d tokens", n_tokens);
+        if (sum && !rotary->freq) return fail(h, AA_ERR_INVALID_ARG, "null pointer: freq");
+        if ((reinterpret_cast<uintptr_t>(rotary->freq) | reinterpret_cast<uintptr_t>(rotary->positions)) & 3u)
+            return fail(h, AA_ERR_INVALID_ARG, "freq and positions must be 4-byte aligned");
+        if (rotary->positions && rotary->positions_batch < 0) return fail(h, AA_ERR_INVALID_ARG, "positions_batch must not be negative");
+        a->axes = rotary->axes;
+        a->freq = rotary->freq;
+        a->positions = rotary->axes ? rotary->positions : nullptr;
+        a->pos_batch = rotary->positions_batch;
+        a->neighbours = rotary->pairs == AA_PAIRS_NEIGHBOURS;
+    }
+    if (norm) {
+        if (!(norm->eps >= 0.f) || std::isinf(norm->eps)) return fail(h, AA_ERR_INVALID_ARG, "eps must be finite and not negative");
+        if ((reinterpret_cast<uintptr_t>(norm->q_gain) | reinterpret_cast<uintptr_t>(norm->k_gain)) & (h->elem_bytes - 1))
+            return fail(h, AA_ERR_INVALID_ARG, "gains must be aligned to their element type");
+        a->norm = 1;
+        a->eps = norm->eps;
+        a->gain[0] = norm->q_gain; a->gain[1] = norm->k_gain;
+    }
+    return AA_OK;
+}
+
+int agent_attn_rotate(agent_attn_handle* h, const void* Q, const void* K, const long long in_strides[3], int n_tokens,
+                      const agent_attn_rotary* rotary, const agent_attn_norm* norm, void* Q_out, void* K_out,
+                      const long long out_strides[3], void* stream) {
+    if (!h) return AA_ERR_INVALID_ARG;
+    h->err[0] = 0;
+    if ((!Q && !K) || (Q && !Q_out) || (K && !K_out)) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    RotateArgs a;
+    if (int rc = rotate_args(h, n_tokens, rotary, norm, &a)) return rc;
+    if (int rc = read_strides(h, in_strides, n_tokens, h->elem_bytes, &a.lin)) return rc;
+    if (int rc = read_strides(h, out_strides, n_tokens, h->elem_bytes, &a.lout)) return rc;
+    a.x[0] = Q; a.x[1] = K;
+    a.y[0] = Q_out; a.y[1] = K_out;
+    for (int i = 0; i < 2; ++i) {
+        if (!a.x[i]) continue;
+        if (misaligned(a.x[i]) || misaligned(a.y[i])) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+        if (a.x[i] == a.y[1 - i] && a.x[1 - i]) return fail(h, AA_ERR_INVALID_ARG, "a result may only take the place of its own input");
+        if (a.x[i] == a.y[i] && !same_layout(a.lin, a.lout)) return fail(h, AA_ERR_INVALID_ARG, "in place, the strides must be the same");
+    }
+    DeviceGuard guard(h->cfg.device);
+    if (!guard.ok) return fail(h, AA_ERR_CUDA, "cannot select device %d", h->cfg.device);
+    const cudaError_t e = launch_rotate(h->cfg.dtype, a, h->sm_count, (cudaStream_t)stream);
+    if (e != cudaSuccess) return fail(h, AA_ERR_CUDA, "rotation launch failed: %s", cudaGetErrorString(e));
+    h->launches = 1;
+    return AA_OK;
+}
+
+size_t agent_attn_rotate_workspace_bytes(const agent_attn_handle* h) { return h ? rotate_backward_bytes(h->cfg.head_dim, h->sm_count) : 0; }
+
+int agent_attn_rotate_backward(agent_attn_handle* h, const float* dQ_out, const float* dK_out, const long long grad_strides[3],
+                               const void* Q, const void* K, const long long in_strides[3], int n_tokens,
+                               const agent_attn_rotary* rotary, const agent_attn_norm* norm, float* dQ, float* dK,
+                               const long long out_strides[3], float* dq_gain, float* dk_gain, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    if (!h) return AA_ERR_INVALID_ARG;
+    h->err[0] = 0;
+    if ((!dQ_out && !dK_out) || (dQ_out && !dQ) || (dK_out && !dK)) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (norm && ((dQ_out && !Q) || (dK_out && !K))) return fail(h, AA_ERR_INVALID_ARG, "the gradient of a norm needs its input");
+    if ((dq_gain && (!norm || !dQ_out)) || (dk_gain && (!norm || !dK_out))) return fail(h, AA_ERR_INVALID_ARG, "gradient of a gain without its norm");
+    RotateBwdArgs b;
+    memset(&b, 0, sizeof(b));
+    if (int rc = rotate_args(h, n_tokens, rotary, norm, &b.fwd)) return rc;
+    if (int rc = read_strides(h, grad_strides, n_tokens, 4, &b.lgrad)) return rc;
+    if (int rc = read_strides(h, in_strides, n_tokens, h->elem_bytes, &b.fwd.lin)) return rc;
+    if (int rc = read_strides(h, out_strides, n_tokens, 4, &b.fwd.lout)) return rc;
+    b.grad[0] = dQ_out; b.grad[1] = dK_out;
+    b.fwd.y[0] = dQ; b.fwd.y[1] = dK;
+    b.fwd.x[0] = dQ_out ? Q : nullptr; b.fwd.x[1] = dK_out ? K : nullptr;
+    for (int i = 0; i < 2; ++i) {
+        if (!b.grad[i]) continue;
+        if (misaligned(b.grad[i]) || misaligned(b.fwd.y[i]) || (norm && misaligned(b.fwd.x[i]))) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+        if (b.grad[i] == b.fwd.y[1 - i] && b.grad[1 - i]) return fail(h, AA_ERR_INVALID_ARG, "a result may only take the place of its own input");
+        if (b.grad[i] == b.fwd.y[i] && !same_layout(b.lgrad, b.fwd.lout)) return fail(h, AA_ERR_INVALID_ARG, "in place, the strides must be the same");
+    }
+    b.dgain[0] = dq_gain; b.dgain[1] = dk_gain;
+    if ((reinterpret_cast<uintptr_t>(dq_gain) | reinterpret_cast<uintptr_t>(dk_gain)) & 3u) return fail(h, AA_ERR_INVALID_ARG, "gradients must be 4-byte aligned");
+    if (norm) {
+        const size_t need = rotate_backward_bytes(h->cfg.head_dim, h->sm_count);
+        if (!workspace || workspace_bytes < need) return fail(h, AA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
+        if (misaligned(workspace)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+        b.part = static_cast<float*>(workspace);
+    }
+    DeviceGuard guard(h->cfg.device);
+    if (!guard.ok) return fail(h, AA_ERR_CUDA, "cannot select device %d", h->cfg.device);
+    cudaError_t e;
+    if (norm) {
+        e = launch_rotate_backward(h->cfg.dtype, b, h->sm_count, (cudaStream_t)stream);
+    } else {                                        // the transpose of a rotation is the rotation back
+        RotateArgs a = b.fwd;
+        a.x[0] = b.grad[0]; a.x[1] = b.grad[1];
+        a.lin = b.lgrad;
+        a.inverse = 1;
+        e = launch_rotate(AA_F32, a, h->sm_count, (cudaStream_t)stream);
+    }
+    if (e != cudaSuccess) return fail(h, AA_ERR_CUDA, "rotation gradient launch failed: %s", cudaGetErrorString(e));
+    h->launches = norm && (dq_gain || dk_gain) ? 2 : 1;
+    return AA_OK;
+}
+
+// ------------------------------------------------------------- gated feed-forward product
+
+static bool gate_shape(int rows, int channels, int hidden) {
+    return rows <= (1 << 24) && channels <= 65536 && hidden <= 65536 && channels % 8 == 0 && hidden % 8 == 0;
+}
+static int gate_call(agent_attn_handle* h, const agent_attn_gate* g, void* workspace, size_t workspace_bytes, bool backward, GatedCall* c) {
+    if (!g || !g->x || !g->w_gate || !g->w_up) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (g->rows <= 0 || g->channels <= 0 || g->hidden <= 0)
+        return fail(h, AA_ERR_INVALID_ARG, "rows, channels and hidden size must be positive (%d, %d, %d)", g->rows, g->channels, g->hidden);
+    if (!gate_shape(g->rows, g->channels, g->hidden))
+        return fail(h, AA_ERR_UNSUPPORTED, "channels=%d and hidden=%d must be multiples of 8 up to 65536, rows=%d at most 2^24", g->channels, g->hidden, g->rows);
+    if (g->activation < AA_ACT_SILU || g->activation > AA_ACT_GELU_TANH) return fail(h, AA_ERR_UNSUPPORTED, "unknown activation %d", g->activation);
+    if (misaligned(g->x) || misaligned(g->w_gate) || misaligned(g->w_up) || misaligned(g->b_gate) || misaligned(g->b_up))
+        return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    const size_t need = gated_bytes(h->cfg.dtype, g->rows, g->channels, g->hidden, backward, h->sm_count);
+    if (need && (!workspace || workspace_bytes < need)) return fail(h, AA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
+    if (need && misaligned(workspace)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    memset(c, 0, sizeof(*c));
+    c->M = g->rows; c->C = g->channels; c->F = g->hidden; c->act = g->activation; c->sm_count = h->sm_count;
+    c->x = g->x; c->wg = g->w_gate; c->wu = g->w_up; c->bg = g->b_gate; c->bu = g->b_up;
+    c->ws = workspace;
+    c->status = h->d_status;
+    return AA_OK;
+}
+static int run_gate(agent_attn_handle* h, const GatedCall& c, void* stream) {
+    DeviceGuard guard(h->cfg.device);
+    if (!guard.ok) return fail(h, AA_ERR_CUDA, "cannot select device %d", h->cfg.device);
+    int launches = 0;
+    const cudaError_t e = launch_gated(h->cfg.dtype, c, (cudaStream_t)stream, &launches);
+    if (e != cudaSuccess) return fail(h, AA_ERR_CUDA, "gated product launch failed: %s", cudaGetErrorString(e));
+    h->launches = launches;
+    return AA_OK;
+}
+
+size_t agent_attn_gated_workspace_bytes(const agent_attn_handle* h, int rows, int channels, int hidden, int backward) {
+    if (!h || rows <= 0 || channels <= 0 || hidden <= 0 || !gate_shape(rows, channels, hidden)) return 0;
+    return gated_bytes(h->cfg.dtype, rows, channels, hidden, backward != 0, h->sm_count);
+}
+
+int agent_attn_gated(agent_attn_handle* h, const agent_attn_gate* gate, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!h) return AA_ERR_INVALID_ARG;
+    h->err[0] = 0;
+    GatedCall c;
+    if (int rc = gate_call(h, gate, workspace, workspace_bytes, false, &c)) return rc;
+    if (!out) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (misaligned(out)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    if (out == c.x || out == c.wg || out == c.wu) return fail(h, AA_ERR_INVALID_ARG, "out aliases an input");
+    c.h = out;
+    return run_gate(h, c, stream);
+}
+
+int agent_attn_gated_backward(agent_attn_handle* h, const agent_attn_gate* gate, const void* d_out, const agent_attn_gate_grads* grads,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    if (!h) return AA_ERR_INVALID_ARG;
+    h->err[0] = 0;
+    GatedCall c;
+    if (int rc = gate_call(h, gate, workspace, workspace_bytes, true, &c)) return rc;
+    if (!d_out || !grads) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (!grads->dw_gate != !grads->dw_up || !grads->db_gate != !grads->db_up) return fail(h, AA_ERR_INVALID_ARG, "gradients of weights and of biases come in pairs");
+    if (!grads->dx && !grads->dw_gate && !grads->db_gate) return fail(h, AA_ERR_INVALID_ARG, "no gradient asked for");
+    const void* outs[] = {grads->dx, grads->dw_gate, grads->dw_up, grads->db_gate, grads->db_up};
+    for (const void* o : outs) {
+        if (o && misaligned(o)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+        if (o && (o == c.x || o == c.wg || o == c.wu || o == d_out)) return fail(h, AA_ERR_INVALID_ARG, "a gradient aliases an input");
+    }
+    if (misaligned(d_out)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    c.dh = d_out;
+    c.dx = grads->dx; c.dwg = grads->dw_gate; c.dwu = grads->dw_up; c.dbg = grads->db_gate; c.dbu = grads->db_up;
+    return run_gate(h, c, stream);
+}
+
 // A call on host buffers is bound by its copies (56 x 56 grid, 64 slabs: 78 MB in, 26 MB out, 1.98 ms in one piece).  It is cut into
 // parts along the batch, or along the heads of a single batch entry: the copies in, the kernels and the copies out of different
 // parts overlap, and what follows the last copy in is the work of the last part.  So parts halve: a half, a quarter, two eighths (few

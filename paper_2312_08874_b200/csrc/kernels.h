@@ -318,4 +318,48 @@ bool backward_umma_eligible(int dtype, int n, int d);
 size_t backward_umma_bytes(int heads, int n, int N);      // copies of the biases: B1, then B2 where it is not read as it is
 cudaError_t launch_backward_umma(int dtype, bool broadcast_stage, const BwdCall& c, cudaStream_t st);
 
+// ------------------------------------------------------------- queries and keys before the attention (rotate.cu)
+// Optional RMS norm of each head row, then rotary positions with up to three axes.
+struct RotateArgs {
+    const void* x[2];         // queries and keys [batch, head, token, d] with strides lin; either may be null
+    void* y[2];               // results, strides lout
+    const void* gain[2];      // [d] each, or null
+    const float* freq;        // radians per unit of position, pair after pair
+    const float* positions;   // [batch or 1][N][axes], or null: the token's place in the grid
+    long long pos_batch;      // elements between batch entries of `positions` (0: shared)
+    TokLayout lin, lout;
+    int slabs, heads, N, d;
+    int axes, extent[3], channels[3];      // of the grid; channels of a head that each axis turns (even)
+    int neighbours;           // pairs are neighbouring channels, else the halves of an axis's segment
+    int norm, inverse;
+    float eps;
+    // set by the launcher: lanes of a token; slabs that share positions, runs of them, slabs of a run; 1 / d
+    int lanes, unit_slabs, chunks, share;
+    float inv_d;
+};
+struct RotateBwdArgs {
+    RotateArgs fwd;           // x: the forward call's inputs; y: fp32 gradients of them
+    const float* grad[2];     // fp32 gradients of the results, strides lgrad
+    TokLayout lgrad;
+    float* dgain[2];          // fp32 [d] each, or null
+    float* part;              // rotate_backward_bytes
+};
+cudaError_t launch_rotate(int dtype, const RotateArgs& a, int sm_count, cudaStream_t st);
+size_t rotate_backward_bytes(int d, int sm_count);
+cudaError_t launch_rotate_backward(int dtype, const RotateBwdArgs& a, int sm_count, cudaStream_t st);
+
+// ------------------------------------------------------------- gated feed-forward product (gated.cu)
+// H = act(X Wg^T + bg) o (X Wu^T + bu), or (dh) its gradients; C and F multiples of 8.
+struct GatedCall {
+    int M, C, F, act, sm_count;
+    const void *x, *wg, *wu, *bg, *bu;        // [M][C], [F][C] twice, [F] twice or null
+    void* h;                                  // [M][F]
+    const void* dh;                           // gradient of h: the backward pass; null: the forward pass
+    void *dx, *dwg, *dwu, *dbg, *dbu;         // in the element type; dx, the weights' pair, the biases' pair may be null
+    void* ws;                                 // gated_bytes
+    int* status;
+};
+size_t gated_bytes(int dtype, int M, int C, int F, bool backward, int sm_count);
+cudaError_t launch_gated(int dtype, const GatedCall& c, cudaStream_t st, int* launches);
+
 }  // namespace aa

@@ -1,0 +1,200 @@
+"""The gated feed-forward product (`gated`, `gated_backward`) against the formulas in 64 bits.
+
+Tolerances.  16-bit types, forward: products of 16-bit numbers are exact in fp32, their sum over up to 600 channels loses at most 40 steps of 2^-23
+of its size in tensor memory, activation and product some 2^-21; then one rounding, at most 2^-8 or 2^-11 of the result: 2e-5 of the largest result beside
+it.  Backward: the gradients of both projections are rounded to the element type (2^-9 / sqrt(3) = 1.1e-3 for bf16, 2.8e-4 for f16,
+of the power of two above), and
+the result again: 1.6e-3 and 4e-4, and twice that for what the few numbers of a small case leave to chance; a bias of few rows sums unrounded
+numbers and is inside that.  fp32: three bf16 terms hold 24 bits; sums lose up to a step of 2^-23 each 16 summands: 2e-6 forward (600 channels),
+4e-6 for sums of up to 2500 numbers and more, which are cut into shares.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2312_08874_b200 import AgentAttention, AgentAttnError
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+STEP = {n: torch.finfo(DT[n]).eps / 2 for n in ("bf16", "f16")}
+REL_FWD, REL_BWD = 2e-6, {"f32": 4e-6, "bf16": 3.2e-3, "f16": 8e-4}
+
+
+def act(name, g):
+    if name == "silu":
+        return g / (1 + torch.exp(-g))
+    if name == "gelu":
+        return 0.5 * g * (1 + torch.erf(g / math.sqrt(2)))
+    return 0.5 * g * (1 + torch.tanh(math.sqrt(2 / math.pi) * (g + 0.044715 * g ** 3)))
+
+
+def inputs(M, C, F, dtype, biases, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+
+    def draw(shape, std=1.0):
+        return (torch.randn(shape, generator=gen, device="cuda") * std).to(DT[dtype])
+    return (draw((M, C)), draw((F, C), C ** -0.5), draw((F, C), C ** -0.5), draw((M, F)),
+            draw((F,), 0.5) if "g" in biases else None, draw((F,), 0.5) if "u" in biases else None)
+
+
+def reference(x, wg, wu, dh, bg, bu, name):
+    leaves = [t.double().requires_grad_() if t is not None else None for t in (x, wg, wu, bg, bu)]
+    g, u = leaves[0] @ leaves[1].T, leaves[0] @ leaves[2].T
+    g = g if bg is None else g + leaves[3]
+    u = u if bu is None else u + leaves[4]
+    h = act(name, g) * u
+    h.backward(dh.double())
+    return h.detach(), {n: t.grad for n, t in zip(("dx", "dw_gate", "dw_up", "db_gate", "db_up"), leaves) if t is not None}
+
+
+def rel(got, ref):
+    return float((got.double() - ref).norm() / ref.norm())
+
+
+def check_forward(got, ref, dtype):
+    assert torch.isfinite(got).all()
+    if dtype == "f32":
+        assert rel(got, ref) <= REL_FWD
+    else:
+        err = (got.double() - ref).abs()
+        assert (err <= STEP[dtype] * ref.abs() + 2e-5 * ref.abs().max()).all()
+
+
+SIZES = [(1, 8, 8), (1, 320, 1280), (2, 40, 136), (63, 72, 200), (128, 64, 128), (129, 136, 264), (300, 600, 72), (257, 192, 520), (1000, 320, 128), (2500, 24, 1368)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("name,biases", [("silu", ""), ("gelu", "gu"), ("gelu_tanh", "g"), ("silu", "u")])
+def test_both_directions_match_the_formulas(size, dtype, name, biases):
+    M, C, F = size
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, biases, seed=M)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    h, grads = reference(x, wg, wu, dh, bg, bu, name)
+    out = torch.full((M, F), float("nan"), device="cuda", dtype=DT[dtype])
+    args = dict(b_gate=bg, b_up=bu, activation=name)
+    got = mod.gated(x, wg, wu, out=out, **args)
+    check_forward(got, h, dtype)
+    need = int(mod.lib.agent_attn_gated_workspace_bytes(mod._h, M, C, F, 1))
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")               # NaN wherever it is read before it is written
+    back = mod.gated_backward(x, wg, wu, dh, workspace=ws, **args)
+    assert mod.query_status() == 0
+    for n, t in back.items():
+        assert torch.isfinite(t).all() and rel(t, grads[n]) <= REL_BWD[dtype], (n, rel(t, grads[n]))
+    assert ("db_gate" in back) == (biases == "gu")
+    again = mod.gated_backward(x, wg, wu, dh, **args)
+    assert all(torch.equal(again[n], back[n]) for n in back)                       # sums in a fixed order
+
+
+@pytest.mark.parametrize("dtype,M,C,F", [("bf16", 20000, 192, 512), ("f16", 8192, 320, 1280), ("f32", 6000, 64, 256), ("bf16", 3000, 1032, 2728), ("f32", 200, 1024, 4096)])
+def test_long_sums_and_large_sizes(dtype, M, C, F):
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, "gu", seed=5)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    h, grads = reference(x, wg, wu, dh, bg, bu, "gelu")
+    args = dict(b_gate=bg, b_up=bu, activation="gelu")
+    check_forward(mod.gated(x, wg, wu, **args), h, dtype)
+    back = mod.gated_backward(x, wg, wu, dh, **args)
+    assert mod.query_status() == 0
+    for n, t in back.items():
+        assert rel(t, grads[n]) <= REL_BWD[dtype], (n, rel(t, grads[n]))
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_activations_over_their_range(name, dtype):
+    """One channel, weights of one: G is the input itself, U a bias of one.  Saturated ends and extreme inputs give neither NaN nor wrong signs."""
+    big = 6e4 if dtype == "f16" else 1e30
+    x = torch.cat([torch.linspace(-12, 12, 2001), torch.tensor([-big, -300.0, -40.0, 40.0, 300.0, big])]).to(DT[dtype]).cuda()[:, None]
+    x = torch.cat([x, torch.zeros((x.shape[0], 7), device="cuda", dtype=x.dtype)], 1)
+    wg = torch.zeros((8, 8), device="cuda", dtype=x.dtype)
+    wg[:, 0] = 1
+    wu, one = torch.zeros_like(wg), torch.ones(8, device="cuda", dtype=x.dtype)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    got = mod.gated(x, wg, wu, b_up=one, activation=name)
+    g = x[:, :1].double()
+    want = torch.where(g < -100, 0.0, torch.where(g > 100, g, act(name, g.clamp(-100, 100))))
+    tol = 2.4e-7 * g.abs().clamp(max=100) + (STEP.get(dtype, 2.0 ** -23)) * want.abs() + (6e-8 if dtype == "f16" else 1e-12)
+    tol = tol + 1e-6 * g.abs().clamp(max=6)                  # absolute error of the sigmoid and of the normal distribution
+    assert torch.isfinite(got).all() and ((got.double() - want).abs() <= tol).all()
+    # derivative: d(act)/dg is the gradient of the gate's bias, row by row
+    for i in (0, 700, 1000, 1200, 2000, 2001, 2006):
+        leaf = g[i:i + 1].clamp(-100, 100).requires_grad_()
+        act(name, leaf).sum().backward()
+        back = mod.gated_backward(x[i:i + 1].contiguous(), wg, wu, torch.ones((1, 8), device="cuda", dtype=x.dtype), b_gate=torch.zeros_like(one), b_up=one, activation=name)
+        assert abs(float(back["db_gate"][0]) - float(leaf.grad)) <= 2 * STEP.get(dtype, 2.0 ** -22) * abs(float(leaf.grad)) + 3e-6
+
+
+def test_gradient_against_differences():
+    """Central differences of the forward call in fp32 with steps of 1e-2."""
+    M, C, F = 40, 24, 64
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, "f32", "gu", seed=9)
+    t = inputs(M, C, F, "f32", "gu", seed=10)
+    mod = AgentAttention(1, 1, 64, 1, 1, torch.float32)
+
+    def loss(s):
+        h = mod.gated(x + s * t[0], wg + s * t[1], wu + s * t[2], b_gate=bg + s * t[4], b_up=bu + s * t[5], activation="gelu")
+        return float((h.double() * dh).sum())
+    back = mod.gated_backward(x, wg, wu, dh, b_gate=bg, b_up=bu, activation="gelu")
+    parts = [back[n].double() * d for n, d in (("dx", t[0]), ("dw_gate", t[1]), ("dw_up", t[2]), ("db_gate", t[4]), ("db_up", t[5]))]
+    slope, size = float(sum(p.sum() for p in parts)), float(sum(p.abs().sum() for p in parts))
+    assert abs((loss(1e-2) - loss(-1e-2)) / 2e-2 - slope) <= 1e-3 * size
+
+
+def test_non_finite_rows_stay_alone():
+    """A NaN or an infinity in a row of X reaches that row only; in a row of a weight, that hidden unit only."""
+    for dtype in ("bf16", "f32"):
+        x, wg, wu, dh, bg, bu = inputs(200, 64, 136, dtype, "", seed=2)
+        mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+        clean = mod.gated(x, wg, wu)
+        x[77, 3], x[130, 0], wu[9, 9] = float("nan"), float("inf"), float("nan")
+        got = mod.gated(x, wg, wu)
+        rows, cols = torch.ones(200, dtype=torch.bool, device="cuda"), torch.ones(136, dtype=torch.bool, device="cuda")
+        rows[[77, 130]], cols[9] = False, False
+        assert torch.equal(got[rows][:, cols], clean[rows][:, cols])
+        assert torch.isnan(got[77]).all() and torch.isnan(got[:, 9]).all()
+
+
+def test_streams_batched_shapes_fused_weights_and_parts():
+    x, wg, wu, dh, bg, bu = inputs(6 * 50, 64, 128, "bf16", "gu", seed=4)
+    mod = AgentAttention(1, 1, 64, 1, 1, torch.bfloat16)
+    want = mod.gated(x, wg, wu, b_gate=bg, b_up=bu, activation="gelu")
+    fused = torch.cat([wg, wu])
+    a, b = fused.chunk(2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = mod.gated(x.view(6, 50, 64), a, b, b_gate=bg, b_up=bu, activation="gelu", stream=side)
+    back = mod.gated_backward(x, a, b, dh, b_gate=bg, b_up=bu, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert got.shape == (6, 50, 128) and torch.equal(got.view(300, 128), want)
+    only_x = mod.gated_backward(x, a, b, dh, b_gate=bg, b_up=bu, need_weight_grads=False)
+    only_w = mod.gated_backward(x, a, b, dh, b_gate=bg, b_up=bu, need_input_grad=False)
+    assert list(only_x) == ["dx"] and "dx" not in only_w
+    assert all(torch.equal(back[n], t) for part in (only_x, only_w) for n, t in part.items())
+
+
+def test_refusals():
+    x, wg, wu, dh, bg, bu = inputs(16, 64, 128, "bf16", "gu")
+    mod = AgentAttention(1, 1, 64, 1, 1, torch.bfloat16)
+    for bad in (lambda: mod.gated(x, wg, wu, activation="relu"), lambda: mod.gated(x.float(), wg, wu), lambda: mod.gated(x, wg, wu[:-1]),
+                lambda: mod.gated(x, wg, wu, b_gate=bg[:-1]), lambda: mod.gated(x[:, ::2], wg[:, ::2], wu), lambda: mod.gated(x.cpu(), wg, wu),
+                lambda: mod.gated_backward(x, wg, wu, dh[:-1])):
+        with pytest.raises(ValueError):
+            bad()
+
+    def status(call):
+        with pytest.raises(AgentAttnError) as e:
+            call()
+        return e.value.status
+    assert status(lambda: mod.gated(x[:, :60].contiguous(), wg[:, :60].contiguous(), wu[:, :60].contiguous())) == 2      # rows of no 16 bytes
+    assert status(lambda: mod.gated(x, wg[:100].contiguous(), wu[:100].contiguous())) == 2
+    assert status(lambda: mod.gated(x[:0], wg, wu)) == 1                                                                  # no rows
+    assert status(lambda: mod.gated_backward(x, wg, wu, dh, need_input_grad=False, need_weight_grads=False)) == 1
+    assert status(lambda: mod.gated_backward(x, wg, wu, dh, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))) == 3
+    wide = torch.empty(16 * 64 + 1, device="cuda", dtype=torch.bfloat16)[1:].view(16, 64)                                 # off by an element
+    assert status(lambda: mod.gated(wide, wg, wu)) == 1
+    assert status(lambda: mod.gated(x, wg[:64].contiguous(), wu[:64].contiguous(), out=x)) == 1
+    lib = mod.lib
+    assert lib.agent_attn_gated(mod._h, None, x.data_ptr(), None, 0, None) == 1
+    assert lib.agent_attn_gated_workspace_bytes(mod._h, 16, 60, 128, 0) == 0 and lib.agent_attn_gated_workspace_bytes(mod._h, 16, 64, 128, 0) == 0
+    assert lib.agent_attn_gated_workspace_bytes(mod._h, 16, 64, 128, 1) > 0
