@@ -13,6 +13,7 @@
 // 16-bit operands enter as they are; dG and dU are rounded to the element type, as every operand of a product on the tensor cores is.  fp32: operands are sums of
 // three bf16 terms, six pairs of terms, small ones first.
 #include "bwd_terms.cuh"
+#include "pair.cuh"
 #include "stream_common.cuh"
 
 namespace aa {
@@ -22,21 +23,22 @@ namespace {
 enum GatedMode { kForward, kGrad, kInput, kWeight };
 constexpr int kEpiWarps = 8, kThreads = 32 * (kEpiWarps + 2);
 constexpr int kATile = 128 * 128;                      // bytes of a [128][64] (or [64][128]) tile of 16-bit elements
-constexpr int kStages = 4;
-constexpr int OFF_RING = 1024;
+constexpr int kPatch = 4096;                           // bytes of a warp's staged box
 constexpr int kTimeoutTile = 3, kTimeoutRole = 6;
-// mbarriers: full [kStages], empty [kStages], accumulator ready [2], accumulator read [2], drain
-constexpr int BAR_FULL = 0, BAR_EMPTY = kStages, BAR_ACC = 2 * kStages, BAR_READ = BAR_ACC + 2, BAR_DRAIN = BAR_READ + 2, kBars = BAR_DRAIN + 1;
+// mbarriers: full [kRing], empty [kRing], accumulator ready [2], accumulator read [2], drain, dH [warps][2 halves]
+constexpr int kRing = 6, BAR_FULL = 0, BAR_EMPTY = kRing, BAR_ACC = 2 * kRing, BAR_READ = BAR_ACC + 2, BAR_DRAIN = BAR_READ + 2, BAR_DH = BAR_DRAIN + 1, kBars = BAR_DH + 2 * kEpiWarps;
+static_assert(kBars * 8 <= 1024, "barriers");
 
 struct GatedArgs {
     int M, C, F, act;
     int tiles_m, tiles_n, splits, chunks;              // chunks: 64 long, of the sum
-    int n;                                             // columns of a tile (kInput, kWeight): a multiple of 16
+    int n;                                             // columns of a tile (kInput, kWeight): a multiple of 32
+    int wide;                                          // results leave as fp32 (fp32 tensors, shares of a split sum)
     const void *bg, *bu, *dh;
-    void *out0, *out1;                                 // H; dG and dU; dX; dWg and dWu
-    float* part;                                       // [splits][rows][C], where splits > 1
+    void *out0, *out1;                                 // H; dG and dU: where they are written without staging
+    float* column;                                     // [slots][2][F]: shares of the column sums of dG and dU, or null
     int* status;
-    alignas(64) CUtensorMap a[2], b[2];
+    alignas(64) CUtensorMap a[2], b[2], s[2], g;       // operands; staged results; dH
 };
 
 template <typename T> struct GatedTerms {              // element of the operands, terms and pairs of terms
@@ -52,25 +54,68 @@ __device__ __forceinline__ void term_pair(int i, int& a, int& b) {     // (2,0) 
     b = (0x010210 >> (4 * i)) & 3;
 }
 
-// act(g) and, for the gradient, its derivative
-struct Activated { float a, da; };
-template <typename T, bool GRAD> __device__ __forceinline__ Activated activate(int act, float g) {
-    Activated r;
-    r.da = 0.f;
-    if (act == 1) {                                                    // GELU: g Phi(g)
-        const float cdf = 0.5f + 0.5f * erff(g * 0.70710678f);
-        r.a = g * cdf;
-        if (GRAD) r.da = fmaf(g * 0.39894228f, expf(-0.5f * g * g), cdf);
-        return r;
+// act(g) and, for the gradient, its derivative, of a pair of values.  SiLU: g sigmoid(g).  GELU by tanh: g sigmoid(2 k (g + c g^3)), since
+// 0.5 (1 + tanh z) = sigmoid(2 z).  GELU: g Phi(g).
+constexpr float kTanh2 = 1.5957691216f, kTanhC = 0.044715f;            // 2 sqrt(2 / pi)
+__device__ __forceinline__ float fast_rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+template <typename T, bool GRAD> __device__ __forceinline__ void activate(int act, float2 g, float2& a, float2& da) {
+    da = both(0.f);
+    if constexpr (sizeof(T) == 4) {                                    // fp32 accuracy
+        const float gs[2] = {g.x, g.y};
+        float r[2], d[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float x = gs[i];
+            if (act == 1) {
+                const float cdf = 0.5f + 0.5f * erff(x * 0.70710678f);
+                r[i] = x * cdf;
+                if (GRAD) d[i] = fmaf(x * 0.39894228f, expf(-0.5f * x * x), cdf);
+            } else {
+                const float x2 = fminf(x * x, 1e4f);                   // (far past where the sigmoid is 0 or 1: no infinity meets a zero)
+                const float s = 1.f / (1.f + expf(act == 2 ? -kTanh2 * x * fmaf(kTanhC, x2, 1.f) : -x));
+                r[i] = x * s;
+                if (GRAD) d[i] = fmaf(x * (1.f - s), act == 2 ? s * kTanh2 * fmaf(3.f * kTanhC, x2, 1.f) : s, s);
+            }
+        }
+        a = make_float2(r[0], r[1]);
+        da = make_float2(d[0], d[1]);
+    } else if (act == 1) {
+        // Upper tail Q(x) = exp(-x^2 / 2) R(x), x = |g|, with R (half of a scaled complementary error function, smooth from 1/2 down) as a
+        // polynomial on [0, 5], fitted with weight exp(-x^2 / 2): Q is within 3e-7 (a 16-bit result of size 1e-3 ends at 2e-6).  One
+        // special-function instruction, which the derivative shares; the fast error function of the library takes 3.4 times the epilogue's time.
+        const float2 x = make_float2(fminf(fabsf(g.x), 5.f), fminf(fabsf(g.y), 5.f));
+        const float2 w = fmul2(fmul2(g, g), both(-0.72134752f));       // log2 of exp(-g^2 / 2)
+        const float2 e = make_float2(fast_exp2(w.x), fast_exp2(w.y));
+        float2 r = both(-8.063080713e-06f);
+        r = ffma2(r, x, both(1.519420184e-04f));
+        r = ffma2(r, x, both(-1.271162881e-03f));
+        r = ffma2(r, x, both(6.382808089e-03f));
+        r = ffma2(r, x, both(-2.223088220e-02f));
+        r = ffma2(r, x, both(5.949680135e-02f));
+        r = ffma2(r, x, both(-1.317728907e-01f));
+        r = ffma2(r, x, both(2.497522980e-01f));
+        r = ffma2(r, x, both(-3.989226222e-01f));
+        r = ffma2(r, x, both(4.999997318e-01f));
+        const float2 h = ffma2(fmul2(e, both(-1.f)), r, both(0.5f));   // 1/2 - Q: Phi is that above 1/2, or below
+        const float2 cdf = fadd2(both(0.5f), make_float2(copysignf(h.x, g.x), copysignf(h.y, g.y)));
+        a = fmul2(g, cdf);
+        if (GRAD) da = ffma2(fmul2(g, both(0.39894228f)), e, cdf);
+    } else {
+        float2 z = fmul2(g, both(-kLog2e)), slope = both(1.f);
+        if (act == 2) {
+            const float2 q = fmul2(g, g), g2 = make_float2(fminf(q.x, 1e4f), fminf(q.y, 1e4f));
+            z = fmul2(fmul2(g, both(-kLog2e * kTanh2)), ffma2(g2, both(kTanhC), both(1.f)));
+            if (GRAD) slope = ffma2(g2, both(3.f * kTanhC * kTanh2), both(kTanh2));
+        }
+        const float2 s = make_float2(fast_rcp(1.f + fast_exp2(z.x)), fast_rcp(1.f + fast_exp2(z.y)));
+        a = fmul2(g, s);
+        if (GRAD) da = ffma2(fmul2(a, slope), ffma2(s, both(-1.f), both(1.f)), s);
     }
-    // SiLU: g sigmoid(g).  GELU by tanh: g sigmoid(2 k (g + c g^3)), since 0.5 (1 + tanh z) = sigmoid(2 z)
-    constexpr float k2 = 1.5957691216f, c = 0.044715f;
-    const float g2 = fminf(g * g, 1e4f);                               // (far past where the sigmoid is 0 or 1: no infinity meets a zero)
-    const float z = act == 2 ? k2 * g * fmaf(c, g2, 1.f) : g;
-    const float s = 1.f / (1.f + expf(-z));
-    r.a = g * s;
-    if (GRAD) r.da = fmaf(g * (1.f - s), act == 2 ? s * k2 * fmaf(3.f * c, g2, 1.f) : s, s);
-    return r;
 }
 
 // eight consecutive elements
@@ -102,23 +147,71 @@ template <typename T> __device__ __forceinline__ void store_operand8(void* base,
         for (int t = 0; t < 3; ++t) *reinterpret_cast<uint4*>(static_cast<E*>(base) + t * plane + at) = make_uint4(o[t][0], o[t][1], o[t][2], o[t][3]);
     }
 }
+__device__ __forceinline__ void st_shared4(uint32_t at, uint4 v) { asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
+__device__ __forceinline__ uint4 ld_shared4(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_shared1(uint32_t at) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
 
-template <GatedMode MODE, int BN> struct GatedShape {
-    static constexpr int kN = MODE <= kGrad ? 2 * BN : 256;            // columns of an accumulator
-    static constexpr int kStage = kATile + kN * 128;
-    static constexpr int kSmem = OFF_RING + kStages * kStage + 1024;
+// A pair of blocks takes a tile of 256 rows, each of its blocks 128 of them and half of the B operand (BN = 128, and kInput and kWeight); a lone
+// block a tile of 128 rows and 2 BN columns (BN = 64 or 32: small problems).
+template <typename T, GatedMode MODE, int BN> struct GatedShape {
+    static constexpr bool kPair = BN == 128, kStaged = MODE >= kInput || (kPair && sizeof(T) == 2);
+    static constexpr int kBTile = kPair ? kATile : 2 * BN * 128;
+    static constexpr int kStage = kATile + kBTile;
+    static constexpr int kPatches = !kStaged ? 0 : MODE == kGrad ? 2 : 1;          // of a warp
+    static constexpr int kStages = MODE == kForward ? 5 : MODE == kGrad ? 4 : 6;
+    static constexpr int kOffPatch = 1024 + kStages * kStage, kOffBias = kOffPatch + kPatches * kEpiWarps * kPatch;
+    static constexpr int kSmem = kOffBias + (MODE <= kGrad && kStaged ? kEpiWarps * 512 : 0) + 1024;
 };
 
+// Units of work of block (or pair) `who` of `count`: kForward and kGrad a run in the order of the rows, so that a run has few column ranges
+template <GatedMode MODE> struct Units {
+    int at, end, step;
+    __device__ Units(int units, int who, int count) {
+        if (MODE <= kGrad) {
+            at = (int)((long long)units * who / count);
+            end = (int)((long long)units * (who + 1) / count);
+            step = 1;
+        } else {
+            at = who; end = units; step = count;
+        }
+    }
+};
+struct Unit { int mt, nt, split, k0, k1; };
+template <GatedMode MODE> __device__ __forceinline__ Unit unit_of(const GatedArgs& p, int u) {
+    Unit t;
+    const int fast = MODE <= kGrad ? p.tiles_m : p.tiles_n, v = u / fast, low = u - v * fast;
+    if (MODE <= kGrad) {
+        t.mt = low; t.nt = v; t.split = 0; t.k0 = 0; t.k1 = p.chunks;
+    } else {
+        t.nt = low;
+        t.split = v / p.tiles_m;
+        t.mt = v - t.split * p.tiles_m;
+        t.k0 = (int)((long long)p.chunks * t.split / p.splits);
+        t.k1 = (int)((long long)p.chunks * (t.split + 1) / p.splits);
+    }
+    return t;
+}
+
 template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constant__ GatedArgs p) {
-    using S = GatedShape<MODE, BN>;
+    using S = GatedShape<T, MODE, BN>;
     using E = typename GatedTerms<T>::E;
-    constexpr int kPairs = GatedTerms<T>::kPairs, kN = S::kN;
+    constexpr int kPairs = GatedTerms<T>::kPairs, kStages = S::kStages;
+    constexpr bool PAIR = S::kPair;
     extern __shared__ unsigned char smem_raw[];
     __shared__ int s_dead;
     __shared__ uint32_t s_tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const int units = p.tiles_m * p.tiles_n * p.splits;
+    const uint32_t rank = PAIR ? cluster_rank() : 0u;
+    const int units = p.tiles_m * p.tiles_n * p.splits, who = PAIR ? blockIdx.x / 2 : blockIdx.x, count = PAIR ? gridDim.x / 2 : gridDim.x;
 
     Pipe pp;
     pp.status = p.status;
@@ -126,188 +219,387 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
     pp.bars = base;
     if (tid == 0) {
         s_dead = 0;
-        for (int i = 0; i < kBars; ++i) mbar_init(pp.bars + 8 * i, i >= BAR_READ && i < BAR_DRAIN ? kEpiWarps : 1u);
+        for (int i = 0; i < kBars; ++i) mbar_init(pp.bars + 8 * i, i >= BAR_READ && i < BAR_DRAIN ? (PAIR ? 2 : 1) * kEpiWarps : 1u);
         mbar_fence_init();
     }
-    if (warp == 0) tmem_alloc<512>(smem_u32(&s_tmem));
+    if (warp == 0) {
+        if (PAIR) tmem_alloc_pair<512>(smem_u32(&s_tmem));
+        else tmem_alloc<512>(smem_u32(&s_tmem));
+    }
     tc_fence_before_sync();
     __syncthreads();
+    if (PAIR) cluster_sync();
     tc_fence_after_sync();
     pp.tmem = s_tmem;
     pdl_wait_prior();
     pdl_release_next();
 
-    const int tiles_f = (p.F + 127) / 128, chunks_f = (p.F + 63) / 64;
-    auto unit_of = [&](int u, int& mt, int& nt, int& k0, int& k1) {
-        nt = u % p.tiles_n;
-        const int v = u / p.tiles_n, split = v / p.tiles_m;
-        mt = v - split * p.tiles_m;
-        k0 = (int)((long long)p.chunks * split / p.splits);
-        k1 = (int)((long long)p.chunks * (split + 1) / p.splits);
-        return split;
-    };
+    const int chunks_f = (p.F + 63) / 64;
+    Units<MODE> run(units, who, count);
 
     if (warp == kEpiWarps) {
         // ------------------------------------------------------------------ producer
         if (lane == 0) {
             int stage = 0, round = 0;
-            for (int u = blockIdx.x; u < units && !pipe_dead(pp); u += gridDim.x) {
-                int mt, nt, k0, k1;
-                unit_of(u, mt, nt, k0, k1);
-                const int boxes = MODE <= kGrad ? 0 : (p.n + 63) / 64;
+            const int half_n = p.n / 2, boxes = MODE <= kGrad ? 0 : (half_n + 63) / 64;        // of 64 columns
+            const uint32_t bytes = MODE <= kGrad ? S::kStage : kATile + boxes * 8192;          // of this block's share
+            const uint32_t full0 = PAIR ? in_block(pipe_bar(pp, BAR_FULL), 0) : pipe_bar(pp, BAR_FULL);
+            auto load = [&](uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+                if (PAIR) tma_load_3d_pair(dst, map, x, y, z, bar);
+                else tma_load_3d(dst, map, x, y, z, bar);
+            };
+            for (int u = run.at; u < run.end && !pipe_dead(pp); u += run.step) {
+                const Unit t = unit_of<MODE>(p, u);
                 for (int pair = 0; pair < kPairs; ++pair) {
                     int ta = 0, tb = 0;
                     if (kPairs > 1) term_pair(pair, ta, tb);
-                    for (int k = k0; k < k1 && !pipe_dead(pp); ++k) {
+                    for (int k = t.k0; k < t.k1 && !pipe_dead(pp); ++k) {
                         if (round > 0) wait_spin(pp, BAR_EMPTY + stage, round - 1, kTimeoutRole);
-                        const uint32_t bar = pipe_bar(pp, BAR_FULL + stage), da = base + OFF_RING + stage * S::kStage, db = da + kATile;
+                        const uint32_t bar = full0 + 8 * stage, da = base + 1024 + stage * S::kStage, db = da + kATile;
+                        if (rank == 0) mbar_arrive_expect_tx(pipe_bar(pp, BAR_FULL + stage), (PAIR ? 2 : 1) * bytes);
                         if constexpr (MODE <= kGrad) {
-                            mbar_arrive_expect_tx(bar, S::kStage);
-                            tma_load_3d(da, &p.a[0], 64 * k, 128 * mt, ta, bar);
-                            tma_load_3d(db, &p.b[0], 64 * k, BN * nt, tb, bar);
-                            tma_load_3d(db + BN * 128, &p.b[1], 64 * k, BN * nt, tb, bar);
-                        } else if constexpr (MODE == kInput) {
-                            const int op = k >= chunks_f, kk = k - op * chunks_f;
-                            mbar_arrive_expect_tx(bar, kATile + boxes * 8192);
-                            tma_load_3d(da, &p.a[op], 64 * kk, 128 * mt, ta, bar);
-                            for (int j = 0; j < boxes; ++j) tma_load_3d(db + j * 8192, &p.b[op], p.n * nt + 64 * j, 64 * kk, tb, bar);
+                            load(da, &p.a[0], 64 * k, (PAIR ? 256 : 128) * t.mt + 128 * rank, ta, bar);
+                            if (PAIR) {
+                                load(db, &p.b[rank], 64 * k, BN * t.nt, tb, bar);               // one block has the gate's rows, the other the rest
+                            } else {
+                                load(db, &p.b[0], 64 * k, BN * t.nt, tb, bar);
+                                load(db + BN * 128, &p.b[1], 64 * k, BN * t.nt, tb, bar);
+                            }
                         } else {
-                            const int op = mt >= tiles_f, f0 = 128 * (mt - op * tiles_f);
-                            mbar_arrive_expect_tx(bar, kATile + boxes * 8192);
-                            tma_load_3d(da, &p.a[op], f0, 64 * k, ta, bar);
-                            tma_load_3d(da + 8192, &p.a[op], f0 + 64, 64 * k, ta, bar);
-                            for (int j = 0; j < boxes; ++j) tma_load_3d(db + j * 8192, &p.b[0], p.n * nt + 64 * j, 64 * k, tb, bar);
+                            const int op = MODE == kInput ? k >= chunks_f : rank, kk = MODE == kInput ? k - op * chunks_f : k, c0 = p.n * t.nt + half_n * rank;
+                            if constexpr (MODE == kInput) {
+                                load(da, &p.a[op], 64 * kk, 256 * t.mt + 128 * rank, ta, bar);
+                            } else {                                                            // one block has dG's columns, the other dU's
+                                load(da, &p.a[op], 128 * t.mt, 64 * k, ta, bar);
+                                load(da + 8192, &p.a[op], 128 * t.mt + 64, 64 * k, ta, bar);
+                            }
+                            for (int j = 0; j < boxes; ++j) load(db + j * 8192, &p.b[MODE == kInput ? op : 0], c0 + 64 * j, 64 * kk, tb, bar);
                         }
                         if (++stage == kStages) { stage = 0; ++round; }
                     }
                 }
             }
-            // no copy may be in flight at the block's end, whatever became of the other roles
+            // no copy, and no arrival of the pair's products, may be under way at the block's end, whatever became of the other roles
             for (int s = 0; s < kStages; ++s) {
                 const int last = s < stage ? round : round - 1;
-                if (last >= 0) mbar_wait_bounded(pipe_bar(pp, BAR_FULL + s), last & 1, 1u << 16);
+                if (last < 0) continue;
+                if (rank == 0) mbar_wait_bounded(pipe_bar(pp, BAR_FULL + s), last & 1, 1u << 16);
+                if (!pipe_dead(pp)) mbar_wait_bounded(pipe_bar(pp, BAR_EMPTY + s), last & 1, 1u << 20);
             }
         }
         __syncwarp();
     } else if (warp == kEpiWarps + 1) {
         // ------------------------------------------------------------------ products
-        constexpr int fmt = Elem<E>::kIsBf16 ? 1 : 0;
-        const uint32_t id = umma_idesc(fmt, 128, MODE <= kGrad ? kN : p.n, MODE >= kInput) | (MODE == kWeight ? 1u << 15 : 0u);
-        const int total = MODE <= kGrad ? p.C : MODE == kInput ? p.F : p.M;
-        int stage = 0, round = 0, ord = 0;
-        for (int u = blockIdx.x; u < units && !pipe_dead(pp); u += gridDim.x, ++ord) {
-            int mt, nt, k0, k1;
-            unit_of(u, mt, nt, k0, k1);
-            const int buf = ord & 1;
-            if (ord >= 2) wait_spin(pp, BAR_READ + buf, (ord >> 1) - 1, kTimeoutRole);
-            tc_fence_after_sync();
-            const uint32_t d = pp.tmem + 256 * buf;
-            uint32_t acc = 0;
-            for (int pair = 0; pair < kPairs; ++pair)
-                for (int k = k0; k < k1 && !pipe_dead(pp); ++k) {
-                    wait_spin(pp, BAR_FULL + stage, round, kTimeoutTile);
-                    tc_fence_after_sync();
-                    const uint32_t at = base + OFF_RING + stage * S::kStage;
-                    const uint64_t da = MODE == kWeight ? desc_mn(at, 8192) : umma_desc_sw128(at);
-                    const uint64_t db = MODE <= kGrad ? umma_desc_sw128(at + kATile) : desc_mn(at + kATile, 8192);
-                    const int kk = MODE == kInput && k >= chunks_f ? k - chunks_f : k;
-                    const int steps = min(4, (total - 64 * kk + 15) / 16);
-                    // descriptor addresses count 16 bytes: a step of 16 is 2 along a K-major row, 128 down MN-major ones
-                    for (int s = 0; s < steps; ++s, acc = 1u) umma_ss_w(d, da + (MODE == kWeight ? 128 : 2) * s, db + (MODE <= kGrad ? 2 : 128) * s, id, acc);
-                    umma_commit_w(pipe_bar(pp, BAR_EMPTY + stage));
-                    if (++stage == kStages) { stage = 0; ++round; }
-                }
-            umma_commit_w(pipe_bar(pp, BAR_ACC + buf));
+        if (rank == 0) {
+            constexpr int fmt = Elem<E>::kIsBf16 ? 1 : 0;
+            const uint32_t id = umma_idesc(fmt, PAIR ? 256 : 128, MODE <= kGrad ? 2 * BN : p.n, MODE >= kInput) | (MODE == kWeight ? 1u << 15 : 0u);
+            const int total = MODE <= kGrad ? p.C : MODE == kInput ? p.F : p.M;
+            int stage = 0, round = 0, ord = 0;
+            for (int u = run.at; u < run.end && !pipe_dead(pp); u += run.step, ++ord) {
+                const Unit t = unit_of<MODE>(p, u);
+                const int buf = ord & 1;
+                if (ord >= 2) wait_spin(pp, BAR_READ + buf, (ord >> 1) - 1, kTimeoutRole);
+                tc_fence_after_sync();
+                const uint32_t d = pp.tmem + 256 * buf;
+                uint32_t acc = 0;
+                for (int pair = 0; pair < kPairs; ++pair)
+                    for (int k = t.k0; k < t.k1 && !pipe_dead(pp); ++k) {
+                        wait_spin(pp, BAR_FULL + stage, round, kTimeoutTile);
+                        tc_fence_after_sync();
+                        const uint32_t at = base + 1024 + stage * S::kStage;
+                        const uint64_t da = MODE == kWeight ? desc_mn(at, 8192) : umma_desc_sw128(at);
+                        const uint64_t db = MODE <= kGrad ? umma_desc_sw128(at + kATile) : desc_mn(at + kATile, 8192);
+                        const int kk = MODE == kInput && k >= chunks_f ? k - chunks_f : k;
+                        const int steps = min(4, (total - 64 * kk + 15) / 16);
+                        // descriptor addresses count 16 bytes: a step of 16 is 2 along a K-major row, 128 down MN-major ones
+                        for (int s = 0; s < steps; ++s, acc = 1u) {
+                            const uint64_t sa = da + (MODE == kWeight ? 128 : 2) * s, sb = db + (MODE <= kGrad ? 2 : 128) * s;
+                            if (PAIR) umma_ss_pair(d, sa, sb, id, acc);
+                            else umma_ss_w(d, sa, sb, id, acc);
+                        }
+                        if (PAIR) umma_commit_pair(pipe_bar(pp, BAR_EMPTY + stage));
+                        else umma_commit_w(pipe_bar(pp, BAR_EMPTY + stage));
+                        if (++stage == kStages) { stage = 0; ++round; }
+                    }
+                if (PAIR) umma_commit_pair(pipe_bar(pp, BAR_ACC + buf));
+                else umma_commit_w(pipe_bar(pp, BAR_ACC + buf));
+            }
+            if (PAIR) {
+                umma_commit_first(pipe_bar(pp, BAR_DRAIN));
+                mbar_wait_bounded(pipe_bar(pp, BAR_DRAIN), 0u, 1u << 20);
+            } else {
+                umma_drain_w(pp, BAR_DRAIN);
+            }
         }
-        umma_drain_w(pp, BAR_DRAIN);
         __syncwarp();
     } else {
         // ------------------------------------------------------------------ epilogue
         const int q = warp & 3, half = warp >> 2;
+        const uint32_t patch = base + S::kOffPatch + warp * S::kPatches * kPatch;
+        const uint32_t read0 = PAIR ? in_block(pipe_bar(pp, BAR_READ), 0) : pipe_bar(pp, BAR_READ);
         int ord = 0;
-        for (int u = blockIdx.x; u < units; u += gridDim.x, ++ord) {
-            int mt, nt, k0, k1;
-            const int split = unit_of(u, mt, nt, k0, k1), buf = ord & 1;
-            const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
-            wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
-            tc_fence_after_sync();
-            auto release = [&] {
-                tc_fence_before_sync();
-                pipe_arrive_warp(pp, BAR_READ + buf, lane);
-            };
-            if constexpr (MODE <= kGrad) {
-                const int row = 128 * mt + 32 * q + lane;
-                const size_t plane = (size_t)p.M * p.F;
+        auto release = [&](int buf) {
+            tc_fence_before_sync();
+            if (PAIR) arrive_cluster_warp(read0 + 8 * buf, lane);
+            else pipe_arrive_warp(pp, BAR_READ + buf, lane);
+        };
+        if constexpr (MODE <= kGrad && S::kStaged) {
+            // Warp: 32 rows, 64 hidden units in two halves of 32.  kGrad: dH arrives by TMA in the place that dG leaves from, a half ahead.
+            const uint32_t bias = base + S::kOffBias + warp * 512;
+            const uint32_t swz = (lane >> 1) & 3;                      // of rows of 64 bytes
+            float2 column[2][2] = {};                                  // [half][dG, dU]: sums of two columns over this run's rows
+            int column_nt = -1;
+            auto flush = [&] {                                         // lanes l and l + 16 have even and odd rows of the same columns
+                const int first = (int)(((long long)column_nt * p.tiles_m + 1) * count - 1) / units;
+                float* dst = p.column + (size_t)(8 * (who - first) + 4 * rank + q) * 2 * p.F;
 #pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int o = 0; o < 2; ++o) {
+                        float2 v = column[h][o];
+                        v.x += __shfl_xor_sync(0xffffffffu, v.x, 16);
+                        v.y += __shfl_xor_sync(0xffffffffu, v.y, 16);
+                        const int f = BN * column_nt + 64 * half + 32 * h + 2 * (lane & 15);
+                        if (lane < 16 && f < p.F) *reinterpret_cast<float2*>(dst + (size_t)o * p.F + f) = v;
+                        column[h][o] = both(0.f);
+                    }
+            };
+            auto fetch = [&](int u, int h) {                           // one lane: dH of a half
+                const Unit t = unit_of<MODE>(p, u);
+                const uint32_t bar = pipe_bar(pp, BAR_DH + 2 * warp + h);
+                mbar_arrive_expect_tx(bar, 2048);
+                tma_load_3d(patch + 2048 * h, &p.g, BN * t.nt + 64 * half + 32 * h, 256 * t.mt + 128 * rank + 32 * q, 0, bar);
+            };
+            if (MODE == kGrad && lane == 0 && run.at < run.end) { fetch(run.at, 0); fetch(run.at, 1); }
+            const bool biased = p.bg || p.bu;
+            for (int u = run.at; u < run.end; u += run.step, ++ord) {
+                const Unit t = unit_of<MODE>(p, u);
+                const int buf = ord & 1, row0 = 256 * t.mt + 128 * rank + 32 * q, f0 = BN * t.nt + 64 * half;
+                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16) + 64 * half;
+                if (MODE == kGrad && p.column && column_nt != t.nt) {
+                    if (column_nt >= 0) flush();
+                    column_nt = t.nt;
+                }
+                if (biased) {                                          // as fp32, two a lane: [gate | up][64]
+                    const int f = f0 + 2 * lane;
+                    float2 bg = both(0.f), bu = bg;
+                    if (p.bg && f < p.F) bg = unpack2<T>(__ldg(reinterpret_cast<const uint32_t*>(static_cast<const T*>(p.bg) + f)));
+                    if (p.bu && f < p.F) bu = unpack2<T>(__ldg(reinterpret_cast<const uint32_t*>(static_cast<const T*>(p.bu) + f)));
+                    __syncwarp();
+                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};\n" ::"r"(bias + 8 * lane), "f"(bg.x), "f"(bg.y) : "memory");
+                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};\n" ::"r"(bias + 256 + 8 * lane), "f"(bu.x), "f"(bu.y) : "memory");
+                    __syncwarp();
+                }
+                wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
+                tc_fence_after_sync();
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    float g[32], v[32];
+                    __syncwarp();
+                    tmem_ld32(acc + 32 * h, reinterpret_cast<uint32_t(&)[32]>(g));
+                    tmem_ld32(acc + BN + 32 * h, reinterpret_cast<uint32_t(&)[32]>(v));
+                    if (MODE == kGrad) wait_par(pp, BAR_DH + 2 * warp + h, ord, kTimeoutTile);
+                    else if (h == 0) {                                 // the tile before has left its patch
+                        if (lane == 0) store_wait_read<0>();
+                        __syncwarp();
+                    }
+                    tmem_ld_wait();
+                    if (h == 1) release(buf);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {                      // pieces of eight hidden units
+                        float2 gg[4], vv[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            gg[i] = make_float2(g[8 * c + 2 * i], g[8 * c + 2 * i + 1]);
+                            vv[i] = make_float2(v[8 * c + 2 * i], v[8 * c + 2 * i + 1]);
+                        }
+                        if (biased) {
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const uint4 x = ld_shared4(bias + 128 * h + 32 * c + 16 * i), y = ld_shared4(bias + 256 + 128 * h + 32 * c + 16 * i);
+                                gg[2 * i] = fadd2(gg[2 * i], make_float2(__uint_as_float(x.x), __uint_as_float(x.y)));
+                                gg[2 * i + 1] = fadd2(gg[2 * i + 1], make_float2(__uint_as_float(x.z), __uint_as_float(x.w)));
+                                vv[2 * i] = fadd2(vv[2 * i], make_float2(__uint_as_float(y.x), __uint_as_float(y.y)));
+                                vv[2 * i + 1] = fadd2(vv[2 * i + 1], make_float2(__uint_as_float(y.z), __uint_as_float(y.w)));
+                            }
+                        }
+                        uint32_t o0[4], o1[4];
+                        if constexpr (MODE == kForward) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                float2 a, da;
+                                activate<T, false>(p.act, gg[i], a, da);
+                                a = fmul2(a, vv[i]);
+                                o0[i] = pack2<T>(a.x, a.y);
+                            }
+                            st_shared4(patch + 128 * lane + (((4 * h + c) ^ (lane & 7)) << 4), make_uint4(o0[0], o0[1], o0[2], o0[3]));
+                        } else {
+                            const uint32_t at = patch + 2048 * h + 64 * lane + ((c ^ swz) << 4);
+                            const uint4 d = ld_shared4(at);
+                            const uint32_t dd[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                float2 a, da;
+                                activate<T, true>(p.act, gg[i], a, da);
+                                const float2 dh = unpack2<T>(dd[i]);
+                                da = fmul2(fmul2(dh, vv[i]), da);
+                                a = fmul2(dh, a);
+                                o0[i] = pack2<T>(da.x, da.y);
+                                o1[i] = pack2<T>(a.x, a.y);
+                            }
+                            st_shared4(at, make_uint4(o0[0], o0[1], o0[2], o0[3]));
+                            st_shared4(at + kPatch, make_uint4(o1[0], o1[1], o1[2], o1[3]));
+                        }
+                        if (MODE == kGrad && c == 1) {                 // the half before has left: dH of the one after next
+                            const int next = h == 1 ? u + run.step : u;
+                            if (lane == 0 && next < run.end && (h == 1 || ord > 0)) {
+                                store_wait_read<0>();
+                                fetch(next, h ^ 1);
+                            }
+                            __syncwarp();
+                        }
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (MODE == kGrad || h == 1) {
+                        if (lane == 0 && row0 < p.M) {
+                            if constexpr (MODE == kForward) {
+                                if (f0 < p.F) tma_store_3d(&p.s[0], f0, row0, 0, patch);
+                            } else if (f0 + 32 * h < p.F) {
+                                tma_store_3d(&p.s[0], f0 + 32 * h, row0, 0, patch + 2048 * h);
+                                tma_store_3d(&p.s[1], f0 + 32 * h, row0, 0, patch + kPatch + 2048 * h);
+                            }
+                            store_commit();
+                        }
+                    }
+                    if (MODE == kGrad && p.column) {                   // columns 2 (lane % 16) of this half, every other row
+                        const uint32_t at = patch + 2048 * h + 64 * (lane >> 4) + 4 * (lane & 3);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const uint32_t a = at + 128 * r + ((((lane & 15) >> 2) ^ (r & 3)) << 4);
+#pragma unroll
+                            for (int o = 0; o < 2; ++o) {
+                                if (h == 0) add_pair<T>(column[0][o], ld_shared1(a + o * kPatch));
+                                else add_pair<T>(column[1][o], ld_shared1(a + o * kPatch));
+                            }
+                        }
+                    }
+                }
+            }
+            if (MODE == kGrad && p.column && column_nt >= 0) flush();
+            if (lane == 0) store_wait_read<0>();
+            __syncwarp();
+        } else if constexpr (MODE <= kGrad) {
+            for (int u = run.at; u < run.end; u += run.step, ++ord) {
+                const Unit t = unit_of<MODE>(p, u);
+                const int buf = ord & 1, row = (PAIR ? 256 : 128) * t.mt + 128 * rank + 32 * q + lane;
+                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
+                const size_t plane = (size_t)p.M * p.F;
+                wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
+                tc_fence_after_sync();
+#pragma unroll 1
                 for (int s = 0; s < BN / 32; ++s) {
-                    const int col = half * (BN / 2) + 16 * s, f0 = BN * nt + col;
+                    const int col = half * (BN / 2) + 16 * s, f0 = BN * t.nt + col;
                     float g[16], v[16];
                     __syncwarp();
                     tmem_ld16(acc + col, g);
                     tmem_ld16(acc + BN + col, v);
                     tmem_ld_wait();
-                    if (s == BN / 32 - 1) release();
+                    if (s == BN / 32 - 1) release(buf);
 #pragma unroll
                     for (int j = 0; j < 16; j += 8) {
                         const int f = f0 + j;
                         if (f >= p.F || row >= p.M) continue;
                         if (p.bg) {
-                            float t[8];
-                            load8<T>(static_cast<const T*>(p.bg) + f, t);
+                            float b[8];
+                            load8<T>(static_cast<const T*>(p.bg) + f, b);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) g[j + i] += t[i];
+                            for (int i = 0; i < 8; ++i) g[j + i] += b[i];
                         }
                         if (p.bu) {
-                            float t[8];
-                            load8<T>(static_cast<const T*>(p.bu) + f, t);
+                            float b[8];
+                            load8<T>(static_cast<const T*>(p.bu) + f, b);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) v[j + i] += t[i];
+                            for (int i = 0; i < 8; ++i) v[j + i] += b[i];
                         }
                         const size_t at = (size_t)row * p.F + f;
-                        if constexpr (MODE == kForward) {
+                        float dh[8];
+                        if (MODE == kGrad) load8<T>(static_cast<const T*>(p.dh) + at, dh);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) v[j + i] *= activate<T, false>(p.act, g[j + i]).a;
+                        for (int i = j; i < j + 8; i += 2) {
+                            float2 a, da;
+                            activate<T, MODE == kGrad>(p.act, make_float2(g[i], g[i + 1]), a, da);
+                            if (MODE == kForward) {
+                                v[i] *= a.x; v[i + 1] *= a.y;
+                            } else {
+                                g[i] = dh[i - j] * v[i] * da.x; g[i + 1] = dh[i + 1 - j] * v[i + 1] * da.y;
+                                v[i] = dh[i - j] * a.x; v[i + 1] = dh[i + 1 - j] * a.y;
+                            }
+                        }
+                        if constexpr (MODE == kForward) {
                             store8<T>(static_cast<T*>(p.out0) + at, v + j);
                         } else {
-                            float t[8];
-                            load8<T>(static_cast<const T*>(p.dh) + at, t);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const Activated r = activate<T, true>(p.act, g[j + i]);
-                                g[j + i] = t[i] * v[j + i] * r.da;
-                                v[j + i] = t[i] * r.a;
-                            }
                             store_operand8<T>(p.out0, plane, at, g + j);
                             store_operand8<T>(p.out1, plane, at, v + j);
                         }
                     }
                 }
-            } else {
-                const int op = MODE == kWeight && mt >= tiles_f, limit = MODE == kWeight ? p.F : p.M;
-                const int row = 128 * (mt - op * tiles_f) + 32 * q + lane;
-                const int blocks = (p.n + 31) / 32;
-                for (int b = half; b < blocks; b += 2) {
+                __syncwarp();
+            }
+        } else {
+            // boxes of 32 columns and 32 rows, those of a tile in turn by the two warps that share its rows
+            int box = 0;
+            for (int u = run.at; u < run.end; u += run.step, ++ord) {
+                const Unit t = unit_of<MODE>(p, u);
+                const int buf = ord & 1, blocks = p.n / 32;
+                const int row0 = MODE == kInput ? 256 * t.mt + 128 * rank + 32 * q : 128 * t.mt + 32 * q, limit = MODE == kInput ? p.M : p.F;
+                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
+                const int z = p.splits == 1 ? 0 : MODE == kInput ? t.split : 2 * t.split + (int)rank;
+                const CUtensorMap* map = MODE == kWeight && p.splits == 1 ? &p.s[rank] : &p.s[0];
+                wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
+                tc_fence_after_sync();
+#pragma unroll 1
+                for (int b = half; b < blocks; b += 2, ++box) {
                     float v[32];
                     __syncwarp();
                     tmem_ld32(acc + 32 * b, reinterpret_cast<uint32_t(&)[32]>(v));
                     tmem_ld_wait();
-                    if (b + 2 >= blocks) release();
+                    if (b + 2 >= blocks) release(buf);
+                    uint32_t src = patch;
+                    if (p.wide) {                                      // rows of 128 bytes, one patch
+                        if (lane == 0) store_wait_read<0>();
+                        __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        const int in_tile = 32 * b + j, c = p.n * nt + in_tile;
-                        if (in_tile >= p.n || c >= p.C || row >= limit) continue;
-                        if (p.splits > 1) store8<float>(p.part + ((size_t)split * (MODE == kWeight ? 2 * (size_t)p.F : (size_t)p.M) + (size_t)op * p.F + row) * p.C + c, v + j);
-                        else store8<T>(static_cast<T*>(op ? p.out1 : p.out0) + (size_t)row * p.C + c, v + j);
+                        for (int c = 0; c < 8; ++c) st_shared4(patch + 128 * lane + ((c ^ (lane & 7)) << 4), pack16<float>(v + 4 * c));
+                    } else if constexpr (sizeof(T) == 2) {             // rows of 64 bytes, two patches in turn
+                        src += 2048 * (box & 1);
+                        if (lane == 0) store_wait_read<1>();
+                        __syncwarp();
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) st_shared4(src + 64 * lane + ((c ^ ((lane >> 1) & 3)) << 4), pack16<T>(v + 8 * c));
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    const int c0 = p.n * t.nt + 32 * b;
+                    if (lane == 0) {
+                        if (row0 < limit && c0 < p.C) tma_store_3d(map, c0, row0, z, src);
+                        store_commit();
                     }
                 }
-                if (half >= blocks) release();
+                if (half >= blocks) release(buf);
             }
+            if (lane == 0) store_wait_read<0>();
             __syncwarp();
         }
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 0) tmem_dealloc<512>(pp.tmem);
+    if (PAIR) {
+        cluster_sync();                                               // the other block's instructions read this one's memory
+        if (warp == 0) tmem_dealloc_pair<512>(pp.tmem);
+    } else if (warp == 0) {
+        tmem_dealloc<512>(pp.tmem);
+    }
 }
 
 // fp32 -> three planes of bf16 terms, eight elements a thread
@@ -371,23 +663,59 @@ template <typename T> __global__ void __launch_bounds__(256) gated_column_kernel
     }
 }
 
-// Work of the two products with a long sum: tiles of at most 256 columns, split while tiles are fewer than SMs
+// Shares of the column sums that kGrad left (gated_kernel's order of units), in that order
+template <typename T> __global__ void __launch_bounds__(256) gated_column_sum_kernel(const float* part, int F, int tiles_m, int units, int count, T* out0, T* out1) {
+    pdl_wait_prior();
+    pdl_release_next();
+    const int lane = threadIdx.x & 31, i = (blockIdx.x * 8 + (threadIdx.x >> 5)) * 8 + (lane & 7);          // a warp: eight columns, four shares at a time
+    if ((i & ~7) >= 2 * F) return;
+    const int op = i >= F, f = i - op * F, nt = f / 128;
+    const int first = (int)((((long long)nt * tiles_m + 1) * count - 1) / units), last = (int)((((long long)(nt + 1) * tiles_m) * count - 1) / units);
+    float v = 0.f;
+    for (int s = lane >> 3; s < 8 * (last - first + 1); s += 4) v += part[(size_t)s * 2 * F + i];
+    v += __shfl_xor_sync(0xffffffffu, v, 8);
+    v += __shfl_xor_sync(0xffffffffu, v, 16);
+    if (lane < 8) (op ? out1 : out0)[f] = Elem<T>::from_f32(v);
+}
+
+// Work of the two products with a long sum: tiles of at most 256 columns, split while pairs of SMs are left without one
 struct GatedSplit { int tiles_m, tiles_n, n, chunks, splits; };
 GatedSplit plan_split(int tiles_m, int chunks, int C, int sm_count) {
     GatedSplit s;
     s.tiles_m = tiles_m;
     s.tiles_n = (C + 255) / 256;
-    s.n = ((C + s.tiles_n - 1) / s.tiles_n + 15) / 16 * 16;
+    s.n = ((C + s.tiles_n - 1) / s.tiles_n + 31) / 32 * 32;
     s.chunks = chunks;
-    const long long tiles = (long long)tiles_m * s.tiles_n;
-    s.splits = 1;
-    if (tiles < sm_count) s.splits = (int)(sm_count / tiles);
+    const long long tiles = (long long)tiles_m * s.tiles_n, pairs = sm_count / 2;
+    s.splits = tiles < pairs ? (int)(pairs / tiles) : 1;
     if (s.splits > chunks / 4) s.splits = chunks / 4;
     if (s.splits < 1) s.splits = 1;
     return s;
 }
-GatedSplit plan_input(int M, int C, int F, int sm_count) { return plan_split((M + 127) / 128, 2 * ((F + 63) / 64), C, sm_count); }
-GatedSplit plan_weight(int M, int C, int F, int sm_count) { return plan_split(2 * ((F + 127) / 128), (M + 63) / 64, C, sm_count); }
+GatedSplit plan_input(int M, int C, int F, int sm_count) { return plan_split((M + 255) / 256, 2 * ((F + 63) / 64), C, sm_count); }
+GatedSplit plan_weight(int M, int C, int F, int sm_count) { return plan_split((F + 127) / 128, (M + 63) / 64, C, sm_count); }
+
+// G and U: 128 hidden units a tile of 256 rows for a pair of blocks; where that leaves SMs without work, tiles of 128 rows and fewer units
+struct GatedTiles { int bn, tiles_m, tiles_n, blocks; };
+GatedTiles plan_tiles(int M, int F, int sm_count) {
+    GatedTiles t;
+    t.bn = 128;
+    t.tiles_m = (M + 255) / 256;
+    t.tiles_n = (F + 127) / 128;
+    const long long pairs = (long long)t.tiles_m * t.tiles_n;
+    if (4 * pairs <= sm_count) {
+        t.bn = (long long)((M + 127) / 128) * ((F + 63) / 64) * 2 <= sm_count ? 32 : 64;
+        t.tiles_m = (M + 127) / 128;
+        t.tiles_n = (F + t.bn - 1) / t.bn;
+    }
+    const long long units = (long long)t.tiles_m * t.tiles_n, most = t.bn == 128 ? sm_count / 2 : sm_count;
+    t.blocks = (int)(units < most ? units : most) * (t.bn == 128 ? 2 : 1);
+    return t;
+}
+int column_slots(const GatedTiles& t) {
+    const int pairs = t.blocks / 2, runs = (pairs + t.tiles_n - 1) / t.tiles_n + 1;
+    return 8 * (runs < t.tiles_m ? runs : t.tiles_m);
+}
 
 // Workspace: terms of X, Wg, Wu (fp32) | dG | dU | shares of dX, dW, of the column sums
 struct GatedWs { size_t x, wg, wu, dg, du, dx, dw, db, total; };
@@ -405,25 +733,58 @@ GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count
         w.dg = take(planes);
         w.du = take(planes);
         const GatedSplit in = plan_input(M, C, F, sm_count), we = plan_weight(M, C, F, sm_count);
+        const GatedTiles t = plan_tiles(M, F, sm_count);
         w.dx = take(in.splits > 1 ? (size_t)in.splits * M * C * 4 : 0);
         w.dw = take(we.splits > 1 ? (size_t)we.splits * 2 * F * C * 4 : 0);
-        w.db = take((size_t)((M + kColRows - 1) / kColRows) * 2 * F * 4);
+        const size_t slots = dtype != kF32 && t.bn == 128 ? column_slots(t) : (M + kColRows - 1) / kColRows;
+        w.db = take(slots * 2 * F * 4);
     }
     w.total = at;
     return w;
 }
 
-template <typename T, GatedMode MODE, int BN> cudaError_t launch_mode(const GatedArgs& a, int sm_count, cudaStream_t st) {
+// Map of [z][rows][cols] elements of `unit` bytes (rows a multiple of 16 bytes); the swizzle spans a row of the box
+bool make_box_map(CUtensorMap* out, const void* base, int unit, uint64_t zs, uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {cols, rows, zs};
+    const cuuint64_t strides[2] = {unit * cols, rows * unit * cols};
+    const cuuint32_t box[3] = {box_cols, box_rows, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(out, unit == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols * unit == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, GatedMode MODE, int BN> cudaError_t launch_mode(const GatedArgs& a, int blocks, cudaStream_t st) {
+    using S = GatedShape<T, MODE, BN>;
+    static_assert(S::kSmem <= 232448, "shared memory");
     static std::atomic<unsigned long long> done{0};
-    const cudaError_t e = allow_smem(gated_kernel<T, MODE, BN>, done, GatedShape<MODE, BN>::kSmem);
+    const cudaError_t e = allow_smem(gated_kernel<T, MODE, BN>, done, S::kSmem);
     if (e != cudaSuccess) return e;
-    const long long units = (long long)a.tiles_m * a.tiles_n * a.splits;
-    return launch_dependent(gated_kernel<T, MODE, BN>, dim3((unsigned)(units < sm_count ? units : sm_count)), kThreads, GatedShape<MODE, BN>::kSmem, st, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 2; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = S::kPair ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, gated_kernel<T, MODE, BN>, a);
+}
+template <typename T, GatedMode MODE> cudaError_t launch_projections(const GatedArgs& a, const GatedTiles& t, cudaStream_t st) {
+    if (t.bn == 128) return launch_mode<T, MODE, 128>(a, t.blocks, st);
+    return t.bn == 64 ? launch_mode<T, MODE, 64>(a, t.blocks, st) : launch_mode<T, MODE, 32>(a, t.blocks, st);
 }
 
 template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st, int* launches) {
     constexpr int kTerms = GatedTerms<T>::kTerms;
-    const GatedWs w = gated_layout(sizeof(T) == 4 ? kF32 : kBF16, c.M, c.C, c.F, c.dh != nullptr, c.sm_count);
+    constexpr bool kWide = sizeof(T) == 4;
+    const GatedWs w = gated_layout(kWide ? kF32 : kBF16, c.M, c.C, c.F, c.dh != nullptr, c.sm_count);
     char* ws = static_cast<char*>(c.ws);
     const void *x = c.x, *wg = c.wg, *wu = c.wu;
     cudaError_t e;
@@ -441,51 +802,64 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     a.M = c.M; a.C = c.C; a.F = c.F; a.act = c.act;
     a.bg = c.bg; a.bu = c.bu; a.dh = c.dh;
     a.status = c.status;
-    // G and U.  Narrower tiles where 128 columns leave SMs without a tile.
-    const int tm = (c.M + 127) / 128;
-    int bn = 128;
-    while (bn > 32 && (long long)tm * ((c.F + bn - 1) / bn) * 2 <= c.sm_count) bn /= 2;
-    a.tiles_m = tm; a.tiles_n = (c.F + bn - 1) / bn; a.splits = 1; a.chunks = (c.C + 63) / 64;
+    const GatedTiles t = plan_tiles(c.M, c.F, c.sm_count);
+    a.tiles_m = t.tiles_m; a.tiles_n = t.tiles_n; a.splits = 1; a.chunks = (c.C + 63) / 64;
     a.out0 = c.dh ? ws + w.dg : static_cast<char*>(c.h);
     a.out1 = ws + w.du;
-    if (!make_map_3d_u16(&a.a[0], x, kTerms, c.M, c.C, 128) || !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, bn) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, bn)) return cudaErrorInvalidValue;
-    if (c.dh) e = bn == 128 ? launch_mode<T, kGrad, 128>(a, c.sm_count, st) : bn == 64 ? launch_mode<T, kGrad, 64>(a, c.sm_count, st) : launch_mode<T, kGrad, 32>(a, c.sm_count, st);
-    else e = bn == 128 ? launch_mode<T, kForward, 128>(a, c.sm_count, st) : bn == 64 ? launch_mode<T, kForward, 64>(a, c.sm_count, st) : launch_mode<T, kForward, 32>(a, c.sm_count, st);
+    const bool fused_columns = c.dbg && !kWide && t.bn == 128;
+    a.column = fused_columns ? reinterpret_cast<float*>(ws + w.db) : nullptr;
+    if (!make_map_3d_u16(&a.a[0], x, kTerms, c.M, c.C, 128) || !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, t.bn) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, t.bn)) return cudaErrorInvalidValue;
+    if (!kWide && t.bn == 128) {
+        const uint32_t cols = c.dh ? 32 : 64;
+        if (!make_box_map(&a.s[0], a.out0, 2, 1, c.M, c.F, cols, 32)) return cudaErrorInvalidValue;
+        if (c.dh && (!make_box_map(&a.s[1], a.out1, 2, 1, c.M, c.F, cols, 32) || !make_box_map(&a.g, c.dh, 2, 1, c.M, c.F, cols, 32))) return cudaErrorInvalidValue;
+    }
+    e = c.dh ? launch_projections<T, kGrad>(a, t, st) : launch_projections<T, kForward>(a, t, st);
     if (e != cudaSuccess) return e;
     ++*launches;
     if (!c.dh) return cudaSuccess;
 
     const void *dg = ws + w.dg, *du = ws + w.du;
+    const int pairs = c.sm_count / 2;
     auto sum = [&](const float* part, int splits, size_t n, size_t first, void* out0, void* out1) {
         ++*launches;
         return launch_dependent(gated_sum_kernel<T>, dim3((unsigned)((n + 1023) / 1024)), 256, 0, st, part, splits, n, first, static_cast<T*>(out0), static_cast<T*>(out1));
     };
+    auto product = [&](const GatedSplit& s) {
+        a.tiles_m = s.tiles_m; a.tiles_n = s.tiles_n; a.n = s.n; a.splits = s.splits; a.chunks = s.chunks;
+        a.wide = kWide || s.splits > 1;
+        const long long units = (long long)s.tiles_m * s.tiles_n * s.splits;
+        return 2 * (int)(units < pairs ? units : pairs);
+    };
     if (c.dx) {
         const GatedSplit s = plan_input(c.M, c.C, c.F, c.sm_count);
-        a.tiles_m = s.tiles_m; a.tiles_n = s.tiles_n; a.n = s.n; a.splits = s.splits; a.chunks = s.chunks;
-        a.out0 = c.dx;
-        a.part = reinterpret_cast<float*>(ws + w.dx);
+        const int blocks = product(s);
+        float* part = reinterpret_cast<float*>(ws + w.dx);
         if (!make_map_3d_u16(&a.a[0], dg, kTerms, c.M, c.F, 128) || !make_map_3d_u16(&a.a[1], du, kTerms, c.M, c.F, 128) ||
-            !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, 64) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, 64)) return cudaErrorInvalidValue;
-        if ((e = launch_mode<T, kInput, 128>(a, c.sm_count, st)) != cudaSuccess) return e;
+            !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, 64) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, 64) ||
+            !make_box_map(&a.s[0], s.splits > 1 ? part : c.dx, a.wide ? 4 : 2, s.splits, c.M, c.C, 32, 32)) return cudaErrorInvalidValue;
+        if ((e = launch_mode<T, kInput, 128>(a, blocks, st)) != cudaSuccess) return e;
         ++*launches;
-        if (s.splits > 1 && (e = sum(a.part, s.splits, (size_t)c.M * c.C, (size_t)c.M * c.C, c.dx, nullptr)) != cudaSuccess) return e;
+        if (s.splits > 1 && (e = sum(part, s.splits, (size_t)c.M * c.C, (size_t)c.M * c.C, c.dx, nullptr)) != cudaSuccess) return e;
     }
     if (c.dwg) {
         const GatedSplit s = plan_weight(c.M, c.C, c.F, c.sm_count);
-        a.tiles_m = s.tiles_m; a.tiles_n = s.tiles_n; a.n = s.n; a.splits = s.splits; a.chunks = s.chunks;
-        a.out0 = c.dwg; a.out1 = c.dwu;
-        a.part = reinterpret_cast<float*>(ws + w.dw);
-        if (!make_map_3d_u16(&a.a[0], dg, kTerms, c.M, c.F, 64) || !make_map_3d_u16(&a.a[1], du, kTerms, c.M, c.F, 64) || !make_map_3d_u16(&a.b[0], x, kTerms, c.M, c.C, 64)) return cudaErrorInvalidValue;
-        if ((e = launch_mode<T, kWeight, 128>(a, c.sm_count, st)) != cudaSuccess) return e;
+        const int blocks = product(s);
+        float* part = reinterpret_cast<float*>(ws + w.dw);
+        if (!make_map_3d_u16(&a.a[0], dg, kTerms, c.M, c.F, 64) || !make_map_3d_u16(&a.a[1], du, kTerms, c.M, c.F, 64) || !make_map_3d_u16(&a.b[0], x, kTerms, c.M, c.C, 64) ||
+            !make_box_map(&a.s[0], s.splits > 1 ? part : c.dwg, a.wide ? 4 : 2, s.splits > 1 ? 2 * s.splits : 1, c.F, c.C, 32, 32) ||
+            (s.splits == 1 && !make_box_map(&a.s[1], c.dwu, a.wide ? 4 : 2, 1, c.F, c.C, 32, 32))) return cudaErrorInvalidValue;
+        if ((e = launch_mode<T, kWeight, 128>(a, blocks, st)) != cudaSuccess) return e;
         ++*launches;
-        if (s.splits > 1 && (e = sum(a.part, s.splits, 2 * (size_t)c.F * c.C, (size_t)c.F * c.C, c.dwg, c.dwu)) != cudaSuccess) return e;
+        if (s.splits > 1 && (e = sum(part, s.splits, 2 * (size_t)c.F * c.C, (size_t)c.F * c.C, c.dwg, c.dwu)) != cudaSuccess) return e;
     }
     if (c.dbg) {
-        const int runs = (c.M + kColRows - 1) / kColRows;
         float* part = reinterpret_cast<float*>(ws + w.db);
-        if ((e = launch_dependent(gated_column_kernel<T>, dim3((c.F + 63) / 64, 2, runs), 256, 0, st, dg, du, c.M, c.F, part)) != cudaSuccess) return e;
         ++*launches;
+        if (fused_columns)
+            return launch_dependent(gated_column_sum_kernel<T>, dim3((2 * c.F + 63) / 64), 256, 0, st, part, c.F, t.tiles_m, t.tiles_m * t.tiles_n, t.blocks / 2, static_cast<T*>(c.dbg), static_cast<T*>(c.dbu));
+        const int runs = (c.M + kColRows - 1) / kColRows;
+        if ((e = launch_dependent(gated_column_kernel<T>, dim3((c.F + 63) / 64, 2, runs), 256, 0, st, dg, du, c.M, c.F, part)) != cudaSuccess) return e;
         if ((e = sum(part, runs, 2 * (size_t)c.F, c.F, c.dbg, c.dbu)) != cudaSuccess) return e;
     }
     return cudaSuccess;
