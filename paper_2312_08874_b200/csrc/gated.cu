@@ -16,17 +16,19 @@
 #include "pair.cuh"
 #include "stream_common.cuh"
 
+#include <type_traits>
+
 namespace aa {
 
 namespace {
 
 enum GatedMode { kForward, kGrad, kInput, kWeight };
-constexpr int kEpiWarps = 8, kThreads = 32 * (kEpiWarps + 2);
+constexpr int kEpiWarps = 16, kThreads = 32 * (kEpiWarps + 2);
 constexpr int kATile = 128 * 128;                      // bytes of a [128][64] (or [64][128]) tile of 16-bit elements
-constexpr int kPatch = 4096;                           // bytes of a warp's staged box
+constexpr int kHalfPatch = 2048;                       // bytes of a warp's staged box of 32 x 32 16-bit values (fp32: two)
 constexpr int kTimeoutTile = 3, kTimeoutRole = 6;
-// mbarriers: full [kRing], empty [kRing], accumulator ready [2], accumulator read [2], drain, dH [warps][2 halves]
-constexpr int kRing = 6, BAR_FULL = 0, BAR_EMPTY = kRing, BAR_ACC = 2 * kRing, BAR_READ = BAR_ACC + 2, BAR_DRAIN = BAR_READ + 2, BAR_DH = BAR_DRAIN + 1, kBars = BAR_DH + 2 * kEpiWarps;
+// mbarriers: full [kRing], empty [kRing], accumulator ready [2], accumulator read [2], drain, dH [warps]
+constexpr int kRing = 6, BAR_FULL = 0, BAR_EMPTY = kRing, BAR_ACC = 2 * kRing, BAR_READ = BAR_ACC + 2, BAR_DRAIN = BAR_READ + 2, BAR_DH = BAR_DRAIN + 1, kBars = BAR_DH + kEpiWarps;
 static_assert(kBars * 8 <= 1024, "barriers");
 
 struct GatedArgs {
@@ -63,7 +65,7 @@ __device__ __forceinline__ float fast_rcp(float x) {
     return y;
 }
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-template <typename T, bool GRAD> __device__ __forceinline__ void activate(int act, float2 g, float2& a, float2& da) {
+template <typename T, int ACT, bool GRAD> __device__ __forceinline__ void activate(float2 g, float2& a, float2& da) {
     da = both(0.f);
     if constexpr (sizeof(T) == 4) {                                    // fp32 accuracy
         const float gs[2] = {g.x, g.y};
@@ -71,20 +73,20 @@ template <typename T, bool GRAD> __device__ __forceinline__ void activate(int ac
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const float x = gs[i];
-            if (act == 1) {
+            if (ACT == 1) {
                 const float cdf = 0.5f + 0.5f * erff(x * 0.70710678f);
                 r[i] = x * cdf;
                 if (GRAD) d[i] = fmaf(x * 0.39894228f, expf(-0.5f * x * x), cdf);
             } else {
                 const float x2 = fminf(x * x, 1e4f);                   // (far past where the sigmoid is 0 or 1: no infinity meets a zero)
-                const float s = 1.f / (1.f + expf(act == 2 ? -kTanh2 * x * fmaf(kTanhC, x2, 1.f) : -x));
+                const float s = 1.f / (1.f + expf(ACT == 2 ? -kTanh2 * x * fmaf(kTanhC, x2, 1.f) : -x));
                 r[i] = x * s;
-                if (GRAD) d[i] = fmaf(x * (1.f - s), act == 2 ? s * kTanh2 * fmaf(3.f * kTanhC, x2, 1.f) : s, s);
+                if (GRAD) d[i] = fmaf(x * (1.f - s), ACT == 2 ? s * kTanh2 * fmaf(3.f * kTanhC, x2, 1.f) : s, s);
             }
         }
         a = make_float2(r[0], r[1]);
         da = make_float2(d[0], d[1]);
-    } else if (act == 1) {
+    } else if constexpr (ACT == 1) {
         // Upper tail Q(x) = exp(-x^2 / 2) R(x), x = |g|, with R (half of a scaled complementary error function, smooth from 1/2 down) as a
         // polynomial on [0, 5], fitted with weight exp(-x^2 / 2): Q is within 3e-7 (a 16-bit result of size 1e-3 ends at 2e-6).  One
         // special-function instruction, which the derivative shares; the fast error function of the library takes 3.4 times the epilogue's time.
@@ -107,7 +109,7 @@ template <typename T, bool GRAD> __device__ __forceinline__ void activate(int ac
         if (GRAD) da = ffma2(fmul2(g, both(0.39894228f)), e, cdf);
     } else {
         float2 z = fmul2(g, both(-kLog2e)), slope = both(1.f);
-        if (act == 2) {
+        if (ACT == 2) {
             const float2 q = fmul2(g, g), g2 = make_float2(fminf(q.x, 1e4f), fminf(q.y, 1e4f));
             z = fmul2(fmul2(g, both(-kLog2e * kTanh2)), ffma2(g2, both(kTanhC), both(1.f)));
             if (GRAD) slope = ffma2(g2, both(3.f * kTanhC * kTanh2), both(kTanh2));
@@ -116,6 +118,12 @@ template <typename T, bool GRAD> __device__ __forceinline__ void activate(int ac
         a = fmul2(g, s);
         if (GRAD) da = ffma2(fmul2(a, slope), ffma2(s, both(-1.f), both(1.f)), s);
     }
+}
+// f(constant of the activation): the choice is made once a tile, not once a value
+template <typename F> __device__ __forceinline__ void by_activation(int act, F f) {
+    if (act == 1) f(std::integral_constant<int, 1>());
+    else if (act == 2) f(std::integral_constant<int, 2>());
+    else f(std::integral_constant<int, 0>());
 }
 
 // eight consecutive elements
@@ -165,10 +173,10 @@ template <typename T, GatedMode MODE, int BN> struct GatedShape {
     static constexpr bool kPair = BN == 128, kStaged = MODE >= kInput || (kPair && sizeof(T) == 2);
     static constexpr int kBTile = kPair ? kATile : 2 * BN * 128;
     static constexpr int kStage = kATile + kBTile;
-    static constexpr int kPatches = !kStaged ? 0 : MODE == kGrad ? 2 : 1;          // of a warp
-    static constexpr int kStages = MODE == kForward ? 5 : MODE == kGrad ? 4 : 6;
-    static constexpr int kOffPatch = 1024 + kStages * kStage, kOffBias = kOffPatch + kPatches * kEpiWarps * kPatch;
-    static constexpr int kSmem = kOffBias + (MODE <= kGrad && kStaged ? kEpiWarps * 512 : 0) + 1024;
+    static constexpr int kPatch = !kStaged ? 0 : MODE == kForward ? kHalfPatch : 2 * kHalfPatch;       // of a warp
+    static constexpr int kStages = MODE == kGrad ? 4 : 5;
+    static constexpr int kOffPatch = 1024 + kStages * kStage, kOffBias = kOffPatch + kEpiWarps * kPatch;
+    static constexpr int kSmem = kOffBias + (MODE <= kGrad && kStaged ? kEpiWarps * 256 : 0) + 1024;
 };
 
 // Units of work of block (or pair) `who` of `count`: kForward and kGrad a run in the order of the rows, so that a run has few column ranges
@@ -334,8 +342,9 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
         __syncwarp();
     } else {
         // ------------------------------------------------------------------ epilogue
-        const int q = warp & 3, half = warp >> 2;
-        const uint32_t patch = base + S::kOffPatch + warp * S::kPatches * kPatch;
+        // warp: 32 rows, and a quarter of a tile's hidden units (kForward, kGrad) or every fourth block of 32 columns
+        const int q = warp & 3, quarter = warp >> 2;
+        const uint32_t patch = base + S::kOffPatch + warp * S::kPatch;
         const uint32_t read0 = PAIR ? in_block(pipe_bar(pp, BAR_READ), 0) : pipe_bar(pp, BAR_READ);
         int ord = 0;
         auto release = [&](int buf) {
@@ -344,152 +353,139 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             else pipe_arrive_warp(pp, BAR_READ + buf, lane);
         };
         if constexpr (MODE <= kGrad && S::kStaged) {
-            // Warp: 32 rows, 64 hidden units in two halves of 32.  kGrad: dH arrives by TMA in the place that dG leaves from, a half ahead.
-            const uint32_t bias = base + S::kOffBias + warp * 512;
-            const uint32_t swz = (lane >> 1) & 3;                      // of rows of 64 bytes
-            float2 column[2][2] = {};                                  // [half][dG, dU]: sums of two columns over this run's rows
+            // Results leave through a patch of 32 rows of 64 bytes with their swizzle.  kGrad: dH arrives in the place that dG leaves from.
+            const uint32_t bias = base + S::kOffBias + warp * 256, row_at = patch + 64 * lane, swz = (lane >> 1) & 3;
+            float2 column[2] = {};                                     // dG, dU: sums of two columns over this run's rows
             int column_nt = -1;
             auto flush = [&] {                                         // lanes l and l + 16 have even and odd rows of the same columns
-                const int first = (int)(((long long)column_nt * p.tiles_m + 1) * count - 1) / units;
+                const int first = (int)((((long long)column_nt * p.tiles_m + 1) * count - 1) / units);
                 float* dst = p.column + (size_t)(8 * (who - first) + 4 * rank + q) * 2 * p.F;
+                const int f = BN * column_nt + 32 * quarter + 2 * (lane & 15);
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int o = 0; o < 2; ++o) {
-                        float2 v = column[h][o];
-                        v.x += __shfl_xor_sync(0xffffffffu, v.x, 16);
-                        v.y += __shfl_xor_sync(0xffffffffu, v.y, 16);
-                        const int f = BN * column_nt + 64 * half + 32 * h + 2 * (lane & 15);
-                        if (lane < 16 && f < p.F) *reinterpret_cast<float2*>(dst + (size_t)o * p.F + f) = v;
-                        column[h][o] = both(0.f);
-                    }
+                for (int o = 0; o < 2; ++o) {
+                    float2 v = column[o];
+                    v.x += __shfl_xor_sync(0xffffffffu, v.x, 16);
+                    v.y += __shfl_xor_sync(0xffffffffu, v.y, 16);
+                    if (lane < 16 && f < p.F) *reinterpret_cast<float2*>(dst + (size_t)o * p.F + f) = v;
+                    column[o] = both(0.f);
+                }
             };
-            auto fetch = [&](int u, int h) {                           // one lane: dH of a half
+            auto fetch = [&](int u) {                                  // one lane: dH of a unit
                 const Unit t = unit_of<MODE>(p, u);
-                const uint32_t bar = pipe_bar(pp, BAR_DH + 2 * warp + h);
-                mbar_arrive_expect_tx(bar, 2048);
-                tma_load_3d(patch + 2048 * h, &p.g, BN * t.nt + 64 * half + 32 * h, 256 * t.mt + 128 * rank + 32 * q, 0, bar);
+                const uint32_t bar = pipe_bar(pp, BAR_DH + warp);
+                mbar_arrive_expect_tx(bar, kHalfPatch);
+                tma_load_3d(patch, &p.g, BN * t.nt + 32 * quarter, 256 * t.mt + 128 * rank + 32 * q, 0, bar);
             };
-            if (MODE == kGrad && lane == 0 && run.at < run.end) { fetch(run.at, 0); fetch(run.at, 1); }
+            if (MODE == kGrad && lane == 0 && run.at < run.end) fetch(run.at);
             const bool biased = p.bg || p.bu;
             for (int u = run.at; u < run.end; u += run.step, ++ord) {
                 const Unit t = unit_of<MODE>(p, u);
-                const int buf = ord & 1, row0 = 256 * t.mt + 128 * rank + 32 * q, f0 = BN * t.nt + 64 * half;
-                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16) + 64 * half;
+                const int buf = ord & 1, row0 = 256 * t.mt + 128 * rank + 32 * q, f0 = BN * t.nt + 32 * quarter;
+                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16) + 32 * quarter;
                 if (MODE == kGrad && p.column && column_nt != t.nt) {
                     if (column_nt >= 0) flush();
                     column_nt = t.nt;
                 }
-                if (biased) {                                          // as fp32, two a lane: [gate | up][64]
-                    const int f = f0 + 2 * lane;
-                    float2 bg = both(0.f), bu = bg;
-                    if (p.bg && f < p.F) bg = unpack2<T>(__ldg(reinterpret_cast<const uint32_t*>(static_cast<const T*>(p.bg) + f)));
-                    if (p.bu && f < p.F) bu = unpack2<T>(__ldg(reinterpret_cast<const uint32_t*>(static_cast<const T*>(p.bu) + f)));
+                if (biased) {                                          // as fp32: [gate | up][32]
+                    const int f = f0 + 2 * (lane & 15);
+                    const void* src = lane < 16 ? p.bg : p.bu;
+                    float2 b = both(0.f);
+                    if (src && f < p.F) b = unpack2<T>(__ldg(reinterpret_cast<const uint32_t*>(static_cast<const T*>(src) + f)));
                     __syncwarp();
-                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};\n" ::"r"(bias + 8 * lane), "f"(bg.x), "f"(bg.y) : "memory");
-                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};\n" ::"r"(bias + 256 + 8 * lane), "f"(bu.x), "f"(bu.y) : "memory");
+                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};\n" ::"r"(bias + 8 * lane), "f"(b.x), "f"(b.y) : "memory");
                     __syncwarp();
                 }
                 wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
                 tc_fence_after_sync();
+                if (MODE == kForward && lane == 0) store_wait_read<0>();            // the tile before has left the patch
+                if (MODE == kGrad) wait_par(pp, BAR_DH + warp, ord, kTimeoutTile);
+                by_activation(p.act, [&](auto act) {
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    float g[32], v[32];
-                    __syncwarp();
-                    tmem_ld32(acc + 32 * h, reinterpret_cast<uint32_t(&)[32]>(g));
-                    tmem_ld32(acc + BN + 32 * h, reinterpret_cast<uint32_t(&)[32]>(v));
-                    if (MODE == kGrad) wait_par(pp, BAR_DH + 2 * warp + h, ord, kTimeoutTile);
-                    else if (h == 0) {                                 // the tile before has left its patch
-                        if (lane == 0) store_wait_read<0>();
+                    for (int h = 0; h < 2; ++h) {                      // 16 hidden units
+                        float g[16], v[16];
                         __syncwarp();
-                    }
-                    tmem_ld_wait();
-                    if (h == 1) release(buf);
+                        tmem_ld16(acc + 16 * h, g);
+                        tmem_ld16(acc + BN + 16 * h, v);
+                        tmem_ld_wait();
+                        if (h == 1) release(buf);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {                      // pieces of eight hidden units
-                        float2 gg[4], vv[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            gg[i] = make_float2(g[8 * c + 2 * i], g[8 * c + 2 * i + 1]);
-                            vv[i] = make_float2(v[8 * c + 2 * i], v[8 * c + 2 * i + 1]);
-                        }
-                        if (biased) {
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const uint4 x = ld_shared4(bias + 128 * h + 32 * c + 16 * i), y = ld_shared4(bias + 256 + 128 * h + 32 * c + 16 * i);
-                                gg[2 * i] = fadd2(gg[2 * i], make_float2(__uint_as_float(x.x), __uint_as_float(x.y)));
-                                gg[2 * i + 1] = fadd2(gg[2 * i + 1], make_float2(__uint_as_float(x.z), __uint_as_float(x.w)));
-                                vv[2 * i] = fadd2(vv[2 * i], make_float2(__uint_as_float(y.x), __uint_as_float(y.y)));
-                                vv[2 * i + 1] = fadd2(vv[2 * i + 1], make_float2(__uint_as_float(y.z), __uint_as_float(y.w)));
-                            }
-                        }
-                        uint32_t o0[4], o1[4];
-                        if constexpr (MODE == kForward) {
+                        for (int c = 0; c < 2; ++c) {                  // pieces of eight
+                            float2 gg[4], vv[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                float2 a, da;
-                                activate<T, false>(p.act, gg[i], a, da);
-                                a = fmul2(a, vv[i]);
-                                o0[i] = pack2<T>(a.x, a.y);
+                                gg[i] = make_float2(g[8 * c + 2 * i], g[8 * c + 2 * i + 1]);
+                                vv[i] = make_float2(v[8 * c + 2 * i], v[8 * c + 2 * i + 1]);
                             }
-                            st_shared4(patch + 128 * lane + (((4 * h + c) ^ (lane & 7)) << 4), make_uint4(o0[0], o0[1], o0[2], o0[3]));
-                        } else {
-                            const uint32_t at = patch + 2048 * h + 64 * lane + ((c ^ swz) << 4);
-                            const uint4 d = ld_shared4(at);
-                            const uint32_t dd[4] = {d.x, d.y, d.z, d.w};
+                            if (biased) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                float2 a, da;
-                                activate<T, true>(p.act, gg[i], a, da);
-                                const float2 dh = unpack2<T>(dd[i]);
-                                da = fmul2(fmul2(dh, vv[i]), da);
-                                a = fmul2(dh, a);
-                                o0[i] = pack2<T>(da.x, da.y);
-                                o1[i] = pack2<T>(a.x, a.y);
+                                for (int i = 0; i < 2; ++i) {
+                                    const uint32_t at = bias + 64 * h + 32 * c + 16 * i;
+                                    const uint4 x = ld_shared4(at), y = ld_shared4(at + 128);
+                                    gg[2 * i] = fadd2(gg[2 * i], make_float2(__uint_as_float(x.x), __uint_as_float(x.y)));
+                                    gg[2 * i + 1] = fadd2(gg[2 * i + 1], make_float2(__uint_as_float(x.z), __uint_as_float(x.w)));
+                                    vv[2 * i] = fadd2(vv[2 * i], make_float2(__uint_as_float(y.x), __uint_as_float(y.y)));
+                                    vv[2 * i + 1] = fadd2(vv[2 * i + 1], make_float2(__uint_as_float(y.z), __uint_as_float(y.w)));
+                                }
+                            }
+                            const uint32_t at = row_at + (((2 * h + c) ^ swz) << 4);
+                            uint32_t o0[4], o1[4];
+                            if constexpr (MODE == kForward) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    float2 a, da;
+                                    activate<T, decltype(act)::value, false>(gg[i], a, da);
+                                    a = fmul2(a, vv[i]);
+                                    o0[i] = pack2<T>(a.x, a.y);
+                                }
+                            } else {
+                                const uint4 d = ld_shared4(at);
+                                const uint32_t dd[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    float2 a, da;
+                                    activate<T, decltype(act)::value, true>(gg[i], a, da);
+                                    const float2 dh = unpack2<T>(dd[i]);
+                                    da = fmul2(fmul2(dh, vv[i]), da);
+                                    a = fmul2(dh, a);
+                                    o0[i] = pack2<T>(da.x, da.y);
+                                    o1[i] = pack2<T>(a.x, a.y);
+                                }
+                                st_shared4(at + kHalfPatch, make_uint4(o1[0], o1[1], o1[2], o1[3]));
                             }
                             st_shared4(at, make_uint4(o0[0], o0[1], o0[2], o0[3]));
-                            st_shared4(at + kPatch, make_uint4(o1[0], o1[1], o1[2], o1[3]));
-                        }
-                        if (MODE == kGrad && c == 1) {                 // the half before has left: dH of the one after next
-                            const int next = h == 1 ? u + run.step : u;
-                            if (lane == 0 && next < run.end && (h == 1 || ord > 0)) {
-                                store_wait_read<0>();
-                                fetch(next, h ^ 1);
-                            }
-                            __syncwarp();
                         }
                     }
-                    fence_proxy_async();
+                });
+                fence_proxy_async();
+                __syncwarp();
+                const bool there = row0 < p.M && f0 < p.F;
+                if (lane == 0) {
+                    if (there) tma_store_3d(&p.s[0], f0, row0, 0, patch);
+                    if (MODE == kGrad && there) tma_store_3d(&p.s[1], f0, row0, 0, patch + kHalfPatch);
+                    store_commit();
+                }
+                if (MODE == kGrad && p.column) {                       // columns 2 (lane % 16), every other row
+                    const uint32_t at = patch + 64 * (lane >> 4) + 4 * (lane & 3);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t a = at + 128 * r + ((((lane & 15) >> 2) ^ (r & 3)) << 4);
+                        add_pair<T>(column[0], ld_shared1(a));
+                        add_pair<T>(column[1], ld_shared1(a + kHalfPatch));
+                    }
+                    // (the sums are there, and with them what was loaded, before any lane goes on and the patch is handed to the next copy)
+                    asm volatile("" ::"f"(column[0].x), "f"(column[0].y), "f"(column[1].x), "f"(column[1].y) : "memory");
                     __syncwarp();
-                    if (MODE == kGrad || h == 1) {
-                        if (lane == 0 && row0 < p.M) {
-                            if constexpr (MODE == kForward) {
-                                if (f0 < p.F) tma_store_3d(&p.s[0], f0, row0, 0, patch);
-                            } else if (f0 + 32 * h < p.F) {
-                                tma_store_3d(&p.s[0], f0 + 32 * h, row0, 0, patch + 2048 * h);
-                                tma_store_3d(&p.s[1], f0 + 32 * h, row0, 0, patch + kPatch + 2048 * h);
-                            }
-                            store_commit();
-                        }
-                    }
-                    if (MODE == kGrad && p.column) {                   // columns 2 (lane % 16) of this half, every other row
-                        const uint32_t at = patch + 2048 * h + 64 * (lane >> 4) + 4 * (lane & 3);
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const uint32_t a = at + 128 * r + ((((lane & 15) >> 2) ^ (r & 3)) << 4);
-#pragma unroll
-                            for (int o = 0; o < 2; ++o) {
-                                if (h == 0) add_pair<T>(column[0][o], ld_shared1(a + o * kPatch));
-                                else add_pair<T>(column[1][o], ld_shared1(a + o * kPatch));
-                            }
-                        }
-                    }
+                }
+                if (MODE == kGrad && lane == 0 && u + run.step < run.end) {
+                    store_wait_read<0>();
+                    fetch(u + run.step);
                 }
             }
             if (MODE == kGrad && p.column && column_nt >= 0) flush();
             if (lane == 0) store_wait_read<0>();
             __syncwarp();
         } else if constexpr (MODE <= kGrad) {
+            constexpr int kCols = BN / 4 > 16 ? BN / 4 : 16;           // of a warp (BN = 32: half of the warps have none)
             for (int u = run.at; u < run.end; u += run.step, ++ord) {
                 const Unit t = unit_of<MODE>(p, u);
                 const int buf = ord & 1, row = (PAIR ? 256 : 128) * t.mt + 128 * rank + 32 * q + lane;
@@ -497,57 +493,63 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 const size_t plane = (size_t)p.M * p.F;
                 wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
                 tc_fence_after_sync();
+                if (quarter * kCols >= BN) {
+                    release(buf);
+                    continue;
+                }
+                by_activation(p.act, [&](auto act) {
 #pragma unroll 1
-                for (int s = 0; s < BN / 32; ++s) {
-                    const int col = half * (BN / 2) + 16 * s, f0 = BN * t.nt + col;
-                    float g[16], v[16];
-                    __syncwarp();
-                    tmem_ld16(acc + col, g);
-                    tmem_ld16(acc + BN + col, v);
-                    tmem_ld_wait();
-                    if (s == BN / 32 - 1) release(buf);
+                    for (int s = 0; s < kCols / 16; ++s) {
+                        const int col = quarter * kCols + 16 * s, f0 = BN * t.nt + col;
+                        float g[16], v[16];
+                        __syncwarp();
+                        tmem_ld16(acc + col, g);
+                        tmem_ld16(acc + BN + col, v);
+                        tmem_ld_wait();
+                        if (s == kCols / 16 - 1) release(buf);
 #pragma unroll
-                    for (int j = 0; j < 16; j += 8) {
-                        const int f = f0 + j;
-                        if (f >= p.F || row >= p.M) continue;
-                        if (p.bg) {
-                            float b[8];
-                            load8<T>(static_cast<const T*>(p.bg) + f, b);
+                        for (int j = 0; j < 16; j += 8) {
+                            const int f = f0 + j;
+                            if (f >= p.F || row >= p.M) continue;
+                            if (p.bg) {
+                                float b[8];
+                                load8<T>(static_cast<const T*>(p.bg) + f, b);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) g[j + i] += b[i];
-                        }
-                        if (p.bu) {
-                            float b[8];
-                            load8<T>(static_cast<const T*>(p.bu) + f, b);
+                                for (int i = 0; i < 8; ++i) g[j + i] += b[i];
+                            }
+                            if (p.bu) {
+                                float b[8];
+                                load8<T>(static_cast<const T*>(p.bu) + f, b);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) v[j + i] += b[i];
-                        }
-                        const size_t at = (size_t)row * p.F + f;
-                        float dh[8];
-                        if (MODE == kGrad) load8<T>(static_cast<const T*>(p.dh) + at, dh);
+                                for (int i = 0; i < 8; ++i) v[j + i] += b[i];
+                            }
+                            const size_t at = (size_t)row * p.F + f;
+                            float dh[8];
+                            if (MODE == kGrad) load8<T>(static_cast<const T*>(p.dh) + at, dh);
 #pragma unroll
-                        for (int i = j; i < j + 8; i += 2) {
-                            float2 a, da;
-                            activate<T, MODE == kGrad>(p.act, make_float2(g[i], g[i + 1]), a, da);
-                            if (MODE == kForward) {
-                                v[i] *= a.x; v[i + 1] *= a.y;
+                            for (int i = j; i < j + 8; i += 2) {
+                                float2 a, da;
+                                activate<T, decltype(act)::value, MODE == kGrad>(make_float2(g[i], g[i + 1]), a, da);
+                                if (MODE == kForward) {
+                                    v[i] *= a.x; v[i + 1] *= a.y;
+                                } else {
+                                    g[i] = dh[i - j] * v[i] * da.x; g[i + 1] = dh[i + 1 - j] * v[i + 1] * da.y;
+                                    v[i] = dh[i - j] * a.x; v[i + 1] = dh[i + 1 - j] * a.y;
+                                }
+                            }
+                            if constexpr (MODE == kForward) {
+                                store8<T>(static_cast<T*>(p.out0) + at, v + j);
                             } else {
-                                g[i] = dh[i - j] * v[i] * da.x; g[i + 1] = dh[i + 1 - j] * v[i + 1] * da.y;
-                                v[i] = dh[i - j] * a.x; v[i + 1] = dh[i + 1 - j] * a.y;
+                                store_operand8<T>(p.out0, plane, at, g + j);
+                                store_operand8<T>(p.out1, plane, at, v + j);
                             }
                         }
-                        if constexpr (MODE == kForward) {
-                            store8<T>(static_cast<T*>(p.out0) + at, v + j);
-                        } else {
-                            store_operand8<T>(p.out0, plane, at, g + j);
-                            store_operand8<T>(p.out1, plane, at, v + j);
-                        }
                     }
-                }
+                });
                 __syncwarp();
             }
         } else {
-            // boxes of 32 columns and 32 rows, those of a tile in turn by the two warps that share its rows
+            // boxes of 32 columns and 32 rows, those of a tile in turn by the four warps that share its rows
             int box = 0;
             for (int u = run.at; u < run.end; u += run.step, ++ord) {
                 const Unit t = unit_of<MODE>(p, u);
@@ -559,12 +561,12 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
                 tc_fence_after_sync();
 #pragma unroll 1
-                for (int b = half; b < blocks; b += 2, ++box) {
+                for (int b = quarter; b < blocks; b += 4, ++box) {
                     float v[32];
                     __syncwarp();
                     tmem_ld32(acc + 32 * b, reinterpret_cast<uint32_t(&)[32]>(v));
                     tmem_ld_wait();
-                    if (b + 2 >= blocks) release(buf);
+                    if (b + 4 >= blocks) release(buf);
                     uint32_t src = patch;
                     if (p.wide) {                                      // rows of 128 bytes, one patch
                         if (lane == 0) store_wait_read<0>();
@@ -572,7 +574,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
 #pragma unroll
                         for (int c = 0; c < 8; ++c) st_shared4(patch + 128 * lane + ((c ^ (lane & 7)) << 4), pack16<float>(v + 4 * c));
                     } else if constexpr (sizeof(T) == 2) {             // rows of 64 bytes, two patches in turn
-                        src += 2048 * (box & 1);
+                        src += kHalfPatch * (box & 1);
                         if (lane == 0) store_wait_read<1>();
                         __syncwarp();
 #pragma unroll
@@ -586,7 +588,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                         store_commit();
                     }
                 }
-                if (half >= blocks) release(buf);
+                if (quarter >= blocks) release(buf);
             }
             if (lane == 0) store_wait_read<0>();
             __syncwarp();
@@ -810,9 +812,8 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     a.column = fused_columns ? reinterpret_cast<float*>(ws + w.db) : nullptr;
     if (!make_map_3d_u16(&a.a[0], x, kTerms, c.M, c.C, 128) || !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, t.bn) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, t.bn)) return cudaErrorInvalidValue;
     if (!kWide && t.bn == 128) {
-        const uint32_t cols = c.dh ? 32 : 64;
-        if (!make_box_map(&a.s[0], a.out0, 2, 1, c.M, c.F, cols, 32)) return cudaErrorInvalidValue;
-        if (c.dh && (!make_box_map(&a.s[1], a.out1, 2, 1, c.M, c.F, cols, 32) || !make_box_map(&a.g, c.dh, 2, 1, c.M, c.F, cols, 32))) return cudaErrorInvalidValue;
+        if (!make_box_map(&a.s[0], a.out0, 2, 1, c.M, c.F, 32, 32)) return cudaErrorInvalidValue;
+        if (c.dh && (!make_box_map(&a.s[1], a.out1, 2, 1, c.M, c.F, 32, 32) || !make_box_map(&a.g, c.dh, 2, 1, c.M, c.F, 32, 32))) return cudaErrorInvalidValue;
     }
     e = c.dh ? launch_projections<T, kGrad>(a, t, st) : launch_projections<T, kForward>(a, t, st);
     if (e != cudaSuccess) return e;
