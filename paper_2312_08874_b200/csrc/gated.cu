@@ -247,63 +247,64 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
 
     if (warp == kEpiWarps) {
         // ------------------------------------------------------------------ producer
-        if (lane == 0) {
-            int stage = 0, round = 0;
-            const int half_n = p.n / 2, boxes = MODE <= kGrad ? 0 : (half_n + 63) / 64;        // of 64 columns
-            const uint32_t bytes = MODE <= kGrad ? S::kStage : kATile + boxes * 8192;          // of this block's share
-            const uint32_t full0 = PAIR ? in_block(pipe_bar(pp, BAR_FULL), 0) : pipe_bar(pp, BAR_FULL);
-            auto load = [&](uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-                if (PAIR) tma_load_3d_pair(dst, map, x, y, z, bar);
-                else tma_load_3d(dst, map, x, y, z, bar);
-            };
-            for (int u = run.at; u < run.end && !pipe_dead(pp); u += run.step) {
-                const Unit t = unit_of<MODE>(p, u);
-                for (int pair = 0; pair < kPairs; ++pair) {
-                    int ta = 0, tb = 0;
-                    if (kPairs > 1) term_pair(pair, ta, tb);
-                    for (int k = t.k0; k < t.k1 && !pipe_dead(pp); ++k) {
-                        if (round > 0) wait_spin(pp, BAR_EMPTY + stage, round - 1, kTimeoutRole);
-                        const uint32_t bar = full0 + 8 * stage, da = base + 1024 + stage * S::kStage, db = da + kATile;
-                        if (rank == 0) mbar_arrive_expect_tx(pipe_bar(pp, BAR_FULL + stage), (PAIR ? 2 : 1) * bytes);
-                        if constexpr (MODE <= kGrad) {
-                            load(da, &p.a[0], 64 * k, (PAIR ? 256 : 128) * t.mt + 128 * rank, ta, bar);
-                            if (PAIR) {
-                                load(db, &p.b[rank], 64 * k, BN * t.nt, tb, bar);               // one block has the gate's rows, the other the rest
-                            } else {
-                                load(db, &p.b[0], 64 * k, BN * t.nt, tb, bar);
-                                load(db + BN * 128, &p.b[1], 64 * k, BN * t.nt, tb, bar);
-                            }
-                        } else {
-                            const int op = MODE == kInput ? k >= chunks_f : rank, kk = MODE == kInput ? k - op * chunks_f : k, c0 = p.n * t.nt + half_n * rank;
-                            if constexpr (MODE == kInput) {
-                                load(da, &p.a[op], 64 * kk, 256 * t.mt + 128 * rank, ta, bar);
-                            } else {                                                            // one block has dG's columns, the other dU's
-                                load(da, &p.a[op], 128 * t.mt, 64 * k, ta, bar);
-                                load(da + 8192, &p.a[op], 128 * t.mt + 64, 64 * k, ta, bar);
-                            }
-                            for (int j = 0; j < boxes; ++j) load(db + j * 8192, &p.b[MODE == kInput ? op : 0], c0 + 64 * j, 64 * kk, tb, bar);
-                        }
-                        if (++stage == kStages) { stage = 0; ++round; }
+        int stage = 0, round = 0;
+        const int half_n = p.n / 2, boxes = MODE <= kGrad ? 0 : (half_n + 63) / 64;            // of 64 columns
+        const uint32_t bytes = MODE <= kGrad ? S::kStage : kATile + boxes * 8192;              // of this block's share
+        const uint32_t full0 = PAIR ? in_block(pipe_bar(pp, BAR_FULL), 0) : pipe_bar(pp, BAR_FULL);
+        bool alive = true;
+        for (int u = run.at; u < run.end && alive; u += run.step) {
+            const Unit t = unit_of<MODE>(p, u);
+            for (int pair = 0; pair < kPairs; ++pair) {
+                int ta = 0, tb = 0;
+                if (kPairs > 1) term_pair(pair, ta, tb);
+                for (int k = t.k0; k < t.k1 && alive; ++k) {
+                    if (round > 0 && !mbar_test(pipe_bar(pp, BAR_EMPTY + stage), (round - 1) & 1u)) {
+                        wait_spin(pp, BAR_EMPTY + stage, round - 1, kTimeoutRole);
+                        if (pipe_dead(pp)) { alive = false; break; }
                     }
+                    const uint32_t bar = full0 + 8 * stage, da = base + 1024 + stage * S::kStage, db = da + kATile;
+                    if (rank == 0) mbar_arrive_expect_tx_w(pipe_bar(pp, BAR_FULL + stage), (PAIR ? 2 : 1) * bytes);
+                    if constexpr (MODE <= kGrad) {
+                        tma_load_3d_w<PAIR>(da, &p.a[0], 64 * k, (PAIR ? 256 : 128) * t.mt + 128 * rank, ta, bar);
+                        if (PAIR) {
+                            tma_load_3d_w<PAIR>(db, &p.b[rank], 64 * k, BN * t.nt, tb, bar);    // one block has the gate's rows, the other the rest
+                        } else {
+                            tma_load_3d_w<PAIR>(db, &p.b[0], 64 * k, BN * t.nt, tb, bar);
+                            tma_load_3d_w<PAIR>(db + BN * 128, &p.b[1], 64 * k, BN * t.nt, tb, bar);
+                        }
+                    } else {
+                        const int op = MODE == kInput ? k >= chunks_f : rank, kk = MODE == kInput ? k - op * chunks_f : k, c0 = p.n * t.nt + half_n * rank;
+                        if constexpr (MODE == kInput) {
+                            tma_load_3d_w<PAIR>(da, &p.a[op], 64 * kk, 256 * t.mt + 128 * rank, ta, bar);
+                        } else {                                                                // one block has dG's columns, the other dU's
+                            tma_load_3d_w<PAIR>(da, &p.a[op], 128 * t.mt, 64 * k, ta, bar);
+                            tma_load_3d_w<PAIR>(da + 8192, &p.a[op], 128 * t.mt + 64, 64 * k, ta, bar);
+                        }
+                        tma_load_3d_w<PAIR>(db, &p.b[MODE == kInput ? op : 0], c0, 64 * kk, tb, bar);
+                        if (boxes > 1) tma_load_3d_w<PAIR>(db + 8192, &p.b[MODE == kInput ? op : 0], c0 + 64, 64 * kk, tb, bar);
+                    }
+                    if (++stage == kStages) { stage = 0; ++round; }
                 }
             }
-            // no copy, and no arrival of the pair's products, may be under way at the block's end, whatever became of the other roles
-            for (int s = 0; s < kStages; ++s) {
-                const int last = s < stage ? round : round - 1;
-                if (last < 0) continue;
-                if (rank == 0) mbar_wait_bounded(pipe_bar(pp, BAR_FULL + s), last & 1, 1u << 16);
-                if (!pipe_dead(pp)) mbar_wait_bounded(pipe_bar(pp, BAR_EMPTY + s), last & 1, 1u << 20);
-            }
+        }
+        // no copy, and no arrival of the pair's products, may be under way at the block's end, whatever became of the other roles
+        for (int s = 0; s < kStages; ++s) {
+            const int last = s < stage ? round : round - 1;
+            if (last < 0) continue;
+            if (rank == 0) mbar_wait_bounded(pipe_bar(pp, BAR_FULL + s), last & 1, 1u << 16);
+            if (!pipe_dead(pp)) mbar_wait_bounded(pipe_bar(pp, BAR_EMPTY + s), last & 1, 1u << 20);
         }
         __syncwarp();
     } else if (warp == kEpiWarps + 1) {
         // ------------------------------------------------------------------ products
         if (rank == 0) {
-            constexpr int fmt = Elem<E>::kIsBf16 ? 1 : 0;
+            constexpr int fmt = Elem<E>::kIsBf16 ? 1 : 0, kA = MODE == kWeight ? 128 : 2, kB = MODE <= kGrad ? 2 : 128;
             const uint32_t id = umma_idesc(fmt, PAIR ? 256 : 128, MODE <= kGrad ? 2 * BN : p.n, MODE >= kInput) | (MODE == kWeight ? 1u << 15 : 0u);
+            const uint32_t elected = elect_lane();
             const int total = MODE <= kGrad ? p.C : MODE == kInput ? p.F : p.M;
             int stage = 0, round = 0, ord = 0;
-            for (int u = run.at; u < run.end && !pipe_dead(pp); u += run.step, ++ord) {
+            bool alive = true, there = false;                          // whether the stage's tiles were seen to be there already
+            for (int u = run.at; u < run.end && alive; u += run.step, ++ord) {
                 const Unit t = unit_of<MODE>(p, u);
                 const int buf = ord & 1;
                 if (ord >= 2) wait_spin(pp, BAR_READ + buf, (ord >> 1) - 1, kTimeoutRole);
@@ -311,33 +312,32 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 const uint32_t d = pp.tmem + 256 * buf;
                 uint32_t acc = 0;
                 for (int pair = 0; pair < kPairs; ++pair)
-                    for (int k = t.k0; k < t.k1 && !pipe_dead(pp); ++k) {
-                        wait_spin(pp, BAR_FULL + stage, round, kTimeoutTile);
+                    for (int k = t.k0; k < t.k1 && alive; ++k) {
+                        if (!there) {
+                            wait_spin(pp, BAR_FULL + stage, round, kTimeoutTile);
+                            alive = !pipe_dead(pp);
+                        }
                         tc_fence_after_sync();
-                        const uint32_t at = base + 1024 + stage * S::kStage;
+                        const uint32_t at = base + 1024 + stage * S::kStage, empty = pipe_bar(pp, BAR_EMPTY + stage);
                         const uint64_t da = MODE == kWeight ? desc_mn(at, 8192) : umma_desc_sw128(at);
                         const uint64_t db = MODE <= kGrad ? umma_desc_sw128(at + kATile) : desc_mn(at + kATile, 8192);
-                        const int kk = MODE == kInput && k >= chunks_f ? k - chunks_f : k;
-                        const int steps = min(4, (total - 64 * kk + 15) / 16);
-                        // descriptor addresses count 16 bytes: a step of 16 is 2 along a K-major row, 128 down MN-major ones
-                        for (int s = 0; s < steps; ++s, acc = 1u) {
-                            const uint64_t sa = da + (MODE == kWeight ? 128 : 2) * s, sb = db + (MODE <= kGrad ? 2 : 128) * s;
-                            if (PAIR) umma_ss_pair(d, sa, sb, id, acc);
-                            else umma_ss_w(d, sa, sb, id, acc);
-                        }
-                        if (PAIR) umma_commit_pair(pipe_bar(pp, BAR_EMPTY + stage));
-                        else umma_commit_w(pipe_bar(pp, BAR_EMPTY + stage));
+                        const int kk = MODE == kInput && k >= chunks_f ? k - chunks_f : k, left = total - 64 * kk;
                         if (++stage == kStages) { stage = 0; ++round; }
+                        there = mbar_test(pipe_bar(pp, BAR_FULL + stage), round & 1u);     // (asked before the instructions are queued)
+                        // descriptor addresses count 16 bytes: a step of 16 is 2 along a K-major row, 128 down MN-major ones
+                        if (left > 48) {
+                            umma_four<PAIR, kA, kB>(elected, d, da, db, id, acc);
+                        } else {
+                            for (int s = 0; 16 * s < left; ++s) umma_step<PAIR>(elected, d, da + kA * s, db + kB * s, id, s ? 1u : acc);
+                        }
+                        acc = 1u;
+                        umma_commit_e<PAIR>(elected, empty);
                     }
-                if (PAIR) umma_commit_pair(pipe_bar(pp, BAR_ACC + buf));
-                else umma_commit_w(pipe_bar(pp, BAR_ACC + buf));
+                umma_commit_e<PAIR>(elected, pipe_bar(pp, BAR_ACC + buf));
             }
-            if (PAIR) {
-                umma_commit_first(pipe_bar(pp, BAR_DRAIN));
-                mbar_wait_bounded(pipe_bar(pp, BAR_DRAIN), 0u, 1u << 20);
-            } else {
-                umma_drain_w(pp, BAR_DRAIN);
-            }
+            if (PAIR) umma_commit_first(elected, pipe_bar(pp, BAR_DRAIN));
+            else umma_commit_e<false>(elected, pipe_bar(pp, BAR_DRAIN));
+            mbar_wait_bounded(pipe_bar(pp, BAR_DRAIN), 0u, 1u << 20);
         }
         __syncwarp();
     } else {

@@ -32,35 +32,82 @@ template <uint32_t kCols> __device__ __forceinline__ void tmem_alloc_pair(uint32
 template <uint32_t kCols> __device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr) {
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(taddr), "n"(kCols) : "memory");
 }
-// D (+)= A B over both blocks (M = 256: 128 rows of A each, half of B's columns each); a warp of the first block, uniform control flow
-__device__ __forceinline__ void umma_ss_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "elect.sync _|q, 0xffffffff;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+// Whether an mbarrier's phase is complete, without waiting
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
 }
-// arrival at the mbarrier of both blocks once the pair's instructions so far are complete
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
-    asm volatile(
-        "{\n\t.reg .pred q;\n\t.reg .b16 m;\n\t"
-        "elect.sync _|q, 0xffffffff;\n\t"
-        "mov.b16 m, 3;\n\t"
-        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}\n" ::"r"(bar) : "memory");
+// One lane of a warp in uniform control flow, chosen once: issues the instructions below.
+__device__ __forceinline__ uint32_t elect_lane() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}\n" : "=r"(e));
+    return e;
 }
-// the same at an mbarrier of the first block alone
-__device__ __forceinline__ void umma_commit_first(uint32_t bar) {
+// D (+)= A B, one step of 16 of the sum.  PAIR: over both blocks of a pair (M = 256: 128 rows of A each, half of B's columns each), by the first.
+#define AA_UMMA_STEP(group) "@q tcgen05.mma.cta_group::" group ".kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
+template <bool PAIR> __device__ __forceinline__ void umma_step(uint32_t elected, uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %5, 0;\n\tsetp.ne.b32 p, %4, 0;\n\t" AA_UMMA_STEP("2") ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(elected) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %5, 0;\n\tsetp.ne.b32 p, %4, 0;\n\t" AA_UMMA_STEP("1") ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(elected) : "memory");
+}
+#undef AA_UMMA_STEP
+// Four steps whose descriptors are kA and kB apart: 64 of the sum.  (As four separate instructions with an election each they took twice the
+// time that the tensor cores need.)
+#define AA_UMMA_FOUR(group)                                                                                  \
+    "{\n\t.reg .pred p, q, t;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 q, %5, 0;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t" \
+    "@q tcgen05.mma.cta_group::" group ".kind::f16 [%0], %1, %2, %3, p;\n\t"                                 \
+    "add.s64 a, %1, %6;\n\tadd.s64 b, %2, %7;\n\t"                                                       \
+    "@q tcgen05.mma.cta_group::" group ".kind::f16 [%0], a, b, %3, t;\n\t"                                   \
+    "add.s64 a, a, %6;\n\tadd.s64 b, b, %7;\n\t"                                                         \
+    "@q tcgen05.mma.cta_group::" group ".kind::f16 [%0], a, b, %3, t;\n\t"                                   \
+    "add.s64 a, a, %6;\n\tadd.s64 b, b, %7;\n\t"                                                         \
+    "@q tcgen05.mma.cta_group::" group ".kind::f16 [%0], a, b, %3, t;\n\t}\n"
+template <bool PAIR, int kA, int kB> __device__ __forceinline__ void umma_four(uint32_t elected, uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+    if constexpr (PAIR) asm volatile(AA_UMMA_FOUR("2") ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(elected), "n"(kA), "n"(kB) : "memory");
+    else asm volatile(AA_UMMA_FOUR("1") ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(elected), "n"(kA), "n"(kB) : "memory");
+}
+#undef AA_UMMA_FOUR
+// Arrival once the instructions so far are complete: PAIR: at the mbarrier of both blocks
+template <bool PAIR> __device__ __forceinline__ void umma_commit_e(uint32_t elected, uint32_t bar) {
+    if constexpr (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\t.reg .b16 m;\n\tsetp.ne.b32 q, %1, 0;\n\tmov.b16 m, 3;\n\t"
+            "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}\n" ::"r"(bar), "r"(elected) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+            "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(bar), "r"(elected) : "memory");
+}
+// the same of a pair's instructions at an mbarrier of the first block alone
+__device__ __forceinline__ void umma_commit_first(uint32_t elected, uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(bar), "r"(elected) : "memory");
+}
+// 3-D tiled load into this block's memory, issued by one elected lane of a warp in uniform control flow (every operand of a load inside an
+// `if (lane == 0)` region takes a detour: 100 ns a load, against 20 this way).  PAIR: it reports to an mbarrier of either block of the pair (a
+// shared::cluster address).
+template <bool PAIR> __device__ __forceinline__ void tma_load_3d_w(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    if constexpr (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\t"
+            "elect.sync _|q, 0xffffffff;\n\t"
+            "@q cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}\n"
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q;\n\t"
+            "elect.sync _|q, 0xffffffff;\n\t"
+            "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}\n"
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_expect_tx_w(uint32_t bar, uint32_t bytes) {
     asm volatile(
         "{\n\t.reg .pred q;\n\t"
         "elect.sync _|q, 0xffffffff;\n\t"
-        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(bar) : "memory");
-}
-// 3-D tiled load into this block's memory that reports to an mbarrier of either block of the pair (a shared::cluster address)
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+        "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}\n" ::"r"(bar), "r"(bytes) : "memory");
 }
 
 // 3-D tiled store of a staged box (what lies outside the tensor is left out), and this thread's groups of stores
