@@ -18,10 +18,11 @@ __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-// one arrival on an mbarrier of a block of the cluster (a shared::cluster address), for a warp whose lanes have all done their part
+// One arrival on an mbarrier of a block of the cluster (a shared::cluster address), for a warp whose lanes have all done their part.  It tells of
+// tensor-memory reads, which are complete; a release at cluster scope would wait for the warp's global stores too (3000 cycles a tile).
 __device__ __forceinline__ void arrive_cluster_warp(uint32_t bar, int lane) {
     __syncwarp();
-    if (lane == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
+    if (lane == 0) asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
 }
 
 // Tensor memory of both blocks: a warp of each calls these
