@@ -3,13 +3,15 @@
 //     G = X Wg^T + bg,  U = X Wu^T + bu,  H = act(G) o U                       X [M][C], Wg and Wu [F][C], H [M][F]
 //     dU = dH o act(G),  dG = dH o U o act'(G);  dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X,  biases: column sums
 //
-// One pipelined product in four forms: a TMA warp fills a ring of operand tiles, one warp issues `tcgen05.mma` into two accumulators in tensor
-// memory that take turns, eight warps read the finished one and do the rest.  Blocks are persistent over (tile, split) units.
-//   kForward  tile of 128 rows x BN columns of G and the same of U: one instruction of 2 BN columns, whose B operand is a tile of Wg above one of
-//             Wu; the epilogue applies biases, activation and product.  G and U never leave the chip.
-//   kGrad     the same product again; the epilogue reads dH and writes dG and dU for the two forms that follow.
-//   kInput    dX: A = dG, then dU (along their rows), B = Wg, then Wu, read as [hidden][channels] = MN-major: nothing is transposed.
-//   kWeight   dWg above dWu: A = dG or dU read MN-major, B = X read MN-major; the sum runs over the rows of X, split over blocks where tiles are few.
+// One pipelined product in three forms: a TMA warp fills a ring of operand tiles, one warp issues `tcgen05.mma` into two accumulators in tensor
+// memory that take turns, sixteen warps read the finished one and do the rest.  A pair of blocks (cta_group::2) has a tile of 256 rows.
+//   kForward   256 rows of 128 hidden units of G and U: one block of the pair holds a tile of Wg, the other one of Wu, so that one instruction of 256
+//              columns makes both; the epilogue applies biases, activation and product.  G and U never leave the chip.
+//   kGrad      the same product again; the epilogue reads dH, writes dG and dU for the third form and sums their columns.
+//   kProducts  dX: A = dG, then dU (along their rows), B = Wg, then Wu, read as [hidden][channels] = MN-major: nothing is transposed.  dWg and dWu:
+//              A = dG in one block of the pair, dU in the other, both MN-major, B = X MN-major.  All their sums, cut into chunks of 64, are one line
+//              that the pairs share evenly: a pair takes a run of it, writes the tiles it has whole and leaves its share of those that it has not,
+//              and gated_finish_kernel adds the shares up in their order.
 // 16-bit operands enter as they are; dG and dU are rounded to the element type, as every operand of a product on the tensor cores is.  fp32: operands are sums of
 // three bf16 terms, six pairs of terms, small ones first.
 #include "bwd_terms.cuh"
@@ -22,7 +24,7 @@ namespace aa {
 
 namespace {
 
-enum GatedMode { kForward, kGrad, kInput, kWeight };
+enum GatedMode { kForward, kGrad, kProducts };
 constexpr int kEpiWarps = 16, kThreads = 32 * (kEpiWarps + 2);
 constexpr int kATile = 128 * 128;                      // bytes of a [128][64] (or [64][128]) tile of 16-bit elements
 constexpr int kHalfPatch = 2048;                       // bytes of a warp's staged box of 32 x 32 16-bit values (fp32: two)
@@ -31,16 +33,23 @@ constexpr int kTimeoutTile = 3, kTimeoutRole = 6;
 constexpr int kRing = 6, BAR_FULL = 0, BAR_EMPTY = kRing, BAR_ACC = 2 * kRing, BAR_READ = BAR_ACC + 2, BAR_DRAIN = BAR_READ + 2, BAR_DH = BAR_DRAIN + 1, kBars = BAR_DH + kEpiWarps;
 static_assert(kBars * 8 <= 1024, "barriers");
 
+// The line of kProducts' work: tiles of dX, of 256 rows, then those of dWg and dWu, of 128 hidden units of both; n columns each
+struct GatedLine {
+    int tiles_x, chunks_x, tiles_w, chunks_w, tiles_n, n, pairs;
+    __host__ __device__ long long length() const { return (long long)tiles_x * chunks_x + (long long)tiles_w * chunks_w; }
+    __host__ __device__ long long begin(int pair) const { return length() * pair / pairs; }
+    __host__ __device__ int pair_of(long long at) const { return (int)(((at + 1) * pairs - 1) / length()); }
+};
 struct GatedArgs {
     int M, C, F, act;
-    int tiles_m, tiles_n, splits, chunks;              // chunks: 64 long, of the sum
-    int n;                                             // columns of a tile (kInput, kWeight): a multiple of 32
-    int wide;                                          // results leave as fp32 (fp32 tensors, shares of a split sum)
+    int tiles_m, tiles_n, chunks;                      // kForward, kGrad; chunks: 64 long, of the sum
+    GatedLine line;
     const void *bg, *bu, *dh;
     void *out0, *out1;                                 // H; dG and dU: where they are written without staging
     float* column;                                     // [slots][2][F]: shares of the column sums of dG and dU, or null
     int* status;
-    alignas(64) CUtensorMap a[2], b[2], s[2], g;       // operands; staged results; dH
+    alignas(64) CUtensorMap a[2], b[2], x;             // operands; kProducts: a, b of dX (a of the weights, too), x: X
+    alignas(64) CUtensorMap s[3], g, w[2], share;      // staged results: H; dG, dU; dX, dWg, dWu; dH; kProducts: dG and dU in boxes of 64 rows; shares of tiles
 };
 
 template <typename T> struct GatedTerms {              // element of the operands, terms and pairs of terms
@@ -167,10 +176,10 @@ __device__ __forceinline__ uint32_t ld_shared1(uint32_t at) {
     return v;
 }
 
-// A pair of blocks takes a tile of 256 rows, each of its blocks 128 of them and half of the B operand (BN = 128, and kInput and kWeight); a lone
-// block a tile of 128 rows and 2 BN columns (BN = 64 or 32: small problems).
+// A pair of blocks takes a tile of 256 rows, each of its blocks 128 of them and half of the B operand (BN = 128, and kProducts); a lone block a tile of
+// 128 rows and 2 BN columns (BN = 64 or 32: small problems).
 template <typename T, GatedMode MODE, int BN> struct GatedShape {
-    static constexpr bool kPair = BN == 128, kStaged = MODE >= kInput || (kPair && sizeof(T) == 2);
+    static constexpr bool kPair = BN == 128, kStaged = MODE == kProducts || (kPair && sizeof(T) == 2);
     static constexpr int kBTile = kPair ? kATile : 2 * BN * 128;
     static constexpr int kStage = kATile + kBTile;
     static constexpr int kPatch = !kStaged ? 0 : MODE == kForward ? kHalfPatch : 2 * kHalfPatch;       // of a warp
@@ -179,34 +188,47 @@ template <typename T, GatedMode MODE, int BN> struct GatedShape {
     static constexpr int kSmem = kOffBias + (MODE <= kGrad && kStaged ? kEpiWarps * 256 : 0) + 1024;
 };
 
-// Units of work of block (or pair) `who` of `count`: kForward and kGrad a run in the order of the rows, so that a run has few column ranges
-template <GatedMode MODE> struct Units {
-    int at, end, step;
-    __device__ Units(int units, int who, int count) {
-        if (MODE <= kGrad) {
-            at = (int)((long long)units * who / count);
-            end = (int)((long long)units * (who + 1) / count);
-            step = 1;
-        } else {
-            at = who; end = units; step = count;
+// What block (or pair) `who` of `count` does, tile by tile.  kForward and kGrad: a run of tiles in the order of the rows, so that a run has few column
+// ranges; kProducts: a run of the line.
+struct Work {
+    int mt, nt, k0, k1;
+    bool weight, whole;                                // kProducts: of dWg and dWu; the whole sum
+    int slot;                                          // of a share
+};
+template <GatedMode MODE> struct Walk {
+    const GatedArgs& p;
+    long long at, first, end;
+    int who;
+    __device__ Walk(const GatedArgs& args, int who_, int count) : p(args), who(who_) {
+        const long long units = (long long)p.tiles_m * p.tiles_n;
+        first = at = MODE == kProducts ? p.line.begin(who) : units * who / count;
+        end = MODE == kProducts ? p.line.begin(who + 1) : units * (who + 1) / count;
+    }
+    __device__ bool next(Work& w) {
+        if (at >= end) return false;
+        if (MODE != kProducts) {
+            w.nt = (int)at / p.tiles_m;
+            w.mt = (int)at - w.nt * p.tiles_m;
+            w.k0 = 0; w.k1 = p.chunks;
+            ++at;
+            return true;
         }
+        const GatedLine& l = p.line;
+        const long long split = (long long)l.tiles_x * l.chunks_x;
+        w.weight = at >= split;
+        const int chunks = w.weight ? l.chunks_w : l.chunks_x;
+        const long long here = w.weight ? at - split : at, left = end - at;
+        const int tile = (int)(here / chunks);
+        w.mt = tile / l.tiles_n;
+        w.nt = tile - w.mt * l.tiles_n;
+        w.k0 = (int)(here - (long long)tile * chunks);
+        w.k1 = chunks - w.k0 < left ? chunks : (int)(w.k0 + left);
+        w.whole = w.k0 == 0 && w.k1 == chunks;
+        w.slot = 2 * who + (at == first ? 0 : 1);
+        at += w.k1 - w.k0;
+        return true;
     }
 };
-struct Unit { int mt, nt, split, k0, k1; };
-template <GatedMode MODE> __device__ __forceinline__ Unit unit_of(const GatedArgs& p, int u) {
-    Unit t;
-    const int fast = MODE <= kGrad ? p.tiles_m : p.tiles_n, v = u / fast, low = u - v * fast;
-    if (MODE <= kGrad) {
-        t.mt = low; t.nt = v; t.split = 0; t.k0 = 0; t.k1 = p.chunks;
-    } else {
-        t.nt = low;
-        t.split = v / p.tiles_m;
-        t.mt = v - t.split * p.tiles_m;
-        t.k0 = (int)((long long)p.chunks * t.split / p.splits);
-        t.k1 = (int)((long long)p.chunks * (t.split + 1) / p.splits);
-    }
-    return t;
-}
 
 template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constant__ GatedArgs p) {
     using S = GatedShape<T, MODE, BN>;
@@ -219,20 +241,28 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t rank = PAIR ? cluster_rank() : 0u;
-    const int units = p.tiles_m * p.tiles_n * p.splits, who = PAIR ? blockIdx.x / 2 : blockIdx.x, count = PAIR ? gridDim.x / 2 : gridDim.x;
+    const int who = PAIR ? blockIdx.x / 2 : blockIdx.x, count = PAIR ? gridDim.x / 2 : gridDim.x;
 
     Pipe pp;
     pp.status = p.status;
     pp.dead = &s_dead;
     pp.bars = base;
-    if (tid == 0) {
-        s_dead = 0;
-        for (int i = 0; i < kBars; ++i) mbar_init(pp.bars + 8 * i, i >= BAR_READ && i < BAR_DRAIN ? (PAIR ? 2 : 1) * kEpiWarps : 1u);
-        mbar_fence_init();
-    }
-    if (warp == 0) {
+    if (tid < kBars) mbar_init(pp.bars + 8 * tid, tid >= BAR_READ && tid < BAR_DRAIN ? (PAIR ? 2 : 1) * kEpiWarps : 1u);
+    if (tid == 0) s_dead = 0;
+    if (warp <= (kBars - 1) / 32) mbar_fence_init();
+    if (warp == kEpiWarps) {
         if (PAIR) tmem_alloc_pair<512>(smem_u32(&s_tmem));
         else tmem_alloc<512>(smem_u32(&s_tmem));
+    }
+    if (warp == kEpiWarps + 1 && lane == 0) {
+        prefetch_map(&p.a[0]);
+        prefetch_map(&p.b[PAIR && MODE != kProducts ? rank : 0]);
+        if (MODE == kProducts) {
+            prefetch_map(&p.a[1]);
+            prefetch_map(&p.b[1]);
+            prefetch_map(&p.w[rank]);
+            prefetch_map(&p.x);
+        }
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -243,17 +273,17 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
     pdl_release_next();
 
     const int chunks_f = (p.F + 63) / 64;
-    Units<MODE> run(units, who, count);
+    Walk<MODE> walk(p, who, count);
+    Work t;
 
     if (warp == kEpiWarps) {
         // ------------------------------------------------------------------ producer
         int stage = 0, round = 0;
-        const int half_n = p.n / 2, boxes = MODE <= kGrad ? 0 : (half_n + 63) / 64;            // of 64 columns
+        const int half_n = p.line.n / 2, boxes = MODE <= kGrad ? 0 : (half_n + 63) / 64;       // of 64 columns
         const uint32_t bytes = MODE <= kGrad ? S::kStage : kATile + boxes * 8192;              // of this block's share
         const uint32_t full0 = PAIR ? in_block(pipe_bar(pp, BAR_FULL), 0) : pipe_bar(pp, BAR_FULL);
         bool alive = true;
-        for (int u = run.at; u < run.end && alive; u += run.step) {
-            const Unit t = unit_of<MODE>(p, u);
+        while (alive && walk.next(t)) {
             for (int pair = 0; pair < kPairs; ++pair) {
                 int ta = 0, tb = 0;
                 if (kPairs > 1) term_pair(pair, ta, tb);
@@ -273,15 +303,16 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                             tma_load_3d_w<PAIR>(db + BN * 128, &p.b[1], 64 * k, BN * t.nt, tb, bar);
                         }
                     } else {
-                        const int op = MODE == kInput ? k >= chunks_f : rank, kk = MODE == kInput ? k - op * chunks_f : k, c0 = p.n * t.nt + half_n * rank;
-                        if constexpr (MODE == kInput) {
+                        const int c0 = p.line.n * t.nt + half_n * rank, op = !t.weight && k >= chunks_f, kk = k - op * chunks_f;
+                        const CUtensorMap* mb = t.weight ? &p.x : &p.b[op];
+                        if (t.weight) {                                                         // one block has dG's columns, the other dU's
+                            tma_load_3d_w<PAIR>(da, &p.w[rank], 128 * t.mt, 64 * k, ta, bar);
+                            tma_load_3d_w<PAIR>(da + 8192, &p.w[rank], 128 * t.mt + 64, 64 * k, ta, bar);
+                        } else {
                             tma_load_3d_w<PAIR>(da, &p.a[op], 64 * kk, 256 * t.mt + 128 * rank, ta, bar);
-                        } else {                                                                // one block has dG's columns, the other dU's
-                            tma_load_3d_w<PAIR>(da, &p.a[op], 128 * t.mt, 64 * k, ta, bar);
-                            tma_load_3d_w<PAIR>(da + 8192, &p.a[op], 128 * t.mt + 64, 64 * k, ta, bar);
                         }
-                        tma_load_3d_w<PAIR>(db, &p.b[MODE == kInput ? op : 0], c0, 64 * kk, tb, bar);
-                        if (boxes > 1) tma_load_3d_w<PAIR>(db + 8192, &p.b[MODE == kInput ? op : 0], c0 + 64, 64 * kk, tb, bar);
+                        tma_load_3d_w<PAIR>(db, mb, c0, 64 * kk, tb, bar);
+                        if (boxes > 1) tma_load_3d_w<PAIR>(db + 8192, mb, c0 + 64, 64 * kk, tb, bar);
                     }
                     if (++stage == kStages) { stage = 0; ++round; }
                 }
@@ -298,18 +329,18 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
     } else if (warp == kEpiWarps + 1) {
         // ------------------------------------------------------------------ products
         if (rank == 0) {
-            constexpr int fmt = Elem<E>::kIsBf16 ? 1 : 0, kA = MODE == kWeight ? 128 : 2, kB = MODE <= kGrad ? 2 : 128;
-            const uint32_t id = umma_idesc(fmt, PAIR ? 256 : 128, MODE <= kGrad ? 2 * BN : p.n, MODE >= kInput) | (MODE == kWeight ? 1u << 15 : 0u);
+            constexpr int fmt = Elem<E>::kIsBf16 ? 1 : 0;
+            const uint32_t id = umma_idesc(fmt, PAIR ? 256 : 128, MODE <= kGrad ? 2 * BN : p.line.n, MODE == kProducts);
             const uint32_t elected = elect_lane();
-            const int total = MODE <= kGrad ? p.C : MODE == kInput ? p.F : p.M;
             int stage = 0, round = 0, ord = 0;
             bool alive = true, there = false;                          // whether the stage's tiles were seen to be there already
-            for (int u = run.at; u < run.end && alive; u += run.step, ++ord) {
-                const Unit t = unit_of<MODE>(p, u);
+            for (; alive && walk.next(t); ++ord) {
                 const int buf = ord & 1;
                 if (ord >= 2) wait_spin(pp, BAR_READ + buf, (ord >> 1) - 1, kTimeoutRole);
                 tc_fence_after_sync();
                 const uint32_t d = pp.tmem + 256 * buf;
+                const bool weight = MODE == kProducts && t.weight;
+                const int total = MODE <= kGrad ? p.C : weight ? p.M : p.F;
                 uint32_t acc = 0;
                 for (int pair = 0; pair < kPairs; ++pair)
                     for (int k = t.k0; k < t.k1 && alive; ++k) {
@@ -319,17 +350,23 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                         }
                         tc_fence_after_sync();
                         const uint32_t at = base + 1024 + stage * S::kStage, empty = pipe_bar(pp, BAR_EMPTY + stage);
-                        const uint64_t da = MODE == kWeight ? desc_mn(at, 8192) : umma_desc_sw128(at);
-                        const uint64_t db = MODE <= kGrad ? umma_desc_sw128(at + kATile) : desc_mn(at + kATile, 8192);
-                        const int kk = MODE == kInput && k >= chunks_f ? k - chunks_f : k, left = total - 64 * kk;
+                        const int kk = MODE == kProducts && !weight && k >= chunks_f ? k - chunks_f : k, left = total - 64 * kk;
                         if (++stage == kStages) { stage = 0; ++round; }
                         there = mbar_test(pipe_bar(pp, BAR_FULL + stage), round & 1u);     // (asked before the instructions are queued)
                         // descriptor addresses count 16 bytes: a step of 16 is 2 along a K-major row, 128 down MN-major ones
-                        if (left > 48) {
-                            umma_four<PAIR, kA, kB>(elected, d, da, db, id, acc);
-                        } else {
-                            for (int s = 0; 16 * s < left; ++s) umma_step<PAIR>(elected, d, da + kA * s, db + kB * s, id, s ? 1u : acc);
-                        }
+                        auto issue = [&](auto ka, auto kb, uint64_t da, uint64_t db, uint32_t desc) {
+                            constexpr int kA = decltype(ka)::value, kB = decltype(kb)::value;
+                            if (left > 48) {
+                                umma_four<PAIR, kA, kB>(elected, d, da, db, desc, acc);
+                            } else {
+                                for (int s = 0; 16 * s < left; ++s) umma_step<PAIR>(elected, d, da + kA * s, db + kB * s, desc, s ? 1u : acc);
+                            }
+                        };
+                        using Row = std::integral_constant<int, 2>;
+                        using Column = std::integral_constant<int, 128>;
+                        if (MODE <= kGrad) issue(Row(), Row(), umma_desc_sw128(at), umma_desc_sw128(at + kATile), id);
+                        else if (weight) issue(Column(), Column(), desc_mn(at, 8192), desc_mn(at + kATile, 8192), id | 1u << 15);
+                        else issue(Row(), Column(), umma_desc_sw128(at), desc_mn(at + kATile, 8192), id);
                         acc = 1u;
                         umma_commit_e<PAIR>(elected, empty);
                     }
@@ -358,7 +395,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             float2 column[2] = {};                                     // dG, dU: sums of two columns over this run's rows
             int column_nt = -1;
             auto flush = [&] {                                         // lanes l and l + 16 have even and odd rows of the same columns
-                const int first = (int)((((long long)column_nt * p.tiles_m + 1) * count - 1) / units);
+                const int first = (int)((((long long)column_nt * p.tiles_m + 1) * count - 1) / ((long long)p.tiles_m * p.tiles_n));
                 float* dst = p.column + (size_t)(8 * (who - first) + 4 * rank + q) * 2 * p.F;
                 const int f = BN * column_nt + 32 * quarter + 2 * (lane & 15);
 #pragma unroll
@@ -370,16 +407,18 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     column[o] = both(0.f);
                 }
             };
-            auto fetch = [&](int u) {                                  // one lane: dH of a unit
-                const Unit t = unit_of<MODE>(p, u);
+            auto fetch = [&](const Work& t) {                          // one lane: dH of a tile
                 const uint32_t bar = pipe_bar(pp, BAR_DH + warp);
                 mbar_arrive_expect_tx(bar, kHalfPatch);
                 tma_load_3d(patch, &p.g, BN * t.nt + 32 * quarter, 256 * t.mt + 128 * rank + 32 * q, 0, bar);
             };
-            if (MODE == kGrad && lane == 0 && run.at < run.end) fetch(run.at);
+            Work ahead;
+            bool more = walk.next(ahead);
+            if (MODE == kGrad && lane == 0 && more) fetch(ahead);
             const bool biased = p.bg || p.bu;
-            for (int u = run.at; u < run.end; u += run.step, ++ord) {
-                const Unit t = unit_of<MODE>(p, u);
+            for (; more; ++ord) {
+                t = ahead;
+                more = walk.next(ahead);
                 const int buf = ord & 1, row0 = 256 * t.mt + 128 * rank + 32 * q, f0 = BN * t.nt + 32 * quarter;
                 const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16) + 32 * quarter;
                 if (MODE == kGrad && p.column && column_nt != t.nt) {
@@ -428,7 +467,8 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                                 }
                             }
                             const uint32_t at = row_at + (((2 * h + c) ^ swz) << 4);
-                            uint32_t o0[4], o1[4];
+                            uint32_t o0[4];
+                            [[maybe_unused]] uint32_t o1[4];
                             if constexpr (MODE == kForward) {
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
@@ -476,9 +516,9 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     asm volatile("" ::"f"(column[0].x), "f"(column[0].y), "f"(column[1].x), "f"(column[1].y) : "memory");
                     __syncwarp();
                 }
-                if (MODE == kGrad && lane == 0 && u + run.step < run.end) {
+                if (MODE == kGrad && lane == 0 && more) {
                     store_wait_read<0>();
-                    fetch(u + run.step);
+                    fetch(ahead);
                 }
             }
             if (MODE == kGrad && p.column && column_nt >= 0) flush();
@@ -486,8 +526,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             __syncwarp();
         } else if constexpr (MODE <= kGrad) {
             constexpr int kCols = BN / 4 > 16 ? BN / 4 : 16;           // of a warp (BN = 32: half of the warps have none)
-            for (int u = run.at; u < run.end; u += run.step, ++ord) {
-                const Unit t = unit_of<MODE>(p, u);
+            for (; walk.next(t); ++ord) {
                 const int buf = ord & 1, row = (PAIR ? 256 : 128) * t.mt + 128 * rank + 32 * q + lane;
                 const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
                 const size_t plane = (size_t)p.M * p.F;
@@ -550,45 +589,41 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             }
         } else {
             // boxes of 32 columns and 32 rows, those of a tile in turn by the four warps that share its rows
-            int box = 0;
-            for (int u = run.at; u < run.end; u += run.step, ++ord) {
-                const Unit t = unit_of<MODE>(p, u);
-                const int buf = ord & 1, blocks = p.n / 32;
-                const int row0 = MODE == kInput ? 256 * t.mt + 128 * rank + 32 * q : 128 * t.mt + 32 * q, limit = MODE == kInput ? p.M : p.F;
+            for (; walk.next(t); ++ord) {
+                const int buf = ord & 1, blocks = p.line.n / 32, limit = t.weight ? p.F : p.M;
+                const int in_tile = 128 * rank + 32 * q, row0 = t.weight ? 128 * t.mt + 32 * q : 256 * t.mt + in_tile;
                 const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
-                const int z = p.splits == 1 ? 0 : MODE == kInput ? t.split : 2 * t.split + (int)rank;
-                const CUtensorMap* map = MODE == kWeight && p.splits == 1 ? &p.s[rank] : &p.s[0];
+                const CUtensorMap* map = !t.whole ? &p.share : t.weight ? &p.s[1 + rank] : &p.s[0];
+                const bool wide = sizeof(T) == 4 || !t.whole;
                 wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
                 tc_fence_after_sync();
 #pragma unroll 1
-                for (int b = quarter; b < blocks; b += 4, ++box) {
+                for (int b = quarter; b < blocks; b += 4) {
                     float v[32];
                     __syncwarp();
                     tmem_ld32(acc + 32 * b, reinterpret_cast<uint32_t(&)[32]>(v));
                     tmem_ld_wait();
                     if (b + 4 >= blocks) release(buf);
-                    uint32_t src = patch;
-                    if (p.wide) {                                      // rows of 128 bytes, one patch
-                        if (lane == 0) store_wait_read<0>();
-                        __syncwarp();
+                    if (lane == 0) store_wait_read<0>();
+                    __syncwarp();
+                    if (wide) {                                        // rows of 128 bytes
 #pragma unroll
                         for (int c = 0; c < 8; ++c) st_shared4(patch + 128 * lane + ((c ^ (lane & 7)) << 4), pack16<float>(v + 4 * c));
-                    } else if constexpr (sizeof(T) == 2) {             // rows of 64 bytes, two patches in turn
-                        src += kHalfPatch * (box & 1);
-                        if (lane == 0) store_wait_read<1>();
-                        __syncwarp();
+                    } else if constexpr (sizeof(T) == 2) {             // rows of 64 bytes
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) st_shared4(src + 64 * lane + ((c ^ ((lane >> 1) & 3)) << 4), pack16<T>(v + 8 * c));
+                        for (int c = 0; c < 4; ++c) st_shared4(patch + 64 * lane + ((c ^ ((lane >> 1) & 3)) << 4), pack16<T>(v + 8 * c));
                     }
                     fence_proxy_async();
                     __syncwarp();
-                    const int c0 = p.n * t.nt + 32 * b;
-                    if (lane == 0) {
-                        if (row0 < limit && c0 < p.C) tma_store_3d(map, c0, row0, z, src);
+                    const int c0 = p.line.n * t.nt + 32 * b;
+                    if (lane == 0 && row0 < limit && c0 < p.C) {
+                        if (t.whole) tma_store_3d(map, c0, row0, 0, patch);
+                        else tma_store_3d(map, 32 * b, in_tile, t.slot, patch);
                         store_commit();
                     }
                 }
                 if (quarter >= blocks) release(buf);
+                __syncwarp();
             }
             if (lane == 0) store_wait_read<0>();
             __syncwarp();
@@ -598,8 +633,8 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
     __syncthreads();
     if (PAIR) {
         cluster_sync();                                               // the other block's instructions read this one's memory
-        if (warp == 0) tmem_dealloc_pair<512>(pp.tmem);
-    } else if (warp == 0) {
+        if (warp == kEpiWarps) tmem_dealloc_pair<512>(pp.tmem);
+    } else if (warp == kEpiWarps) {
         tmem_dealloc<512>(pp.tmem);
     }
 }
@@ -618,21 +653,6 @@ __global__ void __launch_bounds__(256) split_terms_kernel(const __grid_constant_
     float f[8];
     load8<float>(p.src[blockIdx.y] + i, f);
     store_operand8<float>(p.dst[blockIdx.y], n, i, f);
-}
-
-// Sum of `splits` arrays of n fp32 values (a multiple of four) in their order; values from `first` on go to out1
-template <typename T> __global__ void __launch_bounds__(256) gated_sum_kernel(const float* part, int splits, size_t n, size_t first, T* out0, T* out1) {
-    pdl_wait_prior();
-    pdl_release_next();
-    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= n) return;
-    float4 v = *reinterpret_cast<const float4*>(part + i);
-    for (int s = 1; s < splits; ++s) {
-        const float4 w = *reinterpret_cast<const float4*>(part + s * n + i);
-        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-    }
-    T* dst = i < first ? out0 + i : out1 + (i - first);
-    dst[0] = Elem<T>::from_f32(v.x); dst[1] = Elem<T>::from_f32(v.y); dst[2] = Elem<T>::from_f32(v.z); dst[3] = Elem<T>::from_f32(v.w);
 }
 
 // Column sums of dG and dU: a block takes 64 columns of one of them and a run of rows
@@ -665,37 +685,98 @@ template <typename T> __global__ void __launch_bounds__(256) gated_column_kernel
     }
 }
 
-// Shares of the column sums that kGrad left (gated_kernel's order of units), in that order
-template <typename T> __global__ void __launch_bounds__(256) gated_column_sum_kernel(const float* part, int F, int tiles_m, int units, int count, T* out0, T* out1) {
+// What is left after kProducts, always in the same order.  The first blocks: sums of the columns of dG and dU (32 of the 2 F each) over the shares
+// that kGrad left (those of a column range are the pairs' that had it), or over `runs` rows of gated_column_kernel.  The others: 32 rows of a
+// tile that no pair had whole: sum of its shares.
+struct FinishArgs {
+    const float *share, *column;
+    void *dx, *dwg, *dwu, *dbg, *dbu;
+    GatedLine line;
+    int M, C, F;
+    int column_blocks, runs, tiles_m, units, count;      // column sums
+};
+template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel(const __grid_constant__ FinishArgs p) {
+    __shared__ float s_sum[8][32];
     pdl_wait_prior();
     pdl_release_next();
-    const int lane = threadIdx.x & 31, i = (blockIdx.x * 8 + (threadIdx.x >> 5)) * 8 + (lane & 7);          // a warp: eight columns, four shares at a time
-    if ((i & ~7) >= 2 * F) return;
-    const int op = i >= F, f = i - op * F, nt = f / 128;
-    const int first = (int)((((long long)nt * tiles_m + 1) * count - 1) / units), last = (int)((((long long)(nt + 1) * tiles_m) * count - 1) / units);
-    float v = 0.f;
-    for (int s = lane >> 3; s < 8 * (last - first + 1); s += 4) v += part[(size_t)s * 2 * F + i];
-    v += __shfl_xor_sync(0xffffffffu, v, 8);
-    v += __shfl_xor_sync(0xffffffffu, v, 16);
-    if (lane < 8) (op ? out1 : out0)[f] = Elem<T>::from_f32(v);
+    const int r = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if ((int)blockIdx.x < p.column_blocks) {
+        const int i = 32 * blockIdx.x + lane, op = i >= p.F, f = i - op * p.F;
+        float v = 0.f;
+        if (i < 2 * p.F) {
+            int slots = p.runs;
+            if (!slots) {
+                const int nt = f / 128;
+                const int first = (int)((((long long)nt * p.tiles_m + 1) * p.count - 1) / p.units), last = (int)(((long long)(nt + 1) * p.tiles_m * p.count - 1) / p.units);
+                slots = 8 * (last - first + 1);
+            }
+#pragma unroll 4
+            for (int s = r; s < slots; s += 8) v += p.column[(size_t)s * 2 * p.F + i];
+        }
+        s_sum[r][lane] = v;
+        __syncthreads();
+        if (r == 0 && i < 2 * p.F) {
+#pragma unroll
+            for (int k = 1; k < 8; ++k) v += s_sum[k][lane];
+            static_cast<T*>(op ? p.dbu : p.dbg)[f] = Elem<T>::from_f32(v);
+        }
+        return;
+    }
+    const GatedLine& l = p.line;
+    const int block = blockIdx.x - p.column_blocks, tile = block >> 3, row0 = 32 * (block & 7) + r;
+    const bool weight = tile >= l.tiles_x;
+    const int chunks = weight ? l.chunks_w : l.chunks_x, own = weight ? tile - l.tiles_x : tile, mt = own / l.tiles_n, nt = own - mt * l.tiles_n;
+    __shared__ int s_pairs[3];
+    if (threadIdx.x == 0) {                              // (divisions of 64 bits)
+        const long long begin = (weight ? (long long)l.tiles_x * l.chunks_x : 0ll) + (long long)own * chunks;
+        s_pairs[0] = l.pair_of(begin);
+        s_pairs[1] = l.pair_of(begin + chunks - 1);
+        s_pairs[2] = l.begin(s_pairs[0]) < begin;        // the first pair's run begins before the tile: its other slot
+    }
+    __syncthreads();
+    const int first = s_pairs[0], last = s_pairs[1];
+    if (first == last) return;                           // a pair had it whole
+    const int limit = weight ? p.F - 128 * mt : p.M - 256 * mt;
+    for (int j = 4 * lane; j < l.n; j += 128) {
+        const int c = l.n * nt + j;
+        if (c >= p.C) break;
+        const float* src = p.share + ((size_t)(2 * first + s_pairs[2]) * 256 + row0) * l.n + j;
+        float4 v[4];                                     // four rows
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float4*>(src + (size_t)(8 * i) * l.n);
+        src = p.share + ((size_t)(2 * first + 2) * 256 + row0) * l.n + j;
+#pragma unroll 2
+        for (int q = first + 1; q <= last; ++q, src += (size_t)512 * l.n) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 w = *reinterpret_cast<const float4*>(src + (size_t)(8 * i) * l.n);
+                v[i].x += w.x; v[i].y += w.y; v[i].z += w.z; v[i].w += w.w;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = row0 + 8 * i, in_tile = weight ? row & 127 : row;
+            if (in_tile >= limit) continue;
+            T* out = static_cast<T*>(!weight ? p.dx : row < 128 ? p.dwg : p.dwu) + (size_t)(weight ? 128 * mt + in_tile : 256 * mt + row) * p.C + c;
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out) = v[i];
+            else *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(v[i].x, v[i].y), pack2<T>(v[i].z, v[i].w));
+        }
+    }
 }
 
-// Work of the two products with a long sum: tiles of at most 256 columns, split while pairs of SMs are left without one
-struct GatedSplit { int tiles_m, tiles_n, n, chunks, splits; };
-GatedSplit plan_split(int tiles_m, int chunks, int C, int sm_count) {
-    GatedSplit s;
-    s.tiles_m = tiles_m;
-    s.tiles_n = (C + 255) / 256;
-    s.n = ((C + s.tiles_n - 1) / s.tiles_n + 31) / 32 * 32;
-    s.chunks = chunks;
-    const long long tiles = (long long)tiles_m * s.tiles_n, pairs = sm_count / 2;
-    s.splits = tiles < pairs ? (int)(pairs / tiles) : 1;
-    if (s.splits > chunks / 4) s.splits = chunks / 4;
-    if (s.splits < 1) s.splits = 1;
-    return s;
+// Tiles of at most 256 columns; at least six chunks a pair
+GatedLine plan_line(int M, int C, int F, bool dx, bool dw, int sm_count) {
+    GatedLine l;
+    l.tiles_n = (C + 255) / 256;
+    l.n = ((C + l.tiles_n - 1) / l.tiles_n + 31) / 32 * 32;
+    l.tiles_x = dx ? (M + 255) / 256 * l.tiles_n : 0;
+    l.chunks_x = 2 * ((F + 63) / 64);
+    l.tiles_w = dw ? (F + 127) / 128 * l.tiles_n : 0;
+    l.chunks_w = (M + 63) / 64;
+    const long long most = (l.length() + 5) / 6;
+    l.pairs = (int)(most < sm_count / 2 ? most : sm_count / 2);
+    return l;
 }
-GatedSplit plan_input(int M, int C, int F, int sm_count) { return plan_split((M + 255) / 256, 2 * ((F + 63) / 64), C, sm_count); }
-GatedSplit plan_weight(int M, int C, int F, int sm_count) { return plan_split((F + 127) / 128, (M + 63) / 64, C, sm_count); }
 
 // G and U: 128 hidden units a tile of 256 rows for a pair of blocks; where that leaves SMs without work, tiles of 128 rows and fewer units
 struct GatedTiles { int bn, tiles_m, tiles_n, blocks; };
@@ -719,8 +800,8 @@ int column_slots(const GatedTiles& t) {
     return 8 * (runs < t.tiles_m ? runs : t.tiles_m);
 }
 
-// Workspace: terms of X, Wg, Wu (fp32) | dG | dU | shares of dX, dW, of the column sums
-struct GatedWs { size_t x, wg, wu, dg, du, dx, dw, db, total; };
+// Workspace: terms of X, Wg, Wu (fp32) | dG | dU | shares of tiles of dX and the weights' gradients, of the column sums
+struct GatedWs { size_t x, wg, wu, dg, du, share, db, total; };
 GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count) {
     GatedWs w;
     size_t at = 0;
@@ -729,15 +810,13 @@ GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count
     w.x = take(terms * M * C * 2);
     w.wg = take(terms * F * C * 2);
     w.wu = take(terms * F * C * 2);
-    w.dg = w.du = w.dx = w.dw = w.db = at;
+    w.dg = w.du = w.share = w.db = at;
     if (backward) {
         const size_t planes = (dtype == kF32 ? 3 : 1) * (size_t)M * F * 2;
         w.dg = take(planes);
         w.du = take(planes);
-        const GatedSplit in = plan_input(M, C, F, sm_count), we = plan_weight(M, C, F, sm_count);
         const GatedTiles t = plan_tiles(M, F, sm_count);
-        w.dx = take(in.splits > 1 ? (size_t)in.splits * M * C * 4 : 0);
-        w.dw = take(we.splits > 1 ? (size_t)we.splits * 2 * F * C * 4 : 0);
+        w.share = take((size_t)(sm_count / 2) * 2 * 256 * plan_line(M, C, F, true, true, sm_count).n * 4);
         const size_t slots = dtype != kF32 && t.bn == 128 ? column_slots(t) : (M + kColRows - 1) / kColRows;
         w.db = take(slots * 2 * F * 4);
     }
@@ -745,16 +824,16 @@ GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count
     return w;
 }
 
-// Map of [z][rows][cols] elements of `unit` bytes (rows a multiple of 16 bytes); the swizzle spans a row of the box
-bool make_box_map(CUtensorMap* out, const void* base, int unit, uint64_t zs, uint64_t rows, uint64_t cols, uint32_t box_cols, uint32_t box_rows) {
+// Map of [z][rows][cols] elements of `unit` bytes (rows a multiple of 16 bytes) in boxes of 32 x 32; the swizzle spans a row of the box
+bool make_box_map(CUtensorMap* out, const void* base, int unit, uint64_t zs, uint64_t rows, uint64_t cols) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
     const cuuint64_t dims[3] = {cols, rows, zs};
     const cuuint64_t strides[2] = {unit * cols, rows * unit * cols};
-    const cuuint32_t box[3] = {box_cols, box_rows, 1};
+    const cuuint32_t box[3] = {32, 32, 1};
     const cuuint32_t estr[3] = {1, 1, 1};
     return fn(out, unit == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(base), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols * unit == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, unit == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -805,15 +884,16 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     a.bg = c.bg; a.bu = c.bu; a.dh = c.dh;
     a.status = c.status;
     const GatedTiles t = plan_tiles(c.M, c.F, c.sm_count);
-    a.tiles_m = t.tiles_m; a.tiles_n = t.tiles_n; a.splits = 1; a.chunks = (c.C + 63) / 64;
+    a.tiles_m = t.tiles_m; a.tiles_n = t.tiles_n; a.chunks = (c.C + 63) / 64;
     a.out0 = c.dh ? ws + w.dg : static_cast<char*>(c.h);
     a.out1 = ws + w.du;
     const bool fused_columns = c.dbg && !kWide && t.bn == 128;
-    a.column = fused_columns ? reinterpret_cast<float*>(ws + w.db) : nullptr;
+    float* column = reinterpret_cast<float*>(ws + w.db);
+    a.column = fused_columns ? column : nullptr;
     if (!make_map_3d_u16(&a.a[0], x, kTerms, c.M, c.C, 128) || !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, t.bn) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, t.bn)) return cudaErrorInvalidValue;
     if (!kWide && t.bn == 128) {
-        if (!make_box_map(&a.s[0], a.out0, 2, 1, c.M, c.F, 32, 32)) return cudaErrorInvalidValue;
-        if (c.dh && (!make_box_map(&a.s[1], a.out1, 2, 1, c.M, c.F, 32, 32) || !make_box_map(&a.g, c.dh, 2, 1, c.M, c.F, 32, 32))) return cudaErrorInvalidValue;
+        if (!make_box_map(&a.s[0], a.out0, 2, 1, c.M, c.F)) return cudaErrorInvalidValue;
+        if (c.dh && (!make_box_map(&a.s[1], a.out1, 2, 1, c.M, c.F) || !make_box_map(&a.g, c.dh, 2, 1, c.M, c.F))) return cudaErrorInvalidValue;
     }
     e = c.dh ? launch_projections<T, kGrad>(a, t, st) : launch_projections<T, kForward>(a, t, st);
     if (e != cudaSuccess) return e;
@@ -821,48 +901,40 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     if (!c.dh) return cudaSuccess;
 
     const void *dg = ws + w.dg, *du = ws + w.du;
-    const int pairs = c.sm_count / 2;
-    auto sum = [&](const float* part, int splits, size_t n, size_t first, void* out0, void* out1) {
-        ++*launches;
-        return launch_dependent(gated_sum_kernel<T>, dim3((unsigned)((n + 1023) / 1024)), 256, 0, st, part, splits, n, first, static_cast<T*>(out0), static_cast<T*>(out1));
-    };
-    auto product = [&](const GatedSplit& s) {
-        a.tiles_m = s.tiles_m; a.tiles_n = s.tiles_n; a.n = s.n; a.splits = s.splits; a.chunks = s.chunks;
-        a.wide = kWide || s.splits > 1;
-        const long long units = (long long)s.tiles_m * s.tiles_n * s.splits;
-        return 2 * (int)(units < pairs ? units : pairs);
-    };
-    if (c.dx) {
-        const GatedSplit s = plan_input(c.M, c.C, c.F, c.sm_count);
-        const int blocks = product(s);
-        float* part = reinterpret_cast<float*>(ws + w.dx);
-        if (!make_map_3d_u16(&a.a[0], dg, kTerms, c.M, c.F, 128) || !make_map_3d_u16(&a.a[1], du, kTerms, c.M, c.F, 128) ||
-            !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, 64) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, 64) ||
-            !make_box_map(&a.s[0], s.splits > 1 ? part : c.dx, a.wide ? 4 : 2, s.splits, c.M, c.C, 32, 32)) return cudaErrorInvalidValue;
-        if ((e = launch_mode<T, kInput, 128>(a, blocks, st)) != cudaSuccess) return e;
-        ++*launches;
-        if (s.splits > 1 && (e = sum(part, s.splits, (size_t)c.M * c.C, (size_t)c.M * c.C, c.dx, nullptr)) != cudaSuccess) return e;
-    }
-    if (c.dwg) {
-        const GatedSplit s = plan_weight(c.M, c.C, c.F, c.sm_count);
-        const int blocks = product(s);
-        float* part = reinterpret_cast<float*>(ws + w.dw);
-        if (!make_map_3d_u16(&a.a[0], dg, kTerms, c.M, c.F, 64) || !make_map_3d_u16(&a.a[1], du, kTerms, c.M, c.F, 64) || !make_map_3d_u16(&a.b[0], x, kTerms, c.M, c.C, 64) ||
-            !make_box_map(&a.s[0], s.splits > 1 ? part : c.dwg, a.wide ? 4 : 2, s.splits > 1 ? 2 * s.splits : 1, c.F, c.C, 32, 32) ||
-            (s.splits == 1 && !make_box_map(&a.s[1], c.dwu, a.wide ? 4 : 2, 1, c.F, c.C, 32, 32))) return cudaErrorInvalidValue;
-        if ((e = launch_mode<T, kWeight, 128>(a, blocks, st)) != cudaSuccess) return e;
-        ++*launches;
-        if (s.splits > 1 && (e = sum(part, s.splits, 2 * (size_t)c.F * c.C, (size_t)c.F * c.C, c.dwg, c.dwu)) != cudaSuccess) return e;
-    }
+    FinishArgs f;
+    memset(&f, 0, sizeof(f));
+    f.dx = c.dx; f.dwg = c.dwg; f.dwu = c.dwu; f.dbg = c.dbg; f.dbu = c.dbu;
+    f.M = c.M; f.C = c.C; f.F = c.F;
+    f.column = column;
     if (c.dbg) {
-        float* part = reinterpret_cast<float*>(ws + w.db);
-        ++*launches;
-        if (fused_columns)
-            return launch_dependent(gated_column_sum_kernel<T>, dim3((2 * c.F + 63) / 64), 256, 0, st, part, c.F, t.tiles_m, t.tiles_m * t.tiles_n, t.blocks / 2, static_cast<T*>(c.dbg), static_cast<T*>(c.dbu));
-        const int runs = (c.M + kColRows - 1) / kColRows;
-        if ((e = launch_dependent(gated_column_kernel<T>, dim3((c.F + 63) / 64, 2, runs), 256, 0, st, dg, du, c.M, c.F, part)) != cudaSuccess) return e;
-        if ((e = sum(part, runs, 2 * (size_t)c.F, c.F, c.dbg, c.dbu)) != cudaSuccess) return e;
+        f.column_blocks = (2 * c.F + 31) / 32;
+        f.tiles_m = t.tiles_m; f.units = t.tiles_m * t.tiles_n; f.count = t.blocks / 2;
+        if (!fused_columns) {
+            f.runs = (c.M + kColRows - 1) / kColRows;
+            if ((e = launch_dependent(gated_column_kernel<T>, dim3((c.F + 63) / 64, 2, f.runs), 256, 0, st, dg, du, c.M, c.F, column)) != cudaSuccess) return e;
+            ++*launches;
+        }
     }
+    f.line = a.line = plan_line(c.M, c.C, c.F, c.dx != nullptr, c.dwg != nullptr, c.sm_count);
+    float* share = reinterpret_cast<float*>(ws + w.share);
+    f.share = share;
+    int shared_tiles = 0;
+    if (a.line.pairs) {
+        const GatedLine& l = a.line;
+        const int unit = kWide ? 4 : 2;
+        if (!make_map_3d_u16(&a.a[0], dg, kTerms, c.M, c.F, 128) || !make_map_3d_u16(&a.a[1], du, kTerms, c.M, c.F, 128) ||
+            !make_map_3d_u16(&a.w[0], dg, kTerms, c.M, c.F, 64) || !make_map_3d_u16(&a.w[1], du, kTerms, c.M, c.F, 64) ||
+            !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, 64) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, 64) || !make_map_3d_u16(&a.x, x, kTerms, c.M, c.C, 64) ||
+            (c.dx && !make_box_map(&a.s[0], c.dx, unit, 1, c.M, c.C)) ||
+            (c.dwg && (!make_box_map(&a.s[1], c.dwg, unit, 1, c.F, c.C) || !make_box_map(&a.s[2], c.dwu, unit, 1, c.F, c.C))) ||
+            !make_box_map(&a.share, share, 4, 2 * l.pairs, 256, l.n)) return cudaErrorInvalidValue;
+        if ((e = launch_mode<T, kProducts, 128>(a, 2 * l.pairs, st)) != cudaSuccess) return e;
+        ++*launches;
+        shared_tiles = l.tiles_x + l.tiles_w;
+    }
+    const long long blocks = f.column_blocks + 8ll * shared_tiles;
+    if ((e = launch_dependent(gated_finish_kernel<T>, dim3((unsigned)blocks), 256, 0, st, f)) != cudaSuccess) return e;
+    ++*launches;
     return cudaSuccess;
 }
 
