@@ -3,7 +3,7 @@
 //     G = X Wg^T + bg,  U = X Wu^T + bu,  H = act(G) o U                       X [M][C], Wg and Wu [F][C], H [M][F]
 //     dU = dH o act(G),  dG = dH o U o act'(G);  dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X,  biases: column sums
 //
-// One pipelined product in three forms: a TMA warp fills a ring of operand tiles, one warp issues `tcgen05.mma` into two accumulators in tensor
+// One pipelined product in three forms: two TMA warps fill a ring of operand tiles, one warp issues `tcgen05.mma` into two accumulators in tensor
 // memory that take turns, sixteen warps read the finished one and do the rest.  A pair of blocks (cta_group::2) has a tile of 256 rows.
 //   kForward   256 rows of 128 hidden units of G and U: one block of the pair holds a tile of Wg, the other one of Wu, so that one instruction of 256
 //              columns makes both; the epilogue applies biases, activation and product.  G and U never leave the chip.
@@ -25,7 +25,7 @@ namespace aa {
 namespace {
 
 enum GatedMode { kForward, kGrad, kProducts };
-constexpr int kEpiWarps = 16, kThreads = 32 * (kEpiWarps + 2);
+constexpr int kEpiWarps = 16, kThreads = 32 * (kEpiWarps + 3);
 constexpr int kATile = 128 * 128;                      // bytes of a [128][64] (or [64][128]) tile of 16-bit elements
 constexpr int kHalfPatch = 2048;                       // bytes of a warp's staged box of 32 x 32 16-bit values (fp32: two)
 constexpr int kTimeoutTile = 3, kTimeoutRole = 6;
@@ -276,12 +276,13 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
     Walk<MODE> walk(p, who, count);
     Work t;
 
-    if (warp == kEpiWarps) {
-        // ------------------------------------------------------------------ producer
+    if (warp == kEpiWarps || warp == kEpiWarps + 2) {
+        // ------------------------------------------------------------------ producers: one of A, one of B (a warp issues a load in some 130 cycles)
+        const bool of_b = warp != kEpiWarps;
         int stage = 0, round = 0;
         const int half_n = p.line.n / 2, boxes = MODE <= kGrad ? 0 : (half_n + 63) / 64;       // of 64 columns
         const uint32_t bytes = MODE <= kGrad ? S::kStage : kATile + boxes * 8192;              // of this block's share
-        const uint32_t full0 = PAIR ? in_block(pipe_bar(pp, BAR_FULL), 0) : pipe_bar(pp, BAR_FULL);
+        const uint32_t full0 = PAIR ? in_block(pipe_bar(pp, BAR_FULL), 0) : pipe_bar(pp, BAR_FULL), elected = elect_lane();
         bool alive = true;
         while (alive && walk.next(t)) {
             for (int pair = 0; pair < kPairs; ++pair) {
@@ -293,26 +294,27 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                         if (pipe_dead(pp)) { alive = false; break; }
                     }
                     const uint32_t bar = full0 + 8 * stage, da = base + 1024 + stage * S::kStage, db = da + kATile;
-                    if (rank == 0) mbar_arrive_expect_tx_w(pipe_bar(pp, BAR_FULL + stage), (PAIR ? 2 : 1) * bytes);
-                    if constexpr (MODE <= kGrad) {
-                        tma_load_3d_w<PAIR>(da, &p.a[0], 64 * k, (PAIR ? 256 : 128) * t.mt + 128 * rank, ta, bar);
-                        if (PAIR) {
-                            tma_load_3d_w<PAIR>(db, &p.b[rank], 64 * k, BN * t.nt, tb, bar);    // one block has the gate's rows, the other the rest
+                    const int op = MODE == kProducts && !t.weight && k >= chunks_f, kk = k - op * chunks_f;
+                    if (!of_b) {
+                        if (rank == 0) mbar_arrive_expect_tx_e(elected, pipe_bar(pp, BAR_FULL + stage), (PAIR ? 2 : 1) * bytes);
+                        if (MODE == kProducts && t.weight) {                                    // one block has dG's columns, the other dU's
+                            tma_load_3d_e<PAIR>(elected, da, &p.w[rank], 128 * t.mt, 64 * k, ta, bar);
+                            tma_load_3d_e<PAIR>(elected, da + 8192, &p.w[rank], 128 * t.mt + 64, 64 * k, ta, bar);
                         } else {
-                            tma_load_3d_w<PAIR>(db, &p.b[0], 64 * k, BN * t.nt, tb, bar);
-                            tma_load_3d_w<PAIR>(db + BN * 128, &p.b[1], 64 * k, BN * t.nt, tb, bar);
+                            tma_load_3d_e<PAIR>(elected, da, &p.a[op], 64 * kk, (PAIR ? 256 : 128) * t.mt + 128 * rank, ta, bar);
+                        }
+                    } else if constexpr (MODE <= kGrad) {
+                        if (PAIR) {
+                            tma_load_3d_e<PAIR>(elected, db, &p.b[rank], 64 * k, BN * t.nt, tb, bar);     // one block has the gate's rows, the other the rest
+                        } else {
+                            tma_load_3d_e<PAIR>(elected, db, &p.b[0], 64 * k, BN * t.nt, tb, bar);
+                            tma_load_3d_e<PAIR>(elected, db + BN * 128, &p.b[1], 64 * k, BN * t.nt, tb, bar);
                         }
                     } else {
-                        const int c0 = p.line.n * t.nt + half_n * rank, op = !t.weight && k >= chunks_f, kk = k - op * chunks_f;
-                        const CUtensorMap* mb = t.weight ? &p.x : &p.b[op];
-                        if (t.weight) {                                                         // one block has dG's columns, the other dU's
-                            tma_load_3d_w<PAIR>(da, &p.w[rank], 128 * t.mt, 64 * k, ta, bar);
-                            tma_load_3d_w<PAIR>(da + 8192, &p.w[rank], 128 * t.mt + 64, 64 * k, ta, bar);
-                        } else {
-                            tma_load_3d_w<PAIR>(da, &p.a[op], 64 * kk, 256 * t.mt + 128 * rank, ta, bar);
-                        }
-                        tma_load_3d_w<PAIR>(db, mb, c0, 64 * kk, tb, bar);
-                        if (boxes > 1) tma_load_3d_w<PAIR>(db + 8192, mb, c0 + 64, 64 * kk, tb, bar);
+                        const int c0 = p.line.n * t.nt + half_n * rank;
+                        const CUtensorMap* map = t.weight ? &p.x : &p.b[op];
+                        tma_load_3d_e<PAIR>(elected, db, map, c0, 64 * kk, tb, bar);
+                        if (boxes > 1) tma_load_3d_e<PAIR>(elected, db + 8192, map, c0 + 64, 64 * kk, tb, bar);
                     }
                     if (++stage == kStages) { stage = 0; ++round; }
                 }

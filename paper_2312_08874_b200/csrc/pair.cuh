@@ -87,29 +87,25 @@ __device__ __forceinline__ void umma_commit_first(uint32_t elected, uint32_t bar
         "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
         "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(bar), "r"(elected) : "memory");
 }
-// 3-D tiled load into this block's memory, issued by one elected lane of a warp in uniform control flow (every operand of a load inside an
-// `if (lane == 0)` region takes a detour: 100 ns a load, against 20 this way).  PAIR: it reports to an mbarrier of either block of the pair (a
-// shared::cluster address).
-template <bool PAIR> __device__ __forceinline__ void tma_load_3d_w(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+// 3-D tiled load into this block's memory by the elected lane of a warp in uniform control flow (every operand of a load inside an
+// `if (lane == 0)` region takes a detour).  PAIR: it reports to an mbarrier of either block of the pair (a shared::cluster address).
+template <bool PAIR> __device__ __forceinline__ void tma_load_3d_e(uint32_t elected, uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
     if constexpr (PAIR)
         asm volatile(
-            "{\n\t.reg .pred q;\n\t"
-            "elect.sync _|q, 0xffffffff;\n\t"
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
             "@q cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}\n"
-            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(elected) : "memory");
     else
         asm volatile(
-            "{\n\t.reg .pred q;\n\t"
-            "elect.sync _|q, 0xffffffff;\n\t"
+            "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
             "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}\n"
-            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(elected) : "memory");
 }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory"); }
-__device__ __forceinline__ void mbar_arrive_expect_tx_w(uint32_t bar, uint32_t bytes) {
+__device__ __forceinline__ void mbar_arrive_expect_tx_e(uint32_t elected, uint32_t bar, uint32_t bytes) {
     asm volatile(
-        "{\n\t.reg .pred q;\n\t"
-        "elect.sync _|q, 0xffffffff;\n\t"
-        "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}\n" ::"r"(bar), "r"(bytes) : "memory");
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+        "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}\n" ::"r"(bar), "r"(bytes), "r"(elected) : "memory");
 }
 
 // 3-D tiled store of a staged box (what lies outside the tensor is left out), and this thread's groups of stores
