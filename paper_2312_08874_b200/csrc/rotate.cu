@@ -6,11 +6,13 @@
 // result and R the rotation: g' = R^T g, xh = x r, r = 1 / sqrt(mean(x^2) + eps):  dx = r (g' gain - xh mean(g' gain xh)),
 // dgain = sum of g' xh over batch, heads and tokens.
 //
-// A group of lanes owns a token: a lane has 16 bytes of channels and keeps their cosines and sines (with the gains folded in) for all
-// heads, batch entries and both tensors that the block visits, so that an angle is computed once for many rows.  The angle is taken in
-// turns: p f / (2 pi) with its rounding error by fma, less its nearest integer, so that large positions cost no accuracy; the partner of a
-// channel comes from the lane itself (neighbouring channels as pairs), from another lane by a shuffle (halves of a segment, of whole
-// 16-byte pieces) or through shared memory (halves of any other size).
+// A group of lanes owns a token: a lane has 16 bytes of channels and keeps their cosines and sines (forward: with the gains folded in) for all
+// heads and batch entries that the block visits, so that an angle is computed once for many rows.  The angle is taken in turns: p f / (2 pi) with
+// its rounding error by fma, less its nearest integer, so that large positions cost no accuracy.  The partner of a channel comes from the lane
+// itself (neighbouring channels as pairs), from another lane by a shuffle (halves of a segment, of whole 16-byte pieces; the two lanes share the work
+// of their angles) or through shared memory (halves of any other size).  The next rows are loaded before the present ones are worked on.
+// Bound by HBM: forward 2 x 16-bit, backward 10 bytes an element (16-bit types); everything else is in the way of that: angles, unpacking,
+// offsets and the rows in flight.
 #include "common.cuh"
 #include "kernels.h"
 
@@ -21,9 +23,9 @@ namespace {
 constexpr int kRotThreads = 256, kRotWarps = kRotThreads / 32;
 enum PairKind { kNeighbours, kHalvesShuffle, kHalvesShared };
 
-// What a lane knows of its C channels: frequency in turns (two terms), axis and partner of each.
-template <int C, bool NEIGHBOURS> struct LaneAngles {
-    static constexpr int kAngles = NEIGHBOURS ? C / 2 : C;
+// What a lane knows of its C channels: frequency in turns (two terms) and axis of the angles that it computes, partners.
+template <int C, PairKind KIND> struct LaneAngles {
+    static constexpr int kAngles = KIND == kHalvesShared ? C : C / 2;      // (shuffle: the partner lane computes the other half)
     float hi[kAngles], lo[kAngles];
     unsigned axis;                        // two bits an angle
     unsigned rotated;                     // a bit a channel: it has a partner
@@ -31,43 +33,53 @@ template <int C, bool NEIGHBOURS> struct LaneAngles {
     unsigned char partner[C];             // its partner's channel
 };
 
-template <int C, bool NEIGHBOURS> __device__ __forceinline__ void lane_angles(const RotateArgs& p, int c0, LaneAngles<C, NEIGHBOURS>& la) {
+template <int C, PairKind KIND> __device__ __forceinline__ void lane_angles(const RotateArgs& p, int c0, LaneAngles<C, KIND>& la) {
     la.axis = la.rotated = la.second = 0;
+    int freq[C], axes[C];
 #pragma unroll
     for (int j = 0; j < C; ++j) {
         const int c = c0 + j;
-        int at = 0, fr = 0, f = -1, axis = 0, partner = c;
+        int at = 0, fr = 0, partner = c;
         bool second = false;
+        freq[j] = -1;
+        axes[j] = 0;
 #pragma unroll
         for (int a = 0; a < 3; ++a) {
             const int seg = p.channels[a], half = seg >> 1, o = c - at;
             if (o >= 0 && o < seg) {
-                axis = a;
-                if (NEIGHBOURS) { f = fr + (o >> 1); second = o & 1; partner = c ^ 1; }
-                else { second = o >= half; f = fr + (second ? o - half : o); partner = second ? c - half : c + half; }
+                axes[j] = a;
+                if (KIND == kNeighbours) { freq[j] = fr + (o >> 1); second = o & 1; partner = c ^ 1; }
+                else { second = o >= half; freq[j] = fr + (second ? o - half : o); partner = second ? c - half : c + half; }
             }
             at += seg;
             fr += half;
         }
         la.partner[j] = (unsigned char)partner;
-        if (f >= 0) la.rotated |= 1u << j;
+        if (freq[j] >= 0) la.rotated |= 1u << j;
         if (second) la.second |= 1u << j;
-        if (!NEIGHBOURS || j % 2 == 0) {
-            constexpr float kInv = 0.15915494309189535f, kInvLo = 6.420638243e-09f;     // 1 / (2 pi) as a sum of two fp32 numbers
-            const int i = NEIGHBOURS ? j / 2 : j;
-            const float w = f >= 0 ? __ldg(p.freq + f) : 0.f;
-            la.hi[i] = w * kInv;
-            la.lo[i] = fmaf(w, kInv, -la.hi[i]) + w * kInvLo;
-            la.axis |= (unsigned)axis << (2 * i);
-        }
+    }
+#pragma unroll
+    for (int i = 0; i < LaneAngles<C, KIND>::kAngles; ++i) {
+        constexpr float kInv = 0.15915494309189535f, kInvLo = 6.420638243e-09f;     // 1 / (2 pi) as a sum of two fp32 numbers
+        int f = freq[KIND == kNeighbours ? 2 * i : i], a = axes[KIND == kNeighbours ? 2 * i : i];
+        if (KIND == kHalvesShuffle && la.second) { f = freq[i + C / 2]; a = axes[i + C / 2]; }
+        const float w = f >= 0 ? __ldg(p.freq + f) : 0.f;
+        la.hi[i] = w * kInv;
+        la.lo[i] = fmaf(w, kInv, -la.hi[i]) + w * kInvLo;
+        la.axis |= (unsigned)a << (2 * i);
     }
 }
 
-// cos and sin of position * frequency
-__device__ __forceinline__ void turn(float pos, float hi, float lo, float& c, float& s) {
+// cos and sin of position * frequency.  FAST (16-bit results): the special-function unit's, within 5e-7 on half a turn.
+template <bool FAST> __device__ __forceinline__ void turn(float pos, float hi, float lo, float& c, float& s) {
     const float t = pos * hi, e = fmaf(pos, lo, fmaf(pos, hi, -t));
     const float r = (t - rintf(t)) + e;
-    sincospif(2.f * r, &s, &c);
+    if (FAST) {
+        c = __cosf(6.2831853f * r);
+        s = __sinf(6.2831853f * r);
+    } else {
+        sincospif(2.f * r, &s, &c);
+    }
 }
 
 // Position of a token in a batch entry
@@ -90,205 +102,271 @@ __device__ __forceinline__ void token_position(const RotateArgs& p, int b, int t
     }
 }
 
-// Factors of a channel's own value and of its partner's
-template <int C, bool NEIGHBOURS> __device__ __forceinline__ void token_turns(const RotateArgs& p, const LaneAngles<C, NEIGHBOURS>& la, int b, int tok, bool inverse, float (&cs)[C], float (&sn)[C]) {
-    float pos[3];
+// Factors of a channel's own value and of its partner's, in pairs
+template <int C, PairKind KIND, bool FAST> __device__ __forceinline__ void token_turns(const RotateArgs& p, const LaneAngles<C, KIND>& la, int b, int tok, int partner_lane, bool inverse, float2 (&cs)[C / 2], float2 (&sn)[C / 2]) {
+    constexpr int A = LaneAngles<C, KIND>::kAngles;
+    float pos[3], c[C], s[C];
     token_position(p, b, tok, pos);
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-        const int i = NEIGHBOURS ? j / 2 : j;
-        if (NEIGHBOURS && j % 2) { cs[j] = cs[j - 1]; sn[j] = -sn[j - 1]; continue; }
+    for (int i = 0; i < A; ++i) {
         const unsigned a = la.axis >> (2 * i) & 3u;
-        float c, s;
-        turn(a == 0 ? pos[0] : a == 1 ? pos[1] : pos[2], la.hi[i], la.lo[i], c, s);
-        cs[j] = c;
-        sn[j] = ((la.second >> j & 1u) != 0) != inverse ? s : -s;
+        turn<FAST>(a == 0 ? pos[0] : a == 1 ? pos[1] : pos[2], la.hi[i], la.lo[i], c[i], s[i]);
     }
+    if constexpr (KIND == kNeighbours) {
+#pragma unroll
+        for (int i = C / 2 - 1; i >= 0; --i) { c[2 * i + 1] = c[2 * i] = c[i]; s[2 * i + 1] = s[2 * i] = s[i]; }
+    } else if constexpr (KIND == kHalvesShuffle) {
+        const bool second = la.second != 0;
+#pragma unroll
+        for (int i = 0; i < A; ++i) {
+            const float oc = __shfl_sync(0xffffffffu, c[i], partner_lane), os = __shfl_sync(0xffffffffu, s[i], partner_lane);
+            c[i + A] = second ? c[i] : oc;
+            s[i + A] = second ? s[i] : os;
+            c[i] = second ? oc : c[i];
+            s[i] = second ? os : s[i];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+        if (((la.second >> j & 1u) != 0) == inverse) s[j] = -s[j];
+#pragma unroll
+    for (int i = 0; i < C / 2; ++i) { cs[i] = make_float2(c[2 * i], c[2 * i + 1]); sn[i] = make_float2(s[2 * i], s[2 * i + 1]); }
 }
 
 // Values of the partners of this lane's channels
-template <int C, PairKind KIND> __device__ __forceinline__ void partners(const float (&x)[C], const LaneAngles<C, KIND == kNeighbours>& la, int c0, int first_lane, float* patch, float (&y)[C]) {
+template <int C, PairKind KIND> __device__ __forceinline__ void partners(const float2 (&x)[C / 2], const LaneAngles<C, KIND>& la, int c0, int first_lane, int partner_lane, float* patch, float2 (&y)[C / 2]) {
     if constexpr (KIND == kNeighbours) {
 #pragma unroll
-        for (int j = 0; j < C; ++j) y[j] = x[j ^ 1];
+        for (int i = 0; i < C / 2; ++i) y[i] = make_float2(x[i].y, x[i].x);
     } else if constexpr (KIND == kHalvesShuffle) {
-        const int src = first_lane + la.partner[0] / C;
 #pragma unroll
-        for (int j = 0; j < C; ++j) y[j] = __shfl_sync(0xffffffffu, x[j], src);
+        for (int i = 0; i < C / 2; ++i) y[i] = make_float2(__shfl_sync(0xffffffffu, x[i].x, partner_lane), __shfl_sync(0xffffffffu, x[i].y, partner_lane));
     } else {
         const int row = first_lane * C;
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < C; ++j) patch[row + c0 + j] = x[j];
+        for (int i = 0; i < C / 2; ++i) *reinterpret_cast<float2*>(patch + row + c0 + 2 * i) = x[i];
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < C; ++j) y[j] = patch[row + la.partner[j]];
+        for (int i = 0; i < C / 2; ++i) y[i] = make_float2(patch[row + la.partner[2 * i]], patch[row + la.partner[2 * i + 1]]);
     }
 }
 
-template <typename T> __device__ __forceinline__ void load_vec(const T* src, bool live, float (&f)[Elem<T>::kVec]) {
+__device__ __forceinline__ uint4 load_raw(const void* src, bool live) {
     uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-    if (live) raw = *reinterpret_cast<const uint4*>(src);
-    unpack16<T>(raw, f);
+    if (live) raw = *static_cast<const uint4*>(src);
+    return raw;
+}
+template <typename T> __device__ __forceinline__ void unpack_pairs(const uint4& raw, float2 (&f)[Elem<T>::kVec / 2]) {
+    float v[Elem<T>::kVec];
+    unpack16<T>(raw, v);
+#pragma unroll
+    for (int i = 0; i < Elem<T>::kVec / 2; ++i) f[i] = make_float2(v[2 * i], v[2 * i + 1]);
 }
 
 __device__ __forceinline__ float group_sum(float v, int lanes) {
     for (int o = lanes >> 1; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+__device__ __forceinline__ float2 pair_of(float x) { return make_float2(x, x); }
+// (x turned): own values times cs, partners' times sn; a channel without a partner keeps its own
+template <int C> __device__ __forceinline__ void turned(const float2 (&x)[C / 2], float2 (&y)[C / 2], const float2 (&cs)[C / 2], const float2 (&sn)[C / 2], unsigned rotated) {
+#pragma unroll
+    for (int i = 0; i < C / 2; ++i) {
+        const float2 own = fmul2(x[i], cs[i]);
+        y[i] = ffma2(y[i], sn[i], own);
+        if (rotated != (1u << C) - 1u) {
+            if (!(rotated >> (2 * i) & 1u)) y[i].x = own.x;
+            if (!(rotated >> (2 * i + 1) & 1u)) y[i].y = own.y;
+        }
+    }
+}
+// Element offsets of a row, slab after slab
+struct RowWalk {
+    long long at, step, wrap;             // from head to head; from the last head to the next batch entry
+    __device__ RowWalk(const TokLayout& l, int slab, int heads, int tok, int c) : at(tok_offset(l, slab, heads, tok) + c), step(l.sh), wrap(l.sb - (heads - 1) * l.sh) {}
+    __device__ void next(bool last_head) { at += last_head ? wrap : step; }
+};
 
 template <typename T, PairKind KIND, bool NORM> __global__ void __launch_bounds__(kRotThreads) rotate_kernel(const __grid_constant__ RotateArgs p) {
-    constexpr int C = Elem<T>::kVec;
-    __shared__ float s_patch[KIND == kHalvesShared ? kRotWarps : 1][KIND == kHalvesShared ? 32 * C : 1];
+    constexpr int C = Elem<T>::kVec, kSets = NORM ? 2 : 1;
+    __shared__ float s_patch[KIND == kHalvesShared ? kRotWarps : 1][KIND == kHalvesShared ? 32 * C : 2];
     pdl_wait_prior();
     pdl_release_next();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = lane & (p.lanes - 1), c0 = gl * C, first_lane = lane - gl;
     const int tok = blockIdx.x * (kRotThreads / p.lanes) + threadIdx.x / p.lanes;
     const bool live = tok < p.N && c0 < p.d;
     const int unit = blockIdx.y / p.chunks, s0 = unit * p.unit_slabs + (blockIdx.y % p.chunks) * p.share, s1 = min(s0 + p.share, (unit + 1) * p.unit_slabs);
-    LaneAngles<C, KIND == kNeighbours> la;
-    lane_angles<C, KIND == kNeighbours>(p, c0, la);
-    float cs[2][C], sn[2][C];
-    token_turns<C, KIND == kNeighbours>(p, la, s0 / p.heads, min(tok, p.N - 1), p.inverse, cs[0], sn[0]);
-#pragma unroll
-    for (int j = 0; j < C; ++j) { cs[1][j] = cs[0][j]; sn[1][j] = sn[0][j]; }
+    LaneAngles<C, KIND> la;
+    lane_angles<C, KIND>(p, c0, la);
+    const int partner_lane = first_lane + la.partner[0] / C;
+    float2 cs[kSets][C / 2], sn[kSets][C / 2];
+    token_turns<C, KIND, sizeof(T) == 2>(p, la, s0 / p.heads, min(tok, p.N - 1), partner_lane, p.inverse, cs[0], sn[0]);
     if (NORM) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (p.gain[i]) {
-                const T* g = static_cast<const T*>(p.gain[i]);
+        for (int i = 0; i < C / 2; ++i) { cs[kSets - 1][i] = cs[0][i]; sn[kSets - 1][i] = sn[0][i]; }
 #pragma unroll
-                for (int j = 0; j < C; ++j)
-                    if (c0 + j < p.d) { cs[i][j] *= Elem<T>::to_f32(g[c0 + j]); sn[i][j] *= Elem<T>::to_f32(g[la.partner[j]]); }
+        for (int t = 0; t < 2; ++t)
+            if (p.gain[t] && c0 < p.d) {
+                const T* g = static_cast<const T*>(p.gain[t]);
+#pragma unroll
+                for (int i = 0; i < C / 2; ++i) {
+                    cs[t * (kSets - 1)][i] = fmul2(cs[t * (kSets - 1)][i], make_float2(Elem<T>::to_f32(g[c0 + 2 * i]), Elem<T>::to_f32(g[c0 + 2 * i + 1])));
+                    sn[t * (kSets - 1)][i] = fmul2(sn[t * (kSets - 1)][i], make_float2(Elem<T>::to_f32(g[la.partner[2 * i]]), Elem<T>::to_f32(g[la.partner[2 * i + 1]])));
+                }
             }
     }
     float* patch = s_patch[KIND == kHalvesShared ? warp : 0];
+    const T *x0 = static_cast<const T*>(p.x[0]), *x1 = static_cast<const T*>(p.x[1]);
+    RowWalk in(p.lin, s0, p.heads, tok, c0), out(p.lout, s0, p.heads, tok, c0);
+    int head = s0 % p.heads;
+    uint4 ahead[2] = {load_raw(x0 + in.at, live && x0), load_raw(x1 + in.at, live && x1)};
     for (int s = s0; s < s1; ++s) {
-        const long long in = tok_offset(p.lin, s, p.heads, tok) + c0, out = tok_offset(p.lout, s, p.heads, tok) + c0;
-        float x[2][C];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (p.x[i]) load_vec<T>(static_cast<const T*>(p.x[i]) + in, live, x[i]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (!p.x[i]) continue;
-            float r = 1.f;
-            if (NORM) {
-                float sq = 0.f;
-#pragma unroll
-                for (int j = 0; j < C; ++j) sq = fmaf(x[i][j], x[i][j], sq);
-                r = rsqrtf(group_sum(sq, p.lanes) * p.inv_d + p.eps);
-            }
-            float y[C];
-            partners<C, KIND>(x[i], la, c0, first_lane, patch, y);
-#pragma unroll
-            for (int j = 0; j < C; ++j) {
-                const float own = x[i][j] * cs[i][j];
-                y[j] = la.rotated >> j & 1u ? fmaf(y[j], sn[i][j], own) : own;
-                if (NORM) y[j] *= r;
-            }
-            if (live) *reinterpret_cast<uint4*>(static_cast<T*>(p.y[i]) + out) = pack16<T>(y);
+        const bool wrap = ++head == p.heads;
+        if (wrap) head = 0;
+        const uint4 raw[2] = {ahead[0], ahead[1]};
+        if (s + 1 < s1) {
+            in.next(wrap);
+            ahead[0] = load_raw(x0 + in.at, live && x0);
+            ahead[1] = load_raw(x1 + in.at, live && x1);
         }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            if (!p.x[t]) continue;
+            float2 x[C / 2], y[C / 2];
+            unpack_pairs<T>(raw[t], x);
+            if constexpr (KIND == kHalvesShuffle && sizeof(T) == 2) {      // (16-bit pairs as they are: half the shuffles)
+                const uint4 w = make_uint4(__shfl_sync(0xffffffffu, raw[t].x, partner_lane), __shfl_sync(0xffffffffu, raw[t].y, partner_lane),
+                                           __shfl_sync(0xffffffffu, raw[t].z, partner_lane), __shfl_sync(0xffffffffu, raw[t].w, partner_lane));
+                unpack_pairs<T>(w, y);
+            } else {
+                partners<C, KIND>(x, la, c0, first_lane, partner_lane, patch, y);
+            }
+            turned<C>(x, y, cs[t * (kSets - 1)], sn[t * (kSets - 1)], la.rotated);
+            if (NORM) {
+                float2 sq = fmul2(x[0], x[0]);
+#pragma unroll
+                for (int i = 1; i < C / 2; ++i) sq = ffma2(x[i], x[i], sq);
+                const float r = rsqrtf(group_sum(sq.x + sq.y, p.lanes) * p.inv_d + p.eps);
+#pragma unroll
+                for (int i = 0; i < C / 2; ++i) y[i] = fmul2(y[i], pair_of(r));
+            }
+            float v[C];
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) { v[2 * i] = y[i].x; v[2 * i + 1] = y[i].y; }
+            if (live) *reinterpret_cast<uint4*>(static_cast<T*>(p.y[t]) + out.at) = pack16<T>(v);
+        }
+        out.next(wrap);
     }
 }
 
-// Gradient through norm and rotation.  Blocks loop over (tile of tokens, run of slabs); gain gradients stay in registers until the block's end
-// and leave as one row of partial sums a block, which gain_sum_kernel adds up in a fixed order.
-template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThreads) rotate_backward_kernel(const __grid_constant__ RotateBwdArgs p) {
+// Gradient through norm and rotation.  A block has one of the tensors (blockIdx.y) and loops over (tile of tokens, run of slabs); the gain's gradient
+// stays in registers until the block's end and leaves as one row of sums a block, which gain_sum_kernel adds up in a fixed order.
+template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThreads, 3) rotate_backward_kernel(const __grid_constant__ RotateBwdArgs p) {
     constexpr int C = Elem<T>::kVec;
-    __shared__ float s_patch[KIND == kHalvesShared ? kRotWarps : 1][KIND == kHalvesShared ? 32 * C : 1];
+    __shared__ float s_patch[KIND == kHalvesShared ? kRotWarps : 1][KIND == kHalvesShared ? 32 * C : 2];
     __shared__ float s_sum[kRotThreads * C];
     pdl_wait_prior();
     pdl_release_next();
     const RotateArgs& f = p.fwd;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = lane & (f.lanes - 1), c0 = gl * C, first_lane = lane - gl;
-    const int groups = kRotThreads / f.lanes, tiles = (f.N + groups - 1) / groups;
-    LaneAngles<C, KIND == kNeighbours> la;
-    lane_angles<C, KIND == kNeighbours>(f, c0, la);
-    float gain[2][C], sum[2][C];
+    const int groups = kRotThreads / f.lanes, tiles = (f.N + groups - 1) / groups, t = f.x[0] ? blockIdx.y : 1;
+    LaneAngles<C, KIND> la;
+    lane_angles<C, KIND>(f, c0, la);
+    const int partner_lane = first_lane + la.partner[0] / C;
+    const T *xs = static_cast<const T*>(f.x[t]), *gs = static_cast<const T*>(f.gain[t]);
+    const float* grad = p.grad[t];
+    float* dst = static_cast<float*>(f.y[t]);
+    float2 gain[C / 2], sum[C / 2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < C; ++j) {
-            gain[i][j] = f.gain[i] && c0 + j < f.d ? Elem<T>::to_f32(static_cast<const T*>(f.gain[i])[c0 + j]) : 1.f;
-            sum[i][j] = 0.f;
-        }
+    for (int i = 0; i < C / 2; ++i) {
+        gain[i] = gs && c0 < f.d ? make_float2(Elem<T>::to_f32(gs[c0 + 2 * i]), Elem<T>::to_f32(gs[c0 + 2 * i + 1])) : pair_of(1.f);
+        sum[i] = pair_of(0.f);
+    }
     float* patch = s_patch[KIND == kHalvesShared ? warp : 0];
     const int runs = f.chunks * (f.slabs / f.unit_slabs);
     for (long long item = blockIdx.x; item < (long long)tiles * runs; item += gridDim.x) {
         const int run = (int)(item / tiles), tok = (int)(item - (long long)run * tiles) * groups + threadIdx.x / f.lanes;
         const bool live = tok < f.N && c0 < f.d;
         const int unit = run / f.chunks, s0 = unit * f.unit_slabs + (run % f.chunks) * f.share, s1 = min(s0 + f.share, (unit + 1) * f.unit_slabs);
-        float cs[C], sn[C];
-        token_turns<C, KIND == kNeighbours>(f, la, s0 / f.heads, min(tok, f.N - 1), true, cs, sn);
+        RowWalk in(f.lin, s0, f.heads, tok, c0), gin(p.lgrad, s0, f.heads, tok, c0), out(f.lout, s0, f.heads, tok, c0);
+        int head = s0 % f.heads;
+        uint4 ahead = load_raw(xs + in.at, live), gahead[C / 4];
+#pragma unroll
+        for (int i = 0; i < C / 4; ++i) gahead[i] = load_raw(grad + gin.at + 4 * i, live);
+        float2 cs[C / 2], sn[C / 2];
+        token_turns<C, KIND, false>(f, la, s0 / f.heads, min(tok, f.N - 1), partner_lane, true, cs, sn);
         for (int s = s0; s < s1; ++s) {
-            const long long at = tok_offset(f.lin, s, f.heads, tok) + c0, ga = tok_offset(p.lgrad, s, f.heads, tok) + c0, out = tok_offset(f.lout, s, f.heads, tok) + c0;
-            float x[2][C], g[2][C];
+            const bool wrap = ++head == f.heads;
+            if (wrap) head = 0;
+            float2 x[C / 2], g[C / 2], y[C / 2];
+            unpack_pairs<T>(ahead, x);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (f.x[i]) {
-                    load_vec<T>(static_cast<const T*>(f.x[i]) + at, live, x[i]);
-#pragma unroll
-                    for (int j = 0; j < C; j += 4) {
-                        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (live) v = *reinterpret_cast<const float4*>(p.grad[i] + ga + j);
-                        g[i][j] = v.x; g[i][j + 1] = v.y; g[i][j + 2] = v.z; g[i][j + 3] = v.w;
-                    }
-                }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (!f.x[i]) continue;
-                float y[C], sq = 0.f, dot = 0.f;
-                partners<C, KIND>(g[i], la, c0, first_lane, patch, y);
-#pragma unroll
-                for (int j = 0; j < C; ++j) {
-                    y[j] = la.rotated >> j & 1u ? fmaf(y[j], sn[j], g[i][j] * cs[j]) : g[i][j];
-                    sq = fmaf(x[i][j], x[i][j], sq);
-                    dot = fmaf(y[j] * gain[i][j], x[i][j], dot);
-                }
-                const float r = rsqrtf(group_sum(sq, f.lanes) * f.inv_d + f.eps);
-                const float m = group_sum(dot, f.lanes) * f.inv_d * r * r * r;
-#pragma unroll
-                for (int j = 0; j < C; ++j) {
-                    sum[i][j] = fmaf(y[j], x[i][j] * r, sum[i][j]);
-                    y[j] = fmaf(r * gain[i][j], y[j], -m * x[i][j]);
-                }
-                if (live) {
-#pragma unroll
-                    for (int j = 0; j < C; j += 4) *reinterpret_cast<float4*>(static_cast<float*>(f.y[i]) + out + j) = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
-                }
+            for (int i = 0; i < C / 4; ++i) {
+                g[2 * i] = make_float2(__uint_as_float(gahead[i].x), __uint_as_float(gahead[i].y));
+                g[2 * i + 1] = make_float2(__uint_as_float(gahead[i].z), __uint_as_float(gahead[i].w));
             }
+            if (s + 1 < s1) {
+                in.next(wrap);
+                gin.next(wrap);
+                ahead = load_raw(xs + in.at, live);
+#pragma unroll
+                for (int i = 0; i < C / 4; ++i) gahead[i] = load_raw(grad + gin.at + 4 * i, live);
+            }
+            partners<C, KIND>(g, la, c0, first_lane, partner_lane, patch, y);
+            turned<C>(g, y, cs, sn, la.rotated);
+            float2 sq = pair_of(0.f), dot = pair_of(0.f);
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) {
+                sq = ffma2(x[i], x[i], sq);
+                dot = ffma2(fmul2(y[i], gain[i]), x[i], dot);
+            }
+            const float r = rsqrtf(group_sum(sq.x + sq.y, f.lanes) * f.inv_d + f.eps);
+            const float m = -group_sum(dot.x + dot.y, f.lanes) * f.inv_d * r * r * r;
+            float4 v[C / 4];
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) {
+                sum[i] = ffma2(y[i], fmul2(x[i], pair_of(r)), sum[i]);
+                y[i] = ffma2(fmul2(gain[i], pair_of(r)), y[i], fmul2(pair_of(m), x[i]));
+            }
+#pragma unroll
+            for (int i = 0; i < C / 4; ++i) v[i] = make_float4(y[2 * i].x, y[2 * i].y, y[2 * i + 1].x, y[2 * i + 1].y);
+            if (live) {
+#pragma unroll
+                for (int i = 0; i < C / 4; ++i) *reinterpret_cast<float4*>(dst + out.at + 4 * i) = v[i];
+            }
+            out.next(wrap);
         }
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < C; ++j) s_sum[threadIdx.x * C + j] = sum[i][j];
-        __syncthreads();
-        const int width = f.lanes * C;
-        for (int c = threadIdx.x; c < f.d; c += kRotThreads) {
-            float v = 0.f;
-            for (int k = 0; k < groups; ++k) v += s_sum[k * width + c];
-            p.part[((long long)blockIdx.x * 2 + i) * f.d + c] = v;
-        }
+    for (int i = 0; i < C / 2; ++i) *reinterpret_cast<float2*>(s_sum + threadIdx.x * C + 2 * i) = sum[i];
+    __syncthreads();
+    const int width = f.lanes * C;
+    if (threadIdx.x < f.d) {
+        float v = 0.f;
+        for (int k = 0; k < groups; ++k) v += s_sum[k * width + threadIdx.x];
+        p.part[((long long)t * gridDim.x + blockIdx.x) * f.d + threadIdx.x] = v;
     }
 }
 
-// Sum of the blocks' rows: a warp per eight columns of the 2 d, four rows at a time
-__global__ void __launch_bounds__(kRotThreads) gain_sum_kernel(const float* part, int rows, int d, float* dq, float* dk) {
+// Sum of the blocks' rows: 32 columns of a tensor's d, each row's in turn by 32 warps
+__global__ void __launch_bounds__(1024) gain_sum_kernel(const float* part, int rows, int d, float* dq, float* dk) {
+    __shared__ float s_sum[32][33];
     pdl_wait_prior();
     pdl_release_next();
-    const int lane = threadIdx.x & 31, c = (blockIdx.x * kRotWarps + (threadIdx.x >> 5)) * 8 + (lane & 7);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = 32 * blockIdx.x + lane;
+    float* out = blockIdx.y ? dk : dq;
+    if (!out) return;
     float v = 0.f;
-    if (c < 2 * d)
-        for (int r = lane >> 3; r < rows; r += 4) v += part[(long long)r * 2 * d + c];
-    v += __shfl_xor_sync(0xffffffffu, v, 8);
-    v += __shfl_xor_sync(0xffffffffu, v, 16);
-    if (lane < 8 && c < 2 * d) {
-        if (c < d) { if (dq) dq[c] = v; }
-        else if (dk) dk[c - d] = v;
+    if (c < d) {
+#pragma unroll 8
+        for (int r = warp; r < rows; r += 32) v += part[((long long)blockIdx.y * rows + r) * d + c];
     }
+    s_sum[warp][lane] = v;
+    __syncthreads();
+    v = s_sum[lane][warp];
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (lane == 0 && 32 * blockIdx.x + warp < d) out[32 * blockIdx.x + warp] = v;
 }
 
 PairKind pair_kind(const RotateArgs& a, int c) {
@@ -302,18 +380,17 @@ PairKind pair_kind(const RotateArgs& a, int c) {
     return whole && at % c == 0 ? kHalvesShuffle : kHalvesShared;
 }
 
-// Lanes of a token, and how many slabs a block visits with one set of angles: as many as leave about two waves of blocks.
-void plan_rotate(RotateArgs* a, int vec, int sm_count, int* tiles) {
+// Lanes of a token, and how many slabs a block visits with one set of angles: as many as leave `blocks` blocks an SM.
+void plan_rotate(RotateArgs* a, int vec, int blocks, int sm_count, int* tiles) {
     a->lanes = 1;
     while (a->lanes * vec < a->d) a->lanes *= 2;
     const int groups = kRotThreads / a->lanes;
     *tiles = (a->N + groups - 1) / groups;
     a->unit_slabs = a->positions && a->pos_batch ? a->heads : a->slabs;
-    const long long rows = (long long)*tiles * a->slabs;
-    long long share = rows / (16ll * sm_count);
-    if (share < 1) share = 1;
-    if (share > a->unit_slabs) share = a->unit_slabs;
-    a->share = (int)share;
+    const long long alone = (long long)*tiles * (a->slabs / a->unit_slabs);         // blocks if each visits all slabs of its unit
+    long long chunks = ((long long)blocks * sm_count + alone - 1) / alone;
+    if (chunks > a->unit_slabs) chunks = a->unit_slabs;
+    a->share = (int)((a->unit_slabs + chunks - 1) / chunks);
     a->chunks = (a->unit_slabs + a->share - 1) / a->share;
     a->inv_d = 1.f / (float)a->d;
 }
@@ -324,7 +401,7 @@ template <typename T, PairKind KIND> cudaError_t launch_rotate_kind(const Rotate
 }
 template <typename T> cudaError_t launch_rotate_type(RotateArgs a, int sm_count, cudaStream_t st) {
     int tiles;
-    plan_rotate(&a, Elem<T>::kVec, sm_count, &tiles);
+    plan_rotate(&a, Elem<T>::kVec, 12, sm_count, &tiles);
     const dim3 grid(tiles, a.chunks * (a.slabs / a.unit_slabs));
     switch (pair_kind(a, Elem<T>::kVec)) {
         case kNeighbours: return launch_rotate_kind<T, kNeighbours>(a, grid, st);
@@ -332,20 +409,22 @@ template <typename T> cudaError_t launch_rotate_type(RotateArgs a, int sm_count,
         default: return launch_rotate_kind<T, kHalvesShared>(a, grid, st);
     }
 }
-int backward_blocks(int sm_count) { return 4 * sm_count; }
+int backward_blocks(int sm_count) { return 3 * sm_count; }           // of a tensor
 template <typename T> cudaError_t launch_rotate_bwd_type(RotateBwdArgs a, int sm_count, cudaStream_t st) {
     int tiles;
-    plan_rotate(&a.fwd, Elem<T>::kVec, sm_count, &tiles);
+    plan_rotate(&a.fwd, Elem<T>::kVec, 6, sm_count, &tiles);
     const long long items = (long long)tiles * a.fwd.chunks * (a.fwd.slabs / a.fwd.unit_slabs);
-    const int blocks = (int)(items < backward_blocks(sm_count) ? items : backward_blocks(sm_count));
+    const int tensors = (a.fwd.x[0] != nullptr) + (a.fwd.x[1] != nullptr), most = backward_blocks(sm_count) / tensors;
+    const int blocks = (int)(items < most ? items : most);
+    const dim3 grid(blocks, tensors);
     cudaError_t e;
     switch (pair_kind(a.fwd, Elem<T>::kVec)) {
-        case kNeighbours: e = launch_dependent(rotate_backward_kernel<T, kNeighbours>, dim3(blocks), kRotThreads, 0, st, a); break;
-        case kHalvesShuffle: e = launch_dependent(rotate_backward_kernel<T, kHalvesShuffle>, dim3(blocks), kRotThreads, 0, st, a); break;
-        default: e = launch_dependent(rotate_backward_kernel<T, kHalvesShared>, dim3(blocks), kRotThreads, 0, st, a); break;
+        case kNeighbours: e = launch_dependent(rotate_backward_kernel<T, kNeighbours>, grid, kRotThreads, 0, st, a); break;
+        case kHalvesShuffle: e = launch_dependent(rotate_backward_kernel<T, kHalvesShuffle>, grid, kRotThreads, 0, st, a); break;
+        default: e = launch_dependent(rotate_backward_kernel<T, kHalvesShared>, grid, kRotThreads, 0, st, a); break;
     }
     if (e != cudaSuccess || (!a.dgain[0] && !a.dgain[1])) return e;
-    return launch_dependent(gain_sum_kernel, dim3((2 * a.fwd.d + 8 * kRotWarps - 1) / (8 * kRotWarps)), kRotThreads, 0, st, a.part, blocks, a.fwd.d, a.dgain[0], a.dgain[1]);
+    return launch_dependent(gain_sum_kernel, dim3((a.fwd.d + 31) / 32, 2), 1024, 0, st, a.part, blocks, a.fwd.d, a.dgain[0], a.dgain[1]);
 }
 
 }  // namespace
