@@ -707,8 +707,7 @@ static int rotate_args(agent_attn_handle* h, int n_tokens, const agent_attn_rota
     }
     if (norm) {
         if (!(norm->eps >= 0.f) || std::isinf(norm->eps)) return fail(h, AA_ERR_INVALID_ARG, "eps must be finite and not negative");
-        if ((reinterpret_cast<uintptr_t>(norm->q_gain) | reinterpret_cast<uintptr_t>(norm->k_gain)) & (h->elem_bytes - 1))
-            return fail(h, AA_ERR_INVALID_ARG, "gains must be aligned to their element type");
+        if (misaligned(norm->q_gain) || misaligned(norm->k_gain)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
         a->norm = 1;
         a->eps = norm->eps;
         a->gain[0] = norm->q_gain; a->gain[1] = norm->k_gain;

@@ -6,13 +6,15 @@
 // result and R the rotation: g' = R^T g, xh = x r, r = 1 / sqrt(mean(x^2) + eps):  dx = r (g' gain - xh mean(g' gain xh)),
 // dgain = sum of g' xh over batch, heads and tokens.
 //
-// A group of lanes owns a token: a lane has 16 bytes of channels and keeps their cosines and sines (forward: with the gains folded in) for all
-// heads and batch entries that the block visits, so that an angle is computed once for many rows.  The angle is taken in turns: p f / (2 pi) with
-// its rounding error by fma, less its nearest integer, so that large positions cost no accuracy.  The partner of a channel comes from the lane
-// itself (neighbouring channels as pairs), from another lane by a shuffle (halves of a segment, of whole 16-byte pieces; the two lanes share the work
-// of their angles) or through shared memory (halves of any other size).  The next rows are loaded before the present ones are worked on.
-// Bound by HBM: forward 2 x 16-bit, backward 10 bytes an element (16-bit types); everything else is in the way of that: angles, unpacking,
-// offsets and the rows in flight.
+// A group of lanes owns a token and keeps the cosines and sines of its channels (forward: with the gains folded in) for all heads and batch entries
+// that the block visits, so that an angle is computed once for many rows.  The angle is taken in turns: p f / (2 pi) with its rounding error by fma,
+// less its nearest integer, so that large positions cost no accuracy.  Where the channels of a pair lie, in the order of preference:
+//   forward, rotate_pairs_kernel: a lane has two pieces of 16 bytes that hold whole pairs: a piece of a segment's first half and the one half a segment
+//     on, or two pieces with neighbouring channels as pairs.  Nothing crosses lanes but the norm's sum.
+//   forward, rotate_patch_kernel: halves that are no whole pieces: a lane has one piece, its partners come through shared memory.
+//   backward: a lane has one piece; partners by shuffles (whole pieces) or through shared memory.
+// The next rows are loaded before the present ones are worked on.  Bound by HBM: forward 4 bytes an element of 16 bits, backward 10; what stands in the
+// way of that is the issue of instructions.
 #include "common.cuh"
 #include "kernels.h"
 
@@ -21,7 +23,7 @@ namespace aa {
 namespace {
 
 constexpr int kRotThreads = 256, kRotWarps = kRotThreads / 32;
-enum PairKind { kNeighbours, kHalvesShuffle, kHalvesShared };
+enum PairKind { kNeighbours, kHalvesShuffle, kHalvesShared };      // how partners meet
 
 // What a lane knows of its C channels: frequency in turns (two terms) and axis of the angles that it computes, partners.
 template <int C, PairKind KIND> struct LaneAngles {
@@ -128,7 +130,7 @@ template <int C, PairKind KIND, bool FAST> __device__ __forceinline__ void token
     }
 #pragma unroll
     for (int j = 0; j < C; ++j)
-        if (((la.second >> j & 1u) != 0) == inverse) s[j] = -s[j];
+        s[j] = __uint_as_float(__float_as_uint(s[j]) ^ ((~la.second >> j & 1u) ^ (inverse ? 1u : 0u)) << 31);      // minus in a pair's first channel
 #pragma unroll
     for (int i = 0; i < C / 2; ++i) { cs[i] = make_float2(c[2 * i], c[2 * i + 1]); sn[i] = make_float2(s[2 * i], s[2 * i + 1]); }
 }
@@ -165,19 +167,30 @@ template <typename T> __device__ __forceinline__ void unpack_pairs(const uint4& 
 }
 
 __device__ __forceinline__ float group_sum(float v, int lanes) {
-    for (int o = lanes >> 1; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (lanes >= 4) {                     // (heads of 40 to 64 channels have 4 or 8)
+        v += __shfl_xor_sync(0xffffffffu, v, 1);
+        v += __shfl_xor_sync(0xffffffffu, v, 2);
+        for (int o = 4; o < lanes; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+    } else if (lanes == 2) {
+        v += __shfl_xor_sync(0xffffffffu, v, 1);
+    }
     return v;
 }
 __device__ __forceinline__ float2 pair_of(float x) { return make_float2(x, x); }
+// a where bit i is set, else b (by a mask: a predicate for each channel is more than there are)
+__device__ __forceinline__ float pick(unsigned bits, int i, float a, float b) {
+    const unsigned m = 0u - (bits >> i & 1u);
+    return __uint_as_float((__float_as_uint(a) & m) | (__float_as_uint(b) & ~m));
+}
 // (x turned): own values times cs, partners' times sn; a channel without a partner keeps its own
 template <int C> __device__ __forceinline__ void turned(const float2 (&x)[C / 2], float2 (&y)[C / 2], const float2 (&cs)[C / 2], const float2 (&sn)[C / 2], unsigned rotated) {
 #pragma unroll
-    for (int i = 0; i < C / 2; ++i) {
-        const float2 own = fmul2(x[i], cs[i]);
-        y[i] = ffma2(y[i], sn[i], own);
-        if (rotated != (1u << C) - 1u) {
-            if (!(rotated >> (2 * i) & 1u)) y[i].x = own.x;
-            if (!(rotated >> (2 * i + 1) & 1u)) y[i].y = own.y;
+    for (int i = 0; i < C / 2; ++i) y[i] = ffma2(y[i], sn[i], fmul2(x[i], cs[i]));
+    if (rotated != (1u << C) - 1u) {
+#pragma unroll
+        for (int i = 0; i < C / 2; ++i) {
+            y[i].x = pick(rotated, 2 * i, y[i].x, x[i].x * cs[i].x);
+            y[i].y = pick(rotated, 2 * i + 1, y[i].y, x[i].y * cs[i].y);
         }
     }
 }
@@ -188,74 +201,229 @@ struct RowWalk {
     __device__ void next(bool last_head) { at += last_head ? wrap : step; }
 };
 
-template <typename T, PairKind KIND, bool NORM> __global__ void __launch_bounds__(kRotThreads) rotate_kernel(const __grid_constant__ RotateArgs p) {
-    constexpr int C = Elem<T>::kVec, kSets = NORM ? 2 : 1;
-    __shared__ float s_patch[KIND == kHalvesShared ? kRotWarps : 1][KIND == kHalvesShared ? 32 * C : 2];
+// Position of the block's unit (batch entry, or all of them) and its run of slabs
+struct SlabRun { int begin, end; };
+__device__ __forceinline__ SlabRun slab_run(const RotateArgs& p) {
+    const int unit = blockIdx.y / p.chunks, s0 = unit * p.unit_slabs + (blockIdx.y % p.chunks) * p.share;
+    return {s0, min(s0 + p.share, (unit + 1) * p.unit_slabs)};
+}
+template <int C> __device__ __forceinline__ void square_sum(const float2 (&x)[C / 2], float2& sq) {
+#pragma unroll
+    for (int i = 0; i < C / 2; ++i) sq = ffma2(x[i], x[i], sq);
+}
+template <typename T> __device__ __forceinline__ void store_pairs(T* dst, const float2 (&y)[Elem<T>::kVec / 2]) {
+    float v[Elem<T>::kVec];
+#pragma unroll
+    for (int i = 0; i < Elem<T>::kVec / 2; ++i) { v[2 * i] = y[i].x; v[2 * i + 1] = y[i].y; }
+    *reinterpret_cast<uint4*>(dst) = pack16<T>(v);
+}
+
+// One of the tensors (blockIdx.z), a lane with two pieces u and v of its token's row
+template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(kRotThreads, 3) rotate_pairs_kernel(const __grid_constant__ RotateArgs p) {
+    constexpr int C = Elem<T>::kVec;
     pdl_wait_prior();
     pdl_release_next();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = lane & (p.lanes - 1), c0 = gl * C, first_lane = lane - gl;
-    const int tok = blockIdx.x * (kRotThreads / p.lanes) + threadIdx.x / p.lanes;
-    const bool live = tok < p.N && c0 < p.d;
-    const int unit = blockIdx.y / p.chunks, s0 = unit * p.unit_slabs + (blockIdx.y % p.chunks) * p.share, s1 = min(s0 + p.share, (unit + 1) * p.unit_slabs);
-    LaneAngles<C, KIND> la;
-    lane_angles<C, KIND>(p, c0, la);
-    const int partner_lane = first_lane + la.partner[0] / C;
-    float2 cs[kSets][C / 2], sn[kSets][C / 2];
-    token_turns<C, KIND, sizeof(T) == 2>(p, la, s0 / p.heads, min(tok, p.N - 1), partner_lane, p.inverse, cs[0], sn[0]);
-    if (NORM) {
+    const int gl = threadIdx.x & (p.lanes - 1), tok = blockIdx.x * (kRotThreads / p.lanes) + threadIdx.x / p.lanes, t = p.x[0] ? blockIdx.z : 1;
+    const SlabRun run = slab_run(p);
+    // channels of the pieces, and the number of the first angle: with HALVES that of u's first channel, which is v's too
+    int cu = 2 * gl * C, cv = cu + C, angle = 0, axis = 0;
+    bool turns = !HALVES;
+    if (HALVES) {
+        int at = 0, fr = 0, left = gl;
 #pragma unroll
-        for (int i = 0; i < C / 2; ++i) { cs[kSets - 1][i] = cs[0][i]; sn[kSets - 1][i] = sn[0][i]; }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-            if (p.gain[t] && c0 < p.d) {
-                const T* g = static_cast<const T*>(p.gain[t]);
-#pragma unroll
-                for (int i = 0; i < C / 2; ++i) {
-                    cs[t * (kSets - 1)][i] = fmul2(cs[t * (kSets - 1)][i], make_float2(Elem<T>::to_f32(g[c0 + 2 * i]), Elem<T>::to_f32(g[c0 + 2 * i + 1])));
-                    sn[t * (kSets - 1)][i] = fmul2(sn[t * (kSets - 1)][i], make_float2(Elem<T>::to_f32(g[la.partner[2 * i]]), Elem<T>::to_f32(g[la.partner[2 * i + 1]])));
+        for (int a = 0; a < 3; ++a) {
+            const int half = p.channels[a] >> 1;
+            if (!turns && left >= 0) {
+                if (left * C < half) {
+                    turns = true;
+                    cu = at + left * C; cv = cu + half;
+                    angle = fr + left * C;
+                    axis = a;
                 }
+                left -= half / C;
             }
+            at += 2 * half;
+            fr += half;
+        }
+        if (!turns) { cu = at + 2 * left * C; cv = cu + C; }         // past the segments
     }
-    float* patch = s_patch[KIND == kHalvesShared ? warp : 0];
-    const T *x0 = static_cast<const T*>(p.x[0]), *x1 = static_cast<const T*>(p.x[1]);
-    RowWalk in(p.lin, s0, p.heads, tok, c0), out(p.lout, s0, p.heads, tok, c0);
-    int head = s0 % p.heads;
-    uint4 ahead[2] = {load_raw(x0 + in.at, live && x0), load_raw(x1 + in.at, live && x1)};
-    for (int s = s0; s < s1; ++s) {
+    const bool live_u = tok < p.N && cu < p.d, live_v = tok < p.N && cv < p.d;
+    float2 own_u[C / 2], par_u[C / 2], own_v[C / 2], par_v[C / 2];
+    unsigned apart = 0;                                              // neighbours: a bit for each pair (of u, then of v) that does not turn
+    {
+        float pos[3], c[C], s[C];
+        token_position(p, run.begin / p.heads, min(tok, p.N - 1), pos);
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            int f = angle + j, ax = axis;
+            bool on = turns;
+            if (!HALVES) {                                           // pair j of the 16 bytes u, v: channels 2 gl C + 2 j and the next
+                const int ch = cu + 2 * j;
+                f = ch >> 1;
+                ax = ch < p.channels[0] ? 0 : ch < p.channels[0] + p.channels[1] ? 1 : 2;
+                on = ch < p.channels[0] + p.channels[1] + p.channels[2];
+                if (!on) apart |= 1u << j;
+            }
+            const float w = on ? __ldg(p.freq + f) : 0.f;
+            constexpr float kInv = 0.15915494309189535f, kInvLo = 6.420638243e-09f;     // 1 / (2 pi) as a sum of two fp32 numbers
+            const float hi = w * kInv, lo = fmaf(w, kInv, -hi) + w * kInvLo;
+            turn<sizeof(T) == 2>(ax == 0 ? pos[0] : ax == 1 ? pos[1] : pos[2], hi, lo, c[j], s[j]);
+            if (p.inverse) s[j] = -s[j];
+        }
+        if (HALVES) {
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) {
+                own_u[i] = own_v[i] = make_float2(c[2 * i], c[2 * i + 1]);
+                par_u[i] = make_float2(-s[2 * i], -s[2 * i + 1]);
+                par_v[i] = make_float2(s[2 * i], s[2 * i + 1]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) {
+                own_u[i] = pair_of(c[i]);
+                own_v[i] = pair_of(c[C / 2 + i]);
+                par_u[i] = make_float2(-s[i], s[i]);
+                par_v[i] = make_float2(-s[C / 2 + i], s[C / 2 + i]);
+            }
+        }
+        if (NORM && p.gain[t]) {
+            const T* g = static_cast<const T*>(p.gain[t]);
+            float2 gu[C / 2], gv[C / 2];
+            unpack_pairs<T>(load_raw(g + cu, cu < p.d), gu);
+            unpack_pairs<T>(load_raw(g + cv, cv < p.d), gv);
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) {
+                own_u[i] = fmul2(own_u[i], gu[i]);
+                own_v[i] = fmul2(own_v[i], gv[i]);
+                par_u[i] = fmul2(par_u[i], HALVES ? gv[i] : make_float2(gu[i].y, gu[i].x));
+                par_v[i] = fmul2(par_v[i], HALVES ? gu[i] : make_float2(gv[i].y, gv[i].x));
+            }
+        }
+    }
+    // row pointers; a lane without a piece reads and writes its first one again, which no lane needs
+    const long long step_in = p.lin.sh, wrap_in = p.lin.sb - (p.heads - 1) * p.lin.sh, step_out = p.lout.sh, wrap_out = p.lout.sb - (p.heads - 1) * p.lout.sh;
+    const T* in = static_cast<const T*>(p.x[t]) + tok_offset(p.lin, run.begin, p.heads, tok) + cu;
+    T* out = static_cast<T*>(p.y[t]) + tok_offset(p.lout, run.begin, p.heads, tok) + cu;
+    const int dv = cv - cu;
+    int head = run.begin % p.heads;
+    uint4 next_u = load_raw(in, live_u), next_v = load_raw(in + dv, live_v);
+    for (int n = run.end - run.begin; n > 0; --n) {
+        const uint4 raw_u = next_u, raw_v = next_v;
         const bool wrap = ++head == p.heads;
         if (wrap) head = 0;
-        const uint4 raw[2] = {ahead[0], ahead[1]};
-        if (s + 1 < s1) {
+        if (n > 1) {
+            in += wrap ? wrap_in : step_in;
+            next_u = load_raw(in, live_u);
+            next_v = load_raw(in + dv, live_v);
+        }
+        float2 u[C / 2], v[C / 2], yu[C / 2], yv[C / 2];
+        unpack_pairs<T>(raw_u, u);
+        unpack_pairs<T>(raw_v, v);
+        float r = 1.f;
+        if (NORM) {
+            float2 sq = pair_of(0.f);
+            square_sum<C>(u, sq);
+            square_sum<C>(v, sq);
+            r = rsqrtf(group_sum(sq.x + sq.y, p.lanes) * p.inv_d + p.eps);
+        }
+#pragma unroll
+        for (int i = 0; i < C / 2; ++i) {
+            yu[i] = fmul2(u[i], own_u[i]);
+            yv[i] = fmul2(v[i], own_v[i]);
+        }
+        if (turns) {
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) {
+                const float2 tu = ffma2(HALVES ? v[i] : make_float2(u[i].y, u[i].x), par_u[i], yu[i]), tv = ffma2(HALVES ? u[i] : make_float2(v[i].y, v[i].x), par_v[i], yv[i]);
+                if (HALVES || !apart) {
+                    yu[i] = tu;
+                    yv[i] = tv;
+                } else {
+                    yu[i] = make_float2(pick(apart, i, yu[i].x, tu.x), pick(apart, i, yu[i].y, tu.y));
+                    yv[i] = make_float2(pick(apart, C / 2 + i, yv[i].x, tv.x), pick(apart, C / 2 + i, yv[i].y, tv.y));
+                }
+            }
+        }
+        if (NORM) {
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) {
+                yu[i] = fmul2(yu[i], pair_of(r));
+                yv[i] = fmul2(yv[i], pair_of(r));
+            }
+        }
+        if (live_u) store_pairs<T>(out, yu);
+        if (live_v) store_pairs<T>(out + dv, yv);
+        out += wrap ? wrap_out : step_out;
+    }
+}
+
+// One of the tensors, a lane with one piece; partners through shared memory, where the row lies as it is in memory: 32-bit words (WORDS: fp32, or 16-bit
+// segments of a multiple of four channels, whose pairs' partners are pairs), else element by element
+template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(kRotThreads, 3) rotate_patch_kernel(const __grid_constant__ RotateArgs p) {
+    constexpr int C = Elem<T>::kVec, kPer = sizeof(T) == 4 ? 1 : 2;  // elements of a word
+    __shared__ uint4 s_rows[kRotThreads];
+    pdl_wait_prior();
+    pdl_release_next();
+    const int lane = threadIdx.x & 31, gl = lane & (p.lanes - 1), c0 = gl * C, tok = blockIdx.x * (kRotThreads / p.lanes) + threadIdx.x / p.lanes, t = p.x[0] ? blockIdx.z : 1;
+    const SlabRun run = slab_run(p);
+    const bool live = tok < p.N && c0 < p.d;
+    LaneAngles<C, kHalvesShared> la;
+    lane_angles<C, kHalvesShared>(p, c0, la);
+    float2 own[C / 2], par[C / 2];
+    token_turns<C, kHalvesShared, sizeof(T) == 2>(p, la, run.begin / p.heads, min(tok, p.N - 1), lane, p.inverse, own, par);
+    if (NORM && p.gain[t] && c0 < p.d) {
+        const T* g = static_cast<const T*>(p.gain[t]);
+#pragma unroll
+        for (int i = 0; i < C / 2; ++i) {
+            own[i] = fmul2(own[i], make_float2(Elem<T>::to_f32(g[c0 + 2 * i]), Elem<T>::to_f32(g[c0 + 2 * i + 1])));
+            par[i] = fmul2(par[i], make_float2(Elem<T>::to_f32(g[la.partner[2 * i]]), Elem<T>::to_f32(g[la.partner[2 * i + 1]])));
+        }
+    }
+    const T* row = reinterpret_cast<const T*>(s_rows + threadIdx.x - gl);
+    const bool whole = la.rotated == (1u << C) - 1u;
+    RowWalk in(p.lin, run.begin, p.heads, tok, c0), out(p.lout, run.begin, p.heads, tok, c0);
+    const T* src = static_cast<const T*>(p.x[t]);
+    int head = run.begin % p.heads;
+    uint4 next = load_raw(src + in.at, live);
+    for (int n = run.end - run.begin; n > 0; --n) {
+        const uint4 raw = next;
+        const bool wrap = ++head == p.heads;
+        if (wrap) head = 0;
+        if (n > 1) {
             in.next(wrap);
-            ahead[0] = load_raw(x0 + in.at, live && x0);
-            ahead[1] = load_raw(x1 + in.at, live && x1);
+            next = load_raw(src + in.at, live);
+        }
+        __syncwarp();
+        s_rows[threadIdx.x] = raw;
+        __syncwarp();
+        float2 x[C / 2], y[C / 2];
+        unpack_pairs<T>(raw, x);
+        if (WORDS) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint32_t*>(row + la.partner[kPer * i]);
+            unpack_pairs<T>(make_uint4(w[0], w[1], w[2], w[3]), y);
+        } else {
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) y[i] = make_float2(Elem<T>::to_f32(row[la.partner[2 * i]]), Elem<T>::to_f32(row[la.partner[2 * i + 1]]));
+        }
+        float r = 1.f;
+        if (NORM) {
+            float2 sq = pair_of(0.f);
+            square_sum<C>(x, sq);
+            r = rsqrtf(group_sum(sq.x + sq.y, p.lanes) * p.inv_d + p.eps);
         }
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            if (!p.x[t]) continue;
-            float2 x[C / 2], y[C / 2];
-            unpack_pairs<T>(raw[t], x);
-            if constexpr (KIND == kHalvesShuffle && sizeof(T) == 2) {      // (16-bit pairs as they are: half the shuffles)
-                const uint4 w = make_uint4(__shfl_sync(0xffffffffu, raw[t].x, partner_lane), __shfl_sync(0xffffffffu, raw[t].y, partner_lane),
-                                           __shfl_sync(0xffffffffu, raw[t].z, partner_lane), __shfl_sync(0xffffffffu, raw[t].w, partner_lane));
-                unpack_pairs<T>(w, y);
-            } else {
-                partners<C, KIND>(x, la, c0, first_lane, partner_lane, patch, y);
+        for (int i = 0; i < C / 2; ++i) {
+            const float2 o = fmul2(x[i], own[i]);
+            y[i] = ffma2(y[i], par[i], o);
+            if (!whole) {
+                y[i].x = pick(la.rotated, 2 * i, y[i].x, o.x);
+                y[i].y = pick(la.rotated, 2 * i + 1, y[i].y, o.y);
             }
-            turned<C>(x, y, cs[t * (kSets - 1)], sn[t * (kSets - 1)], la.rotated);
-            if (NORM) {
-                float2 sq = fmul2(x[0], x[0]);
-#pragma unroll
-                for (int i = 1; i < C / 2; ++i) sq = ffma2(x[i], x[i], sq);
-                const float r = rsqrtf(group_sum(sq.x + sq.y, p.lanes) * p.inv_d + p.eps);
-#pragma unroll
-                for (int i = 0; i < C / 2; ++i) y[i] = fmul2(y[i], pair_of(r));
-            }
-            float v[C];
-#pragma unroll
-            for (int i = 0; i < C / 2; ++i) { v[2 * i] = y[i].x; v[2 * i + 1] = y[i].y; }
-            if (live) *reinterpret_cast<uint4*>(static_cast<T*>(p.y[t]) + out.at) = pack16<T>(v);
+            if (NORM) y[i] = fmul2(y[i], pair_of(r));
         }
+        if (live) store_pairs<T>(static_cast<T*>(p.y[t]) + out.at, y);
         out.next(wrap);
     }
 }
@@ -380,39 +548,44 @@ PairKind pair_kind(const RotateArgs& a, int c) {
     return whole && at % c == 0 ? kHalvesShuffle : kHalvesShared;
 }
 
-// Lanes of a token, and how many slabs a block visits with one set of angles: as many as leave `blocks` blocks an SM.
-void plan_rotate(RotateArgs* a, int vec, int blocks, int sm_count, int* tiles) {
+// How many slabs a block visits with one set of angles: as many as leave `blocks` blocks an SM.  `lanes`: of a token, rounded up to a power of two.
+int plan_rotate(RotateArgs* a, int lanes, int blocks, int sm_count) {
     a->lanes = 1;
-    while (a->lanes * vec < a->d) a->lanes *= 2;
-    const int groups = kRotThreads / a->lanes;
-    *tiles = (a->N + groups - 1) / groups;
+    while (a->lanes < lanes) a->lanes *= 2;
+    const int groups = kRotThreads / a->lanes, tiles = (a->N + groups - 1) / groups;
     a->unit_slabs = a->positions && a->pos_batch ? a->heads : a->slabs;
-    const long long alone = (long long)*tiles * (a->slabs / a->unit_slabs);         // blocks if each visits all slabs of its unit
+    const long long alone = (long long)tiles * (a->slabs / a->unit_slabs);          // blocks if each visits all slabs of its unit
     long long chunks = ((long long)blocks * sm_count + alone - 1) / alone;
     if (chunks > a->unit_slabs) chunks = a->unit_slabs;
     a->share = (int)((a->unit_slabs + chunks - 1) / chunks);
     a->chunks = (a->unit_slabs + a->share - 1) / a->share;
     a->inv_d = 1.f / (float)a->d;
+    return tiles;
 }
 
-template <typename T, PairKind KIND> cudaError_t launch_rotate_kind(const RotateArgs& a, dim3 grid, cudaStream_t st) {
-    if (a.norm) return launch_dependent(rotate_kernel<T, KIND, true>, grid, kRotThreads, 0, st, a);
-    return launch_dependent(rotate_kernel<T, KIND, false>, grid, kRotThreads, 0, st, a);
-}
 template <typename T> cudaError_t launch_rotate_type(RotateArgs a, int sm_count, cudaStream_t st) {
-    int tiles;
-    plan_rotate(&a, Elem<T>::kVec, 12, sm_count, &tiles);
-    const dim3 grid(tiles, a.chunks * (a.slabs / a.unit_slabs));
-    switch (pair_kind(a, Elem<T>::kVec)) {
-        case kNeighbours: return launch_rotate_kind<T, kNeighbours>(a, grid, st);
-        case kHalvesShuffle: return launch_rotate_kind<T, kHalvesShuffle>(a, grid, st);
-        default: return launch_rotate_kind<T, kHalvesShared>(a, grid, st);
+    constexpr int C = Elem<T>::kVec;
+    const int tensors = (a.x[0] != nullptr) + (a.x[1] != nullptr);
+    const PairKind kind = pair_kind(a, C);
+    int lanes = (a.d + C - 1) / C;
+    if (kind == kNeighbours) lanes = (a.d + 2 * C - 1) / (2 * C);
+    if (kind == kHalvesShuffle) {
+        const int turning = a.channels[0] + a.channels[1] + a.channels[2];
+        lanes = turning / (2 * C) + (a.d - turning + 2 * C - 1) / (2 * C);
     }
+    const int tiles = plan_rotate(&a, lanes, 12 / tensors, sm_count);
+    const dim3 grid(tiles, a.chunks * (a.slabs / a.unit_slabs), tensors);
+    auto launch = [&](auto plain, auto norm) { return launch_dependent(a.norm ? norm : plain, grid, kRotThreads, 0, st, a); };
+    if (kind == kNeighbours) return launch(rotate_pairs_kernel<T, false, false>, rotate_pairs_kernel<T, false, true>);
+    if (kind == kHalvesShuffle) return launch(rotate_pairs_kernel<T, true, false>, rotate_pairs_kernel<T, true, true>);
+    const bool words = C == 4 || (a.channels[0] % 4 == 0 && a.channels[1] % 4 == 0 && a.channels[2] % 4 == 0);
+    if (words) return launch(rotate_patch_kernel<T, true, false>, rotate_patch_kernel<T, true, true>);
+    return launch(rotate_patch_kernel<T, C == 4, false>, rotate_patch_kernel<T, C == 4, true>);
 }
+
 int backward_blocks(int sm_count) { return 3 * sm_count; }           // of a tensor
 template <typename T> cudaError_t launch_rotate_bwd_type(RotateBwdArgs a, int sm_count, cudaStream_t st) {
-    int tiles;
-    plan_rotate(&a.fwd, Elem<T>::kVec, 6, sm_count, &tiles);
+    const int tiles = plan_rotate(&a.fwd, (a.fwd.d + Elem<T>::kVec - 1) / Elem<T>::kVec, 6, sm_count);
     const long long items = (long long)tiles * a.fwd.chunks * (a.fwd.slabs / a.fwd.unit_slabs);
     const int tensors = (a.fwd.x[0] != nullptr) + (a.fwd.x[1] != nullptr), most = backward_blocks(sm_count) / tensors;
     const int blocks = (int)(items < most ? items : most);
