@@ -135,25 +135,6 @@ template <int C, PairKind KIND, bool FAST> __device__ __forceinline__ void token
     for (int i = 0; i < C / 2; ++i) { cs[i] = make_float2(c[2 * i], c[2 * i + 1]); sn[i] = make_float2(s[2 * i], s[2 * i + 1]); }
 }
 
-// Values of the partners of this lane's channels
-template <int C, PairKind KIND> __device__ __forceinline__ void partners(const float2 (&x)[C / 2], const LaneAngles<C, KIND>& la, int c0, int first_lane, int partner_lane, float* patch, float2 (&y)[C / 2]) {
-    if constexpr (KIND == kNeighbours) {
-#pragma unroll
-        for (int i = 0; i < C / 2; ++i) y[i] = make_float2(x[i].y, x[i].x);
-    } else if constexpr (KIND == kHalvesShuffle) {
-#pragma unroll
-        for (int i = 0; i < C / 2; ++i) y[i] = make_float2(__shfl_sync(0xffffffffu, x[i].x, partner_lane), __shfl_sync(0xffffffffu, x[i].y, partner_lane));
-    } else {
-        const int row = first_lane * C;
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < C / 2; ++i) *reinterpret_cast<float2*>(patch + row + c0 + 2 * i) = x[i];
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < C / 2; ++i) y[i] = make_float2(patch[row + la.partner[2 * i]], patch[row + la.partner[2 * i + 1]]);
-    }
-}
-
 __device__ __forceinline__ uint4 load_raw(const void* src, bool live) {
     uint4 raw = make_uint4(0u, 0u, 0u, 0u);
     if (live) raw = *static_cast<const uint4*>(src);
@@ -218,12 +199,49 @@ template <typename T> __device__ __forceinline__ void store_pairs(T* dst, const 
     *reinterpret_cast<uint4*>(dst) = pack16<T>(v);
 }
 
-// One of the tensors (blockIdx.z), a lane with two pieces u and v of its token's row
+// Rows of a block's run, tensor after tensor, slab after slab: where the next one lies
+template <typename T> struct RowCursor {
+    const T* at;
+    long long step, wrap;
+    int head, heads, left, tensor;
+    const RotateArgs& p;
+    long long start;
+    int run, first_head;
+    bool output;
+    __device__ RowCursor(const RotateArgs& args, const SlabRun& r, int tok, int c, bool out, int first)
+        : heads(args.heads), tensor(first), p(args), run(r.end - r.begin), first_head(r.begin % args.heads), output(out) {
+        const TokLayout& l = out ? args.lout : args.lin;
+        start = tok_offset(l, r.begin, heads, tok) + c;
+        step = l.sh;
+        wrap = l.sb - (heads - 1) * l.sh;
+        begin();
+    }
+    __device__ void begin() {
+        left = run;
+        head = first_head;
+        at = static_cast<const T*>(output ? p.y[tensor] : p.x[tensor]) + start;
+    }
+    __device__ void next() {              // (past the last row it stays somewhere that nobody reads)
+        if (--left == 0) {
+            tensor = 1;
+            begin();
+            return;
+        }
+        if (++head == heads) { head = 0; at += wrap; }
+        else at += step;
+    }
+};
+
+// A lane has two pieces u and v of its token's row.  Rows arrive by asynchronous copies, kDepth - 1 ahead: in registers one row ahead is all there is
+// room for, which leaves the 256 x 256 grid at 118 us.
+constexpr int kDepth = 4;
 template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(kRotThreads, 3) rotate_pairs_kernel(const __grid_constant__ RotateArgs p) {
     constexpr int C = Elem<T>::kVec;
+    __shared__ uint4 s_ring[kDepth][2][kRotThreads];
+    __shared__ float2 s_turn[NORM ? C : 1][NORM ? kRotThreads : 1];          // (cos, sin): the gains are folded into them tensor by tensor
     pdl_wait_prior();
     pdl_release_next();
-    const int gl = threadIdx.x & (p.lanes - 1), tok = blockIdx.x * (kRotThreads / p.lanes) + threadIdx.x / p.lanes, t = p.x[0] ? blockIdx.z : 1;
+    const int gl = threadIdx.x & (p.lanes - 1), tok = blockIdx.x * (kRotThreads / p.lanes) + threadIdx.x / p.lanes, first = p.x[0] ? 0 : 1, tensors = p.x[0] && p.x[1] ? 2 : 1;
     const SlabRun run = slab_run(p);
     // channels of the pieces, and the number of the first angle: with HALVES that of u's first channel, which is v's too
     int cu = 2 * gl * C, cv = cu + C, angle = 0, axis = 0;
@@ -247,11 +265,25 @@ template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(
         }
         if (!turns) { cu = at + 2 * left * C; cv = cu + C; }         // past the segments
     }
-    const bool live_u = tok < p.N && cu < p.d, live_v = tok < p.N && cv < p.d;
+    const int dv = cv - cu, size_u = tok < p.N && cu < p.d ? 16 : 0, size_v = tok < p.N && cv < p.d ? 16 : 0;
+    const int n = run.end - run.begin, rows = n * tensors;
+    RowCursor<T> in(p, run, min(tok, p.N - 1), cu < p.d ? cu : 0, false, first);
+    auto fetch = [&](int i) {
+        if (i < rows) {
+            cp_async16(&s_ring[i % kDepth][0][threadIdx.x], in.at, size_u);
+            cp_async16(&s_ring[i % kDepth][1][threadIdx.x], size_v ? in.at + dv : in.at, size_v);
+            in.next();
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kDepth - 1; ++i) fetch(i);
+
     float2 own_u[C / 2], par_u[C / 2], own_v[C / 2], par_v[C / 2];
     unsigned apart = 0;                                              // neighbours: a bit for each pair (of u, then of v) that does not turn
+    float c[C], s[C];
     {
-        float pos[3], c[C], s[C];
+        float pos[3];
         token_position(p, run.begin / p.heads, min(tok, p.N - 1), pos);
 #pragma unroll
         for (int j = 0; j < C; ++j) {
@@ -262,14 +294,17 @@ template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(
                 f = ch >> 1;
                 ax = ch < p.channels[0] ? 0 : ch < p.channels[0] + p.channels[1] ? 1 : 2;
                 on = ch < p.channels[0] + p.channels[1] + p.channels[2];
-                if (!on) apart |= 1u << j;
+                if (!on && ch < p.d) apart |= 1u << j;
             }
             const float w = on ? __ldg(p.freq + f) : 0.f;
             constexpr float kInv = 0.15915494309189535f, kInvLo = 6.420638243e-09f;     // 1 / (2 pi) as a sum of two fp32 numbers
             const float hi = w * kInv, lo = fmaf(w, kInv, -hi) + w * kInvLo;
             turn<sizeof(T) == 2>(ax == 0 ? pos[0] : ax == 1 ? pos[1] : pos[2], hi, lo, c[j], s[j]);
             if (p.inverse) s[j] = -s[j];
+            if (NORM) s_turn[j][threadIdx.x] = make_float2(c[j], s[j]);
         }
+    }
+    auto factors = [&](int t) {
         if (HALVES) {
 #pragma unroll
             for (int i = 0; i < C / 2; ++i) {
@@ -299,26 +334,21 @@ template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(
                 par_v[i] = fmul2(par_v[i], HALVES ? gu[i] : make_float2(gv[i].y, gv[i].x));
             }
         }
-    }
-    // row pointers; a lane without a piece reads and writes its first one again, which no lane needs
-    const long long step_in = p.lin.sh, wrap_in = p.lin.sb - (p.heads - 1) * p.lin.sh, step_out = p.lout.sh, wrap_out = p.lout.sb - (p.heads - 1) * p.lout.sh;
-    const T* in = static_cast<const T*>(p.x[t]) + tok_offset(p.lin, run.begin, p.heads, tok) + cu;
-    T* out = static_cast<T*>(p.y[t]) + tok_offset(p.lout, run.begin, p.heads, tok) + cu;
-    const int dv = cv - cu;
-    int head = run.begin % p.heads;
-    uint4 next_u = load_raw(in, live_u), next_v = load_raw(in + dv, live_v);
-    for (int n = run.end - run.begin; n > 0; --n) {
-        const uint4 raw_u = next_u, raw_v = next_v;
-        const bool wrap = ++head == p.heads;
-        if (wrap) head = 0;
-        if (n > 1) {
-            in += wrap ? wrap_in : step_in;
-            next_u = load_raw(in, live_u);
-            next_v = load_raw(in + dv, live_v);
+    };
+    factors(first);
+    RowCursor<T> out(p, run, tok, cu, true, first);
+#pragma unroll 1
+    for (int i = 0; i < rows; ++i) {
+        if (NORM && i == n) {                                        // the keys: other gains
+#pragma unroll
+            for (int j = 0; j < C; ++j) { c[j] = s_turn[j][threadIdx.x].x; s[j] = s_turn[j][threadIdx.x].y; }
+            factors(1);
         }
+        fetch(i + kDepth - 1);
+        cp_async_wait<kDepth - 1>();
         float2 u[C / 2], v[C / 2], yu[C / 2], yv[C / 2];
-        unpack_pairs<T>(raw_u, u);
-        unpack_pairs<T>(raw_v, v);
+        unpack_pairs<T>(s_ring[i % kDepth][0][threadIdx.x], u);
+        unpack_pairs<T>(s_ring[i % kDepth][1][threadIdx.x], v);
         float r = 1.f;
         if (NORM) {
             float2 sq = pair_of(0.f);
@@ -327,85 +357,95 @@ template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(
             r = rsqrtf(group_sum(sq.x + sq.y, p.lanes) * p.inv_d + p.eps);
         }
 #pragma unroll
-        for (int i = 0; i < C / 2; ++i) {
-            yu[i] = fmul2(u[i], own_u[i]);
-            yv[i] = fmul2(v[i], own_v[i]);
+        for (int k = 0; k < C / 2; ++k) {
+            yu[k] = fmul2(u[k], own_u[k]);
+            yv[k] = fmul2(v[k], own_v[k]);
         }
         if (turns) {
 #pragma unroll
-            for (int i = 0; i < C / 2; ++i) {
-                const float2 tu = ffma2(HALVES ? v[i] : make_float2(u[i].y, u[i].x), par_u[i], yu[i]), tv = ffma2(HALVES ? u[i] : make_float2(v[i].y, v[i].x), par_v[i], yv[i]);
+            for (int k = 0; k < C / 2; ++k) {
+                const float2 tu = ffma2(HALVES ? v[k] : make_float2(u[k].y, u[k].x), par_u[k], yu[k]), tv = ffma2(HALVES ? u[k] : make_float2(v[k].y, v[k].x), par_v[k], yv[k]);
                 if (HALVES || !apart) {
-                    yu[i] = tu;
-                    yv[i] = tv;
+                    yu[k] = tu;
+                    yv[k] = tv;
                 } else {
-                    yu[i] = make_float2(pick(apart, i, yu[i].x, tu.x), pick(apart, i, yu[i].y, tu.y));
-                    yv[i] = make_float2(pick(apart, C / 2 + i, yv[i].x, tv.x), pick(apart, C / 2 + i, yv[i].y, tv.y));
+                    yu[k] = make_float2(pick(apart, k, yu[k].x, tu.x), pick(apart, k, yu[k].y, tu.y));
+                    yv[k] = make_float2(pick(apart, C / 2 + k, yv[k].x, tv.x), pick(apart, C / 2 + k, yv[k].y, tv.y));
                 }
             }
         }
         if (NORM) {
 #pragma unroll
-            for (int i = 0; i < C / 2; ++i) {
-                yu[i] = fmul2(yu[i], pair_of(r));
-                yv[i] = fmul2(yv[i], pair_of(r));
+            for (int k = 0; k < C / 2; ++k) {
+                yu[k] = fmul2(yu[k], pair_of(r));
+                yv[k] = fmul2(yv[k], pair_of(r));
             }
         }
-        if (live_u) store_pairs<T>(out, yu);
-        if (live_v) store_pairs<T>(out + dv, yv);
-        out += wrap ? wrap_out : step_out;
+        T* dst = const_cast<T*>(out.at);
+        if (size_u) store_pairs<T>(dst, yu);
+        if (size_v) store_pairs<T>(dst + dv, yv);
+        out.next();
     }
 }
 
-// One of the tensors, a lane with one piece; partners through shared memory, where the row lies as it is in memory: 32-bit words (WORDS: fp32, or 16-bit
-// segments of a multiple of four channels, whose pairs' partners are pairs), else element by element
+// A lane has one piece; partners through shared memory, where the row lies as it is in memory: 32-bit words (WORDS: fp32, or 16-bit segments of a
+// multiple of four channels, whose pairs' partners are pairs), else element by element.
 template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(kRotThreads, 3) rotate_patch_kernel(const __grid_constant__ RotateArgs p) {
     constexpr int C = Elem<T>::kVec, kPer = sizeof(T) == 4 ? 1 : 2;  // elements of a word
-    __shared__ uint4 s_rows[kRotThreads];
+    __shared__ uint4 s_ring[kDepth][kRotThreads];
     pdl_wait_prior();
     pdl_release_next();
-    const int lane = threadIdx.x & 31, gl = lane & (p.lanes - 1), c0 = gl * C, tok = blockIdx.x * (kRotThreads / p.lanes) + threadIdx.x / p.lanes, t = p.x[0] ? blockIdx.z : 1;
+    const int lane = threadIdx.x & 31, gl = lane & (p.lanes - 1), c0 = gl * C, tok = blockIdx.x * (kRotThreads / p.lanes) + threadIdx.x / p.lanes;
+    const int first = p.x[0] ? 0 : 1, tensors = p.x[0] && p.x[1] ? 2 : 1;
     const SlabRun run = slab_run(p);
-    const bool live = tok < p.N && c0 < p.d;
+    const int size = tok < p.N && c0 < p.d ? 16 : 0, n = run.end - run.begin, rows = n * tensors;
+    RowCursor<T> in(p, run, min(tok, p.N - 1), c0 < p.d ? c0 : 0, false, first);
+    auto fetch = [&](int i) {
+        if (i < rows) {
+            cp_async16(&s_ring[i % kDepth][threadIdx.x], in.at, size);
+            in.next();
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kDepth - 1; ++i) fetch(i);
     LaneAngles<C, kHalvesShared> la;
     lane_angles<C, kHalvesShared>(p, c0, la);
-    float2 own[C / 2], par[C / 2];
-    token_turns<C, kHalvesShared, sizeof(T) == 2>(p, la, run.begin / p.heads, min(tok, p.N - 1), lane, p.inverse, own, par);
-    if (NORM && p.gain[t] && c0 < p.d) {
-        const T* g = static_cast<const T*>(p.gain[t]);
+    float2 cs[C / 2], sn[C / 2], own[C / 2], par[C / 2];
+    token_turns<C, kHalvesShared, sizeof(T) == 2>(p, la, run.begin / p.heads, min(tok, p.N - 1), lane, p.inverse, cs, sn);
+    auto factors = [&](int t) {
 #pragma unroll
-        for (int i = 0; i < C / 2; ++i) {
-            own[i] = fmul2(own[i], make_float2(Elem<T>::to_f32(g[c0 + 2 * i]), Elem<T>::to_f32(g[c0 + 2 * i + 1])));
-            par[i] = fmul2(par[i], make_float2(Elem<T>::to_f32(g[la.partner[2 * i]]), Elem<T>::to_f32(g[la.partner[2 * i + 1]])));
+        for (int i = 0; i < C / 2; ++i) { own[i] = cs[i]; par[i] = sn[i]; }
+        if (NORM && p.gain[t] && c0 < p.d) {
+            const T* g = static_cast<const T*>(p.gain[t]);
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) {
+                own[i] = fmul2(own[i], make_float2(Elem<T>::to_f32(g[c0 + 2 * i]), Elem<T>::to_f32(g[c0 + 2 * i + 1])));
+                par[i] = fmul2(par[i], make_float2(Elem<T>::to_f32(g[la.partner[2 * i]]), Elem<T>::to_f32(g[la.partner[2 * i + 1]])));
+            }
         }
-    }
-    const T* row = reinterpret_cast<const T*>(s_rows + threadIdx.x - gl);
+    };
+    factors(first);
     const bool whole = la.rotated == (1u << C) - 1u;
-    RowWalk in(p.lin, run.begin, p.heads, tok, c0), out(p.lout, run.begin, p.heads, tok, c0);
-    const T* src = static_cast<const T*>(p.x[t]);
-    int head = run.begin % p.heads;
-    uint4 next = load_raw(src + in.at, live);
-    for (int n = run.end - run.begin; n > 0; --n) {
-        const uint4 raw = next;
-        const bool wrap = ++head == p.heads;
-        if (wrap) head = 0;
-        if (n > 1) {
-            in.next(wrap);
-            next = load_raw(src + in.at, live);
-        }
+    RowCursor<T> out(p, run, tok, c0, true, first);
+#pragma unroll 1
+    for (int i = 0; i < rows; ++i) {
+        if (NORM && i == n) factors(1);
+        __syncwarp();                                                // (the stage that is filled next has been read by the whole warp)
+        fetch(i + kDepth - 1);
+        cp_async_wait<kDepth - 1>();
         __syncwarp();
-        s_rows[threadIdx.x] = raw;
-        __syncwarp();
+        const T* row = reinterpret_cast<const T*>(&s_ring[i % kDepth][threadIdx.x - gl]);
         float2 x[C / 2], y[C / 2];
-        unpack_pairs<T>(raw, x);
+        unpack_pairs<T>(s_ring[i % kDepth][threadIdx.x], x);
         if (WORDS) {
             uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint32_t*>(row + la.partner[kPer * i]);
+            for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const uint32_t*>(row + la.partner[kPer * k]);
             unpack_pairs<T>(make_uint4(w[0], w[1], w[2], w[3]), y);
         } else {
 #pragma unroll
-            for (int i = 0; i < C / 2; ++i) y[i] = make_float2(Elem<T>::to_f32(row[la.partner[2 * i]]), Elem<T>::to_f32(row[la.partner[2 * i + 1]]));
+            for (int k = 0; k < C / 2; ++k) y[k] = make_float2(Elem<T>::to_f32(row[la.partner[2 * k]]), Elem<T>::to_f32(row[la.partner[2 * k + 1]]));
         }
         float r = 1.f;
         if (NORM) {
@@ -414,30 +454,33 @@ template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(k
             r = rsqrtf(group_sum(sq.x + sq.y, p.lanes) * p.inv_d + p.eps);
         }
 #pragma unroll
-        for (int i = 0; i < C / 2; ++i) {
-            const float2 o = fmul2(x[i], own[i]);
-            y[i] = ffma2(y[i], par[i], o);
+        for (int k = 0; k < C / 2; ++k) {
+            const float2 o = fmul2(x[k], own[k]);
+            y[k] = ffma2(y[k], par[k], o);
             if (!whole) {
-                y[i].x = pick(la.rotated, 2 * i, y[i].x, o.x);
-                y[i].y = pick(la.rotated, 2 * i + 1, y[i].y, o.y);
+                y[k].x = pick(la.rotated, 2 * k, y[k].x, o.x);
+                y[k].y = pick(la.rotated, 2 * k + 1, y[k].y, o.y);
             }
-            if (NORM) y[i] = fmul2(y[i], pair_of(r));
+            if (NORM) y[k] = fmul2(y[k], pair_of(r));
         }
-        if (live) store_pairs<T>(static_cast<T*>(p.y[t]) + out.at, y);
-        out.next(wrap);
+        if (size) store_pairs<T>(const_cast<T*>(out.at), y);
+        out.next();
     }
 }
 
 // Gradient through norm and rotation.  A block has one of the tensors (blockIdx.y) and loops over (tile of tokens, run of slabs); the gain's gradient
-// stays in registers until the block's end and leaves as one row of sums a block, which gain_sum_kernel adds up in a fixed order.
+// stays in registers until the block's end and leaves as one row of sums a block, which gain_sum_kernel adds up in a fixed order.  A lane has 16 bytes of
+// x; the gradient's row (fp32) is copied by the group's lanes in whole sectors and lies in shared memory as it is in memory, from where a lane reads
+// its channels and their partners.  Results change hands between two lanes so that they leave in whole sectors.
 template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThreads, 3) rotate_backward_kernel(const __grid_constant__ RotateBwdArgs p) {
-    constexpr int C = Elem<T>::kVec;
-    __shared__ float s_patch[KIND == kHalvesShared ? kRotWarps : 1][KIND == kHalvesShared ? 32 * C : 2];
-    __shared__ float s_sum[kRotThreads * C];
+    constexpr int C = Elem<T>::kVec, kPieces = C / 4, kAhead = 3;            // 16-byte pieces of a lane's fp32 channels
+    extern __shared__ __align__(16) unsigned char s_dyn[];                   // [kAhead][1 + kPieces][threads] uint4; at the end sums
+    uint4* ring = reinterpret_cast<uint4*>(s_dyn);
+    constexpr int kStage = (1 + kPieces) * kRotThreads;
     pdl_wait_prior();
     pdl_release_next();
     const RotateArgs& f = p.fwd;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = lane & (f.lanes - 1), c0 = gl * C, first_lane = lane - gl;
+    const int lane = threadIdx.x & 31, gl = lane & (f.lanes - 1), c0 = gl * C, first_lane = lane - gl;
     const int groups = kRotThreads / f.lanes, tiles = (f.N + groups - 1) / groups, t = f.x[0] ? blockIdx.y : 1;
     LaneAngles<C, KIND> la;
     lane_angles<C, KIND>(f, c0, la);
@@ -451,61 +494,111 @@ template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThrea
         gain[i] = gs && c0 < f.d ? make_float2(Elem<T>::to_f32(gs[c0 + 2 * i]), Elem<T>::to_f32(gs[c0 + 2 * i + 1])) : pair_of(1.f);
         sum[i] = pair_of(0.f);
     }
-    float* patch = s_patch[KIND == kHalvesShared ? warp : 0];
-    const int runs = f.chunks * (f.slabs / f.unit_slabs);
+    const int runs = f.chunks * (f.slabs / f.unit_slabs), row_at = kRotThreads + (threadIdx.x - gl) * kPieces;       // of the group's gradient row in a stage
     for (long long item = blockIdx.x; item < (long long)tiles * runs; item += gridDim.x) {
         const int run = (int)(item / tiles), tok = (int)(item - (long long)run * tiles) * groups + threadIdx.x / f.lanes;
-        const bool live = tok < f.N && c0 < f.d;
-        const int unit = run / f.chunks, s0 = unit * f.unit_slabs + (run % f.chunks) * f.share, s1 = min(s0 + f.share, (unit + 1) * f.unit_slabs);
-        RowWalk in(f.lin, s0, f.heads, tok, c0), gin(p.lgrad, s0, f.heads, tok, c0), out(f.lout, s0, f.heads, tok, c0);
-        int head = s0 % f.heads;
-        uint4 ahead = load_raw(xs + in.at, live), gahead[C / 4];
+        const bool token = tok < f.N, live = token && c0 < f.d;
+        const int here = min(tok, f.N - 1), ch = c0 < f.d ? c0 : 0;
+        const int unit = run / f.chunks, s0 = unit * f.unit_slabs + (run % f.chunks) * f.share, n = min(f.share, (unit + 1) * f.unit_slabs - s0);
+        RowWalk in(f.lin, s0, f.heads, here, ch), gin(p.lgrad, s0, f.heads, here, 0), out(f.lout, s0, f.heads, here, 0);
+        int head = s0 % f.heads, fhead = head;
+        auto fetch = [&](int i) {
+            if (i < n) {
+                uint4* to = ring + (i % kAhead) * kStage;
+                cp_async16(to + threadIdx.x, xs + in.at, live ? 16 : 0);
 #pragma unroll
-        for (int i = 0; i < C / 4; ++i) gahead[i] = load_raw(grad + gin.at + 4 * i, live);
-        float2 cs[C / 2], sn[C / 2];
-        token_turns<C, KIND, false>(f, la, s0 / f.heads, min(tok, f.N - 1), partner_lane, true, cs, sn);
-        for (int s = s0; s < s1; ++s) {
-            const bool wrap = ++head == f.heads;
-            if (wrap) head = 0;
-            float2 x[C / 2], g[C / 2], y[C / 2];
-            unpack_pairs<T>(ahead, x);
-#pragma unroll
-            for (int i = 0; i < C / 4; ++i) {
-                g[2 * i] = make_float2(__uint_as_float(gahead[i].x), __uint_as_float(gahead[i].y));
-                g[2 * i + 1] = make_float2(__uint_as_float(gahead[i].z), __uint_as_float(gahead[i].w));
-            }
-            if (s + 1 < s1) {
+                for (int k = 0; k < kPieces; ++k) {
+                    const int piece = gl + k * f.lanes;
+                    const bool there = token && 4 * piece < f.d;
+                    cp_async16(to + row_at + piece, grad + gin.at + (there ? 4 * piece : 0), there ? 16 : 0);
+                }
+                const bool wrap = ++fhead == f.heads;
+                if (wrap) fhead = 0;
                 in.next(wrap);
                 gin.next(wrap);
-                ahead = load_raw(xs + in.at, live);
-#pragma unroll
-                for (int i = 0; i < C / 4; ++i) gahead[i] = load_raw(grad + gin.at + 4 * i, live);
             }
-            partners<C, KIND>(g, la, c0, first_lane, partner_lane, patch, y);
+            cp_async_commit();
+        };
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kAhead - 1; ++i) fetch(i);
+        float2 cs[C / 2], sn[C / 2];
+        token_turns<C, KIND, false>(f, la, s0 / f.heads, here, partner_lane, true, cs, sn);
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            __syncwarp();                                                    // (the stage that is filled next has been read by the whole warp)
+            fetch(i + kAhead - 1);
+            cp_async_wait<kAhead - 1>();
+            __syncwarp();
+            const uint4* from = ring + (i % kAhead) * kStage;
+            const float* row = reinterpret_cast<const float*>(from + row_at);
+            float2 x[C / 2], g[C / 2], y[C / 2];
+            unpack_pairs<T>(from[threadIdx.x], x);
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) {
+                const float4 w = *reinterpret_cast<const float4*>(row + c0 + 4 * k);
+                g[2 * k] = make_float2(w.x, w.y);
+                g[2 * k + 1] = make_float2(w.z, w.w);
+            }
+            if constexpr (KIND == kNeighbours) {
+#pragma unroll
+                for (int k = 0; k < C / 2; ++k) y[k] = make_float2(g[k].y, g[k].x);
+            } else if constexpr (KIND == kHalvesShuffle) {
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    const float4 w = *reinterpret_cast<const float4*>(row + la.partner[0] + 4 * k);
+                    y[2 * k] = make_float2(w.x, w.y);
+                    y[2 * k + 1] = make_float2(w.z, w.w);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < C / 2; ++k) y[k] = make_float2(row[la.partner[2 * k]], row[la.partner[2 * k + 1]]);
+            }
             turned<C>(g, y, cs, sn, la.rotated);
             float2 sq = pair_of(0.f), dot = pair_of(0.f);
 #pragma unroll
-            for (int i = 0; i < C / 2; ++i) {
-                sq = ffma2(x[i], x[i], sq);
-                dot = ffma2(fmul2(y[i], gain[i]), x[i], dot);
+            for (int k = 0; k < C / 2; ++k) {
+                sq = ffma2(x[k], x[k], sq);
+                dot = ffma2(fmul2(y[k], gain[k]), x[k], dot);
             }
             const float r = rsqrtf(group_sum(sq.x + sq.y, f.lanes) * f.inv_d + f.eps);
             const float m = -group_sum(dot.x + dot.y, f.lanes) * f.inv_d * r * r * r;
-            float4 v[C / 4];
+            float v[C];
 #pragma unroll
-            for (int i = 0; i < C / 2; ++i) {
-                sum[i] = ffma2(y[i], fmul2(x[i], pair_of(r)), sum[i]);
-                y[i] = ffma2(fmul2(gain[i], pair_of(r)), y[i], fmul2(pair_of(m), x[i]));
+            for (int k = 0; k < C / 2; ++k) {
+                sum[k] = ffma2(y[k], fmul2(x[k], pair_of(r)), sum[k]);
+                y[k] = ffma2(fmul2(gain[k], pair_of(r)), y[k], fmul2(pair_of(m), x[k]));
+                v[2 * k] = y[k].x;
+                v[2 * k + 1] = y[k].y;
             }
+            float* to = dst + out.at;
+            if (kPieces == 1) {
+                if (live) *reinterpret_cast<float4*>(to + c0) = make_float4(v[0], v[1], v[2], v[3]);
+            } else if (f.lanes == 1) {
+                if (live) {
 #pragma unroll
-            for (int i = 0; i < C / 4; ++i) v[i] = make_float4(y[2 * i].x, y[2 * i].y, y[2 * i + 1].x, y[2 * i + 1].y);
-            if (live) {
+                    for (int k = 0; k < kPieces; ++k) *reinterpret_cast<float4*>(to + c0 + 4 * k) = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                }
+            } else {
+                // the even lane of two gets its first piece and the odd one's first, the odd lane the second ones: 32 bytes side by side a store
+                const bool odd = gl & 1;
+                float w[4];
 #pragma unroll
-                for (int i = 0; i < C / 4; ++i) *reinterpret_cast<float4*>(dst + out.at + 4 * i) = v[i];
+                for (int k = 0; k < 4; ++k) {
+                    w[k] = __shfl_xor_sync(0xffffffffu, odd ? v[k] : v[(4 + k) % C], 1);
+                    if (odd) { v[k] = w[k]; w[k] = v[(4 + k) % C]; }
+                }
+                const int pair = (gl & ~1) * C + (odd ? 4 : 0);
+                if (token && pair < f.d) *reinterpret_cast<float4*>(to + pair) = make_float4(v[0], v[1], v[2], v[3]);
+                if (token && pair + C < f.d) *reinterpret_cast<float4*>(to + pair + C) = make_float4(w[0], w[1], w[2], w[3]);
             }
+            const bool wrap = ++head == f.heads;
+            if (wrap) head = 0;
             out.next(wrap);
         }
     }
+    float* s_sum = reinterpret_cast<float*>(s_dyn);
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < C / 2; ++i) *reinterpret_cast<float2*>(s_sum + threadIdx.x * C + 2 * i) = sum[i];
     __syncthreads();
@@ -548,16 +641,24 @@ PairKind pair_kind(const RotateArgs& a, int c) {
     return whole && at % c == 0 ? kHalvesShuffle : kHalvesShared;
 }
 
-// How many slabs a block visits with one set of angles: as many as leave `blocks` blocks an SM.  `lanes`: of a token, rounded up to a power of two.
-int plan_rotate(RotateArgs* a, int lanes, int blocks, int sm_count) {
+// Lanes of a token (rounded up to a power of two), and how many slabs a block visits with one set of angles.  Fewer: the angles cost more, as much as
+// four rows; more: the last of the waves of `resident` blocks is emptier.  `rows`: of a slab (the tensors of a block).
+int plan_rotate(RotateArgs* a, int lanes, int rows, int resident) {
     a->lanes = 1;
     while (a->lanes < lanes) a->lanes *= 2;
     const int groups = kRotThreads / a->lanes, tiles = (a->N + groups - 1) / groups;
     a->unit_slabs = a->positions && a->pos_batch ? a->heads : a->slabs;
     const long long alone = (long long)tiles * (a->slabs / a->unit_slabs);          // blocks if each visits all slabs of its unit
-    long long chunks = ((long long)blocks * sm_count + alone - 1) / alone;
-    if (chunks > a->unit_slabs) chunks = a->unit_slabs;
-    a->share = (int)((a->unit_slabs + chunks - 1) / chunks);
+    long long best = 0;
+    for (int chunks = 1; chunks <= a->unit_slabs; ++chunks) {
+        const int share = (a->unit_slabs + chunks - 1) / chunks;
+        const long long blocks = alone * ((a->unit_slabs + share - 1) / share), cost = (blocks + resident - 1) / resident * (4 + rows * share);
+        if (chunks == 1 || cost < best) {
+            best = cost;
+            a->share = share;
+        }
+        if (blocks > 16ll * resident) break;
+    }
     a->chunks = (a->unit_slabs + a->share - 1) / a->share;
     a->inv_d = 1.f / (float)a->d;
     return tiles;
@@ -573,8 +674,8 @@ template <typename T> cudaError_t launch_rotate_type(RotateArgs a, int sm_count,
         const int turning = a.channels[0] + a.channels[1] + a.channels[2];
         lanes = turning / (2 * C) + (a.d - turning + 2 * C - 1) / (2 * C);
     }
-    const int tiles = plan_rotate(&a, lanes, 12 / tensors, sm_count);
-    const dim3 grid(tiles, a.chunks * (a.slabs / a.unit_slabs), tensors);
+    const int tiles = plan_rotate(&a, lanes, tensors, 3 * sm_count);
+    const dim3 grid(tiles, a.chunks * (a.slabs / a.unit_slabs));
     auto launch = [&](auto plain, auto norm) { return launch_dependent(a.norm ? norm : plain, grid, kRotThreads, 0, st, a); };
     if (kind == kNeighbours) return launch(rotate_pairs_kernel<T, false, false>, rotate_pairs_kernel<T, false, true>);
     if (kind == kHalvesShuffle) return launch(rotate_pairs_kernel<T, true, false>, rotate_pairs_kernel<T, true, true>);
@@ -584,17 +685,21 @@ template <typename T> cudaError_t launch_rotate_type(RotateArgs a, int sm_count,
 }
 
 int backward_blocks(int sm_count) { return 3 * sm_count; }           // of a tensor
+template <typename T, PairKind KIND> cudaError_t launch_backward_kind(const RotateBwdArgs& a, dim3 grid, cudaStream_t st) {
+    constexpr int kBytes = 3 * (1 + Elem<T>::kVec / 4) * kRotThreads * 16;
+    return launch_dependent(rotate_backward_kernel<T, KIND>, grid, kRotThreads, kBytes, st, a);
+}
 template <typename T> cudaError_t launch_rotate_bwd_type(RotateBwdArgs a, int sm_count, cudaStream_t st) {
-    const int tiles = plan_rotate(&a.fwd, (a.fwd.d + Elem<T>::kVec - 1) / Elem<T>::kVec, 6, sm_count);
-    const long long items = (long long)tiles * a.fwd.chunks * (a.fwd.slabs / a.fwd.unit_slabs);
     const int tensors = (a.fwd.x[0] != nullptr) + (a.fwd.x[1] != nullptr), most = backward_blocks(sm_count) / tensors;
+    const int tiles = plan_rotate(&a.fwd, (a.fwd.d + Elem<T>::kVec - 1) / Elem<T>::kVec, 1, most);
+    const long long items = (long long)tiles * a.fwd.chunks * (a.fwd.slabs / a.fwd.unit_slabs);
     const int blocks = (int)(items < most ? items : most);
     const dim3 grid(blocks, tensors);
     cudaError_t e;
     switch (pair_kind(a.fwd, Elem<T>::kVec)) {
-        case kNeighbours: e = launch_dependent(rotate_backward_kernel<T, kNeighbours>, grid, kRotThreads, 0, st, a); break;
-        case kHalvesShuffle: e = launch_dependent(rotate_backward_kernel<T, kHalvesShuffle>, grid, kRotThreads, 0, st, a); break;
-        default: e = launch_dependent(rotate_backward_kernel<T, kHalvesShared>, grid, kRotThreads, 0, st, a); break;
+        case kNeighbours: e = launch_backward_kind<T, kNeighbours>(a, grid, st); break;
+        case kHalvesShuffle: e = launch_backward_kind<T, kHalvesShuffle>(a, grid, st); break;
+        default: e = launch_backward_kind<T, kHalvesShared>(a, grid, st); break;
     }
     if (e != cudaSuccess || (!a.dgain[0] && !a.dgain[1])) return e;
     return launch_dependent(gain_sum_kernel, dim3((a.fwd.d + 31) / 32, 2), 1024, 0, st, a.part, blocks, a.fwd.d, a.dgain[0], a.dgain[1]);
