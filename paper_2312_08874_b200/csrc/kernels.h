@@ -333,7 +333,7 @@ struct RotateArgs {
     int neighbours;           // pairs are neighbouring channels, else the halves of an axis's segment
     int norm, inverse;
     float eps;
-    // set by the launcher: lanes of a token; slabs that share positions, runs of them, slabs of a run; 1 / d
+    // set by the launcher: lanes of a token (gradient: a power of two); slabs that share positions, runs of them, slabs of a run; 1 / d
     int lanes, unit_slabs, chunks, share;
     float inv_d;
 };

@@ -22,7 +22,7 @@ namespace aa {
 
 namespace {
 
-constexpr int kRotThreads = 256, kRotWarps = kRotThreads / 32;
+constexpr int kRotThreads = 256;
 enum PairKind { kNeighbours, kHalvesShuffle, kHalvesShared };      // how partners meet
 
 // What a lane knows of its C channels: frequency in turns (two terms) and axis of the angles that it computes, partners.
@@ -147,6 +147,16 @@ template <typename T> __device__ __forceinline__ void unpack_pairs(const uint4& 
     for (int i = 0; i < Elem<T>::kVec / 2; ++i) f[i] = make_float2(v[2 * i], v[2 * i + 1]);
 }
 
+// Sum over the lanes of a token.  Forward kernels: any number of lanes, in one order for all of them.
+__device__ __forceinline__ float token_sum(float v, int lanes, int first_lane) {
+    if (lanes == 4) {
+        v += __shfl_xor_sync(0xffffffffu, v, 1);
+        return v + __shfl_xor_sync(0xffffffffu, v, 2);
+    }
+    float sum = __shfl_sync(0xffffffffu, v, first_lane);
+    for (int k = 1; k < lanes; ++k) sum += __shfl_sync(0xffffffffu, v, first_lane + k);
+    return sum;
+}
 __device__ __forceinline__ float group_sum(float v, int lanes) {
     if (lanes >= 4) {                     // (heads of 40 to 64 channels have 4 or 8)
         v += __shfl_xor_sync(0xffffffffu, v, 1);
@@ -199,6 +209,17 @@ template <typename T> __device__ __forceinline__ void store_pairs(T* dst, const 
     *reinterpret_cast<uint4*>(dst) = pack16<T>(v);
 }
 
+// A thread's place in the forward kernels: the warp's lanes make up as many whole groups as there are
+struct Place {
+    int gl, first, tok;                   // lane of the group, the group's first lane, token (past the last: none)
+    __device__ explicit Place(const RotateArgs& p) {
+        const int lane = threadIdx.x & 31, in_warp = 32 / p.lanes, group = lane / p.lanes;
+        gl = lane - group * p.lanes;
+        first = lane - gl;
+        tok = group < in_warp ? (blockIdx.x * (kRotThreads / 32) + (threadIdx.x >> 5)) * in_warp + group : p.N;
+    }
+};
+
 // Rows of a block's run, tensor after tensor, slab after slab: where the next one lies
 template <typename T> struct RowCursor {
     const T* at;
@@ -241,43 +262,44 @@ template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(
     __shared__ float2 s_turn[NORM ? C : 1][NORM ? kRotThreads : 1];          // (cos, sin): the gains are folded into them tensor by tensor
     pdl_wait_prior();
     pdl_release_next();
-    const int gl = threadIdx.x & (p.lanes - 1), tok = blockIdx.x * (kRotThreads / p.lanes) + threadIdx.x / p.lanes, first = p.x[0] ? 0 : 1, tensors = p.x[0] && p.x[1] ? 2 : 1;
+    const Place at(p);
+    const int gl = at.gl, tok = at.tok, first = p.x[0] ? 0 : 1, tensors = p.x[0] && p.x[1] ? 2 : 1;
     const SlabRun run = slab_run(p);
     // channels of the pieces, and the number of the first angle: with HALVES that of u's first channel, which is v's too
     int cu = 2 * gl * C, cv = cu + C, angle = 0, axis = 0;
     bool turns = !HALVES;
     if (HALVES) {
-        int at = 0, fr = 0, left = gl;
+        int start = 0, fr = 0, left = gl;
 #pragma unroll
         for (int a = 0; a < 3; ++a) {
             const int half = p.channels[a] >> 1;
             if (!turns && left >= 0) {
                 if (left * C < half) {
                     turns = true;
-                    cu = at + left * C; cv = cu + half;
+                    cu = start + left * C; cv = cu + half;
                     angle = fr + left * C;
                     axis = a;
                 }
                 left -= half / C;
             }
-            at += 2 * half;
+            start += 2 * half;
             fr += half;
         }
-        if (!turns) { cu = at + 2 * left * C; cv = cu + C; }         // past the segments
+        if (!turns) { cu = start + 2 * left * C; cv = cu + C; }         // past the segments
     }
     const int dv = cv - cu, size_u = tok < p.N && cu < p.d ? 16 : 0, size_v = tok < p.N && cv < p.d ? 16 : 0;
     const int n = run.end - run.begin, rows = n * tensors;
     RowCursor<T> in(p, run, min(tok, p.N - 1), cu < p.d ? cu : 0, false, first);
-    auto fetch = [&](int i) {
+    auto fetch = [&](int i, int stage) {
         if (i < rows) {
-            cp_async16(&s_ring[i % kDepth][0][threadIdx.x], in.at, size_u);
-            cp_async16(&s_ring[i % kDepth][1][threadIdx.x], size_v ? in.at + dv : in.at, size_v);
+            cp_async16(&s_ring[stage][0][threadIdx.x], in.at, size_u);
+            cp_async16(&s_ring[stage][1][threadIdx.x], in.at + (size_v ? dv : 0), size_v);
             in.next();
         }
         cp_async_commit();
     };
 #pragma unroll
-    for (int i = 0; i < kDepth - 1; ++i) fetch(i);
+    for (int i = 0; i < kDepth - 1; ++i) fetch(i, i);
 
     float2 own_u[C / 2], par_u[C / 2], own_v[C / 2], par_v[C / 2];
     unsigned apart = 0;                                              // neighbours: a bit for each pair (of u, then of v) that does not turn
@@ -336,25 +358,24 @@ template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(
         }
     };
     factors(first);
-    RowCursor<T> out(p, run, tok, cu, true, first);
-#pragma unroll 1
-    for (int i = 0; i < rows; ++i) {
+    RowCursor<T> out(p, run, min(tok, p.N - 1), cu, true, first);
+    auto row = [&](int i, int stage) {
         if (NORM && i == n) {                                        // the keys: other gains
 #pragma unroll
             for (int j = 0; j < C; ++j) { c[j] = s_turn[j][threadIdx.x].x; s[j] = s_turn[j][threadIdx.x].y; }
             factors(1);
         }
-        fetch(i + kDepth - 1);
+        fetch(i + kDepth - 1, (stage + kDepth - 1) % kDepth);
         cp_async_wait<kDepth - 1>();
         float2 u[C / 2], v[C / 2], yu[C / 2], yv[C / 2];
-        unpack_pairs<T>(s_ring[i % kDepth][0][threadIdx.x], u);
-        unpack_pairs<T>(s_ring[i % kDepth][1][threadIdx.x], v);
+        unpack_pairs<T>(s_ring[stage][0][threadIdx.x], u);
+        unpack_pairs<T>(s_ring[stage][1][threadIdx.x], v);
         float r = 1.f;
         if (NORM) {
             float2 sq = pair_of(0.f);
             square_sum<C>(u, sq);
             square_sum<C>(v, sq);
-            r = rsqrtf(group_sum(sq.x + sq.y, p.lanes) * p.inv_d + p.eps);
+            r = rsqrtf(token_sum(sq.x + sq.y, p.lanes, at.first) * p.inv_d + p.eps);
         }
 #pragma unroll
         for (int k = 0; k < C / 2; ++k) {
@@ -385,6 +406,12 @@ template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(
         if (size_u) store_pairs<T>(dst, yu);
         if (size_v) store_pairs<T>(dst + dv, yv);
         out.next();
+    };
+#pragma unroll 1
+    for (int i = 0; i < rows; i += kDepth) {
+#pragma unroll
+        for (int k = 0; k < kDepth; ++k)
+            if (i + k < rows) row(i + k, k);
     }
 }
 
@@ -395,24 +422,25 @@ template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(k
     __shared__ uint4 s_ring[kDepth][kRotThreads];
     pdl_wait_prior();
     pdl_release_next();
-    const int lane = threadIdx.x & 31, gl = lane & (p.lanes - 1), c0 = gl * C, tok = blockIdx.x * (kRotThreads / p.lanes) + threadIdx.x / p.lanes;
+    const Place at(p);
+    const int gl = at.gl, c0 = gl * C, tok = at.tok;
     const int first = p.x[0] ? 0 : 1, tensors = p.x[0] && p.x[1] ? 2 : 1;
     const SlabRun run = slab_run(p);
     const int size = tok < p.N && c0 < p.d ? 16 : 0, n = run.end - run.begin, rows = n * tensors;
     RowCursor<T> in(p, run, min(tok, p.N - 1), c0 < p.d ? c0 : 0, false, first);
-    auto fetch = [&](int i) {
+    auto fetch = [&](int i, int stage) {
         if (i < rows) {
-            cp_async16(&s_ring[i % kDepth][threadIdx.x], in.at, size);
+            cp_async16(&s_ring[stage][threadIdx.x], in.at, size);
             in.next();
         }
         cp_async_commit();
     };
 #pragma unroll
-    for (int i = 0; i < kDepth - 1; ++i) fetch(i);
+    for (int i = 0; i < kDepth - 1; ++i) fetch(i, i);
     LaneAngles<C, kHalvesShared> la;
     lane_angles<C, kHalvesShared>(p, c0, la);
     float2 cs[C / 2], sn[C / 2], own[C / 2], par[C / 2];
-    token_turns<C, kHalvesShared, sizeof(T) == 2>(p, la, run.begin / p.heads, min(tok, p.N - 1), lane, p.inverse, cs, sn);
+    token_turns<C, kHalvesShared, sizeof(T) == 2>(p, la, run.begin / p.heads, min(tok, p.N - 1), at.first, p.inverse, cs, sn);
     auto factors = [&](int t) {
 #pragma unroll
         for (int i = 0; i < C / 2; ++i) { own[i] = cs[i]; par[i] = sn[i]; }
@@ -427,17 +455,16 @@ template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(k
     };
     factors(first);
     const bool whole = la.rotated == (1u << C) - 1u;
-    RowCursor<T> out(p, run, tok, c0, true, first);
-#pragma unroll 1
-    for (int i = 0; i < rows; ++i) {
+    RowCursor<T> out(p, run, min(tok, p.N - 1), c0, true, first);
+    auto row_of = [&](int i, int stage) {
         if (NORM && i == n) factors(1);
         __syncwarp();                                                // (the stage that is filled next has been read by the whole warp)
-        fetch(i + kDepth - 1);
+        fetch(i + kDepth - 1, (stage + kDepth - 1) % kDepth);
         cp_async_wait<kDepth - 1>();
         __syncwarp();
-        const T* row = reinterpret_cast<const T*>(&s_ring[i % kDepth][threadIdx.x - gl]);
+        const T* row = reinterpret_cast<const T*>(&s_ring[stage][threadIdx.x - gl]);
         float2 x[C / 2], y[C / 2];
-        unpack_pairs<T>(s_ring[i % kDepth][threadIdx.x], x);
+        unpack_pairs<T>(s_ring[stage][threadIdx.x], x);
         if (WORDS) {
             uint32_t w[4];
 #pragma unroll
@@ -451,7 +478,7 @@ template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(k
         if (NORM) {
             float2 sq = pair_of(0.f);
             square_sum<C>(x, sq);
-            r = rsqrtf(group_sum(sq.x + sq.y, p.lanes) * p.inv_d + p.eps);
+            r = rsqrtf(token_sum(sq.x + sq.y, p.lanes, at.first) * p.inv_d + p.eps);
         }
 #pragma unroll
         for (int k = 0; k < C / 2; ++k) {
@@ -465,6 +492,12 @@ template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(k
         }
         if (size) store_pairs<T>(const_cast<T*>(out.at), y);
         out.next();
+    };
+#pragma unroll 1
+    for (int i = 0; i < rows; i += kDepth) {
+#pragma unroll
+        for (int k = 0; k < kDepth; ++k)
+            if (i + k < rows) row_of(i + k, k);
     }
 }
 
@@ -641,12 +674,10 @@ PairKind pair_kind(const RotateArgs& a, int c) {
     return whole && at % c == 0 ? kHalvesShuffle : kHalvesShared;
 }
 
-// Lanes of a token (rounded up to a power of two), and how many slabs a block visits with one set of angles.  Fewer: the angles cost more, as much as
+// How many slabs a block visits with one set of angles; `tokens` of a block.  Fewer: the angles cost more, as much as
 // four rows; more: the last of the waves of `resident` blocks is emptier.  `rows`: of a slab (the tensors of a block).
-int plan_rotate(RotateArgs* a, int lanes, int rows, int resident) {
-    a->lanes = 1;
-    while (a->lanes < lanes) a->lanes *= 2;
-    const int groups = kRotThreads / a->lanes, tiles = (a->N + groups - 1) / groups;
+int plan_rotate(RotateArgs* a, int tokens, int rows, int resident) {
+    const int tiles = (a->N + tokens - 1) / tokens;
     a->unit_slabs = a->positions && a->pos_batch ? a->heads : a->slabs;
     const long long alone = (long long)tiles * (a->slabs / a->unit_slabs);          // blocks if each visits all slabs of its unit
     long long best = 0;
@@ -674,7 +705,8 @@ template <typename T> cudaError_t launch_rotate_type(RotateArgs a, int sm_count,
         const int turning = a.channels[0] + a.channels[1] + a.channels[2];
         lanes = turning / (2 * C) + (a.d - turning + 2 * C - 1) / (2 * C);
     }
-    const int tiles = plan_rotate(&a, lanes, tensors, 3 * sm_count);
+    a.lanes = lanes;
+    const int tiles = plan_rotate(&a, kRotThreads / 32 * (32 / lanes), tensors, 3 * sm_count);
     const dim3 grid(tiles, a.chunks * (a.slabs / a.unit_slabs));
     auto launch = [&](auto plain, auto norm) { return launch_dependent(a.norm ? norm : plain, grid, kRotThreads, 0, st, a); };
     if (kind == kNeighbours) return launch(rotate_pairs_kernel<T, false, false>, rotate_pairs_kernel<T, false, true>);
@@ -691,7 +723,9 @@ template <typename T, PairKind KIND> cudaError_t launch_backward_kind(const Rota
 }
 template <typename T> cudaError_t launch_rotate_bwd_type(RotateBwdArgs a, int sm_count, cudaStream_t st) {
     const int tensors = (a.fwd.x[0] != nullptr) + (a.fwd.x[1] != nullptr), most = backward_blocks(sm_count) / tensors;
-    const int tiles = plan_rotate(&a.fwd, (a.fwd.d + Elem<T>::kVec - 1) / Elem<T>::kVec, 1, most);
+    a.fwd.lanes = 1;
+    while (a.fwd.lanes * Elem<T>::kVec < a.fwd.d) a.fwd.lanes *= 2;
+    const int tiles = plan_rotate(&a.fwd, kRotThreads / a.fwd.lanes, 1, most);
     const long long items = (long long)tiles * a.fwd.chunks * (a.fwd.slabs / a.fwd.unit_slabs);
     const int blocks = (int)(items < most ? items : most);
     const dim3 grid(blocks, tensors);
