@@ -160,6 +160,10 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+def _dense_like(t: Optional[torch.Tensor]):
+    return None if t is None else torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 # torch.cuda.current_stream() builds a stream object (3.2 us); the raw handle costs 0.1 us
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _raw_device = getattr(torch._C, "_cuda_getDevice", None)
@@ -504,28 +508,36 @@ class AgentAttention:
         return out
 
     # ------------------------------------------------------------------ queries and keys before the attention
-    def _chk_views(self, named, n_tokens: int, dtype: torch.dtype):
-        """Views of shape [B, heads, N, d] that share their strides, or None; the strides as the library takes them."""
-        strides = None
-        for name, t in named:
+    def _chk_views(self, names, tensors, n_tokens: int, dtype: torch.dtype):
+        """Views of shape [B, heads, N, d] that share their strides, or None; the strides as the library takes them (None: dense)."""
+        shape, strides, dense = (self.batch, self.heads, n_tokens, self.head_dim), None, True
+        for name, t in zip(names, tensors):
             if t is None:
                 continue
-            if t.shape != (self.batch, self.heads, n_tokens, self.head_dim) or t.dtype is not dtype or not t.is_cuda or t.stride(3) != 1:
-                raise ValueError(f"{name}: expected a cuda {dtype} view of shape {(self.batch, self.heads, n_tokens, self.head_dim)} with contiguous "
-                                 f"channels, got {tuple(t.shape)} {t.dtype} on {t.device}")
-            st = tuple(s if n > 1 else self.head_dim for n, s in zip(t.shape, t.stride()[:3]))     # (of a single entry no stride is used)
+            if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
+                raise ValueError(f"{name}: expected a cuda {dtype} view of shape {shape} with contiguous channels, got {tuple(t.shape)} {t.dtype} on {t.device}")
+            if not t.is_contiguous():
+                dense = False
+        if dense:
+            return None
+        for name, t in zip(names, tensors):
+            if t is None:
+                continue
+            if t.stride(3) != 1:
+                raise ValueError(f"{name}: expected contiguous channels, got strides {t.stride()}")
+            st = tuple(s if n > 1 else self.head_dim for n, s in zip(shape, t.stride()[:3]))     # (of a single entry no stride is used)
             if strides is not None and st != strides:
                 raise ValueError(f"{name}: expected the strides {strides} of the other tensor, got {st}")
             strides = st
-        return None if strides is None else (ctypes.c_longlong * 3)(*strides)
+        return (ctypes.c_longlong * 3)(*strides)
 
     def _norm(self, q_gain, k_gain, eps):
-        self._chk_tensor(q_gain, (self.head_dim,), "q_gain")
-        self._chk_tensor(k_gain, (self.head_dim,), "k_gain")
         if eps is None:
             if q_gain is not None or k_gain is not None:
                 raise ValueError("a gain belongs to a norm: give eps")
             return None
+        self._chk_tensor(q_gain, (self.head_dim,), "q_gain")
+        self._chk_tensor(k_gain, (self.head_dim,), "k_gain")
         return ctypes.byref(AgentAttnNorm(_ptr(q_gain), _ptr(k_gain), eps))
 
     def rotate(self, q, k, rotary: Optional[Rotary] = None, q_gain=None, k_gain=None, eps: Optional[float] = None, out=None, stream=None):
@@ -540,18 +552,16 @@ class AgentAttention:
         if some is None:
             raise ValueError("q or k is required")
         N = some.shape[2] if some.dim() == 4 else 0
-        sin = self._chk_views((("q", q), ("k", k)), N, self.dtype)
+        sin = self._chk_views(("q", "k"), (q, k), N, self.dtype)
         if rotary is not None:
             rotary._check(self.batch, N)
         norm = self._norm(q_gain, k_gain, eps)
         if out is None:
-            shape = (self.batch, self.heads, N, self.head_dim)
-            out = tuple(None if t is None else torch.empty(shape, dtype=self.dtype, device=self.device) for t in (q, k))
-            sout = None
+            out, sout = (_dense_like(q), _dense_like(k)), None
         else:
             if any((t is None) != (o is None) for t, o in zip((q, k), out)):
                 raise ValueError("out: expected a tensor for each of q and k that is given")
-            sout = self._chk_views((("out[0]", out[0]), ("out[1]", out[1])), N, self.dtype)
+            sout = self._chk_views(("out[0]", "out[1]"), out, N, self.dtype)
         self._check(self.lib.agent_attn_rotate(self._h, _ptr(q), _ptr(k), sin, N, None if rotary is None else ctypes.byref(rotary._c), norm,
                                                _ptr(out[0]), _ptr(out[1]), sout, _stream_ptr(stream)))
         return out[0], out[1]
@@ -568,7 +578,7 @@ class AgentAttention:
             raise ValueError("dq_out or dk_out is required")
         N = some.shape[2] if some.dim() == 4 else 0
         f32 = torch.float32
-        sgrad = self._chk_views((("dq_out", dq_out), ("dk_out", dk_out)), N, f32)
+        sgrad = self._chk_views(("dq_out", "dk_out"), (dq_out, dk_out), N, f32)
         if rotary is not None:
             rotary._check(self.batch, N)
         norm = self._norm(q_gain, k_gain, eps)
@@ -576,15 +586,13 @@ class AgentAttention:
         if norm is not None:
             if (dq_out is not None and q is None) or (dk_out is not None and k is None):
                 raise ValueError("the gradient of a norm needs q and k")
-            sin = self._chk_views((("q", q), ("k", k)), N, self.dtype)
+            sin = self._chk_views(("q", "k"), (q, k), N, self.dtype)
         if out is None:
-            shape = (self.batch, self.heads, N, self.head_dim)
-            out = tuple(None if t is None else torch.empty(shape, dtype=f32, device=self.device) for t in (dq_out, dk_out))
-            sout = None
+            out, sout = (_dense_like(dq_out), _dense_like(dk_out)), None
         else:
             if any((t is None) != (o is None) for t, o in zip((dq_out, dk_out), out)):
                 raise ValueError("out: expected a tensor for each gradient that is given")
-            sout = self._chk_views((("out[0]", out[0]), ("out[1]", out[1])), N, f32)
+            sout = self._chk_views(("out[0]", "out[1]"), out, N, f32)
         got = {name: t for name, t in zip(("dq", "dk"), out) if t is not None}
         for name, gain, grad in (("dq_gain", q_gain, dq_out), ("dk_gain", k_gain, dk_out)):
             if gain is not None and grad is not None:
@@ -601,14 +609,16 @@ class AgentAttention:
     def _gate(self, x, w_gate, w_up, b_gate, b_up, activation):
         if activation not in _ACTIVATIONS:
             raise ValueError(f"activation: expected one of {sorted(_ACTIVATIONS)}, got {activation!r}")
-        if x.dim() < 1 or w_gate.dim() != 2:
+        if x.dim() == 0 or w_gate.dim() != 2:
             raise ValueError(f"expected x [..., channels] and weights [hidden, channels], got {tuple(x.shape)} and {tuple(w_gate.shape)}")
         F, C = w_gate.shape
         self._chk_tensor(x, x.shape[:-1] + (C,), "x")
-        self._chk_tensor(w_gate, (F, C), "w_gate")
-        self._chk_tensor(w_up, (F, C), "w_up")
-        self._chk_tensor(b_gate, (F,), "b_gate")
-        self._chk_tensor(b_up, (F,), "b_up")
+        for t, name in ((w_gate, "w_gate"), (w_up, "w_up")):
+            self._chk_tensor(t, (F, C), name)
+        if b_gate is not None:
+            self._chk_tensor(b_gate, (F,), "b_gate")
+        if b_up is not None:
+            self._chk_tensor(b_up, (F,), "b_up")
         rows = x.numel() // C if C else 0
         return AgentAttnGate(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(b_gate), _ptr(b_up), rows, C, F, _ACTIVATIONS[activation])
 
@@ -641,8 +651,9 @@ class AgentAttention:
         gate = self._gate(x, w_gate, w_up, b_gate, b_up, activation)
         shape = x.shape[:-1] + (gate.hidden,)
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
-        self._chk_tensor(out, shape, "out")
+            out = x.new_empty(shape)
+        else:
+            self._chk_tensor(out, shape, "out")
         ws = self._gate_workspace(gate, 0, workspace, stream)
         self._check(self.lib.agent_attn_gated(self._h, ctypes.byref(gate), _ptr(out), _ptr(ws), 0 if ws is None else ws.numel(), _stream_ptr(stream)))
         return out

@@ -417,7 +417,7 @@ template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(
 
 // A lane has one piece; partners through shared memory, where the row lies as it is in memory: 32-bit words (WORDS: fp32, or 16-bit segments of a
 // multiple of four channels, whose pairs' partners are pairs), else element by element.
-template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(kRotThreads, 3) rotate_patch_kernel(const __grid_constant__ RotateArgs p) {
+template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(kRotThreads, NORM ? 3 : 4) rotate_patch_kernel(const __grid_constant__ RotateArgs p) {
     constexpr int C = Elem<T>::kVec, kPer = sizeof(T) == 4 ? 1 : 2;  // elements of a word
     __shared__ uint4 s_ring[kDepth][kRotThreads];
     pdl_wait_prior();
@@ -706,7 +706,7 @@ template <typename T> cudaError_t launch_rotate_type(RotateArgs a, int sm_count,
         lanes = turning / (2 * C) + (a.d - turning + 2 * C - 1) / (2 * C);
     }
     a.lanes = lanes;
-    const int tiles = plan_rotate(&a, kRotThreads / 32 * (32 / lanes), tensors, 3 * sm_count);
+    const int tiles = plan_rotate(&a, kRotThreads / 32 * (32 / lanes), tensors, (kind == kHalvesShared && !a.norm ? 4 : 3) * sm_count);
     const dim3 grid(tiles, a.chunks * (a.slabs / a.unit_slabs));
     auto launch = [&](auto plain, auto norm) { return launch_dependent(a.norm ? norm : plain, grid, kRotThreads, 0, st, a); };
     if (kind == kNeighbours) return launch(rotate_pairs_kernel<T, false, false>, rotate_pairs_kernel<T, false, true>);
