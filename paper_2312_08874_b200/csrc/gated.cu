@@ -9,9 +9,9 @@
 //              columns makes both; the epilogue applies biases, activation and product.  G and U never leave the chip.
 //   kGrad      the same product again; the epilogue reads dH, writes dG and dU for the third form and sums their columns.
 //   kProducts  dX: A = dG, then dU (along their rows), B = Wg, then Wu, read as [hidden][channels] = MN-major: nothing is transposed.  dWg and dWu:
-//              A = dG in one block of the pair, dU in the other, both MN-major, B = X MN-major.  All their sums, cut into chunks of 64, are one line
-//              that the pairs share evenly: a pair takes a run of it, writes the tiles it has whole and leaves its share of those that it has not,
-//              and gated_finish_kernel adds the shares up in their order.
+//              A = dG in one block of the pair, dU in the other, both MN-major, B = X MN-major.  Their sums are cut into chunks of 64, of which all pairs
+//              have as many: whole tiles of dX, then a run of the other tiles; a pair writes what it has whole and leaves its share of what it has
+//              not, and gated_finish_kernel adds the shares up in their order.
 // 16-bit operands enter as they are; dG and dU are rounded to the element type, as every operand of a product on the tensor cores is.  fp32: operands are sums of
 // three bf16 terms, six pairs of terms, small ones first.
 #include "bwd_terms.cuh"
@@ -33,12 +33,16 @@ constexpr int kTimeoutTile = 3, kTimeoutRole = 6;
 constexpr int kRing = 6, BAR_FULL = 0, BAR_EMPTY = kRing, BAR_ACC = 2 * kRing, BAR_READ = BAR_ACC + 2, BAR_DRAIN = BAR_READ + 2, BAR_DH = BAR_DRAIN + 1, kBars = BAR_DH + kEpiWarps;
 static_assert(kBars * 8 <= 1024, "barriers");
 
-// The line of kProducts' work: tiles of dX, of 256 rows, then those of dWg and dWu, of 128 hidden units of both; n columns each
+// kProducts' work: tiles of dX, of 256 rows, and of dWg and dWu, of 128 hidden units of both; n columns each.  Every pair has some of the first `whole`
+// tiles of dX for itself; the other tiles of dX and those of the weights, cut into chunks, are a line of which it has a run, so long that all
+// pairs have as many chunks.  Where only one of the two is asked for, the other's tiles are left out, and the cuts stay where they are: the bits of a
+// gradient do not depend on what else is asked for.
 struct GatedLine {
-    int tiles_x, chunks_x, tiles_w, chunks_w, tiles_n, n, pairs;
-    __host__ __device__ long long length() const { return (long long)tiles_x * chunks_x + (long long)tiles_w * chunks_w; }
-    __host__ __device__ long long begin(int pair) const { return length() * pair / pairs; }
-    __host__ __device__ int pair_of(long long at) const { return (int)(((at + 1) * pairs - 1) / length()); }
+    int tiles_x, chunks_x, tiles_w, chunks_w, tiles_n, n, pairs, whole;
+    int dx, dw;                                        // asked for
+    __host__ __device__ long long total() const { return (long long)tiles_x * chunks_x + (long long)tiles_w * chunks_w; }
+    __host__ __device__ int own(int pair) const { return (int)((long long)whole * pair / pairs); }           // first tile of a pair's own
+    __host__ __device__ long long begin(int pair) const { return total() * pair / pairs - (long long)own(pair) * chunks_x; }
 };
 struct GatedArgs {
     int M, C, F, act;
@@ -182,14 +186,14 @@ template <typename T, GatedMode MODE, int BN> struct GatedShape {
     static constexpr bool kPair = BN == 128, kStaged = MODE == kProducts || (kPair && sizeof(T) == 2);
     static constexpr int kBTile = kPair ? kATile : 2 * BN * 128;
     static constexpr int kStage = kATile + kBTile;
-    static constexpr int kPatch = !kStaged ? 0 : MODE == kForward ? kHalfPatch : 2 * kHalfPatch;       // of a warp
-    static constexpr int kStages = MODE == kGrad ? 4 : 5;
+    static constexpr int kPatch = !kStaged ? 0 : MODE == kForward ? kHalfPatch : MODE == kGrad ? 3 * kHalfPatch : 2 * kHalfPatch;       // of a warp
+    static constexpr int kStages = kStaged && MODE == kGrad ? 3 : 5;
     static constexpr int kOffPatch = 1024 + kStages * kStage, kOffBias = kOffPatch + kEpiWarps * kPatch;
     static constexpr int kSmem = kOffBias + (MODE <= kGrad && kStaged ? kEpiWarps * 256 : 0) + 1024;
 };
 
 // What block (or pair) `who` of `count` does, tile by tile.  kForward and kGrad: a run of tiles in the order of the rows, so that a run has few column
-// ranges; kProducts: a run of the line.
+// ranges; kProducts: its own tiles, then its run of the line.
 struct Work {
     int mt, nt, k0, k1;
     bool weight, whole;                                // kProducts: of dWg and dWu; the whole sum
@@ -198,15 +202,22 @@ struct Work {
 template <GatedMode MODE> struct Walk {
     const GatedArgs& p;
     long long at, first, end;
-    int who;
+    int who, own, own_end;
     __device__ Walk(const GatedArgs& args, int who_, int count) : p(args), who(who_) {
-        const long long units = (long long)p.tiles_m * p.tiles_n;
-        first = at = MODE == kProducts ? p.line.begin(who) : units * who / count;
-        end = MODE == kProducts ? p.line.begin(who + 1) : units * (who + 1) / count;
+        if (MODE == kProducts) {
+            first = at = p.line.begin(who);
+            end = p.line.begin(who + 1);
+            own = p.line.own(who);
+            own_end = p.line.dx ? p.line.own(who + 1) : own;
+        } else {
+            const long long units = (long long)p.tiles_m * p.tiles_n;
+            first = at = units * who / count;
+            end = units * (who + 1) / count;
+        }
     }
     __device__ bool next(Work& w) {
-        if (at >= end) return false;
         if (MODE != kProducts) {
+            if (at >= end) return false;
             w.nt = (int)at / p.tiles_m;
             w.mt = (int)at - w.nt * p.tiles_m;
             w.k0 = 0; w.k1 = p.chunks;
@@ -214,18 +225,32 @@ template <GatedMode MODE> struct Walk {
             return true;
         }
         const GatedLine& l = p.line;
-        const long long split = (long long)l.tiles_x * l.chunks_x;
-        w.weight = at >= split;
-        const int chunks = w.weight ? l.chunks_w : l.chunks_x;
-        const long long here = w.weight ? at - split : at, left = end - at;
-        const int tile = (int)(here / chunks);
+        int tile = 0, chunks = l.chunks_x;
+        bool wanted = false;
+        if (own < own_end) {
+            tile = own++;
+            w.k0 = 0;
+            w.k1 = chunks;
+            w.weight = false;
+            wanted = true;
+        }
+        while (!wanted) {
+            if (at >= end) return false;
+            const long long rest = (long long)(l.tiles_x - l.whole) * l.chunks_x, left = end - at;
+            w.weight = at >= rest;
+            chunks = w.weight ? l.chunks_w : l.chunks_x;
+            const long long here = w.weight ? at - rest : at;
+            tile = (int)(here / chunks);
+            w.k0 = (int)(here - (long long)tile * chunks);
+            w.k1 = chunks - w.k0 < left ? chunks : (int)(w.k0 + left);
+            if (!w.weight) tile += l.whole;
+            w.slot = 2 * who + (at == first ? 0 : 1);
+            at += w.k1 - w.k0;
+            wanted = w.weight ? l.dw : l.dx;
+        }
         w.mt = tile / l.tiles_n;
         w.nt = tile - w.mt * l.tiles_n;
-        w.k0 = (int)(here - (long long)tile * chunks);
-        w.k1 = chunks - w.k0 < left ? chunks : (int)(w.k0 + left);
         w.whole = w.k0 == 0 && w.k1 == chunks;
-        w.slot = 2 * who + (at == first ? 0 : 1);
-        at += w.k1 - w.k0;
         return true;
     }
 };
@@ -392,8 +417,9 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             else pipe_arrive_warp(pp, BAR_READ + buf, lane);
         };
         if constexpr (MODE <= kGrad && S::kStaged) {
-            // Results leave through a patch of 32 rows of 64 bytes with their swizzle.  kGrad: dH arrives in the place that dG leaves from.
-            const uint32_t bias = base + S::kOffBias + warp * 256, row_at = patch + 64 * lane, swz = (lane >> 1) & 3;
+            // Results leave through a patch of 32 rows of 64 bytes with their swizzle.  kGrad: dU has one patch, dG two in turn, in which dH arrives a
+            // tile ahead and is overwritten.
+            const uint32_t bias = base + S::kOffBias + warp * 256, row_at = 64 * lane, swz = (lane >> 1) & 3;
             float2 column[2] = {};                                     // dG, dU: sums of two columns over this run's rows
             int column_nt = -1;
             auto flush = [&] {                                         // lanes l and l + 16 have even and odd rows of the same columns
@@ -409,14 +435,14 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     column[o] = both(0.f);
                 }
             };
-            auto fetch = [&](const Work& t) {                          // one lane: dH of a tile
+            auto fetch = [&](const Work& t, int i) {                   // one lane: dH of tile i
                 const uint32_t bar = pipe_bar(pp, BAR_DH + warp);
                 mbar_arrive_expect_tx(bar, kHalfPatch);
-                tma_load_3d(patch, &p.g, BN * t.nt + 32 * quarter, 256 * t.mt + 128 * rank + 32 * q, 0, bar);
+                tma_load_3d(patch + kHalfPatch * (i & 1), &p.g, BN * t.nt + 32 * quarter, 256 * t.mt + 128 * rank + 32 * q, 0, bar);
             };
             Work ahead;
             bool more = walk.next(ahead);
-            if (MODE == kGrad && lane == 0 && more) fetch(ahead);
+            if (MODE == kGrad && lane == 0 && more) fetch(ahead, 0);
             const bool biased = p.bg || p.bu;
             for (; more; ++ord) {
                 t = ahead;
@@ -438,8 +464,12 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 }
                 wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
                 tc_fence_after_sync();
-                if (MODE == kForward && lane == 0) store_wait_read<0>();            // the tile before has left the patch
-                if (MODE == kGrad) wait_par(pp, BAR_DH + warp, ord, kTimeoutTile);
+                if (lane == 0) store_wait_read<0>();                   // the tile before has left the patches
+                const uint32_t mine = patch + (MODE == kGrad ? kHalfPatch * (ord & 1) : 0), other = patch + 2 * kHalfPatch;
+                if (MODE == kGrad) {
+                    wait_par(pp, BAR_DH + warp, ord, kTimeoutTile);
+                    if (lane == 0 && more) fetch(ahead, ord + 1);
+                }
                 by_activation(p.act, [&](auto act) {
 #pragma unroll 1
                     for (int h = 0; h < 2; ++h) {                      // 16 hidden units
@@ -468,7 +498,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                                     vv[2 * i + 1] = fadd2(vv[2 * i + 1], make_float2(__uint_as_float(y.z), __uint_as_float(y.w)));
                                 }
                             }
-                            const uint32_t at = row_at + (((2 * h + c) ^ swz) << 4);
+                            const uint32_t at = mine + row_at + (((2 * h + c) ^ swz) << 4);
                             uint32_t o0[4];
                             [[maybe_unused]] uint32_t o1[4];
                             if constexpr (MODE == kForward) {
@@ -492,7 +522,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                                     o0[i] = pack2<T>(da.x, da.y);
                                     o1[i] = pack2<T>(a.x, a.y);
                                 }
-                                st_shared4(at + kHalfPatch, make_uint4(o1[0], o1[1], o1[2], o1[3]));
+                                st_shared4(at - mine + other, make_uint4(o1[0], o1[1], o1[2], o1[3]));
                             }
                             st_shared4(at, make_uint4(o0[0], o0[1], o0[2], o0[3]));
                         }
@@ -502,25 +532,21 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 __syncwarp();
                 const bool there = row0 < p.M && f0 < p.F;
                 if (lane == 0) {
-                    if (there) tma_store_3d(&p.s[0], f0, row0, 0, patch);
-                    if (MODE == kGrad && there) tma_store_3d(&p.s[1], f0, row0, 0, patch + kHalfPatch);
+                    if (there) tma_store_3d(&p.s[0], f0, row0, 0, mine);
+                    if (MODE == kGrad && there) tma_store_3d(&p.s[1], f0, row0, 0, other);
                     store_commit();
                 }
                 if (MODE == kGrad && p.column) {                       // columns 2 (lane % 16), every other row
-                    const uint32_t at = patch + 64 * (lane >> 4) + 4 * (lane & 3);
+                    const uint32_t at = 64 * (lane >> 4) + 4 * (lane & 3);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const uint32_t a = at + 128 * r + ((((lane & 15) >> 2) ^ (r & 3)) << 4);
-                        add_pair<T>(column[0], ld_shared1(a));
-                        add_pair<T>(column[1], ld_shared1(a + kHalfPatch));
+                        add_pair<T>(column[0], ld_shared1(mine + a));
+                        add_pair<T>(column[1], ld_shared1(other + a));
                     }
                     // (the sums are there, and with them what was loaded, before any lane goes on and the patch is handed to the next copy)
                     asm volatile("" ::"f"(column[0].x), "f"(column[0].y), "f"(column[1].x), "f"(column[1].y) : "memory");
                     __syncwarp();
-                }
-                if (MODE == kGrad && lane == 0 && more) {
-                    store_wait_read<0>();
-                    fetch(ahead);
                 }
             }
             if (MODE == kGrad && p.column && column_nt >= 0) flush();
@@ -688,7 +714,7 @@ template <typename T> __global__ void __launch_bounds__(256) gated_column_kernel
 }
 
 // What is left after kProducts, always in the same order.  The first blocks: sums of the columns of dG and dU (32 of the 2 F each) over the shares
-// that kGrad left (those of a column range are the pairs' that had it), or over `runs` rows of gated_column_kernel.  The others: 32 rows of a
+// that kGrad left (those of a column range are the pairs' that had it), or over `runs` rows of gated_column_kernel.  The others: eight rows of a
 // tile that no pair had whole: sum of its shares.
 struct FinishArgs {
     const float *share, *column;
@@ -697,7 +723,8 @@ struct FinishArgs {
     int M, C, F;
     int column_blocks, runs, tiles_m, units, count;      // column sums
 };
-template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel(const __grid_constant__ FinishArgs p) {
+constexpr int kThreadsFinish = 256;                      // more than there are pairs
+template <typename T> __global__ void __launch_bounds__(kThreadsFinish) gated_finish_kernel(const __grid_constant__ FinishArgs p) {
     __shared__ float s_sum[8][32];
     pdl_wait_prior();
     pdl_release_next();
@@ -712,7 +739,7 @@ template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel
                 const int first = (int)((((long long)nt * p.tiles_m + 1) * p.count - 1) / p.units), last = (int)(((long long)(nt + 1) * p.tiles_m * p.count - 1) / p.units);
                 slots = 8 * (last - first + 1);
             }
-#pragma unroll 4
+#pragma unroll 8
             for (int s = r; s < slots; s += 8) v += p.column[(size_t)s * 2 * p.F + i];
         }
         s_sum[r][lane] = v;
@@ -725,58 +752,67 @@ template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel
         return;
     }
     const GatedLine& l = p.line;
-    const int block = blockIdx.x - p.column_blocks, tile = block >> 3, row0 = 32 * (block & 7) + r;
+    const int block = blockIdx.x - p.column_blocks, tile = l.whole + (block >> 5), row0 = 8 * (block & 31);
     const bool weight = tile >= l.tiles_x;
+    if (!(weight ? l.dw : l.dx)) return;
     const int chunks = weight ? l.chunks_w : l.chunks_x, own = weight ? tile - l.tiles_x : tile, mt = own / l.tiles_n, nt = own - mt * l.tiles_n;
-    __shared__ int s_pairs[3];
-    if (threadIdx.x == 0) {                              // (divisions of 64 bits)
-        const long long begin = (weight ? (long long)l.tiles_x * l.chunks_x : 0ll) + (long long)own * chunks;
-        s_pairs[0] = l.pair_of(begin);
-        s_pairs[1] = l.pair_of(begin + chunks - 1);
-        s_pairs[2] = l.begin(s_pairs[0]) < begin;        // the first pair's run begins before the tile: its other slot
-    }
-    __syncthreads();
-    const int first = s_pairs[0], last = s_pairs[1];
-    if (first == last) return;                           // a pair had it whole
     const int limit = weight ? p.F - 128 * mt : p.M - 256 * mt;
-    for (int j = 4 * lane; j < l.n; j += 128) {
-        const int c = l.n * nt + j;
-        if (c >= p.C) break;
-        const float* src = p.share + ((size_t)(2 * first + s_pairs[2]) * 256 + row0) * l.n + j;
-        float4 v[4];                                     // four rows
+    if ((weight ? row0 & 127 : row0) >= limit) return;
+    // the pairs whose runs meet the tile, and the slots of their shares in their order: of the first pair, whose run begins before the tile or at it; of
+    // the others, whose runs begin in it (none where one is empty)
+    __shared__ long long s_begin[kThreadsFinish + 1];
+    __shared__ int s_slots[kThreadsFinish], s_counts[kThreadsFinish / 32];
+    const int q = threadIdx.x;
+    const long long begin = weight ? (long long)(l.tiles_x - l.whole) * l.chunks_x + (long long)own * chunks : (long long)(own - l.whole) * chunks;
+    const long long mine = q < l.pairs ? l.begin(q) : l.begin(l.pairs);
+    s_begin[q] = mine;
+    if (q == 0) s_begin[kThreadsFinish] = l.begin(l.pairs);
+    const int first = __syncthreads_count(q < l.pairs && mine <= begin) - 1, last = __syncthreads_count(q < l.pairs && mine < begin + chunks) - 1;
+    if (first == last) return;                           // a pair had it whole
+    const bool has = q >= first && q <= last && mine < s_begin[q + 1];
+    const unsigned there = __ballot_sync(0xffffffffu, has);
+    if (lane == 0) s_counts[r] = __popc(there);
+    __syncthreads();
+    int before = 0, count = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float4*>(src + (size_t)(8 * i) * l.n);
-        src = p.share + ((size_t)(2 * first + 2) * 256 + row0) * l.n + j;
-#pragma unroll 2
-        for (int q = first + 1; q <= last; ++q, src += (size_t)512 * l.n) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float4 w = *reinterpret_cast<const float4*>(src + (size_t)(8 * i) * l.n);
-                v[i].x += w.x; v[i].y += w.y; v[i].z += w.z; v[i].w += w.w;
-            }
+    for (int w = 0; w < kThreadsFinish / 32; ++w) {
+        before += w < r ? s_counts[w] : 0;
+        count += s_counts[w];
+    }
+    if (has) s_slots[before + __popc(there & ((1u << lane) - 1u))] = 2 * q + (mine < begin);
+    __syncthreads();
+    const int quads = l.n / 4;                           // of a row
+    for (int i = threadIdx.x; i < 8 * quads; i += kThreadsFinish) {
+        const int row = row0 + i / quads, j = 4 * (i % quads), in_tile = weight ? row & 127 : row, c = l.n * nt + j;
+        if (in_tile >= limit || c >= p.C) continue;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float* src = p.share + (size_t)row * l.n + j;
+#pragma unroll 8
+        for (int k = 0; k < count; ++k) {
+            const float4 w = *reinterpret_cast<const float4*>(src + (size_t)s_slots[k] * 256 * l.n);
+            v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = row0 + 8 * i, in_tile = weight ? row & 127 : row;
-            if (in_tile >= limit) continue;
-            T* out = static_cast<T*>(!weight ? p.dx : row < 128 ? p.dwg : p.dwu) + (size_t)(weight ? 128 * mt + in_tile : 256 * mt + row) * p.C + c;
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out) = v[i];
-            else *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(v[i].x, v[i].y), pack2<T>(v[i].z, v[i].w));
-        }
+        T* out = static_cast<T*>(!weight ? p.dx : row < 128 ? p.dwg : p.dwu) + (size_t)(weight ? 128 * mt + in_tile : 256 * mt + row) * p.C + c;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out) = v;
+        else *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(v.x, v.y), pack2<T>(v.z, v.w));
     }
 }
 
 // Tiles of at most 256 columns; at least six chunks a pair
-GatedLine plan_line(int M, int C, int F, bool dx, bool dw, int sm_count) {
+GatedLine plan_line(int M, int C, int F, int sm_count) {
     GatedLine l;
+    l.dx = l.dw = 1;
     l.tiles_n = (C + 255) / 256;
     l.n = ((C + l.tiles_n - 1) / l.tiles_n + 31) / 32 * 32;
-    l.tiles_x = dx ? (M + 255) / 256 * l.tiles_n : 0;
+    l.tiles_x = (M + 255) / 256 * l.tiles_n;
     l.chunks_x = 2 * ((F + 63) / 64);
-    l.tiles_w = dw ? (F + 127) / 128 * l.tiles_n : 0;
+    l.tiles_w = (F + 127) / 128 * l.tiles_n;
     l.chunks_w = (M + 63) / 64;
-    const long long most = (l.length() + 5) / 6;
-    l.pairs = (int)(most < sm_count / 2 ? most : sm_count / 2);
+    const long long most = (l.total() + 5) / 6;
+    const int pairs = sm_count / 2 < kThreadsFinish ? sm_count / 2 : kThreadsFinish;
+    l.pairs = (int)(most < pairs ? most : pairs);
+    const long long all = l.total() / l.pairs / l.chunks_x * l.pairs;        // no more whole tiles a pair than it has chunks
+    l.whole = (int)(all < l.tiles_x ? all : l.tiles_x);
     return l;
 }
 
@@ -818,7 +854,7 @@ GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count
         w.dg = take(planes);
         w.du = take(planes);
         const GatedTiles t = plan_tiles(M, F, sm_count);
-        w.share = take((size_t)(sm_count / 2) * 2 * 256 * plan_line(M, C, F, true, true, sm_count).n * 4);
+        w.share = take((size_t)(sm_count / 2) * 2 * 256 * plan_line(M, C, F, sm_count).n * 4);
         const size_t slots = dtype != kF32 && t.bn == 128 ? column_slots(t) : (M + kColRows - 1) / kColRows;
         w.db = take(slots * 2 * F * 4);
     }
@@ -917,11 +953,14 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
             ++*launches;
         }
     }
-    f.line = a.line = plan_line(c.M, c.C, c.F, c.dx != nullptr, c.dwg != nullptr, c.sm_count);
+    a.line = plan_line(c.M, c.C, c.F, c.sm_count);
+    a.line.dx = c.dx != nullptr;
+    a.line.dw = c.dwg != nullptr;
+    f.line = a.line;
     float* share = reinterpret_cast<float*>(ws + w.share);
     f.share = share;
     int shared_tiles = 0;
-    if (a.line.pairs) {
+    if (c.dx || c.dwg) {
         const GatedLine& l = a.line;
         const int unit = kWide ? 4 : 2;
         if (!make_map_3d_u16(&a.a[0], dg, kTerms, c.M, c.F, 128) || !make_map_3d_u16(&a.a[1], du, kTerms, c.M, c.F, 128) ||
@@ -932,9 +971,10 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
             !make_box_map(&a.share, share, 4, 2 * l.pairs, 256, l.n)) return cudaErrorInvalidValue;
         if ((e = launch_mode<T, kProducts, 128>(a, 2 * l.pairs, st)) != cudaSuccess) return e;
         ++*launches;
-        shared_tiles = l.tiles_x + l.tiles_w;
+        shared_tiles = l.tiles_x - l.whole + l.tiles_w;
     }
-    const long long blocks = f.column_blocks + 8ll * shared_tiles;
+    const long long blocks = f.column_blocks + 32ll * shared_tiles;
+    if (!blocks) return cudaSuccess;                       // (no biases, every tile a pair's own)
     if ((e = launch_dependent(gated_finish_kernel<T>, dim3((unsigned)blocks), 256, 0, st, f)) != cudaSuccess) return e;
     ++*launches;
     return cudaSuccess;
