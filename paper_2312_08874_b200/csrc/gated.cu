@@ -101,25 +101,30 @@ template <typename T, int ACT, bool GRAD> __device__ __forceinline__ void activa
         da = make_float2(d[0], d[1]);
     } else if constexpr (ACT == 1) {
         // Upper tail Q(x) = exp(-x^2 / 2) R(x), x = |g|, with R (half of a scaled complementary error function, smooth from 1/2 down) as a
-        // polynomial on [0, 5], fitted with weight exp(-x^2 / 2): Q is within 3e-7 (a 16-bit result of size 1e-3 ends at 2e-6).  One
-        // special-function instruction, which the derivative shares; the fast error function of the library takes 3.4 times the epilogue's time.
+        // polynomial on [0, 5], fitted with weight exp(-x^2 / 2): Q is within 3e-7 (a 16-bit result of size 1e-3 ends at 2e-6).  g Phi(g) =
+        // max(g, 0) - x Q(x).  One special-function instruction, which the derivative shares; with the library's error function the epilogue
+        // takes 3.4 times as long.
         const float2 x = make_float2(fminf(fabsf(g.x), 5.f), fminf(fabsf(g.y), 5.f));
         const float2 w = fmul2(fmul2(g, g), both(-0.72134752f));       // log2 of exp(-g^2 / 2)
         const float2 e = make_float2(fast_exp2(w.x), fast_exp2(w.y));
-        float2 r = both(-8.063080713e-06f);
-        r = ffma2(r, x, both(1.519420184e-04f));
-        r = ffma2(r, x, both(-1.271162881e-03f));
-        r = ffma2(r, x, both(6.382808089e-03f));
-        r = ffma2(r, x, both(-2.223088220e-02f));
-        r = ffma2(r, x, both(5.949680135e-02f));
-        r = ffma2(r, x, both(-1.317728907e-01f));
-        r = ffma2(r, x, both(2.497522980e-01f));
-        r = ffma2(r, x, both(-3.989226222e-01f));
-        r = ffma2(r, x, both(4.999997318e-01f));
-        const float2 h = ffma2(fmul2(e, both(-1.f)), r, both(0.5f));   // 1/2 - Q: Phi is that above 1/2, or below
-        const float2 cdf = fadd2(both(0.5f), make_float2(copysignf(h.x, g.x), copysignf(h.y, g.y)));
-        a = fmul2(g, cdf);
-        if (GRAD) da = ffma2(fmul2(g, both(0.39894228f)), e, cdf);
+        float2 r = both(8.063080713e-06f);                             // -R
+        r = ffma2(r, x, both(-1.519420184e-04f));
+        r = ffma2(r, x, both(1.271162881e-03f));
+        r = ffma2(r, x, both(-6.382808089e-03f));
+        r = ffma2(r, x, both(2.223088220e-02f));
+        r = ffma2(r, x, both(-5.949680135e-02f));
+        r = ffma2(r, x, both(1.317728907e-01f));
+        r = ffma2(r, x, both(-2.497522980e-01f));
+        r = ffma2(r, x, both(3.989226222e-01f));
+        r = ffma2(r, x, both(-4.999997318e-01f));
+        if (GRAD) {
+            const float2 h = ffma2(e, r, both(0.5f));                  // 1/2 - Q: Phi is that above 1/2, or below
+            const float2 cdf = fadd2(both(0.5f), make_float2(copysignf(h.x, g.x), copysignf(h.y, g.y)));
+            a = fmul2(g, cdf);
+            da = ffma2(fmul2(g, both(0.39894228f)), e, cdf);
+        } else {
+            a = ffma2(x, fmul2(e, r), make_float2(fmaxf(g.x, 0.f), fmaxf(g.y, 0.f)));
+        }
     } else {
         float2 z = fmul2(g, both(-kLog2e)), slope = both(1.f);
         if (ACT == 2) {
@@ -716,15 +721,16 @@ template <typename T> __global__ void __launch_bounds__(256) gated_column_kernel
 // What is left after kProducts, always in the same order.  The first blocks: sums of the columns of dG and dU (32 of the 2 F each) over the shares
 // that kGrad left (those of a column range are the pairs' that had it), or over `runs` rows of gated_column_kernel.  The others: eight rows of a
 // tile that no pair had whole: sum of its shares.
+constexpr int kMostPairs = 128;
 struct FinishArgs {
     const float *share, *column;
     void *dx, *dwg, *dwu, *dbg, *dbu;
     GatedLine line;
     int M, C, F;
     int column_blocks, runs, tiles_m, units, count;      // column sums
+    long long begin[kMostPairs + 1];                     // of the pairs' runs
 };
-constexpr int kThreadsFinish = 256;                      // more than there are pairs
-template <typename T> __global__ void __launch_bounds__(kThreadsFinish) gated_finish_kernel(const __grid_constant__ FinishArgs p) {
+template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel(const __grid_constant__ FinishArgs p) {
     __shared__ float s_sum[8][32];
     pdl_wait_prior();
     pdl_release_next();
@@ -739,8 +745,13 @@ template <typename T> __global__ void __launch_bounds__(kThreadsFinish) gated_fi
                 const int first = (int)((((long long)nt * p.tiles_m + 1) * p.count - 1) / p.units), last = (int)(((long long)(nt + 1) * p.tiles_m * p.count - 1) / p.units);
                 slots = 8 * (last - first + 1);
             }
-#pragma unroll 8
-            for (int s = r; s < slots; s += 8) v += p.column[(size_t)s * 2 * p.F + i];
+            for (int s = r; s < slots; s += 64) {        // eight in flight
+                float w[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) w[u] = s + 8 * u < slots ? p.column[(size_t)(s + 8 * u) * 2 * p.F + i] : 0.f;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v += w[u];
+            }
         }
         s_sum[r][lane] = v;
         __syncthreads();
@@ -760,42 +771,53 @@ template <typename T> __global__ void __launch_bounds__(kThreadsFinish) gated_fi
     if ((weight ? row0 & 127 : row0) >= limit) return;
     // the pairs whose runs meet the tile, and the slots of their shares in their order: of the first pair, whose run begins before the tile or at it; of
     // the others, whose runs begin in it (none where one is empty)
-    __shared__ long long s_begin[kThreadsFinish + 1];
-    __shared__ int s_slots[kThreadsFinish], s_counts[kThreadsFinish / 32];
+    __shared__ int s_slots[kMostPairs], s_counts[kMostPairs / 32];
     const int q = threadIdx.x;
     const long long begin = weight ? (long long)(l.tiles_x - l.whole) * l.chunks_x + (long long)own * chunks : (long long)(own - l.whole) * chunks;
-    const long long mine = q < l.pairs ? l.begin(q) : l.begin(l.pairs);
-    s_begin[q] = mine;
-    if (q == 0) s_begin[kThreadsFinish] = l.begin(l.pairs);
+    const long long mine = q < l.pairs ? p.begin[q] : 0, next = q < l.pairs ? p.begin[q + 1] : 0;
     const int first = __syncthreads_count(q < l.pairs && mine <= begin) - 1, last = __syncthreads_count(q < l.pairs && mine < begin + chunks) - 1;
     if (first == last) return;                           // a pair had it whole
-    const bool has = q >= first && q <= last && mine < s_begin[q + 1];
+    const bool has = q >= first && q <= last && mine < next;
     const unsigned there = __ballot_sync(0xffffffffu, has);
-    if (lane == 0) s_counts[r] = __popc(there);
+    if (lane == 0 && r < kMostPairs / 32) s_counts[r] = __popc(there);
     __syncthreads();
     int before = 0, count = 0;
 #pragma unroll
-    for (int w = 0; w < kThreadsFinish / 32; ++w) {
+    for (int w = 0; w < kMostPairs / 32; ++w) {
         before += w < r ? s_counts[w] : 0;
         count += s_counts[w];
     }
     if (has) s_slots[before + __popc(there & ((1u << lane) - 1u))] = 2 * q + (mine < begin);
     __syncthreads();
-    const int quads = l.n / 4;                           // of a row
-    for (int i = threadIdx.x; i < 8 * quads; i += kThreadsFinish) {
-        const int row = row0 + i / quads, j = 4 * (i % quads), in_tile = weight ? row & 127 : row, c = l.n * nt + j;
-        if (in_tile >= limit || c >= p.C) continue;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        const float* src = p.share + (size_t)row * l.n + j;
-#pragma unroll 8
-        for (int k = 0; k < count; ++k) {
-            const float4 w = *reinterpret_cast<const float4*>(src + (size_t)s_slots[k] * 256 * l.n);
-            v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-        }
-        T* out = static_cast<T*>(!weight ? p.dx : row < 128 ? p.dwg : p.dwu) + (size_t)(weight ? 128 * mt + in_tile : 256 * mt + row) * p.C + c;
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out) = v;
-        else *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(v.x, v.y), pack2<T>(v.z, v.w));
+    const int row = row0 + r, in_tile = weight ? row & 127 : row;
+    if (in_tile >= limit) return;
+    // a warp: a row of up to 256 columns
+    const int j0 = 4 * lane, c0 = l.n * nt + j0;
+    const bool live[2] = {j0 < l.n && c0 < p.C, j0 + 128 < l.n && c0 + 128 < p.C};
+    const float* src = p.share + (size_t)row * l.n + j0;
+    const size_t slot_size = (size_t)256 * l.n;
+    float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+    for (int k = 0; k < count; k += 8) {                 // eight shares in flight
+        float4 w[8][2];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                w[u][h] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (live[h] && k + u < count) w[u][h] = *reinterpret_cast<const float4*>(src + s_slots[k + u] * slot_size + 128 * h);
+            }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) { v[h].x += w[u][h].x; v[h].y += w[u][h].y; v[h].z += w[u][h].z; v[h].w += w[u][h].w; }
     }
+    T* out = static_cast<T*>(!weight ? p.dx : row < 128 ? p.dwg : p.dwu) + (size_t)(weight ? 128 * mt + in_tile : 256 * mt + row) * p.C + c0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (live[h]) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out + 128 * h) = v[h];
+            else *reinterpret_cast<uint2*>(out + 128 * h) = make_uint2(pack2<T>(v[h].x, v[h].y), pack2<T>(v[h].z, v[h].w));
+        }
 }
 
 // Tiles of at most 256 columns; at least six chunks a pair
@@ -809,7 +831,7 @@ GatedLine plan_line(int M, int C, int F, int sm_count) {
     l.tiles_w = (F + 127) / 128 * l.tiles_n;
     l.chunks_w = (M + 63) / 64;
     const long long most = (l.total() + 5) / 6;
-    const int pairs = sm_count / 2 < kThreadsFinish ? sm_count / 2 : kThreadsFinish;
+    const int pairs = sm_count / 2 < kMostPairs ? sm_count / 2 : kMostPairs;
     l.pairs = (int)(most < pairs ? most : pairs);
     const long long all = l.total() / l.pairs / l.chunks_x * l.pairs;        // no more whole tiles a pair than it has chunks
     l.whole = (int)(all < l.tiles_x ? all : l.tiles_x);
@@ -957,6 +979,7 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     a.line.dx = c.dx != nullptr;
     a.line.dw = c.dwg != nullptr;
     f.line = a.line;
+    for (int q = 0; q <= a.line.pairs; ++q) f.begin[q] = a.line.begin(q);
     float* share = reinterpret_cast<float*>(ws + w.share);
     f.share = share;
     int shared_tiles = 0;
