@@ -207,7 +207,7 @@ struct Work {
 template <GatedMode MODE> struct Walk {
     const GatedArgs& p;
     long long at, first, end;
-    int who, own, own_end;
+    int who, own, own_end, mt, nt;
     __device__ Walk(const GatedArgs& args, int who_, int count) : p(args), who(who_) {
         if (MODE == kProducts) {
             first = at = p.line.begin(who);
@@ -218,15 +218,17 @@ template <GatedMode MODE> struct Walk {
             const long long units = (long long)p.tiles_m * p.tiles_n;
             first = at = units * who / count;
             end = units * (who + 1) / count;
+            nt = (int)(at / p.tiles_m);
+            mt = (int)(at - (long long)nt * p.tiles_m);
         }
     }
     __device__ bool next(Work& w) {
         if (MODE != kProducts) {
             if (at >= end) return false;
-            w.nt = (int)at / p.tiles_m;
-            w.mt = (int)at - w.nt * p.tiles_m;
+            w.nt = nt; w.mt = mt;
             w.k0 = 0; w.k1 = p.chunks;
             ++at;
+            if (++mt == p.tiles_m) { mt = 0; ++nt; }
             return true;
         }
         const GatedLine& l = p.line;
@@ -414,12 +416,14 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
         // warp: 32 rows, and a quarter of a tile's hidden units (kForward, kGrad) or every fourth block of 32 columns
         const int q = warp & 3, quarter = warp >> 2;
         const uint32_t patch = base + S::kOffPatch + warp * S::kPatch;
-        const uint32_t read0 = PAIR ? in_block(pipe_bar(pp, BAR_READ), 0) : pipe_bar(pp, BAR_READ);
+        const uint32_t read0 = PAIR ? in_block(pipe_bar(pp, BAR_READ), 0) : pipe_bar(pp, BAR_READ), elected = elect_lane();
         int ord = 0;
         auto release = [&](int buf) {
             tc_fence_before_sync();
-            if (PAIR) arrive_cluster_warp(read0 + 8 * buf, lane);
-            else pipe_arrive_warp(pp, BAR_READ + buf, lane);
+            arrive_warp_e<PAIR>(elected, read0 + 8 * buf);
+        };
+        auto await = [&](int bar, int parity) {
+            if (!mbar_test(pipe_bar(pp, bar), parity & 1)) wait_par(pp, bar, parity, kTimeoutTile);
         };
         if constexpr (MODE <= kGrad && S::kStaged) {
             // Results leave through a patch of 32 rows of 64 bytes with their swizzle.  kGrad: dU has one patch, dG two in turn, in which dH arrives a
@@ -440,14 +444,14 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     column[o] = both(0.f);
                 }
             };
-            auto fetch = [&](const Work& t, int i) {                   // one lane: dH of tile i
+            auto fetch = [&](const Work& t, int i) {                   // dH of tile i
                 const uint32_t bar = pipe_bar(pp, BAR_DH + warp);
-                mbar_arrive_expect_tx(bar, kHalfPatch);
-                tma_load_3d(patch + kHalfPatch * (i & 1), &p.g, BN * t.nt + 32 * quarter, 256 * t.mt + 128 * rank + 32 * q, 0, bar);
+                mbar_arrive_expect_tx_e(elected, bar, kHalfPatch);
+                tma_load_3d_e<false>(elected, patch + kHalfPatch * (i & 1), &p.g, BN * t.nt + 32 * quarter, 256 * t.mt + 128 * rank + 32 * q, 0, bar);
             };
             Work ahead;
             bool more = walk.next(ahead);
-            if (MODE == kGrad && lane == 0 && more) fetch(ahead, 0);
+            if (MODE == kGrad && more) fetch(ahead, 0);
             const bool biased = p.bg || p.bu;
             for (; more; ++ord) {
                 t = ahead;
@@ -467,13 +471,14 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     asm volatile("st.shared.v2.f32 [%0], {%1, %2};\n" ::"r"(bias + 8 * lane), "f"(b.x), "f"(b.y) : "memory");
                     __syncwarp();
                 }
-                wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
+                await(BAR_ACC + buf, ord >> 1);
                 tc_fence_after_sync();
-                if (lane == 0) store_wait_read<0>();                   // the tile before has left the patches
+                store_wait_read<0>();                                  // the tile before has left the patches
+                __syncwarp();
                 const uint32_t mine = patch + (MODE == kGrad ? kHalfPatch * (ord & 1) : 0), other = patch + 2 * kHalfPatch;
                 if (MODE == kGrad) {
-                    wait_par(pp, BAR_DH + warp, ord, kTimeoutTile);
-                    if (lane == 0 && more) fetch(ahead, ord + 1);
+                    await(BAR_DH + warp, ord);
+                    if (more) fetch(ahead, ord + 1);
                 }
                 by_activation(p.act, [&](auto act) {
 #pragma unroll 1
@@ -535,12 +540,11 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 });
                 fence_proxy_async();
                 __syncwarp();
-                const bool there = row0 < p.M && f0 < p.F;
-                if (lane == 0) {
-                    if (there) tma_store_3d(&p.s[0], f0, row0, 0, mine);
-                    if (MODE == kGrad && there) tma_store_3d(&p.s[1], f0, row0, 0, other);
-                    store_commit();
+                if (row0 < p.M && f0 < p.F) {
+                    tma_store_3d_e(elected, &p.s[0], f0, row0, 0, mine);
+                    if (MODE == kGrad) tma_store_3d_e(elected, &p.s[1], f0, row0, 0, other);
                 }
+                store_commit();
                 if (MODE == kGrad && p.column) {                       // columns 2 (lane % 16), every other row
                     const uint32_t at = 64 * (lane >> 4) + 4 * (lane & 3);
 #pragma unroll
@@ -555,7 +559,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 }
             }
             if (MODE == kGrad && p.column && column_nt >= 0) flush();
-            if (lane == 0) store_wait_read<0>();
+            store_wait_read<0>();
             __syncwarp();
         } else if constexpr (MODE <= kGrad) {
             constexpr int kCols = BN / 4 > 16 ? BN / 4 : 16;           // of a warp (BN = 32: half of the warps have none)
@@ -563,7 +567,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 const int buf = ord & 1, row = (PAIR ? 256 : 128) * t.mt + 128 * rank + 32 * q + lane;
                 const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
                 const size_t plane = (size_t)p.M * p.F;
-                wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
+                await(BAR_ACC + buf, ord >> 1);
                 tc_fence_after_sync();
                 if (quarter * kCols >= BN) {
                     release(buf);
@@ -628,7 +632,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
                 const CUtensorMap* map = !t.whole ? &p.share : t.weight ? &p.s[1 + rank] : &p.s[0];
                 const bool wide = sizeof(T) == 4 || !t.whole;
-                wait_par(pp, BAR_ACC + buf, ord >> 1, kTimeoutTile);
+                await(BAR_ACC + buf, ord >> 1);
                 tc_fence_after_sync();
 #pragma unroll 1
                 for (int b = quarter; b < blocks; b += 4) {
@@ -637,7 +641,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     tmem_ld32(acc + 32 * b, reinterpret_cast<uint32_t(&)[32]>(v));
                     tmem_ld_wait();
                     if (b + 4 >= blocks) release(buf);
-                    if (lane == 0) store_wait_read<0>();
+                    store_wait_read<0>();
                     __syncwarp();
                     if (wide) {                                        // rows of 128 bytes
 #pragma unroll
@@ -649,16 +653,13 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     fence_proxy_async();
                     __syncwarp();
                     const int c0 = p.line.n * t.nt + 32 * b;
-                    if (lane == 0 && row0 < limit && c0 < p.C) {
-                        if (t.whole) tma_store_3d(map, c0, row0, 0, patch);
-                        else tma_store_3d(map, 32 * b, in_tile, t.slot, patch);
-                        store_commit();
-                    }
+                    if (row0 < limit && c0 < p.C) tma_store_3d_e(elected, map, t.whole ? c0 : 32 * b, t.whole ? row0 : in_tile, t.whole ? 0 : t.slot, patch);
+                    store_commit();
                 }
                 if (quarter >= blocks) release(buf);
                 __syncwarp();
             }
-            if (lane == 0) store_wait_read<0>();
+            store_wait_read<0>();
             __syncwarp();
         }
     }

@@ -18,11 +18,15 @@ __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-// One arrival on an mbarrier of a block of the cluster (a shared::cluster address), for a warp whose lanes have all done their part.  It tells of
-// tensor-memory reads, which are complete; a release at cluster scope would wait for the warp's global stores too (3000 cycles a tile).
-__device__ __forceinline__ void arrive_cluster_warp(uint32_t bar, int lane) {
+// One arrival of a warp whose lanes have all done their part, by its elected lane, on an mbarrier; CLUSTER: of a block of the cluster (a
+// shared::cluster address).  It tells of tensor-memory reads, which are complete; a release at cluster scope would wait for the warp's global stores
+// too (3000 cycles a tile).
+template <bool CLUSTER> __device__ __forceinline__ void arrive_warp_e(uint32_t elected, uint32_t bar) {
     __syncwarp();
-    if (lane == 0) asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
+    if constexpr (CLUSTER)
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}\n" ::"r"(bar), "r"(elected) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}\n" ::"r"(bar), "r"(elected) : "memory");
 }
 
 // Tensor memory of both blocks: a warp of each calls these
@@ -108,10 +112,13 @@ __device__ __forceinline__ void mbar_arrive_expect_tx_e(uint32_t elected, uint32
         "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}\n" ::"r"(bar), "r"(bytes), "r"(elected) : "memory");
 }
 
-// 3-D tiled store of a staged box (what lies outside the tensor is left out), and this thread's groups of stores
-__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];\n"
-                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
+// 3-D tiled store of a staged box by the elected lane (what lies outside the tensor is left out); the groups of stores are a thread's own, so that a warp
+// commits and waits as a whole
+__device__ __forceinline__ void tma_store_3d_e(uint32_t elected, const CUtensorMap* map, int x, int y, int z, uint32_t src) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+        "@q cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];\n\t}\n"
+        ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(src), "r"(elected) : "memory");
 }
 __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;\n" ::: "memory"); }
 // until all but the last N groups have been read out of shared memory
