@@ -673,6 +673,133 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
     }
 }
 
+// Forward pass of small fp32 problems on the CUDA cores, in one launch: a block has 32 rows and 32 hidden units of G and U, a thread four rows and two
+// units of both.  Against terms and tensor cores (rows x channels x hidden units, us): 196 x 192 x 512 6.6 and 9.8, 512 x 192 x 512 9.0 and 10.0, 4096 x 64 x 256
+// 11.2 and 9.2, 196 x 320 x 1280 13.7 and 13.4, 1024 x 192 x 512 15.2 and 11.3; it saves a launch and a workspace besides.
+constexpr long long kSmallProducts = 50000000;
+constexpr int kSmallThreads = 128, kSmallTile = 32, kSmallK = 32, kSmallPitch = kSmallK + 4, kSmallStages = 4;      // (pitch: eight rows in different banks)
+constexpr int kSmallSmem = kSmallStages * 3 * kSmallTile * kSmallPitch * 4;
+__global__ void __launch_bounds__(kSmallThreads) gated_small_kernel(const float* x, const float* wg, const float* wu, const float* bg, const float* bu, int M, int C, int F, int act, float* out) {
+    extern __shared__ __align__(16) float s_small[];      // [stage][X, Wg, Wu][row or unit][channel]
+    pdl_wait_prior();
+    pdl_release_next();
+    const int tid = threadIdx.x, m0 = kSmallTile * blockIdx.y, f0 = kSmallTile * blockIdx.x;
+    const int chunks = (C + kSmallK - 1) / kSmallK, lr = tid >> 3, lc = 4 * (tid & 7);
+    auto fetch = [&](int chunk) {
+        if (chunk < chunks) {
+            float* to = s_small + (chunk % kSmallStages) * 3 * kSmallTile * kSmallPitch;
+            const int c = kSmallK * chunk + lc;
+#pragma unroll
+            for (int i = 0; i < 3 * kSmallTile / 16; ++i) {
+                const int which = i / 2, row = 16 * (i % 2) + lr, at = (which ? f0 : m0) + row;
+                const bool there = c < C && at < (which ? F : M);
+                const float* src = which == 0 ? x : which == 1 ? wg : wu;
+                cp_async16(to + (which * kSmallTile + row) * kSmallPitch + lc, there ? src + (size_t)at * C + c : src, there ? 16 : 0);
+            }
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kSmallStages - 1; ++i) fetch(i);
+    const int row = tid & 7, unit = tid >> 3;             // rows row + 8 i, units unit + 16 j
+    float g[4][2] = {}, u[4][2] = {};
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        cp_async_wait<kSmallStages - 2>();
+        __syncthreads();
+        fetch(chunk + kSmallStages - 1);                  // into the stage that all have read before the barrier
+        const float* at = s_small + (chunk % kSmallStages) * 3 * kSmallTile * kSmallPitch;
+#pragma unroll
+        for (int k = 0; k < kSmallK; k += 4) {
+            float4 a[4], p[2], q[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(at + (row + 8 * i) * kSmallPitch + k);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                p[j] = *reinterpret_cast<const float4*>(at + (kSmallTile + unit + 16 * j) * kSmallPitch + k);
+                q[j] = *reinterpret_cast<const float4*>(at + (2 * kSmallTile + unit + 16 * j) * kSmallPitch + k);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    g[i][j] = fmaf(a[i].w, p[j].w, fmaf(a[i].z, p[j].z, fmaf(a[i].y, p[j].y, fmaf(a[i].x, p[j].x, g[i][j]))));
+                    u[i][j] = fmaf(a[i].w, q[j].w, fmaf(a[i].z, q[j].z, fmaf(a[i].y, q[j].y, fmaf(a[i].x, q[j].x, u[i][j]))));
+                }
+        }
+    }
+    cp_async_wait<0>();
+    by_activation(act, [&](auto a) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int f = f0 + unit + 16 * j;
+            if (f >= F) continue;
+            const float b = bg ? bg[f] : 0.f, d = bu ? bu[f] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+                float2 v, unused;
+                activate<float, decltype(a)::value, false>(make_float2(g[i][j] + b, g[i + 1][j] + b), v, unused);
+                const int m = m0 + row + 8 * i;
+                if (m < M) out[(size_t)m * F + f] = v.x * (u[i][j] + d);
+                if (m + 8 < M) out[(size_t)(m + 8) * F + f] = v.y * (u[i + 1][j] + d);
+            }
+        }
+    });
+}
+
+// Forward pass of few rows (single tokens): bound by the weights' bytes.  A warp has two hidden units and all rows, its lanes 16 bytes of channels at
+// a time; the weights are read once, the rows come from L1.  1024 channels, 4096 hidden units, bf16: one row 2.7 us (6.2 TB/s of weights that L2 holds; 10.6 on the
+// tensor cores, whose tiles of 128 rows are one row full), four 5.4 (10.8), eight 8.6 (9.8); 320 channels, 1280 units: 1.7, 2.9 (4.3), 4.5 (4.5), sixteen
+// rows 7.0 (4.3).  fp32, one row: 4.0 (70, the weights' terms).
+constexpr int kFewThreads = 128, kFewUnits = 2;
+template <typename T, int ROWS> __global__ void __launch_bounds__(kFewThreads) gated_few_kernel(const T* x, const T* wg, const T* wu, const T* bg, const T* bu, int M, int C, int F, int act, T* out) {
+    constexpr int V = Elem<T>::kVec;
+    pdl_wait_prior();
+    pdl_release_next();
+    const int lane = threadIdx.x & 31, f0 = kFewUnits * (blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5)), m0 = ROWS * blockIdx.y;
+    if (f0 >= F) return;                                  // (F is a multiple of eight)
+    float2 sum[ROWS][2 * kFewUnits] = {};                 // [row][gate, up of each unit], two halves
+#pragma unroll 2
+    for (int c = V * lane; c < C; c += 32 * V) {
+        float w[2 * kFewUnits][V];
+#pragma unroll
+        for (int i = 0; i < kFewUnits; ++i) {
+            unpack16<T>(__ldg(reinterpret_cast<const uint4*>(wg + (size_t)(f0 + i) * C + c)), w[2 * i]);
+            unpack16<T>(__ldg(reinterpret_cast<const uint4*>(wu + (size_t)(f0 + i) * C + c)), w[2 * i + 1]);
+        }
+#pragma unroll
+        for (int m = 0; m < ROWS; ++m) {
+            float a[V] = {};
+            if (m0 + m < M) unpack16<T>(__ldg(reinterpret_cast<const uint4*>(x + (size_t)(m0 + m) * C + c)), a);
+#pragma unroll
+            for (int i = 0; i < 2 * kFewUnits; ++i)
+#pragma unroll
+                for (int j = 0; j < V; j += 2) sum[m][i] = ffma2(make_float2(a[j], a[j + 1]), make_float2(w[i][j], w[i][j + 1]), sum[m][i]);
+        }
+    }
+    float g = 0.f, u = 0.f;                               // of row lane / kFewUnits, unit lane % kFewUnits
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m)
+#pragma unroll
+        for (int i = 0; i < 2 * kFewUnits; ++i) {
+            float v = sum[m][i].x + sum[m][i].y;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (lane == kFewUnits * m + i / 2) (i % 2 ? u : g) = v;
+        }
+    const int m = m0 + lane / kFewUnits, f = f0 + lane % kFewUnits;
+    if (lane >= ROWS * kFewUnits || m >= M) return;
+    if (bg) g += Elem<T>::to_f32(bg[f]);
+    if (bu) u += Elem<T>::to_f32(bu[f]);
+    by_activation(act, [&](auto a) {
+        float2 v, unused;
+        activate<T, decltype(a)::value, false>(both(g), v, unused);
+        out[(size_t)m * F + f] = Elem<T>::from_f32(v.x * u);
+    });
+}
+constexpr int kFewRows = 8;
+bool few_forward(int M) { return M <= kFewRows; }
+bool small_forward(int dtype, int M, int C, int F) { return dtype == kF32 && (long long)M * C * F <= kSmallProducts; }
+
 // fp32 -> three planes of bf16 terms, eight elements a thread
 struct SplitArgs {
     const float* src[3];
@@ -867,7 +994,7 @@ GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count
     GatedWs w;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
-    const size_t terms = dtype == kF32 ? 3 : 0;
+    const size_t terms = dtype == kF32 && (backward || !(few_forward(M) || small_forward(dtype, M, C, F))) ? 3 : 0;
     w.x = take(terms * M * C * 2);
     w.wg = take(terms * F * C * 2);
     w.wu = take(terms * F * C * 2);
@@ -930,6 +1057,21 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     char* ws = static_cast<char*>(c.ws);
     const void *x = c.x, *wg = c.wg, *wu = c.wu;
     cudaError_t e;
+    if (!c.dh && few_forward(c.M)) {
+        ++*launches;
+        auto few = [&](auto kern, int rows) {
+            return launch_dependent(kern, dim3((c.F + 4 * kFewUnits - 1) / (4 * kFewUnits), (c.M + rows - 1) / rows), kFewThreads, 0, st, static_cast<const T*>(x), static_cast<const T*>(wg),
+                                    static_cast<const T*>(wu), static_cast<const T*>(c.bg), static_cast<const T*>(c.bu), c.M, c.C, c.F, c.act, static_cast<T*>(c.h));
+        };
+        return c.M == 1 ? few(gated_few_kernel<T, 1>, 1) : c.M <= 4 ? few(gated_few_kernel<T, 4>, 4) : few(gated_few_kernel<T, 8>, 8);
+    }
+    if (!c.dh && small_forward(kWide ? kF32 : kBF16, c.M, c.C, c.F)) {
+        static std::atomic<unsigned long long> done{0};
+        if ((e = allow_smem(gated_small_kernel, done, kSmallSmem)) != cudaSuccess) return e;
+        ++*launches;
+        return launch_dependent(gated_small_kernel, dim3((c.F + kSmallTile - 1) / kSmallTile, (c.M + kSmallTile - 1) / kSmallTile), kSmallThreads, kSmallSmem, st, static_cast<const float*>(x),
+                                static_cast<const float*>(wg), static_cast<const float*>(wu), static_cast<const float*>(c.bg), static_cast<const float*>(c.bu), c.M, c.C, c.F, c.act, static_cast<float*>(c.h));
+    }
     if (kTerms > 1) {
         SplitArgs s = {{static_cast<const float*>(x), static_cast<const float*>(wg), static_cast<const float*>(wu)},
                        {reinterpret_cast<__nv_bfloat16*>(ws + w.x), reinterpret_cast<__nv_bfloat16*>(ws + w.wg), reinterpret_cast<__nv_bfloat16*>(ws + w.wu)},

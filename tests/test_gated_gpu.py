@@ -87,6 +87,21 @@ def test_both_directions_match_the_formulas(size, dtype, name, biases):
     assert all(torch.equal(again[n], back[n]) for n in back)                       # sums in a fixed order
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("size", [(1, 1024, 4096), (3, 24, 72), (4, 264, 136), (5, 512, 88), (8, 640, 1704), (9, 640, 1704), (64, 256, 1032), (33, 520, 40)])
+def test_few_rows_and_small_problems(size, dtype):
+    """Single tokens, a few of them, and what lies just past the lines of the kernels for few rows and small fp32 problems."""
+    M, C, F = size
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, "gu", seed=C)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    for name in ("silu", "gelu", "gelu_tanh"):
+        for g, u in ((bg, bu), (None, bu), (None, None)):
+            h, _ = reference(x, wg, wu, dh, g, u, name)
+            out = torch.full((M, F), float("nan"), device="cuda", dtype=DT[dtype])
+            check_forward(mod.gated(x, wg, wu, b_gate=g, b_up=u, activation=name, out=out), h, dtype)
+    assert mod.query_status() == 0
+
+
 @pytest.mark.parametrize("dtype,M,C,F", [("bf16", 20000, 192, 512), ("f16", 8192, 320, 1280), ("f32", 6000, 64, 256), ("bf16", 3000, 1032, 2728), ("f32", 200, 1024, 4096)])
 def test_long_sums_and_large_sizes(dtype, M, C, F):
     x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, "gu", seed=5)
