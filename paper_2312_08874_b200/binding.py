@@ -626,12 +626,12 @@ class AgentAttention:
         """The workspace of a call: the caller's, or a new one where one is needed."""
         if workspace is not None:
             return workspace
-        key = ("gated", gate.rows, gate.channels, gate.hidden, backward)
+        key = (gate.rows, gate.channels, gate.hidden, backward)
         need = self._bytes.get(key)
         if need is None:
             if len(self._bytes) >= 64:
                 self._bytes.clear()
-            need = self._bytes[key] = int(self.lib.agent_attn_gated_workspace_bytes(self._h, gate.rows, gate.channels, gate.hidden, backward))
+            need = self._bytes[key] = int(self.lib.agent_attn_gated_workspace_bytes(self._h, *key))
         return self._scratch(need, stream)
 
     def _scratch(self, nbytes: int, stream) -> Optional[torch.Tensor]:

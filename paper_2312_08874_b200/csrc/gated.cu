@@ -847,11 +847,13 @@ template <typename T> __global__ void __launch_bounds__(256) gated_column_kernel
 }
 
 // What is left after kProducts, always in the same order.  The first blocks: sums of the columns of dG and dU (32 of the 2 F each) over the shares
-// that kGrad left (those of a column range are the pairs' that had it), or over `runs` rows of gated_column_kernel.  The others: eight rows of a
+// that kGrad left (those of a column range are the pairs' that had it), over `runs` rows of gated_column_kernel, or over dG and dU themselves (few
+// rows: a launch less).  The others: eight rows of a
 // tile that no pair had whole: sum of its shares.
 constexpr int kMostPairs = 128;
 struct FinishArgs {
     const float *share, *column;
+    const void *dg, *du;                                 // summed here where they have at most kColRows rows and no shares
     void *dx, *dwg, *dwu, *dbg, *dbu;
     GatedLine line;
     int M, C, F;
@@ -866,7 +868,22 @@ template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel
     if ((int)blockIdx.x < p.column_blocks) {
         const int i = 32 * blockIdx.x + lane, op = i >= p.F, f = i - op * p.F;
         float v = 0.f;
-        if (i < 2 * p.F) {
+        if (i < 2 * p.F && p.dg) {
+            using E = typename GatedTerms<T>::E;
+            constexpr int kTerms = GatedTerms<T>::kTerms, kBatch = 8 / kTerms;
+            const E* src = static_cast<const E*>(op ? p.du : p.dg) + f;
+            for (int m = r; m < p.M; m += 8 * kBatch) {
+                float w[kBatch][kTerms];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t) w[u][t] = m + 8 * u < p.M ? Elem<E>::to_f32(src[((size_t)t * p.M + m + 8 * u) * p.F]) : 0.f;
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t) v += w[u][t];
+            }
+        } else if (i < 2 * p.F) {
             int slots = p.runs;
             if (!slots) {
                 const int nt = f / 128;
@@ -1112,7 +1129,10 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     if (c.dbg) {
         f.column_blocks = (2 * c.F + 31) / 32;
         f.tiles_m = t.tiles_m; f.units = t.tiles_m * t.tiles_n; f.count = t.blocks / 2;
-        if (!fused_columns) {
+        if (!fused_columns && c.M <= kColRows) {
+            f.dg = dg;
+            f.du = du;
+        } else if (!fused_columns) {
             f.runs = (c.M + kColRows - 1) / kColRows;
             if ((e = launch_dependent(gated_column_kernel<T>, dim3((c.F + 63) / 64, 2, f.runs), 256, 0, st, dg, du, c.M, c.F, column)) != cudaSuccess) return e;
             ++*launches;
