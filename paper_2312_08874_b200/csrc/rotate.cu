@@ -212,11 +212,13 @@ template <typename T> __device__ __forceinline__ void store_pairs(T* dst, const 
 // A thread's place in the forward kernels: the warp's lanes make up as many whole groups as there are
 struct Place {
     int gl, first, tok;                   // lane of the group, the group's first lane, token (past the last: none)
+    int row;                              // thread that has the first piece of the group's row; lanes that make up no whole group look at the warp's first row
     __device__ explicit Place(const RotateArgs& p) {
         const int lane = threadIdx.x & 31, in_warp = 32 / p.lanes, group = lane / p.lanes;
         gl = lane - group * p.lanes;
         first = lane - gl;
         tok = group < in_warp ? (blockIdx.x * (kRotThreads / 32) + (threadIdx.x >> 5)) * in_warp + group : p.N;
+        row = group < in_warp ? threadIdx.x - gl : threadIdx.x & ~31;
     }
 };
 
@@ -462,7 +464,7 @@ template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(k
         fetch(i + kDepth - 1, (stage + kDepth - 1) % kDepth);
         cp_async_wait<kDepth - 1>();
         __syncwarp();
-        const T* row = reinterpret_cast<const T*>(&s_ring[stage][threadIdx.x - gl]);
+        const T* row = reinterpret_cast<const T*>(&s_ring[stage][at.row]);
         float2 x[C / 2], y[C / 2];
         unpack_pairs<T>(s_ring[stage][threadIdx.x], x);
         if (WORDS) {

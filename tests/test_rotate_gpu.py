@@ -255,3 +255,23 @@ def test_refusals():
     assert lib.agent_attn_rotate_backward(h, g.data_ptr(), None, None, None, None, None, 16, None, None, g.data_ptr(), None, None, g.data_ptr(), None,
                                           None, 0, None) == 1                                              # a gain's gradient without a norm
     assert b"gain" in lib.agent_attn_last_error(h)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("d", [24, 40, 48, 56, 72, 80, 88, 104, 120])
+def test_heads_whose_lanes_leave_some_of_a_warp_idle(d, dtype):
+    """So many rows that a block works on more of them than its ring has stages, with groups of lanes that do not fill a warp: no lane may look past the
+    ring.  Halves of segments that are no whole pieces."""
+    B, h, extent, dt = 1, 16, (64, 64), DT[dtype]
+    N = extent[0] * extent[1]
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    q, k = views("dense", B, h, N, d, dt, gen)
+    gains = [(1 + 0.2 * torch.randn(d, generator=gen, device="cuda")).to(dt) for _ in range(2)]
+    mod = AgentAttention(B, h, d, N, 1, dt)
+    for channels in ((d // 2, d // 2), (d // 2 - 2, d // 2 + 2)):           # partners of 16 bits by words, one by one
+        freq = Rotary.frequencies(channels)
+        rotary = Rotary(freq, channels, extent)
+        for norm in (False, True):
+            given = dict(q_gain=gains[0], k_gain=gains[1], eps=1e-5) if norm else {}
+            for got, x, gain in zip(mod.rotate(q, k, rotary, **given), (q, k), gains):
+                check(got, *reference(x, grid_positions(extent), channels, freq, False, gain if norm else None, 1e-5 if norm else None), dtype)
