@@ -11,10 +11,14 @@
 // less its nearest integer, so that large positions cost no accuracy.  Where the channels of a pair lie, in the order of preference:
 //   forward, rotate_pairs_kernel: a lane has two pieces of 16 bytes that hold whole pairs: a piece of a segment's first half and the one half a segment
 //     on, or two pieces with neighbouring channels as pairs.  Nothing crosses lanes but the norm's sum.
-//   forward, rotate_patch_kernel: halves that are no whole pieces: a lane has one piece, its partners come through shared memory.
-//   backward: a lane has one piece; partners by shuffles (whole pieces) or through shared memory.
-// The next rows are loaded before the present ones are worked on.  Bound by HBM: forward 4 bytes an element of 16 bits, backward 10; what stands in the
-// way of that is the issue of instructions.
+//   forward, rotate_patch_kernel: halves that are no whole pieces, and 16 bits without a norm: a lane has one piece, its partners come through shared
+//     memory.  Whole pieces both ways (us, pairs and patch): bf16 with a norm 64 slabs of 56 x 56 18.8 and 32.0, 16 of 128 x 128 25.6 and 39.3; without
+//     a norm 19.6 and 18.0, 25.4 and 23.7 (four blocks an SM instead of three); fp32 8 slabs of 128 x 128 x 32 channels 15.2 and 19.6, 10.9 and 11.7.
+//   backward: a lane has one piece; partners are whole pieces of the row in shared memory, or single channels (48 and 66 us on 64 slabs of 56 x 56).
+// Rows arrive by asynchronous copies, three ahead.  Bound by HBM, forward 4 bytes an element of 16 bits, backward 10, with the issue of instructions close
+// behind it (57 % to 73 % of the slots).  A pass among others, inputs that L2 does not hold, 64 channels: norm and rotation on a 256 x 256 grid, 16 slabs,
+// 537 MB in 100 us (5.4 TB/s); 64 slabs of 56 x 56, 103 MB in 23 us (4.4 TB/s, starts and angles 5 us of it); rotation of a video grid, 236 MB in 45 us
+// (5.2 TB/s); gradient on a 128 x 128 grid, 336 MB in 66 us (5.1 TB/s).
 #include "common.cuh"
 #include "kernels.h"
 
@@ -185,10 +189,11 @@ template <int C> __device__ __forceinline__ void turned(const float2 (&x)[C / 2]
         }
     }
 }
-// Element offsets of a row, slab after slab
-struct RowWalk {
-    long long at, step, wrap;             // from head to head; from the last head to the next batch entry
-    __device__ RowWalk(const TokLayout& l, int slab, int heads, int tok, int c) : at(tok_offset(l, slab, heads, tok) + c), step(l.sh), wrap(l.sb - (heads - 1) * l.sh) {}
+// Where a row lies, slab after slab
+template <typename T> struct RowWalk {
+    T* at;
+    long long step, wrap;                 // from head to head; from the last head to the next batch entry
+    __device__ RowWalk(T* base, const TokLayout& l, int slab, int heads, int tok, int c) : at(base + tok_offset(l, slab, heads, tok) + c), step(l.sh), wrap(l.sb - (heads - 1) * l.sh) {}
     __device__ void next(bool last_head) { at += last_head ? wrap : step; }
 };
 
@@ -535,18 +540,23 @@ template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThrea
         const bool token = tok < f.N, live = token && c0 < f.d;
         const int here = min(tok, f.N - 1), ch = c0 < f.d ? c0 : 0;
         const int unit = run / f.chunks, s0 = unit * f.unit_slabs + (run % f.chunks) * f.share, n = min(f.share, (unit + 1) * f.unit_slabs - s0);
-        RowWalk in(f.lin, s0, f.heads, here, ch), gin(p.lgrad, s0, f.heads, here, 0), out(f.lout, s0, f.heads, here, 0);
+        RowWalk<const T> in(xs, f.lin, s0, f.heads, here, ch);
+        RowWalk<const float> gin(grad, p.lgrad, s0, f.heads, here, 0);
+        RowWalk<float> out(dst, f.lout, s0, f.heads, here, 0);
         int head = s0 % f.heads, fhead = head;
-        auto fetch = [&](int i) {
-            if (i < n) {
-                uint4* to = ring + (i % kAhead) * kStage;
-                cp_async16(to + threadIdx.x, xs + in.at, live ? 16 : 0);
+        int piece_at[kPieces], piece_size[kPieces];
 #pragma unroll
-                for (int k = 0; k < kPieces; ++k) {
-                    const int piece = gl + k * f.lanes;
-                    const bool there = token && 4 * piece < f.d;
-                    cp_async16(to + row_at + piece, grad + gin.at + (there ? 4 * piece : 0), there ? 16 : 0);
-                }
+        for (int k = 0; k < kPieces; ++k) {
+            const int at = 4 * (gl + k * f.lanes);
+            piece_size[k] = token && at < f.d ? 16 : 0;
+            piece_at[k] = at < f.d ? at : 0;
+        }
+        auto fetch = [&](int i, int stage) {
+            if (i < n) {
+                uint4* to = ring + stage * kStage;
+                cp_async16(to + threadIdx.x, in.at, live ? 16 : 0);
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) cp_async16(to + row_at + gl + k * f.lanes, gin.at + piece_at[k], piece_size[k]);
                 const bool wrap = ++fhead == f.heads;
                 if (wrap) fhead = 0;
                 in.next(wrap);
@@ -556,16 +566,15 @@ template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThrea
         };
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < kAhead - 1; ++i) fetch(i);
+        for (int i = 0; i < kAhead - 1; ++i) fetch(i, i);
         float2 cs[C / 2], sn[C / 2];
         token_turns<C, KIND, false>(f, la, s0 / f.heads, here, partner_lane, true, cs, sn);
-#pragma unroll 1
-        for (int i = 0; i < n; ++i) {
+        auto row_of = [&](int i, int stage) {
             __syncwarp();                                                    // (the stage that is filled next has been read by the whole warp)
-            fetch(i + kAhead - 1);
+            fetch(i + kAhead - 1, (stage + kAhead - 1) % kAhead);
             cp_async_wait<kAhead - 1>();
             __syncwarp();
-            const uint4* from = ring + (i % kAhead) * kStage;
+            const uint4* from = ring + stage * kStage;
             const float* row = reinterpret_cast<const float*>(from + row_at);
             float2 x[C / 2], g[C / 2], y[C / 2];
             unpack_pairs<T>(from[threadIdx.x], x);
@@ -606,7 +615,7 @@ template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThrea
                 v[2 * k] = y[k].x;
                 v[2 * k + 1] = y[k].y;
             }
-            float* to = dst + out.at;
+            float* to = out.at;
             if (kPieces == 1) {
                 if (live) *reinterpret_cast<float4*>(to + c0) = make_float4(v[0], v[1], v[2], v[3]);
             } else if (f.lanes == 1) {
@@ -630,6 +639,12 @@ template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThrea
             const bool wrap = ++head == f.heads;
             if (wrap) head = 0;
             out.next(wrap);
+        };
+#pragma unroll 1
+        for (int i = 0; i < n; i += kAhead) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (i + k < n) row_of(i + k, k);
         }
     }
     float* s_sum = reinterpret_cast<float*>(s_dyn);
@@ -677,7 +692,8 @@ PairKind pair_kind(const RotateArgs& a, int c) {
 }
 
 // How many slabs a block visits with one set of angles; `tokens` of a block.  Fewer: the angles cost more, as much as
-// four rows; more: the last of the waves of `resident` blocks is emptier.  `rows`: of a slab (the tensors of a block).
+// four rows; more: the last of the waves of `resident` blocks is emptier.  `rows`: of a slab (the tensors of a block).  With angles at
+// 0, 2, 4, 8 and 16 rows norm and rotation of 16 slabs of 128 x 128 take 96, 45, 39, 39 and 43 us.
 int plan_rotate(RotateArgs* a, int tokens, int rows, int resident) {
     const int tiles = (a->N + tokens - 1) / tokens;
     a->unit_slabs = a->positions && a->pos_batch ? a->heads : a->slabs;
@@ -700,7 +716,8 @@ int plan_rotate(RotateArgs* a, int tokens, int rows, int resident) {
 template <typename T> cudaError_t launch_rotate_type(RotateArgs a, int sm_count, cudaStream_t st) {
     constexpr int C = Elem<T>::kVec;
     const int tensors = (a.x[0] != nullptr) + (a.x[1] != nullptr);
-    const PairKind kind = pair_kind(a, C);
+    PairKind kind = pair_kind(a, C);
+    if (C == 8 && !a.norm && kind == kHalvesShuffle) kind = kHalvesShared;
     int lanes = (a.d + C - 1) / C;
     if (kind == kNeighbours) lanes = (a.d + 2 * C - 1) / (2 * C);
     if (kind == kHalvesShuffle) {
@@ -712,7 +729,7 @@ template <typename T> cudaError_t launch_rotate_type(RotateArgs a, int sm_count,
     const dim3 grid(tiles, a.chunks * (a.slabs / a.unit_slabs));
     auto launch = [&](auto plain, auto norm) { return launch_dependent(a.norm ? norm : plain, grid, kRotThreads, 0, st, a); };
     if (kind == kNeighbours) return launch(rotate_pairs_kernel<T, false, false>, rotate_pairs_kernel<T, false, true>);
-    if (kind == kHalvesShuffle) return launch(rotate_pairs_kernel<T, true, false>, rotate_pairs_kernel<T, true, true>);
+    if (kind == kHalvesShuffle) return launch(rotate_pairs_kernel<T, true, C == 8>, rotate_pairs_kernel<T, true, true>);
     const bool words = C == 4 || (a.channels[0] % 4 == 0 && a.channels[1] % 4 == 0 && a.channels[2] % 4 == 0);
     if (words) return launch(rotate_patch_kernel<T, true, false>, rotate_patch_kernel<T, true, true>);
     return launch(rotate_patch_kernel<T, C == 4, false>, rotate_patch_kernel<T, C == 4, true>);
