@@ -179,10 +179,8 @@ __device__ __forceinline__ uint4 ld_shared4(uint32_t at) {
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
-__device__ __forceinline__ uint32_t ld_shared1(uint32_t at) {
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(v) : "r"(at) : "memory");
-    return v;
+__device__ __forceinline__ void ld_matrix4_trans(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
 
 // A pair of blocks takes a tile of 256 rows, each of its blocks 128 of them and half of the B operand (BN = 128, and kProducts); a lone block a tile of
@@ -429,19 +427,19 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             // Results leave through a patch of 32 rows of 64 bytes with their swizzle.  kGrad: dU has one patch, dG two in turn, in which dH arrives a
             // tile ahead and is overwritten.
             const uint32_t bias = base + S::kOffBias + warp * 256, row_at = 64 * lane, swz = (lane >> 1) & 3;
-            float2 column[2] = {};                                     // dG, dU: sums of two columns over this run's rows
+            // dG, dU: sums of the columns over this run's rows, as products of their transpose with ones: a lane has those of columns lane / 4 + 8 i
+            float column[2][2][4] = {};                                // [dG, dU][16 columns][i, twice]
             int column_nt = -1;
-            auto flush = [&] {                                         // lanes l and l + 16 have even and odd rows of the same columns
+            auto flush = [&] {
                 const int first = (int)((((long long)column_nt * p.tiles_m + 1) * count - 1) / ((long long)p.tiles_m * p.tiles_n));
                 float* dst = p.column + (size_t)(8 * (who - first) + 4 * rank + q) * 2 * p.F;
-                const int f = BN * column_nt + 32 * quarter + 2 * (lane & 15);
+                const int f = BN * column_nt + 32 * quarter + 8 * (lane & 3) + (lane >> 2);
 #pragma unroll
                 for (int o = 0; o < 2; ++o) {
-                    float2 v = column[o];
-                    v.x += __shfl_xor_sync(0xffffffffu, v.x, 16);
-                    v.y += __shfl_xor_sync(0xffffffffu, v.y, 16);
-                    if (lane < 16 && f < p.F) *reinterpret_cast<float2*>(dst + (size_t)o * p.F + f) = v;
-                    column[o] = both(0.f);
+                    const float lo = lane & 1 ? column[o][0][2] : column[o][0][0], hi = lane & 1 ? column[o][1][2] : column[o][1][0];
+                    if (f < p.F) dst[(size_t)o * p.F + f] = lane & 2 ? hi : lo;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) column[o][i / 4][i % 4] = 0.f;
                 }
             };
             auto fetch = [&](const Work& t, int i) {                   // dH of tile i
@@ -453,6 +451,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             bool more = walk.next(ahead);
             if (MODE == kGrad && more) fetch(ahead, 0);
             const bool biased = p.bg || p.bu;
+            int bias_nt = -1;
             for (; more; ++ord) {
                 t = ahead;
                 more = walk.next(ahead);
@@ -462,7 +461,8 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     if (column_nt >= 0) flush();
                     column_nt = t.nt;
                 }
-                if (biased) {                                          // as fp32: [gate | up][32]
+                if (biased && bias_nt != t.nt) {                       // as fp32: [gate | up][32]
+                    bias_nt = t.nt;
                     const int f = f0 + 2 * (lane & 15);
                     const void* src = lane < 16 ? p.bg : p.bu;
                     float2 b = both(0.f);
@@ -545,17 +545,19 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     if (MODE == kGrad) tma_store_3d_e(elected, &p.s[1], f0, row0, 0, other);
                 }
                 store_commit();
-                if (MODE == kGrad && p.column) {                       // columns 2 (lane % 16), every other row
-                    const uint32_t at = 64 * (lane >> 4) + 4 * (lane & 3);
+                if (MODE == kGrad && p.column) {
+                    constexpr uint32_t kOnes = Elem<T>::kIsBf16 ? 0x3f803f80u : 0x3c003c00u;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const uint32_t a = at + 128 * r + ((((lane & 15) >> 2) ^ (r & 3)) << 4);
-                        add_pair<T>(column[0], ld_shared1(mine + a));
-                        add_pair<T>(column[1], ld_shared1(other + a));
+                    for (int k = 0; k < 4; ++k) {                      // 16 rows (k / 2) of 16 columns (k % 2)
+                        const int row = 16 * (k >> 1) + (lane & 7) + 8 * (lane >> 4), piece = 2 * (k & 1) + ((lane >> 3) & 1);
+                        const uint32_t a = 64 * row + ((piece ^ ((row >> 1) & 3)) << 4);
+                        uint32_t m0[4], m1[4];
+                        ld_matrix4_trans(m0, mine + a);
+                        ld_matrix4_trans(m1, other + a);
+                        mma16816<T>(column[0][k & 1], m0, kOnes, kOnes);
+                        mma16816<T>(column[1][k & 1], m1, kOnes, kOnes);
                     }
-                    // (the sums are there, and with them what was loaded, before any lane goes on and the patch is handed to the next copy)
-                    asm volatile("" ::"f"(column[0].x), "f"(column[0].y), "f"(column[1].x), "f"(column[1].y) : "memory");
-                    __syncwarp();
+                    __syncwarp();                                      // (every lane has read before the patch is handed to the next copy)
                 }
             }
             if (MODE == kGrad && p.column && column_nt >= 0) flush();
@@ -848,9 +850,8 @@ template <typename T> __global__ void __launch_bounds__(256) gated_column_kernel
 
 // What is left after kProducts, always in the same order.  The first blocks: sums of the columns of dG and dU (32 of the 2 F each) over the shares
 // that kGrad left (those of a column range are the pairs' that had it), over `runs` rows of gated_column_kernel, or over dG and dU themselves (few
-// rows: a launch less).  The others: eight rows of a
-// tile that no pair had whole: sum of its shares.
-constexpr int kMostPairs = 128;
+// rows: a launch less).  The others: 1024 values of a tile that no pair had whole, as the sum of its shares, whose list the host makes.
+constexpr int kMostPairs = 128, kShares = 12;            // shares in flight
 struct FinishArgs {
     const float *share, *column;
     const void *dg, *du;                                 // summed here where they have at most kColRows rows and no shares
@@ -858,8 +859,39 @@ struct FinishArgs {
     GatedLine line;
     int M, C, F;
     int column_blocks, runs, tiles_m, units, count;      // column sums
-    long long begin[kMostPairs + 1];                     // of the pairs' runs
+    int tiles;                                           // with shares: which ones, and their slots in their order
+    int tile[kMostPairs];
+    unsigned short first[kMostPairs + 1];
+    unsigned char slot[2 * kMostPairs];
 };
+// A pair has at most two tiles in part: the first and the last of its run
+void list_shares(FinishArgs* f) {
+    const GatedLine& l = f->line;
+    const long long rest = (long long)(l.tiles_x - l.whole) * l.chunks_x;
+    int entries = 0;
+    for (int q = 0; q < l.pairs; ++q) {
+        const long long first = l.begin(q), end = l.begin(q + 1);
+        for (long long at = first; at < end;) {
+            const bool weight = at >= rest;
+            const int chunks = weight ? l.chunks_w : l.chunks_x, own = (int)((weight ? at - rest : at) / chunks);
+            const long long begin = (weight ? rest : 0) + (long long)own * chunks, limit = weight || end < rest ? end : rest;
+            if (at == begin && limit - at >= chunks) {                // whole tiles
+                at += (limit - at) / chunks * chunks;
+                continue;
+            }
+            if (weight ? l.dw : l.dx) {
+                const int tile = weight ? l.tiles_x + own : l.whole + own;
+                if (!f->tiles || f->tile[f->tiles - 1] != tile) {
+                    f->first[f->tiles] = (unsigned short)entries;
+                    f->tile[f->tiles++] = tile;
+                }
+                f->slot[entries++] = (unsigned char)(2 * q + (at == first ? 0 : 1));
+            }
+            at = begin + chunks < end ? begin + chunks : end;
+        }
+    }
+    f->first[f->tiles] = (unsigned short)entries;
+}
 template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel(const __grid_constant__ FinishArgs p) {
     __shared__ float s_sum[8][32];
     pdl_wait_prior();
@@ -890,12 +922,12 @@ template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel
                 const int first = (int)((((long long)nt * p.tiles_m + 1) * p.count - 1) / p.units), last = (int)(((long long)(nt + 1) * p.tiles_m * p.count - 1) / p.units);
                 slots = 8 * (last - first + 1);
             }
-            for (int s = r; s < slots; s += 64) {        // eight in flight
-                float w[8];
+            for (int s = r; s < slots; s += 8 * kShares) {
+                float w[kShares];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) w[u] = s + 8 * u < slots ? p.column[(size_t)(s + 8 * u) * 2 * p.F + i] : 0.f;
+                for (int u = 0; u < kShares; ++u) w[u] = s + 8 * u < slots ? p.column[(size_t)(s + 8 * u) * 2 * p.F + i] : 0.f;
 #pragma unroll
-                for (int u = 0; u < 8; ++u) v += w[u];
+                for (int u = 0; u < kShares; ++u) v += w[u];
             }
         }
         s_sum[r][lane] = v;
@@ -908,61 +940,25 @@ template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel
         return;
     }
     const GatedLine& l = p.line;
-    const int block = blockIdx.x - p.column_blocks, tile = l.whole + (block >> 5), row0 = 8 * (block & 31);
+    const int per = l.n / 4, block = blockIdx.x - p.column_blocks, which = block / per, tile = p.tile[which], e = 1024 * (block - which * per) + 4 * threadIdx.x;
     const bool weight = tile >= l.tiles_x;
-    if (!(weight ? l.dw : l.dx)) return;
-    const int chunks = weight ? l.chunks_w : l.chunks_x, own = weight ? tile - l.tiles_x : tile, mt = own / l.tiles_n, nt = own - mt * l.tiles_n;
-    const int limit = weight ? p.F - 128 * mt : p.M - 256 * mt;
-    if ((weight ? row0 & 127 : row0) >= limit) return;
-    // the pairs whose runs meet the tile, and the slots of their shares in their order: of the first pair, whose run begins before the tile or at it; of
-    // the others, whose runs begin in it (none where one is empty)
-    __shared__ int s_slots[kMostPairs], s_counts[kMostPairs / 32];
-    const int q = threadIdx.x;
-    const long long begin = weight ? (long long)(l.tiles_x - l.whole) * l.chunks_x + (long long)own * chunks : (long long)(own - l.whole) * chunks;
-    const long long mine = q < l.pairs ? p.begin[q] : 0, next = q < l.pairs ? p.begin[q + 1] : 0;
-    const int first = __syncthreads_count(q < l.pairs && mine <= begin) - 1, last = __syncthreads_count(q < l.pairs && mine < begin + chunks) - 1;
-    if (first == last) return;                           // a pair had it whole
-    const bool has = q >= first && q <= last && mine < next;
-    const unsigned there = __ballot_sync(0xffffffffu, has);
-    if (lane == 0 && r < kMostPairs / 32) s_counts[r] = __popc(there);
-    __syncthreads();
-    int before = 0, count = 0;
-#pragma unroll
-    for (int w = 0; w < kMostPairs / 32; ++w) {
-        before += w < r ? s_counts[w] : 0;
-        count += s_counts[w];
-    }
-    if (has) s_slots[before + __popc(there & ((1u << lane) - 1u))] = 2 * q + (mine < begin);
-    __syncthreads();
-    const int row = row0 + r, in_tile = weight ? row & 127 : row;
-    if (in_tile >= limit) return;
-    // a warp: a row of up to 256 columns
-    const int j0 = 4 * lane, c0 = l.n * nt + j0;
-    const bool live[2] = {j0 < l.n && c0 < p.C, j0 + 128 < l.n && c0 + 128 < p.C};
-    const float* src = p.share + (size_t)row * l.n + j0;
+    const int own = weight ? tile - l.tiles_x : tile, mt = own / l.tiles_n, nt = own - mt * l.tiles_n;
+    const int row = e / l.n, c0 = l.n * nt + e - row * l.n, in_tile = weight ? row & 127 : row;
+    if (in_tile >= (weight ? p.F - 128 * mt : p.M - 256 * mt) || c0 >= p.C) return;
+    const float* src = p.share + e;
     const size_t slot_size = (size_t)256 * l.n;
-    float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-    for (int k = 0; k < count; k += 8) {                 // eight shares in flight
-        float4 w[8][2];
+    const int last = p.first[which + 1];
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = p.first[which]; k < last; k += kShares) {
+        float4 w[kShares];
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
+        for (int u = 0; u < kShares; ++u) w[u] = k + u < last ? *reinterpret_cast<const float4*>(src + p.slot[k + u] * slot_size) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                w[u][h] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (live[h] && k + u < count) w[u][h] = *reinterpret_cast<const float4*>(src + s_slots[k + u] * slot_size + 128 * h);
-            }
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) { v[h].x += w[u][h].x; v[h].y += w[u][h].y; v[h].z += w[u][h].z; v[h].w += w[u][h].w; }
+        for (int u = 0; u < kShares; ++u) { v.x += w[u].x; v.y += w[u].y; v.z += w[u].z; v.w += w[u].w; }
     }
     T* out = static_cast<T*>(!weight ? p.dx : row < 128 ? p.dwg : p.dwu) + (size_t)(weight ? 128 * mt + in_tile : 256 * mt + row) * p.C + c0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-        if (live[h]) {
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out + 128 * h) = v[h];
-            else *reinterpret_cast<uint2*>(out + 128 * h) = make_uint2(pack2<T>(v[h].x, v[h].y), pack2<T>(v[h].z, v[h].w));
-        }
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out) = v;
+    else *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(v.x, v.y), pack2<T>(v.z, v.w));
 }
 
 // Tiles of at most 256 columns; at least six chunks a pair
@@ -1142,10 +1138,8 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     a.line.dx = c.dx != nullptr;
     a.line.dw = c.dwg != nullptr;
     f.line = a.line;
-    for (int q = 0; q <= a.line.pairs; ++q) f.begin[q] = a.line.begin(q);
     float* share = reinterpret_cast<float*>(ws + w.share);
     f.share = share;
-    int shared_tiles = 0;
     if (c.dx || c.dwg) {
         const GatedLine& l = a.line;
         const int unit = kWide ? 4 : 2;
@@ -1157,11 +1151,11 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
             !make_box_map(&a.share, share, 4, 2 * l.pairs, 256, l.n)) return cudaErrorInvalidValue;
         if ((e = launch_mode<T, kProducts, 128>(a, 2 * l.pairs, st)) != cudaSuccess) return e;
         ++*launches;
-        shared_tiles = l.tiles_x - l.whole + l.tiles_w;
+        list_shares(&f);
     }
-    const long long blocks = f.column_blocks + 32ll * shared_tiles;
+    const int blocks = f.column_blocks + f.tiles * (a.line.n / 4);
     if (!blocks) return cudaSuccess;                       // (no biases, every tile a pair's own)
-    if ((e = launch_dependent(gated_finish_kernel<T>, dim3((unsigned)blocks), 256, 0, st, f)) != cudaSuccess) return e;
+    if ((e = launch_dependent(gated_finish_kernel<T>, dim3(blocks), 256, 0, st, f)) != cudaSuccess) return e;
     ++*launches;
     return cudaSuccess;
 }
