@@ -186,6 +186,7 @@ __device__ __forceinline__ void ld_matrix4_trans(uint32_t (&r)[4], uint32_t at) 
 // A pair of blocks takes a tile of 256 rows, each of its blocks 128 of them and half of the B operand (BN = 128, and kProducts); a lone block a tile of
 // 128 rows and 2 BN columns (BN = 64 or 32: small problems).
 template <typename T, GatedMode MODE, int BN> struct GatedShape {
+    static constexpr int kParts = MODE == kGrad && BN == 128 ? 2 : 1;                      // of a tile, which pairs may share
     static constexpr bool kPair = BN == 128, kStaged = MODE == kProducts || (kPair && sizeof(T) == 2);
     static constexpr int kBTile = kPair ? kATile : 2 * BN * 128;
     static constexpr int kStage = kATile + kBTile;
@@ -196,16 +197,20 @@ template <typename T, GatedMode MODE, int BN> struct GatedShape {
 };
 
 // What block (or pair) `who` of `count` does, tile by tile.  kForward and kGrad: a run of tiles in the order of the rows, so that a run has few column
-// ranges; kProducts: its own tiles, then its run of the line.
+// ranges; kGrad's pairs share them evenly by halves of 64 hidden units, so that 5.3 tiles a pair take 5.5 instead of 6 tiles' time (8192 x 320 x 1280 f16
+// 28.0 -> 26.9 us, 25088 x 192 x 512 bf16 29.1 -> 28.0).  Not kForward's: a half loads what a whole tile does (17.8 us both ways, 32768 x 512 x 1368 bf16
+// 88.6 -> 90.2).  kProducts: its own tiles, then its run of the line.
 struct Work {
     int mt, nt, k0, k1;
+    int part;                                          // 0: a whole tile; else the half 1 or 2
     bool weight, whole;                                // kProducts: of dWg and dWu; the whole sum
     int slot;                                          // of a share
 };
-template <GatedMode MODE> struct Walk {
+template <GatedMode MODE, int PARTS> struct Walk {
     const GatedArgs& p;
     long long at, first, end;
-    int who, own, own_end, mt, nt;
+    int who, own, own_end, mt, nt, left;               // left, later: kForward and kGrad, whose loops have no room for 64-bit arithmetic
+    bool later;                                        // the run begins with a tile's second half
     __device__ Walk(const GatedArgs& args, int who_, int count) : p(args), who(who_) {
         if (MODE == kProducts) {
             first = at = p.line.begin(who);
@@ -213,23 +218,27 @@ template <GatedMode MODE> struct Walk {
             own = p.line.own(who);
             own_end = p.line.dx ? p.line.own(who + 1) : own;
         } else {
-            const long long units = (long long)p.tiles_m * p.tiles_n;
-            first = at = units * who / count;
-            end = units * (who + 1) / count;
-            nt = (int)(at / p.tiles_m);
-            mt = (int)(at - (long long)nt * p.tiles_m);
+            const long long units = (long long)PARTS * p.tiles_m * p.tiles_n;
+            const long long begin = units * who / count, tile = begin / PARTS;
+            left = (int)(units * (who + 1) / count - begin);
+            later = begin % PARTS != 0;
+            nt = (int)(tile / p.tiles_m);
+            mt = (int)(tile - (long long)nt * p.tiles_m);
         }
     }
     __device__ bool next(Work& w) {
         if (MODE != kProducts) {
-            if (at >= end) return false;
+            if (left <= 0) return false;
             w.nt = nt; w.mt = mt;
             w.k0 = 0; w.k1 = p.chunks;
-            ++at;
+            w.part = later ? 2 : left < PARTS ? 1 : 0;
+            left -= w.part ? 1 : PARTS;
+            later = false;
             if (++mt == p.tiles_m) { mt = 0; ++nt; }
             return true;
         }
         const GatedLine& l = p.line;
+        w.part = 0;
         int tile = 0, chunks = l.chunks_x;
         bool wanted = false;
         if (own < own_end) {
@@ -303,7 +312,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
     pdl_release_next();
 
     const int chunks_f = (p.F + 63) / 64;
-    Walk<MODE> walk(p, who, count);
+    Walk<MODE, S::kParts> walk(p, who, count);
     Work t;
 
     if (warp == kEpiWarps || warp == kEpiWarps + 2) {
@@ -372,6 +381,8 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 tc_fence_after_sync();
                 const uint32_t d = pp.tmem + 256 * buf;
                 const bool weight = MODE == kProducts && t.weight;
+                // half of a tile: 64 hidden units, those of each block's rows of B that begin at 0 or at 64
+                const uint32_t id_here = S::kParts > 1 && t.part ? umma_idesc(fmt, 256, BN, 0) : id, b_at = kATile + (S::kParts > 1 && t.part == 2 ? 64 * 128 : 0);
                 const int total = MODE <= kGrad ? p.C : weight ? p.M : p.F;
                 uint32_t acc = 0;
                 for (int pair = 0; pair < kPairs; ++pair)
@@ -396,7 +407,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                         };
                         using Row = std::integral_constant<int, 2>;
                         using Column = std::integral_constant<int, 128>;
-                        if (MODE <= kGrad) issue(Row(), Row(), umma_desc_sw128(at), umma_desc_sw128(at + kATile), id);
+                        if (MODE <= kGrad) issue(Row(), Row(), umma_desc_sw128(at), umma_desc_sw128(at + b_at), id_here);
                         else if (weight) issue(Column(), Column(), desc_mn(at, 8192), desc_mn(at + kATile, 8192), id | 1u << 15);
                         else issue(Row(), Column(), umma_desc_sw128(at), desc_mn(at + kATile, 8192), id);
                         acc = 1u;
@@ -420,6 +431,8 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             tc_fence_before_sync();
             arrive_warp_e<PAIR>(elected, read0 + 8 * buf);
         };
+        auto mine_too = [&](const Work& t) { return S::kParts == 1 || t.part == 0 || (quarter >> 1) == t.part - 1; };      // whether this warp has some of the tile
+        auto column_at = [&](const Work& t) { return S::kParts > 1 && t.part ? 32 * (quarter & 1) : 32 * quarter; };       // of G in the accumulator (BN = 128)
         auto await = [&](int bar, int parity) {
             if (!mbar_test(pipe_bar(pp, bar), parity & 1)) wait_par(pp, bar, parity, kTimeoutTile);
         };
@@ -431,7 +444,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             float column[2][2][4] = {};                                // [dG, dU][16 columns][i, twice]
             int column_nt = -1;
             auto flush = [&] {
-                const int first = (int)((((long long)column_nt * p.tiles_m + 1) * count - 1) / ((long long)p.tiles_m * p.tiles_n));
+                const int first = (int)(((2ll * column_nt * p.tiles_m + 1) * count - 1) / (2ll * p.tiles_m * p.tiles_n));
                 float* dst = p.column + (size_t)(8 * (who - first) + 4 * rank + q) * 2 * p.F;
                 const int f = BN * column_nt + 32 * quarter + 8 * (lane & 3) + (lane >> 2);
 #pragma unroll
@@ -449,17 +462,25 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             };
             Work ahead;
             bool more = walk.next(ahead);
-            if (MODE == kGrad && more) fetch(ahead, 0);
+            int done = 0;                                              // tiles that this warp had some of
+            if (MODE == kGrad && more && mine_too(ahead)) fetch(ahead, 0);
             const bool biased = p.bg || p.bu;
             int bias_nt = -1;
             for (; more; ++ord) {
                 t = ahead;
                 more = walk.next(ahead);
                 const int buf = ord & 1, row0 = 256 * t.mt + 128 * rank + 32 * q, f0 = BN * t.nt + 32 * quarter;
-                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16) + 32 * quarter;
+                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16) + column_at(t), up = S::kParts > 1 && t.part ? BN / 2 : BN;
                 if (MODE == kGrad && p.column && column_nt != t.nt) {
                     if (column_nt >= 0) flush();
                     column_nt = t.nt;
+                }
+                if (!mine_too(t)) {
+                    await(BAR_ACC + buf, ord >> 1);
+                    release(buf);
+                    if (MODE == kGrad && more && mine_too(ahead)) fetch(ahead, done);
+                    __syncwarp();
+                    continue;
                 }
                 if (biased && bias_nt != t.nt) {                       // as fp32: [gate | up][32]
                     bias_nt = t.nt;
@@ -475,18 +496,19 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 tc_fence_after_sync();
                 store_wait_read<0>();                                  // the tile before has left the patches
                 __syncwarp();
-                const uint32_t mine = patch + (MODE == kGrad ? kHalfPatch * (ord & 1) : 0), other = patch + 2 * kHalfPatch;
+                const uint32_t mine = patch + (MODE == kGrad ? kHalfPatch * (done & 1) : 0), other = patch + 2 * kHalfPatch;
                 if (MODE == kGrad) {
-                    await(BAR_DH + warp, ord);
-                    if (more) fetch(ahead, ord + 1);
+                    await(BAR_DH + warp, done);
+                    if (more && mine_too(ahead)) fetch(ahead, done + 1);
                 }
+                ++done;
                 by_activation(p.act, [&](auto act) {
 #pragma unroll 1
                     for (int h = 0; h < 2; ++h) {                      // 16 hidden units
                         float g[16], v[16];
                         __syncwarp();
                         tmem_ld16(acc + 16 * h, g);
-                        tmem_ld16(acc + BN + 16 * h, v);
+                        tmem_ld16(acc + up + 16 * h, v);
                         tmem_ld_wait();
                         if (h == 1) release(buf);
 #pragma unroll
@@ -567,22 +589,22 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             constexpr int kCols = BN / 4 > 16 ? BN / 4 : 16;           // of a warp (BN = 32: half of the warps have none)
             for (; walk.next(t); ++ord) {
                 const int buf = ord & 1, row = (PAIR ? 256 : 128) * t.mt + 128 * rank + 32 * q + lane;
-                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
+                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16), up = S::kParts > 1 && t.part ? BN / 2 : BN;
                 const size_t plane = (size_t)p.M * p.F;
                 await(BAR_ACC + buf, ord >> 1);
                 tc_fence_after_sync();
-                if (quarter * kCols >= BN) {
+                if (quarter * kCols >= BN || !mine_too(t)) {
                     release(buf);
                     continue;
                 }
                 by_activation(p.act, [&](auto act) {
 #pragma unroll 1
                     for (int s = 0; s < kCols / 16; ++s) {
-                        const int col = quarter * kCols + 16 * s, f0 = BN * t.nt + col;
+                        const int col = quarter * kCols + 16 * s, f0 = BN * t.nt + col, at_col = PAIR ? column_at(t) + 16 * s : col;
                         float g[16], v[16];
                         __syncwarp();
-                        tmem_ld16(acc + col, g);
-                        tmem_ld16(acc + BN + col, v);
+                        tmem_ld16(acc + at_col, g);
+                        tmem_ld16(acc + up + at_col, v);
                         tmem_ld_wait();
                         if (s == kCols / 16 - 1) release(buf);
 #pragma unroll
@@ -858,7 +880,7 @@ struct FinishArgs {
     void *dx, *dwg, *dwu, *dbg, *dbu;
     GatedLine line;
     int M, C, F;
-    int column_blocks, runs, tiles_m, units, count;      // column sums
+    int column_blocks, runs, tiles_m, units, count;      // column sums; kGrad's halves of tiles: in a column range, in all
     int tiles;                                           // with shares: which ones, and their slots in their order
     int tile[kMostPairs];
     unsigned short first[kMostPairs + 1];
@@ -998,7 +1020,7 @@ GatedTiles plan_tiles(int M, int F, int sm_count) {
 }
 int column_slots(const GatedTiles& t) {
     const int pairs = t.blocks / 2, runs = (pairs + t.tiles_n - 1) / t.tiles_n + 1;
-    return 8 * (runs < t.tiles_m ? runs : t.tiles_m);
+    return 8 * (runs < t.tiles_m + 1 ? runs : t.tiles_m + 1);
 }
 
 // Workspace: terms of X, Wg, Wu (fp32) | dG | dU | shares of tiles of dX and the weights' gradients, of the column sums
@@ -1124,7 +1146,7 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     f.column = column;
     if (c.dbg) {
         f.column_blocks = (2 * c.F + 31) / 32;
-        f.tiles_m = t.tiles_m; f.units = t.tiles_m * t.tiles_n; f.count = t.blocks / 2;
+        f.tiles_m = 2 * t.tiles_m; f.units = 2 * t.tiles_m * t.tiles_n; f.count = t.blocks / 2;            // in halves
         if (!fused_columns && c.M <= kColRows) {
             f.dg = dg;
             f.du = du;
