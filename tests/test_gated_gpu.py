@@ -213,3 +213,21 @@ def test_refusals():
     assert lib.agent_attn_gated(mod._h, None, x.data_ptr(), None, 0, None) == 1
     assert lib.agent_attn_gated_workspace_bytes(mod._h, 16, 60, 128, 0) == 0 and lib.agent_attn_gated_workspace_bytes(mod._h, 16, 64, 128, 0) == 0
     assert lib.agent_attn_gated_workspace_bytes(mod._h, 16, 64, 128, 1) > 0
+
+
+@pytest.mark.parametrize("name", ["gelu", "silu"])
+@pytest.mark.parametrize("dtype,M,C,F", [("f32", 12000, 64, 264), ("f16", 9000, 72, 648), ("bf16", 5200, 520, 1032), ("bf16", 9473, 136, 320)])
+def test_tiles_that_pairs_of_blocks_share(dtype, M, C, F, name):
+    """More tiles than pairs of blocks and no multiple of them: runs that begin or end with half of a tile, with a tile whose second half lies past the
+    hidden units, and gradients whose shares come from many pairs."""
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, "gu", seed=M)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    h, grads = reference(x, wg, wu, dh, bg, bu, name)
+    args = dict(b_gate=bg, b_up=bu, activation=name)
+    check_forward(mod.gated(x, wg, wu, **args), h, dtype)
+    back = mod.gated_backward(x, wg, wu, dh, **args)
+    assert mod.query_status() == 0
+    for n, t in back.items():
+        assert torch.isfinite(t).all() and rel(t, grads[n]) <= REL_BWD[dtype], (n, rel(t, grads[n]))
+    again = mod.gated_backward(x, wg, wu, dh, need_input_grad=False, **args)
+    assert all(torch.equal(again[n], back[n]) for n in again)
