@@ -50,6 +50,7 @@ struct GatedArgs {
     GatedLine line;
     const void *bg, *bu, *dh;
     void *out0, *out1;                                 // H; dG and dU: where they are written without staging
+    int terms;                                         // kGrad, kProducts of 16-bit elements: of dG and dU (1 or 2)
     float* column;                                     // [slots][2][F]: shares of the column sums of dG and dU, or null
     int* status;
     alignas(64) CUtensorMap a[2], b[2], x;             // operands; kProducts: a, b of dX (a of the weights, too), x: X
@@ -155,11 +156,17 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float* 
 #pragma unroll
     for (int i = 0; i < 8; i += V) *reinterpret_cast<uint4*>(p + i) = pack16<T>(f + i);
 }
-// eight values as operands of a later product: rounded to the element type, or (fp32) as three planes of terms
-template <typename T> __device__ __forceinline__ void store_operand8(void* base, size_t plane, size_t at, const float* f) {
+// eight values as operands of a later product: rounded to the element type (and what that leaves in a second plane), or (fp32) as three planes of terms
+template <typename T> __device__ __forceinline__ void store_operand8(void* base, size_t plane, size_t at, const float* f, bool second = false) {
     using E = typename GatedTerms<T>::E;
     if constexpr (GatedTerms<T>::kTerms == 1) {
         store8<T>(static_cast<T*>(base) + at, f);
+        if (second) {
+            float rest[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rest[i] = f[i] - Elem<T>::to_f32(Elem<T>::from_f32(f[i]));
+            store8<T>(static_cast<T*>(base) + plane + at, rest);
+        }
     } else {
         uint32_t o[3][4];
 #pragma unroll
@@ -174,13 +181,39 @@ template <typename T> __device__ __forceinline__ void store_operand8(void* base,
     }
 }
 __device__ __forceinline__ void st_shared4(uint32_t at, uint4 v) { asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); }
-__device__ __forceinline__ uint4 ld_shared4(uint32_t at) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+// 16 rows of 64 bytes each: 8 x 8 values a register, in the layout of tmem_ld_16x256b
+__device__ __forceinline__ void ld_matrix4(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void st_matrix4(uint32_t at, const uint32_t (&r)[4]) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};\n" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+// 16 rows of 32 columns of an accumulator: r[4 j + 2 h + e] is row lane / 4 + 8 h, column 8 j + 2 (lane % 4) + e
+__device__ __forceinline__ void tmem_ld_16x256b_x4(uint32_t taddr, float (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]),
+                   "=f"(r[14]), "=f"(r[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ float2 ld_shared_pair(uint32_t at) {
+    float2 v;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];\n" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
     return v;
 }
-__device__ __forceinline__ void ld_matrix4_trans(uint32_t (&r)[4], uint32_t at) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+// Sum over the lanes of 16 values each: lane l gets that of value l / 2
+__device__ __forceinline__ float sum_lanes16(const float (&x)[16], int lane) {
+    float y[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = x[i];
+#pragma unroll
+    for (int n = 8; n; n >>= 1) {
+        const bool upper = lane & 2 * n;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float other = __shfl_xor_sync(0xffffffffu, upper ? y[i] : y[i + n], 2 * n);
+            y[i] = (upper ? y[i + n] : y[i]) + other;
+        }
+    }
+    return y[0] + __shfl_xor_sync(0xffffffffu, y[0], 1);
 }
 
 // A pair of blocks takes a tile of 256 rows, each of its blocks 128 of them and half of the B operand (BN = 128, and kProducts); a lone block a tile of
@@ -312,6 +345,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
     pdl_release_next();
 
     const int chunks_f = (p.F + 63) / 64;
+    const int pairs = MODE == kProducts && kPairs == 1 ? p.terms : kPairs;
     Walk<MODE, S::kParts> walk(p, who, count);
     Work t;
 
@@ -324,8 +358,8 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
         const uint32_t full0 = PAIR ? in_block(pipe_bar(pp, BAR_FULL), 0) : pipe_bar(pp, BAR_FULL), elected = elect_lane();
         bool alive = true;
         while (alive && walk.next(t)) {
-            for (int pair = 0; pair < kPairs; ++pair) {
-                int ta = 0, tb = 0;
+            for (int pair = 0; pair < pairs; ++pair) {
+                int ta = pairs - 1 - pair, tb = 0;
                 if (kPairs > 1) term_pair(pair, ta, tb);
                 for (int k = t.k0; k < t.k1 && alive; ++k) {
                     if (round > 0 && !mbar_test(pipe_bar(pp, BAR_EMPTY + stage), (round - 1) & 1u)) {
@@ -385,7 +419,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 const uint32_t id_here = S::kParts > 1 && t.part ? umma_idesc(fmt, 256, BN, 0) : id, b_at = kATile + (S::kParts > 1 && t.part == 2 ? 64 * 128 : 0);
                 const int total = MODE <= kGrad ? p.C : weight ? p.M : p.F;
                 uint32_t acc = 0;
-                for (int pair = 0; pair < kPairs; ++pair)
+                for (int pair = 0; pair < pairs; ++pair)
                     for (int k = t.k0; k < t.k1 && alive; ++k) {
                         if (!there) {
                             wait_spin(pp, BAR_FULL + stage, round, kTimeoutTile);
@@ -439,20 +473,21 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
         if constexpr (MODE <= kGrad && S::kStaged) {
             // Results leave through a patch of 32 rows of 64 bytes with their swizzle.  kGrad: dU has one patch, dG two in turn, in which dH arrives a
             // tile ahead and is overwritten.
-            const uint32_t bias = base + S::kOffBias + warp * 256, row_at = 64 * lane, swz = (lane >> 1) & 3;
-            // dG, dU: sums of the columns over this run's rows, as products of their transpose with ones: a lane has those of columns lane / 4 + 8 i
-            float column[2][2][4] = {};                                // [dG, dU][16 columns][i, twice]
+            const uint32_t bias = base + S::kOffBias + warp * 256;
+            const uint32_t matrix = 64 * (lane & 15), piece = lane >> 4, swz = (lane >> 1) & 3;      // this lane's row of four 8 x 8 values
+            float2 column[2][4] = {};                                  // dG, dU: sums over this run's rows lane / 4 + 8 i, of columns 8 j + 2 (lane % 4) and the next
             int column_nt = -1;
             auto flush = [&] {
                 const int first = (int)(((2ll * column_nt * p.tiles_m + 1) * count - 1) / (2ll * p.tiles_m * p.tiles_n));
                 float* dst = p.column + (size_t)(8 * (who - first) + 4 * rank + q) * 2 * p.F;
-                const int f = BN * column_nt + 32 * quarter + 8 * (lane & 3) + (lane >> 2);
 #pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                    const float lo = lane & 1 ? column[o][0][2] : column[o][0][0], hi = lane & 1 ? column[o][1][2] : column[o][1][0];
-                    if (f < p.F) dst[(size_t)o * p.F + f] = lane & 2 ? hi : lo;
+                for (int k = 0; k < 8; ++k) {
+                    float2 v = column[k >> 2][k & 3];
+                    column[k >> 2][k & 3] = both(0.f);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) column[o][i / 4][i % 4] = 0.f;
+                    for (int o = 4; o < 32; o *= 2) v = fadd2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+                    const int f = BN * column_nt + 32 * quarter + 8 * (k & 3) + 2 * (lane & 3);
+                    if (lane >> 2 == k && f < p.F) *reinterpret_cast<float2*>(dst + (size_t)(k >> 2) * p.F + f) = v;
                 }
             };
             auto fetch = [&](const Work& t, int i) {                   // dH of tile i
@@ -504,16 +539,17 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                 ++done;
                 by_activation(p.act, [&](auto act) {
 #pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {                      // 16 hidden units
+                    for (int h = 0; h < 2; ++h) {                      // 16 rows
                         float g[16], v[16];
                         __syncwarp();
-                        tmem_ld16(acc + 16 * h, g);
-                        tmem_ld16(acc + up + 16 * h, v);
+                        tmem_ld_16x256b_x4(acc + ((uint32_t)(16 * h) << 16), g);
+                        tmem_ld_16x256b_x4(acc + ((uint32_t)(16 * h) << 16) + up, v);
                         tmem_ld_wait();
                         if (h == 1) release(buf);
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {                  // pieces of eight
-                            float2 gg[4], vv[4];
+                        for (int c = 0; c < 2; ++c) {                  // 16 hidden units
+                            const uint32_t at = mine + matrix + 1024 * h + (((2 * c + piece) ^ swz) << 4);
+                            float2 gg[4], vv[4];                       // [2 j + i]: hidden units 8 j + 2 (lane % 4), row lane / 4 + 8 i
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 gg[i] = make_float2(g[8 * c + 2 * i], g[8 * c + 2 * i + 1]);
@@ -521,18 +557,17 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                             }
                             if (biased) {
 #pragma unroll
-                                for (int i = 0; i < 2; ++i) {
-                                    const uint32_t at = bias + 64 * h + 32 * c + 16 * i;
-                                    const uint4 x = ld_shared4(at), y = ld_shared4(at + 128);
-                                    gg[2 * i] = fadd2(gg[2 * i], make_float2(__uint_as_float(x.x), __uint_as_float(x.y)));
-                                    gg[2 * i + 1] = fadd2(gg[2 * i + 1], make_float2(__uint_as_float(x.z), __uint_as_float(x.w)));
-                                    vv[2 * i] = fadd2(vv[2 * i], make_float2(__uint_as_float(y.x), __uint_as_float(y.y)));
-                                    vv[2 * i + 1] = fadd2(vv[2 * i + 1], make_float2(__uint_as_float(y.z), __uint_as_float(y.w)));
+                                for (int j = 0; j < 2; ++j) {
+                                    const uint32_t b = bias + 64 * c + 32 * j + 8 * (lane & 3);
+                                    const float2 x = ld_shared_pair(b), y = ld_shared_pair(b + 128);
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) {
+                                        gg[2 * j + i] = fadd2(gg[2 * j + i], x);
+                                        vv[2 * j + i] = fadd2(vv[2 * j + i], y);
+                                    }
                                 }
                             }
-                            const uint32_t at = mine + row_at + (((2 * h + c) ^ swz) << 4);
                             uint32_t o0[4];
-                            [[maybe_unused]] uint32_t o1[4];
                             if constexpr (MODE == kForward) {
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
@@ -542,21 +577,24 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                                     o0[i] = pack2<T>(a.x, a.y);
                                 }
                             } else {
-                                const uint4 d = ld_shared4(at);
-                                const uint32_t dd[4] = {d.x, d.y, d.z, d.w};
+                                uint32_t d[4], o1[4];
+                                ld_matrix4(d, at);
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
                                     float2 a, da;
                                     activate<T, decltype(act)::value, true>(gg[i], a, da);
-                                    const float2 dh = unpack2<T>(dd[i]);
+                                    const float2 dh = unpack2<T>(d[i]);
                                     da = fmul2(fmul2(dh, vv[i]), da);
                                     a = fmul2(dh, a);
                                     o0[i] = pack2<T>(da.x, da.y);
                                     o1[i] = pack2<T>(a.x, a.y);
+                                    column[0][2 * c + i / 2] = fadd2(column[0][2 * c + i / 2], da);      // (before they are rounded)
+                                    column[1][2 * c + i / 2] = fadd2(column[1][2 * c + i / 2], a);
                                 }
-                                st_shared4(at - mine + other, make_uint4(o1[0], o1[1], o1[2], o1[3]));
+                                __syncwarp();
+                                st_matrix4(at - mine + other, o1);
                             }
-                            st_shared4(at, make_uint4(o0[0], o0[1], o0[2], o0[3]));
+                            st_matrix4(at, o0);
                         }
                     }
                 });
@@ -567,20 +605,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     if (MODE == kGrad) tma_store_3d_e(elected, &p.s[1], f0, row0, 0, other);
                 }
                 store_commit();
-                if (MODE == kGrad && p.column) {
-                    constexpr uint32_t kOnes = Elem<T>::kIsBf16 ? 0x3f803f80u : 0x3c003c00u;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {                      // 16 rows (k / 2) of 16 columns (k % 2)
-                        const int row = 16 * (k >> 1) + (lane & 7) + 8 * (lane >> 4), piece = 2 * (k & 1) + ((lane >> 3) & 1);
-                        const uint32_t a = 64 * row + ((piece ^ ((row >> 1) & 3)) << 4);
-                        uint32_t m0[4], m1[4];
-                        ld_matrix4_trans(m0, mine + a);
-                        ld_matrix4_trans(m1, other + a);
-                        mma16816<T>(column[0][k & 1], m0, kOnes, kOnes);
-                        mma16816<T>(column[1][k & 1], m1, kOnes, kOnes);
-                    }
-                    __syncwarp();                                      // (every lane has read before the patch is handed to the next copy)
-                }
+                __syncwarp();
             }
             if (MODE == kGrad && p.column && column_nt >= 0) flush();
             store_wait_read<0>();
@@ -610,7 +635,11 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
 #pragma unroll
                         for (int j = 0; j < 16; j += 8) {
                             const int f = f0 + j;
-                            if (f >= p.F || row >= p.M) continue;
+                            if (f >= p.F || row >= p.M) {
+#pragma unroll
+                                for (int i = j; i < j + 8; ++i) g[i] = v[i] = 0.f;
+                                continue;
+                            }
                             if (p.bg) {
                                 float b[8];
                                 load8<T>(static_cast<const T*>(p.bg) + f, b);
@@ -640,8 +669,18 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                             if constexpr (MODE == kForward) {
                                 store8<T>(static_cast<T*>(p.out0) + at, v + j);
                             } else {
-                                store_operand8<T>(p.out0, plane, at, g + j);
-                                store_operand8<T>(p.out1, plane, at, v + j);
+                                store_operand8<T>(p.out0, plane, at, g + j, p.terms > 1);
+                                store_operand8<T>(p.out1, plane, at, v + j, p.terms > 1);
+                            }
+                        }
+                        if (MODE == kGrad && p.column) {               // sums of the warp's rows, a slot for every 32
+                            __syncwarp();
+                            const float sg = sum_lanes16(g, lane), su = sum_lanes16(v, lane);
+                            const int f = f0 + (lane >> 1);
+                            if (!(lane & 1) && f < p.F && row - lane < p.M) {
+                                float* dst = p.column + (size_t)(row >> 5) * 2 * p.F + f;
+                                dst[0] = sg;
+                                dst[p.F] = su;
                             }
                         }
                     }
@@ -840,43 +879,11 @@ __global__ void __launch_bounds__(256) split_terms_kernel(const __grid_constant_
     store_operand8<float>(p.dst[blockIdx.y], n, i, f);
 }
 
-// Column sums of dG and dU: a block takes 64 columns of one of them and a run of rows
-constexpr int kColRows = 512;
-template <typename T> __global__ void __launch_bounds__(256) gated_column_kernel(const void* dg, const void* du, int M, int F, float* part) {
-    using E = typename GatedTerms<T>::E;
-    __shared__ float s_sum[32][64];
-    pdl_wait_prior();
-    pdl_release_next();
-    const int c = threadIdx.x & 7, r = threadIdx.x >> 3, f = 64 * blockIdx.x + 8 * c;
-    const int r0 = kColRows * blockIdx.z, r1 = min(r0 + kColRows, M);
-    const E* src = static_cast<const E*>(blockIdx.y ? du : dg);
-    float sum[8] = {};
-    if (f < F)
-        for (int row = r0 + r; row < r1; row += 32)
-#pragma unroll
-            for (int t = 0; t < GatedTerms<T>::kTerms; ++t) {
-                float v[8];
-                load8<E>(src + ((size_t)t * M + row) * F + f, v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] += v[i];
-            }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s_sum[r][8 * c + i] = sum[i];
-    __syncthreads();
-    if (threadIdx.x < 64 && 64 * blockIdx.x + threadIdx.x < F) {
-        float v = 0.f;
-        for (int k = 0; k < 32; ++k) v += s_sum[k][threadIdx.x];
-        part[((size_t)blockIdx.z * 2 + blockIdx.y) * F + 64 * blockIdx.x + threadIdx.x] = v;
-    }
-}
-
 // What is left after kProducts, always in the same order.  The first blocks: sums of the columns of dG and dU (32 of the 2 F each) over the shares
-// that kGrad left (those of a column range are the pairs' that had it), over `runs` rows of gated_column_kernel, or over dG and dU themselves (few
-// rows: a launch less).  The others: 1024 values of a tile that no pair had whole, as the sum of its shares, whose list the host makes.
+// that kGrad left: one for every 32 rows (`runs`), or those of the pairs that had the column range.  The others: 1024 values of a tile that no pair had whole, as the sum of its shares, whose list the host makes.
 constexpr int kMostPairs = 128, kShares = 12;            // shares in flight
 struct FinishArgs {
     const float *share, *column;
-    const void *dg, *du;                                 // summed here where they have at most kColRows rows and no shares
     void *dx, *dwg, *dwu, *dbg, *dbu;
     GatedLine line;
     int M, C, F;
@@ -922,22 +929,7 @@ template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel
     if ((int)blockIdx.x < p.column_blocks) {
         const int i = 32 * blockIdx.x + lane, op = i >= p.F, f = i - op * p.F;
         float v = 0.f;
-        if (i < 2 * p.F && p.dg) {
-            using E = typename GatedTerms<T>::E;
-            constexpr int kTerms = GatedTerms<T>::kTerms, kBatch = 8 / kTerms;
-            const E* src = static_cast<const E*>(op ? p.du : p.dg) + f;
-            for (int m = r; m < p.M; m += 8 * kBatch) {
-                float w[kBatch][kTerms];
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u)
-#pragma unroll
-                    for (int t = 0; t < kTerms; ++t) w[u][t] = m + 8 * u < p.M ? Elem<E>::to_f32(src[((size_t)t * p.M + m + 8 * u) * p.F]) : 0.f;
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u)
-#pragma unroll
-                    for (int t = 0; t < kTerms; ++t) v += w[u][t];
-            }
-        } else if (i < 2 * p.F) {
+        if (i < 2 * p.F) {
             int slots = p.runs;
             if (!slots) {
                 const int nt = f / 128;
@@ -1023,6 +1015,11 @@ int column_slots(const GatedTiles& t) {
     return 8 * (runs < t.tiles_m + 1 ? runs : t.tiles_m + 1);
 }
 
+// 16-bit elements: dG and dU as one term, rounded to the element type, which makes the error of dX and the weights' gradients 1.4 times that of their own
+// rounding; over few rows it is more by chance (up to 2.1 times with one row, 1.6 with 32, 1.5 with 128), and there two terms keep it at 1.  (64 x 320 x 1280
+// bf16 17.7 and 19.3 us; 256 x 640 x 2560 25.6 and 30.4, which one term has.)
+int gradient_terms(const GatedTiles& t, int M) { return t.bn < 128 && M <= 128 ? 2 : 1; }
+
 // Workspace: terms of X, Wg, Wu (fp32) | dG | dU | shares of tiles of dX and the weights' gradients, of the column sums
 struct GatedWs { size_t x, wg, wu, dg, du, share, db, total; };
 GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count) {
@@ -1035,12 +1032,12 @@ GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count
     w.wu = take(terms * F * C * 2);
     w.dg = w.du = w.share = w.db = at;
     if (backward) {
-        const size_t planes = (dtype == kF32 ? 3 : 1) * (size_t)M * F * 2;
+        const GatedTiles t = plan_tiles(M, F, sm_count);
+        const size_t planes = (dtype == kF32 ? 3 : gradient_terms(t, M)) * (size_t)M * F * 2;
         w.dg = take(planes);
         w.du = take(planes);
-        const GatedTiles t = plan_tiles(M, F, sm_count);
         w.share = take((size_t)(sm_count / 2) * 2 * 256 * plan_line(M, C, F, sm_count).n * 4);
-        const size_t slots = dtype != kF32 && t.bn == 128 ? column_slots(t) : (M + kColRows - 1) / kColRows;
+        const size_t slots = dtype != kF32 && t.bn == 128 ? column_slots(t) : (M + 31) / 32;
         w.db = take(slots * 2 * F * 4);
     }
     w.total = at;
@@ -1125,9 +1122,9 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     a.tiles_m = t.tiles_m; a.tiles_n = t.tiles_n; a.chunks = (c.C + 63) / 64;
     a.out0 = c.dh ? ws + w.dg : static_cast<char*>(c.h);
     a.out1 = ws + w.du;
-    const bool fused_columns = c.dbg && !kWide && t.bn == 128;
+    a.terms = kWide ? kTerms : gradient_terms(t, c.M);
     float* column = reinterpret_cast<float*>(ws + w.db);
-    a.column = fused_columns ? column : nullptr;
+    a.column = c.dbg ? column : nullptr;
     if (!make_map_3d_u16(&a.a[0], x, kTerms, c.M, c.C, 128) || !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, t.bn) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, t.bn)) return cudaErrorInvalidValue;
     if (!kWide && t.bn == 128) {
         if (!make_box_map(&a.s[0], a.out0, 2, 1, c.M, c.F)) return cudaErrorInvalidValue;
@@ -1147,14 +1144,7 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     if (c.dbg) {
         f.column_blocks = (2 * c.F + 31) / 32;
         f.tiles_m = 2 * t.tiles_m; f.units = 2 * t.tiles_m * t.tiles_n; f.count = t.blocks / 2;            // in halves
-        if (!fused_columns && c.M <= kColRows) {
-            f.dg = dg;
-            f.du = du;
-        } else if (!fused_columns) {
-            f.runs = (c.M + kColRows - 1) / kColRows;
-            if ((e = launch_dependent(gated_column_kernel<T>, dim3((c.F + 63) / 64, 2, f.runs), 256, 0, st, dg, du, c.M, c.F, column)) != cudaSuccess) return e;
-            ++*launches;
-        }
+        if (kWide || t.bn < 128) f.runs = (c.M + 31) / 32;
     }
     a.line = plan_line(c.M, c.C, c.F, c.sm_count);
     a.line.dx = c.dx != nullptr;
@@ -1165,8 +1155,8 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     if (c.dx || c.dwg) {
         const GatedLine& l = a.line;
         const int unit = kWide ? 4 : 2;
-        if (!make_map_3d_u16(&a.a[0], dg, kTerms, c.M, c.F, 128) || !make_map_3d_u16(&a.a[1], du, kTerms, c.M, c.F, 128) ||
-            !make_map_3d_u16(&a.w[0], dg, kTerms, c.M, c.F, 64) || !make_map_3d_u16(&a.w[1], du, kTerms, c.M, c.F, 64) ||
+        if (!make_map_3d_u16(&a.a[0], dg, a.terms, c.M, c.F, 128) || !make_map_3d_u16(&a.a[1], du, a.terms, c.M, c.F, 128) ||
+            !make_map_3d_u16(&a.w[0], dg, a.terms, c.M, c.F, 64) || !make_map_3d_u16(&a.w[1], du, a.terms, c.M, c.F, 64) ||
             !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, 64) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, 64) || !make_map_3d_u16(&a.x, x, kTerms, c.M, c.C, 64) ||
             (c.dx && !make_box_map(&a.s[0], c.dx, unit, 1, c.M, c.C)) ||
             (c.dwg && (!make_box_map(&a.s[1], c.dwg, unit, 1, c.F, c.C) || !make_box_map(&a.s[2], c.dwu, unit, 1, c.F, c.C))) ||

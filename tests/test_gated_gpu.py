@@ -231,3 +231,44 @@ def test_tiles_that_pairs_of_blocks_share(dtype, M, C, F, name):
         assert torch.isfinite(t).all() and rel(t, grads[n]) <= REL_BWD[dtype], (n, rel(t, grads[n]))
     again = mod.gated_backward(x, wg, wu, dh, need_input_grad=False, **args)
     assert all(torch.equal(again[n], back[n]) for n in again)
+
+
+def hidden_errors(x, wg, wu, dh, bg, bu, name, step, tiny):
+    """What an element of dG and dU may be off by: `step` of itself (how it is held, the order of the sum), 4e-6 of dH U for the derivative and its
+    argument and of dH act' for U (sums of fp32 numbers around 1), 2e-6 of dH (1 + |G|) for the activation."""
+    g, u = x.double() @ wg.double().T + bg.double(), x.double() @ wu.double().T + bu.double()
+    g.requires_grad_()
+    a = act(name, g)
+    da, = torch.autograd.grad(a.sum(), g)
+    d, a = dh.double(), a.detach()
+    return (step * (d * u * da).abs() + 4e-6 * ((d * u).abs() + (d * da).abs()) + tiny, step * (d * a).abs() + 2e-6 * (d * (1 + g.detach().abs())).abs() + tiny)
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [(1, 32, 64), (1, 320, 1280), (7, 64, 176), (33, 96, 256), (128, 40, 72)])
+def test_gradients_of_few_rows_are_rounded_once(size, dtype, name):
+    """Element by element: one rounding of the result, and what the two terms of each summand leave (`hidden_errors`); in f16 half a step of its
+    smallest numbers for each second term."""
+    M, C, F = size
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, "gu", seed=M + F)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    _, grads = reference(x, wg, wu, dh, bg, bu, name)
+    back = mod.gated_backward(x, wg, wu, dh, b_gate=bg, b_up=bu, activation=name)
+    eg, eu = hidden_errors(x, wg, wu, dh, bg, bu, name, 2.0 ** -16 + 1e-5, 6e-8 if dtype == "f16" else 0.0)
+    xa = x.double().abs()
+    left = dict(dx=eg @ wg.double().abs() + eu @ wu.double().abs(), dw_gate=eg.T @ xa, dw_up=eu.T @ xa, db_gate=eg.sum(0), db_up=eu.sum(0))
+    for n, t in back.items():
+        bound = STEP[dtype] * grads[n].abs() + left[n] + (6e-8 if dtype == "f16" else 0.0)
+        assert ((t.double() - grads[n]).abs() <= bound).all(), (n, float(((t.double() - grads[n]).abs() / bound).max()))
+
+
+@pytest.mark.parametrize("dtype,M,C,F", [("bf16", 9473, 136, 320), ("f16", 700, 64, 256), ("f16", 8192, 64, 2560), ("bf16", 300, 64, 136)])
+def test_biases_are_summed_before_they_are_rounded(dtype, M, C, F):
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, "gu", seed=F)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    _, grads = reference(x, wg, wu, dh, bg, bu, "gelu")
+    back = mod.gated_backward(x, wg, wu, dh, b_gate=bg, b_up=bu, activation="gelu")
+    for n, e in zip(("db_gate", "db_up"), hidden_errors(x, wg, wu, dh, bg, bu, "gelu", 1e-5, 0.0)):
+        bound = STEP[dtype] * grads[n].abs() + e.sum(0) + (6e-8 if dtype == "f16" else 0.0)
+        assert ((back[n].double() - grads[n]).abs() <= bound).all()
