@@ -398,8 +398,8 @@ typedef struct {
     int activation;           /* aa_activation                                                     */
 } agent_attn_gate;
 
-/* Bytes of device workspace of agent_attn_gated (backward == 0; none for 16-bit types) or
- * agent_attn_gated_backward.  0 on invalid arguments, too. */
+/* Bytes of device workspace of agent_attn_gated (backward == 0; none for 16-bit types, and for fp32 up to 8 rows or
+ * 50 million products) or agent_attn_gated_backward.  0 on invalid arguments, too. */
 size_t agent_attn_gated_workspace_bytes(const agent_attn_handle* h, int rows, int channels, int hidden, int backward);
 
 /* out device [rows][hidden].  Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED (limits above), AA_ERR_WORKSPACE,
@@ -419,7 +419,8 @@ typedef struct {
 
 /* Gradients of agent_attn_gated for d_out = dL/dH (device [rows][hidden], element type).  Both projections are
  * recomputed; nothing has to be saved.  The gradients of the two projections are rounded to the element type, as
- * operands of the products that follow, which is why the results have that type and not fp32; sums are fp32, in a
+ * operands of the products that follow (up to 128 rows they keep what that leaves as a second term), which is why the
+ * results have that type and not fp32; the biases' gradients are sums of unrounded numbers.  Sums are fp32, in a
  * fixed order.  Errors as above. */
 int agent_attn_gated_backward(agent_attn_handle* h, const agent_attn_gate* gate, const void* d_out,
                               const agent_attn_gate_grads* grads, void* workspace, size_t workspace_bytes, void* stream);

@@ -7,13 +7,22 @@
 // memory that take turns, sixteen warps read the finished one and do the rest.  A pair of blocks (cta_group::2) has a tile of 256 rows.
 //   kForward   256 rows of 128 hidden units of G and U: one block of the pair holds a tile of Wg, the other one of Wu, so that one instruction of 256
 //              columns makes both; the epilogue applies biases, activation and product.  G and U never leave the chip.
-//   kGrad      the same product again; the epilogue reads dH, writes dG and dU for the third form and sums their columns.
+//   kGrad      the same product again; the epilogue reads dH, writes dG and dU for the third form and sums their columns before they are rounded.
 //   kProducts  dX: A = dG, then dU (along their rows), B = Wg, then Wu, read as [hidden][channels] = MN-major: nothing is transposed.  dWg and dWu:
 //              A = dG in one block of the pair, dU in the other, both MN-major, B = X MN-major.  Their sums are cut into chunks of 64, of which all pairs
 //              have as many: whole tiles of dX, then a run of the other tiles; a pair writes what it has whole and leaves its share of what it has
 //              not, and gated_finish_kernel adds the shares up in their order.
-// 16-bit operands enter as they are; dG and dU are rounded to the element type, as every operand of a product on the tensor cores is.  fp32: operands are sums of
-// three bf16 terms, six pairs of terms, small ones first.
+// 16-bit operands enter as they are; dG and dU are rounded to the element type, as every operand of a product on the tensor cores is (few rows: and what that
+// leaves as a second term).  fp32: operands are sums of three bf16 terms, six pairs of terms, small ones first.
+//
+// What bounds it (us of a launch among others; rows x channels x hidden units):
+//   kForward   32768 x 512 x 1368 bf16, SiLU: 88 to 92, 1.0 PFLOP/s.  Tensor pipe 75 % busy (a chunk of 64 takes 600 cycles of 512), clocks under the power
+//              limit; the two products alone take 85 in the vendor's library.  8192 x 320 x 1280 f16, GELU: 18, 0.74 PFLOP/s: the epilogue (4000 cycles a tile,
+//              products 2600), a first accumulator after 4.2 us, 1.1 us from the last store to the end.  The library's products alone: 19.
+//   kGrad      8192 x 320 x 1280 f16 27, 25088 x 192 x 512 bf16 28: the epilogue, 7000 cycles a tile at half of the issue slots, and the same start and end.
+//   kProducts  30 and 24: operands out of L2, 32 KB a block and chunk of 64 in 480 to 600 cycles (instructions for 160 or 192 columns take 320 or 384).
+//   finishing  5.8 and 6.1: 16 MB of shares out of L2, a start.
+// Tiles of 512 columns would halve what kProducts reads of A, and double the shares: 64.6 -> 69.8 us for 8192 x 320 x 1280.
 #include "bwd_terms.cuh"
 #include "pair.cuh"
 #include "stream_common.cuh"
@@ -475,7 +484,9 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             // tile ahead and is overwritten.
             const uint32_t bias = base + S::kOffBias + warp * 256;
             const uint32_t matrix = 64 * (lane & 15), piece = lane >> 4, swz = (lane >> 1) & 3;      // this lane's row of four 8 x 8 values
-            float2 column[2][4] = {};                                  // dG, dU: sums over this run's rows lane / 4 + 8 i, of columns 8 j + 2 (lane % 4) and the next
+            // An accumulator is read as 16 x 256 bits: a lane has rows lane / 4 and that plus 8, hidden units 8 j + 2 (lane % 4) and the next, so that it keeps
+            // sums of its columns over all of a run's rows in registers, and the eight lanes that share them meet when the columns change.
+            float2 column[2][4] = {};                                  // dG, dU
             int column_nt = -1;
             auto flush = [&] {
                 const int first = (int)(((2ll * column_nt * p.tiles_m + 1) * count - 1) / (2ll * p.tiles_m * p.tiles_n));
@@ -880,7 +891,8 @@ __global__ void __launch_bounds__(256) split_terms_kernel(const __grid_constant_
 }
 
 // What is left after kProducts, always in the same order.  The first blocks: sums of the columns of dG and dU (32 of the 2 F each) over the shares
-// that kGrad left: one for every 32 rows (`runs`), or those of the pairs that had the column range.  The others: 1024 values of a tile that no pair had whole, as the sum of its shares, whose list the host makes.
+// that kGrad left: one for every 32 rows (`runs`), or those of the pairs that had the column range.  The others: 1024 values of a tile that no pair
+// had whole, as the sum of its shares, whose list the host makes (found by the blocks themselves: 7.0 and 8.4 us instead of 5.8 and 6.1).
 constexpr int kMostPairs = 128, kShares = 12;            // shares in flight
 struct FinishArgs {
     const float *share, *column;
@@ -975,7 +987,8 @@ template <typename T> __global__ void __launch_bounds__(256) gated_finish_kernel
     else *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(v.x, v.y), pack2<T>(v.z, v.w));
 }
 
-// Tiles of at most 256 columns; at least six chunks a pair
+// Tiles of at most 256 columns; at least six chunks a pair, so that shares stay few: backward of 512 x 320 x 1280 bf16 with 3, 6 and 12 26.3, 22.7 and 24.2 us,
+// 1568 x 192 x 512 25.4, 21.5 and 22.1 (64 x 192 x 512 16.9, 19.3 and 20.3).
 GatedLine plan_line(int M, int C, int F, int sm_count) {
     GatedLine l;
     l.dx = l.dw = 1;
@@ -993,7 +1006,9 @@ GatedLine plan_line(int M, int C, int F, int sm_count) {
     return l;
 }
 
-// G and U: 128 hidden units a tile of 256 rows for a pair of blocks; where that leaves SMs without work, tiles of 128 rows and fewer units
+// G and U: 128 hidden units a tile of 256 rows for a pair of blocks; where that leaves half of the SMs without work, tiles of 128 rows and 64 units, or 32
+// where those still do.  Forward, bf16 (us with 128, 64, 32 units): 512 x 192 x 512 5.8, 4.4, 3.9; 768 x 320 x 1280 6.5, 5.0, 6.0; 1536 x 320 x 1280 7.2, 7.0, 9.2;
+// 512 x 1024 x 4096 10.7, 12.2, 18.8.  fp32: 256 x 320 x 1280 18.1, 14.1, 13.0; 768 18.7, 15.4, 20.3; 1024 20.0, 22.9, 27.5.
 struct GatedTiles { int bn, tiles_m, tiles_n, blocks; };
 GatedTiles plan_tiles(int M, int F, int sm_count) {
     GatedTiles t;
