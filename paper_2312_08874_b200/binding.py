@@ -237,6 +237,7 @@ class AgentAttention:
         self._ws: Optional[torch.Tensor] = None
         self._staging: Optional[torch.Tensor] = None
         self._bytes: dict = {}             # scratch sizes by call shape: they depend on nothing else
+        self._strides: dict = {}           # strides as the library takes them, by token count and strides
 
     def close(self):
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -523,13 +524,21 @@ class AgentAttention:
         for name, t in zip(names, tensors):
             if t is None:
                 continue
-            if t.stride(3) != 1:
-                raise ValueError(f"{name}: expected contiguous channels, got strides {t.stride()}")
-            st = tuple(s if n > 1 else self.head_dim for n, s in zip(shape, t.stride()[:3]))     # (of a single entry no stride is used)
-            if strides is not None and st != strides:
+            st = t.stride()
+            if st == strides:
+                continue
+            if st[3] != 1:
+                raise ValueError(f"{name}: expected contiguous channels, got strides {st}")
+            if strides is not None and any(n > 1 and s != o for n, s, o in zip(shape, st, strides)):       # (of a single entry no stride is used)
                 raise ValueError(f"{name}: expected the strides {strides} of the other tensor, got {st}")
-            strides = st
-        return (ctypes.c_longlong * 3)(*strides)
+            strides = st if strides is None else strides
+        key = (n_tokens, strides)
+        got = self._strides.get(key)
+        if got is None:
+            if len(self._strides) >= 64:
+                self._strides.clear()
+            got = self._strides[key] = (ctypes.c_longlong * 3)(*(s if n > 1 else self.head_dim for n, s in zip(shape, strides[:3])))
+        return got
 
     def _norm(self, q_gain, k_gain, eps):
         if eps is None:
