@@ -333,8 +333,8 @@ struct RotateArgs {
     int neighbours;           // pairs are neighbouring channels, else the halves of an axis's segment
     int norm, inverse;
     float eps;
-    // set by the launcher: lanes of a token (gradient: a power of two); slabs that share positions, runs of them, slabs of a run; 1 / d
-    int lanes, unit_slabs, chunks, share;
+    // set by the launcher: lanes of a token (gradient: a power of two); slabs that share positions; tiles; forward: runs of slabs, slabs of a run; 1 / d
+    int lanes, unit_slabs, tiles, chunks, share;
     float inv_d;
 };
 struct RotateBwdArgs {

@@ -18,7 +18,7 @@
 // Rows arrive by asynchronous copies, three ahead.  Bound by HBM, forward 4 bytes an element of 16 bits, backward 10, with the issue of instructions close
 // behind it (57 % to 73 % of the slots).  A pass among others, inputs that L2 does not hold, 64 channels: norm and rotation on a 256 x 256 grid, 16 slabs,
 // 537 MB in 100 us (5.4 TB/s); 64 slabs of 56 x 56, 103 MB in 23 us (4.4 TB/s, starts and angles 5 us of it); rotation of a video grid, 236 MB in 45 us
-// (5.2 TB/s); gradient on a 128 x 128 grid, 336 MB in 66 us (5.1 TB/s).
+// (5.2 TB/s); gradient on a 128 x 128 grid, 336 MB in 64 us (5.3 TB/s).
 #include "common.cuh"
 #include "kernels.h"
 
@@ -508,10 +508,32 @@ template <typename T, bool WORDS, bool NORM> __global__ void __launch_bounds__(k
     }
 }
 
-// Gradient through norm and rotation.  A block has one of the tensors (blockIdx.y) and loops over (tile of tokens, run of slabs); the gain's gradient
-// stays in registers until the block's end and leaves as one row of sums a block, which gain_sum_kernel adds up in a fixed order.  A lane has 16 bytes of
-// x; the gradient's row (fp32) is copied by the group's lanes in whole sectors and lies in shared memory as it is in memory, from where a lane reads
-// its channels and their partners.  Results change hands between two lanes so that they leave in whole sectors.
+// The gradient's work: a line of slabs, in which those of a tile of tokens (and of a batch entry, where positions differ) lie side by side.  A block has an
+// even part of it: runs of a few tiles, angles once for each.  Runs of one length, dealt out block by block, left the last round of them emptier: 384
+// slabs of 196 tokens took 27.5 us instead of 24.1, 16 of 128 x 128 66 instead of 63.6.  (Not the forward kernels': blocks that come and go keep to one region of
+// memory at a time; as a line the 256 x 256 grid takes 110 us instead of 100.)
+struct SlabLine {
+    long long at, end;
+    __device__ explicit SlabLine(const RotateArgs& p) {
+        const long long total = (long long)p.tiles * p.slabs;
+        at = total * blockIdx.x / gridDim.x;
+        end = total * (blockIdx.x + 1) / gridDim.x;
+    }
+    __device__ bool next(const RotateArgs& p, int& tile, SlabRun& r) {
+        if (at >= end) return false;
+        const long long column = at / p.unit_slabs;
+        const int first = (int)(at - column * p.unit_slabs), unit = (int)(column / p.tiles);
+        tile = (int)(column - (long long)unit * p.tiles);
+        r.begin = unit * p.unit_slabs + first;
+        r.end = r.begin + (int)min((long long)(p.unit_slabs - first), end - at);
+        at += r.end - r.begin;
+        return true;
+    }
+};
+// Gradient through norm and rotation.  A block has one of the tensors (blockIdx.y); the gain's gradient stays in registers until the block's end and
+// leaves as one row of sums a block, which gain_sum_kernel adds up in a fixed order.  A lane has 16 bytes of x; the gradient's row (fp32) is copied by
+// the group's lanes in whole sectors and lies in shared memory as it is in memory, from where a lane reads its channels and their partners.  Results
+// change hands between two lanes so that they leave in whole sectors.
 template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThreads, 3) rotate_backward_kernel(const __grid_constant__ RotateBwdArgs p) {
     constexpr int C = Elem<T>::kVec, kPieces = C / 4, kAhead = 3;            // 16-byte pieces of a lane's fp32 channels
     extern __shared__ __align__(16) unsigned char s_dyn[];                   // [kAhead][1 + kPieces][threads] uint4; at the end sums
@@ -521,7 +543,7 @@ template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThrea
     pdl_release_next();
     const RotateArgs& f = p.fwd;
     const int lane = threadIdx.x & 31, gl = lane & (f.lanes - 1), c0 = gl * C, first_lane = lane - gl;
-    const int groups = kRotThreads / f.lanes, tiles = (f.N + groups - 1) / groups, t = f.x[0] ? blockIdx.y : 1;
+    const int groups = kRotThreads / f.lanes, t = f.x[0] ? blockIdx.y : 1;
     LaneAngles<C, KIND> la;
     lane_angles<C, KIND>(f, c0, la);
     const int partner_lane = first_lane + la.partner[0] / C;
@@ -534,12 +556,16 @@ template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThrea
         gain[i] = gs && c0 < f.d ? make_float2(Elem<T>::to_f32(gs[c0 + 2 * i]), Elem<T>::to_f32(gs[c0 + 2 * i + 1])) : pair_of(1.f);
         sum[i] = pair_of(0.f);
     }
-    const int runs = f.chunks * (f.slabs / f.unit_slabs), row_at = kRotThreads + (threadIdx.x - gl) * kPieces;       // of the group's gradient row in a stage
-    for (long long item = blockIdx.x; item < (long long)tiles * runs; item += gridDim.x) {
-        const int run = (int)(item / tiles), tok = (int)(item - (long long)run * tiles) * groups + threadIdx.x / f.lanes;
+    const int row_at = kRotThreads + (threadIdx.x - gl) * kPieces;       // of the group's gradient row in a stage
+    SlabLine line(f);
+    SlabRun run;
+    int tile;
+#pragma unroll 1
+    while (line.next(f, tile, run)) {
+        const int tok = tile * groups + threadIdx.x / f.lanes;
         const bool token = tok < f.N, live = token && c0 < f.d;
         const int here = min(tok, f.N - 1), ch = c0 < f.d ? c0 : 0;
-        const int unit = run / f.chunks, s0 = unit * f.unit_slabs + (run % f.chunks) * f.share, n = min(f.share, (unit + 1) * f.unit_slabs - s0);
+        const int s0 = run.begin, n = run.end - run.begin;
         RowWalk<const T> in(xs, f.lin, s0, f.heads, here, ch);
         RowWalk<const float> gin(grad, p.lgrad, s0, f.heads, here, 0);
         RowWalk<float> out(dst, f.lout, s0, f.heads, here, 0);
@@ -691,12 +717,17 @@ PairKind pair_kind(const RotateArgs& a, int c) {
     return whole && at % c == 0 ? kHalvesShuffle : kHalvesShared;
 }
 
+// Tiles of `tokens`, and slabs whose positions are the same
+int units_of(RotateArgs* a, int tokens) {
+    a->unit_slabs = a->positions && a->pos_batch ? a->heads : a->slabs;
+    a->inv_d = 1.f / (float)a->d;
+    return a->tiles = (a->N + tokens - 1) / tokens;
+}
 // How many slabs a block visits with one set of angles; `tokens` of a block.  Fewer: the angles cost more, as much as
 // four rows; more: the last of the waves of `resident` blocks is emptier.  `rows`: of a slab (the tensors of a block).  With angles at
 // 0, 2, 4, 8 and 16 rows norm and rotation of 16 slabs of 128 x 128 take 96, 45, 39, 39 and 43 us.
 int plan_rotate(RotateArgs* a, int tokens, int rows, int resident) {
-    const int tiles = (a->N + tokens - 1) / tokens;
-    a->unit_slabs = a->positions && a->pos_batch ? a->heads : a->slabs;
+    const int tiles = units_of(a, tokens);
     const long long alone = (long long)tiles * (a->slabs / a->unit_slabs);          // blocks if each visits all slabs of its unit
     long long best = 0;
     for (int chunks = 1; chunks <= a->unit_slabs; ++chunks) {
@@ -709,7 +740,6 @@ int plan_rotate(RotateArgs* a, int tokens, int rows, int resident) {
         if (blocks > 16ll * resident) break;
     }
     a->chunks = (a->unit_slabs + a->share - 1) / a->share;
-    a->inv_d = 1.f / (float)a->d;
     return tiles;
 }
 
@@ -730,6 +760,7 @@ template <typename T> cudaError_t launch_rotate_type(RotateArgs a, int sm_count,
     auto launch = [&](auto plain, auto norm) { return launch_dependent(a.norm ? norm : plain, grid, kRotThreads, 0, st, a); };
     if (kind == kNeighbours) return launch(rotate_pairs_kernel<T, false, false>, rotate_pairs_kernel<T, false, true>);
     if (kind == kHalvesShuffle) return launch(rotate_pairs_kernel<T, true, C == 8>, rotate_pairs_kernel<T, true, true>);
+    // 32-bit words, or element by element: the video grid of 8 x 45 x 80, bf16, 44.8 and 51.2 us
     const bool words = C == 4 || (a.channels[0] % 4 == 0 && a.channels[1] % 4 == 0 && a.channels[2] % 4 == 0);
     if (words) return launch(rotate_patch_kernel<T, true, false>, rotate_patch_kernel<T, true, true>);
     return launch(rotate_patch_kernel<T, C == 4, false>, rotate_patch_kernel<T, C == 4, true>);
@@ -744,9 +775,8 @@ template <typename T> cudaError_t launch_rotate_bwd_type(RotateBwdArgs a, int sm
     const int tensors = (a.fwd.x[0] != nullptr) + (a.fwd.x[1] != nullptr), most = backward_blocks(sm_count) / tensors;
     a.fwd.lanes = 1;
     while (a.fwd.lanes * Elem<T>::kVec < a.fwd.d) a.fwd.lanes *= 2;
-    const int tiles = plan_rotate(&a.fwd, kRotThreads / a.fwd.lanes, 1, most);
-    const long long items = (long long)tiles * a.fwd.chunks * (a.fwd.slabs / a.fwd.unit_slabs);
-    const int blocks = (int)(items < most ? items : most);
+    const long long all = (long long)units_of(&a.fwd, kRotThreads / a.fwd.lanes) * a.fwd.slabs;
+    const int blocks = (int)(all < most ? all : most);
     const dim3 grid(blocks, tensors);
     cudaError_t e;
     switch (pair_kind(a.fwd, Elem<T>::kVec)) {
