@@ -355,6 +355,9 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
 
     const int chunks_f = (p.F + 63) / 64;
     const int pairs = MODE == kProducts && kPairs == 1 ? p.terms : kPairs;
+    // fp32 sums along hidden units or rows: tensor memory cuts the last bit off at every step, which over thousands of summands shows; the two accumulators have
+    // a half of the sum each and are added in the epilogue, instead of taking turns (dX of 2000 x 512 x 1536 was 2.1 times as far off as sums in plain fp32)
+    constexpr bool kHalfSums = MODE == kProducts && kPairs > 1;
     Walk<MODE, S::kParts> walk(p, who, count);
     Work t;
 
@@ -419,10 +422,10 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             int stage = 0, round = 0, ord = 0;
             bool alive = true, there = false;                          // whether the stage's tiles were seen to be there already
             for (; alive && walk.next(t); ++ord) {
-                const int buf = ord & 1;
-                if (ord >= 2) wait_spin(pp, BAR_READ + buf, (ord >> 1) - 1, kTimeoutRole);
+                const int buf = kHalfSums ? 0 : ord & 1, use = kHalfSums ? ord : ord >> 1, middle = (t.k0 + t.k1 + 1) >> 1;
+                if (use > 0) wait_spin(pp, BAR_READ + buf, use - 1, kTimeoutRole);
                 tc_fence_after_sync();
-                const uint32_t d = pp.tmem + 256 * buf;
+                uint32_t d = pp.tmem + 256 * buf;
                 const bool weight = MODE == kProducts && t.weight;
                 // half of a tile: 64 hidden units, those of each block's rows of B that begin at 0 or at 64
                 const uint32_t id_here = S::kParts > 1 && t.part ? umma_idesc(fmt, 256, BN, 0) : id, b_at = kATile + (S::kParts > 1 && t.part == 2 ? 64 * 128 : 0);
@@ -435,6 +438,10 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                             alive = !pipe_dead(pp);
                         }
                         tc_fence_after_sync();
+                        if (kHalfSums) {
+                            d = pp.tmem + (k < middle ? 0 : 256);
+                            acc = pair > 0 || (k != t.k0 && k != middle);
+                        }
                         const uint32_t at = base + 1024 + stage * S::kStage, empty = pipe_bar(pp, BAR_EMPTY + stage);
                         const int kk = MODE == kProducts && !weight && k >= chunks_f ? k - chunks_f : k, left = total - 64 * kk;
                         if (++stage == kStages) { stage = 0; ++round; }
@@ -701,12 +708,12 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
         } else {
             // boxes of 32 columns and 32 rows, those of a tile in turn by the four warps that share its rows
             for (; walk.next(t); ++ord) {
-                const int buf = ord & 1, blocks = p.line.n / 32, limit = t.weight ? p.F : p.M;
+                const int buf = kHalfSums ? 0 : ord & 1, blocks = p.line.n / 32, limit = t.weight ? p.F : p.M;
                 const int in_tile = 128 * rank + 32 * q, row0 = t.weight ? 128 * t.mt + 32 * q : 256 * t.mt + in_tile;
                 const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
                 const CUtensorMap* map = !t.whole ? &p.share : t.weight ? &p.s[1 + rank] : &p.s[0];
                 const bool wide = sizeof(T) == 4 || !t.whole;
-                await(BAR_ACC + buf, ord >> 1);
+                await(BAR_ACC + buf, kHalfSums ? ord : ord >> 1);
                 tc_fence_after_sync();
 #pragma unroll 1
                 for (int b = quarter; b < blocks; b += 4) {
@@ -714,6 +721,16 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     __syncwarp();
                     tmem_ld32(acc + 32 * b, reinterpret_cast<uint32_t(&)[32]>(v));
                     tmem_ld_wait();
+                    if (kHalfSums && t.k1 - t.k0 > 1) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 16) {
+                            float w[16];
+                            tmem_ld16(acc + 256 + 32 * b + i, w);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[i + j] += w[j];
+                        }
+                    }
                     if (b + 4 >= blocks) release(buf);
                     store_wait_read<0>();
                     __syncwarp();
