@@ -355,9 +355,10 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
 
     const int chunks_f = (p.F + 63) / 64;
     const int pairs = MODE == kProducts && kPairs == 1 ? p.terms : kPairs;
-    // fp32 sums along hidden units or rows: tensor memory cuts the last bit off at every step, which over thousands of summands shows; the two accumulators have
-    // a half of the sum each and are added in the epilogue, instead of taking turns (dX of 2000 x 512 x 1536 was 2.1 times as far off as sums in plain fp32)
-    constexpr bool kHalfSums = MODE == kProducts && kPairs > 1;
+    // fp32: tensor memory cuts the last bit off at every step of a sum, which shows from some hundred summands on; the two accumulators have a half of the sum
+    // each and are added in the epilogue, instead of taking turns.  Relative error with one accumulator, with two, and of sums in plain fp32: H of 64 x 640 x 2560
+    // 1.2e-6, 0.6e-6, 0.7e-6, its dX 1.1e-6, 0.5e-6, 0.7e-6; dW of 30000 x 64 x 256 1.2e-6, 0.6e-6, 0.8e-6.  It costs H of 1568 x 192 x 512 0.7 of 11.5 us.
+    constexpr bool kHalfSums = kPairs > 1;
     Walk<MODE, S::kParts> walk(p, who, count);
     Work t;
 
@@ -631,10 +632,10 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
         } else if constexpr (MODE <= kGrad) {
             constexpr int kCols = BN / 4 > 16 ? BN / 4 : 16;           // of a warp (BN = 32: half of the warps have none)
             for (; walk.next(t); ++ord) {
-                const int buf = ord & 1, row = (PAIR ? 256 : 128) * t.mt + 128 * rank + 32 * q + lane;
+                const int buf = kHalfSums ? 0 : ord & 1, row = (PAIR ? 256 : 128) * t.mt + 128 * rank + 32 * q + lane;
                 const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16), up = S::kParts > 1 && t.part ? BN / 2 : BN;
                 const size_t plane = (size_t)p.M * p.F;
-                await(BAR_ACC + buf, ord >> 1);
+                await(BAR_ACC + buf, kHalfSums ? ord : ord >> 1);
                 tc_fence_after_sync();
                 if (quarter * kCols >= BN || !mine_too(t)) {
                     release(buf);
@@ -649,6 +650,14 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                         tmem_ld16(acc + at_col, g);
                         tmem_ld16(acc + up + at_col, v);
                         tmem_ld_wait();
+                        if (kHalfSums && p.chunks > 1) {
+                            float g2[16], v2[16];
+                            tmem_ld16(acc + 256 + at_col, g2);
+                            tmem_ld16(acc + 256 + up + at_col, v2);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) { g[i] += g2[i]; v[i] += v2[i]; }
+                        }
                         if (s == kCols / 16 - 1) release(buf);
 #pragma unroll
                         for (int j = 0; j < 16; j += 8) {
@@ -1025,7 +1034,7 @@ GatedLine plan_line(int M, int C, int F, int sm_count) {
 
 // G and U: 128 hidden units a tile of 256 rows for a pair of blocks; where that leaves half of the SMs without work, tiles of 128 rows and 64 units, or 32
 // where those still do.  Forward, bf16 (us with 128, 64, 32 units): 512 x 192 x 512 5.8, 4.4, 3.9; 768 x 320 x 1280 6.5, 5.0, 6.0; 1536 x 320 x 1280 7.2, 7.0, 9.2;
-// 512 x 1024 x 4096 10.7, 12.2, 18.8.  fp32: 256 x 320 x 1280 18.1, 14.1, 13.0; 768 18.7, 15.4, 20.3; 1024 20.0, 22.9, 27.5.
+// 512 x 1024 x 4096 10.7, 12.2, 18.8.  fp32: 256 x 320 x 1280 18.0, 14.5, 13.3; 768 18.9, 16.4, 21.5; 1024 19.8, 24.7, 29.5.
 struct GatedTiles { int bn, tiles_m, tiles_n, blocks; };
 GatedTiles plan_tiles(int M, int F, int sm_count) {
     GatedTiles t;
