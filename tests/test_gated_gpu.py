@@ -272,3 +272,23 @@ def test_biases_are_summed_before_they_are_rounded(dtype, M, C, F):
     for n, e in zip(("db_gate", "db_up"), hidden_errors(x, wg, wu, dh, bg, bu, "gelu", 1e-5, 0.0)):
         bound = STEP[dtype] * grads[n].abs() + e.sum(0) + (6e-8 if dtype == "f16" else 0.0)
         assert ((back[n].double() - grads[n]).abs() <= bound).all()
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 hidden values.  Only some rows have a gradient, among them the last: what the others add is zero."""
+    M, C, F, dtype = 2100000, 8, 1032, "bf16"
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    x, wg, wu = ((torch.randn(s, generator=gen, device="cuda") * f).to(DT[dtype]) for s, f in (((M, C), 1.0), ((F, C), C ** -0.5), ((F, C), C ** -0.5)))
+    some = torch.tensor([0, 1, 127, 255, 256, M // 2, M // 2 + 77, M - 300, M - 2, M - 1], device="cuda")
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    out = mod.gated(x, wg, wu, activation="gelu")
+    dh = torch.randn((len(some), F), generator=gen, device="cuda").to(DT[dtype])
+    h, grads = reference(x[some], wg, wu, dh, None, None, "gelu")
+    check_forward(out[some], h, dtype)
+    out.zero_()
+    out[some] = dh
+    back = mod.gated_backward(x, wg, wu, out, activation="gelu")
+    assert mod.query_status() == 0
+    assert rel(back["dx"][some], grads["dx"]) <= REL_BWD[dtype] and int(back["dx"].abs().sum(1).count_nonzero()) <= len(some)
+    for n in ("dw_gate", "dw_up"):
+        assert rel(back[n], grads[n]) <= REL_BWD[dtype]

@@ -275,3 +275,23 @@ def test_heads_whose_lanes_leave_some_of_a_warp_idle(d, dtype):
             given = dict(q_gain=gains[0], k_gain=gains[1], eps=1e-5) if norm else {}
             for got, x, gain in zip(mod.rotate(q, k, rotary, **given), (q, k), gains):
                 check(got, *reference(x, grid_positions(extent), channels, freq, False, gain if norm else None, 1e-5 if norm else None), dtype)
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_offsets_past_32_bits(norm):
+    """Batch entries more than 2^32 bytes, and 2^31 elements, apart, in place and back."""
+    B, h, d, extent, dt = 2, 2, 64, (16, 8), torch.bfloat16
+    N, apart = extent[0] * extent[1], (1 << 31) + 4096
+    room = torch.empty(apart + 2 * N * h * d, dtype=dt, device="cuda")
+    q, k = (room[i * N * h * d:].as_strided((B, h, N, d), (apart, d, h * d, 1)) for i in range(2))
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for t in (q, k):
+        t.copy_(torch.randn((B, h, N, d), generator=gen, device="cuda"))
+    gains = [(1 + 0.2 * torch.randn(d, generator=gen, device="cuda")).to(dt) for _ in range(2)]
+    given = dict(q_gain=gains[0], k_gain=gains[1], eps=1e-5) if norm else {}
+    freq = Rotary.frequencies((32, 32))
+    mod, rotary = AgentAttention(B, h, d, N, 1, dt), Rotary(freq, (32, 32), extent)
+    want = [reference(t.clone(), grid_positions(extent), (32, 32), freq, False, g if norm else None, 1e-5 if norm else None) for t, g in zip((q, k), gains)]
+    mod.rotate(q, k, rotary, out=(q, k), **given)
+    for got, (ref, size) in zip((q, k), want):
+        check(got, ref, size, "bf16")
