@@ -173,7 +173,10 @@ template <typename T> __device__ __forceinline__ void store_operand8(void* base,
         if (second) {
             float rest[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) rest[i] = f[i] - Elem<T>::to_f32(Elem<T>::from_f32(f[i]));
+            for (int i = 0; i < 8; ++i) {
+                const float r = f[i] - Elem<T>::to_f32(Elem<T>::from_f32(f[i]));
+                rest[i] = r - r == 0.f ? r : 0.f;         // (an infinity leaves nothing, not NaN)
+            }
             store8<T>(static_cast<T*>(base) + plane + at, rest);
         }
     } else {

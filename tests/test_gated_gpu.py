@@ -292,3 +292,21 @@ def test_offsets_past_32_bits():
     assert rel(back["dx"][some], grads["dx"]) <= REL_BWD[dtype] and int(back["dx"].abs().sum(1).count_nonzero()) <= len(some)
     for n in ("dw_gate", "dw_up"):
         assert rel(back[n], grads[n]) <= REL_BWD[dtype]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_infinite_gradients_of_few_rows_stay_infinite(dtype):
+    """What rounding an infinity to the element type leaves is nothing: the second term does not make NaN of it."""
+    x, wg, wu, dh, bg, bu = inputs(3, 16, 24, dtype, "gu", seed=2)
+    dh[1, 5] = math.inf
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    g, u = x.double() @ wg.double().T + bg.double(), x.double() @ wu.double().T + bu.double()
+    s = torch.sigmoid(g)
+    dg, du = dh.double() * u * (s + g * s * (1 - s)), dh.double() * g * s
+    want = dict(dw_gate=dg.T @ x.double(), dw_up=du.T @ x.double(), db_gate=dg.sum(0), db_up=du.sum(0))
+    back = mod.gated_backward(x, wg, wu, dh, b_gate=bg, b_up=bu, activation="silu")
+    rest = torch.arange(24, device="cuda") != 5
+    for n in want:
+        assert want[n][5].isinf().all() and torch.equal(back[n][5].double(), want[n][5])
+        assert rel(back[n][rest], want[n][rest]) <= REL_BWD[dtype]
+    assert back["dx"][1].isfinite().sum() == 0 and back["dx"][[0, 2]].isfinite().all()
