@@ -631,7 +631,8 @@ template <typename T, PairKind KIND> __global__ void __launch_bounds__(kRotThrea
                 sq = ffma2(x[k], x[k], sq);
                 dot = ffma2(fmul2(y[k], gain[k]), x[k], dot);
             }
-            const float r = rsqrtf(group_sum(sq.x + sq.y, f.lanes) * f.inv_d + f.eps);
+            const float ms = group_sum(sq.x + sq.y, f.lanes) * f.inv_d;
+            const float r = token ? rsqrtf(ms + f.eps) : 0.f;                // (past the last token nothing is added to the gains' sums, not 0 / sqrt(0) for eps = 0)
             const float m = -group_sum(dot.x + dot.y, f.lanes) * f.inv_d * r * r * r;
             float v[C];
 #pragma unroll

@@ -295,3 +295,33 @@ def test_offsets_past_32_bits(norm):
     mod.rotate(q, k, rotary, out=(q, k), **given)
     for got, (ref, size) in zip((q, k), want):
         check(got, ref, size, "bf16")
+
+
+def gradients(x, g, positions, channels, freq, neighbours, gain, eps):
+    """In 64 bits: dX, and the bound of an element's error (head of this file); the gain's gradient, and the sum of its summands' sizes."""
+    xd, w = x.double(), 1.0 if gain is None else gain.double()
+    back = turned(g.double(), positions, channels, freq, neighbours, -1.0)
+    r = (xd.square().mean(-1, keepdim=True) + eps).rsqrt()
+    dx = r * (back * w - xd * r * (back * w * xd * r).mean(-1, keepdim=True))
+    terms = back * xd * r
+    return dx, 4e-6 * torch.maximum(dx.abs(), back.abs() * r).amax(-1, keepdim=True), terms.sum((0, 1, 2)), terms.abs().sum((0, 1, 2))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("extent,d", [((14, 14), 64), ((1, 1), 64), ((14, 14), 40), ((3, 11), 128), ((1, 5), 8)])
+def test_gradients_with_eps_of_zero(extent, d, dtype):
+    """No row of the input is zero, so that every gradient is finite; rows past the last token of a tile are no rows."""
+    B, h, dt = 2, 3, DT[dtype]
+    N, channels = extent[0] * extent[1], (d // 4 * 2, d // 4 * 2)
+    gen = torch.Generator(device="cuda").manual_seed(d + N)
+    x, g = views("interleaved", B, h, N, d, dt, gen), views("dense", B, h, N, d, torch.float32, gen)
+    gains = [(1 + 0.2 * torch.randn(d, generator=gen, device="cuda")).to(dt) for _ in range(2)]
+    freq = Rotary.frequencies(channels)
+    mod, rotary = AgentAttention(B, h, d, N, 1, dt), Rotary(freq, channels, extent)
+    got = mod.rotate_backward(*g, rotary, q=x[0], k=x[1], q_gain=gains[0], k_gain=gains[1], eps=0.0)
+    for i, n in enumerate("qk"):
+        dx, bound, dgain, size = gradients(x[i], g[i], grid_positions(extent), channels, freq, False, gains[i], 0.0)
+        assert ((got[f"d{n}"].double() - dx).abs() <= bound).all()
+        assert ((got[f"d{n}_gain"].double() - dgain).abs() <= 4e-6 * size).all()
+    for i, out in enumerate(mod.rotate(*x, rotary, q_gain=gains[0], k_gain=gains[1], eps=0.0)):
+        check(out, *reference(x[i], grid_positions(extent), channels, freq, False, gains[i], 0.0), dtype)
