@@ -48,7 +48,7 @@ template <int C, PairKind KIND> __device__ __forceinline__ void lane_angles(cons
         int at = 0, fr = 0, partner = c;
         bool second = false;
         freq[j] = -1;
-        axes[j] = 0;
+        axes[j] = 3;                      // none: it keeps its value whatever the position, an infinite one too
 #pragma unroll
         for (int a = 0; a < 3; ++a) {
             const int seg = p.channels[a], half = seg >> 1, o = c - at;
@@ -108,6 +108,8 @@ __device__ __forceinline__ void token_position(const RotateArgs& p, int b, int t
     }
 }
 
+__device__ __forceinline__ float on_axis(const float (&pos)[3], unsigned a) { return a == 0 ? pos[0] : a == 1 ? pos[1] : a == 2 ? pos[2] : 0.f; }
+
 // Factors of a channel's own value and of its partner's, in pairs
 template <int C, PairKind KIND, bool FAST> __device__ __forceinline__ void token_turns(const RotateArgs& p, const LaneAngles<C, KIND>& la, int b, int tok, int partner_lane, bool inverse, float2 (&cs)[C / 2], float2 (&sn)[C / 2]) {
     constexpr int A = LaneAngles<C, KIND>::kAngles;
@@ -116,7 +118,7 @@ template <int C, PairKind KIND, bool FAST> __device__ __forceinline__ void token
 #pragma unroll
     for (int i = 0; i < A; ++i) {
         const unsigned a = la.axis >> (2 * i) & 3u;
-        turn<FAST>(a == 0 ? pos[0] : a == 1 ? pos[1] : pos[2], la.hi[i], la.lo[i], c[i], s[i]);
+        turn<FAST>(on_axis(pos, a), la.hi[i], la.lo[i], c[i], s[i]);
     }
     if constexpr (KIND == kNeighbours) {
 #pragma unroll
@@ -328,7 +330,7 @@ template <typename T, bool HALVES, bool NORM> __global__ void __launch_bounds__(
             const float w = on ? __ldg(p.freq + f) : 0.f;
             constexpr float kInv = 0.15915494309189535f, kInvLo = 6.420638243e-09f;     // 1 / (2 pi) as a sum of two fp32 numbers
             const float hi = w * kInv, lo = fmaf(w, kInv, -hi) + w * kInvLo;
-            turn<sizeof(T) == 2>(ax == 0 ? pos[0] : ax == 1 ? pos[1] : pos[2], hi, lo, c[j], s[j]);
+            turn<sizeof(T) == 2>(on_axis(pos, on ? ax : 3), hi, lo, c[j], s[j]);
             if (p.inverse) s[j] = -s[j];
             if (NORM) s_turn[j][threadIdx.x] = make_float2(c[j], s[j]);
         }

@@ -325,3 +325,32 @@ def test_gradients_with_eps_of_zero(extent, d, dtype):
         assert ((got[f"d{n}_gain"].double() - dgain).abs() <= 4e-6 * size).all()
     for i, out in enumerate(mod.rotate(*x, rotary, q_gain=gains[0], k_gain=gains[1], eps=0.0)):
         check(out, *reference(x[i], grid_positions(extent), channels, freq, False, gains[i], 0.0), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("channels,neighbours", [((16,), False), ((12,), False), ((8, 16), False), ((6, 8), True), ((0, 16), False)])
+def test_non_finite_positions_reach_their_axis_alone(channels, neighbours, dtype):
+    """A token whose position on an axis is infinite or NaN: the channels of that axis are lost; those of the others and those past the segments are not, nor
+    is any other token."""
+    B, h, d, N, axes = 2, 2, 64, 9, len(channels)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    positions = torch.rand((1, N, axes), generator=gen, device="cuda") * 20
+    fine = positions.clone()
+    positions[0, 2, 0], positions[0, 7, axes - 1] = float("inf"), float("nan")
+    q, k = views("dense", B, h, N, d, DT[dtype], gen)
+    g = views("dense", B, h, N, d, torch.float32, gen)
+    freq = Rotary.frequencies(channels)
+    mod = AgentAttention(B, h, d, N, 1, DT[dtype])
+    lost = torch.zeros((N, d), dtype=torch.bool, device="cuda")
+    lost[2, :channels[0]], lost[7, sum(channels[:-1]):sum(channels)] = True, True
+    bad, good = (Rotary(freq, channels, positions=p, pairs=neighbours) for p in (positions, fine))
+    for given in ({}, {"eps": 1e-5}):
+        for got, want in zip(mod.rotate(q, k, bad, **given), mod.rotate(q, k, good, **given)):
+            assert torch.equal(got[:, :, ~lost], want[:, :, ~lost]) and torch.isnan(got[:, :, lost]).all()
+    for got, want in zip(mod.rotate_backward(*g, bad).values(), mod.rotate_backward(*g, good).values()):
+        assert torch.equal(got[:, :, ~lost], want[:, :, ~lost]) and torch.isnan(got[:, :, lost]).all()
+    # a norm's gradient takes the whole row with it
+    row = lost.any(1)
+    got, want = (mod.rotate_backward(*g, r, q=q, k=k, eps=1e-5) for r in (bad, good))
+    for n in got:
+        assert torch.equal(got[n][:, :, ~row], want[n][:, :, ~row]) and torch.isnan(got[n][:, :, row]).all()
