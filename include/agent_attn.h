@@ -323,7 +323,8 @@ typedef enum {
 typedef struct {
     int axes;                 /* 0 (no rotation) .. 3                                              */
     int extent[3];            /* grid of the tokens, row-major over extent[0 .. axes - 1], whose product
-                                 is the token count; not read where `positions` is given          */
+                                 is the token count, at most 2^24 each (coordinates are fp32 numbers); not read
+                                 where `positions` is given                                        */
     int channels[3];          /* channels of a head that each axis turns: even, sum <= head_dim    */
     int pairs;                /* aa_pairs                                                          */
     const float* freq;        /* device fp32 [sum(channels) / 2]: radians per unit, axis after axis */
@@ -347,7 +348,7 @@ typedef struct {
  *   Q_out, K_out device, strides out_strides (NULL: dense).  Either may be its own input where both have the
  *                same strides (in place: a fused projection's output is prepared where
  *                agent_attn_forward_strided reads it); no other overlap
- * Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED (N > max_tokens), AA_ERR_CUDA.  No host synchronisation,
+ * Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED (N > max_tokens, an extent past 2^24), AA_ERR_CUDA.  No host synchronisation,
  * no allocation. */
 int agent_attn_rotate(agent_attn_handle* h, const void* Q, const void* K, const long long in_strides[3], int n_tokens,
                       const agent_attn_rotary* rotary, const agent_attn_norm* norm,

@@ -691,6 +691,8 @@ static int rotate_args(agent_attn_handle* h, int n_tokens, const agent_attn_rota
                 return fail(h, AA_ERR_INVALID_ARG, "channels of the axes must be even and add up to at most head_dim=%d", h->cfg.head_dim);
             if (!rotary->positions && (rotary->extent[i] <= 0 || (tokens *= rotary->extent[i]) > n_tokens))
                 return fail(h, AA_ERR_INVALID_ARG, "the grid does not have N=%d tokens", n_tokens);
+            if (!rotary->positions && rotary->extent[i] > (1 << 24))      // coordinates are fp32 numbers
+                return fail(h, AA_ERR_UNSUPPORTED, "an axis of the grid has at most 2^24 tokens, not %d", rotary->extent[i]);
             a->channels[i] = c;
             a->extent[i] = rotary->positions ? 1 : rotary->extent[i];
         }

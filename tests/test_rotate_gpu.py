@@ -354,3 +354,24 @@ def test_non_finite_positions_reach_their_axis_alone(channels, neighbours, dtype
     got, want = (mod.rotate_backward(*g, r, q=q, k=k, eps=1e-5) for r in (bad, good))
     for n in got:
         assert torch.equal(got[n][:, :, ~row], want[n][:, :, ~row]) and torch.isnan(got[n][:, :, row]).all()
+
+
+def test_axes_past_what_fp32_counts_are_refused():
+    """An odd coordinate past 2^24 is no fp32 number; up to there every token has its own angle, the last one too."""
+    N, d = (1 << 24) + 2, 8
+    mod, freq = AgentAttention(1, 1, d, N, 1, torch.bfloat16), torch.ones(1, device="cuda")
+    q = torch.ones((1, 1, N, d), dtype=torch.bfloat16, device="cuda")
+    for extent, channels in (((N,), (2,)), ((1, N), (0, 2))):
+        with pytest.raises(AgentAttnError) as e:
+            mod.rotate(q, None, Rotary(freq, channels, extent))
+        assert e.value.status == 2
+    with pytest.raises(AgentAttnError) as e:
+        mod.rotate_backward(q.float(), None, Rotary(freq, (2,), (N,)))
+    assert e.value.status == 2
+    last = 1 << 24
+    got, _ = mod.rotate(q[:, :, :last], None, Rotary(freq, (2,), (last,)))
+    t = torch.arange(last - 100, last, dtype=torch.float64, device="cuda")
+    assert ((got[0, 0, -100:, 0].double() - (t.cos() - t.sin())).abs() <= 2.0 ** -8 * 1.5).all()
+    two = mod.rotate(q, None, Rotary(torch.ones(2, device="cuda"), (2, 2), (2, N // 2)))[0]        # two axes have room for more
+    t = torch.tensor([N // 2 - 1], dtype=torch.float64, device="cuda")
+    assert ((two[0, 0, -1, 2].double() - (t.cos() - t.sin())).abs() <= 2.0 ** -8 * 1.5).all()
