@@ -375,3 +375,106 @@ def test_axes_past_what_fp32_counts_are_refused():
     two = mod.rotate(q, None, Rotary(torch.ones(2, device="cuda"), (2, 2), (2, N // 2)))[0]        # two axes have room for more
     t = torch.tensor([N // 2 - 1], dtype=torch.float64, device="cuda")
     assert ((two[0, 0, -1, 2].double() - (t.cos() - t.sin())).abs() <= 2.0 ** -8 * 1.5).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("own", [False, True])
+@pytest.mark.parametrize("N,d,neighbours", [(50, 64, False), (129, 40, True), (7, 128, False)])
+def test_norms_and_gradients_over_given_positions(N, d, neighbours, own, dtype):
+    """Positions of all entries, or each entry's own: runs of a block that go from one entry to the next change their angles there, in both directions."""
+    B, h, channels, eps = 5, 3, (d // 4 * 2, d // 4 * 2), 1e-5
+    gen = torch.Generator(device="cuda").manual_seed(N + d)
+    positions = torch.rand((B if own else 1, N, 2), generator=gen, device="cuda") * 200 - 100
+    x, g = views("interleaved", B, h, N, d, DT[dtype], gen), views("apart", B, h, N, d, torch.float32, gen)
+    gains = [(1 + 0.2 * torch.randn(d, generator=gen, device="cuda")).to(DT[dtype]) for _ in range(2)]
+    freq = Rotary.frequencies(channels)
+    mod, rotary = AgentAttention(B, h, d, N, 1, DT[dtype]), Rotary(freq, channels, positions=positions, pairs=neighbours)
+    at = positions.cpu()
+    for i, out in enumerate(mod.rotate(*x, rotary, q_gain=gains[0], k_gain=gains[1], eps=eps)):
+        check(out, *reference(x[i], at, channels, freq, neighbours, gains[i], eps), dtype)
+    got = mod.rotate_backward(*g, rotary, q=x[0], k=x[1], q_gain=gains[0], k_gain=gains[1], eps=eps)
+    bare = mod.rotate_backward(*g, rotary)
+    for i, n in enumerate("qk"):
+        dx, bound, dgain, size = gradients(x[i], g[i], at, channels, freq, neighbours, gains[i], eps)
+        assert ((got[f"d{n}"].double() - dx).abs() <= bound).all()
+        assert ((got[f"d{n}_gain"].double() - dgain).abs() <= 4e-6 * size).all()
+        check(bare[f"d{n}"], turned(g[i].double(), at, channels, freq, neighbours, -1.0), reference(g[i], at, channels, freq, neighbours, None, None)[1], "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_keys_alone_and_norms_without_gains(neighbours, dtype):
+    """One tensor has the results that it has beside the other one.  (A gain's sum is shared out to other blocks then: inside its bound.)"""
+    B, h, d, extent, channels, eps = 3, 2, 64, (9, 13), (20, 20), 1e-5
+    N = extent[0] * extent[1]
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    x, g = views("dense", B, h, N, d, DT[dtype], gen), views("interleaved", B, h, N, d, torch.float32, gen)
+    gain = (1 + 0.2 * torch.randn(d, generator=gen, device="cuda")).to(DT[dtype])
+    freq = Rotary.frequencies(channels)
+    mod, rotary = AgentAttention(B, h, d, N, 1, DT[dtype]), Rotary(freq, channels, extent, pairs=neighbours)
+    for given in ({}, {"eps": eps}, {"eps": eps, "k_gain": gain}):
+        both, alone = mod.rotate(*x, rotary, **given), mod.rotate(None, x[1], rotary, **given)
+        assert alone[0] is None and torch.equal(alone[1], both[1])
+        norm = "eps" in given
+        ins = dict(q=x[0], k=x[1]) if norm else {}
+        both, alone = mod.rotate_backward(*g, rotary, **ins, **given), mod.rotate_backward(None, g[1], rotary, k=x[1], **given)
+        assert set(alone) == {"dk"} | ({"dk_gain"} if "k_gain" in given else set()) and torch.equal(alone["dk"], both["dk"])
+        if not norm:
+            continue
+        for i, n in enumerate("qk"):
+            dx, bound, dgain, size = gradients(x[i], g[i], grid_positions(extent), channels, freq, neighbours, given.get(f"{n}_gain"), eps)
+            assert ((both[f"d{n}"].double() - dx).abs() <= bound).all()
+        if "k_gain" in given:
+            assert all(((t["dk_gain"].double() - dgain).abs() <= 4e-6 * size).all() for t in (both, alone))
+
+
+def test_non_finite_gradients_stay_in_their_row():
+    """An infinity or a NaN in the gradient of a result: its row of dX, and in the gain's gradient the two channels of its pair."""
+    B, h, d, extent, channels, eps = 2, 2, 64, (5, 7), (32, 32), 1e-5
+    N = 35
+    for dtype in ("f32", "bf16"):
+        gen = torch.Generator(device="cuda").manual_seed(12)
+        x, g = views("dense", B, h, N, d, DT[dtype], gen), views("dense", B, h, N, d, torch.float32, gen)
+        gain = (1 + 0.2 * torch.randn(d, generator=gen, device="cuda")).to(DT[dtype])
+        freq = Rotary.frequencies(channels)
+        mod, rotary = AgentAttention(B, h, d, N, 1, DT[dtype]), Rotary(freq, channels, extent)
+        dx, bound, dgain, size = gradients(x[0], g[0], grid_positions(extent), channels, freq, False, gain, eps)
+        for value in (float("inf"), float("nan")):
+            bad = g[0].clone()
+            bad[1, 0, 11, 37] = value                        # of the pair 37, 53
+            got = mod.rotate_backward(bad, g[1], rotary, q=x[0], k=x[1], q_gain=gain, k_gain=gain, eps=eps)
+            rows, cols = torch.ones((B, h, N), dtype=torch.bool, device="cuda"), torch.ones(d, dtype=torch.bool, device="cuda")
+            rows[1, 0, 11], cols[[37, 53]] = False, False
+            assert not got["dq"][1, 0, 11].isfinite().any() and ((got["dq"].double() - dx).abs() <= bound)[rows].all()
+            assert not got["dq_gain"][~cols].isfinite().any() and ((got["dq_gain"].double() - dgain).abs() <= 4e-6 * size)[cols].all()
+            assert got["dk"].isfinite().all() and got["dk_gain"].isfinite().all()
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_gradients_at_offsets_past_32_bits(norm):
+    """Batch entries 2^31 elements apart, of the gradients (8 GB) and of the inputs, in place."""
+    B, h, d, extent, channels, eps = 2, 2, 64, (16, 8), (32, 32), 1e-5
+    N, apart = 128, (1 << 31) + 4096
+    gen = torch.Generator(device="cuda").manual_seed(13)
+
+    def far(dtype):
+        room = torch.empty(apart + 2 * N * h * d, dtype=dtype, device="cuda")
+        got = [room[i * N * h * d:].as_strided((B, h, N, d), (apart, d, h * d, 1)) for i in range(2)]
+        for t in got:
+            t.copy_(torch.randn((B, h, N, d), generator=gen, device="cuda"))
+        return got
+    g = far(torch.float32)
+    x = far(torch.bfloat16) if norm else [None, None]
+    freq = Rotary.frequencies(channels)
+    mod, rotary = AgentAttention(B, h, d, N, 1, torch.bfloat16), Rotary(freq, channels, extent)
+    if norm:
+        gain = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+        want = [gradients(a.clone(), b.clone(), grid_positions(extent), channels, freq, False, gain, eps) for a, b in zip(x, g)]
+        got = mod.rotate_backward(*g, rotary, q=x[0], k=x[1], q_gain=gain, k_gain=gain, eps=eps, out=g)
+        for n, t, (dx, bound, dgain, size) in zip("qk", g, want):
+            assert ((t.double() - dx).abs() <= bound).all() and ((got[f"d{n}_gain"].double() - dgain).abs() <= 4e-6 * size).all()
+    else:
+        want = [(turned(t.double(), grid_positions(extent), channels, freq, False, -1.0), reference(t.clone(), grid_positions(extent), channels, freq, False, None, None)[1]) for t in g]
+        mod.rotate_backward(*g, rotary, out=g)
+        for t, (dx, size) in zip(g, want):
+            check(t, dx, size, "f32")
