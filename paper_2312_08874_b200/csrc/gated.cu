@@ -1038,14 +1038,15 @@ GatedLine plan_line(int M, int C, int F, int sm_count) {
 // G and U: 128 hidden units a tile of 256 rows for a pair of blocks; where that leaves half of the SMs without work, tiles of 128 rows and 64 units, or 32
 // where those still do.  Forward, bf16 (us with 128, 64, 32 units): 512 x 192 x 512 5.8, 4.4, 3.9; 768 x 320 x 1280 6.5, 5.0, 6.0; 1536 x 320 x 1280 7.2, 7.0, 9.2;
 // 512 x 1024 x 4096 10.7, 12.2, 18.8.  fp32: 256 x 320 x 1280 18.0, 14.5, 13.3; 768 18.9, 16.4, 21.5; 1024 19.8, 24.7, 29.5.
+// `lone`: tiles of a pair are out (their epilogue writes one term of dG and dU).
 struct GatedTiles { int bn, tiles_m, tiles_n, blocks; };
-GatedTiles plan_tiles(int M, int F, int sm_count) {
+GatedTiles plan_tiles(int M, int F, bool lone, int sm_count) {
     GatedTiles t;
     t.bn = 128;
     t.tiles_m = (M + 255) / 256;
     t.tiles_n = (F + 127) / 128;
     const long long pairs = (long long)t.tiles_m * t.tiles_n;
-    if (4 * pairs <= sm_count) {
+    if (lone || 4 * pairs <= sm_count) {
         t.bn = (long long)((M + 127) / 128) * ((F + 63) / 64) * 2 <= sm_count ? 32 : 64;
         t.tiles_m = (M + 127) / 128;
         t.tiles_n = (F + t.bn - 1) / t.bn;
@@ -1061,8 +1062,10 @@ int column_slots(const GatedTiles& t) {
 
 // 16-bit elements: dG and dU as one term, rounded to the element type, which makes the error of dX and the weights' gradients 1.4 times that of their own
 // rounding; over few rows it is more by chance (up to 2.1 times with one row, 1.6 with 32, 1.5 with 128), and there two terms keep it at 1.  (64 x 320 x 1280
-// bf16 17.7 and 19.3 us; 256 x 640 x 2560 25.6 and 30.4, which one term has.)
-int gradient_terms(const GatedTiles& t, int M) { return t.bn < 128 && M <= 128 ? 2 : 1; }
+// bf16 17.7 and 19.3 us, 128 x 1024 x 8192 46.6 and 50.5, 128 x 2048 x 11008 f16 107 and 116; 256 x 640 x 2560 25.6 and 30.4, which one term has.)
+int gradient_terms(int M) { return M <= 128 ? 2 : 1; }
+// Tiles of the projections of a call
+GatedTiles call_tiles(int dtype, int M, int F, bool backward, int sm_count) { return plan_tiles(M, F, backward && dtype != kF32 && gradient_terms(M) > 1, sm_count); }
 
 // Workspace: terms of X, Wg, Wu (fp32) | dG | dU | shares of tiles of dX and the weights' gradients, of the column sums
 struct GatedWs { size_t x, wg, wu, dg, du, share, db, total; };
@@ -1076,8 +1079,8 @@ GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count
     w.wu = take(terms * F * C * 2);
     w.dg = w.du = w.share = w.db = at;
     if (backward) {
-        const GatedTiles t = plan_tiles(M, F, sm_count);
-        const size_t planes = (dtype == kF32 ? 3 : gradient_terms(t, M)) * (size_t)M * F * 2;
+        const GatedTiles t = call_tiles(dtype, M, F, true, sm_count);
+        const size_t planes = (dtype == kF32 ? 3 : gradient_terms(M)) * (size_t)M * F * 2;
         w.dg = take(planes);
         w.du = take(planes);
         w.share = take((size_t)(sm_count / 2) * 2 * 256 * plan_line(M, C, F, sm_count).n * 4);
@@ -1162,11 +1165,11 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     a.M = c.M; a.C = c.C; a.F = c.F; a.act = c.act;
     a.bg = c.bg; a.bu = c.bu; a.dh = c.dh;
     a.status = c.status;
-    const GatedTiles t = plan_tiles(c.M, c.F, c.sm_count);
+    const GatedTiles t = call_tiles(kWide ? kF32 : kBF16, c.M, c.F, c.dh != nullptr, c.sm_count);
     a.tiles_m = t.tiles_m; a.tiles_n = t.tiles_n; a.chunks = (c.C + 63) / 64;
     a.out0 = c.dh ? ws + w.dg : static_cast<char*>(c.h);
     a.out1 = ws + w.du;
-    a.terms = kWide ? kTerms : gradient_terms(t, c.M);
+    a.terms = kWide ? kTerms : gradient_terms(c.M);
     float* column = reinterpret_cast<float*>(ws + w.db);
     a.column = c.dbg ? column : nullptr;
     if (!make_map_3d_u16(&a.a[0], x, kTerms, c.M, c.C, 128) || !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, t.bn) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, t.bn)) return cudaErrorInvalidValue;

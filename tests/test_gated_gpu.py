@@ -310,3 +310,23 @@ def test_infinite_gradients_of_few_rows_stay_infinite(dtype):
         assert want[n][5].isinf().all() and torch.equal(back[n][5].double(), want[n][5])
         assert rel(back[n][rest], want[n][rest]) <= REL_BWD[dtype]
     assert back["dx"][1].isfinite().sum() == 0 and back["dx"][[0, 2]].isfinite().all()
+
+
+@pytest.mark.parametrize("name,dtype", [("silu", "bf16"), ("gelu", "f16")])
+@pytest.mark.parametrize("size", [(1, 64, 4744), (128, 64, 8192), (33, 40, 11008), (128, 512, 5128)])
+def test_gradients_of_few_rows_and_many_hidden_units_are_rounded_once(size, name, dtype):
+    """The bound of `test_gradients_of_few_rows_are_rounded_once`, with so many hidden units that their tiles fill the GPU."""
+    M, C, F = size
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, "gu", seed=M + F)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    _, grads = reference(x, wg, wu, dh, bg, bu, name)
+    need = int(mod.lib.agent_attn_gated_workspace_bytes(mod._h, M, C, F, 1))
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    back = mod.gated_backward(x, wg, wu, dh, b_gate=bg, b_up=bu, activation=name, workspace=ws)
+    assert mod.query_status() == 0
+    eg, eu = hidden_errors(x, wg, wu, dh, bg, bu, name, 2.0 ** -16 + 1e-5, 6e-8 if dtype == "f16" else 0.0)
+    xa = x.double().abs()
+    left = dict(dx=eg @ wg.double().abs() + eu @ wu.double().abs(), dw_gate=eg.T @ xa, dw_up=eu.T @ xa, db_gate=eg.sum(0), db_up=eu.sum(0))
+    for n, t in back.items():
+        bound = STEP[dtype] * grads[n].abs() + left[n] + (6e-8 if dtype == "f16" else 0.0)
+        assert ((t.double() - grads[n]).abs() <= bound).all(), (n, float(((t.double() - grads[n]).abs() / bound).max()))
