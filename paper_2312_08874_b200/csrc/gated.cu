@@ -66,13 +66,16 @@ struct GatedArgs {
     alignas(64) CUtensorMap s[3], g, w[2], share;      // staged results: H; dG, dU; dX, dWg, dWu; dH; kProducts: dG and dU in boxes of 64 rows; shares of tiles
 };
 
-template <typename T> struct GatedTerms {              // element of the operands, terms and pairs of terms
+// Element of the operands, terms and pairs of terms; and how long a sum in tensor memory gets (kMost, kPiece, in chunks of 64).  The tensor cores cut off what
+// lies below the last bit at every step of 16, always towards zero: 3e-8 of the sum a step, 1.9e-5 where 16384 channels are summed up in two halves.  Longer sums
+// are cut into pieces, which the epilogue adds up in fp32: 16 bits 1024 steps, 3e-5 (f16 itself 2e-4); fp32 32 steps, 1e-6.
+template <typename T> struct GatedTerms {
     using E = T;
-    static constexpr int kTerms = 1, kPairs = 1;
+    static constexpr int kTerms = 1, kPairs = 1, kMost = 256, kPiece = 256;
 };
 template <> struct GatedTerms<float> {
     using E = __nv_bfloat16;
-    static constexpr int kTerms = 3, kPairs = 6;
+    static constexpr int kTerms = 3, kPairs = 6, kMost = 16, kPiece = 8;
 };
 __device__ __forceinline__ void term_pair(int i, int& a, int& b) {     // (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
     a = (0x001012 >> (4 * i)) & 3;
@@ -200,12 +203,6 @@ __device__ __forceinline__ void ld_matrix4(uint32_t (&r)[4], uint32_t at) {
 __device__ __forceinline__ void st_matrix4(uint32_t at, const uint32_t (&r)[4]) {
     asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};\n" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
-// 16 rows of 32 columns of an accumulator: r[4 j + 2 h + e] is row lane / 4 + 8 h, column 8 j + 2 (lane % 4) + e
-__device__ __forceinline__ void tmem_ld_16x256b_x4(uint32_t taddr, float (&r)[16]) {
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
-                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]),
-                   "=f"(r[14]), "=f"(r[15]) : "r"(taddr) : "memory");
-}
 __device__ __forceinline__ float2 ld_shared_pair(uint32_t at) {
     float2 v;
     asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];\n" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
@@ -250,13 +247,16 @@ struct Work {
     int part;                                          // 0: a whole tile; else the half 1 or 2
     bool weight, whole;                                // kProducts: of dWg and dWu; the whole sum
     int slot;                                          // of a share
+    bool cut, first, last;                             // a piece of a long sum: which one
 };
-template <GatedMode MODE, int PARTS> struct Walk {
+// MOST (0: no sum of the launch is longer): a longer sum comes in pieces of at most PIECE chunks
+template <GatedMode MODE, int PARTS, int MOST, int PIECE> struct Walk {
     const GatedArgs& p;
     long long at, first, end;
     int who, own, own_end, mt, nt, left;               // left, later: kForward and kGrad, whose loops have no room for 64-bit arithmetic
     bool later;                                        // the run begins with a tile's second half
-    __device__ Walk(const GatedArgs& args, int who_, int count) : p(args), who(who_) {
+    int each, until;                                   // of a long sum: chunks of a piece, the last one's end (0: none is under way)
+    __device__ Walk(const GatedArgs& args, int who_, int count) : p(args), who(who_), each(0), until(0) {
         if (MODE == kProducts) {
             first = at = p.line.begin(who);
             end = p.line.begin(who + 1);
@@ -271,7 +271,30 @@ template <GatedMode MODE, int PARTS> struct Walk {
             mt = (int)(tile - (long long)nt * p.tiles_m);
         }
     }
-    __device__ bool next(Work& w) {
+    __device__ bool next(Work& w) {                    // (w: as the call before left it)
+        if (MOST == 0) return next_sum(w);
+        if (until) {
+            w.k0 = w.k1;
+            w.k1 = min(w.k0 + each, until);
+            w.first = false;
+            w.last = w.k1 == until;
+            if (w.last) until = 0;
+            return true;
+        }
+        if (!next_sum(w)) return false;
+        const int n = w.k1 - w.k0;
+        w.cut = n > MOST;
+        w.first = true;
+        w.last = !w.cut;
+        if (w.cut) {
+            const int pieces = (n + PIECE - 1) / PIECE;
+            each = (n + pieces - 1) / pieces;
+            until = w.k1;
+            w.k1 = w.k0 + each;
+        }
+        return true;
+    }
+    __device__ bool next_sum(Work& w) {
         if (MODE != kProducts) {
             if (left <= 0) return false;
             w.nt = nt; w.mt = mt;
@@ -314,7 +337,9 @@ template <GatedMode MODE, int PARTS> struct Walk {
     }
 };
 
-template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constant__ GatedArgs p) {
+// LONG: some sum is longer than GatedTerms::kMost.  Its pieces come in the first accumulator, and the epilogue's warps keep their sum, each its own part, in the
+// second one.
+template <typename T, GatedMode MODE, int BN, bool LONG> __global__ void __launch_bounds__(kThreads, 1) gated_kernel(const __grid_constant__ GatedArgs p) {
     using S = GatedShape<T, MODE, BN>;
     using E = typename GatedTerms<T>::E;
     constexpr int kPairs = GatedTerms<T>::kPairs, kStages = S::kStages;
@@ -362,8 +387,10 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
     // each and are added in the epilogue, instead of taking turns.  Relative error with one accumulator, with two, and of sums in plain fp32: H of 64 x 640 x 2560
     // 1.2e-6, 0.6e-6, 0.7e-6, its dX 1.1e-6, 0.5e-6, 0.7e-6; dW of 30000 x 64 x 256 1.2e-6, 0.6e-6, 0.8e-6.  It costs H of 1568 x 192 x 512 0.7 of 11.5 us.
     constexpr bool kHalfSums = kPairs > 1;
-    Walk<MODE, S::kParts> walk(p, who, count);
+    Walk<MODE, S::kParts, LONG ? GatedTerms<T>::kMost : 0, GatedTerms<T>::kPiece> walk(p, who, count);
     Work t;
+    // 16 bits, LONG: sums in one piece take turns with the accumulators (turn: whose it is next); how often each was in use
+    int turn = 0, used0 = 0, used1 = 0;
 
     if (warp == kEpiWarps || warp == kEpiWarps + 2) {
         // ------------------------------------------------------------------ producers: one of A, one of B (a warp issues a load in some 130 cycles)
@@ -426,7 +453,14 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             int stage = 0, round = 0, ord = 0;
             bool alive = true, there = false;                          // whether the stage's tiles were seen to be there already
             for (; alive && walk.next(t); ++ord) {
-                const int buf = kHalfSums ? 0 : ord & 1, use = kHalfSums ? ord : ord >> 1, middle = (t.k0 + t.k1 + 1) >> 1;
+                int buf = kHalfSums ? 0 : ord & 1, use = kHalfSums ? ord : ord >> 1;
+                if (LONG && !kHalfSums) {
+                    buf = t.cut ? 0 : turn;
+                    use = buf ? used1++ : used0++;
+                    if (!t.cut) turn ^= 1;
+                    else if (t.last) ++used1;                          // the epilogue reads the sum of the pieces there
+                }
+                const int middle = LONG && t.cut ? t.k1 : (t.k0 + t.k1 + 1) >> 1;
                 if (use > 0) wait_spin(pp, BAR_READ + buf, use - 1, kTimeoutRole);
                 tc_fence_after_sync();
                 uint32_t d = pp.tmem + 256 * buf;
@@ -487,6 +521,45 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
         };
         auto mine_too = [&](const Work& t) { return S::kParts == 1 || t.part == 0 || (quarter >> 1) == t.part - 1; };      // whether this warp has some of the tile
         auto column_at = [&](const Work& t) { return S::kParts > 1 && t.part ? 32 * (quarter & 1) : 32 * quarter; };       // of G in the accumulator (BN = 128)
+        // accumulator of the next sum or piece, and the parity of its arrival
+        auto accumulator = [&](const Work& t, int& parity) {
+            if (!LONG || kHalfSums) {
+                parity = kHalfSums ? ord : ord >> 1;
+                return kHalfSums ? 0 : ord & 1;
+            }
+            const int buf = t.cut ? 0 : turn;
+            parity = buf ? used1++ : used0++;
+            if (!t.cut) turn ^= 1;
+            return buf;
+        };
+        // a piece's columns of this warp are added to the sum
+        auto add_piece = [&](const Work& t, int col, int n) {
+#pragma unroll 1
+            for (int c = col; c < col + n; c += 16) {
+                const uint32_t at = pp.tmem + ((uint32_t)(32 * q) << 16) + c;
+                float v[16];
+                __syncwarp();
+                tmem_ld16(at, v);
+                tmem_ld_wait();
+                if (!t.first) {
+                    float w[16];
+                    tmem_ld16(at + 256, w);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] += w[i];
+                }
+                uint32_t o[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(v[i]);
+                tmem_st16(at + 256, o);
+                tmem_st_wait();
+            }
+        };
+        // after a piece: whether the sum is there (in the second accumulator)
+        auto summed = [&](const Work& t) {
+            if (!kHalfSums || !t.last) release(0);                     // (fp32: what it reserves are both, until the sum has been read)
+            return t.last;
+        };
         auto await = [&](int bar, int parity) {
             if (!mbar_test(pipe_bar(pp, bar), parity & 1)) wait_par(pp, bar, parity, kTimeoutTile);
         };
@@ -520,22 +593,33 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
             Work ahead;
             bool more = walk.next(ahead);
             int done = 0;                                              // tiles that this warp had some of
-            if (MODE == kGrad && more && mine_too(ahead)) fetch(ahead, 0);
+            if (MODE == kGrad && !LONG && more && mine_too(ahead)) fetch(ahead, 0);
             const bool biased = p.bg || p.bu;
             int bias_nt = -1;
             for (; more; ++ord) {
                 t = ahead;
                 more = walk.next(ahead);
-                const int buf = ord & 1, row0 = 256 * t.mt + 128 * rank + 32 * q, f0 = BN * t.nt + 32 * quarter;
-                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16) + column_at(t), up = S::kParts > 1 && t.part ? BN / 2 : BN;
+                const int row0 = 256 * t.mt + 128 * rank + 32 * q, f0 = BN * t.nt + 32 * quarter, up = S::kParts > 1 && t.part ? BN / 2 : BN;
+                int parity, buf = accumulator(t, parity);
+                if (LONG && t.cut) {
+                    await(BAR_ACC + buf, parity);
+                    tc_fence_after_sync();
+                    if (mine_too(t)) {
+                        add_piece(t, column_at(t), 32);
+                        add_piece(t, column_at(t) + up, 32);
+                    }
+                    if (!summed(t)) continue;
+                    buf = 1;
+                }
+                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16) + column_at(t);
                 if (MODE == kGrad && p.column && column_nt != t.nt) {
                     if (column_nt >= 0) flush();
                     column_nt = t.nt;
                 }
                 if (!mine_too(t)) {
-                    await(BAR_ACC + buf, ord >> 1);
+                    if (!LONG || !t.cut) await(BAR_ACC + buf, parity);
                     release(buf);
-                    if (MODE == kGrad && more && mine_too(ahead)) fetch(ahead, done);
+                    if (MODE == kGrad && !LONG && more && mine_too(ahead)) fetch(ahead, done);
                     __syncwarp();
                     continue;
                 }
@@ -549,14 +633,15 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     asm volatile("st.shared.v2.f32 [%0], {%1, %2};\n" ::"r"(bias + 8 * lane), "f"(b.x), "f"(b.y) : "memory");
                     __syncwarp();
                 }
-                await(BAR_ACC + buf, ord >> 1);
+                if (!LONG || !t.cut) await(BAR_ACC + buf, parity);
                 tc_fence_after_sync();
                 store_wait_read<0>();                                  // the tile before has left the patches
                 __syncwarp();
                 const uint32_t mine = patch + (MODE == kGrad ? kHalfPatch * (done & 1) : 0), other = patch + 2 * kHalfPatch;
                 if (MODE == kGrad) {
+                    if (LONG) fetch(t, done);                          // (not ahead: pieces may come between)
                     await(BAR_DH + warp, done);
-                    if (more && mine_too(ahead)) fetch(ahead, done + 1);
+                    if (!LONG && more && mine_too(ahead)) fetch(ahead, done + 1);
                 }
                 ++done;
                 by_activation(p.act, [&](auto act) {
@@ -635,13 +720,24 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
         } else if constexpr (MODE <= kGrad) {
             constexpr int kCols = BN / 4 > 16 ? BN / 4 : 16;           // of a warp (BN = 32: half of the warps have none)
             for (; walk.next(t); ++ord) {
-                const int buf = kHalfSums ? 0 : ord & 1, row = (PAIR ? 256 : 128) * t.mt + 128 * rank + 32 * q + lane;
-                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16), up = S::kParts > 1 && t.part ? BN / 2 : BN;
+                const int row = (PAIR ? 256 : 128) * t.mt + 128 * rank + 32 * q + lane, up = S::kParts > 1 && t.part ? BN / 2 : BN;
                 const size_t plane = (size_t)p.M * p.F;
-                await(BAR_ACC + buf, kHalfSums ? ord : ord >> 1);
+                const bool mine = quarter * kCols < BN && mine_too(t);
+                int parity, buf = accumulator(t, parity);
+                await(BAR_ACC + buf, parity);
                 tc_fence_after_sync();
-                if (quarter * kCols >= BN || !mine_too(t)) {
-                    release(buf);
+                if (LONG && t.cut) {
+                    if (mine) {
+                        add_piece(t, PAIR ? column_at(t) : quarter * kCols, kCols);
+                        add_piece(t, (PAIR ? column_at(t) : quarter * kCols) + up, kCols);
+                    }
+                    if (!summed(t)) continue;
+                    buf = 1;
+                }
+                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
+                const int lent = kHalfSums ? 0 : buf;
+                if (!mine) {
+                    release(lent);
                     continue;
                 }
                 by_activation(p.act, [&](auto act) {
@@ -653,7 +749,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                         tmem_ld16(acc + at_col, g);
                         tmem_ld16(acc + up + at_col, v);
                         tmem_ld_wait();
-                        if (kHalfSums && p.chunks > 1) {
+                        if (kHalfSums && p.chunks > 1 && !(LONG && t.cut)) {
                             float g2[16], v2[16];
                             tmem_ld16(acc + 256 + at_col, g2);
                             tmem_ld16(acc + 256 + up + at_col, v2);
@@ -661,7 +757,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
 #pragma unroll
                             for (int i = 0; i < 16; ++i) { g[i] += g2[i]; v[i] += v2[i]; }
                         }
-                        if (s == kCols / 16 - 1) release(buf);
+                        if (s == kCols / 16 - 1) release(lent);
 #pragma unroll
                         for (int j = 0; j < 16; j += 8) {
                             const int f = f0 + j;
@@ -720,20 +816,27 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
         } else {
             // boxes of 32 columns and 32 rows, those of a tile in turn by the four warps that share its rows
             for (; walk.next(t); ++ord) {
-                const int buf = kHalfSums ? 0 : ord & 1, blocks = p.line.n / 32, limit = t.weight ? p.F : p.M;
+                const int blocks = p.line.n / 32, limit = t.weight ? p.F : p.M;
                 const int in_tile = 128 * rank + 32 * q, row0 = t.weight ? 128 * t.mt + 32 * q : 256 * t.mt + in_tile;
-                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
                 const CUtensorMap* map = !t.whole ? &p.share : t.weight ? &p.s[1 + rank] : &p.s[0];
                 const bool wide = sizeof(T) == 4 || !t.whole;
-                await(BAR_ACC + buf, kHalfSums ? ord : ord >> 1);
+                int parity, buf = accumulator(t, parity);
+                await(BAR_ACC + buf, parity);
                 tc_fence_after_sync();
+                if (LONG && t.cut) {
+                    for (int b = quarter; b < blocks; b += 4) add_piece(t, 32 * b, 32);
+                    if (!summed(t)) continue;
+                    buf = 1;
+                }
+                const uint32_t acc = pp.tmem + 256 * buf + ((uint32_t)(32 * q) << 16);
+                const int lent = kHalfSums ? 0 : buf;
 #pragma unroll 1
                 for (int b = quarter; b < blocks; b += 4) {
                     float v[32];
                     __syncwarp();
                     tmem_ld32(acc + 32 * b, reinterpret_cast<uint32_t(&)[32]>(v));
                     tmem_ld_wait();
-                    if (kHalfSums && t.k1 - t.k0 > 1) {
+                    if (kHalfSums && t.k1 - t.k0 > 1 && !(LONG && t.cut)) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 16) {
                             float w[16];
@@ -743,7 +846,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                             for (int j = 0; j < 16; ++j) v[i + j] += w[j];
                         }
                     }
-                    if (b + 4 >= blocks) release(buf);
+                    if (b + 4 >= blocks) release(lent);
                     store_wait_read<0>();
                     __syncwarp();
                     if (wide) {                                        // rows of 128 bytes
@@ -759,7 +862,7 @@ template <typename T, GatedMode MODE, int BN> __global__ void __launch_bounds__(
                     if (row0 < limit && c0 < p.C) tma_store_3d_e(elected, map, t.whole ? c0 : 32 * b, t.whole ? row0 : in_tile, t.whole ? 0 : t.slot, patch);
                     store_commit();
                 }
-                if (quarter >= blocks) release(buf);
+                if (quarter >= blocks) release(lent);
                 __syncwarp();
             }
             store_wait_read<0>();
@@ -1035,6 +1138,13 @@ GatedLine plan_line(int M, int C, int F, int sm_count) {
     return l;
 }
 
+// At least as many chunks as a pair has of any tile
+long long longest_sum(const GatedLine& l) {
+    const long long own = l.whole ? l.chunks_x : 0, run = l.total() / l.pairs + 1 - (long long)(l.whole / l.pairs) * l.chunks_x;
+    const long long tile = l.tiles_x > l.whole && l.chunks_x > l.chunks_w ? l.chunks_x : l.chunks_w, part = tile < run ? tile : run;
+    return own > part ? own : part;
+}
+
 // G and U: 128 hidden units a tile of 256 rows for a pair of blocks; where that leaves half of the SMs without work, tiles of 128 rows and 64 units, or 32
 // where those still do.  Forward, bf16 (us with 128, 64, 32 units): 512 x 192 x 512 5.8, 4.4, 3.9; 768 x 320 x 1280 6.5, 5.0, 6.0; 1536 x 320 x 1280 7.2, 7.0, 9.2;
 // 512 x 1024 x 4096 10.7, 12.2, 18.8.  fp32: 256 x 320 x 1280 18.0, 14.5, 13.3; 768 18.9, 16.4, 21.5; 1024 19.8, 24.7, 29.5.
@@ -1104,11 +1214,11 @@ bool make_box_map(CUtensorMap* out, const void* base, int unit, uint64_t zs, uin
               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, GatedMode MODE, int BN> cudaError_t launch_mode(const GatedArgs& a, int blocks, cudaStream_t st) {
+template <typename T, GatedMode MODE, int BN, bool LONG> cudaError_t launch_kernel(const GatedArgs& a, int blocks, cudaStream_t st) {
     using S = GatedShape<T, MODE, BN>;
     static_assert(S::kSmem <= 232448, "shared memory");
     static std::atomic<unsigned long long> done{0};
-    const cudaError_t e = allow_smem(gated_kernel<T, MODE, BN>, done, S::kSmem);
+    const cudaError_t e = allow_smem(gated_kernel<T, MODE, BN, LONG>, done, S::kSmem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
@@ -1122,11 +1232,15 @@ template <typename T, GatedMode MODE, int BN> cudaError_t launch_mode(const Gate
     at[1].val.clusterDim.x = 2; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = S::kPair ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, gated_kernel<T, MODE, BN>, a);
+    return cudaLaunchKernelEx(&cfg, gated_kernel<T, MODE, BN, LONG>, a);
+}
+// `longest`: chunks of the longest sum
+template <typename T, GatedMode MODE, int BN> cudaError_t launch_mode(const GatedArgs& a, int blocks, long long longest, cudaStream_t st) {
+    return longest > GatedTerms<T>::kMost ? launch_kernel<T, MODE, BN, true>(a, blocks, st) : launch_kernel<T, MODE, BN, false>(a, blocks, st);
 }
 template <typename T, GatedMode MODE> cudaError_t launch_projections(const GatedArgs& a, const GatedTiles& t, cudaStream_t st) {
-    if (t.bn == 128) return launch_mode<T, MODE, 128>(a, t.blocks, st);
-    return t.bn == 64 ? launch_mode<T, MODE, 64>(a, t.blocks, st) : launch_mode<T, MODE, 32>(a, t.blocks, st);
+    if (t.bn == 128) return launch_mode<T, MODE, 128>(a, t.blocks, a.chunks, st);
+    return t.bn == 64 ? launch_mode<T, MODE, 64>(a, t.blocks, a.chunks, st) : launch_mode<T, MODE, 32>(a, t.blocks, a.chunks, st);
 }
 
 template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st, int* launches) {
@@ -1208,7 +1322,7 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
             (c.dx && !make_box_map(&a.s[0], c.dx, unit, 1, c.M, c.C)) ||
             (c.dwg && (!make_box_map(&a.s[1], c.dwg, unit, 1, c.F, c.C) || !make_box_map(&a.s[2], c.dwu, unit, 1, c.F, c.C))) ||
             !make_box_map(&a.share, share, 4, 2 * l.pairs, 256, l.n)) return cudaErrorInvalidValue;
-        if ((e = launch_mode<T, kProducts, 128>(a, 2 * l.pairs, st)) != cudaSuccess) return e;
+        if ((e = launch_mode<T, kProducts, 128>(a, 2 * l.pairs, longest_sum(l), st)) != cudaSuccess) return e;
         ++*launches;
         list_shares(&f);
     }

@@ -330,3 +330,28 @@ def test_gradients_of_few_rows_and_many_hidden_units_are_rounded_once(size, name
     for n, t in back.items():
         bound = STEP[dtype] * grads[n].abs() + left[n] + (6e-8 if dtype == "f16" else 0.0)
         assert ((t.double() - grads[n]).abs() <= bound).all(), (n, float(((t.double() - grads[n]).abs() / bound).max()))
+
+
+LONG_SUMS = [("f32", 500000, 32, 128), ("f32", 300, 16384, 256), ("f32", 3000, 1032, 2048), ("f32", 2500, 64, 8192),
+             ("f16", 300, 65536, 256), ("f16", 3000, 16448, 2048), ("bf16", 3000, 16448, 2048), ("bf16", 2500, 64, 65536), ("f16", 3000000, 24, 72), ("bf16", 100, 20000, 64)]
+
+
+@pytest.mark.parametrize("dtype,M,C,F", LONG_SUMS)
+def test_sums_of_any_length(dtype, M, C, F):
+    """Sums in tensor memory lose 3e-8 of themselves a step of 16, towards zero.  fp32: 32 steps, 1e-6, and the pieces' sum in fp32 another 1e-6 (thousands of
+    pieces): the bounds of short sums hold.  16 bits: 1024 steps, 3e-5 in G and in U, which the activation's slope makes 8e-5 of H, beside its rounding."""
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, "gu", seed=6)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    h, grads = reference(x, wg, wu, dh, bg, bu, "silu")
+    args = dict(b_gate=bg, b_up=bu, activation="silu")
+    got = mod.gated(x, wg, wu, **args)
+    assert rel(got, h) <= (REL_FWD if dtype == "f32" else math.hypot(rel(h.to(DT[dtype]), h), 8e-5)), rel(got, h)
+    need = int(mod.lib.agent_attn_gated_workspace_bytes(mod._h, M, C, F, 1))
+    back = mod.gated_backward(x, wg, wu, dh, workspace=torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda"), **args)
+    assert mod.query_status() == 0
+    for n, t in back.items():
+        assert torch.isfinite(t).all() and rel(t, grads[n]) <= REL_BWD[dtype], (n, rel(t, grads[n]))
+    again = mod.gated_backward(x, wg, wu, dh, need_input_grad=False, **args)
+    assert all(torch.equal(again[n], back[n]) for n in again)
+    only = mod.gated_backward(x, wg, wu, dh, need_weight_grads=False, **args)
+    assert torch.equal(only["dx"], back["dx"])
