@@ -421,8 +421,9 @@ typedef struct {
 /* Gradients of agent_attn_gated for d_out = dL/dH (device [rows][hidden], element type).  Both projections are
  * recomputed; nothing has to be saved.  The gradients of the two projections are rounded to the element type, as
  * operands of the products that follow (up to 128 rows they keep what that leaves as a second term), which is why the
- * results have that type and not fp32; the biases' gradients are sums of unrounded numbers.  Sums are fp32, in a
- * fixed order.  Errors as above. */
+ * results have that type and not fp32; the biases' gradients are sums of unrounded numbers.  In f16 they are held
+ * times a power of two where their largest is not in [2, 65504], so that the results have the type's range, whatever
+ * theirs.  Sums are fp32, in a fixed order.  Errors as above. */
 int agent_attn_gated_backward(agent_attn_handle* h, const agent_attn_gate* gate, const void* d_out,
                               const agent_attn_gate_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
 

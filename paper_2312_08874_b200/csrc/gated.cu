@@ -13,7 +13,7 @@
 //              have as many: whole tiles of dX, then a run of the other tiles; a pair writes what it has whole and leaves its share of what it has
 //              not, and gated_finish_kernel adds the shares up in their order.
 // 16-bit operands enter as they are; dG and dU are rounded to the element type, as every operand of a product on the tensor cores is (few rows: and what that
-// leaves as a second term).  fp32: operands are sums of three bf16 terms, six pairs of terms, small ones first.
+// leaves as a second term).  In f16 kGrad is launched twice: the second one ends at once unless dG and dU leave the type's range (gated_scale).  fp32: operands are sums of three bf16 terms, six pairs of terms, small ones first.
 //
 // What bounds it (us of a launch among others; rows x channels x hidden units):
 //   kForward   32768 x 512 x 1368 bf16, SiLU: 88 to 92, 1.0 PFLOP/s.  Tensor pipe 75 % busy (a chunk of 64 takes 600 cycles of 512), clocks under the power
@@ -61,6 +61,8 @@ struct GatedArgs {
     void *out0, *out1;                                 // H; dG and dU: where they are written without staging
     int terms;                                         // kGrad, kProducts of 16-bit elements: of dG and dU (1 or 2)
     float* column;                                     // [slots][2][F]: shares of the column sums of dG and dU, or null
+    float* largest;                                    // f16: [largest_parts] by kGrad's blocks: the largest |dG| and |dU|
+    int largest_parts, again;                          // again: kGrad's second pass, where that is out of f16's range
     int* status;
     alignas(64) CUtensorMap a[2], b[2], x;             // operands; kProducts: a, b of dX (a of the weights, too), x: X
     alignas(64) CUtensorMap s[3], g, w[2], share;      // staged results: H; dG, dU; dX, dWg, dWu; dH; kProducts: dG and dU in boxes of 64 rows; shares of tiles
@@ -149,6 +151,34 @@ template <typename T, int ACT, bool GRAD> __device__ __forceinline__ void activa
         a = fmul2(g, s);
         if (GRAD) da = ffma2(fmul2(a, slope), ffma2(s, both(-1.f), both(1.f)), s);
     }
+}
+// f16: dG and dU leave its range before the results do (an infinity past 65504, fewer bits below 6e-5).  Where their largest lies outside [2, 65504], kGrad runs
+// again and holds them times this power of two, which brings the largest to 2^14 and more, and kProducts divides by it.  From 2 on a row or a hidden unit
+// whose gradients are a thousandth of the usual ones (a 32nd of the largest) keeps all bits.  8192 x 320 x 1280: 57.2 -> 61.2 us for the launch that ends at once
+// and the sizes; scaled by a bound from the inputs (a pass over dH, X and the weights before kGrad): 72.7.  Called by whole warps.
+__device__ __forceinline__ float gated_scale(const float* largest, int parts, int lane) {
+    float m = 0.f;
+    for (int i = lane; i < parts; i += 32) m = fmaxf(m, largest[i]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (m == 0.f || (m >= 2.f && m <= 65504.f)) return 1.f;
+    return exp2f((float)max(-60, min(60, 14 - ilogbf(m))));
+}
+// m and the sizes of N values, of which infinities and NaN do not count
+template <int N> __device__ __forceinline__ float largest_finite(float m, const float (&v)[N]) {
+    static_assert(N % 2 == 0, "pairs");
+    float n = m;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) n = max3(n, fabsf(v[i]), fabsf(v[i + 1]));
+    if (n < INFINITY) return n;
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+        float a = 0.f;
+#pragma unroll
+        for (int k = 0; k < N; ++k) a = k == i ? fabsf(v[k]) : a;      // (no indexed registers)
+        if (a < INFINITY) m = fmaxf(m, a);
+    }
+    return m;
 }
 // f(constant of the activation): the choice is made once a tile, not once a value
 template <typename F> __device__ __forceinline__ void by_activation(int act, F f) {
@@ -345,19 +375,24 @@ template <typename T, GatedMode MODE, int BN, bool LONG> __global__ void __launc
     constexpr int kPairs = GatedTerms<T>::kPairs, kStages = S::kStages;
     constexpr bool PAIR = S::kPair;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ int s_dead;
+    __shared__ int s_dead, s_largest;
     __shared__ uint32_t s_tmem;
+    constexpr bool kScaled = MODE >= kGrad && std::is_same<T, __half>::value;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t rank = PAIR ? cluster_rank() : 0u;
     const int who = PAIR ? blockIdx.x / 2 : blockIdx.x, count = PAIR ? gridDim.x / 2 : gridDim.x;
 
+    if (MODE == kGrad && kScaled && p.again) {
+        pdl_wait_prior();
+        if (gated_scale(p.largest, p.largest_parts, lane) == 1.f) return;      // (all threads of all blocks; what follows waits for this kernel's end)
+    }
     Pipe pp;
     pp.status = p.status;
     pp.dead = &s_dead;
     pp.bars = base;
     if (tid < kBars) mbar_init(pp.bars + 8 * tid, tid >= BAR_READ && tid < BAR_DRAIN ? (PAIR ? 2 : 1) * kEpiWarps : 1u);
-    if (tid == 0) s_dead = 0;
+    if (tid == 0) s_dead = s_largest = 0;
     if (warp <= (kBars - 1) / 32) mbar_fence_init();
     if (warp == kEpiWarps) {
         if (PAIR) tmem_alloc_pair<512>(smem_u32(&s_tmem));
@@ -387,6 +422,7 @@ template <typename T, GatedMode MODE, int BN, bool LONG> __global__ void __launc
     // each and are added in the epilogue, instead of taking turns.  Relative error with one accumulator, with two, and of sums in plain fp32: H of 64 x 640 x 2560
     // 1.2e-6, 0.6e-6, 0.7e-6, its dX 1.1e-6, 0.5e-6, 0.7e-6; dW of 30000 x 64 x 256 1.2e-6, 0.6e-6, 0.8e-6.  It costs H of 1568 x 192 x 512 0.7 of 11.5 us.
     constexpr bool kHalfSums = kPairs > 1;
+    [[maybe_unused]] float scale = 1.f, largest = 0.f;
     Walk<MODE, S::kParts, LONG ? GatedTerms<T>::kMost : 0, GatedTerms<T>::kPiece> walk(p, who, count);
     Work t;
     // 16 bits, LONG: sums in one piece take turns with the accumulators (turn: whose it is next); how often each was in use
@@ -512,6 +548,8 @@ template <typename T, GatedMode MODE, int BN, bool LONG> __global__ void __launc
         // ------------------------------------------------------------------ epilogue
         // warp: 32 rows, and a quarter of a tile's hidden units (kForward, kGrad) or every fourth block of 32 columns
         const int q = warp & 3, quarter = warp >> 2;
+        if constexpr (kScaled)
+            if (MODE == kProducts || p.again) scale = gated_scale(p.largest, p.largest_parts, lane);
         const uint32_t patch = base + S::kOffPatch + warp * S::kPatch;
         const uint32_t read0 = PAIR ? in_block(pipe_bar(pp, BAR_READ), 0) : pipe_bar(pp, BAR_READ), elected = elect_lane();
         int ord = 0;
@@ -685,6 +723,7 @@ template <typename T, GatedMode MODE, int BN, bool LONG> __global__ void __launc
                                 }
                             } else {
                                 uint32_t d[4], o1[4];
+                                [[maybe_unused]] float sizes[16];
                                 ld_matrix4(d, at);
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
@@ -693,11 +732,19 @@ template <typename T, GatedMode MODE, int BN, bool LONG> __global__ void __launc
                                     const float2 dh = unpack2<T>(d[i]);
                                     da = fmul2(fmul2(dh, vv[i]), da);
                                     a = fmul2(dh, a);
-                                    o0[i] = pack2<T>(da.x, da.y);
-                                    o1[i] = pack2<T>(a.x, a.y);
+                                    if constexpr (kScaled) {
+                                        const float2 x = fmul2(da, both(scale)), y = fmul2(a, both(scale));
+                                        o0[i] = pack2<T>(x.x, x.y);
+                                        o1[i] = pack2<T>(y.x, y.y);
+                                        sizes[4 * i] = da.x; sizes[4 * i + 1] = da.y; sizes[4 * i + 2] = a.x; sizes[4 * i + 3] = a.y;
+                                    } else {
+                                        o0[i] = pack2<T>(da.x, da.y);
+                                        o1[i] = pack2<T>(a.x, a.y);
+                                    }
                                     column[0][2 * c + i / 2] = fadd2(column[0][2 * c + i / 2], da);      // (before they are rounded)
                                     column[1][2 * c + i / 2] = fadd2(column[1][2 * c + i / 2], a);
                                 }
+                                if constexpr (kScaled) largest = largest_finite(largest, sizes);
                                 __syncwarp();
                                 st_matrix4(at - mine + other, o1);
                             }
@@ -794,6 +841,15 @@ template <typename T, GatedMode MODE, int BN, bool LONG> __global__ void __launc
                             }
                             if constexpr (MODE == kForward) {
                                 store8<T>(static_cast<T*>(p.out0) + at, v + j);
+                            } else if constexpr (kScaled) {
+                                float x[8], y[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) { x[i] = g[j + i]; y[i] = v[j + i]; }
+                                largest = largest_finite(largest_finite(largest, x), y);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) { x[i] *= scale; y[i] *= scale; }
+                                store_operand8<T>(p.out0, plane, at, x, p.terms > 1);
+                                store_operand8<T>(p.out1, plane, at, y, p.terms > 1);
                             } else {
                                 store_operand8<T>(p.out0, plane, at, g + j, p.terms > 1);
                                 store_operand8<T>(p.out1, plane, at, v + j, p.terms > 1);
@@ -815,6 +871,7 @@ template <typename T, GatedMode MODE, int BN, bool LONG> __global__ void __launc
             }
         } else {
             // boxes of 32 columns and 32 rows, those of a tile in turn by the four warps that share its rows
+            [[maybe_unused]] const float back = 1.f / scale;
             for (; walk.next(t); ++ord) {
                 const int blocks = p.line.n / 32, limit = t.weight ? p.F : p.M;
                 const int in_tile = 128 * rank + 32 * q, row0 = t.weight ? 128 * t.mt + 32 * q : 256 * t.mt + in_tile;
@@ -847,6 +904,10 @@ template <typename T, GatedMode MODE, int BN, bool LONG> __global__ void __launc
                         }
                     }
                     if (b + 4 >= blocks) release(lent);
+                    if constexpr (kScaled) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] *= back;
+                    }
                     store_wait_read<0>();
                     __syncwarp();
                     if (wide) {                                        // rows of 128 bytes
@@ -869,8 +930,15 @@ template <typename T, GatedMode MODE, int BN, bool LONG> __global__ void __launc
             __syncwarp();
         }
     }
+    if constexpr (MODE == kGrad && kScaled) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
+        if (lane == 0) atomicMax(&s_largest, __float_as_int(largest));         // (of numbers that are not negative the order is that of their bits)
+    }
     tc_fence_before_sync();
     __syncthreads();
+    if constexpr (MODE == kGrad && kScaled)
+        if (tid == 0 && !p.again) p.largest[blockIdx.x] = __int_as_float(s_largest);
     if (PAIR) {
         cluster_sync();                                               // the other block's instructions read this one's memory
         if (warp == kEpiWarps) tmem_dealloc_pair<512>(pp.tmem);
@@ -1187,8 +1255,8 @@ int gradient_terms(int M) { return M <= 128 ? 2 : 1; }
 // Tiles of the projections of a call
 GatedTiles call_tiles(int dtype, int M, int F, bool backward, int sm_count) { return plan_tiles(M, F, backward && dtype != kF32 && gradient_terms(M) > 1, sm_count); }
 
-// Workspace: terms of X, Wg, Wu (fp32) | dG | dU | shares of tiles of dX and the weights' gradients, of the column sums
-struct GatedWs { size_t x, wg, wu, dg, du, share, db, total; };
+// Workspace: terms of X, Wg, Wu (fp32) | dG | dU | shares of tiles of dX and the weights' gradients, of the column sums | largest of dG and dU (f16)
+struct GatedWs { size_t x, wg, wu, dg, du, share, db, largest, total; };
 GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count) {
     GatedWs w;
     size_t at = 0;
@@ -1197,7 +1265,7 @@ GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count
     w.x = take(terms * M * C * 2);
     w.wg = take(terms * F * C * 2);
     w.wu = take(terms * F * C * 2);
-    w.dg = w.du = w.share = w.db = at;
+    w.dg = w.du = w.share = w.db = w.largest = at;
     if (backward) {
         const GatedTiles t = call_tiles(dtype, M, F, true, sm_count);
         const size_t planes = (dtype == kF32 ? 3 : gradient_terms(M)) * (size_t)M * F * 2;
@@ -1206,6 +1274,7 @@ GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count
         w.share = take((size_t)(sm_count / 2) * 2 * 256 * plan_line(M, C, F, sm_count).n * 4);
         const size_t slots = dtype != kF32 && t.bn == 128 ? column_slots(t) : (M + 31) / 32;
         w.db = take(slots * 2 * F * 4);
+        w.largest = take(dtype == kF16 ? t.blocks * 4 : 0);
     }
     w.total = at;
     return w;
@@ -1256,7 +1325,8 @@ template <typename T, GatedMode MODE> cudaError_t launch_projections(const Gated
 template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st, int* launches) {
     constexpr int kTerms = GatedTerms<T>::kTerms;
     constexpr bool kWide = sizeof(T) == 4;
-    const GatedWs w = gated_layout(kWide ? kF32 : kBF16, c.M, c.C, c.F, c.dh != nullptr, c.sm_count);
+    constexpr int kType = kWide ? kF32 : Elem<T>::kIsBf16 ? kBF16 : kF16;
+    const GatedWs w = gated_layout(kType, c.M, c.C, c.F, c.dh != nullptr, c.sm_count);
     char* ws = static_cast<char*>(c.ws);
     const void *x = c.x, *wg = c.wg, *wu = c.wu;
     cudaError_t e;
@@ -1268,7 +1338,7 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
         };
         return c.M == 1 ? few(gated_few_kernel<T, 1>, 1) : c.M <= 4 ? few(gated_few_kernel<T, 4>, 4) : few(gated_few_kernel<T, 8>, 8);
     }
-    if (!c.dh && small_forward(kWide ? kF32 : kBF16, c.M, c.C, c.F)) {
+    if (!c.dh && small_forward(kType, c.M, c.C, c.F)) {
         static std::atomic<unsigned long long> done{0};
         if ((e = allow_smem(gated_small_kernel, done, kSmallSmem)) != cudaSuccess) return e;
         ++*launches;
@@ -1289,13 +1359,15 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     a.M = c.M; a.C = c.C; a.F = c.F; a.act = c.act;
     a.bg = c.bg; a.bu = c.bu; a.dh = c.dh;
     a.status = c.status;
-    const GatedTiles t = call_tiles(kWide ? kF32 : kBF16, c.M, c.F, c.dh != nullptr, c.sm_count);
+    const GatedTiles t = call_tiles(kType, c.M, c.F, c.dh != nullptr, c.sm_count);
     a.tiles_m = t.tiles_m; a.tiles_n = t.tiles_n; a.chunks = (c.C + 63) / 64;
     a.out0 = c.dh ? ws + w.dg : static_cast<char*>(c.h);
     a.out1 = ws + w.du;
     a.terms = kWide ? kTerms : gradient_terms(c.M);
     float* column = reinterpret_cast<float*>(ws + w.db);
     a.column = c.dbg ? column : nullptr;
+    a.largest = reinterpret_cast<float*>(ws + w.largest);
+    a.largest_parts = t.blocks;
     if (!make_map_3d_u16(&a.a[0], x, kTerms, c.M, c.C, 128) || !make_map_3d_u16(&a.b[0], wg, kTerms, c.F, c.C, t.bn) || !make_map_3d_u16(&a.b[1], wu, kTerms, c.F, c.C, t.bn)) return cudaErrorInvalidValue;
     if (!kWide && t.bn == 128) {
         if (!make_box_map(&a.s[0], a.out0, 2, 1, c.M, c.F)) return cudaErrorInvalidValue;
@@ -1305,6 +1377,11 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     if (e != cudaSuccess) return e;
     ++*launches;
     if (!c.dh) return cudaSuccess;
+    if (kType == kF16 && (c.dx || c.dwg)) {                // (biases sum numbers that are not rounded)
+        a.again = 1;
+        if ((e = launch_projections<T, kGrad>(a, t, st)) != cudaSuccess) return e;
+        ++*launches;
+    }
 
     const void *dg = ws + w.dg, *du = ws + w.du;
     FinishArgs f;

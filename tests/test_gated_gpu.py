@@ -355,3 +355,47 @@ def test_sums_of_any_length(dtype, M, C, F):
     assert all(torch.equal(again[n], back[n]) for n in again)
     only = mod.gated_backward(x, wg, wu, dh, need_weight_grads=False, **args)
     assert torch.equal(only["dx"], back["dx"])
+
+
+@pytest.mark.parametrize("M,C,F", [(9, 40, 136), (100, 320, 1280), (700, 320, 1280), (8192, 320, 1280)])
+@pytest.mark.parametrize("kind", ["large", "small"])
+def test_half_precision_gradients_over_their_whole_range(kind, M, C, F):
+    """f16 results in range out of gradients of the projections that are not: far past 65504, or so small that f16 has a few bits left of them.  The bound of other
+    magnitudes, and half a step of the smallest results (3e-8)."""
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, "f16", "gu", seed=M)
+    if kind == "large":
+        x, wg, wu, dh, bu = x * 1e-3, (wg.float() * 2e-3).half(), (wu.float() * 2e-3).half(), dh * 3000, bu * 100 + 30
+    else:
+        dh = (dh.float() * 1e-6).half()
+    mod = AgentAttention(1, 1, 64, 1, 1, torch.float16)
+    _, grads = reference(x, wg, wu, dh, bg, bu, "gelu")
+    back = mod.gated_backward(x, wg, wu, dh, b_gate=bg, b_up=bu, activation="gelu")
+    assert mod.query_status() == 0
+    if kind == "large":
+        g, u = x.double() @ wg.double().T + bg.double(), x.double() @ wu.double().T + bu.double()
+        assert float((dh.double() * u * act("gelu", g)).abs().max()) > 2e5                 # (what used to be infinite)
+    for n, t in back.items():
+        fits = grads[n].half().isfinite()
+        clear = (grads[n].abs() / 65520 - 1).abs() > REL_BWD["f16"]                           # (not beside the first number that rounds to an infinity)
+        assert torch.equal(t.isinf()[clear], ~fits[clear]) and (n[1] == "b" or fits.float().mean() > 0.99)
+        fits &= t.isfinite()
+        err, ref = (t.double() - grads[n])[fits], grads[n][fits]
+        assert float(err.norm()) <= REL_BWD["f16"] * float(ref.norm()) + 3e-8 * fits.sum().item() ** 0.5, (n, float(err.norm() / ref.norm()))
+
+
+def test_half_precision_gradients_beside_extreme_rows():
+    """Rows of zeros, an infinite gradient or a NaN in an input leave the small gradients of the other rows what they are; no gradient at all gives zeros."""
+    M, C, F = 300, 64, 136
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, "f16", "gu", seed=1)
+    dh = (dh.float() * 1e-6).half()
+    mod = AgentAttention(1, 1, 64, 1, 1, torch.float16)
+    back = mod.gated_backward(x, wg, wu, torch.zeros_like(dh), b_gate=bg, b_up=bu)
+    assert all((t == 0).all() for t in back.values())
+    x[7], dh[8], dh[100, 3], x[200, 5] = 0, 0, math.inf, math.nan
+    rows = torch.ones(M, dtype=torch.bool, device="cuda")
+    rows[[100, 200]] = False
+    _, grads = reference(x[rows], wg, wu, dh[rows], bg, bu, "silu")
+    back = mod.gated_backward(x, wg, wu, dh, b_gate=bg, b_up=bu)
+    err = back["dx"][rows].double() - grads["dx"]
+    assert float(err.norm()) <= REL_BWD["f16"] * float(grads["dx"].norm()) + 3e-8 * err.numel() ** 0.5
+    assert not back["dx"][100].isfinite().any() and back["dx"][200].isnan().all()
