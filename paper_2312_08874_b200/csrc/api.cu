@@ -800,7 +800,7 @@ int agent_attn_rotate_backward(agent_attn_handle* h, const float* dQ_out, const 
 static bool gate_shape(int rows, int channels, int hidden) {
     return rows <= (1 << 24) && channels <= 65536 && hidden <= 65536 && channels % 8 == 0 && hidden % 8 == 0;
 }
-static int gate_call(agent_attn_handle* h, const agent_attn_gate* g, void* workspace, size_t workspace_bytes, bool backward, GatedCall* c) {
+static int gate_call(agent_attn_handle* h, const agent_attn_gate* g, void* workspace, size_t workspace_bytes, bool backward, bool two_terms, GatedCall* c) {
     if (!g || !g->x || !g->w_gate || !g->w_up) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
     if (g->rows <= 0 || g->channels <= 0 || g->hidden <= 0)
         return fail(h, AA_ERR_INVALID_ARG, "rows, channels and hidden size must be positive (%d, %d, %d)", g->rows, g->channels, g->hidden);
@@ -809,13 +809,14 @@ static int gate_call(agent_attn_handle* h, const agent_attn_gate* g, void* works
     if (g->activation < AA_ACT_SILU || g->activation > AA_ACT_GELU_TANH) return fail(h, AA_ERR_UNSUPPORTED, "unknown activation %d", g->activation);
     if (misaligned(g->x) || misaligned(g->w_gate) || misaligned(g->w_up) || misaligned(g->b_gate) || misaligned(g->b_up))
         return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
-    const size_t need = gated_bytes(h->cfg.dtype, g->rows, g->channels, g->hidden, backward, h->sm_count);
+    const size_t need = gated_bytes(h->cfg.dtype, g->rows, g->channels, g->hidden, backward, two_terms, h->sm_count);
     if (need && (!workspace || workspace_bytes < need)) return fail(h, AA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
     if (need && misaligned(workspace)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
     memset(c, 0, sizeof(*c));
     c->M = g->rows; c->C = g->channels; c->F = g->hidden; c->act = g->activation; c->sm_count = h->sm_count;
     c->x = g->x; c->wg = g->w_gate; c->wu = g->w_up; c->bg = g->b_gate; c->bu = g->b_up;
     c->ws = workspace;
+    c->two_terms = two_terms;
     c->status = h->d_status;
     return AA_OK;
 }
@@ -831,14 +832,14 @@ static int run_gate(agent_attn_handle* h, const GatedCall& c, void* stream) {
 
 size_t agent_attn_gated_workspace_bytes(const agent_attn_handle* h, int rows, int channels, int hidden, int backward) {
     if (!h || rows <= 0 || channels <= 0 || hidden <= 0 || !gate_shape(rows, channels, hidden)) return 0;
-    return gated_bytes(h->cfg.dtype, rows, channels, hidden, backward != 0, h->sm_count);
+    return gated_bytes(h->cfg.dtype, rows, channels, hidden, backward != 0, backward == AA_GATED_TWO_TERMS, h->sm_count);
 }
 
 int agent_attn_gated(agent_attn_handle* h, const agent_attn_gate* gate, void* out, void* workspace, size_t workspace_bytes, void* stream) {
     if (!h) return AA_ERR_INVALID_ARG;
     h->err[0] = 0;
     GatedCall c;
-    if (int rc = gate_call(h, gate, workspace, workspace_bytes, false, &c)) return rc;
+    if (int rc = gate_call(h, gate, workspace, workspace_bytes, false, false, &c)) return rc;
     if (!out) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
     if (misaligned(out)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
     if (out == c.x || out == c.wg || out == c.wu) return fail(h, AA_ERR_INVALID_ARG, "out aliases an input");
@@ -851,8 +852,9 @@ int agent_attn_gated_backward(agent_attn_handle* h, const agent_attn_gate* gate,
     if (!h) return AA_ERR_INVALID_ARG;
     h->err[0] = 0;
     GatedCall c;
-    if (int rc = gate_call(h, gate, workspace, workspace_bytes, true, &c)) return rc;
-    if (!d_out || !grads) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (!grads) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (int rc = gate_call(h, gate, workspace, workspace_bytes, true, grads->two_terms != 0, &c)) return rc;
+    if (!d_out) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
     if (!grads->dw_gate != !grads->dw_up || !grads->db_gate != !grads->db_up) return fail(h, AA_ERR_INVALID_ARG, "gradients of weights and of biases come in pairs");
     if (!grads->dx && !grads->dw_gate && !grads->db_gate) return fail(h, AA_ERR_INVALID_ARG, "no gradient asked for");
     const void* outs[] = {grads->dx, grads->dw_gate, grads->dw_up, grads->db_gate, grads->db_up};

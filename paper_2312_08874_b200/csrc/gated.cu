@@ -1251,13 +1251,15 @@ int column_slots(const GatedTiles& t) {
 // 16-bit elements: dG and dU as one term, rounded to the element type, which makes the error of dX and the weights' gradients 1.4 times that of their own
 // rounding; over few rows it is more by chance (up to 2.1 times with one row, 1.6 with 32, 1.5 with 128), and there two terms keep it at 1.  (64 x 320 x 1280
 // bf16 17.7 and 19.3 us, 128 x 1024 x 8192 46.6 and 50.5, 128 x 2048 x 11008 f16 107 and 116; 256 x 640 x 2560 25.6 and 30.4, which one term has.)
-int gradient_terms(int M) { return M <= 128 ? 2 : 1; }
+// A caller may ask for two over any number of rows, whose G and U then come in tiles of 64: 8192 x 320 x 1280 f16 59 and
+// 132 us, 25088 x 192 x 512 bf16 53 and 132.
+int gradient_terms(int M, bool two) { return two || M <= 128 ? 2 : 1; }
 // Tiles of the projections of a call
-GatedTiles call_tiles(int dtype, int M, int F, bool backward, int sm_count) { return plan_tiles(M, F, backward && dtype != kF32 && gradient_terms(M) > 1, sm_count); }
+GatedTiles call_tiles(int dtype, int M, int F, bool backward, bool two, int sm_count) { return plan_tiles(M, F, backward && dtype != kF32 && gradient_terms(M, two) > 1, sm_count); }
 
 // Workspace: terms of X, Wg, Wu (fp32) | dG | dU | shares of tiles of dX and the weights' gradients, of the column sums | largest of dG and dU (f16)
 struct GatedWs { size_t x, wg, wu, dg, du, share, db, largest, total; };
-GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count) {
+GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, bool two, int sm_count) {
     GatedWs w;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
@@ -1267,8 +1269,8 @@ GatedWs gated_layout(int dtype, int M, int C, int F, bool backward, int sm_count
     w.wu = take(terms * F * C * 2);
     w.dg = w.du = w.share = w.db = w.largest = at;
     if (backward) {
-        const GatedTiles t = call_tiles(dtype, M, F, true, sm_count);
-        const size_t planes = (dtype == kF32 ? 3 : gradient_terms(M)) * (size_t)M * F * 2;
+        const GatedTiles t = call_tiles(dtype, M, F, true, two, sm_count);
+        const size_t planes = (dtype == kF32 ? 3 : gradient_terms(M, two)) * (size_t)M * F * 2;
         w.dg = take(planes);
         w.du = take(planes);
         w.share = take((size_t)(sm_count / 2) * 2 * 256 * plan_line(M, C, F, sm_count).n * 4);
@@ -1326,7 +1328,7 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     constexpr int kTerms = GatedTerms<T>::kTerms;
     constexpr bool kWide = sizeof(T) == 4;
     constexpr int kType = kWide ? kF32 : Elem<T>::kIsBf16 ? kBF16 : kF16;
-    const GatedWs w = gated_layout(kType, c.M, c.C, c.F, c.dh != nullptr, c.sm_count);
+    const GatedWs w = gated_layout(kType, c.M, c.C, c.F, c.dh != nullptr, c.two_terms, c.sm_count);
     char* ws = static_cast<char*>(c.ws);
     const void *x = c.x, *wg = c.wg, *wu = c.wu;
     cudaError_t e;
@@ -1359,11 +1361,11 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
     a.M = c.M; a.C = c.C; a.F = c.F; a.act = c.act;
     a.bg = c.bg; a.bu = c.bu; a.dh = c.dh;
     a.status = c.status;
-    const GatedTiles t = call_tiles(kType, c.M, c.F, c.dh != nullptr, c.sm_count);
+    const GatedTiles t = call_tiles(kType, c.M, c.F, c.dh != nullptr, c.two_terms, c.sm_count);
     a.tiles_m = t.tiles_m; a.tiles_n = t.tiles_n; a.chunks = (c.C + 63) / 64;
     a.out0 = c.dh ? ws + w.dg : static_cast<char*>(c.h);
     a.out1 = ws + w.du;
-    a.terms = kWide ? kTerms : gradient_terms(c.M);
+    a.terms = kWide ? kTerms : gradient_terms(c.M, c.two_terms);
     float* column = reinterpret_cast<float*>(ws + w.db);
     a.column = c.dbg ? column : nullptr;
     a.largest = reinterpret_cast<float*>(ws + w.largest);
@@ -1422,7 +1424,7 @@ template <typename T> cudaError_t run_gated(const GatedCall& c, cudaStream_t st,
 
 }  // namespace
 
-size_t gated_bytes(int dtype, int M, int C, int F, bool backward, int sm_count) { return gated_layout(dtype, M, C, F, backward, sm_count).total; }
+size_t gated_bytes(int dtype, int M, int C, int F, bool backward, bool two_terms, int sm_count) { return gated_layout(dtype, M, C, F, backward, two_terms, sm_count).total; }
 
 cudaError_t launch_gated(int dtype, const GatedCall& c, cudaStream_t st, int* launches) {
     switch (dtype) {

@@ -356,10 +356,11 @@ struct GatedCall {
     void* h;                                  // [M][F]
     const void* dh;                           // gradient of h: the backward pass; null: the forward pass
     void *dx, *dwg, *dwu, *dbg, *dbu;         // in the element type; dx, the weights' pair, the biases' pair may be null
+    bool two_terms;                           // of dG and dU, over any number of rows (16-bit types)
     void* ws;                                 // gated_bytes
     int* status;
 };
-size_t gated_bytes(int dtype, int M, int C, int F, bool backward, int sm_count);
+size_t gated_bytes(int dtype, int M, int C, int F, bool backward, bool two_terms, int sm_count);
 cudaError_t launch_gated(int dtype, const GatedCall& c, cudaStream_t st, int* launches);
 
 }  // namespace aa

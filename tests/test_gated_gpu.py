@@ -399,3 +399,29 @@ def test_half_precision_gradients_beside_extreme_rows():
     err = back["dx"][rows].double() - grads["dx"]
     assert float(err.norm()) <= REL_BWD["f16"] * float(grads["dx"].norm()) + 3e-8 * err.numel() ** 0.5
     assert not back["dx"][100].isfinite().any() and back["dx"][200].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("M,C,F", [(129, 136, 264), (700, 64, 256), (8192, 320, 1280), (5200, 520, 1032)])
+def test_two_terms_on_request(M, C, F, dtype):
+    """Over any number of rows, the bound of `test_gradients_of_few_rows_are_rounded_once`."""
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, "gu", seed=M)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    _, grads = reference(x, wg, wu, dh, bg, bu, "gelu")
+    need = int(mod.lib.agent_attn_gated_workspace_bytes(mod._h, M, C, F, 2))
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    args = dict(b_gate=bg, b_up=bu, activation="gelu")
+    back = mod.gated_backward(x, wg, wu, dh, two_terms=True, workspace=ws, **args)
+    assert mod.query_status() == 0
+    eg, eu = hidden_errors(x, wg, wu, dh, bg, bu, "gelu", 2.0 ** -16 + 1e-5, 6e-8 if dtype == "f16" else 0.0)
+    xa = x.double().abs()
+    left = dict(dx=eg @ wg.double().abs() + eu @ wu.double().abs(), dw_gate=eg.T @ xa, dw_up=eu.T @ xa, db_gate=eg.sum(0), db_up=eu.sum(0))
+    for n, t in back.items():
+        bound = STEP[dtype] * grads[n].abs() + left[n] + (6e-8 if dtype == "f16" else 0.0)
+        assert ((t.double() - grads[n]).abs() <= bound).all(), (n, float(((t.double() - grads[n]).abs() / bound).max()))
+        assert rel(t, grads[n]) <= 1.05 * rel(grads[n].to(DT[dtype]), grads[n])
+    one = mod.gated_backward(x, wg, wu, dh, **args)
+    assert rel(one["dx"], grads["dx"]) > 1.2 * rel(back["dx"], grads["dx"])              # (what it is for)
+    with pytest.raises(AgentAttnError) as e:                                             # the workspace of one term is too small
+        mod.gated_backward(x, wg, wu, dh, two_terms=True, workspace=torch.empty(int(mod.lib.agent_attn_gated_workspace_bytes(mod._h, M, C, F, 1)), dtype=torch.uint8, device="cuda"), **args)
+    assert e.value.status == 3
