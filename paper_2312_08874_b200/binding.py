@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import warnings
 from typing import Optional
 
 import torch
@@ -668,11 +669,13 @@ class AgentAttention:
         return out
 
     def gated_backward(self, x, w_gate, w_up, d_out, b_gate=None, b_up=None, activation: str = "silu", need_input_grad: bool = True,
-                       need_weight_grads: bool = True, two_terms: bool = False, workspace=None, stream=None) -> dict:
+                       need_weight_grads: bool = True, two_terms: bool = False, need_bias_grads: Optional[bool] = None, workspace=None, stream=None) -> dict:
         """`agent_attn_gated_backward`: gradients of `gated` for the upstream gradient `d_out`, in the element type.
 
         `two_terms` (16-bit types): the projections' gradients are not rounded to the element type on the way, so that each result is
-        rounded once; some 2.4 times the time.  Returns a dict with `dx`, `dw_gate`, `dw_up` and, where both biases are given, `db_gate`, `db_up`.
+        rounded once; some 2.4 times the time.  Returns a dict with `dx`, `dw_gate`, `dw_up` and
+        `db_gate`, `db_up`: by default with the weights' gradients and only where both biases are given (else a warning);
+        `need_bias_grads=True` returns that of each bias that is given, `False` none.
         """
         gate = self._gate(x, w_gate, w_up, b_gate, b_up, activation)
         self._chk_tensor(d_out, x.shape[:-1] + (gate.hidden,), "d_out")
@@ -681,9 +684,16 @@ class AgentAttention:
             g["dx"] = torch.empty_like(x)
         if need_weight_grads:
             g["dw_gate"], g["dw_up"] = torch.empty_like(w_gate), torch.empty_like(w_up)
-            if b_gate is not None and b_up is not None:
-                g["db_gate"], g["db_up"] = torch.empty_like(b_gate), torch.empty_like(b_up)
-        grads = AgentAttnGateGrads(_ptr(g.get("dx")), _ptr(g.get("dw_gate")), _ptr(g.get("dw_up")), _ptr(g.get("db_gate")), _ptr(g.get("db_up")), int(two_terms))
+        db = (None, None)
+        given = (b_gate is not None) + (b_up is not None)
+        if need_bias_grads is None:
+            need_bias_grads = need_weight_grads and given == 2
+            if need_weight_grads and given == 1:
+                warnings.warn("gated_backward: the gradient of a bias without the other one is returned with need_bias_grads=True only", stacklevel=2)
+        if need_bias_grads and given:                      # (the library sums both)
+            db = torch.empty_like(b_up if b_gate is None else b_gate), torch.empty_like(b_gate if b_up is None else b_up)
+            g.update((n, t) for n, t, b in zip(("db_gate", "db_up"), db, (b_gate, b_up)) if b is not None)
+        grads = AgentAttnGateGrads(_ptr(g.get("dx")), _ptr(g.get("dw_gate")), _ptr(g.get("dw_up")), _ptr(db[0]), _ptr(db[1]), int(two_terms))
         ws = self._gate_workspace(gate, 2 if two_terms else 1, workspace, stream)
         self._check(self.lib.agent_attn_gated_backward(self._h, ctypes.byref(gate), _ptr(d_out), ctypes.byref(grads), _ptr(ws),
                                                        0 if ws is None else ws.numel(), _stream_ptr(stream)))

@@ -425,3 +425,24 @@ def test_two_terms_on_request(M, C, F, dtype):
     with pytest.raises(AgentAttnError) as e:                                             # the workspace of one term is too small
         mod.gated_backward(x, wg, wu, dh, two_terms=True, workspace=torch.empty(int(mod.lib.agent_attn_gated_workspace_bytes(mod._h, M, C, F, 1)), dtype=torch.uint8, device="cuda"), **args)
     assert e.value.status == 3
+
+
+@pytest.mark.parametrize("dtype,M,C,F", [("f32", 63, 72, 200), ("bf16", 5, 40, 136), ("f16", 700, 64, 256), ("bf16", 9473, 136, 320)])
+def test_gradient_of_a_bias_alone(dtype, M, C, F):
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, dtype, "gu", seed=3)
+    mod = AgentAttention(1, 1, 64, 1, 1, DT[dtype])
+    for name, args in (("db_gate", dict(b_gate=bg)), ("db_up", dict(b_up=bu))):
+        _, grads = reference(x, wg, wu, dh, args.get("b_gate"), args.get("b_up"), "gelu")
+        with pytest.warns(UserWarning, match="need_bias_grads"):
+            silent = mod.gated_backward(x, wg, wu, dh, activation="gelu", **args)
+        back = mod.gated_backward(x, wg, wu, dh, activation="gelu", need_bias_grads=True, **args)
+        assert set(back) == {"dx", "dw_gate", "dw_up", name} and rel(back[name], grads[name]) <= REL_BWD[dtype]
+        assert all(torch.equal(back[n], t) for n, t in silent.items())
+        only = mod.gated_backward(x, wg, wu, dh, activation="gelu", need_bias_grads=True, need_input_grad=False, need_weight_grads=False, **args)
+        assert list(only) == [name] and torch.equal(only[name], back[name])
+    both = dict(b_gate=bg, b_up=bg)                          # one tensor for both is two biases
+    _, grads = reference(x, wg, wu, dh, bg, bg, "silu")
+    back = mod.gated_backward(x, wg, wu, dh, **both)
+    assert all(rel(back[n], grads[n]) <= REL_BWD[dtype] for n in ("db_gate", "db_up"))
+    assert set(mod.gated_backward(x, wg, wu, dh, need_bias_grads=False, **both)) == {"dx", "dw_gate", "dw_up"}
+    assert set(mod.gated_backward(x, wg, wu, dh, need_bias_grads=True)) == {"dx", "dw_gate", "dw_up"}
