@@ -19,6 +19,7 @@ AA_F32, AA_BF16, AA_F16 = 0, 1, 2
 AA_PATH_AUTO, AA_PATH_SIMT, AA_PATH_UNFUSED, AA_PATH_QUEUE = 0, 1, 2, 3
 STATUS_NAMES = {0: "AA_OK", 1: "AA_ERR_INVALID_ARG", 2: "AA_ERR_UNSUPPORTED", 3: "AA_ERR_WORKSPACE",
                 4: "AA_ERR_CUDA", 5: "AA_ERR_TIMEOUT"}
+_INT_MAX = 0x7fffffff                  # ctypes cuts larger numbers off without a word
 _ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 _DTYPES = {torch.float32: AA_F32, torch.bfloat16: AA_BF16, torch.float16: AA_F16}
 
@@ -200,12 +201,12 @@ class Rotary:
         if positions is not None:
             if positions.dim() != 3 or positions.shape[2] != axes or positions.dtype is not torch.float32 or not positions.is_cuda or not positions.is_contiguous():
                 raise ValueError(f"positions: expected a contiguous cuda float32 tensor [B or 1, N, {axes}], got {tuple(positions.shape)} {positions.dtype} on {positions.device}")
-        elif extent is None or len(extent) != axes:
-            raise ValueError(f"extent: expected {axes} values, got {extent}")
+        elif extent is None or len(extent) != axes or any(not 0 < e <= _INT_MAX for e in extent):
+            raise ValueError(f"extent: expected {axes} positive values of 32 bits, got {extent}")
         self.freq, self.positions, self.channels, self.axes = freq, positions, channels, axes
         self.extent = (1,) * axes if extent is None else tuple(int(e) for e in extent)
         self._batch = 0 if positions is None else positions.shape[0]
-        self._c = AgentAttnRotary(axes, (ctypes.c_int * 3)(*self.extent), (ctypes.c_int * 3)(*channels), int(pairs), freq.data_ptr(), _ptr(positions),
+        self._c = AgentAttnRotary(axes, (ctypes.c_int * 3)(*(self.extent if positions is None else ())), (ctypes.c_int * 3)(*channels), int(pairs), freq.data_ptr(), _ptr(positions),
                                   positions.shape[1] * axes if self._batch > 1 else 0)
 
     @staticmethod
@@ -541,6 +542,12 @@ class AgentAttention:
             got = self._strides[key] = (ctypes.c_longlong * 3)(*(s if n > 1 else self.head_dim for n, s in zip(shape, strides[:3])))
         return got
 
+    def _tokens(self, t: torch.Tensor) -> int:
+        N = t.shape[2] if t.dim() == 4 else 0
+        if N > self.cfg.max_tokens:                        # (the library's count has 32 bits)
+            raise AgentAttnError(2, f"N={N} exceeds the handle's max_tokens={self.cfg.max_tokens}")
+        return N
+
     def _norm(self, q_gain, k_gain, eps):
         if eps is None:
             if q_gain is not None or k_gain is not None:
@@ -561,7 +568,7 @@ class AgentAttention:
         some = q if q is not None else k
         if some is None:
             raise ValueError("q or k is required")
-        N = some.shape[2] if some.dim() == 4 else 0
+        N = self._tokens(some)
         sin = self._chk_views(("q", "k"), (q, k), N, self.dtype)
         if rotary is not None:
             rotary._check(self.batch, N)
@@ -586,7 +593,7 @@ class AgentAttention:
         some = dq_out if dq_out is not None else dk_out
         if some is None:
             raise ValueError("dq_out or dk_out is required")
-        N = some.shape[2] if some.dim() == 4 else 0
+        N = self._tokens(some)
         f32 = torch.float32
         sgrad = self._chk_views(("dq_out", "dk_out"), (dq_out, dk_out), N, f32)
         if rotary is not None:
@@ -629,7 +636,7 @@ class AgentAttention:
             self._chk_tensor(b_gate, (F,), "b_gate")
         if b_up is not None:
             self._chk_tensor(b_up, (F,), "b_up")
-        rows = x.numel() // C if C else 0
+        rows, C, F = (min(n, _INT_MAX) for n in (x.numel() // C if C else 0, C, F))            # (which the library refuses)
         return AgentAttnGate(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(b_gate), _ptr(b_up), rows, C, F, _ACTIVATIONS[activation])
 
     def _gate_workspace(self, gate, backward: int, workspace, stream):

@@ -1,6 +1,10 @@
 """Host side of the operators around the attention that needs no GPU: null handles at the C ABI, struct layouts."""
 import os
 import re
+from types import SimpleNamespace
+
+import pytest
+import torch
 
 import paper_2312_08874_b200 as pkg
 from paper_2312_08874_b200 import binding
@@ -26,3 +30,22 @@ def test_structs_match_the_header():
         body = re.sub(r"/\*.*?\*/", "", body, flags=re.S)
         fields = [f for line in re.findall(r"(?:int|float|void|long long)\b\*?\s*([^;]+);", body) for f in re.findall(r"\b(\w+)(?:\[\d\])?\s*(?:,|$)", line.strip())]
         assert fields == [f[0] for f in struct._fields_], name
+
+
+def test_sizes_past_32_bits_are_not_cut_off():
+    """2^32 + 4 tokens or rows are not four: the first is refused here, the others reach the library as a number that it refuses."""
+    big = (1 << 32) + 4
+    handle = SimpleNamespace(cfg=SimpleNamespace(max_tokens=16), _chk_tensor=lambda *a: None)
+    with pytest.raises(pkg.AgentAttnError) as e:
+        pkg.AgentAttention._tokens(handle, torch.empty((1, 1, big, 8), device="meta"))
+    assert e.value.status == 2
+    assert pkg.AgentAttention._tokens(handle, torch.empty((1, 1, 16, 8), device="meta")) == 16
+    for x, w in ((torch.empty((big, 8), device="meta"), torch.empty((16, 8), device="meta")), (torch.empty((2, 8), device="meta"), torch.empty((big, 8), device="meta")),
+                 (torch.empty((1, big), device="meta"), torch.empty((16, big), device="meta"))):
+        gate = pkg.AgentAttention._gate(handle, x, w, w, None, None, "silu")
+        assert max(gate.rows, gate.channels, gate.hidden) == (1 << 31) - 1
+    freq = SimpleNamespace(shape=(1,), dtype=torch.float32, is_cuda=True, is_contiguous=lambda: True, data_ptr=lambda: 0, device="cuda")
+    for extent in ((big,), (0,), (-3,)):
+        with pytest.raises(ValueError):
+            pkg.Rotary(freq, (2,), extent)
+    assert list(pkg.Rotary(freq, (2,), (16,))._c.extent)[:1] == [16]
