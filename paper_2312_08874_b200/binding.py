@@ -214,7 +214,9 @@ class Rotary:
         """theta ** (-i / pairs) for pair i of each axis."""
         return torch.tensor([theta ** (-i / (c // 2)) for c in channels for i in range(c // 2)], dtype=torch.float32, device=torch.device("cuda", device))
 
-    def _check(self, batch: int, n_tokens: int):
+    def _check(self, batch: int, n_tokens: int, device: int):
+        if self.freq.get_device() != device or (self.positions is not None and self.positions.get_device() != device):
+            raise ValueError(f"rotary: expected freq and positions on cuda:{device}, got {self.freq.device}{'' if self.positions is None else f' and {self.positions.device}'}")
         if self.positions is not None and (self.positions.shape[1] != n_tokens or self._batch not in (1, batch)):
             raise ValueError(f"positions: expected [{batch} or 1, {n_tokens}, {self.axes}], got {tuple(self.positions.shape)}")
 
@@ -229,7 +231,7 @@ class AgentAttention:
         self.cfg = AgentAttnConfig(batch, heads, head_dim, max_tokens, max_agents, _DTYPES[dtype],
                                    scale1, scale2, device, path)
         self.dtype = dtype
-        self.device = torch.device("cuda", device)
+        self.device, self._index = torch.device("cuda", device), device
         self.batch, self.heads, self.head_dim = batch, heads, head_dim
         self._h = ctypes.c_void_p()
         rc = self.lib.agent_attn_create(ctypes.byref(self._h), ctypes.byref(self.cfg))
@@ -256,8 +258,8 @@ class AgentAttention:
     def _chk_tensor(self, t: Optional[torch.Tensor], shape, name: str, cuda: bool = True):
         if t is None:
             return
-        if t.shape != shape or t.dtype is not self.dtype or not t.is_contiguous() or t.is_cuda is not cuda:
-            raise ValueError(f"{name}: expected contiguous {'cuda' if cuda else 'cpu'} {self.dtype} tensor of "
+        if t.shape != shape or t.dtype is not self.dtype or not t.is_contiguous() or t.get_device() != (self._index if cuda else -1):
+            raise ValueError(f"{name}: expected contiguous {self.device if cuda else 'cpu'} {self.dtype} tensor of "
                              f"shape {tuple(shape)}, got {tuple(t.shape)} {t.dtype} on {t.device}")
 
     def _scratch_bytes(self, query: str, grid_h: int, grid_w: int, n_agents: int) -> int:
@@ -338,8 +340,8 @@ class AgentAttention:
         for t, nm in ((q, "q"), (k, "k"), (v, "v"), (out, "out")):
             if t is None:
                 continue
-            if t.shape != (B, h, N, d) or t.dtype is not self.dtype or not t.is_cuda or t.stride(3) != 1:
-                raise ValueError(f"{nm}: expected a cuda {self.dtype} view of shape {(B, h, N, d)} with contiguous channels")
+            if t.shape != (B, h, N, d) or t.dtype is not self.dtype or t.get_device() != self._index or t.stride(3) != 1:
+                raise ValueError(f"{nm}: expected a {self.device} {self.dtype} view of shape {(B, h, N, d)} with contiguous channels")
         if q.stride() != k.stride() or q.stride() != v.stride():
             raise ValueError("q, k and v must have the same strides")
         self._chk_tensor(agents, (B, h, n_agents, d), "agents")
@@ -517,8 +519,8 @@ class AgentAttention:
         for name, t in zip(names, tensors):
             if t is None:
                 continue
-            if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
-                raise ValueError(f"{name}: expected a cuda {dtype} view of shape {shape} with contiguous channels, got {tuple(t.shape)} {t.dtype} on {t.device}")
+            if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index:
+                raise ValueError(f"{name}: expected a {self.device} {dtype} view of shape {shape} with contiguous channels, got {tuple(t.shape)} {t.dtype} on {t.device}")
             if not t.is_contiguous():
                 dense = False
         if dense:
@@ -571,7 +573,7 @@ class AgentAttention:
         N = self._tokens(some)
         sin = self._chk_views(("q", "k"), (q, k), N, self.dtype)
         if rotary is not None:
-            rotary._check(self.batch, N)
+            rotary._check(self.batch, N, self._index)
         norm = self._norm(q_gain, k_gain, eps)
         if out is None:
             out, sout = (_dense_like(q), _dense_like(k)), None
@@ -597,7 +599,7 @@ class AgentAttention:
         f32 = torch.float32
         sgrad = self._chk_views(("dq_out", "dk_out"), (dq_out, dk_out), N, f32)
         if rotary is not None:
-            rotary._check(self.batch, N)
+            rotary._check(self.batch, N, self._index)
         norm = self._norm(q_gain, k_gain, eps)
         sin = None
         if norm is not None:
@@ -614,7 +616,9 @@ class AgentAttention:
         for name, gain, grad in (("dq_gain", q_gain, dq_out), ("dk_gain", k_gain, dk_out)):
             if gain is not None and grad is not None:
                 got[name] = torch.empty(self.head_dim, dtype=f32, device=self.device)
-        if norm is not None and workspace is None:
+        if workspace is not None:
+            self._chk_workspace(workspace)
+        elif norm is not None:
             workspace = self._scratch(int(self.lib.agent_attn_rotate_workspace_bytes(self._h)), stream)
         self._check(self.lib.agent_attn_rotate_backward(
             self._h, _ptr(dq_out), _ptr(dk_out), sgrad, _ptr(q), _ptr(k), sin, N, None if rotary is None else ctypes.byref(rotary._c), norm,
@@ -642,6 +646,7 @@ class AgentAttention:
     def _gate_workspace(self, gate, backward: int, workspace, stream):
         """The workspace of a call: the caller's, or a new one where one is needed."""
         if workspace is not None:
+            self._chk_workspace(workspace)
             return workspace
         key = (gate.rows, gate.channels, gate.hidden, backward)
         need = self._bytes.get(key)
@@ -650,6 +655,10 @@ class AgentAttention:
                 self._bytes.clear()
             need = self._bytes[key] = int(self.lib.agent_attn_gated_workspace_bytes(self._h, *key))
         return self._scratch(need, stream)
+
+    def _chk_workspace(self, t: torch.Tensor):
+        if t.dtype is not torch.uint8 or t.get_device() != self._index or not t.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous {self.device} uint8 tensor, got {t.dtype} on {t.device}")
 
     def _scratch(self, nbytes: int, stream) -> Optional[torch.Tensor]:
         """Memory of one call: kept from reuse until `stream` is done with it where that is not the current stream."""

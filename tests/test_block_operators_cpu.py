@@ -49,3 +49,39 @@ def test_sizes_past_32_bits_are_not_cut_off():
         with pytest.raises(ValueError):
             pkg.Rotary(freq, (2,), extent)
     assert list(pkg.Rotary(freq, (2,), (16,))._c.extent)[:1] == [16]
+
+
+class OnDevice:
+    """What the checks look at of a tensor, on any device."""
+
+    def __init__(self, shape, dtype, device):
+        self.shape, self.dtype, self.device = torch.Size(shape), dtype, torch.device("cuda", device) if device >= 0 else torch.device("cpu")
+        self.is_cuda = device >= 0
+
+    def get_device(self):
+        return self.device.index if self.is_cuda else -1
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0
+
+
+def test_tensors_of_another_device_are_refused():
+    """The kernels of a handle run on its device: a pointer of another one (or of the host) never reaches them."""
+    handle = SimpleNamespace(_index=1, device=torch.device("cuda", 1), dtype=torch.float32, batch=1, heads=2, head_dim=8, _strides={}, cfg=SimpleNamespace(max_tokens=4))
+    cls, shape = pkg.AgentAttention, (1, 2, 4, 8)
+    checks = [lambda d: cls._chk_tensor(handle, OnDevice(shape, torch.float32, d), shape, "x"),
+              lambda d: cls._chk_views(handle, ("q", "k"), (OnDevice(shape, torch.float32, 1), OnDevice(shape, torch.float32, d)), 4, torch.float32),
+              lambda d: cls._chk_workspace(handle, OnDevice((64,), torch.uint8, d)),
+              lambda d: pkg.Rotary(OnDevice((1,), torch.float32, d), (2,), (4,))._check(1, 4, handle._index)]
+    for check in checks:
+        check(1)
+        for other in (0, 2, -1):
+            with pytest.raises(ValueError):
+                check(other)
+    cls._chk_tensor(handle, OnDevice(shape, torch.float32, -1), shape, "x", cuda=False)
+    for tensor in (OnDevice((64,), torch.float32, 1), torch.zeros(64, dtype=torch.uint8)):
+        with pytest.raises(ValueError):
+            cls._chk_workspace(handle, tensor)
