@@ -162,8 +162,19 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _dense_like(t: Optional[torch.Tensor]):
-    return None if t is None else torch.empty_like(t, memory_format=torch.contiguous_format)
+def _empty(shape, dtype: torch.dtype, device: torch.device, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Memory that work on `stream` (None: the current one) may write at once: what the current stream's allocator hands out may still be read by earlier
+    work there.  The current stream may use it, too, until it is freed."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _dense_like(t: Optional[torch.Tensor], stream=None):
+    return None if t is None else _empty(t.shape, t.dtype, t.device, stream)
 
 
 # torch.cuda.current_stream() builds a stream object (3.2 us); the raw handle costs 0.1 us
@@ -576,7 +587,7 @@ class AgentAttention:
             rotary._check(self.batch, N, self._index)
         norm = self._norm(q_gain, k_gain, eps)
         if out is None:
-            out, sout = (_dense_like(q), _dense_like(k)), None
+            out, sout = (_dense_like(q, stream), _dense_like(k, stream)), None
         else:
             if any((t is None) != (o is None) for t, o in zip((q, k), out)):
                 raise ValueError("out: expected a tensor for each of q and k that is given")
@@ -607,7 +618,7 @@ class AgentAttention:
                 raise ValueError("the gradient of a norm needs q and k")
             sin = self._chk_views(("q", "k"), (q, k), N, self.dtype)
         if out is None:
-            out, sout = (_dense_like(dq_out), _dense_like(dk_out)), None
+            out, sout = (_dense_like(dq_out, stream), _dense_like(dk_out, stream)), None
         else:
             if any((t is None) != (o is None) for t, o in zip((dq_out, dk_out), out)):
                 raise ValueError("out: expected a tensor for each gradient that is given")
@@ -615,7 +626,7 @@ class AgentAttention:
         got = {name: t for name, t in zip(("dq", "dk"), out) if t is not None}
         for name, gain, grad in (("dq_gain", q_gain, dq_out), ("dk_gain", k_gain, dk_out)):
             if gain is not None and grad is not None:
-                got[name] = torch.empty(self.head_dim, dtype=f32, device=self.device)
+                got[name] = _empty(self.head_dim, f32, self.device, stream)
         if workspace is not None:
             self._chk_workspace(workspace)
         elif norm is not None:
@@ -661,13 +672,8 @@ class AgentAttention:
             raise ValueError(f"workspace: expected a contiguous {self.device} uint8 tensor, got {t.dtype} on {t.device}")
 
     def _scratch(self, nbytes: int, stream) -> Optional[torch.Tensor]:
-        """Memory of one call: kept from reuse until `stream` is done with it where that is not the current stream."""
-        if nbytes == 0:
-            return None
-        t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        if stream is not None:
-            t.record_stream(stream)
-        return t
+        """Memory of one call on `stream`."""
+        return _empty(nbytes, torch.uint8, self.device, stream) if nbytes else None
 
     def gated(self, x, w_gate, w_up, b_gate=None, b_up=None, activation: str = "silu", out=None, workspace=None, stream=None) -> torch.Tensor:
         """`agent_attn_gated`: act(x w_gate^T + b_gate) * (x w_up^T + b_up) for x [..., channels] and weights [hidden, channels].
@@ -677,7 +683,7 @@ class AgentAttention:
         gate = self._gate(x, w_gate, w_up, b_gate, b_up, activation)
         shape = x.shape[:-1] + (gate.hidden,)
         if out is None:
-            out = x.new_empty(shape)
+            out = _empty(shape, x.dtype, x.device, stream)
         else:
             self._chk_tensor(out, shape, "out")
         ws = self._gate_workspace(gate, 0, workspace, stream)
@@ -697,9 +703,9 @@ class AgentAttention:
         self._chk_tensor(d_out, x.shape[:-1] + (gate.hidden,), "d_out")
         g = {}
         if need_input_grad:
-            g["dx"] = torch.empty_like(x)
+            g["dx"] = _dense_like(x, stream)
         if need_weight_grads:
-            g["dw_gate"], g["dw_up"] = torch.empty_like(w_gate), torch.empty_like(w_up)
+            g["dw_gate"], g["dw_up"] = _dense_like(w_gate, stream), _dense_like(w_up, stream)
         db = (None, None)
         given = (b_gate is not None) + (b_up is not None)
         if need_bias_grads is None:
@@ -707,7 +713,7 @@ class AgentAttention:
             if need_weight_grads and given == 1:
                 warnings.warn("gated_backward: the gradient of a bias without the other one is returned with need_bias_grads=True only", stacklevel=2)
         if need_bias_grads and given:                      # (the library sums both)
-            db = torch.empty_like(b_up if b_gate is None else b_gate), torch.empty_like(b_gate if b_up is None else b_up)
+            db = tuple(_empty(gate.hidden, self.dtype, self.device, stream) for _ in range(2))
             g.update((n, t) for n, t, b in zip(("db_gate", "db_up"), db, (b_gate, b_up)) if b is not None)
         grads = AgentAttnGateGrads(_ptr(g.get("dx")), _ptr(g.get("dw_gate")), _ptr(g.get("dw_up")), _ptr(db[0]), _ptr(db[1]), int(two_terms))
         ws = self._gate_workspace(gate, 2 if two_terms else 1, workspace, stream)

@@ -76,3 +76,35 @@ def test_example_runs(capsys):
     text = capsys.readouterr().out
     losses = [float(line.split()[-1]) for line in text.splitlines() if line.startswith("step")]
     assert len(losses) == 5 and losses[-1] < losses[0] and "status 0" in text
+
+
+def test_results_on_another_stream_take_no_memory_in_use():
+    """A tensor freed while work of the current stream has yet to read it: a call on another stream does not get its memory for results or workspace."""
+    from paper_2312_08874_b200 import AgentAttention, Rotary
+    M, C, F, B, h, N, d = 512, 320, 1280, 4, 8, 256, 64
+    mod = AgentAttention(B, h, d, N, 1, torch.bfloat16)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x, wg, wu, dh = ((torch.randn(s, generator=gen, device="cuda") * f).bfloat16() for s, f in (((M, C), 1.0), ((F, C), C ** -0.5), ((F, C), C ** -0.5), ((M, F), 1.0)))
+    q, k = (torch.randn((B, h, N, d), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    gq, gk = q.float(), k.float()
+    gain = torch.ones(d, device="cuda").bfloat16()
+    rotary = Rotary(Rotary.frequencies((32, 32)), (32, 32), (16, 16))
+    norm = dict(q_gain=gain, k_gain=gain, eps=1e-6)
+    calls = [(lambda s: [mod.gated(x, wg, wu, stream=s)], [(M, F)]),
+             (lambda s: list(mod.gated_backward(x, wg, wu, dh, stream=s).values()), [(M, C), (F, C), (F, C)]),
+             (lambda s: list(mod.rotate(q, k, rotary, stream=s, **norm)), [(B, h, N, d)] * 2),
+             (lambda s: list(mod.rotate_backward(gq, gk, rotary, q=q, k=k, stream=s, **norm).values()), [(B, h, N, 2 * d)] * 2)]
+    side = torch.cuda.Stream()
+    for call, shapes in calls:
+        want = call(None)
+        victims = [torch.randn(s, device="cuda").bfloat16() for s in shapes for _ in range(2)] + [torch.randn(1 << n, device="cuda").bfloat16() for n in (16, 20, 23)]
+        kept, read = [v.clone() for v in victims], [torch.empty_like(v) for v in victims]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(30_000_000)                        # 15 ms and more, in which the call below ends
+        for r, v in zip(read, victims):
+            r.copy_(v)
+        del v, victims
+        got = call(side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(read, kept)) and all(torch.equal(a, b) for a, b in zip(got, want))
