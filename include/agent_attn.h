@@ -348,8 +348,8 @@ typedef struct {
  *   Q_out, K_out device, strides out_strides (NULL: dense).  Either may be its own input where both have the
  *                same strides (in place: a fused projection's output is prepared where
  *                agent_attn_forward_strided reads it); no other overlap
- * Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED (N > max_tokens, an extent past 2^24), AA_ERR_CUDA.  No host synchronisation,
- * no allocation. */
+ * Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED (N > max_tokens or past 2^31 - 2^16 - 1, an extent past 2^24),
+ * AA_ERR_CUDA.  No host synchronisation, no allocation. */
 int agent_attn_rotate(agent_attn_handle* h, const void* Q, const void* K, const long long in_strides[3], int n_tokens,
                       const agent_attn_rotary* rotary, const agent_attn_norm* norm,
                       void* Q_out, void* K_out, const long long out_strides[3], void* stream);

@@ -4,6 +4,7 @@
 #include "kernels.h"
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -680,6 +681,7 @@ static int rotate_args(agent_attn_handle* h, int n_tokens, const agent_attn_rota
     memset(a, 0, sizeof(*a));
     if (n_tokens <= 0) return fail(h, AA_ERR_INVALID_ARG, "token count must be positive (N=%d)", n_tokens);
     if (n_tokens > h->cfg.max_tokens) return fail(h, AA_ERR_UNSUPPORTED, "N=%d exceeds the handle's max_tokens=%d", n_tokens, h->cfg.max_tokens);
+    if (n_tokens > INT_MAX - 65536) return fail(h, AA_ERR_UNSUPPORTED, "N=%d: token numbers of whole tiles must fit in 32 bits", n_tokens);
     a->slabs = h->cfg.batch * h->cfg.heads; a->heads = h->cfg.heads; a->N = n_tokens; a->d = h->cfg.head_dim;
     if (rotary) {
         if (rotary->axes < 0 || rotary->axes > 3) return fail(h, AA_ERR_INVALID_ARG, "0 to 3 axes, not %d", rotary->axes);

@@ -478,3 +478,16 @@ def test_gradients_at_offsets_past_32_bits(norm):
         mod.rotate_backward(*g, rotary, out=g)
         for t, (dx, size) in zip(g, want):
             check(t, dx, size, "f32")
+
+
+def test_token_counts_that_32_bits_hold_but_not_their_tiles():
+    """Refused before anything is launched: the pointers are of one token."""
+    N = (1 << 31) - 100
+    mod = AgentAttention(1, 1, 8, N, 1, torch.bfloat16)
+    q, g = torch.zeros(8, dtype=torch.bfloat16, device="cuda"), torch.zeros(8, device="cuda")
+    ws = torch.empty(int(mod.lib.agent_attn_rotate_workspace_bytes(mod._h)), dtype=torch.uint8, device="cuda")
+    norm = mod._norm(None, None, 1e-6)
+    assert mod.lib.agent_attn_rotate(mod._h, q.data_ptr(), None, None, N, None, norm, q.data_ptr(), None, None, None) == 2
+    assert mod.lib.agent_attn_rotate_backward(mod._h, g.data_ptr(), None, None, q.data_ptr(), None, None, N, None, norm, g.data_ptr(), None, None, None, None,
+                                              ws.data_ptr(), ws.numel(), None) == 2
+    assert b"32 bits" in mod.lib.agent_attn_last_error(mod._h)
