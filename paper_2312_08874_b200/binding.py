@@ -162,11 +162,9 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _empty(shape, dtype: torch.dtype, device: torch.device, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-    """Memory that work on `stream` (None: the current one) may write at once: what the current stream's allocator hands out may still be read by earlier
-    work there.  The current stream may use it, too, until it is freed."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+def _empty(shape, dtype: torch.dtype, device: torch.device, stream: torch.cuda.Stream) -> torch.Tensor:
+    """Memory that work on `stream` may write at once: what the current stream's allocator hands out may still be read by earlier work there.  The
+    current stream may use it, too, until it is freed."""
     with torch.cuda.stream(stream):
         t = torch.empty(shape, dtype=dtype, device=device)
     t.record_stream(torch.cuda.current_stream(device))
@@ -174,7 +172,15 @@ def _empty(shape, dtype: torch.dtype, device: torch.device, stream: Optional[tor
 
 
 def _dense_like(t: Optional[torch.Tensor], stream=None):
-    return None if t is None else _empty(t.shape, t.dtype, t.device, stream)
+    if t is None:
+        return None
+    if stream is None:                     # (half of the host time of torch.empty with type and device)
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    return _empty(t.shape, t.dtype, t.device, stream)
+
+
+def _dense(t: torch.Tensor, shape, stream=None):
+    return t.new_empty(shape) if stream is None else _empty(shape, t.dtype, t.device, stream)
 
 
 # torch.cuda.current_stream() builds a stream object (3.2 us); the raw handle costs 0.1 us
@@ -214,7 +220,9 @@ class Rotary:
                 raise ValueError(f"positions: expected a contiguous cuda float32 tensor [B or 1, N, {axes}], got {tuple(positions.shape)} {positions.dtype} on {positions.device}")
         elif extent is None or len(extent) != axes or any(not 0 < e <= _INT_MAX for e in extent):
             raise ValueError(f"extent: expected {axes} positive values of 32 bits, got {extent}")
-        self.freq, self.positions, self.channels, self.axes = freq, positions, channels, axes
+        if positions is not None and positions.device != freq.device:
+            raise ValueError(f"positions: expected them on {freq.device} with freq, got {positions.device}")
+        self.freq, self.positions, self.channels, self.axes, self._index = freq, positions, channels, axes, None
         self.extent = (1,) * axes if extent is None else tuple(int(e) for e in extent)
         self._batch = 0 if positions is None else positions.shape[0]
         self._c = AgentAttnRotary(axes, (ctypes.c_int * 3)(*(self.extent if positions is None else ())), (ctypes.c_int * 3)(*channels), int(pairs), freq.data_ptr(), _ptr(positions),
@@ -226,8 +234,10 @@ class Rotary:
         return torch.tensor([theta ** (-i / (c // 2)) for c in channels for i in range(c // 2)], dtype=torch.float32, device=torch.device("cuda", device))
 
     def _check(self, batch: int, n_tokens: int, device: int):
-        if self.freq.get_device() != device or (self.positions is not None and self.positions.get_device() != device):
-            raise ValueError(f"rotary: expected freq and positions on cuda:{device}, got {self.freq.device}{'' if self.positions is None else f' and {self.positions.device}'}")
+        if self._index is None:
+            self._index = self.freq.get_device()
+        if self._index != device:
+            raise ValueError(f"rotary: expected freq and positions on cuda:{device}, got {self.freq.device}")
         if self.positions is not None and (self.positions.shape[1] != n_tokens or self._batch not in (1, batch)):
             raise ValueError(f"positions: expected [{batch} or 1, {n_tokens}, {self.axes}], got {tuple(self.positions.shape)}")
 
@@ -252,6 +262,7 @@ class AgentAttention:
         self._ws: Optional[torch.Tensor] = None
         self._staging: Optional[torch.Tensor] = None
         self._bytes: dict = {}             # scratch sizes by call shape: they depend on nothing else
+        self._rotate_bytes: Optional[int] = None
         self._strides: dict = {}           # strides as the library takes them, by token count and strides
 
     def close(self):
@@ -626,11 +637,13 @@ class AgentAttention:
         got = {name: t for name, t in zip(("dq", "dk"), out) if t is not None}
         for name, gain, grad in (("dq_gain", q_gain, dq_out), ("dk_gain", k_gain, dk_out)):
             if gain is not None and grad is not None:
-                got[name] = _empty(self.head_dim, f32, self.device, stream)
+                got[name] = _dense(grad, (self.head_dim,), stream)
         if workspace is not None:
             self._chk_workspace(workspace)
         elif norm is not None:
-            workspace = self._scratch(int(self.lib.agent_attn_rotate_workspace_bytes(self._h)), stream)
+            if self._rotate_bytes is None:
+                self._rotate_bytes = int(self.lib.agent_attn_rotate_workspace_bytes(self._h))
+            workspace = self._scratch(self._rotate_bytes, stream)
         self._check(self.lib.agent_attn_rotate_backward(
             self._h, _ptr(dq_out), _ptr(dk_out), sgrad, _ptr(q), _ptr(k), sin, N, None if rotary is None else ctypes.byref(rotary._c), norm,
             _ptr(out[0]), _ptr(out[1]), sout, _ptr(got.get("dq_gain")), _ptr(got.get("dk_gain")),
@@ -651,7 +664,9 @@ class AgentAttention:
             self._chk_tensor(b_gate, (F,), "b_gate")
         if b_up is not None:
             self._chk_tensor(b_up, (F,), "b_up")
-        rows, C, F = (min(n, _INT_MAX) for n in (x.numel() // C if C else 0, C, F))            # (which the library refuses)
+        rows = x.numel() // C if C else 0
+        if rows > _INT_MAX or C > _INT_MAX or F > _INT_MAX:
+            rows, C, F = (min(n, _INT_MAX) for n in (rows, C, F))                              # (which the library refuses)
         return AgentAttnGate(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(b_gate), _ptr(b_up), rows, C, F, _ACTIVATIONS[activation])
 
     def _gate_workspace(self, gate, backward: int, workspace, stream):
@@ -673,7 +688,9 @@ class AgentAttention:
 
     def _scratch(self, nbytes: int, stream) -> Optional[torch.Tensor]:
         """Memory of one call on `stream`."""
-        return _empty(nbytes, torch.uint8, self.device, stream) if nbytes else None
+        if nbytes == 0:
+            return None
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.device) if stream is None else _empty(nbytes, torch.uint8, self.device, stream)
 
     def gated(self, x, w_gate, w_up, b_gate=None, b_up=None, activation: str = "silu", out=None, workspace=None, stream=None) -> torch.Tensor:
         """`agent_attn_gated`: act(x w_gate^T + b_gate) * (x w_up^T + b_up) for x [..., channels] and weights [hidden, channels].
@@ -683,7 +700,7 @@ class AgentAttention:
         gate = self._gate(x, w_gate, w_up, b_gate, b_up, activation)
         shape = x.shape[:-1] + (gate.hidden,)
         if out is None:
-            out = _empty(shape, x.dtype, x.device, stream)
+            out = _dense(x, shape, stream)
         else:
             self._chk_tensor(out, shape, "out")
         ws = self._gate_workspace(gate, 0, workspace, stream)
@@ -702,20 +719,24 @@ class AgentAttention:
         gate = self._gate(x, w_gate, w_up, b_gate, b_up, activation)
         self._chk_tensor(d_out, x.shape[:-1] + (gate.hidden,), "d_out")
         g = {}
+        dx = dw_gate = dw_up = db_gate = db_up = None
         if need_input_grad:
-            g["dx"] = _dense_like(x, stream)
+            g["dx"] = dx = _dense_like(x, stream)
         if need_weight_grads:
-            g["dw_gate"], g["dw_up"] = _dense_like(w_gate, stream), _dense_like(w_up, stream)
-        db = (None, None)
-        given = (b_gate is not None) + (b_up is not None)
+            g["dw_gate"], g["dw_up"] = dw_gate, dw_up = _dense_like(w_gate, stream), _dense_like(w_up, stream)
+        one = (b_gate is None) != (b_up is None)
         if need_bias_grads is None:
-            need_bias_grads = need_weight_grads and given == 2
-            if need_weight_grads and given == 1:
+            need_bias_grads = need_weight_grads and not one
+            if need_weight_grads and one:
                 warnings.warn("gated_backward: the gradient of a bias without the other one is returned with need_bias_grads=True only", stacklevel=2)
-        if need_bias_grads and given:                      # (the library sums both)
-            db = tuple(_empty(gate.hidden, self.dtype, self.device, stream) for _ in range(2))
-            g.update((n, t) for n, t, b in zip(("db_gate", "db_up"), db, (b_gate, b_up)) if b is not None)
-        grads = AgentAttnGateGrads(_ptr(g.get("dx")), _ptr(g.get("dw_gate")), _ptr(g.get("dw_up")), _ptr(db[0]), _ptr(db[1]), int(two_terms))
+        some = b_up if b_gate is None else b_gate
+        if need_bias_grads and some is not None:           # (the library sums both)
+            db_gate, db_up = _dense_like(some, stream), _dense_like(some, stream)
+            if b_gate is not None:
+                g["db_gate"] = db_gate
+            if b_up is not None:
+                g["db_up"] = db_up
+        grads = AgentAttnGateGrads(_ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(db_gate), _ptr(db_up), 1 if two_terms else 0)
         ws = self._gate_workspace(gate, 2 if two_terms else 1, workspace, stream)
         self._check(self.lib.agent_attn_gated_backward(self._h, ctypes.byref(gate), _ptr(d_out), ctypes.byref(grads), _ptr(ws),
                                                        0 if ws is None else ws.numel(), _stream_ptr(stream)))
