@@ -446,3 +446,18 @@ def test_gradient_of_a_bias_alone(dtype, M, C, F):
     assert all(rel(back[n], grads[n]) <= REL_BWD[dtype] for n in ("db_gate", "db_up"))
     assert set(mod.gated_backward(x, wg, wu, dh, need_bias_grads=False, **both)) == {"dx", "dw_gate", "dw_up"}
     assert set(mod.gated_backward(x, wg, wu, dh, need_bias_grads=True)) == {"dx", "dw_gate", "dw_up"}
+
+
+@pytest.mark.parametrize("M,C,F", [(300, 16448, 256), (1000, 16448, 2048), (2500, 64, 20480), (100, 16448, 256)])
+def test_small_half_precision_gradients_of_long_sums(M, C, F):
+    """Both at once: the second pass over G and U that come in pieces, and results that are divided after their pieces have met."""
+    x, wg, wu, dh, bg, bu = inputs(M, C, F, "f16", "gu", seed=8)
+    dh = (dh.float() * 1e-6).half()
+    mod = AgentAttention(1, 1, 64, 1, 1, torch.float16)
+    _, grads = reference(x, wg, wu, dh, bg, bu, "silu")
+    back = mod.gated_backward(x, wg, wu, dh, b_gate=bg, b_up=bu)
+    assert mod.query_status() == 0
+    for n, t in back.items():
+        assert float((t.double() - grads[n]).norm()) <= REL_BWD["f16"] * float(grads[n].norm()) + 3e-8 * t.numel() ** 0.5, n
+    again = mod.gated_backward(x, wg, wu, dh, b_gate=bg, b_up=bu)
+    assert all(torch.equal(again[n], back[n]) for n in back)
