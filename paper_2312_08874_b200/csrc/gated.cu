@@ -12,14 +12,15 @@
 //              A = dG in one block of the pair, dU in the other, both MN-major, B = X MN-major.  Their sums are cut into chunks of 64, of which all pairs
 //              have as many: whole tiles of dX, then a run of the other tiles; a pair writes what it has whole and leaves its share of what it has
 //              not, and gated_finish_kernel adds the shares up in their order.
-// 16-bit operands enter as they are; dG and dU are rounded to the element type, as every operand of a product on the tensor cores is (few rows: and what that
-// leaves as a second term).  In f16 kGrad is launched twice: the second one ends at once unless dG and dU leave the type's range (gated_scale).  fp32: operands are sums of three bf16 terms, six pairs of terms, small ones first.
+// 16-bit operands enter as they are; dG and dU are rounded to the element type, as every operand of a product on the tensor cores is (few rows, or where the
+// caller asks for it: and what that leaves as a second term).  In f16 kGrad is launched twice: the second one ends at once unless dG and dU leave the type's range
+// (gated_scale).  fp32: operands are sums of three bf16 terms, six pairs of terms, small ones first.
 //
 // What bounds it (us of a launch among others; rows x channels x hidden units):
 //   kForward   32768 x 512 x 1368 bf16, SiLU: 88 to 92, 1.0 PFLOP/s.  Tensor pipe 75 % busy (a chunk of 64 takes 600 cycles of 512), clocks under the power
 //              limit; the two products alone take 85 in the vendor's library.  8192 x 320 x 1280 f16, GELU: 18, 0.74 PFLOP/s: the epilogue (4000 cycles a tile,
 //              products 2600), a first accumulator after 4.2 us, 1.1 us from the last store to the end.  The library's products alone: 19.
-//   kGrad      8192 x 320 x 1280 f16 27, 25088 x 192 x 512 bf16 28: the epilogue, 7000 cycles a tile at half of the issue slots, and the same start and end.
+//   kGrad      8192 x 320 x 1280 f16 27 (its second launch 4), 25088 x 192 x 512 bf16 28: the epilogue, 7000 cycles a tile at half of the issue slots, and the same start and end.
 //   kProducts  30 and 24: operands out of L2, 32 KB a block and chunk of 64 in 480 to 600 cycles (instructions for 160 or 192 columns take 320 or 384).
 //   finishing  5.8 and 6.1: 16 MB of shares out of L2, a start.
 // Tiles of 512 columns would halve what kProducts reads of A, and double the shares: 64.6 -> 69.8 us for 8192 x 320 x 1280.

@@ -727,8 +727,9 @@ int units_of(RotateArgs* a, int tokens) {
     return a->tiles = (a->N + tokens - 1) / tokens;
 }
 // How many slabs a block visits with one set of angles; `tokens` of a block.  Fewer: the angles cost more, as much as
-// four rows; more: the last of the waves of `resident` blocks is emptier.  `rows`: of a slab (the tensors of a block).  With angles at
-// 0, 2, 4, 8 and 16 rows norm and rotation of 16 slabs of 128 x 128 take 96, 45, 39, 39 and 43 us.
+// four rows; more: the last of the waves of `resident` blocks is emptier.  `rows`: of a slab (the tensors of a block).  With angles at 0, 1, 2, 4, 8 and 16
+// rows (us): norm and rotation of 16 slabs of 128 x 128, bf16, in whole pairs 30.2, 30.3, 26.5, 26.5, 31.7 and 31.6, through shared memory 101, 49, 48, 42, 42 and
+// 46; rotation of the video grid 130, 52, 42, 42, 42 and 42; fp32, 16 slabs of 128 x 128 x 64 channels 69, 43, 43, 46, 46 and 52 (two rows would do there).
 int plan_rotate(RotateArgs* a, int tokens, int rows, int resident) {
     const int tiles = units_of(a, tokens);
     const long long alone = (long long)tiles * (a->slabs / a->unit_slabs);          // blocks if each visits all slabs of its unit
