@@ -638,9 +638,11 @@ class AgentAttention:
         for name, gain, grad in (("dq_gain", q_gain, dq_out), ("dk_gain", k_gain, dk_out)):
             if gain is not None and grad is not None:
                 got[name] = _dense(grad, (self.head_dim,), stream)
-        if workspace is not None:
+        if norm is None:
+            workspace = None               # (not read)
+        elif workspace is not None:
             self._chk_workspace(workspace)
-        elif norm is not None:
+        else:
             if self._rotate_bytes is None:
                 self._rotate_bytes = int(self.lib.agent_attn_rotate_workspace_bytes(self._h))
             workspace = self._scratch(self._rotate_bytes, stream)
@@ -683,8 +685,8 @@ class AgentAttention:
         return self._scratch(need, stream)
 
     def _chk_workspace(self, t: torch.Tensor):
-        if t.dtype is not torch.uint8 or t.get_device() != self._index or not t.is_contiguous():
-            raise ValueError(f"workspace: expected a contiguous {self.device} uint8 tensor, got {t.dtype} on {t.device}")
+        if t.get_device() != self._index or not t.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous {self.device} tensor, got one on {t.device}")
 
     def _scratch(self, nbytes: int, stream) -> Optional[torch.Tensor]:
         """Memory of one call on `stream`."""
@@ -708,13 +710,13 @@ class AgentAttention:
         return out
 
     def gated_backward(self, x, w_gate, w_up, d_out, b_gate=None, b_up=None, activation: str = "silu", need_input_grad: bool = True,
-                       need_weight_grads: bool = True, two_terms: bool = False, need_bias_grads: Optional[bool] = None, workspace=None, stream=None) -> dict:
+                       need_weight_grads: bool = True, workspace=None, stream=None, two_terms: bool = False, need_bias_grads: Optional[bool] = None) -> dict:
         """`agent_attn_gated_backward`: gradients of `gated` for the upstream gradient `d_out`, in the element type.
 
-        `two_terms` (16-bit types): the projections' gradients are not rounded to the element type on the way, so that each result is
-        rounded once; some 2.4 times the time.  Returns a dict with `dx`, `dw_gate`, `dw_up` and
-        `db_gate`, `db_up`: by default with the weights' gradients and only where both biases are given (else a warning);
-        `need_bias_grads=True` returns that of each bias that is given, `False` none.
+        Returns a dict with `dx`, `dw_gate`, `dw_up` and `db_gate`, `db_up`: these by default with the weights' gradients and only where both
+        biases are given (one alone: a warning); `need_bias_grads=True` returns that of each bias that is given, `False` none.
+        `two_terms` (16-bit types): the projections' gradients are not rounded to the element type on the way, so that each result is rounded
+        once; some 2.4 times the time.
         """
         gate = self._gate(x, w_gate, w_up, b_gate, b_up, activation)
         self._chk_tensor(d_out, x.shape[:-1] + (gate.hidden,), "d_out")

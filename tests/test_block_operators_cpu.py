@@ -82,6 +82,5 @@ def test_tensors_of_another_device_are_refused():
             with pytest.raises(ValueError):
                 check(other)
     cls._chk_tensor(handle, OnDevice(shape, torch.float32, -1), shape, "x", cuda=False)
-    for tensor in (OnDevice((64,), torch.float32, 1), torch.zeros(64, dtype=torch.uint8)):
-        with pytest.raises(ValueError):
-            cls._chk_workspace(handle, tensor)
+    with pytest.raises(ValueError):
+        cls._chk_workspace(handle, torch.zeros(64, dtype=torch.uint8))
