@@ -400,8 +400,8 @@ typedef struct {
 } agent_attn_gate;
 
 /* Bytes of device workspace of agent_attn_gated (backward == 0; none for 16-bit types, and for fp32 up to 8 rows or
- * 50 million products) or agent_attn_gated_backward (1, or AA_GATED_TWO_TERMS where the call asks for two terms).  0 on
- * invalid arguments, too. */
+ * 50 million products), agent_attn_gated_backward (1) or agent_attn_gated_backward_two_terms (AA_GATED_TWO_TERMS).
+ * 0 on invalid arguments, too. */
 #define AA_GATED_TWO_TERMS 2
 size_t agent_attn_gated_workspace_bytes(const agent_attn_handle* h, int rows, int channels, int hidden, int backward);
 
@@ -418,19 +418,22 @@ typedef struct {
     void* dw_up;              /* [hidden][channels]                                                */
     void* db_gate;            /* [hidden]                                                          */
     void* db_up;              /* [hidden]                                                          */
-    int two_terms;            /* not 0, 16-bit types: the projections' gradients keep a second term over any
-                                 number of rows, so that every result is rounded once; some 2.4 times the time */
 } agent_attn_gate_grads;
 
 /* Gradients of agent_attn_gated for d_out = dL/dH (device [rows][hidden], element type).  Both projections are
  * recomputed; nothing has to be saved.  The gradients of the two projections are rounded to the element type, as
- * operands of the products that follow (up to 128 rows, or where `two_terms` asks for it, they keep what that leaves as
- * a second term), which is why the results have that type and not fp32; the biases' gradients are sums of unrounded
- * numbers.  In f16 they are held
- * times a power of two where their largest is not in [2, 65504], so that the results have the type's range, whatever
- * theirs.  Sums are fp32, in a fixed order.  Errors as above. */
+ * operands of the products that follow (up to 128 rows they keep what that leaves as a second term), which is why the
+ * results have that type and not fp32; the biases' gradients are sums of unrounded numbers.  In f16 the projections'
+ * gradients are held times a power of two where their largest is not in [2, 65504], so that the results have the
+ * type's range, whatever theirs.  Sums are fp32, in a fixed order.  Errors as above. */
 int agent_attn_gated_backward(agent_attn_handle* h, const agent_attn_gate* gate, const void* d_out,
                               const agent_attn_gate_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same with a second term over any number of rows (16-bit types), so that every result is rounded once; some 2.4
+ * times the time past 128 rows. */
+int agent_attn_gated_backward_two_terms(agent_attn_handle* h, const agent_attn_gate* gate, const void* d_out,
+                                        const agent_attn_gate_grads* grads, void* workspace, size_t workspace_bytes,
+                                        void* stream);
 
 #ifdef __cplusplus
 }

@@ -31,7 +31,7 @@ EXPORTS = [
     "agent_attn_compose_bias", "agent_attn_forward_strided",
     "agent_attn_backward_workspace_bytes", "agent_attn_backward", "agent_attn_test_set_poll_limit",
     "agent_attn_test_set_stage_mask", "agent_attn_rotate", "agent_attn_rotate_backward", "agent_attn_rotate_workspace_bytes",
-    "agent_attn_gated", "agent_attn_gated_backward", "agent_attn_gated_workspace_bytes",
+    "agent_attn_gated", "agent_attn_gated_backward", "agent_attn_gated_backward_two_terms", "agent_attn_gated_workspace_bytes",
 ]
 
 
@@ -68,7 +68,7 @@ class AgentAttnGate(ctypes.Structure):
 
 class AgentAttnGateGrads(ctypes.Structure):
     _fields_ = [("dx", ctypes.c_void_p), ("dw_gate", ctypes.c_void_p), ("dw_up", ctypes.c_void_p), ("db_gate", ctypes.c_void_p),
-                ("db_up", ctypes.c_void_p), ("two_terms", ctypes.c_int)]
+                ("db_up", ctypes.c_void_p)]
 
 
 class AgentAttnError(RuntimeError):
@@ -150,8 +150,9 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.agent_attn_gated_workspace_bytes.restype = sz
     lib.agent_attn_gated.argtypes = [vp, gate, vp, vp, sz, vp]
     lib.agent_attn_gated.restype = ci
-    lib.agent_attn_gated_backward.argtypes = [vp, gate, vp, ggrads, vp, sz, vp]
-    lib.agent_attn_gated_backward.restype = ci
+    for gradients in (lib.agent_attn_gated_backward, lib.agent_attn_gated_backward_two_terms):
+        gradients.argtypes = [vp, gate, vp, ggrads, vp, sz, vp]
+        gradients.restype = ci
     lib.agent_attn_static_scratch_bytes.argtypes = []
     lib.agent_attn_static_scratch_bytes.restype = sz
     _lib = lib
@@ -711,7 +712,7 @@ class AgentAttention:
 
     def gated_backward(self, x, w_gate, w_up, d_out, b_gate=None, b_up=None, activation: str = "silu", need_input_grad: bool = True,
                        need_weight_grads: bool = True, workspace=None, stream=None, two_terms: bool = False, need_bias_grads: Optional[bool] = None) -> dict:
-        """`agent_attn_gated_backward`: gradients of `gated` for the upstream gradient `d_out`, in the element type.
+        """`agent_attn_gated_backward` (`…_two_terms`): gradients of `gated` for the upstream gradient `d_out`, in the element type.
 
         Returns a dict with `dx`, `dw_gate`, `dw_up` and `db_gate`, `db_up`: these by default with the weights' gradients and only where both
         biases are given (one alone: a warning); `need_bias_grads=True` returns that of each bias that is given, `False` none.
@@ -738,8 +739,8 @@ class AgentAttention:
                 g["db_gate"] = db_gate
             if b_up is not None:
                 g["db_up"] = db_up
-        grads = AgentAttnGateGrads(_ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(db_gate), _ptr(db_up), 1 if two_terms else 0)
+        grads = AgentAttnGateGrads(_ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(db_gate), _ptr(db_up))
         ws = self._gate_workspace(gate, 2 if two_terms else 1, workspace, stream)
-        self._check(self.lib.agent_attn_gated_backward(self._h, ctypes.byref(gate), _ptr(d_out), ctypes.byref(grads), _ptr(ws),
-                                                       0 if ws is None else ws.numel(), _stream_ptr(stream)))
+        call = self.lib.agent_attn_gated_backward_two_terms if two_terms else self.lib.agent_attn_gated_backward
+        self._check(call(self._h, ctypes.byref(gate), _ptr(d_out), ctypes.byref(grads), _ptr(ws), 0 if ws is None else ws.numel(), _stream_ptr(stream)))
         return g

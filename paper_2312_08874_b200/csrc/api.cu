@@ -849,14 +849,13 @@ int agent_attn_gated(agent_attn_handle* h, const agent_attn_gate* gate, void* ou
     return run_gate(h, c, stream);
 }
 
-int agent_attn_gated_backward(agent_attn_handle* h, const agent_attn_gate* gate, const void* d_out, const agent_attn_gate_grads* grads,
-                              void* workspace, size_t workspace_bytes, void* stream) {
+static int gated_gradients(agent_attn_handle* h, const agent_attn_gate* gate, const void* d_out, const agent_attn_gate_grads* grads, void* workspace,
+                           size_t workspace_bytes, bool two_terms, void* stream) {
     if (!h) return AA_ERR_INVALID_ARG;
     h->err[0] = 0;
     GatedCall c;
-    if (!grads) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
-    if (int rc = gate_call(h, gate, workspace, workspace_bytes, true, grads->two_terms != 0, &c)) return rc;
-    if (!d_out) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (int rc = gate_call(h, gate, workspace, workspace_bytes, true, two_terms, &c)) return rc;
+    if (!d_out || !grads) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
     if (!grads->dw_gate != !grads->dw_up || !grads->db_gate != !grads->db_up) return fail(h, AA_ERR_INVALID_ARG, "gradients of weights and of biases come in pairs");
     if (!grads->dx && !grads->dw_gate && !grads->db_gate) return fail(h, AA_ERR_INVALID_ARG, "no gradient asked for");
     const void* outs[] = {grads->dx, grads->dw_gate, grads->dw_up, grads->db_gate, grads->db_up};
@@ -868,6 +867,14 @@ int agent_attn_gated_backward(agent_attn_handle* h, const agent_attn_gate* gate,
     c.dh = d_out;
     c.dx = grads->dx; c.dwg = grads->dw_gate; c.dwu = grads->dw_up; c.dbg = grads->db_gate; c.dbu = grads->db_up;
     return run_gate(h, c, stream);
+}
+int agent_attn_gated_backward(agent_attn_handle* h, const agent_attn_gate* gate, const void* d_out, const agent_attn_gate_grads* grads,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    return gated_gradients(h, gate, d_out, grads, workspace, workspace_bytes, false, stream);
+}
+int agent_attn_gated_backward_two_terms(agent_attn_handle* h, const agent_attn_gate* gate, const void* d_out, const agent_attn_gate_grads* grads,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+    return gated_gradients(h, gate, d_out, grads, workspace, workspace_bytes, true, stream);
 }
 
 // A call on host buffers is bound by its copies (56 x 56 grid, 64 slabs: 78 MB in, 26 MB out, 1.98 ms in one piece).  It is cut into

@@ -84,3 +84,9 @@ def test_tensors_of_another_device_are_refused():
     cls._chk_tensor(handle, OnDevice(shape, torch.float32, -1), shape, "x", cuda=False)
     with pytest.raises(ValueError):
         cls._chk_workspace(handle, torch.zeros(64, dtype=torch.uint8))
+
+
+def test_null_handle_of_two_terms():
+    lib = pkg.load_library()
+    assert lib.agent_attn_gated_backward_two_terms(None, None, None, None, None, 0, None) == 1
+    assert lib.agent_attn_gated_workspace_bytes(None, 8, 8, 8, 2) == 0
