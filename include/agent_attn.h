@@ -435,6 +435,87 @@ int agent_attn_gated_backward_two_terms(agent_attn_handle* h, const agent_attn_g
                                         const agent_attn_gate_grads* grads, void* workspace, size_t workspace_bytes,
                                         void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Softmax attention over whole sequences: what a network uses where it has no agents (short grids, text).
+ *     P = softmax(scale Q K^T) over the keys that a query sees,  O = P V
+ * Head h of the queries reads head h / (heads / kv_heads) of the keys and values.  A sequence is a run of n_q
+ * queries and n_k keys.  By default every batch entry is one.  With offsets (batch 1: packed), sequence s has
+ * the queries q_offsets[s] .. q_offsets[s + 1] - 1 and the keys k_offsets[s] .. k_offsets[s + 1] - 1; with lengths
+ * (batch entries of their own), entry b has its first q_lengths[b] queries and k_lengths[b] keys.  Causal: query i sees
+ * the keys j <= i + n_k - n_q, so that the last query sees all (a chunk of new tokens after a cache; one token
+ * of a generation).  A query that sees no key has the result 0 and the log-sum-exp -inf, and no gradient.
+ * Rows that belong to no sequence are neither read nor written.  Offsets and lengths are device numbers: they may
+ * change between replays of a captured call, and the kernels hold them to the tensors (offsets that
+ * do not rise make results meaningless, but no access outside).
+ * Logits, softmax and sums are fp32 (fp32 tensors: products as sums of bf16 terms, fp32 accuracy); 16-bit types round the
+ * probabilities, and in the gradient dS, once to the element type.  A row whose logits have an infinity or a
+ * NaN is NaN; an infinite or NaN value makes its channel non-finite in the rows that see it, and in no other. */
+typedef struct {
+    const void *q;            /* device; element (b, head, token, c) at base + b * strides[0] + head * strides[1]
+                                 + token * strides[2] + c                                          */
+    const void *k, *v;        /* device, kv_heads heads                                            */
+    long long q_strides[3];   /* elements, multiples of 16 bytes, token stride >= head_dim         */
+    long long k_strides[3], v_strides[3];
+    int queries, keys;        /* rows of a batch entry: 1 .. max_tokens                            */
+    int kv_heads;             /* divides the handle's heads                                        */
+    int causal;
+    float scale;              /* of the logits; 0: 1 / sqrt(head_dim)                              */
+    int sequences;            /* packed: their number; else 0                                      */
+    const int *q_offsets, *k_offsets;   /* device [sequences + 1], rising, or both NULL            */
+    const int *q_lengths, *k_lengths;   /* device [batch], or NULL (all); not with offsets         */
+} agent_attn_sequences;
+
+/* Bytes of device workspace of agent_attn_attend (backward == 0: none but where few queries meet many keys) or
+ * agent_attn_attend_backward (1).  Depends on queries, keys, kv_heads, sequences and whether offsets are
+ * given.  0 on invalid arguments, too. */
+size_t agent_attn_attend_workspace_bytes(const agent_attn_handle* h, const agent_attn_sequences* s, int backward);
+
+/* out  device, element type, strides out_strides;  lse  device fp32 [B][heads][queries], or NULL: natural
+ * log-sum-exp of the logits, which the gradient takes.  No overlap of results with inputs.
+ * Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED (tokens past max_tokens; queries x heads, or keys, past
+ * 2^31 - 2^16 - 1), AA_ERR_WORKSPACE, AA_ERR_CUDA.  No host synchronisation, no allocation. */
+int agent_attn_attend(agent_attn_handle* h, const agent_attn_sequences* s, void* out, const long long out_strides[3],
+                      float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients in the element type (16-bit operands of the products round P and dS to it); strides as above. */
+typedef struct {
+    void *dq, *dk, *dv;       /* device, the shapes of q, k, v                                     */
+    long long dq_strides[3], dk_strides[3], dv_strides[3];
+} agent_attn_attend_grads;
+
+/* Gradients of agent_attn_attend for d_out = dL/dout: `out` and `lse` are the forward call's results.  Each key's
+ * gradient is the sum over the heads that share it.  Sums are fp32, in a fixed order.  In f16, P and dS are held
+ * times powers of two, so that small ones keep their bits.  Errors as above. */
+int agent_attn_attend_backward(agent_attn_handle* h, const agent_attn_sequences* s, const void* out, const long long out_strides[3],
+                               const float* lse, const void* d_out, const long long d_out_strides[3],
+                               const agent_attn_attend_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Layer norm of every row x of `channels` elements:
+ *     y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * weight + bias
+ * Of the handle it uses device and element type.  Sums are fp32, taken about the mean; y is rounded once. */
+typedef struct {
+    const void* x;            /* device [rows][channels], element type                             */
+    const void* weight;       /* device [channels], or NULL (1)                                    */
+    const void* bias;         /* device [channels], or NULL (0)                                    */
+    long long rows;           /* 1 .. 2^31 - 1                                                     */
+    int channels;             /* 1 .. 65536                                                        */
+    float eps;                /* >= 0                                                              */
+} agent_attn_layer_norm_args;
+
+/* y device [rows][channels], may be x itself.  Any alignment (16 bytes and whole vectors of 16 bytes are fast).
+ * Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED, AA_ERR_CUDA.  No host synchronisation, no allocation. */
+int agent_attn_layer_norm(agent_attn_handle* h, const agent_attn_layer_norm_args* a, void* y, void* stream);
+
+/* Bytes of device workspace of agent_attn_layer_norm_backward with gradients of weight or bias.  0 on invalid arguments. */
+size_t agent_attn_layer_norm_workspace_bytes(const agent_attn_handle* h, long long rows, int channels);
+
+/* Gradients for d_y = dL/dy (device [rows][channels], element type): dx [rows][channels] in the element type (may be
+ * d_y itself), d_weight and d_bias fp32 [channels]; each may be NULL.  Row statistics are taken again from x; `bias` is not
+ * read.  Sums over the rows are fp32, in a fixed order.  Errors as above, and AA_ERR_WORKSPACE. */
+int agent_attn_layer_norm_backward(agent_attn_handle* h, const agent_attn_layer_norm_args* a, const void* d_y, void* dx,
+                                   float* d_weight, float* d_bias, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,6 +32,8 @@ EXPORTS = [
     "agent_attn_backward_workspace_bytes", "agent_attn_backward", "agent_attn_test_set_poll_limit",
     "agent_attn_test_set_stage_mask", "agent_attn_rotate", "agent_attn_rotate_backward", "agent_attn_rotate_workspace_bytes",
     "agent_attn_gated", "agent_attn_gated_backward", "agent_attn_gated_backward_two_terms", "agent_attn_gated_workspace_bytes",
+    "agent_attn_attend", "agent_attn_attend_backward", "agent_attn_attend_workspace_bytes",
+    "agent_attn_layer_norm", "agent_attn_layer_norm_backward", "agent_attn_layer_norm_workspace_bytes",
 ]
 
 
@@ -69,6 +71,23 @@ class AgentAttnGate(ctypes.Structure):
 class AgentAttnGateGrads(ctypes.Structure):
     _fields_ = [("dx", ctypes.c_void_p), ("dw_gate", ctypes.c_void_p), ("dw_up", ctypes.c_void_p), ("db_gate", ctypes.c_void_p),
                 ("db_up", ctypes.c_void_p)]
+
+
+class AgentAttnSequences(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_strides", ctypes.c_longlong * 3),
+                ("k_strides", ctypes.c_longlong * 3), ("v_strides", ctypes.c_longlong * 3), ("queries", ctypes.c_int), ("keys", ctypes.c_int),
+                ("kv_heads", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float), ("sequences", ctypes.c_int),
+                ("q_offsets", ctypes.c_void_p), ("k_offsets", ctypes.c_void_p), ("q_lengths", ctypes.c_void_p), ("k_lengths", ctypes.c_void_p)]
+
+
+class AgentAttnAttendGrads(ctypes.Structure):
+    _fields_ = [("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p), ("dq_strides", ctypes.c_longlong * 3),
+                ("dk_strides", ctypes.c_longlong * 3), ("dv_strides", ctypes.c_longlong * 3)]
+
+
+class AgentAttnLayerNorm(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("rows", ctypes.c_longlong),
+                ("channels", ctypes.c_int), ("eps", ctypes.c_float)]
 
 
 class AgentAttnError(RuntimeError):
@@ -153,6 +172,20 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     for gradients in (lib.agent_attn_gated_backward, lib.agent_attn_gated_backward_two_terms):
         gradients.argtypes = [vp, gate, vp, ggrads, vp, sz, vp]
         gradients.restype = ci
+    seqs, agrads = ctypes.POINTER(AgentAttnSequences), ctypes.POINTER(AgentAttnAttendGrads)
+    lib.agent_attn_attend_workspace_bytes.argtypes = [vp, seqs, ci]
+    lib.agent_attn_attend_workspace_bytes.restype = sz
+    lib.agent_attn_attend.argtypes = [vp, seqs, vp, ll3, vp, vp, sz, vp]
+    lib.agent_attn_attend.restype = ci
+    lib.agent_attn_attend_backward.argtypes = [vp, seqs, vp, ll3, vp, vp, ll3, agrads, vp, sz, vp]
+    lib.agent_attn_attend_backward.restype = ci
+    lnorm = ctypes.POINTER(AgentAttnLayerNorm)
+    lib.agent_attn_layer_norm.argtypes = [vp, lnorm, vp, vp]
+    lib.agent_attn_layer_norm.restype = ci
+    lib.agent_attn_layer_norm_workspace_bytes.argtypes = [vp, ctypes.c_longlong, ci]
+    lib.agent_attn_layer_norm_workspace_bytes.restype = sz
+    lib.agent_attn_layer_norm_backward.argtypes = [vp, lnorm, vp, vp, vp, vp, vp, sz, vp]
+    lib.agent_attn_layer_norm_backward.restype = ci
     lib.agent_attn_static_scratch_bytes.argtypes = []
     lib.agent_attn_static_scratch_bytes.restype = sz
     _lib = lib
@@ -743,4 +776,163 @@ class AgentAttention:
         ws = self._gate_workspace(gate, 2 if two_terms else 1, workspace, stream)
         call = self.lib.agent_attn_gated_backward_two_terms if two_terms else self.lib.agent_attn_gated_backward
         self._check(call(self._h, ctypes.byref(gate), _ptr(d_out), ctypes.byref(grads), _ptr(ws), 0 if ws is None else ws.numel(), _stream_ptr(stream)))
+        return g
+
+    # ------------------------------------------------------------------ softmax attention over whole sequences
+    def _view(self, t: torch.Tensor, shape, name: str, strides=None):
+        """A view of `shape` [B, heads, N, d] with contiguous channels; its strides as the library takes them (those of single entries are never
+        used: they are given as dense ones)."""
+        if t.shape != shape or t.dtype is not self.dtype or t.get_device() != self._index or (t.stride(3) != 1 and shape[3] != 1):
+            raise ValueError(f"{name}: expected a {self.device} {self.dtype} view of shape {tuple(shape)} with contiguous channels, got {tuple(t.shape)} {t.dtype} on {t.device}")
+        st, d = t.stride(), shape[3]
+        token = st[2] if shape[2] > 1 else d
+        return (st[0] if shape[0] > 1 else d, st[1] if shape[1] > 1 else d, token)
+
+    def _numbers(self, t: Optional[torch.Tensor], count: Optional[int], name: str):
+        if t is not None and (t.dim() != 1 or t.dtype is not torch.int32 or t.get_device() != self._index or not t.is_contiguous() or (count is not None and t.shape[0] != count)):
+            raise ValueError(f"{name}: expected a contiguous {self.device} int32 tensor of {'offsets' if count is None else count}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+
+    def _sequences(self, q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths) -> AgentAttnSequences:
+        if q.dim() != 4 or k.dim() != 4:
+            raise ValueError(f"expected views [B, heads, N, d], got {tuple(q.shape)} and {tuple(k.shape)}")
+        B, h, d = self.batch, self.heads, self.head_dim
+        N, M, kv = self._tokens(q), self._tokens(k), k.shape[1]
+        if kv < 1 or h % kv:
+            raise ValueError(f"k: expected a number of heads that divides {h}, got {kv}")
+        if scale is not None and not scale > 0:
+            raise ValueError(f"scale: expected a positive number or None, got {scale}")
+        if q_offsets is None and k_offsets is not None:
+            raise ValueError("k_offsets belong to q_offsets")
+        if q_offsets is not None and k_offsets is None:
+            if N != M:
+                raise ValueError(f"k_offsets are required where queries ({N}) and keys ({M}) differ")
+            k_offsets = q_offsets
+        self._numbers(q_offsets, None, "q_offsets")
+        self._numbers(k_offsets, None if q_offsets is None else q_offsets.shape[0], "k_offsets")
+        self._numbers(q_lengths, B, "q_lengths")
+        self._numbers(k_lengths, B, "k_lengths")
+        s = AgentAttnSequences(_ptr(q), _ptr(k), _ptr(v), self._view(q, (B, h, N, d), "q"), self._view(k, (B, kv, M, d), "k"), self._view(v, (B, kv, M, d), "v"),
+                               N, M, kv, int(bool(causal)), 0.0 if scale is None else scale, 0 if q_offsets is None else min(q_offsets.shape[0] - 1, _INT_MAX),
+                               _ptr(q_offsets), _ptr(k_offsets), _ptr(q_lengths), _ptr(k_lengths))
+        return s
+
+    def _new_view(self, t: torch.Tensor, partial: bool, stream) -> torch.Tensor:
+        """A new tensor with t's shape, token-major where t is; zeros where its rows need not all belong to a sequence."""
+        if stream is None:
+            return torch.zeros_like(t) if partial else torch.empty_like(t)
+        with torch.cuda.stream(stream):
+            new = torch.zeros_like(t) if partial else torch.empty_like(t)
+        new.record_stream(torch.cuda.current_stream(self.device))
+        return new
+
+    def _attend_workspace(self, s: AgentAttnSequences, backward: int, workspace, stream):
+        if workspace is not None:
+            self._chk_workspace(workspace)
+            return workspace
+        key = ("attend", s.queries, s.keys, s.kv_heads, s.sequences, backward)
+        need = self._bytes.get(key)
+        if need is None:
+            if len(self._bytes) >= 64:
+                self._bytes.clear()
+            need = self._bytes[key] = int(self.lib.agent_attn_attend_workspace_bytes(self._h, ctypes.byref(s), backward))
+        return self._scratch(need, stream)
+
+    def attend(self, q, k, v, causal: bool = False, scale: Optional[float] = None, q_offsets=None, k_offsets=None, q_lengths=None, k_lengths=None,
+               need_lse: bool = False, out=None, workspace=None, stream=None):
+        """`agent_attn_attend`: softmax attention, softmax(scale q k^T) v, over whole sequences.
+
+        `q` is a view [B, heads, N, d] with contiguous channels, `k` and `v` are views [B, kv_heads, M, d]; kv_heads divides heads, and neighbouring
+        heads of the queries share a head of the keys.  Every batch entry is a sequence; its first `q_lengths`[b] queries and `k_lengths`[b] keys,
+        where these are given (int32 [B] on the device: a padded batch, or caches of M rows that are partly filled).  Or, with B = 1, sequences
+        follow one another: s has the queries `q_offsets`[s] to `q_offsets`[s + 1] and the keys between `k_offsets` (by default the same), int32
+        on the device.  `causal`: the last query sees every key of its sequence, each one before it a key less.  A query without a key has the result 0.
+
+        Returns the result, [B, heads, N, d] (token-major where q is), with `need_lse` also the log-sum-exp of the logits, fp32 [B, heads, N], which
+        `attend_backward` takes.  Rows of no sequence are zero in a new result and left as they are in `out`.
+        """
+        s = self._sequences(q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths)
+        partial = q_offsets is not None or q_lengths is not None
+        if out is None:
+            out = self._new_view(q, partial, stream)
+        sout = (ctypes.c_longlong * 3)(*self._view(out, q.shape, "out"))
+        lse = None
+        if need_lse:
+            lse = _empty(q.shape[:3], torch.float32, self.device, stream) if stream is not None else q.new_empty(q.shape[:3], dtype=torch.float32)
+        ws = self._attend_workspace(s, 0, workspace, stream)
+        self._check(self.lib.agent_attn_attend(self._h, ctypes.byref(s), _ptr(out), sout, _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+                                               _stream_ptr(stream)))
+        return (out, lse) if need_lse else out
+
+    def attend_backward(self, q, k, v, out, lse, d_out, causal: bool = False, scale: Optional[float] = None, q_offsets=None, k_offsets=None, q_lengths=None,
+                        k_lengths=None, grads=None, workspace=None, stream=None) -> dict:
+        """`agent_attn_attend_backward`: gradients of `attend` for the upstream gradient `d_out` (a view like `out`), in the element type.
+
+        `out` and `lse` are the forward call's results, the other arguments its own.  Returns a dict with `dq`, `dk`, `dv`, laid out as q, k and v are, or
+        the three views `grads`; rows of no sequence are zero in new tensors and left as they are in given ones.
+        """
+        s = self._sequences(q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths)
+        sout = (ctypes.c_longlong * 3)(*self._view(out, q.shape, "out"))
+        sdo = (ctypes.c_longlong * 3)(*self._view(d_out, q.shape, "d_out"))
+        if lse.shape != q.shape[:3] or lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.get_device() != self._index:
+            raise ValueError(f"lse: expected a contiguous {self.device} float32 tensor of shape {tuple(q.shape[:3])}, got {tuple(lse.shape)} {lse.dtype} on {lse.device}")
+        if grads is None:
+            packed = q_offsets is not None
+            grads = tuple(self._new_view(t, packed or n is not None, stream) for t, n in ((q, q_lengths), (k, k_lengths), (v, k_lengths)))
+        g = AgentAttnAttendGrads(*(_ptr(t) for t in grads), *(self._view(t, like.shape, name) for t, like, name in zip(grads, (q, k, v), ("dq", "dk", "dv"))))
+        ws = self._attend_workspace(s, 1, workspace, stream)
+        self._check(self.lib.agent_attn_attend_backward(self._h, ctypes.byref(s), _ptr(out), sout, _ptr(lse), _ptr(d_out), sdo, ctypes.byref(g), _ptr(ws),
+                                                        0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream)))
+        return dict(zip(("dq", "dk", "dv"), grads))
+
+    # ------------------------------------------------------------------ layer norm
+    def _layer_norm(self, x, weight, bias, eps) -> AgentAttnLayerNorm:
+        if x.dim() == 0:
+            raise ValueError("x: expected [..., channels]")
+        C = x.shape[-1]
+        self._chk_tensor(x, x.shape, "x")
+        self._chk_tensor(weight, (C,), "weight")
+        self._chk_tensor(bias, (C,), "bias")
+        return AgentAttnLayerNorm(_ptr(x), _ptr(weight), _ptr(bias), x.numel() // C if C else 0, min(C, _INT_MAX), eps)
+
+    def layer_norm(self, x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=None) -> torch.Tensor:
+        """`agent_attn_layer_norm`: (x - mean) / sqrt(var + eps) * weight + bias over the last dimension of x.  `out` may be x itself."""
+        a = self._layer_norm(x, weight, bias, eps)
+        if out is None:
+            out = _dense_like(x, stream)
+        else:
+            self._chk_tensor(out, x.shape, "out")
+        self._check(self.lib.agent_attn_layer_norm(self._h, ctypes.byref(a), _ptr(out), _stream_ptr(stream)))
+        return out
+
+    def layer_norm_backward(self, x, d_out, weight=None, bias=None, eps: float = 1e-5, need_input_grad: bool = True, need_weight_grads: bool = True,
+                            out=None, workspace=None, stream=None) -> dict:
+        """`agent_attn_layer_norm_backward`: gradients of `layer_norm` for the upstream gradient `d_out`.
+
+        Returns a dict with `dx` (the element type; `out`, which may be d_out itself) and, for the weight and the bias that were given, fp32
+        `dw` and `db`.  Nothing of the forward call is needed but its inputs.
+        """
+        a = self._layer_norm(x, weight, bias, eps)
+        self._chk_tensor(d_out, x.shape, "d_out")
+        g = {}
+        if need_input_grad:
+            g["dx"] = _dense_like(x, stream) if out is None else out
+            self._chk_tensor(g["dx"], x.shape, "out")
+        if need_weight_grads:
+            for name, t in (("dw", weight), ("db", bias)):
+                if t is not None:
+                    g[name] = t.new_empty(t.shape, dtype=torch.float32) if stream is None else _empty(t.shape, torch.float32, self.device, stream)
+        if not ("dw" in g or "db" in g):
+            workspace = None               # (not read)
+        elif workspace is not None:
+            self._chk_workspace(workspace)
+        else:
+            key = ("norm", a.rows, a.channels)
+            need = self._bytes.get(key)
+            if need is None:
+                if len(self._bytes) >= 64:
+                    self._bytes.clear()
+                need = self._bytes[key] = int(self.lib.agent_attn_layer_norm_workspace_bytes(self._h, a.rows, a.channels))
+            workspace = self._scratch(need, stream)
+        self._check(self.lib.agent_attn_layer_norm_backward(self._h, ctypes.byref(a), _ptr(d_out), _ptr(g.get("dx")), _ptr(g.get("dw")), _ptr(g.get("db")), _ptr(workspace),
+                                                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
         return g

@@ -877,6 +877,188 @@ int agent_attn_gated_backward_two_terms(agent_attn_handle* h, const agent_attn_g
     return gated_gradients(h, gate, d_out, grads, workspace, workspace_bytes, true, stream);
 }
 
+// ------------------------------------------------------------- softmax attention over whole sequences
+static int attend_strides(agent_attn_handle* h, const long long* s, int unit, TokLayout* l) {
+    if (!s) return fail(h, AA_ERR_INVALID_ARG, "null pointer: strides");
+    return read_strides(h, s, 1, unit, l);
+}
+// What both directions share; false: refused, with the code in *rc
+static int attend_args(agent_attn_handle* h, const agent_attn_sequences* s, AttendArgs* a) {
+    memset(a, 0, sizeof(*a));
+    if (!s) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (s->queries <= 0 || s->keys <= 0) return fail(h, AA_ERR_INVALID_ARG, "token counts must be positive (%d queries, %d keys)", s->queries, s->keys);
+    if (s->queries > h->cfg.max_tokens || s->keys > h->cfg.max_tokens)
+        return fail(h, AA_ERR_UNSUPPORTED, "N=%d exceeds the handle's max_tokens=%d", std::max(s->queries, s->keys), h->cfg.max_tokens);
+    if (s->kv_heads <= 0 || h->cfg.heads % s->kv_heads) return fail(h, AA_ERR_INVALID_ARG, "%d heads of keys do not divide %d heads", s->kv_heads, h->cfg.heads);
+    if (!(s->scale >= 0.f) || std::isinf(s->scale)) return fail(h, AA_ERR_INVALID_ARG, "scale must be finite and not negative");
+    if (!s->q_offsets != !s->k_offsets) return fail(h, AA_ERR_INVALID_ARG, "offsets of queries and keys belong together");
+    if (s->q_offsets) {
+        if (h->cfg.batch != 1) return fail(h, AA_ERR_INVALID_ARG, "packed sequences need a handle of one batch entry, not %d", h->cfg.batch);
+        if (s->sequences <= 0) return fail(h, AA_ERR_INVALID_ARG, "packed sequences must be at least one, not %d", s->sequences);
+        if (s->q_lengths || s->k_lengths) return fail(h, AA_ERR_INVALID_ARG, "offsets and lengths exclude each other");
+    } else if (s->sequences) {
+        return fail(h, AA_ERR_INVALID_ARG, "a number of sequences needs offsets");
+    }
+    const void* numbers[] = {s->q_offsets, s->k_offsets, s->q_lengths, s->k_lengths};
+    for (const void* p : numbers)
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(h, AA_ERR_INVALID_ARG, "offsets and lengths must be 4-byte aligned");
+    a->batch = h->cfg.batch; a->heads = h->cfg.heads; a->kv_heads = s->kv_heads; a->N = s->queries; a->M = s->keys; a->d = h->cfg.head_dim;
+    a->sequences = s->q_offsets ? s->sequences : h->cfg.batch;
+    // rows of queries x heads and of keys, and tiles of them, are numbers of 31 bits
+    const long long most = INT_MAX - 65536LL, rows = (long long)a->N * a->heads;
+    if (rows > most || (long long)a->sequences > most / 16 || rows / 16 + a->sequences > most || a->M > most ||
+        (!s->q_offsets && ((rows + 15) / 16 * a->batch > most || ((long long)a->M + 63) / 64 * a->batch > most)))
+        return fail(h, AA_ERR_UNSUPPORTED, "%d queries of %d heads over %d keys: rows must fit in 31 bits", a->N, a->heads, a->M);
+    a->q_offsets = s->q_offsets; a->k_offsets = s->k_offsets; a->q_lengths = s->q_lengths; a->k_lengths = s->k_lengths;
+    a->causal = s->causal != 0;
+    a->scale = s->scale > 0.f ? s->scale : 1.0f / std::sqrt((float)h->cfg.head_dim);
+    a->q = s->q; a->k = s->k; a->v = s->v;
+    a->status = h->d_status;
+    return AA_OK;
+}
+// The tensors of a call besides what attend_args has looked at
+static int attend_tensors(agent_attn_handle* h, const agent_attn_sequences* s, AttendArgs* a) {
+    if (!s->q || !s->k || !s->v) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (int rc = attend_strides(h, s->q_strides, h->elem_bytes, &a->lq)) return rc;
+    if (int rc = attend_strides(h, s->k_strides, h->elem_bytes, &a->lk)) return rc;
+    if (int rc = attend_strides(h, s->v_strides, h->elem_bytes, &a->lv)) return rc;
+    if (misaligned(s->q) || misaligned(s->k) || misaligned(s->v)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    return AA_OK;
+}
+
+size_t agent_attn_attend_workspace_bytes(const agent_attn_handle* h, const agent_attn_sequences* s, int backward) {
+    if (!h || (backward != 0 && backward != 1)) return 0;
+    AttendArgs a;
+    agent_attn_handle scratch;                     // (refusals write their message here)
+    memset(&scratch, 0, sizeof(scratch));
+    scratch.cfg = h->cfg;
+    if (attend_args(&scratch, s, &a)) return 0;
+    return backward ? attend_backward_workspace(h->cfg.dtype, a, h->sm_count) : attend_workspace(h->cfg.dtype, a, h->sm_count);
+}
+
+int agent_attn_attend(agent_attn_handle* h, const agent_attn_sequences* s, void* out, const long long out_strides[3], float* lse, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+    if (!h) return AA_ERR_INVALID_ARG;
+    h->err[0] = 0;
+    AttendArgs a;
+    if (int rc = attend_args(h, s, &a)) return rc;
+    if (int rc = attend_tensors(h, s, &a)) return rc;
+    if (!out) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (int rc = attend_strides(h, out_strides, h->elem_bytes, &a.lo)) return rc;
+    if (misaligned(out) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned (lse 4)");
+    if (out == s->q || out == s->k || out == s->v) return fail(h, AA_ERR_INVALID_ARG, "the result must not take the place of an input");
+    const size_t need = attend_workspace(h->cfg.dtype, a, h->sm_count);
+    if (need && !workspace) return fail(h, AA_ERR_WORKSPACE, "workspace has 0 bytes, %zu needed", need);
+    if (need > workspace_bytes) return fail(h, AA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+    if (need && misaligned(workspace)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    a.out = out; a.lse = lse; a.ws = static_cast<float*>(workspace);
+    DeviceGuard guard(h->cfg.device);
+    if (!guard.ok) return fail(h, AA_ERR_CUDA, "cannot select device %d", h->cfg.device);
+    int launches = 0;
+    const cudaError_t e = launch_attend(h->cfg.dtype, a, h->sm_count, (cudaStream_t)stream, &launches);
+    if (e != cudaSuccess) return fail(h, AA_ERR_CUDA, "attention launch failed: %s", cudaGetErrorString(e));
+    h->launches = launches;
+    return AA_OK;
+}
+
+int agent_attn_attend_backward(agent_attn_handle* h, const agent_attn_sequences* s, const void* out, const long long out_strides[3], const float* lse,
+                               const void* d_out, const long long d_out_strides[3], const agent_attn_attend_grads* grads, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    if (!h) return AA_ERR_INVALID_ARG;
+    h->err[0] = 0;
+    AttendArgs a;
+    if (int rc = attend_args(h, s, &a)) return rc;
+    if (int rc = attend_tensors(h, s, &a)) return rc;
+    if (!out || !lse || !d_out || !grads || !grads->dq || !grads->dk || !grads->dv) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (int rc = attend_strides(h, out_strides, h->elem_bytes, &a.lo)) return rc;
+    if (int rc = attend_strides(h, d_out_strides, h->elem_bytes, &a.ldo)) return rc;
+    if (int rc = attend_strides(h, grads->dq_strides, h->elem_bytes, &a.ldq)) return rc;
+    if (int rc = attend_strides(h, grads->dk_strides, h->elem_bytes, &a.ldk)) return rc;
+    if (int rc = attend_strides(h, grads->dv_strides, h->elem_bytes, &a.ldv)) return rc;
+    const void* ins[] = {s->q, s->k, s->v, out, d_out};
+    const void* outs[] = {grads->dq, grads->dk, grads->dv};
+    for (int i = 0; i < 3; ++i) {
+        if (misaligned(outs[i])) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned (lse 4)");
+        for (const void* p : ins)
+            if (outs[i] == p) return fail(h, AA_ERR_INVALID_ARG, "a gradient buffer aliases an input");
+        for (int j = 0; j < i; ++j)
+            if (outs[i] == outs[j]) return fail(h, AA_ERR_INVALID_ARG, "two gradient buffers alias");
+    }
+    if (misaligned(out) || misaligned(d_out) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned (lse 4)");
+    const size_t need = attend_backward_workspace(h->cfg.dtype, a, h->sm_count);
+    if (!workspace || need > workspace_bytes) return fail(h, AA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, need);
+    if (misaligned(workspace)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+    a.out = const_cast<void*>(out); a.lse = const_cast<float*>(lse); a.dout = d_out; a.ws = static_cast<float*>(workspace);
+    a.dq = grads->dq; a.dk = grads->dk; a.dv = grads->dv;
+    DeviceGuard guard(h->cfg.device);
+    if (!guard.ok) return fail(h, AA_ERR_CUDA, "cannot select device %d", h->cfg.device);
+    int launches = 0;
+    const cudaError_t e = launch_attend_backward(h->cfg.dtype, a, h->sm_count, (cudaStream_t)stream, &launches);
+    if (e != cudaSuccess) return fail(h, AA_ERR_CUDA, "attention gradient launch failed: %s", cudaGetErrorString(e));
+    h->launches = launches;
+    return AA_OK;
+}
+
+// ------------------------------------------------------------- layer norm
+static int norm_args(agent_attn_handle* h, const agent_attn_layer_norm_args* s, NormArgs* a) {
+    memset(a, 0, sizeof(*a));
+    if (!s || !s->x) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (s->rows <= 0 || s->channels <= 0) return fail(h, AA_ERR_INVALID_ARG, "rows and channels must be positive (%lld, %d)", s->rows, s->channels);
+    if (s->rows > INT_MAX || s->channels > 65536) return fail(h, AA_ERR_UNSUPPORTED, "%lld rows of %d channels: at most 2^31 - 1 of 65536", s->rows, s->channels);
+    if (!(s->eps >= 0.f) || std::isinf(s->eps)) return fail(h, AA_ERR_INVALID_ARG, "eps must be finite and not negative");
+    a->x = s->x; a->w = s->weight; a->b = s->bias; a->rows = s->rows; a->C = s->channels; a->eps = s->eps;
+    return AA_OK;
+}
+static bool off_elements(const agent_attn_handle* h, const void* p) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)h->elem_bytes != 0; }
+
+int agent_attn_layer_norm(agent_attn_handle* h, const agent_attn_layer_norm_args* s, void* y, void* stream) {
+    if (!h) return AA_ERR_INVALID_ARG;
+    h->err[0] = 0;
+    NormArgs a;
+    if (int rc = norm_args(h, s, &a)) return rc;
+    if (!y) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (off_elements(h, a.x) || off_elements(h, a.w) || off_elements(h, a.b) || off_elements(h, y)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be aligned to their elements");
+    if (y == a.w || y == a.b) return fail(h, AA_ERR_INVALID_ARG, "the result must not take the place of a weight");
+    a.y = y;
+    DeviceGuard guard(h->cfg.device);
+    if (!guard.ok) return fail(h, AA_ERR_CUDA, "cannot select device %d", h->cfg.device);
+    const cudaError_t e = launch_norm(h->cfg.dtype, a, h->sm_count, (cudaStream_t)stream);
+    if (e != cudaSuccess) return fail(h, AA_ERR_CUDA, "layer norm launch failed: %s", cudaGetErrorString(e));
+    h->launches = 1;
+    return AA_OK;
+}
+
+size_t agent_attn_layer_norm_workspace_bytes(const agent_attn_handle* h, long long rows, int channels) {
+    if (!h || rows <= 0 || rows > INT_MAX || channels <= 0 || channels > 65536) return 0;
+    return norm_backward_bytes(h->cfg.dtype, rows, channels, h->sm_count);
+}
+
+int agent_attn_layer_norm_backward(agent_attn_handle* h, const agent_attn_layer_norm_args* s, const void* d_y, void* dx, float* d_weight, float* d_bias,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+    if (!h) return AA_ERR_INVALID_ARG;
+    h->err[0] = 0;
+    NormArgs a;
+    if (int rc = norm_args(h, s, &a)) return rc;
+    if (!d_y || (!dx && !d_weight && !d_bias)) return fail(h, AA_ERR_INVALID_ARG, "null pointer");
+    if (off_elements(h, a.x) || off_elements(h, a.w) || off_elements(h, d_y) || off_elements(h, dx) || ((reinterpret_cast<uintptr_t>(d_weight) | reinterpret_cast<uintptr_t>(d_bias)) & 3u))
+        return fail(h, AA_ERR_INVALID_ARG, "pointers must be aligned to their elements");
+    if (dx == a.x || (dx && dx == a.w)) return fail(h, AA_ERR_INVALID_ARG, "a gradient buffer aliases an input");
+    if (d_weight || d_bias) {
+        const size_t need = norm_backward_bytes(h->cfg.dtype, a.rows, a.C, h->sm_count);
+        if (!workspace || need > workspace_bytes) return fail(h, AA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, need);
+        if (misaligned(workspace)) return fail(h, AA_ERR_INVALID_ARG, "pointers must be 16-byte aligned");
+        a.ws = static_cast<float*>(workspace);
+    }
+    a.b = nullptr; a.dy = d_y; a.dx = dx; a.dw = d_weight; a.db = d_bias;
+    DeviceGuard guard(h->cfg.device);
+    if (!guard.ok) return fail(h, AA_ERR_CUDA, "cannot select device %d", h->cfg.device);
+    int launches = 0;
+    const cudaError_t e = launch_norm_backward(h->cfg.dtype, a, h->sm_count, (cudaStream_t)stream, &launches);
+    if (e != cudaSuccess) return fail(h, AA_ERR_CUDA, "layer norm gradient launch failed: %s", cudaGetErrorString(e));
+    h->launches = launches;
+    return AA_OK;
+}
+
 // A call on host buffers is bound by its copies (56 x 56 grid, 64 slabs: 78 MB in, 26 MB out, 1.98 ms in one piece).  It is cut into
 // parts along the batch, or along the heads of a single batch entry: the copies in, the kernels and the copies out of different
 // parts overlap, and what follows the last copy in is the work of the last part.  So parts halve: a half, a quarter, two eighths (few

@@ -1,0 +1,624 @@
+// Softmax attention over whole sequences on mma.sync: fp32 tensors as sums of three bf16 terms, and few queries over many keys in any type.
+//
+// A row is a query of one head; the heads that share keys stand side by side (row = query * group + head), so that single tokens fill a tile's rows
+// with their heads.  Forward: WR warps own 16 rows each, WK of them share the rows and take turns at blocks of 32 keys; logits, probabilities and
+// results stay in registers, the softmax keeps a running maximum and sum in fp32.  One kernel serves both directions of the gradient, too: rows
+// are queries (dQ) or keys (dK, dV, whose columns are the queries of all heads of the group, so no share of theirs is added up elsewhere).
+//
+// fp32: a product of two numbers is six products of their terms (what is left out is below 2^-24), small ones first; sums over the columns leave the
+// tensor core after 32 of them and join in fp32 registers, since its accumulators cut off what lies below the last bit.
+//
+// Few rows on a long axis: shares of `chunk` keys a block, whose states (maximum, sum, result) a second kernel joins in order.  Bound by HBM then.
+#include "attend.cuh"
+#include "bwd_terms.cuh"
+
+#include <algorithm>
+
+namespace aa {
+
+namespace {
+
+template <typename T> struct Oper { using E = T; static constexpr int kTerms = 1; };
+template <> struct Oper<float> { using E = __nv_bfloat16; static constexpr int kTerms = 3; };
+
+// `count` rows of DK channels (d of them exist, the others are zero) -> planes of terms at `dst`; row(i): address or null (zeros)
+template <typename T, int DK, int THREADS, typename F> __device__ __forceinline__ void load_tile(unsigned char* dst, uint32_t plane, int count, int d, const void* some, F row) {
+    constexpr int kPitch = TileGeom<DK>::kPitch, kGroups = DK / 8;
+    for (int i = threadIdx.x; i < count * kGroups; i += THREADS) {
+        const int r = i / kGroups, c = i % kGroups * 8;
+        const T* src = row(r);
+        unsigned char* to = dst + r * kPitch + c * 2;
+        if constexpr (sizeof(T) == 2) {
+            cp_async16(to, src && c < d ? src + c : some, src && c < d ? 16 : 0);      // (d is a multiple of 8; of no bytes nothing is read)
+        } else {
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+            if (src && c < d) a = __ldg(reinterpret_cast<const float4*>(src + c));
+            if (src && c + 4 < d) b = __ldg(reinterpret_cast<const float4*>(src + c + 4));
+            const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            uint32_t w[3][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint32_t t[3];
+                split_pair<__nv_bfloat16, 3>(f[2 * k], f[2 * k + 1], t);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) w[n][k] = t[n];
+            }
+#pragma unroll
+            for (int n = 0; n < 3; ++n) *reinterpret_cast<uint4*>(to + n * plane) = make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
+        }
+    }
+}
+
+// s (16 x 32) = rows . columns^T; a, b: this lane's ldmatrix addresses of the warp's rows and of the block of 32 column rows
+template <typename E, int NT, int DK> __device__ __forceinline__ void block_logits(float (&s)[4][4], uint32_t a, uint32_t a_plane, uint32_t b, uint32_t b_plane) {
+    constexpr int P = TileGeom<DK>::kPitch;
+    float small[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[j][e] = small[j][e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < DK / 16; ++ks) {
+        uint32_t x[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) ldsm4(x[n], a + n * a_plane + ks * 32);
+#pragma unroll
+        for (int j2 = 0; j2 < 2; ++j2) {
+            uint32_t y[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) ldsm4(y[n], b + n * b_plane + j2 * 16 * P + ks * 32);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int sum = NT - 1; sum >= 0; --sum)
+#pragma unroll
+                    for (int n = 0; n <= sum; ++n) mma_acc<E>(sum ? small[2 * j2 + e] : s[2 * j2 + e], x[sum - n], y[n][2 * e], y[n][2 * e + 1]);
+        }
+    }
+    if constexpr (NT > 1) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[j][e] += small[j][e];
+    }
+}
+// acc (16 x DK) += p (16 x 32, as terms) . columns; b: this lane's transposing ldmatrix address
+template <typename E, int NT, int DK> __device__ __forceinline__ void block_product(float (&acc)[DK / 8][4], const uint32_t (&p)[NT][2][4], uint32_t b, uint32_t b_plane) {
+    constexpr int P = TileGeom<DK>::kPitch;
+#pragma unroll
+    for (int c = 0; c < DK / 16; ++c) {
+        float t[2][4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[e][i] = 0.f;
+        uint32_t y[NT][2][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) ldsm4t(y[n][ks], b + n * b_plane + ks * 16 * P + c * 32);
+#pragma unroll
+        for (int sum = NT - 1; sum >= 0; --sum)
+#pragma unroll
+            for (int n = 0; n <= sum; ++n)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) mma_acc<E>(t[e], p[sum - n][ks], y[n][ks][2 * e], y[n][ks][2 * e + 1]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[2 * c + e][i] += t[e][i];
+    }
+}
+// 16 x 32 fp32 numbers in accumulator layout -> terms as an A operand
+template <typename E, int NT> __device__ __forceinline__ void block_operand(const float (&s)[4][4], uint32_t (&p)[NT][2][4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t w[NT];
+            split_pair<E, NT>(s[j][2 * h], s[j][2 * h + 1], w);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) p[n][j >> 1][(j & 1) * 2 + h] = w[n];
+        }
+}
+// Values that are not finite, in a block of which some rows see only a part: zero in shared memory (0 * infinity is NaN), and first_bad keeps
+// for every channel the first key that has one, so that the rows that do see it become NaN at the end.
+template <typename E, int NT, int DK, int THREADS> __device__ void clean_values(unsigned char* v, uint32_t plane, int keys, int k0, int* first_bad) {
+    constexpr int kPitch = TileGeom<DK>::kPitch;
+    for (int i = threadIdx.x; i < keys * DK; i += THREADS) {
+        E* at = reinterpret_cast<E*>(v + i / DK * kPitch) + i % DK;
+        bool bad = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) bad |= !(fabsf(Elem<E>::to_f32(*reinterpret_cast<E*>(reinterpret_cast<unsigned char*>(at) + n * plane))) < INFINITY);
+        if (bad) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) *reinterpret_cast<E*>(reinterpret_cast<unsigned char*>(at) + n * plane) = Elem<E>::from_f32(0.f);
+            atomicMin(first_bad + i % DK, k0 + i / DK);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ forward
+template <typename T, int DK, int WR, int WK> struct RowsGeom {
+    static constexpr int NT = Oper<T>::kTerms, kRows = 16 * WR, kStep = 32 * WK, kThreads = 32 * WR * WK, kPitch = TileGeom<DK>::kPitch;
+    static constexpr int kStages = NT > 1 ? 1 : 3;
+    static constexpr uint32_t kQPlane = kRows * kPitch, kPlane = kStep * kPitch, kStage = 2 * NT * kPlane;
+    static constexpr int kJoin = WK > 1 ? WK * kRows * (DK + 4) * 4 : 0;                  // states of the warps that share rows
+    static constexpr int kRing = kStages * (int)kStage > kJoin ? kStages * (int)kStage : kJoin;
+    static constexpr int kSmem = NT * (int)kQPlane + kRing + DK * 4;
+};
+
+// Partial state of a row and share: [row of the tensor][share]: maximum (log2 units) and sum; results behind them
+__device__ __forceinline__ long long row_index(const AttendArgs& a, const Span& q, int token, int head) {
+    return ((long long)q.batch * a.N + q.first + token) * a.heads + head;
+}
+
+template <typename T, int DK, int WR, int WK>
+__global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
+    using G = RowsGeom<T, DK, WR, WK>;
+    using E = typename Oper<T>::E;
+    constexpr int NT = G::NT, P = G::kPitch;
+    extern __shared__ __align__(128) unsigned char smem[];
+    unsigned char* ring = smem + NT * G::kQPlane;
+    int* first_bad = reinterpret_cast<int*>(smem + NT * G::kQPlane + G::kRing);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wr = warp % WR, wk = warp / WR, g = lane >> 2, t = lane & 3;
+    const int group = a.heads / a.kv_heads, hk = blockIdx.y;
+    int seq, tile;
+    if (!find_slot(a.q_offsets, a.sequences, a.N, group, G::kRows, blockIdx.x, &seq, &tile)) return;
+    const Span q = span_of(a.q_offsets, a.q_lengths, a.N, seq), k = span_of(a.k_offsets, a.k_lengths, a.M, seq);
+    const int rows = q.count * group, row0 = tile * G::kRows;      // (the host refuses more than 31 bits of them)
+    if (row0 >= rows) return;
+    const int last = min(rows, row0 + G::kRows) - 1;
+    const int k_all = visible_keys(a.causal, last / group, q.count, k.count);            // of the tile's last query
+    const int share = blockIdx.z, begin = (int)min((long long)k_all, (long long)share * a.chunk);
+    const int end = (int)min((long long)k_all, (long long)begin + a.chunk);
+    if (share > 0 && begin >= k_all) return;
+    const int k_whole = visible_keys(a.causal, row0 / group, q.count, k.count);    // keys that every row sees
+
+    const T* kp = static_cast<const T*>(a.k) + k.batch * a.lk.sb + hk * a.lk.sh + (long long)k.first * a.lk.st;
+    const T* vp = static_cast<const T*>(a.v) + k.batch * a.lv.sb + hk * a.lv.sh + (long long)k.first * a.lv.st;
+    load_tile<T, DK, G::kThreads>(smem, G::kQPlane, G::kRows, a.d, a.q, [&](int r) -> const T* {
+        const int i = row0 + r;
+        return i < rows ? static_cast<const T*>(a.q) + q.batch * a.lq.sb + (hk * group + i % group) * a.lq.sh + (long long)(q.first + i / group) * a.lq.st : nullptr;
+    });
+    for (int c = tid; c < DK; c += G::kThreads) first_bad[c] = INT_MAX;
+    const int steps = (end - begin + G::kStep - 1) / G::kStep;
+    auto fetch = [&](int s) {
+        unsigned char* to = ring + (s % G::kStages) * G::kStage;
+        const int k0 = begin + s * G::kStep;
+        load_tile<T, DK, G::kThreads>(to, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return k0 + r < end ? kp + (long long)(k0 + r) * a.lk.st : nullptr; });
+        load_tile<T, DK, G::kThreads>(to + NT * G::kPlane, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return k0 + r < end ? vp + (long long)(k0 + r) * a.lv.st : nullptr; });
+    };
+    if (G::kStages > 1) {
+#pragma unroll
+        for (int s = 0; s < G::kStages - 1; ++s) {
+            if (s < steps) fetch(s);
+            cp_async_commit();
+        }
+    }
+
+    int limit[2], row[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        row[h] = row0 + wr * 16 + g + 8 * h;
+        limit[h] = row[h] < rows ? min(end, visible_keys(a.causal, row[h] / group, q.count, k.count)) : 0;
+    }
+    const float c1 = a.scale * kLog2e;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[DK / 8][4];
+#pragma unroll
+    for (int c = 0; c < DK / 8; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[c][e] = 0.f;
+    const uint32_t qa = smem_u32(smem) + wr * 16 * P + val_lane_offset<DK>(lane);
+
+    for (int s = 0; s < steps; ++s) {
+        if (G::kStages > 1) {
+            cp_async_wait<(G::kStages > 1 ? G::kStages - 2 : 0)>();
+            __syncthreads();
+            if (s + G::kStages - 1 < steps) fetch(s + G::kStages - 1);
+            cp_async_commit();
+        } else {
+            if (s) __syncthreads();
+            fetch(s);
+            __syncthreads();
+        }
+        unsigned char* stage = ring + (s % G::kStages) * G::kStage;
+        const int block0 = begin + s * G::kStep;
+        if (block0 + G::kStep > k_whole) {
+            clean_values<E, NT, DK, G::kThreads>(stage + NT * G::kPlane, G::kPlane, min(G::kStep, end - block0), block0, first_bad);
+            __syncthreads();
+        }
+        const int k0 = block0 + wk * 32;
+        if (k0 >= end) continue;                   // (warp-uniform; the barriers above are met by all)
+        const uint32_t kb = smem_u32(stage) + wk * 32 * P;
+        float x[4][4];
+        block_logits<E, NT, DK>(x, qa, G::kQPlane, kb + key_lane_offset<DK>(lane), G::kPlane);
+        if (k0 + 32 > min(limit[0], limit[1])) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (k0 + 8 * j + 2 * t + (e & 1) >= limit[e >> 1]) x[j][e] = -INFINITY;
+        }
+        float f[2], base[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float n = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) n = max3(n, x[j][2 * h], x[j][2 * h + 1]);
+            n = fmaxf(m[h], quad_max(n) * c1);
+            base[h] = n == -INFINITY ? 0.f : n;                          // (no visible key so far)
+            f[h] = m[h] == -INFINITY ? 0.f : fast_exp2(m[h] - base[h]);
+            m[h] = n;
+            l[h] *= f[h];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[j][e] = fast_exp2(fmaf(x[j][e], c1, -base[e >> 1]));
+                l[e >> 1] += x[j][e];
+            }
+#pragma unroll
+        for (int c = 0; c < DK / 8; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][e] *= f[e >> 1];
+        uint32_t p[NT][2][4];
+        block_operand<E, NT>(x, p);
+        block_product<E, NT, DK>(o, p, kb + NT * G::kPlane + val_lane_offset<DK>(lane), G::kPlane);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) l[h] = quad_sum(l[h]);
+    const bool whole = gridDim.z == 1;
+    __syncthreads();                               // (first_bad is complete; the ring may be written)
+    // one row's channels, once its state is known
+    auto finish = [&](int r, int c, float v0, float v1, float sum, float top) {
+        const int token = r / group, head = hk * group + r % group, lim = min(end, visible_keys(a.causal, token, q.count, k.count));
+        if (first_bad[c] < lim) v0 = NAN;
+        if (first_bad[c + 1] < lim) v1 = NAN;
+        if (whole) {
+            const float inv = lim > 0 ? 1.f / sum : 0.f;
+            T* to = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + token) * a.lo.st + c;
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(to) = pack2<T>(v0 * inv, v1 * inv);
+            else *reinterpret_cast<float2*>(to) = make_float2(v0 * inv, v1 * inv);
+            if (c == 0 && a.lse) a.lse[((long long)q.batch * a.heads + head) * a.N + q.first + token] = lim > 0 ? (top + log2f(sum)) * kLn2 : -INFINITY;
+        } else {
+            const long long at = row_index(a, q, token, head) * gridDim.z + share, all = (long long)a.batch * a.N * a.heads * gridDim.z;
+            *reinterpret_cast<float2*>(a.ws + (2 * all + 3) / 4 * 4 + at * a.d + c) = make_float2(v0, v1);
+            if (c == 0) *reinterpret_cast<float2*>(a.ws + 2 * at) = make_float2(top, sum);
+        }
+    };
+    if constexpr (WK == 1) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (row[h] >= rows) continue;
+#pragma unroll
+            for (int c = 0; c < DK / 8; ++c)
+                if (8 * c + 2 * t < a.d) finish(row[h], 8 * c + 2 * t, o[c][2 * h], o[c][2 * h + 1], l[h], m[h]);
+        }
+    } else {
+        float* join = reinterpret_cast<float*>(ring);                    // [WK][rows][DK + 4]: results, maximum, sum
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float* to = join + (wk * G::kRows + wr * 16 + g + 8 * h) * (DK + 4);
+#pragma unroll
+            for (int c = 0; c < DK / 8; ++c) *reinterpret_cast<float2*>(to + 8 * c + 2 * t) = make_float2(o[c][2 * h], o[c][2 * h + 1]);
+            if (t == 0) { to[DK] = m[h]; to[DK + 1] = l[h]; }
+        }
+        __syncthreads();
+        for (int i = tid; i < G::kRows * (DK / 2); i += G::kThreads) {
+            const int r = i / (DK / 2), c = i % (DK / 2) * 2;
+            if (row0 + r >= rows || c >= a.d) continue;
+            float top = -INFINITY, sum = 0.f, v0 = 0.f, v1 = 0.f;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) top = fmaxf(top, join[(w * G::kRows + r) * (DK + 4) + DK]);
+            const float b = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                const float* s = join + (w * G::kRows + r) * (DK + 4);
+                const float f = fast_exp2(s[DK] - b);
+                sum = fmaf(f, s[DK + 1], sum);
+                v0 = fmaf(f, s[c], v0);
+                v1 = fmaf(f, s[c + 1], v1);
+            }
+            finish(row0 + r, c, v0, v1, sum, top);
+        }
+    }
+}
+
+// Joins the states of a row's shares in order; a warp takes a row, a lane four channels.
+template <typename T, int ROWS> __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a, int shares) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = a.heads / a.kv_heads, hk = blockIdx.y;
+    int seq, tile;
+    if (!find_slot(a.q_offsets, a.sequences, a.N, group, ROWS, blockIdx.x, &seq, &tile)) return;
+    const Span q = span_of(a.q_offsets, a.q_lengths, a.N, seq), k = span_of(a.k_offsets, a.k_lengths, a.M, seq);
+    const int rows = q.count * group, row0 = tile * ROWS;
+    if (row0 >= rows) return;
+    const int last = min(rows, row0 + ROWS) - 1, k_all = visible_keys(a.causal, last / group, q.count, k.count);
+    const int live = max(1, (int)((k_all + (long long)a.chunk - 1) / a.chunk));
+    const long long all = (long long)a.batch * a.N * a.heads * shares;
+    for (int r = row0 + warp; r <= last; r += 4) {
+        const int token = r / group, head = hk * group + r % group;
+        const long long at = row_index(a, q, token, head) * shares;
+        const float2* state = reinterpret_cast<const float2*>(a.ws) + at;
+        float top = -INFINITY;
+        for (int s = lane; s < live; s += 32) top = fmaxf(top, state[s].x);
+#pragma unroll
+        for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
+        const float b = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float* acc = a.ws + (2 * all + 3) / 4 * 4 + at * a.d + 4 * lane;
+        const bool mine = 4 * lane < a.d;
+#pragma unroll 4
+        for (int s = 0; s < live; ++s) {
+            const float2 st = state[s];
+            const float f = fast_exp2(st.x - b);
+            const float4 w = mine ? *reinterpret_cast<const float4*>(acc + (long long)s * a.d) : v;
+            sum = fmaf(f, st.y, sum);
+            v.x = fmaf(f, w.x, v.x); v.y = fmaf(f, w.y, v.y); v.z = fmaf(f, w.z, v.z); v.w = fmaf(f, w.w, v.w);
+        }
+        const bool some = visible_keys(a.causal, token, q.count, k.count) > 0;
+        const float inv = some ? 1.f / sum : 0.f;
+        if (mine) {
+            T* to = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + token) * a.lo.st + 4 * lane;
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2<T>(v.x * inv, v.y * inv), pack2<T>(v.z * inv, v.w * inv));
+            else *reinterpret_cast<float4*>(to) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+        }
+        if (lane == 0 && a.lse) a.lse[((long long)q.batch * a.heads + head) * a.N + q.first + token] = some ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    }
+}
+
+template <typename T, int DK, int WR, int WK> cudaError_t run_rows(const AttendArgs& a, int shares, cudaStream_t st) {
+    using G = RowsGeom<T, DK, WR, WK>;
+    static std::atomic<unsigned long long> done{0};
+    if (cudaError_t e = allow_smem(attend_rows_kernel<T, DK, WR, WK>, done, G::kSmem)) return e;
+    const long long slots = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, G::kRows);
+    attend_rows_kernel<T, DK, WR, WK><<<dim3((unsigned)slots, a.kv_heads, shares), G::kThreads, G::kSmem, st>>>(a);
+    if (cudaError_t e = cudaGetLastError()) return e;
+    if (shares > 1) {
+        attend_join_kernel<T, G::kRows><<<dim3((unsigned)slots, a.kv_heads), 128, 0, st>>>(a, shares);
+        return cudaGetLastError();
+    }
+    return cudaSuccess;
+}
+
+// Few rows a sequence: sixteen of them a block, whose four warps take turns at the keys.
+bool few_rows(const AttendArgs& a) {
+    const long long rows = (long long)a.N * (a.heads / a.kv_heads), sequences = a.q_offsets ? a.sequences : 1;
+    return rows <= 16 * sequences;
+}
+// Shares of the keys where blocks are too few to fill the GPU
+int shares_of(const AttendArgs& a, int sm_count, int* chunk) {
+    *chunk = std::max(1, a.M);
+    if (!few_rows(a)) return 1;
+    const long long blocks = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, 16) * a.kv_heads;
+    const long long want = std::max(1LL, 6LL * sm_count / blocks);
+    long long c = (a.M + want - 1) / want;
+    c = std::max(256LL, (c + 127) / 128 * 128);
+    *chunk = (int)std::min<long long>(c, a.M);
+    return (a.M + *chunk - 1) / *chunk;
+}
+
+template <typename T> cudaError_t rows_of_type(const AttendArgs& a, int shares, cudaStream_t st) {
+    const bool few = few_rows(a);
+    if (a.d <= 32) return few ? run_rows<T, 32, 1, 4>(a, shares, st) : run_rows<T, 32, 4, 1>(a, shares, st);
+    if (a.d <= 64) return few ? run_rows<T, 64, 1, 4>(a, shares, st) : run_rows<T, 64, 4, 1>(a, shares, st);
+    if (a.d <= 96) return few ? run_rows<T, 96, 1, 4>(a, shares, st) : run_rows<T, 96, 4, 1>(a, shares, st);
+    return few ? run_rows<T, 128, 1, 4>(a, shares, st) : run_rows<T, 128, 4, 1>(a, shares, st);
+}
+
+// ------------------------------------------------------------------------------------------------ backward
+// (log2-sum-exp, D) of every row of a sequence, eight lanes a row, and for f16 what the powers of two that hold small gradients are made of: the norm of
+// every row of dO, the largest of a sequence and head of keys, and the largest of the rows of V (blocks past the first `q_slots`).
+template <typename T> __global__ void __launch_bounds__(256) attend_dot_kernel(const __grid_constant__ AttendArgs a, unsigned q_slots) {
+    constexpr int V = Elem<T>::kVec;
+    constexpr bool kNorms = is_f16<T>;
+    const int group = a.heads / a.kv_heads, hk = blockIdx.y, lane8 = threadIdx.x & 7;
+    const bool values = blockIdx.x >= q_slots;
+    int seq, tile;
+    if (!(values ? find_slot(a.k_offsets, a.sequences, a.M, 1, kDotRows, blockIdx.x - q_slots, &seq, &tile)
+                 : find_slot(a.q_offsets, a.sequences, a.N, group, kDotRows, blockIdx.x, &seq, &tile))) return;
+    const Span r = values ? span_of(a.k_offsets, a.k_lengths, a.M, seq) : span_of(a.q_offsets, a.q_lengths, a.N, seq);
+    const int rows = r.count * (values ? 1 : group), first = tile * kDotRows;
+    if (first >= rows) return;
+    float most = 0.f;
+    for (int i = first + (threadIdx.x >> 3); i < min(rows, first + kDotRows); i += 32) {       // (lanes of a row stay together)
+        const int head = values ? hk : hk * group + i % group, at = r.first + (values ? i : i / group);
+        const T* g = values ? static_cast<const T*>(a.v) + r.batch * a.lv.sb + head * a.lv.sh + (long long)at * a.lv.st
+                            : static_cast<const T*>(a.dout) + r.batch * a.ldo.sb + head * a.ldo.sh + (long long)at * a.ldo.st;
+        const T* o = values ? g : static_cast<const T*>(a.out) + r.batch * a.lo.sb + head * a.lo.sh + (long long)at * a.lo.st;
+        float sum = 0.f, square = 0.f;
+        for (int c = lane8 * V; c < a.d; c += 8 * V) {
+            float x[V], y[V];
+            unpack16<T>(__ldg(reinterpret_cast<const uint4*>(g + c)), x);
+            unpack16<T>(__ldg(reinterpret_cast<const uint4*>(o + c)), y);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                sum = fmaf(x[e], y[e], sum);
+                square = fmaf(x[e], x[e], square);
+            }
+        }
+        const unsigned mask = 0xffu << (threadIdx.x & 24);
+#pragma unroll
+        for (int e = 4; e; e >>= 1) {
+            sum += __shfl_xor_sync(mask, sum, e);
+            if (kNorms) square += __shfl_xor_sync(mask, square, e);
+        }
+        if (lane8 == 0) {
+            if (!values) {
+                const long long row = ((long long)r.batch * a.heads + head) * a.N + at;
+                reinterpret_cast<float2*>(a.ws)[row] = make_float2(a.lse[row] * kLog2e, sum);
+                if (kNorms) grad_norms(a)[row] = sqrtf(square);
+            }
+            if (square < INFINITY) most = fmaxf(most, sqrtf(square));
+        }
+    }
+    if (kNorms && most > 0.f) atomicMax(grad_most(a, seq, hk) + (values ? 1 : 0), __float_as_uint(most));      // (positive numbers keep their order; any order of arrival)
+}
+
+template <typename T, int DK> struct GradGeom {
+    static constexpr int NT = Oper<T>::kTerms, kRows = 64, kStep = 32, kPitch = TileGeom<DK>::kPitch;
+    static constexpr uint32_t kRowPlane = kRows * kPitch, kPlane = kStep * kPitch;
+    static constexpr int kSmem = 2 * NT * (int)(kRowPlane + kPlane) + kStep * 8;
+};
+
+// KEYS: rows are keys (x = K, y = V), columns queries (u = Q, w = dO); else rows are queries (x = Q, y = dO), columns keys (u = K, w = V).
+template <typename T, int DK, bool KEYS>
+__global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant__ AttendArgs a) {
+    using G = GradGeom<T, DK>;
+    using E = typename Oper<T>::E;
+    constexpr int NT = G::NT, P = G::kPitch;
+    extern __shared__ __align__(128) unsigned char smem[];
+    unsigned char *xs = smem, *ys = xs + NT * G::kRowPlane, *us = ys + NT * G::kRowPlane, *ws = us + NT * G::kPlane;
+    float2* stats = reinterpret_cast<float2*>(ws + NT * G::kPlane);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int group = a.heads / a.kv_heads, hk = blockIdx.y;
+    int seq, tile;
+    if (!find_slot(KEYS ? a.k_offsets : a.q_offsets, a.sequences, KEYS ? a.M : a.N, KEYS ? 1 : group, G::kRows, blockIdx.x, &seq, &tile)) return;
+    const Span q = span_of(a.q_offsets, a.q_lengths, a.N, seq), k = span_of(a.k_offsets, a.k_lengths, a.M, seq);
+    const int queries = q.count * group, rows = KEYS ? k.count : queries, row0 = tile * G::kRows;      // (the host refuses more than 31 bits of them)
+    if (row0 >= rows) return;
+    auto query = [&](const void* p, const TokLayout& l, int i) {
+        return static_cast<const T*>(p) + q.batch * l.sb + (hk * group + i % group) * l.sh + (long long)(q.first + i / group) * l.st;
+    };
+    auto key = [&](const void* p, const TokLayout& l, int j) { return static_cast<const T*>(p) + k.batch * l.sb + hk * l.sh + (long long)(k.first + j) * l.st; };
+    auto stat = [&](int i) {
+        return __ldg(reinterpret_cast<const float2*>(a.ws) + ((long long)q.batch * a.heads + hk * group + i % group) * a.N + q.first + i / group);
+    };
+    load_tile<T, DK, 128>(xs, G::kRowPlane, G::kRows, a.d, a.q, [&](int r) -> const T* { return row0 + r < rows ? (KEYS ? key(a.k, a.lk, row0 + r) : query(a.q, a.lq, row0 + r)) : nullptr; });
+    load_tile<T, DK, 128>(ys, G::kRowPlane, G::kRows, a.d, a.q, [&](int r) -> const T* { return row0 + r < rows ? (KEYS ? key(a.v, a.lv, row0 + r) : query(a.dout, a.ldo, row0 + r)) : nullptr; });
+    // columns that some row of the tile meets
+    int begin = 0, end;
+    if (KEYS) {
+        if (a.causal) begin = max(0, row0 - k.count + q.count) * group;
+        end = queries;
+    } else {
+        end = visible_keys(a.causal, ((min(rows, row0 + G::kRows) - 1) / group), q.count, k.count);
+    }
+    const float c1 = a.scale * kLog2e;
+    float kappa[2] = {1.f, 1.f};                   // f16: power of two that P (dP - D) is held times, over that of P
+    if (is_f16<T>) kappa[0] = kappa[1] = grad_factor(__uint_as_float(grad_most(a, seq, hk)[0]), __uint_as_float(grad_most(a, seq, hk)[1]));
+    int row[2], limit[2];                          // rows are queries: the keys that they see; keys: the first column that sees them
+    float2 st[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        row[h] = row0 + warp * 16 + g + 8 * h;
+        if (KEYS) {
+            limit[h] = row[h] >= rows ? INT_MAX : a.causal ? max(0, row[h] - k.count + q.count) * group : 0;
+        } else {
+            st[h] = row[h] < rows ? stat(row[h]) : make_float2(0.f, 0.f);
+            limit[h] = row[h] < rows ? visible_keys(a.causal, row[h] / group, q.count, k.count) : 0;
+            if (is_f16<T> && row[h] < rows)
+                kappa[h] = grad_factor(grad_norms(a)[((long long)q.batch * a.heads + hk * group + row[h] % group) * a.N + q.first + row[h] / group],
+                                       __uint_as_float(grad_most(a, seq, hk)[1]));
+        }
+    }
+    float acc[DK / 8][4], acc2[KEYS ? DK / 8 : 1][4];
+#pragma unroll
+    for (int c = 0; c < DK / 8; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            acc[c][e] = 0.f;
+            if (KEYS) acc2[c][e] = 0.f;
+        }
+    const uint32_t xa = smem_u32(xs) + warp * 16 * P + val_lane_offset<DK>(lane), ya = xa + (uint32_t)(ys - xs);
+    const uint32_t ub = smem_u32(us) + key_lane_offset<DK>(lane), wb = ub + (uint32_t)(ws - us);
+    const uint32_t ut = smem_u32(us) + val_lane_offset<DK>(lane), wt = ut + (uint32_t)(ws - us);
+    for (int c0 = begin; c0 < end; c0 += G::kStep) {
+        if (c0 != begin) __syncthreads();
+        load_tile<T, DK, 128>(us, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.q, a.lq, c0 + r) : key(a.k, a.lk, c0 + r)) : nullptr; });
+        load_tile<T, DK, 128>(ws, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.dout, a.ldo, c0 + r) : key(a.v, a.lv, c0 + r)) : nullptr; });
+        if (KEYS && tid < G::kStep) stats[tid] = c0 + tid < end ? stat(c0 + tid) : make_float2(0.f, 0.f);
+        cp_async_commit();
+        cp_async_wait<0>();
+        __syncthreads();
+        float x[4][4], y[4][4];
+        block_logits<E, NT, DK>(x, xa, G::kRowPlane, ub, G::kPlane);
+        block_logits<E, NT, DK>(y, ya, G::kRowPlane, wb, G::kPlane);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int c = 8 * j + 2 * t + (e & 1), h = e >> 1;
+                const float2 s = KEYS ? stats[c] : st[h];
+                const bool seen = KEYS ? c0 + c < end && c0 + c >= limit[h] : c0 + c < limit[h];
+                const float p = seen ? fast_exp2(fmaf(x[j][e], c1, (is_f16<T> ? kHeldP : 0) - s.x)) : 0.f;
+                x[j][e] = p;
+                y[j][e] = seen ? p * ((y[j][e] - s.y) * kappa[h]) : 0.f;
+            }
+        uint32_t w[NT][2][4];
+        block_operand<E, NT>(y, w);
+        block_product<E, NT, DK>(acc, w, ut, G::kPlane);
+        if constexpr (KEYS) {
+            block_operand<E, NT>(x, w);
+            block_product<E, NT, DK>(acc2, w, wt, G::kPlane);
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (row[h] >= rows) continue;
+        const float out_p = is_f16<T> ? kHeldBack : 1.f, out_s = a.scale * out_p / kappa[h];
+        auto put = [&](void* p, const TokLayout& l, int c, float v0, float v1) {
+            T* to = static_cast<T*>(p) + (KEYS ? k.batch * l.sb + hk * l.sh + (long long)(k.first + row[h]) * l.st : q.batch * l.sb + (hk * group + row[h] % group) * l.sh + (long long)(q.first + row[h] / group) * l.st) + c;
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(to) = pack2<T>(v0, v1);
+            else *reinterpret_cast<float2*>(to) = make_float2(v0, v1);
+        };
+#pragma unroll
+        for (int c = 0; c < DK / 8; ++c) {
+            if (8 * c + 2 * t >= a.d) continue;
+            put(KEYS ? a.dk : a.dq, KEYS ? a.ldk : a.ldq, 8 * c + 2 * t, acc[c][2 * h] * out_s, acc[c][2 * h + 1] * out_s);
+            if constexpr (KEYS) put(a.dv, a.ldv, 8 * c + 2 * t, acc2[c][2 * h] * out_p, acc2[c][2 * h + 1] * out_p);
+        }
+    }
+}
+
+template <typename T, int DK, bool KEYS> cudaError_t run_grad(const AttendArgs& a, cudaStream_t st) {
+    using G = GradGeom<T, DK>;
+    static std::atomic<unsigned long long> done{0};
+    if (cudaError_t e = allow_smem(attend_grad_kernel<T, DK, KEYS>, done, G::kSmem)) return e;
+    const long long slots = KEYS ? slots_of(a.k_offsets != nullptr, a.sequences, a.M, 1, G::kRows) : slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, G::kRows);
+    attend_grad_kernel<T, DK, KEYS><<<dim3((unsigned)slots, a.kv_heads), 128, G::kSmem, st>>>(a);
+    return cudaGetLastError();
+}
+template <typename T, int DK> cudaError_t run_grads(const AttendArgs& a, cudaStream_t st) {
+    if (cudaError_t e = run_grad<T, DK, true>(a, st)) return e;
+    return run_grad<T, DK, false>(a, st);
+}
+template <typename T> cudaError_t grads_of_type(const AttendArgs& a, cudaStream_t st) {
+    const long long q_slots = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, kDotRows);
+    const long long v_slots = is_f16<T> ? slots_of(a.k_offsets != nullptr, a.sequences, a.M, 1, kDotRows) : 0;
+    if (is_f16<T>)
+        if (cudaError_t e = cudaMemsetAsync(grad_most(a, 0, 0), 0, (size_t)a.sequences * a.kv_heads * 2 * sizeof(unsigned), st)) return e;
+    attend_dot_kernel<T><<<dim3((unsigned)(q_slots + v_slots), a.kv_heads), 256, 0, st>>>(a, (unsigned)q_slots);
+    if (cudaError_t e = cudaGetLastError()) return e;
+    if (a.d <= 32) return run_grads<T, 32>(a, st);
+    if (a.d <= 64) return run_grads<T, 64>(a, st);
+    if (a.d <= 96) return run_grads<T, 96>(a, st);
+    return run_grads<T, 128>(a, st);
+}
+
+}  // namespace
+
+size_t attend_workspace(int dtype, const AttendArgs& a, int sm_count) {
+    int chunk;
+    const int shares = shares_of(a, sm_count, &chunk);
+    return shares > 1 ? (size_t)a.batch * a.N * a.heads * shares * (a.d + 2) * sizeof(float) + 16 : 0;
+}
+size_t attend_backward_workspace(int dtype, const AttendArgs& a, int sm_count) {
+    return (size_t)a.batch * a.N * a.heads * sizeof(float) * (dtype == 2 ? 3 : 2) + (dtype == 2 ? (size_t)a.sequences * a.kv_heads * 2 * sizeof(unsigned) : 0);
+}
+
+cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st, int* launches) {
+    const int shares = shares_of(a, sm_count, &a.chunk);
+    *launches = shares > 1 ? 2 : 1;
+    return dtype == 0 ? rows_of_type<float>(a, shares, st) : dtype == 1 ? rows_of_type<__nv_bfloat16>(a, shares, st) : rows_of_type<__half>(a, shares, st);
+}
+cudaError_t launch_attend_backward(int dtype, const AttendArgs& a, int sm_count, cudaStream_t st, int* launches) {
+    *launches = 3;
+    return dtype == 0 ? grads_of_type<float>(a, st) : dtype == 1 ? grads_of_type<__nv_bfloat16>(a, st) : grads_of_type<__half>(a, st);
+}
+
+}  // namespace aa

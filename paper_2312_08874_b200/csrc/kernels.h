@@ -363,4 +363,46 @@ struct GatedCall {
 size_t gated_bytes(int dtype, int M, int C, int F, bool backward, bool two_terms, int sm_count);
 cudaError_t launch_gated(int dtype, const GatedCall& c, cudaStream_t st, int* launches);
 
+// Softmax attention over whole sequences (attend.cu, attend_umma.cu)
+struct AttendArgs {
+    const void *q, *k, *v;
+    TokLayout lq, lk, lv;                 // strides in elements
+    void* out;                            // forward: result; backward: the forward call's
+    TokLayout lo;
+    float* lse;                           // [batch][heads][N] natural log-sum-exp, or null (forward)
+    const void* dout;
+    TokLayout ldo;
+    void *dq, *dk, *dv;
+    TokLayout ldq, ldk, ldv;
+    float* ws;                            // forward: partial states; backward: (log2-sum-exp, D) of every row
+    const int *q_offsets, *k_offsets;     // packed
+    const int *q_lengths, *k_lengths;     // dense
+    int batch, heads, kv_heads, N, M, d;
+    int sequences;                        // = batch without offsets
+    int causal;
+    float scale;
+    int chunk;                            // keys of a block's share (forward; M: all)
+    int* status;
+};
+size_t attend_workspace(int dtype, const AttendArgs& a, int sm_count);            // (sets nothing; reads the sizes)
+cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st, int* launches);
+size_t attend_backward_workspace(int dtype, const AttendArgs& a, int sm_count);
+cudaError_t launch_attend_backward(int dtype, const AttendArgs& a, int sm_count, cudaStream_t st, int* launches);
+
+// Layer norm over the channels of every row (norm.cu)
+struct NormArgs {
+    const void *x, *w, *b;                // [rows][C], [C] or null, [C] or null
+    void* y;                              // forward: [rows][C]
+    const void* dy;                       // backward: gradient of y
+    void* dx;                             // [rows][C] or null
+    float *dw, *db;                       // [C] or null
+    float* ws;
+    long long rows;
+    int C;
+    float eps;
+};
+size_t norm_backward_bytes(int dtype, long long rows, int C, int sm_count);
+cudaError_t launch_norm(int dtype, const NormArgs& a, int sm_count, cudaStream_t st);
+cudaError_t launch_norm_backward(int dtype, const NormArgs& a, int sm_count, cudaStream_t st, int* launches);
+
 }  // namespace aa

@@ -1,0 +1,361 @@
+// Layer norm over the channels of a row, and its gradient.
+//
+//     y = (x - m) r w + b,  m = mean(x),  r = 1 / sqrt(mean((x - m)^2) + eps)
+//     xh = (x - m) r,  g = dy w:   dx = r (g - mean(g) - xh mean(g xh)),  dw = sum over rows of dy xh,  db = sum over rows of dy
+//
+// Bound by HBM: every row is read once (x; x and dy) and stays in registers for its sums, which are fp32 and taken about the mean.  TPR threads share a
+// row, so that a thread holds at most four vectors of 16 bytes: 4 to 32 lanes of a warp, which meet by shuffles, or a block of 128 or 512 threads.
+// Blocks walk rows with the gains in registers; the gains' gradients are summed there too, leave as one row of sums a block and are added in a
+// fixed order by a second launch.  Rows that are no whole vectors (channel counts, or addresses) go element by element, up to 8192 of them; rows that no
+// such share holds (more than that, or more than 16384 channels in whole vectors, 8192 in fp32) are read from memory, in practice from L2, for each of their sums.
+#include "common.cuh"
+#include "kernels.h"
+
+#include <algorithm>
+
+namespace aa {
+
+namespace {
+
+// V elements of a row <-> fp32
+template <typename T, int V> __device__ __forceinline__ void read_vec(const T* p, float* f) {
+    if constexpr (V == 1) f[0] = Elem<T>::to_f32(__ldg(p));
+    else unpack16<T>(__ldg(reinterpret_cast<const uint4*>(p)), f);
+}
+template <typename T, int V> __device__ __forceinline__ void write_vec(T* p, const float* f) {
+    if constexpr (V == 1) *p = Elem<T>::from_f32(f[0]);
+    else *reinterpret_cast<uint4*>(p) = pack16<T>(f);
+}
+
+// Sums over the TPR threads of a row; `part`: two rounds of shared memory for rows of several warps, taken in turns
+template <int TPR, int N> __device__ __forceinline__ void row_sums(float (&s)[N], float* part, int& turn) {
+#pragma unroll
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o; o >>= 1)
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[n] += __shfl_xor_sync(0xffffffffu, s[n], o);
+    if constexpr (TPR > 32) {
+        constexpr int W = TPR / 32;
+        float* p = part + turn * 2 * W;
+        turn ^= 1;
+        if ((threadIdx.x & 31) == 0)
+#pragma unroll
+            for (int n = 0; n < N; ++n) p[n * W + (threadIdx.x >> 5)] = s[n];
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            s[n] = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) s[n] += p[n * W + w];
+        }
+    }
+}
+
+// How a block's threads share rows
+template <int TPR> constexpr int kBlock = TPR > 32 ? TPR : 256;
+
+template <typename T, int TPR, int NV, int V, bool BACK>
+__global__ void __launch_bounds__(kBlock<TPR>, TPR == 512 ? 1 : BACK ? 2 : TPR > 32 ? 4 : 3) norm_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int THREADS = kBlock<TPR>, RPB = THREADS / TPR, F = NV * V;
+    extern __shared__ float sums[];                        // backward: [2][C]
+    __shared__ float part[TPR > 32 ? 4 * (TPR / 32) : 1];
+    const int tid = threadIdx.x, lane = tid % TPR, C = a.C;
+    const float inv = 1.f / (float)C;
+    int turn = 0;
+    float w[F], b[BACK ? 1 : F], dw[BACK ? F : 1], db[BACK ? F : 1];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int c = (v * TPR + lane) * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            w[v * V + e] = 1.f;
+            if (!BACK) b[v * V + e] = 0.f;
+        }
+        if (c < C && a.w) read_vec<T, V>(static_cast<const T*>(a.w) + c, w + v * V);
+        if (!BACK && c < C && a.b) read_vec<T, V>(static_cast<const T*>(a.b) + c, b + v * V);
+    }
+    if (BACK)
+#pragma unroll
+        for (int i = 0; i < F; ++i) dw[i] = db[i] = 0.f;
+    // (every thread of a block takes the same number of turns: shuffles and barriers are met by all)
+    for (long long r0 = (long long)blockIdx.x * RPB; r0 < a.rows; r0 += (long long)gridDim.x * RPB) {
+        const long long r = r0 + tid / TPR;
+        const bool live = r < a.rows;
+        const T* x = static_cast<const T*>(a.x) + r * C;
+        float f[F], g[BACK ? F : 1];
+        float s[1] = {0.f};
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * TPR + lane) * V;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                f[v * V + e] = 0.f;
+                if (BACK) g[v * V + e] = 0.f;
+            }
+            if (live && c < C) {
+                read_vec<T, V>(x + c, f + v * V);
+                if constexpr (BACK) read_vec<T, V>(static_cast<const T*>(a.dy) + r * C + c, g + v * V);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < F; ++i) s[0] += f[i];
+        row_sums<TPR, 1>(s, part, turn);
+        const float mean = s[0] * inv;
+        s[0] = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const bool in = (v * TPR + lane) * V < C;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float& z = f[v * V + e];
+                z = in ? z - mean : 0.f;
+                s[0] = fmaf(z, z, s[0]);
+            }
+        }
+        row_sums<TPR, 1>(s, part, turn);
+        const float rs = 1.f / sqrtf(s[0] * inv + a.eps);
+        if constexpr (!BACK) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * TPR + lane) * V;
+                float y[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = fmaf(f[v * V + e] * rs, w[v * V + e], b[v * V + e]);
+                if (live && c < C) write_vec<T, V>(static_cast<T*>(a.y) + r * C + c, y);
+            }
+        } else {
+            float t[2] = {0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                f[i] *= rs;
+                if (live) {                                // (a row that is none has r = 1 / sqrt(eps), which may be infinite)
+                    dw[i] = fmaf(g[i], f[i], dw[i]);
+                    db[i] += g[i];
+                }
+                g[i] *= w[i];
+                t[0] += g[i];
+                t[1] = fmaf(g[i], f[i], t[1]);
+            }
+            if (a.dx) {
+                row_sums<TPR, 2>(t, part, turn);
+                t[0] *= inv;
+                t[1] *= inv;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int c = (v * TPR + lane) * V;
+                    float y[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) y[e] = rs * (g[v * V + e] - t[0] - f[v * V + e] * t[1]);
+                    if (live && c < C) write_vec<T, V>(static_cast<T*>(a.dx) + r * C + c, y);
+                }
+            }
+        }
+    }
+    if constexpr (BACK) {
+        if (!a.ws) return;
+        // one row of sums a block: warps add theirs in turn
+        if constexpr (TPR < 32) {
+#pragma unroll
+            for (int o = TPR; o < 32; o <<= 1)
+#pragma unroll
+                for (int i = 0; i < F; ++i) {
+                    dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
+                    db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
+                }
+        }
+        float* out = a.ws + (long long)blockIdx.x * 2 * C;
+        constexpr int TURNS = TPR > 32 ? 1 : THREADS / 32;
+        for (int k = 0; k < TURNS; ++k) {
+            if (TURNS == 1 || (tid >> 5) == k) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const int c = (v * TPR + lane) * V + e, i = v * V + e;
+                        if (c >= C || (TPR < 32 && (tid & 31) >= TPR)) continue;
+                        const float p = k ? sums[c] + dw[i] : dw[i], q = k ? sums[C + c] + db[i] : db[i];
+                        if (k + 1 < TURNS) {
+                            sums[c] = p;
+                            sums[C + c] = q;
+                        } else {
+                            out[c] = p;
+                            out[C + c] = q;
+                        }
+                    }
+            }
+            if (TURNS > 1) __syncthreads();
+        }
+    }
+}
+
+// Rows of any length, a block each, read again for each sum.  Backward: dx, and (mean, r) of every row for the gains' gradients.
+template <typename T, bool BACK> __global__ void __launch_bounds__(512) norm_wide_kernel(const __grid_constant__ NormArgs a, float2* stats) {
+    __shared__ float part[4 * 16];
+    int turn = 0;
+    const int C = a.C;
+    const float inv = 1.f / (float)C;
+    for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const T* x = static_cast<const T*>(a.x) + r * C;
+        float s[1] = {0.f};
+        for (int c = threadIdx.x; c < C; c += 512) s[0] += Elem<T>::to_f32(x[c]);
+        row_sums<512, 1>(s, part, turn);
+        const float mean = s[0] * inv;
+        s[0] = 0.f;
+        for (int c = threadIdx.x; c < C; c += 512) {
+            const float z = Elem<T>::to_f32(x[c]) - mean;
+            s[0] = fmaf(z, z, s[0]);
+        }
+        row_sums<512, 1>(s, part, turn);
+        const float rs = 1.f / sqrtf(s[0] * inv + a.eps);
+        auto gain = [&](int c) { return a.w ? Elem<T>::to_f32(static_cast<const T*>(a.w)[c]) : 1.f; };
+        if constexpr (!BACK) {
+            for (int c = threadIdx.x; c < C; c += 512)
+                static_cast<T*>(a.y)[r * C + c] = Elem<T>::from_f32(fmaf((Elem<T>::to_f32(x[c]) - mean) * rs, gain(c), a.b ? Elem<T>::to_f32(static_cast<const T*>(a.b)[c]) : 0.f));
+        } else {
+            if (stats && threadIdx.x == 0) stats[r] = make_float2(mean, rs);
+            if (!a.dx) continue;
+            const T* dy = static_cast<const T*>(a.dy) + r * C;
+            float t[2] = {0.f, 0.f};
+            for (int c = threadIdx.x; c < C; c += 512) {
+                const float g = Elem<T>::to_f32(dy[c]) * gain(c);
+                t[0] += g;
+                t[1] = fmaf(g, (Elem<T>::to_f32(x[c]) - mean) * rs, t[1]);
+            }
+            row_sums<512, 2>(t, part, turn);
+            for (int c = threadIdx.x; c < C; c += 512)
+                static_cast<T*>(a.dx)[r * C + c] = Elem<T>::from_f32(rs * (Elem<T>::to_f32(dy[c]) * gain(c) - t[0] * inv - (Elem<T>::to_f32(x[c]) - mean) * rs * t[1] * inv));
+        }
+    }
+}
+// Sums of a run of rows for 256 columns
+template <typename T> __global__ void __launch_bounds__(256) norm_columns_kernel(const __grid_constant__ NormArgs a, const float2* stats, float* out) {
+    const int c = blockIdx.x * 256 + threadIdx.x, C = a.C;
+    const long long first = a.rows * blockIdx.y / gridDim.y, last = a.rows * (blockIdx.y + 1) / gridDim.y;
+    if (c >= C) return;
+    float p = 0.f, q = 0.f;
+    for (long long r = first; r < last; ++r) {
+        const float2 s = __ldg(stats + r);
+        const float g = Elem<T>::to_f32(static_cast<const T*>(a.dy)[r * C + c]);
+        p = fmaf(g, (Elem<T>::to_f32(static_cast<const T*>(a.x)[r * C + c]) - s.x) * s.y, p);
+        q += g;
+    }
+    out[(long long)blockIdx.y * 2 * C + c] = p;
+    out[(long long)blockIdx.y * 2 * C + C + c] = q;
+}
+// Rows of sums [shares][2][C] -> dw, db: 32 columns a block, every warp a run of shares, joined in order
+__global__ void __launch_bounds__(1024) norm_join_kernel(const float* __restrict__ in, int shares, int C, float* dw, float* db) {
+    __shared__ float part[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + lane;
+    float s = 0.f;
+    if (c < 2 * C)
+#pragma unroll 8
+        for (int k = shares * warp / 32; k < shares * (warp + 1) / 32; ++k) s += in[(long long)k * 2 * C + c];
+    part[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && c < 2 * C) {
+        s = 0.f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) s += part[k][lane];
+        float* out = c < C ? dw : db;
+        if (out) out[c < C ? c : c - C] = s;
+    }
+}
+
+constexpr int kColumnShares = 64;
+
+bool aligned16(const NormArgs& a) {
+    const void* const p[] = {a.x, a.w, a.b, a.y, a.dy, a.dx};
+    uintptr_t bits = 0;
+    for (const void* q : p) bits |= reinterpret_cast<uintptr_t>(q);
+    return bits % 16 == 0;
+}
+// How rows of C channels are shared: threads a row, vectors a thread, elements a vector; 0: norm_wide_kernel
+struct NormPlan {
+    int tpr, nv, v;
+};
+NormPlan plan_of(int dtype, int C, bool aligned) {
+    const int vec = dtype == 0 ? 4 : 8;
+    NormPlan p{0, 0, 0};
+    if (C % vec == 0 && aligned) {
+        const int n = C / vec;
+        p.v = vec;
+        // the fewest lanes that hold a row in two vectors each, three where that leaves none idle
+        for (int t : {4, 8, 16}) {
+            if (n <= 2 * t) { p.tpr = t; p.nv = n <= t ? 1 : 2; return p; }
+            if (n == 3 * t) { p.tpr = t; p.nv = 3; return p; }
+        }
+        for (int t : {32, 128, 512})
+            if (n <= 4 * t) { p.tpr = t; p.nv = (n + t - 1) / t; return p; }
+    } else {
+        p.v = 1;
+        for (int t : {8, 32, 128, 512})
+            if (C <= 16 * t) { p.tpr = t; p.nv = C <= 4 * t ? 4 : 16; return p; }
+    }
+    p.tpr = 0;
+    return p;
+}
+// Blocks that walk the rows: as many as run at once; with gains' gradients fewer where their rows of sums would cost more than the rows.
+long long blocks_of(const NormPlan& p, long long rows, int sm_count, bool back) {
+    const int rpb = p.tpr > 32 ? 1 : 256 / p.tpr;
+    const long long need = (rows + rpb - 1) / rpb, most = (long long)sm_count * (p.tpr == 512 ? 2 : p.tpr == 128 ? 8 : back ? 2 : 8);
+    return std::max(1LL, std::min(need, most));
+}
+
+template <typename T, int TPR, int NV, int V, bool BACK> cudaError_t run_norm(const NormArgs& a, const NormPlan& p, int sm_count, cudaStream_t st) {
+    const int smem = BACK && a.ws && TPR <= 32 ? 2 * a.C * 4 : 0;
+    norm_kernel<T, TPR, NV, V, BACK><<<(unsigned)blocks_of(p, a.rows, sm_count, BACK), kBlock<TPR>, smem, st>>>(a);
+    return cudaGetLastError();
+}
+template <typename T, bool BACK> cudaError_t norm_of(const NormArgs& a, int sm_count, cudaStream_t st) {
+    constexpr int V = Elem<T>::kVec;
+    const NormPlan p = plan_of(sizeof(T) == 4 ? 0 : 1, a.C, aligned16(a));
+#define AA_NORM(TPR, NV, VEC) if (p.tpr == TPR && p.nv == NV && p.v == VEC) return run_norm<T, TPR, NV, VEC, BACK>(a, p, sm_count, st);
+    AA_NORM(4, 1, V) AA_NORM(4, 2, V) AA_NORM(4, 3, V)
+    AA_NORM(8, 1, V) AA_NORM(8, 2, V) AA_NORM(8, 3, V)
+    AA_NORM(16, 1, V) AA_NORM(16, 2, V) AA_NORM(16, 3, V)
+    AA_NORM(32, 1, V) AA_NORM(32, 2, V) AA_NORM(32, 3, V) AA_NORM(32, 4, V)
+    AA_NORM(128, 1, V) AA_NORM(128, 2, V) AA_NORM(128, 3, V) AA_NORM(128, 4, V)
+    AA_NORM(512, 1, V) AA_NORM(512, 2, V) AA_NORM(512, 3, V) AA_NORM(512, 4, V)
+    AA_NORM(8, 4, 1) AA_NORM(8, 16, 1) AA_NORM(32, 4, 1) AA_NORM(32, 16, 1)
+    AA_NORM(128, 4, 1) AA_NORM(128, 16, 1) AA_NORM(512, 4, 1) AA_NORM(512, 16, 1)
+#undef AA_NORM
+    const unsigned blocks = (unsigned)std::min<long long>(a.rows, (long long)sm_count * 4);
+    float2* stats = BACK && a.ws ? reinterpret_cast<float2*>(a.ws + (long long)kColumnShares * 2 * a.C) : nullptr;
+    const bool place = BACK && stats && a.dx == a.dy;      // dx takes the place of dy: after the gains' gradients have read it
+    NormArgs first = a;
+    if (place) first.dx = nullptr;
+    norm_wide_kernel<T, BACK><<<blocks, 512, 0, st>>>(first, stats);
+    if (cudaError_t e = cudaGetLastError()) return e;
+    if (stats) norm_columns_kernel<T><<<dim3((a.C + 255) / 256, kColumnShares), 256, 0, st>>>(a, stats, a.ws);
+    if (cudaError_t e = cudaGetLastError()) return e;
+    if (place) norm_wide_kernel<T, BACK><<<blocks, 512, 0, st>>>(a, nullptr);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t norm_backward_bytes(int dtype, long long rows, int C, int sm_count) {
+    size_t most = 0;                               // (the size does not depend on the pointers)
+    for (bool aligned : {false, true}) {
+        const NormPlan p = plan_of(dtype, C, aligned);
+        const size_t shares = p.tpr ? (size_t)blocks_of(p, rows, sm_count, true) : (size_t)kColumnShares;
+        most = std::max(most, shares * 2 * C * sizeof(float) + (p.tpr ? 0 : (size_t)rows * sizeof(float2)));
+    }
+    return most;
+}
+cudaError_t launch_norm(int dtype, const NormArgs& a, int sm_count, cudaStream_t st) {
+    return dtype == 0 ? norm_of<float, false>(a, sm_count, st) : dtype == 1 ? norm_of<__nv_bfloat16, false>(a, sm_count, st) : norm_of<__half, false>(a, sm_count, st);
+}
+cudaError_t launch_norm_backward(int dtype, const NormArgs& a, int sm_count, cudaStream_t st, int* launches) {
+    NormArgs b = a;
+    if (!a.dw && !a.db) b.ws = nullptr;
+    const cudaError_t e = dtype == 0 ? norm_of<float, true>(b, sm_count, st) : dtype == 1 ? norm_of<__nv_bfloat16, true>(b, sm_count, st) : norm_of<__half, true>(b, sm_count, st);
+    const NormPlan p = plan_of(dtype, a.C, aligned16(a));
+    *launches = (p.tpr || !b.ws ? 1 : a.dx == a.dy ? 3 : 2) + (b.ws ? 1 : 0);
+    if (e != cudaSuccess || !b.ws) return e;
+    const int shares = p.tpr ? (int)blocks_of(p, a.rows, sm_count, true) : kColumnShares;
+    norm_join_kernel<<<(2 * a.C + 31) / 32, 1024, 0, st>>>(b.ws, shares, a.C, a.dw, a.db);
+    return cudaGetLastError();
+}
+
+}  // namespace aa
