@@ -614,6 +614,11 @@ size_t attend_backward_workspace(int dtype, const AttendArgs& a, int sm_count) {
 cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st, int* launches) {
     const int shares = shares_of(a, sm_count, &a.chunk);
     *launches = shares > 1 ? 2 : 1;
+    if (dtype != 0 && !few_rows(a)) {
+        bool taken;
+        const cudaError_t e = launch_attend_umma(dtype, a, st, &taken);
+        if (taken || e != cudaSuccess) return e;
+    }
     return dtype == 0 ? rows_of_type<float>(a, shares, st) : dtype == 1 ? rows_of_type<__nv_bfloat16>(a, shares, st) : rows_of_type<__half>(a, shares, st);
 }
 cudaError_t launch_attend_backward(int dtype, const AttendArgs& a, int sm_count, cudaStream_t st, int* launches) {

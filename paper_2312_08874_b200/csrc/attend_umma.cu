@@ -1,0 +1,325 @@
+// Softmax attention over whole sequences, forward, 16-bit types, on the 5th-generation tensor cores.
+//
+// A block takes two tiles of 128 queries of a head and walks the keys in tiles of 128 that both share.  Roles:
+//   warps 0-3, 4-7  a tile each: thread = query.  Logits come out of tensor memory into registers, 128 at a time; probabilities go back to tensor memory as the
+//                   A operand of P V.  The exponents' reference moves only when a logit exceeds it by more than 8 (log2 units): then the thread
+//                   rescales its row of the result in tensor memory.  Sums in fp32, of unrounded probabilities; probabilities are rounded to the type
+//                   (half a step each, independent of one another: sums over many keys see less).
+//   warp 8          issues the products: the logits of a tile's next keys while its probabilities are made
+//   warp 9          TMA: queries, keys and values
+//   warp 10         looks after the values of tiles that not every query sees whole: rows behind the sequence become zero, and so do numbers that are
+//                   not finite (0 * infinity is NaN); the queries that do see these get their NaN at the end
+// Results are stored from registers, rows of the sequence alone.
+#include "attend_umma.cuh"
+
+#include <cstring>
+
+namespace aa {
+
+namespace {
+
+struct UmmaArgs {
+    AttendArgs a;
+    unsigned slots;
+    RowMap q, k, v;
+};
+
+template <int BOXES> struct FwdGeom {
+    static constexpr int kStages = BOXES == 1 ? 4 : 2, kOperand = BOXES * kTileBytes;
+    // shared memory (bytes from a 1024-aligned base)
+    static constexpr int OFF_BAD = 512, OFF_Q = 1024, OFF_K = OFF_Q + 2 * kOperand, OFF_V = OFF_K + kStages * kOperand, kSmem = OFF_V + kStages * kOperand + 1024;
+    static_assert(OFF_BAD + BOXES * 64 * 4 <= OFF_Q && kSmem <= 232448, "shared memory");
+    // tensor memory columns: logits, probabilities (two channels' boxes: in place of the logits), results; of the first tile, the second one `step` further
+    static constexpr uint32_t TM_S = 0, kS = 128, TM_P = BOXES == 1 ? 256 : 0, kP = BOXES == 1 ? 64 : 128, TM_O = BOXES == 1 ? 384 : 256, kO = 64 * BOXES;
+    // mbarriers
+    static constexpr int BAR_Q = 0, BAR_KFULL = 1, BAR_KFREE = BAR_KFULL + kStages, BAR_VFULL = BAR_KFREE + kStages, BAR_VREADY = BAR_VFULL + kStages,
+                         BAR_VFREE = BAR_VREADY + kStages, BAR_S = BAR_VFREE + kStages, BAR_READ = BAR_S + 2, BAR_P = BAR_READ + 2, BAR_O = BAR_P + 2,
+                         BAR_MENDED = BAR_O + 2, BAR_DRAIN = BAR_MENDED + 1, kBars = BAR_DRAIN + 1;
+    static_assert(8 * kBars <= 256, "mbarriers");
+};
+constexpr int OFF_DEAD = 256, OFF_TMEM = 260;
+constexpr int kThreads = 384;
+constexpr int kRowRegs = 208, kRoleRegs = 80;       // 256 x 208 + 128 x 80 of the 384 x 168 that the block starts with
+static_assert(256 * kRowRegs + 128 * kRoleRegs <= kThreads * 168, "registers");
+
+template <typename T, int BOXES>
+__global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_constant__ UmmaArgs u) {
+    using G = FwdGeom<BOXES>;
+    constexpr int kStages = G::kStages, kFmt = Elem<T>::kIsBf16 ? 1 : 0;
+    const AttendArgs& a = u.a;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t base = smem_u32(smem);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int head = blockIdx.x % a.heads, hk = head / (a.heads / a.kv_heads);
+    const unsigned slot = blockIdx.x / a.heads;
+    int seq, tile;
+    // (causal: the last queries, which see most, first)
+    if (!find_slot(a.q_offsets, a.sequences, a.N, 1, 2 * kTileRows, a.causal ? u.slots - 1 - slot : slot, &seq, &tile)) return;
+    const Span q = span_of(a.q_offsets, a.q_lengths, a.N, seq), k = span_of(a.k_offsets, a.k_lengths, a.M, seq);
+    const int q0 = tile * 2 * kTileRows;
+    if (q0 >= q.count) return;
+    // key tiles of either tile of queries, and the first of them that not every query of it sees whole
+    int n[2], part[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const int first = q0 + w * kTileRows, last = min(q.count, first + kTileRows) - 1;
+        n[w] = first < q.count ? (visible_keys(a.causal, last, q.count, k.count) + kTileRows - 1) / kTileRows : 0;
+        part[w] = first < q.count ? visible_keys(a.causal, first, q.count, k.count) / kTileRows : INT_MAX;
+    }
+    const int tiles = max(n[0], n[1]), steps = (a.d + 15) / 16;
+
+    Pipe pp;
+    pp.status = a.status;
+    pp.dead = reinterpret_cast<int*>(smem + OFF_DEAD);
+    pp.bars = base;
+    int* first_bad = reinterpret_cast<int*>(smem + G::OFF_BAD);
+    if (tid == 0) {
+        *pp.dead = 0;
+        for (int i = 0; i < G::kBars; ++i) mbar_init(pp.bars + 8 * i, i >= G::BAR_READ && i < G::BAR_O ? 4u : 1u);
+        mbar_fence_init();
+    }
+    if (tid < 64 * BOXES) first_bad[tid] = INT_MAX;
+    if (warp == 8) tmem_alloc<512>(base + OFF_TMEM);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    pp.tmem = *reinterpret_cast<const volatile uint32_t*>(smem + OFF_TMEM);
+
+    if (warp >= 8) {
+    set_regs_dec<kRoleRegs>();
+    if (warp == 9) {
+        // ------------------------------------------------------------------ producer
+        if (lane == 0 && tiles) {
+            const int both = n[1] ? 2 : 1;
+            mbar_arrive_expect_tx(pipe_bar(pp, G::BAR_Q), both * G::kOperand);
+            for (int w = 0; w < both; ++w)
+                for (int b = 0; b < BOXES; ++b)
+                    load_rows(base + G::OFF_Q + w * G::kOperand + b * kTileBytes, u.q, 64 * b, q.first + q0 + w * kTileRows, head, q.batch, pipe_bar(pp, G::BAR_Q));
+            for (int j = 0; j < tiles && !pipe_dead(pp); ++j) {
+                const int s = j % kStages;
+                for (int kind = 0; kind < 2; ++kind) {
+                    if (j >= kStages) wait_spin(pp, (kind ? G::BAR_VFREE : G::BAR_KFREE) + s, j / kStages - 1, kAttendTimeout);
+                    const uint32_t bar = pipe_bar(pp, (kind ? G::BAR_VFULL : G::BAR_KFULL) + s), dst = base + (kind ? G::OFF_V : G::OFF_K) + s * G::kOperand;
+                    mbar_arrive_expect_tx(bar, G::kOperand);
+                    for (int b = 0; b < BOXES; ++b) load_rows(dst + b * kTileBytes, kind ? u.v : u.k, 64 * b, k.first + j * kTileRows, hk, k.batch, bar);
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 10) {
+        // ------------------------------------------------------------------ values that not every query sees
+        for (int j = 0; j < tiles && !pipe_dead(pp); ++j) {
+            const int s = j % kStages;
+            const uint32_t v = base + G::OFF_V + s * G::kOperand;
+            wait_spin(pp, G::BAR_VFULL + s, j / kStages, kAttendTimeout);
+            const bool masked = (j < n[0] && j >= part[0]) || (j < n[1] && j >= part[1]);
+            if (masked) {
+                const int left = min(kTileRows, k.count - j * kTileRows);
+                clear_rows(v, BOXES, left, lane);
+                for (int b = 0; b < BOXES; ++b)
+                    for (int at = lane * 16; at < left * 128; at += 512) {
+                        uint4* w = reinterpret_cast<uint4*>(smem + (v - base) + b * kTileBytes + at);
+                        const uint4 x = *w;
+                        // an exponent of ones: infinity or NaN
+                        constexpr uint32_t kExp = Elem<T>::kIsBf16 ? 0x7f807f80u : 0x7c007c00u;
+                        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+                        bool bad = false;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) bad |= (y[i] & kExp & 0xffffu) == (kExp & 0xffffu) || (y[i] & kExp) >> 16 == kExp >> 16;
+                        if (bad) {
+                            const int row = at / 128, c0 = 64 * b + (((at >> 4) & 7) ^ (row & 7)) * 8;
+                            unsigned short* e = reinterpret_cast<unsigned short*>(w);
+                            for (int i = 0; i < 8; ++i)
+                                if ((e[i] & (kExp & 0xffffu)) == (kExp & 0xffffu)) {
+                                    e[i] = 0;
+                                    atomicMin(first_bad + c0 + i, j * kTileRows + row);
+                                }
+                        }
+                    }
+                fence_proxy_async();
+            }
+            __syncwarp();
+            if (lane == 0) pipe_arrive(pp, G::BAR_VREADY + s);
+        }
+        __syncwarp();
+        if (lane == 0) pipe_arrive(pp, G::BAR_MENDED);
+        __syncwarp();
+    } else if (warp == 8) {
+        // ------------------------------------------------------------------ products
+        const uint32_t id_s = umma_idesc(kFmt, 128, 128, 0), id_o = umma_idesc(kFmt, 128, steps * 16, 1);
+        auto logits = [&](int w, int j) {
+            const int s = j % kStages;
+            wait_spin(pp, G::BAR_KFULL + s, j / kStages, kAttendTimeout);
+            tc_fence_after_sync();
+            mma_rows<BOXES>(pp.tmem + G::TM_S + w * G::kS, base + G::OFF_Q + w * G::kOperand, base + G::OFF_K + s * G::kOperand, id_s, steps);
+            umma_commit_w(pipe_bar(pp, G::BAR_S + w));
+            if (w == 1 || j >= n[1]) umma_commit_w(pipe_bar(pp, G::BAR_KFREE + s));      // (its last user: n[0] <= n[1] where there is a second tile)
+        };
+        if (tiles) {
+            wait_spin(pp, G::BAR_Q, 0, kAttendTimeout);
+            for (int w = 0; w < 2; ++w)
+                if (n[w]) logits(w, 0);
+        }
+        for (int j = 0; j < tiles && !pipe_dead(pp); ++j) {
+            const int s = j % kStages;
+            for (int w = 0; w < 2; ++w) {
+                if (j >= n[w]) continue;
+                if (BOXES == 1 && j + 1 < n[w]) {
+                    wait_spin(pp, G::BAR_READ + w, j, kAttendTimeout);
+                    logits(w, j + 1);
+                }
+                wait_spin(pp, G::BAR_P + w, j, kAttendTimeout);
+                wait_spin(pp, G::BAR_VREADY + s, j / kStages, kAttendTimeout);
+                tc_fence_after_sync();
+                mma_sum<BOXES>(pp.tmem + G::TM_O + w * G::kO, pp.tmem + G::TM_P + w * G::kP, base + G::OFF_V + s * G::kOperand, id_o, j > 0);
+                umma_commit_w(pipe_bar(pp, G::BAR_O + w));
+                if (w == 1 || j >= n[1]) umma_commit_w(pipe_bar(pp, G::BAR_VFREE + s));
+                if (BOXES == 2 && j + 1 < n[w]) {
+                    wait_spin(pp, G::BAR_O + w, j, kAttendTimeout);          // (the logits take the place of the probabilities)
+                    logits(w, j + 1);
+                }
+            }
+        }
+        umma_drain_w(pp, G::BAR_DRAIN);
+        __syncwarp();
+    }
+    } else {
+        // ------------------------------------------------------------------ softmax: thread = query
+        set_regs_inc<kRowRegs>();
+        const int w = warp >> 2, row = 32 * (warp & 3) + lane, token = q0 + w * kTileRows + row;
+        const int limit = visible_keys(a.causal, min(token, q.count - 1), q.count, k.count);
+        const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+        const uint32_t ts = pp.tmem + G::TM_S + w * G::kS + lanes, tp = pp.tmem + G::TM_P + w * G::kP + lanes, to = pp.tmem + G::TM_O + w * G::kO + lanes;
+        const float c1 = a.scale * kLog2e;
+        float ref = -INFINITY;
+        float2 sum = make_float2(0.f, 0.f);
+        for (int j = 0; j < n[w]; ++j) {
+            wait_soon(pp, G::BAR_S + w, j);
+            tc_fence_after_sync();
+            float2 x[64];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                uint32_t o[32];
+                tmem_ld32(ts + 32 * h, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[16 * h + i] = make_float2(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1]));
+            }
+            if (BOXES == 1) {
+                tc_fence_before_sync();
+                pipe_arrive_warp(pp, G::BAR_READ + w, lane);
+            }
+            if (j >= part[w]) {
+                const int left = limit - j * kTileRows;
+#pragma unroll
+                for (int i = 0; i < 64; ++i) {
+                    if (2 * i >= left) x[i].x = -INFINITY;
+                    if (2 * i + 1 >= left) x[i].y = -INFINITY;
+                }
+            }
+            float m = fmaxf(x[0].x, x[0].y);
+#pragma unroll
+            for (int i = 1; i < 64; ++i) m = max3(m, x[i].x, x[i].y);
+            m *= c1;
+            const bool grow = m > ref + 8.f;                                     // (always of a row without a key so far)
+            if (__any_sync(0xffffffffu, grow)) {
+                const float next = grow ? m : ref, f = grow ? fast_exp2(ref - next) : 1.f;      // (exp2(-inf) = 0)
+                ref = next;
+                sum = fmul2(sum, make_float2(f, f));
+                if (j > 0) {
+                    wait_soon(pp, G::BAR_O + w, j - 1);
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (int h = 0; h < 2 * BOXES; ++h) {
+                        uint32_t o[32];
+                        tmem_ld32(to + 32 * h, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        tmem_st32(to + 32 * h, o);
+                    }
+                }
+            } else if (BOXES == 1 && j > 0) {
+                wait_soon(pp, G::BAR_O + w, j - 1);                              // (P V of the keys before has read its probabilities)
+                tc_fence_after_sync();
+            }
+            const float nr = ref == -INFINITY ? 0.f : -ref;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                uint32_t p[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float2 e = ffma2(x[16 * h + i], make_float2(c1, c1), make_float2(nr, nr));
+                    const float2 v = make_float2(fast_exp2(e.x), fast_exp2(e.y));
+                    sum = fadd2(sum, v);
+                    p[i] = pack2<T>(v.x, v.y);
+                }
+                tmem_st16(tp + 16 * h, p);
+            }
+            tmem_st_wait();
+            tc_fence_before_sync();
+            pipe_arrive_warp(pp, G::BAR_P + w, lane);
+        }
+        const bool live = token < q.count;
+        if (n[w]) {
+            wait_soon(pp, G::BAR_O + w, n[w] - 1);
+            wait_soon(pp, G::BAR_MENDED, 0);
+            tc_fence_after_sync();
+        }
+        const float total = sum.x + sum.y, inv = limit > 0 ? 1.f / total : 0.f;
+        T* out = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + token) * a.lo.st;
+#pragma unroll
+        for (int h = 0; h < 2 * BOXES; ++h) {
+            uint32_t o[32] = {};
+            if (n[w]) {
+                tmem_ld32(to + 32 * h, o);
+                tmem_ld_wait();
+            }
+            if (!live) continue;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int c = 32 * h + 8 * g;
+                if (c >= a.d) continue;
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = limit > 0 ? __uint_as_float(o[8 * g + i]) * inv : 0.f;
+                if (part[0] < n[0] || part[1] < n[1])
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (first_bad[c + i] < limit) f[i] = NAN;
+                *reinterpret_cast<uint4*>(out + c) = pack16<T>(f);
+            }
+        }
+        if (live && a.lse) a.lse[((long long)q.batch * a.heads + head) * a.N + q.first + token] = limit > 0 ? (ref + log2f(total)) * kLn2 : -INFINITY;
+        tc_fence_before_sync();
+    }
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after_sync();
+        tmem_dealloc<512>(pp.tmem);
+    }
+}
+
+template <typename T, int BOXES> cudaError_t run(const UmmaArgs& u, cudaStream_t st) {
+    using G = FwdGeom<BOXES>;
+    static std::atomic<unsigned long long> done{0};
+    if (cudaError_t e = allow_smem(attend_umma_kernel<T, BOXES>, done, G::kSmem)) return e;
+    attend_umma_kernel<T, BOXES><<<(unsigned)((long long)u.slots * u.a.heads), kThreads, G::kSmem, st>>>(u);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attend_umma(int dtype, const AttendArgs& a, cudaStream_t st, bool* done) {
+    UmmaArgs u;
+    u.a = a;
+    u.slots = (unsigned)slots_of(a.q_offsets != nullptr, a.sequences, a.N, 1, 2 * kTileRows);
+    *done = make_row_map(&u.q, a.q, a.lq, a.batch, a.heads, a.N, a.d) && make_row_map(&u.k, a.k, a.lk, a.batch, a.kv_heads, a.M, a.d) &&
+            make_row_map(&u.v, a.v, a.lv, a.batch, a.kv_heads, a.M, a.d);
+    if (!*done) return cudaSuccess;
+    if (dtype == 1) return a.d <= 64 ? run<__nv_bfloat16, 1>(u, st) : run<__nv_bfloat16, 2>(u, st);
+    return a.d <= 64 ? run<__half, 1>(u, st) : run<__half, 2>(u, st);
+}
+
+}  // namespace aa

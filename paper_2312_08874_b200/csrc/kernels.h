@@ -386,6 +386,7 @@ struct AttendArgs {
 };
 size_t attend_workspace(int dtype, const AttendArgs& a, int sm_count);            // (sets nothing; reads the sizes)
 cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st, int* launches);
+cudaError_t launch_attend_umma(int dtype, const AttendArgs& a, cudaStream_t st, bool* done);       // (done: false where tensor maps cannot describe the strides)
 size_t attend_backward_workspace(int dtype, const AttendArgs& a, int sm_count);
 cudaError_t launch_attend_backward(int dtype, const AttendArgs& a, int sm_count, cudaStream_t st, int* launches);
 
