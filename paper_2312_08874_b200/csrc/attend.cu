@@ -2,7 +2,7 @@
 //
 // A row is a query of one head; the heads that share keys stand side by side (row = query * group + head), so that single tokens fill a tile's rows
 // with their heads.  Forward: WR warps own 16 rows each, WK of them share the rows and take turns at blocks of 32 keys; logits, probabilities and
-// results stay in registers, the softmax keeps a running maximum and sum in fp32.  One kernel serves both directions of the gradient, too: rows
+// results stay in registers, the softmax keeps a running maximum and sum in fp32.  The gradient of fp32 tensors has one kernel for both directions: rows
 // are queries (dQ) or keys (dK, dV, whose columns are the queries of all heads of the group, so no share of theirs is added up elsewhere).
 //
 // fp32: a product of two numbers is six products of their terms (what is left out is below 2^-24), small ones first; sums over the columns leave the
@@ -402,12 +402,11 @@ int shares_of(const AttendArgs& a, int sm_count, int* chunk) {
     return (a.M + *chunk - 1) / *chunk;
 }
 
-template <typename T> cudaError_t rows_of_type(const AttendArgs& a, int shares, cudaStream_t st) {
-    const bool few = few_rows(a);
-    if (a.d <= 32) return few ? run_rows<T, 32, 1, 4>(a, shares, st) : run_rows<T, 32, 4, 1>(a, shares, st);
-    if (a.d <= 64) return few ? run_rows<T, 64, 1, 4>(a, shares, st) : run_rows<T, 64, 4, 1>(a, shares, st);
-    if (a.d <= 96) return few ? run_rows<T, 96, 1, 4>(a, shares, st) : run_rows<T, 96, 4, 1>(a, shares, st);
-    return few ? run_rows<T, 128, 1, 4>(a, shares, st) : run_rows<T, 128, 4, 1>(a, shares, st);
+template <typename T, int WR, int WK> cudaError_t rows_of_type(const AttendArgs& a, int shares, cudaStream_t st) {
+    if (a.d <= 32) return run_rows<T, 32, WR, WK>(a, shares, st);
+    if (a.d <= 64) return run_rows<T, 64, WR, WK>(a, shares, st);
+    if (a.d <= 96) return run_rows<T, 96, WR, WK>(a, shares, st);
+    return run_rows<T, 128, WR, WK>(a, shares, st);
 }
 
 // ------------------------------------------------------------------------------------------------ backward
@@ -459,17 +458,18 @@ template <typename T> __global__ void __launch_bounds__(256) attend_dot_kernel(c
     if (kNorms && most > 0.f) atomicMax(grad_most(a, seq, hk) + (values ? 1 : 0), __float_as_uint(most));      // (positive numbers keep their order; any order of arrival)
 }
 
-template <typename T, int DK> struct GradGeom {
-    static constexpr int NT = Oper<T>::kTerms, kRows = 64, kStep = 32, kPitch = TileGeom<DK>::kPitch;
+template <int DK> struct GradGeom {
+    static constexpr int NT = 3, kRows = 64, kStep = 32, kPitch = TileGeom<DK>::kPitch;
     static constexpr uint32_t kRowPlane = kRows * kPitch, kPlane = kStep * kPitch;
     static constexpr int kSmem = 2 * NT * (int)(kRowPlane + kPlane) + kStep * 8;
 };
 
 // KEYS: rows are keys (x = K, y = V), columns queries (u = Q, w = dO); else rows are queries (x = Q, y = dO), columns keys (u = K, w = V).
-template <typename T, int DK, bool KEYS>
+template <int DK, bool KEYS>
 __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant__ AttendArgs a) {
-    using G = GradGeom<T, DK>;
-    using E = typename Oper<T>::E;
+    using T = float;
+    using G = GradGeom<DK>;
+    using E = __nv_bfloat16;
     constexpr int NT = G::NT, P = G::kPitch;
     extern __shared__ __align__(128) unsigned char smem[];
     unsigned char *xs = smem, *ys = xs + NT * G::kRowPlane, *us = ys + NT * G::kRowPlane, *ws = us + NT * G::kPlane;
@@ -499,8 +499,6 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
         end = visible_keys(a.causal, ((min(rows, row0 + G::kRows) - 1) / group), q.count, k.count);
     }
     const float c1 = a.scale * kLog2e;
-    float kappa[2] = {1.f, 1.f};                   // f16: power of two that P (dP - D) is held times, over that of P
-    if (is_f16<T>) kappa[0] = kappa[1] = grad_factor(__uint_as_float(grad_most(a, seq, hk)[0]), __uint_as_float(grad_most(a, seq, hk)[1]));
     int row[2], limit[2];                          // rows are queries: the keys that they see; keys: the first column that sees them
     float2 st[2];
 #pragma unroll
@@ -511,9 +509,6 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
         } else {
             st[h] = row[h] < rows ? stat(row[h]) : make_float2(0.f, 0.f);
             limit[h] = row[h] < rows ? visible_keys(a.causal, row[h] / group, q.count, k.count) : 0;
-            if (is_f16<T> && row[h] < rows)
-                kappa[h] = grad_factor(grad_norms(a)[((long long)q.batch * a.heads + hk * group + row[h] % group) * a.N + q.first + row[h] / group],
-                                       __uint_as_float(grad_most(a, seq, hk)[1]));
         }
     }
     float acc[DK / 8][4], acc2[KEYS ? DK / 8 : 1][4];
@@ -532,8 +527,6 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
         load_tile<T, DK, 128>(us, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.q, a.lq, c0 + r) : key(a.k, a.lk, c0 + r)) : nullptr; });
         load_tile<T, DK, 128>(ws, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.dout, a.ldo, c0 + r) : key(a.v, a.lv, c0 + r)) : nullptr; });
         if (KEYS && tid < G::kStep) stats[tid] = c0 + tid < end ? stat(c0 + tid) : make_float2(0.f, 0.f);
-        cp_async_commit();
-        cp_async_wait<0>();
         __syncthreads();
         float x[4][4], y[4][4];
         block_logits<E, NT, DK>(x, xa, G::kRowPlane, ub, G::kPlane);
@@ -545,9 +538,9 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
                 const int c = 8 * j + 2 * t + (e & 1), h = e >> 1;
                 const float2 s = KEYS ? stats[c] : st[h];
                 const bool seen = KEYS ? c0 + c < end && c0 + c >= limit[h] : c0 + c < limit[h];
-                const float p = seen ? fast_exp2(fmaf(x[j][e], c1, (is_f16<T> ? kHeldP : 0) - s.x)) : 0.f;
+                const float p = seen ? fast_exp2(fmaf(x[j][e], c1, -s.x)) : 0.f;
                 x[j][e] = p;
-                y[j][e] = seen ? p * ((y[j][e] - s.y) * kappa[h]) : 0.f;
+                y[j][e] = seen ? p * (y[j][e] - s.y) : 0.f;
             }
         uint32_t w[NT][2][4];
         block_operand<E, NT>(y, w);
@@ -560,44 +553,38 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         if (row[h] >= rows) continue;
-        const float out_p = is_f16<T> ? kHeldBack : 1.f, out_s = a.scale * out_p / kappa[h];
         auto put = [&](void* p, const TokLayout& l, int c, float v0, float v1) {
             T* to = static_cast<T*>(p) + (KEYS ? k.batch * l.sb + hk * l.sh + (long long)(k.first + row[h]) * l.st : q.batch * l.sb + (hk * group + row[h] % group) * l.sh + (long long)(q.first + row[h] / group) * l.st) + c;
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(to) = pack2<T>(v0, v1);
-            else *reinterpret_cast<float2*>(to) = make_float2(v0, v1);
+            *reinterpret_cast<float2*>(to) = make_float2(v0, v1);
         };
 #pragma unroll
         for (int c = 0; c < DK / 8; ++c) {
             if (8 * c + 2 * t >= a.d) continue;
-            put(KEYS ? a.dk : a.dq, KEYS ? a.ldk : a.ldq, 8 * c + 2 * t, acc[c][2 * h] * out_s, acc[c][2 * h + 1] * out_s);
-            if constexpr (KEYS) put(a.dv, a.ldv, 8 * c + 2 * t, acc2[c][2 * h] * out_p, acc2[c][2 * h + 1] * out_p);
+            put(KEYS ? a.dk : a.dq, KEYS ? a.ldk : a.ldq, 8 * c + 2 * t, acc[c][2 * h] * a.scale, acc[c][2 * h + 1] * a.scale);
+            if constexpr (KEYS) put(a.dv, a.ldv, 8 * c + 2 * t, acc2[c][2 * h], acc2[c][2 * h + 1]);
         }
     }
 }
 
-template <typename T, int DK, bool KEYS> cudaError_t run_grad(const AttendArgs& a, cudaStream_t st) {
-    using G = GradGeom<T, DK>;
+template <int DK, bool KEYS> cudaError_t run_grad(const AttendArgs& a, cudaStream_t st) {
+    using G = GradGeom<DK>;
     static std::atomic<unsigned long long> done{0};
-    if (cudaError_t e = allow_smem(attend_grad_kernel<T, DK, KEYS>, done, G::kSmem)) return e;
+    if (cudaError_t e = allow_smem(attend_grad_kernel<DK, KEYS>, done, G::kSmem)) return e;
     const long long slots = KEYS ? slots_of(a.k_offsets != nullptr, a.sequences, a.M, 1, G::kRows) : slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, G::kRows);
-    attend_grad_kernel<T, DK, KEYS><<<dim3((unsigned)slots, a.kv_heads), 128, G::kSmem, st>>>(a);
+    attend_grad_kernel<DK, KEYS><<<dim3((unsigned)slots, a.kv_heads), 128, G::kSmem, st>>>(a);
     return cudaGetLastError();
 }
-template <typename T, int DK> cudaError_t run_grads(const AttendArgs& a, cudaStream_t st) {
-    if (cudaError_t e = run_grad<T, DK, true>(a, st)) return e;
-    return run_grad<T, DK, false>(a, st);
+template <int DK> cudaError_t run_grads(const AttendArgs& a, cudaStream_t st) {
+    if (cudaError_t e = run_grad<DK, true>(a, st)) return e;
+    return run_grad<DK, false>(a, st);
 }
-template <typename T> cudaError_t grads_of_type(const AttendArgs& a, cudaStream_t st) {
+template <typename T> cudaError_t run_dot(const AttendArgs& a, cudaStream_t st) {
     const long long q_slots = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, kDotRows);
     const long long v_slots = is_f16<T> ? slots_of(a.k_offsets != nullptr, a.sequences, a.M, 1, kDotRows) : 0;
     if (is_f16<T>)
         if (cudaError_t e = cudaMemsetAsync(grad_most(a, 0, 0), 0, (size_t)a.sequences * a.kv_heads * 2 * sizeof(unsigned), st)) return e;
     attend_dot_kernel<T><<<dim3((unsigned)(q_slots + v_slots), a.kv_heads), 256, 0, st>>>(a, (unsigned)q_slots);
-    if (cudaError_t e = cudaGetLastError()) return e;
-    if (a.d <= 32) return run_grads<T, 32>(a, st);
-    if (a.d <= 64) return run_grads<T, 64>(a, st);
-    if (a.d <= 96) return run_grads<T, 96>(a, st);
-    return run_grads<T, 128>(a, st);
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -614,16 +601,20 @@ size_t attend_backward_workspace(int dtype, const AttendArgs& a, int sm_count) {
 cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st, int* launches) {
     const int shares = shares_of(a, sm_count, &a.chunk);
     *launches = shares > 1 ? 2 : 1;
-    if (dtype != 0 && !few_rows(a)) {
-        bool taken;
-        const cudaError_t e = launch_attend_umma(dtype, a, st, &taken);
-        if (taken || e != cudaSuccess) return e;
-    }
-    return dtype == 0 ? rows_of_type<float>(a, shares, st) : dtype == 1 ? rows_of_type<__nv_bfloat16>(a, shares, st) : rows_of_type<__half>(a, shares, st);
+    if (dtype != 0 && !few_rows(a)) return launch_attend_umma(dtype, a, st);
+    if (dtype == 1) return rows_of_type<__nv_bfloat16, 1, 4>(a, shares, st);
+    if (dtype == 2) return rows_of_type<__half, 1, 4>(a, shares, st);
+    return few_rows(a) ? rows_of_type<float, 1, 4>(a, shares, st) : rows_of_type<float, 4, 1>(a, shares, st);
 }
 cudaError_t launch_attend_backward(int dtype, const AttendArgs& a, int sm_count, cudaStream_t st, int* launches) {
     *launches = 3;
-    return dtype == 0 ? grads_of_type<float>(a, st) : dtype == 1 ? grads_of_type<__nv_bfloat16>(a, st) : grads_of_type<__half>(a, st);
+    const cudaError_t e = dtype == 0 ? run_dot<float>(a, st) : dtype == 1 ? run_dot<__nv_bfloat16>(a, st) : run_dot<__half>(a, st);
+    if (e != cudaSuccess) return e;
+    if (dtype != 0) return launch_attend_grad_umma(dtype, a, st);
+    if (a.d <= 32) return run_grads<32>(a, st);
+    if (a.d <= 64) return run_grads<64>(a, st);
+    if (a.d <= 96) return run_grads<96>(a, st);
+    return run_grads<128>(a, st);
 }
 
 }  // namespace aa

@@ -311,13 +311,13 @@ template <typename T, int BOXES> cudaError_t run(const UmmaArgs& u, cudaStream_t
 
 }  // namespace
 
-cudaError_t launch_attend_umma(int dtype, const AttendArgs& a, cudaStream_t st, bool* done) {
+cudaError_t launch_attend_umma(int dtype, const AttendArgs& a, cudaStream_t st) {
     UmmaArgs u;
     u.a = a;
     u.slots = (unsigned)slots_of(a.q_offsets != nullptr, a.sequences, a.N, 1, 2 * kTileRows);
-    *done = make_row_map(&u.q, a.q, a.lq, a.batch, a.heads, a.N, a.d) && make_row_map(&u.k, a.k, a.lk, a.batch, a.kv_heads, a.M, a.d) &&
-            make_row_map(&u.v, a.v, a.lv, a.batch, a.kv_heads, a.M, a.d);
-    if (!*done) return cudaSuccess;
+    if (!make_row_map(&u.q, a.q, a.lq, a.batch, a.heads, a.N, a.d) || !make_row_map(&u.k, a.k, a.lk, a.batch, a.kv_heads, a.M, a.d) ||
+        !make_row_map(&u.v, a.v, a.lv, a.batch, a.kv_heads, a.M, a.d))
+        return cudaErrorInvalidValue;
     if (dtype == 1) return a.d <= 64 ? run<__nv_bfloat16, 1>(u, st) : run<__nv_bfloat16, 2>(u, st);
     return a.d <= 64 ? run<__half, 1>(u, st) : run<__half, 2>(u, st);
 }

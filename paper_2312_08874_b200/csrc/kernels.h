@@ -363,7 +363,7 @@ struct GatedCall {
 size_t gated_bytes(int dtype, int M, int C, int F, bool backward, bool two_terms, int sm_count);
 cudaError_t launch_gated(int dtype, const GatedCall& c, cudaStream_t st, int* launches);
 
-// Softmax attention over whole sequences (attend.cu, attend_umma.cu)
+// Softmax attention over whole sequences (attend.cu, attend_umma.cu, attend_grad_umma.cu)
 struct AttendArgs {
     const void *q, *k, *v;
     TokLayout lq, lk, lv;                 // strides in elements
@@ -386,7 +386,8 @@ struct AttendArgs {
 };
 size_t attend_workspace(int dtype, const AttendArgs& a, int sm_count);            // (sets nothing; reads the sizes)
 cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st, int* launches);
-cudaError_t launch_attend_umma(int dtype, const AttendArgs& a, cudaStream_t st, bool* done);       // (done: false where tensor maps cannot describe the strides)
+cudaError_t launch_attend_umma(int dtype, const AttendArgs& a, cudaStream_t st);
+cudaError_t launch_attend_grad_umma(int dtype, const AttendArgs& a, cudaStream_t st);
 size_t attend_backward_workspace(int dtype, const AttendArgs& a, int sm_count);
 cudaError_t launch_attend_backward(int dtype, const AttendArgs& a, int sm_count, cudaStream_t st, int* launches);
 
