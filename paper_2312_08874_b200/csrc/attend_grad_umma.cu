@@ -144,23 +144,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_grad_umma_kernel(const __g
         __syncwarp();
     } else if (warp == 8) {
         // ------------------------------------------------------------------ products
-        const uint32_t id_s = umma_idesc(kFmt, 128, 128, 0), id_a = umma_idesc(kFmt, 128, steps * 16, 1);
+        const uint32_t id_s = umma_idesc(kFmt, 128, 128, 0), id_a = umma_idesc(kFmt, 128, steps * 16, 1), elected = elect_lane();
         auto ring = [&](int j, int which) { return base + G::OFF_RING + (j % kStages) * 2 * G::kOperand + which * G::kOperand; };
         auto logits = [&](int j) {
             wait_spin(pp, G::BAR_READY + j % kStages, j / kStages, kAttendTimeout);
             tc_fence_after_sync();
-            mma_rows<BOXES>(pp.tmem + (KEYS ? 0 : (j & 1) * kCols), base + G::OFF_X, ring(j, 0), id_s, steps);
-            umma_commit_w(pipe_bar(pp, G::BAR_S + (KEYS ? 0 : j & 1)));
+            mma_rows<BOXES>(elected, pp.tmem + (KEYS ? 0 : (j & 1) * kCols), base + G::OFF_X, ring(j, 0), id_s, steps);
+            umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_S + (KEYS ? 0 : j & 1)));
         };
         auto slopes = [&](int j) {
-            mma_rows<BOXES>(pp.tmem + TM_T, base + G::OFF_X + G::kOperand, ring(j, 1), id_s, steps);
-            umma_commit_w(pipe_bar(pp, G::BAR_T));
+            mma_rows<BOXES>(elected, pp.tmem + TM_T, base + G::OFF_X + G::kOperand, ring(j, 1), id_s, steps);
+            umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_T));
         };
-        auto sums = [&](uint32_t acc, uint32_t operand, int j, int which) {
-            const uint64_t db = BOXES == 1 ? umma_desc_sw128(ring(j, which)) : desc_mn(ring(j, which), kTileBytes);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) umma_ts_w(acc, operand + (i >> 2) * 64 + 8 * (i & 3), db + 128 * i, id_a, j > 0 || i > 0);
-        };
+        auto sums = [&](uint32_t acc, uint32_t operand, int j, int which) { mma_sum<BOXES>(elected, acc, operand, operand + 64, ring(j, which), id_a, j > 0); };
         if (total) {
             wait_spin(pp, G::BAR_X, 0, kAttendTimeout);
             logits(0);
@@ -171,7 +167,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_grad_umma_kernel(const __g
                 wait_spin(pp, G::BAR_P, j, kAttendTimeout);
                 tc_fence_after_sync();
                 sums(pp.tmem + TM_V, pp.tmem, j, 1);
-                umma_commit_w(pipe_bar(pp, G::BAR_ACC));
+                umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_ACC));
                 if (j + 1 < total) {
                     wait_spin(pp, G::BAR_ACC, j, kAttendTimeout);            // (the next logits take the place of the probabilities)
                     logits(j + 1);
@@ -182,8 +178,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_grad_umma_kernel(const __g
             wait_spin(pp, G::BAR_DS, j, kAttendTimeout);
             tc_fence_after_sync();
             sums(pp.tmem + TM_A, pp.tmem + TM_T, j, 0);
-            umma_commit_w(pipe_bar(pp, G::BAR_FREE + j % kStages));
-            umma_commit_w(pipe_bar(pp, G::BAR_ACC + 1));
+            umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_FREE + j % kStages));
+            umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_ACC + 1));
             if (j + 1 < total) {
                 wait_spin(pp, G::BAR_ACC + 1, j, kAttendTimeout);
                 tc_fence_after_sync();

@@ -5,7 +5,8 @@
 //                   A operand of P V.  The exponents' reference moves only when a logit exceeds it by more than 8 (log2 units): then the thread
 //                   rescales its row of the result in tensor memory.  Sums in fp32, of unrounded probabilities; probabilities are rounded to the type
 //                   (half a step each, independent of one another: sums over many keys see less).
-//   warp 8          issues the products: the logits of a tile's next keys while its probabilities are made
+//   warps 8, 11     issue the products of a tile of queries each: the logits of its next keys while its probabilities are made (one warp for both took
+//                   2800 cycles for two tiles of 64 channels, of which the tensor cores worked 1000)
 //   warp 9          TMA: queries, keys and values
 //   warp 10         looks after the values of tiles that not every query sees whole: rows behind the sequence become zero, and so do numbers that are
 //                   not finite (0 * infinity is NaN); the queries that do see these get their NaN at the end
@@ -34,7 +35,7 @@ template <int BOXES> struct FwdGeom {
     // mbarriers
     static constexpr int BAR_Q = 0, BAR_KFULL = 1, BAR_KFREE = BAR_KFULL + kStages, BAR_VFULL = BAR_KFREE + kStages, BAR_VREADY = BAR_VFULL + kStages,
                          BAR_VFREE = BAR_VREADY + kStages, BAR_S = BAR_VFREE + kStages, BAR_READ = BAR_S + 2, BAR_P = BAR_READ + 2, BAR_O = BAR_P + 2,
-                         BAR_MENDED = BAR_O + 2, BAR_DRAIN = BAR_MENDED + 1, kBars = BAR_DRAIN + 1;
+                         BAR_MENDED = BAR_O + 2, BAR_DRAIN = BAR_MENDED + 1, kBars = BAR_DRAIN + 2;
     static_assert(8 * kBars <= 256, "mbarriers");
 };
 constexpr int OFF_DEAD = 256, OFF_TMEM = 260;
@@ -42,10 +43,16 @@ constexpr int kThreads = 384;
 constexpr int kRowRegs = 208, kRoleRegs = 80;       // 256 x 208 + 128 x 80 of the 384 x 168 that the block starts with
 static_assert(256 * kRowRegs + 128 * kRoleRegs <= kThreads * 168, "registers");
 
+// Turns of two warps, one of each tile, that share a scheduler (more than 64 channels): the exponentials of one run beside the products of the other.  In step with
+// each other both would wait for the tensor cores, and then both for the special-function unit (8 heads of 8192 x 8192 x 128: 323 -> 287 us).
+__device__ __forceinline__ void bar_sync_pair(int id) { asm volatile("bar.sync %0, 64;\n" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void bar_arrive_pair(int id) { asm volatile("bar.arrive %0, 64;\n" ::"r"(id) : "memory"); }
+
 template <typename T, int BOXES>
 __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_constant__ UmmaArgs u) {
     using G = FwdGeom<BOXES>;
     constexpr int kStages = G::kStages, kFmt = Elem<T>::kIsBf16 ? 1 : 0;
+    constexpr bool TURNS = BOXES == 2;
     const AttendArgs& a = u.a;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -76,7 +83,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
     int* first_bad = reinterpret_cast<int*>(smem + G::OFF_BAD);
     if (tid == 0) {
         *pp.dead = 0;
-        for (int i = 0; i < G::kBars; ++i) mbar_init(pp.bars + 8 * i, i >= G::BAR_READ && i < G::BAR_O ? 4u : 1u);
+        for (int i = 0; i < G::kBars; ++i) mbar_init(pp.bars + 8 * i, i >= G::BAR_READ && i < G::BAR_O ? 4u : (i >= G::BAR_KFREE && i < G::BAR_VFULL) || (i >= G::BAR_VFREE && i < G::BAR_S) ? 2u : 1u);
         mbar_fence_init();
     }
     if (tid < 64 * BOXES) first_bad[tid] = INT_MAX;
@@ -145,43 +152,52 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
         __syncwarp();
         if (lane == 0) pipe_arrive(pp, G::BAR_MENDED);
         __syncwarp();
-    } else if (warp == 8) {
-        // ------------------------------------------------------------------ products
-        const uint32_t id_s = umma_idesc(kFmt, 128, 128, 0), id_o = umma_idesc(kFmt, 128, steps * 16, 1);
-        auto logits = [&](int w, int j) {
+    } else {
+        // ------------------------------------------------------------------ products of one tile of queries
+        const int w = warp == 8 ? 0 : 1;
+        const uint32_t id_s = umma_idesc(kFmt, 128, 128, 0), id_o = umma_idesc(kFmt, 128, steps * 16, 1), elected = elect_lane();
+        const uint32_t tp = pp.tmem + G::TM_P + w * G::kP;
+        auto logits = [&](int j) {
             const int s = j % kStages;
             wait_spin(pp, G::BAR_KFULL + s, j / kStages, kAttendTimeout);
             tc_fence_after_sync();
-            mma_rows<BOXES>(pp.tmem + G::TM_S + w * G::kS, base + G::OFF_Q + w * G::kOperand, base + G::OFF_K + s * G::kOperand, id_s, steps);
-            umma_commit_w(pipe_bar(pp, G::BAR_S + w));
-            if (w == 1 || j >= n[1]) umma_commit_w(pipe_bar(pp, G::BAR_KFREE + s));      // (its last user: n[0] <= n[1] where there is a second tile)
+            mma_rows<BOXES>(elected, pp.tmem + G::TM_S + w * G::kS, base + G::OFF_Q + w * G::kOperand, base + G::OFF_K + s * G::kOperand, id_s, steps);
+            umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_S + w));
+            umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_KFREE + s));
         };
-        if (tiles) {
+        if (n[w]) {
             wait_spin(pp, G::BAR_Q, 0, kAttendTimeout);
-            for (int w = 0; w < 2; ++w)
-                if (n[w]) logits(w, 0);
+            logits(0);
         }
-        for (int j = 0; j < tiles && !pipe_dead(pp); ++j) {
+        for (int j = 0; j < n[w] && !pipe_dead(pp); ++j) {
             const int s = j % kStages;
-            for (int w = 0; w < 2; ++w) {
-                if (j >= n[w]) continue;
-                if (BOXES == 1 && j + 1 < n[w]) {
-                    wait_spin(pp, G::BAR_READ + w, j, kAttendTimeout);
-                    logits(w, j + 1);
-                }
-                wait_spin(pp, G::BAR_P + w, j, kAttendTimeout);
-                wait_spin(pp, G::BAR_VREADY + s, j / kStages, kAttendTimeout);
-                tc_fence_after_sync();
-                mma_sum<BOXES>(pp.tmem + G::TM_O + w * G::kO, pp.tmem + G::TM_P + w * G::kP, base + G::OFF_V + s * G::kOperand, id_o, j > 0);
-                umma_commit_w(pipe_bar(pp, G::BAR_O + w));
-                if (w == 1 || j >= n[1]) umma_commit_w(pipe_bar(pp, G::BAR_VFREE + s));
-                if (BOXES == 2 && j + 1 < n[w]) {
-                    wait_spin(pp, G::BAR_O + w, j, kAttendTimeout);          // (the logits take the place of the probabilities)
-                    logits(w, j + 1);
-                }
+            if (BOXES == 1 && j + 1 < n[w]) {
+                wait_spin(pp, G::BAR_READ + w, j, kAttendTimeout);
+                logits(j + 1);
+            }
+            wait_spin(pp, G::BAR_VREADY + s, j / kStages, kAttendTimeout);
+            wait_spin(pp, G::BAR_P + w, j, kAttendTimeout);
+            tc_fence_after_sync();
+            mma_sum<BOXES>(elected, pp.tmem + G::TM_O + w * G::kO, tp, tp + 32, base + G::OFF_V + s * G::kOperand, id_o, j > 0);
+            umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_O + w));
+            umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_VFREE + s));
+            if (BOXES == 2 && j + 1 < n[w]) {
+                wait_spin(pp, G::BAR_O + w, j, kAttendTimeout);              // (the logits take the place of the probabilities)
+                logits(j + 1);
             }
         }
-        umma_drain_w(pp, G::BAR_DRAIN);
+        // tiles that only the other one needs: released as they come
+        for (int j = n[w]; j < tiles && !pipe_dead(pp); ++j) {
+            const int s = j % kStages;
+            wait_spin(pp, G::BAR_KFULL + s, j / kStages, kAttendTimeout);
+            wait_spin(pp, G::BAR_VREADY + s, j / kStages, kAttendTimeout);
+            if (lane == 0) {
+                pipe_arrive(pp, G::BAR_KFREE + s);
+                pipe_arrive(pp, G::BAR_VFREE + s);
+            }
+            __syncwarp();
+        }
+        umma_drain_w(pp, G::BAR_DRAIN + w);
         __syncwarp();
     }
     } else {
@@ -193,19 +209,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
         const uint32_t ts = pp.tmem + G::TM_S + w * G::kS + lanes, tp = pp.tmem + G::TM_P + w * G::kP + lanes, to = pp.tmem + G::TM_O + w * G::kO + lanes;
         const float c1 = a.scale * kLog2e;
         float ref = -INFINITY;
-        float2 sum = make_float2(0.f, 0.f);
+        float2 sum[2] = {};
         for (int j = 0; j < n[w]; ++j) {
             wait_soon(pp, G::BAR_S + w, j);
             tc_fence_after_sync();
+            uint32_t o[4][32];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) tmem_ld32(ts + 32 * h, o[h]);
+            tmem_ld_wait();
             float2 x[64];
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                uint32_t o[32];
-                tmem_ld32(ts + 32 * h, o);
-                tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[16 * h + i] = make_float2(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1]));
-            }
+            for (int i = 0; i < 64; ++i) x[i] = make_float2(__uint_as_float(o[i >> 4][2 * (i & 15)]), __uint_as_float(o[i >> 4][2 * (i & 15) + 1]));
             if (BOXES == 1) {
                 tc_fence_before_sync();
                 pipe_arrive_warp(pp, G::BAR_READ + w, lane);
@@ -218,15 +232,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
                     if (2 * i + 1 >= left) x[i].y = -INFINITY;
                 }
             }
-            float m = fmaxf(x[0].x, x[0].y);
+            float top[4];                                                        // (four chains: one of 64 would take longer than the rest)
 #pragma unroll
-            for (int i = 1; i < 64; ++i) m = max3(m, x[i].x, x[i].y);
-            m *= c1;
-            const bool grow = m > ref + 8.f;                                     // (always of a row without a key so far)
+            for (int i = 0; i < 4; ++i) top[i] = max_nan(x[i].x, x[i].y);
+#pragma unroll
+            for (int i = 4; i < 64; ++i) top[i & 3] = max3_nan(top[i & 3], x[i].x, x[i].y);
+            const float m = max_nan(max3_nan(top[0], top[1], top[2]), top[3]) * c1;
+            const bool grow = !(m <= ref + 8.f);                                 // (a NaN makes its row NaN)
             if (__any_sync(0xffffffffu, grow)) {
                 const float next = grow ? m : ref, f = grow ? fast_exp2(ref - next) : 1.f;      // (exp2(-inf) = 0)
                 ref = next;
-                sum = fmul2(sum, make_float2(f, f));
+                sum[0] = fmul2(sum[0], make_float2(f, f));
+                sum[1] = fmul2(sum[1], make_float2(f, f));
                 if (j > 0) {
                     wait_soon(pp, G::BAR_O + w, j - 1);
                     tc_fence_after_sync();
@@ -240,23 +257,42 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
                         tmem_st32(to + 32 * h, o);
                     }
                 }
-            } else if (BOXES == 1 && j > 0) {
-                wait_soon(pp, G::BAR_O + w, j - 1);                              // (P V of the keys before has read its probabilities)
-                tc_fence_after_sync();
             }
             const float nr = ref == -INFINITY ? 0.f : -ref;
+            uint32_t p[4][16];
+            if (TURNS && (w == 0 ? j > 0 && j <= n[1] : j < n[0])) bar_sync_pair(1 + (warp & 3) + 4 * w);
+            // groups of eight pairs: exponentials of one, sums and roundings of the one before
+            float2 v[2][8];
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                uint32_t p[16];
+            for (int g = 0; g <= 8; ++g) {
+                if (g < 8) {
+                    float2 e[8];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float2 e = ffma2(x[16 * h + i], make_float2(c1, c1), make_float2(nr, nr));
-                    const float2 v = make_float2(fast_exp2(e.x), fast_exp2(e.y));
-                    sum = fadd2(sum, v);
-                    p[i] = pack2<T>(v.x, v.y);
+                    for (int i = 0; i < 8; ++i) e[i] = ffma2(x[8 * g + i], make_float2(c1, c1), make_float2(nr, nr));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[g & 1][i] = false ? exp2_fma(e[i]) : make_float2(fast_exp2(e[i].x), fast_exp2(e[i].y));
                 }
-                tmem_st16(tp + 16 * h, p);
+                if (g > 0) {
+                    const int k = g - 1;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        sum[i & 1] = fadd2(sum[i & 1], v[k & 1][i]);
+                        p[k >> 1][8 * (k & 1) + i] = pack2<T>(v[k & 1][i].x, v[k & 1][i].y);
+                    }
+                    if (BOXES == 1 && k == 5 && j > 0) {                         // P V of the keys before has read its probabilities
+                        wait_soon(pp, G::BAR_O + w, j - 1);
+                        tc_fence_after_sync();
+                    }
+                    if (k & 1) {
+                        if (BOXES == 2 || k >= 5) tmem_st16(tp + 8 * (k - 1), p[k >> 1]);
+                        if (BOXES == 1 && k == 5) {
+                            tmem_st16(tp, p[0]);
+                            tmem_st16(tp + 16, p[1]);
+                        }
+                    }
+                }
             }
+            if (TURNS && (w == 0 ? j < n[1] : j + 1 < n[0])) bar_arrive_pair(5 + (warp & 3) - 4 * w);
             tmem_st_wait();
             tc_fence_before_sync();
             pipe_arrive_warp(pp, G::BAR_P + w, lane);
@@ -267,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             wait_soon(pp, G::BAR_MENDED, 0);
             tc_fence_after_sync();
         }
-        const float total = sum.x + sum.y, inv = limit > 0 ? 1.f / total : 0.f;
+        const float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y), inv = limit > 0 ? 1.f / total : 0.f;
         T* out = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + token) * a.lo.st;
 #pragma unroll
         for (int h = 0; h < 2 * BOXES; ++h) {

@@ -1,6 +1,7 @@
 // Softmax attention over whole sequences on the 5th-generation tensor cores: what the forward kernel and the gradients' share.
 #pragma once
 #include "attend.cuh"
+#include "pair.cuh"
 #include "stream_common.cuh"
 
 namespace aa {
@@ -52,24 +53,66 @@ __device__ __forceinline__ void wait_soon(Pipe& pp, int i, uint32_t parity) {
     *reinterpret_cast<volatile int*>(pp.dead) = 1;
     if (pp.status) atomicCAS(pp.status, 0, kAttendTimeout);
 }
+// 2^x of a pair on the FMA pipe: the special-function unit makes 16 exponentials a cycle and SM and bounds these kernels, so that a share of them is made here.
+// x = n + f, |f| <= 1/2, n by adding 1.5 2^23; 2^f as a polynomial of degree 5 fitted here for the least relative error (2.4e-7 in fp32).  Below -126: 2^-126;
+// what is masked does not come here.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;\n" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float2 exp2_fma(float2 x) {
+    x.x = max_nan(x.x, -126.f);
+    x.y = max_nan(x.y, -126.f);
+    const float2 t = fadd2(x, make_float2(12582912.f, 12582912.f));
+    const float2 f = fadd2(x, fadd2(make_float2(12582912.f, 12582912.f), make_float2(-t.x, -t.y)));
+    auto c = [](float v) { return make_float2(v, v); };
+    float2 p = ffma2(f, c(0.0013276472f), c(0.0096755419f));
+    p = ffma2(p, f, c(0.055507131f));
+    p = ffma2(p, f, c(0.2402212f));
+    p = ffma2(p, f, c(0.69314694f));
+    p = ffma2(p, f, c(1.0000001f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
 // Rows `from` .. 127 of a tile in shared memory (`boxes` of 64 channels) become zero: what lies behind a sequence must not meet a probability of zero.
 __device__ __forceinline__ void clear_rows(uint32_t tile, int boxes, int from, int lane) {
     for (int b = 0; b < boxes; ++b)
         for (uint32_t at = from * 128 + lane * 16; at < (uint32_t)kTileBytes; at += 512)
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(tile + b * kTileBytes + at), "r"(0) : "memory");
 }
-// D (+)= A B with A (128 rows) and B in shared memory, both K-major: `steps` of 16 channels
-template <int BOXES> __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t id, int steps) {
-    const uint64_t da = umma_desc_sw128(a), db = umma_desc_sw128(b);
-#pragma unroll
-    for (int k = 0; k < 4 * BOXES; ++k)
-        if (k < steps) umma_ss_w(d, da + (k >> 2) * (kTileBytes >> 4) + 2 * (k & 3), db + (k >> 2) * (kTileBytes >> 4) + 2 * (k & 3), id, k > 0);
+// Four steps of 16 of a sum with A in tensor memory (8 columns a step) and B's rows the sum's, by the elected lane
+__device__ __forceinline__ void umma_four_ts(uint32_t elected, uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q, t;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\tsetp.ne.b32 q, %5, 0;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+        "add.s32 a, %1, 8;\n\tadd.s64 b, %2, 128;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+        "add.s32 a, a, 8;\n\tadd.s64 b, b, 128;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+        "add.s32 a, a, 8;\n\tadd.s64 b, b, 128;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t}\n"
+        ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate), "r"(elected) : "memory");
 }
-// D (+)= P B: P (128 rows, 128 columns of 16 bits) in tensor memory, B's rows are the sum's
-template <int BOXES> __device__ __forceinline__ void mma_sum(uint32_t d, uint32_t p, uint32_t b, uint32_t id, bool add) {
-    const uint64_t db = BOXES == 1 ? umma_desc_sw128(b) : desc_mn(b, kTileBytes);
+// D = A B with A (128 rows) and B in shared memory, both K-major: `steps` of 16 channels
+template <int BOXES> __device__ __forceinline__ void mma_rows(uint32_t elected, uint32_t d, uint32_t a, uint32_t b, uint32_t id, int steps) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) umma_ts_w(d, p + 8 * k, db + 128 * k, id, add || k > 0);
+    for (int x = 0; x < BOXES; ++x) {
+        const uint64_t da = umma_desc_sw128(a + x * kTileBytes), db = umma_desc_sw128(b + x * kTileBytes);
+        if (steps >= 4 * x + 4) umma_four<false, 2, 2>(elected, d, da, db, id, x);
+        else
+            for (int k = 0; k < steps - 4 * x; ++k) umma_step<false>(elected, d, da + 2 * k, db + 2 * k, id, x | k);
+    }
+}
+// D (+)= P B: P (128 rows, 128 columns of 16 bits: 64 in `p`, 64 in `p2`) in tensor memory, B's rows are the sum's
+template <int BOXES> __device__ __forceinline__ void mma_sum(uint32_t elected, uint32_t d, uint32_t p, uint32_t p2, uint32_t b, uint32_t id, bool add) {
+    const uint64_t db = BOXES == 1 ? umma_desc_sw128(b) : desc_mn(b, kTileBytes);
+    umma_four_ts(elected, d, p, db, id, add);
+    umma_four_ts(elected, d, p2, db + 512, id, 1);
 }
 
 }  // namespace aa
