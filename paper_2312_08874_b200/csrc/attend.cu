@@ -21,10 +21,10 @@ namespace {
 template <typename T> struct Oper { using E = T; static constexpr int kTerms = 1; };
 template <> struct Oper<float> { using E = __nv_bfloat16; static constexpr int kTerms = 3; };
 
-// `count` rows of DK channels (d of them exist, the others are zero) -> planes of terms at `dst`; row(i): address or null (zeros)
-template <typename T, int DK, int THREADS, typename F> __device__ __forceinline__ void load_tile(unsigned char* dst, uint32_t plane, int count, int d, const void* some, F row) {
+// `count` rows of DK channels (d of them exist, the others are zero) -> planes of terms at `dst`, by THREADS threads; row(i): address or null (zeros)
+template <typename T, int DK, int THREADS, typename F> __device__ __forceinline__ void load_tile(int me, unsigned char* dst, uint32_t plane, int count, int d, const void* some, F row) {
     constexpr int kPitch = TileGeom<DK>::kPitch, kGroups = DK / 8;
-    for (int i = threadIdx.x; i < count * kGroups; i += THREADS) {
+    for (int i = me; i < count * kGroups; i += THREADS) {
         const int r = i / kGroups, c = i % kGroups * 8;
         const T* src = row(r);
         unsigned char* to = dst + r * kPitch + c * 2;
@@ -125,9 +125,9 @@ template <typename E, int NT> __device__ __forceinline__ void block_operand(cons
 }
 // Values that are not finite, in a block of which some rows see only a part: zero in shared memory (0 * infinity is NaN), and first_bad keeps
 // for every channel the first key that has one, so that the rows that do see it become NaN at the end.
-template <typename E, int NT, int DK, int THREADS> __device__ void clean_values(unsigned char* v, uint32_t plane, int keys, int k0, int* first_bad) {
+template <typename E, int NT, int DK, int THREADS> __device__ void clean_values(int me, unsigned char* v, uint32_t plane, int keys, int k0, int* first_bad) {
     constexpr int kPitch = TileGeom<DK>::kPitch;
-    for (int i = threadIdx.x; i < keys * DK; i += THREADS) {
+    for (int i = me; i < keys * DK; i += THREADS) {
         E* at = reinterpret_cast<E*>(v + i / DK * kPitch) + i % DK;
         bool bad = false;
 #pragma unroll
@@ -179,17 +179,25 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
 
     const T* kp = static_cast<const T*>(a.k) + k.batch * a.lk.sb + hk * a.lk.sh + (long long)k.first * a.lk.st;
     const T* vp = static_cast<const T*>(a.v) + k.batch * a.lv.sb + hk * a.lv.sh + (long long)k.first * a.lv.st;
-    load_tile<T, DK, G::kThreads>(smem, G::kQPlane, G::kRows, a.d, a.q, [&](int r) -> const T* {
+    load_tile<T, DK, G::kThreads>(tid, smem, G::kQPlane, G::kRows, a.d, a.q, [&](int r) -> const T* {
         const int i = row0 + r;
         return i < rows ? static_cast<const T*>(a.q) + q.batch * a.lq.sb + (hk * group + i % group) * a.lq.sh + (long long)(q.first + i / group) * a.lq.st : nullptr;
     });
+    if (G::kStages > 1) cp_async_commit();
     for (int c = tid; c < DK; c += G::kThreads) first_bad[c] = INT_MAX;
     const int steps = (end - begin + G::kStep - 1) / G::kStep;
+    // warps that share their keys fetch them together; one that has its own (WK > 1) waits for no other
+    constexpr int LOADERS = WK > 1 ? 32 : G::kThreads, OWN = WK > 1 ? 32 : G::kStep;
+    const int me = WK > 1 ? lane : tid;
+    auto meet = [&] {
+        if (WK > 1) __syncwarp();
+        else __syncthreads();
+    };
     auto fetch = [&](int s) {
-        unsigned char* to = ring + (s % G::kStages) * G::kStage;
-        const int k0 = begin + s * G::kStep;
-        load_tile<T, DK, G::kThreads>(to, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return k0 + r < end ? kp + (long long)(k0 + r) * a.lk.st : nullptr; });
-        load_tile<T, DK, G::kThreads>(to + NT * G::kPlane, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return k0 + r < end ? vp + (long long)(k0 + r) * a.lv.st : nullptr; });
+        unsigned char* to = ring + (s % G::kStages) * G::kStage + (WK > 1 ? wk * 32 * P : 0);
+        const int k0 = begin + s * G::kStep + (WK > 1 ? wk * 32 : 0);
+        load_tile<T, DK, LOADERS>(me, to, G::kPlane, OWN, a.d, a.q, [&](int r) -> const T* { return k0 + r < end ? kp + (long long)(k0 + r) * a.lk.st : nullptr; });
+        load_tile<T, DK, LOADERS>(me, to + NT * G::kPlane, G::kPlane, OWN, a.d, a.q, [&](int r) -> const T* { return k0 + r < end ? vp + (long long)(k0 + r) * a.lv.st : nullptr; });
     };
     if (G::kStages > 1) {
 #pragma unroll
@@ -211,27 +219,31 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
     for (int c = 0; c < DK / 8; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[c][e] = 0.f;
+    if (WK > 1 || G::kStages == 1) {               // (the queries, and first_bad)
+        if (G::kStages > 1) cp_async_wait<G::kStages - 1>();
+        __syncthreads();
+    }
     const uint32_t qa = smem_u32(smem) + wr * 16 * P + val_lane_offset<DK>(lane);
 
     for (int s = 0; s < steps; ++s) {
         if (G::kStages > 1) {
             cp_async_wait<(G::kStages > 1 ? G::kStages - 2 : 0)>();
-            __syncthreads();
+            meet();
             if (s + G::kStages - 1 < steps) fetch(s + G::kStages - 1);
             cp_async_commit();
         } else {
-            if (s) __syncthreads();
+            if (s) meet();
             fetch(s);
-            __syncthreads();
+            meet();
         }
         unsigned char* stage = ring + (s % G::kStages) * G::kStage;
         const int block0 = begin + s * G::kStep;
-        if (block0 + G::kStep > k_whole) {
-            clean_values<E, NT, DK, G::kThreads>(stage + NT * G::kPlane, G::kPlane, min(G::kStep, end - block0), block0, first_bad);
-            __syncthreads();
-        }
         const int k0 = block0 + wk * 32;
-        if (k0 >= end) continue;                   // (warp-uniform; the barriers above are met by all)
+        if (k0 >= end) continue;                   // (of a warp with its own keys: nothing is left to do but the barriers behind the loop)
+        if (k0 + OWN > k_whole) {
+            clean_values<E, NT, DK, LOADERS>(me, stage + NT * G::kPlane + (WK > 1 ? wk * 32 * P : 0), G::kPlane, min(OWN, end - k0), k0, first_bad);
+            meet();
+        }
         const uint32_t kb = smem_u32(stage) + wk * 32 * P;
         float x[4][4];
         block_logits<E, NT, DK>(x, qa, G::kQPlane, kb + key_lane_offset<DK>(lane), G::kPlane);
@@ -488,8 +500,8 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
     auto stat = [&](int i) {
         return __ldg(reinterpret_cast<const float2*>(a.ws) + ((long long)q.batch * a.heads + hk * group + i % group) * a.N + q.first + i / group);
     };
-    load_tile<T, DK, 128>(xs, G::kRowPlane, G::kRows, a.d, a.q, [&](int r) -> const T* { return row0 + r < rows ? (KEYS ? key(a.k, a.lk, row0 + r) : query(a.q, a.lq, row0 + r)) : nullptr; });
-    load_tile<T, DK, 128>(ys, G::kRowPlane, G::kRows, a.d, a.q, [&](int r) -> const T* { return row0 + r < rows ? (KEYS ? key(a.v, a.lv, row0 + r) : query(a.dout, a.ldo, row0 + r)) : nullptr; });
+    load_tile<T, DK, 128>(tid, xs, G::kRowPlane, G::kRows, a.d, a.q, [&](int r) -> const T* { return row0 + r < rows ? (KEYS ? key(a.k, a.lk, row0 + r) : query(a.q, a.lq, row0 + r)) : nullptr; });
+    load_tile<T, DK, 128>(tid, ys, G::kRowPlane, G::kRows, a.d, a.q, [&](int r) -> const T* { return row0 + r < rows ? (KEYS ? key(a.v, a.lv, row0 + r) : query(a.dout, a.ldo, row0 + r)) : nullptr; });
     // columns that some row of the tile meets
     int begin = 0, end;
     if (KEYS) {
@@ -524,8 +536,8 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
     const uint32_t ut = smem_u32(us) + val_lane_offset<DK>(lane), wt = ut + (uint32_t)(ws - us);
     for (int c0 = begin; c0 < end; c0 += G::kStep) {
         if (c0 != begin) __syncthreads();
-        load_tile<T, DK, 128>(us, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.q, a.lq, c0 + r) : key(a.k, a.lk, c0 + r)) : nullptr; });
-        load_tile<T, DK, 128>(ws, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.dout, a.ldo, c0 + r) : key(a.v, a.lv, c0 + r)) : nullptr; });
+        load_tile<T, DK, 128>(tid, us, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.q, a.lq, c0 + r) : key(a.k, a.lk, c0 + r)) : nullptr; });
+        load_tile<T, DK, 128>(tid, ws, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.dout, a.ldo, c0 + r) : key(a.v, a.lv, c0 + r)) : nullptr; });
         if (KEYS && tid < G::kStep) stats[tid] = c0 + tid < end ? stat(c0 + tid) : make_float2(0.f, 0.f);
         __syncthreads();
         float x[4][4], y[4][4];
@@ -604,7 +616,10 @@ cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st
     if (dtype != 0 && !few_rows(a)) return launch_attend_umma(dtype, a, st);
     if (dtype == 1) return rows_of_type<__nv_bfloat16, 1, 4>(a, shares, st);
     if (dtype == 2) return rows_of_type<__half, 1, 4>(a, shares, st);
-    return few_rows(a) ? rows_of_type<float, 1, 4>(a, shares, st) : rows_of_type<float, 4, 1>(a, shares, st);
+    // Sixteen rows a block and four warps on the keys, too, where 64 rows would leave half of the SMs idle (196 tokens, 3 heads of 64: 26.6 -> x us); elsewhere
+    // every block of keys is split into terms for four times the rows.
+    const long long blocks = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, 64) * a.kv_heads;
+    return few_rows(a) || 2 * blocks <= sm_count ? rows_of_type<float, 1, 4>(a, shares, st) : rows_of_type<float, 4, 1>(a, shares, st);
 }
 cudaError_t launch_attend_backward(int dtype, const AttendArgs& a, int sm_count, cudaStream_t st, int* launches) {
     *launches = 3;
