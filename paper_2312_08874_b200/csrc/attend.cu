@@ -155,6 +155,46 @@ __device__ __forceinline__ long long row_index(const AttendArgs& a, const Span& 
     return ((long long)q.batch * a.N + q.first + token) * a.heads + head;
 }
 
+// Two channels of row r of a tile, once its state is known: the result, or a share's partial state
+template <typename T> __device__ __forceinline__ void put_pair(const AttendArgs& a, const Span& q, const Span& k, int hk, int end, const int* first_bad, int r, int c, float v0, float v1,
+                                                               float sum, float top) {
+    const int group = a.heads / a.kv_heads, token = r / group, head = hk * group + r % group, lim = min(end, visible_keys(a.causal, token, q.count, k.count));
+    if (first_bad[c] < lim) v0 = NAN;
+    if (first_bad[c + 1] < lim) v1 = NAN;
+    if (gridDim.z == 1) {
+        const float inv = lim > 0 ? 1.f / sum : 0.f;
+        T* to = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + token) * a.lo.st + c;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(to) = pack2<T>(v0 * inv, v1 * inv);
+        else *reinterpret_cast<float2*>(to) = make_float2(v0 * inv, v1 * inv);
+        if (c == 0 && a.lse) a.lse[((long long)q.batch * a.heads + head) * a.N + q.first + token] = lim > 0 ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    } else {
+        const long long at = row_index(a, q, token, head) * gridDim.z + blockIdx.z, all = (long long)a.batch * a.N * a.heads * gridDim.z;
+        *reinterpret_cast<float2*>(a.ws + (2 * all + 3) / 4 * 4 + at * a.d + c) = make_float2(v0, v1);
+        if (c == 0) *reinterpret_cast<float2*>(a.ws + 2 * at) = make_float2(top, sum);
+    }
+}
+// The states of WK warps that share rows meet in shared memory: [WK][ROWS][DK + 4], results, maximum, sum
+template <typename T, int DK, int ROWS, int WK, int THREADS>
+__device__ __forceinline__ void join_warps(const AttendArgs& a, const Span& q, const Span& k, int hk, int end, const int* first_bad, const float* join, int row0, int rows) {
+    for (int i = threadIdx.x; i < ROWS * (DK / 2); i += THREADS) {
+        const int r = i / (DK / 2), c = i % (DK / 2) * 2;
+        if (row0 + r >= rows || c >= a.d) continue;
+        float top = -INFINITY, sum = 0.f, v0 = 0.f, v1 = 0.f;
+#pragma unroll
+        for (int w = 0; w < WK; ++w) top = fmaxf(top, join[(w * ROWS + r) * (DK + 4) + DK]);
+        const float b = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int w = 0; w < WK; ++w) {
+            const float* s = join + (w * ROWS + r) * (DK + 4);
+            const float f = fast_exp2(s[DK] - b);
+            sum = fmaf(f, s[DK + 1], sum);
+            v0 = fmaf(f, s[c], v0);
+            v1 = fmaf(f, s[c + 1], v1);
+        }
+        put_pair<T>(a, q, k, hk, end, first_bad, row0 + r, c, v0, v1, sum, top);
+    }
+}
+
 template <typename T, int DK, int WR, int WK>
 __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     using G = RowsGeom<T, DK, WR, WK>;
@@ -283,25 +323,8 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) l[h] = quad_sum(l[h]);
-    const bool whole = gridDim.z == 1;
     __syncthreads();                               // (first_bad is complete; the ring may be written)
-    // one row's channels, once its state is known
-    auto finish = [&](int r, int c, float v0, float v1, float sum, float top) {
-        const int token = r / group, head = hk * group + r % group, lim = min(end, visible_keys(a.causal, token, q.count, k.count));
-        if (first_bad[c] < lim) v0 = NAN;
-        if (first_bad[c + 1] < lim) v1 = NAN;
-        if (whole) {
-            const float inv = lim > 0 ? 1.f / sum : 0.f;
-            T* to = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + token) * a.lo.st + c;
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(to) = pack2<T>(v0 * inv, v1 * inv);
-            else *reinterpret_cast<float2*>(to) = make_float2(v0 * inv, v1 * inv);
-            if (c == 0 && a.lse) a.lse[((long long)q.batch * a.heads + head) * a.N + q.first + token] = lim > 0 ? (top + log2f(sum)) * kLn2 : -INFINITY;
-        } else {
-            const long long at = row_index(a, q, token, head) * gridDim.z + share, all = (long long)a.batch * a.N * a.heads * gridDim.z;
-            *reinterpret_cast<float2*>(a.ws + (2 * all + 3) / 4 * 4 + at * a.d + c) = make_float2(v0, v1);
-            if (c == 0) *reinterpret_cast<float2*>(a.ws + 2 * at) = make_float2(top, sum);
-        }
-    };
+    auto finish = [&](int r, int c, float v0, float v1, float sum, float top) { put_pair<T>(a, q, k, hk, end, first_bad, r, c, v0, v1, sum, top); };
     if constexpr (WK == 1) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -320,28 +343,187 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
             if (t == 0) { to[DK] = m[h]; to[DK + 1] = l[h]; }
         }
         __syncthreads();
-        for (int i = tid; i < G::kRows * (DK / 2); i += G::kThreads) {
-            const int r = i / (DK / 2), c = i % (DK / 2) * 2;
-            if (row0 + r >= rows || c >= a.d) continue;
-            float top = -INFINITY, sum = 0.f, v0 = 0.f, v1 = 0.f;
-#pragma unroll
-            for (int w = 0; w < WK; ++w) top = fmaxf(top, join[(w * G::kRows + r) * (DK + 4) + DK]);
-            const float b = top == -INFINITY ? 0.f : top;
-#pragma unroll
-            for (int w = 0; w < WK; ++w) {
-                const float* s = join + (w * G::kRows + r) * (DK + 4);
-                const float f = fast_exp2(s[DK] - b);
-                sum = fmaf(f, s[DK + 1], sum);
-                v0 = fmaf(f, s[c], v0);
-                v1 = fmaf(f, s[c + 1], v1);
-            }
-            finish(row0 + r, c, v0, v1, sum, top);
-        }
+        join_warps<T, DK, G::kRows, WK, G::kThreads>(a, q, k, hk, end, first_bad, join, row0, rows);
     }
 }
 
+// Few queries over many keys, 16-bit types: sixteen rows a block, eight warps that take turns at sixteen keys each.  Bound by HBM, so keys and values go straight from
+// global memory into registers, a turn ahead, 16 bytes a lane and in whole lines:
+//   logits   lane (g, t) brings the channels 32 i + 8 t .. + 7 of key g: two steps of the product's sum, whose channels may come in any order if the queries' do so, too
+//   P V      lane (g, t) brings the channels 8 g .. 8 g + 7 of the keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9; byte permutes make the pairs of keys that the product wants,
+//            and column n of its tile i is channel 8 n + i
+// The exponents' reference moves only when a logit exceeds it by more than 8 (log2 units).
+template <int DK> struct FewKV {
+    uint4 k[2][DK / 32], v[4][DK / 64];
+};
+template <typename T, int DK> __global__ void __launch_bounds__(256) attend_few_kernel(const __grid_constant__ AttendArgs a) {
+    constexpr int WK = 8, kRows = 16, KI = DK / 32, VI = DK / 64;
+    extern __shared__ __align__(128) unsigned char smem[];
+    float* join = reinterpret_cast<float*>(smem);                       // [WK][16][DK + 4]
+    __shared__ int first_bad[DK];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int group = a.heads / a.kv_heads, hk = blockIdx.y;
+    int seq, tile;
+    if (!find_slot(a.q_offsets, a.sequences, a.N, group, kRows, blockIdx.x, &seq, &tile)) return;
+    const Span q = span_of(a.q_offsets, a.q_lengths, a.N, seq), k = span_of(a.k_offsets, a.k_lengths, a.M, seq);
+    const int rows = q.count * group, row0 = tile * kRows;
+    if (row0 >= rows) return;
+    const int last = min(rows, row0 + kRows) - 1, k_all = visible_keys(a.causal, last / group, q.count, k.count);
+    const int begin = (int)min((long long)k_all, (long long)blockIdx.z * a.chunk), end = (int)min((long long)k_all, (long long)begin + a.chunk);
+    if (blockIdx.z > 0 && begin >= k_all) return;
+    const int k_whole = visible_keys(a.causal, row0 / group, q.count, k.count);          // keys that every row sees
+    const T* kp = static_cast<const T*>(a.k) + k.batch * a.lk.sb + hk * a.lk.sh + (long long)k.first * a.lk.st;
+    const T* vp = static_cast<const T*>(a.v) + k.batch * a.lv.sb + hk * a.lv.sh + (long long)k.first * a.lv.st;
+    for (int c = tid; c < DK; c += 256) first_bad[c] = INT_MAX;
+    __syncthreads();
+
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    uint4 x[2][KI];                                                     // queries: rows g and g + 8, channels 32 i + 8 t
+    int limit[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = row0 + g + 8 * h;
+        limit[h] = r < rows ? min(end, visible_keys(a.causal, r / group, q.count, k.count)) : 0;
+        const T* src = static_cast<const T*>(a.q) + q.batch * a.lq.sb + (hk * group + r % group) * a.lq.sh + (long long)(q.first + r / group) * a.lq.st;
+#pragma unroll
+        for (int i = 0; i < KI; ++i) x[h][i] = r < rows && 32 * i + 8 * t < a.d ? __ldg(reinterpret_cast<const uint4*>(src + 32 * i + 8 * t)) : zero;
+    }
+    auto load = [&](FewKV<DK>& f, int k0) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int key = k0 + 8 * n + g;
+            const T* src = kp + (long long)key * a.lk.st;
+#pragma unroll
+            for (int i = 0; i < KI; ++i) f.k[n][i] = key < end && 32 * i + 8 * t < a.d ? __ldg(reinterpret_cast<const uint4*>(src + 32 * i + 8 * t)) : zero;
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const int key = k0 + 2 * t + (n & 1) + 8 * (n >> 1);
+            const T* src = vp + (long long)key * a.lv.st;
+#pragma unroll
+            for (int i = 0; i < VI; ++i) f.v[n][i] = key < end && 64 * i + 8 * g < a.d ? __ldg(reinterpret_cast<const uint4*>(src + 64 * i + 8 * g)) : zero;
+        }
+    };
+    const float c1 = a.scale * kLog2e;
+    float ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[VI][8][4];
+#pragma unroll
+    for (int i = 0; i < VI; ++i)
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][n][e] = 0.f;
+    auto use = [&](FewKV<DK>& f, int k0) {
+        float s[2][4];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < KI; ++i) {
+                const uint32_t a0[4] = {x[0][i].x, x[1][i].x, x[0][i].y, x[1][i].y}, a1[4] = {x[0][i].z, x[1][i].z, x[0][i].w, x[1][i].w};
+                if (i == 0) mma_set<T>(s[n], a0, f.k[n][i].x, f.k[n][i].y);
+                else mma_acc<T>(s[n], a0, f.k[n][i].x, f.k[n][i].y);
+                mma_acc<T>(s[n], a1, f.k[n][i].z, f.k[n][i].w);
+            }
+        if (k0 + 16 > k_whole || k0 + 16 > end) {                       // (some rows do not see all: see clean_values)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (k0 + 8 * n + 2 * t + (e & 1) >= limit[e >> 1]) s[n][e] = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int i = 0; i < VI; ++i) {
+                    uint32_t* w = reinterpret_cast<uint32_t*>(&f.v[n][i]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 p = unpack2<T>(w[e >> 1]);
+                        if (!(fabsf(e & 1 ? p.y : p.x) < INFINITY)) {
+                            w[e >> 1] &= e & 1 ? 0xffffu : 0xffff0000u;
+                            atomicMin(first_bad + 64 * i + 8 * g + e, k0 + 2 * t + (n & 1) + 8 * (n >> 1));
+                        }
+                    }
+                }
+        }
+        float m[2];
+        bool grow = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            m[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1])) * c1;
+            grow |= m[h] > ref[h] + 8.f;
+        }
+        if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float top = quad_max(m[h]);
+                if (!(top > ref[h] + 8.f)) continue;                    // (the same of a row's four lanes; no shuffles below)
+                const float f = fast_exp2(ref[h] - top);                // (0 of a row without a key so far)
+                ref[h] = top;
+                l[h] *= f;
+#pragma unroll
+                for (int i = 0; i < VI; ++i)
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        o[i][n][2 * h] *= f;
+                        o[i][n][2 * h + 1] *= f;
+                    }
+            }
+        }
+        const float base[2] = {ref[0] == -INFINITY ? 0.f : ref[0], ref[1] == -INFINITY ? 0.f : ref[1]};
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[n][e] = fast_exp2(fmaf(s[n][e], c1, -base[e >> 1]));
+                l[e >> 1] += s[n][e];
+            }
+        const uint32_t p[4] = {pack2<T>(s[0][0], s[0][1]), pack2<T>(s[0][2], s[0][3]), pack2<T>(s[1][0], s[1][1]), pack2<T>(s[1][2], s[1][3])};
+#pragma unroll
+        for (int i = 0; i < VI; ++i) {
+            const uint32_t *v0 = reinterpret_cast<const uint32_t*>(&f.v[0][i]), *v1 = reinterpret_cast<const uint32_t*>(&f.v[1][i]);
+            const uint32_t *v2 = reinterpret_cast<const uint32_t*>(&f.v[2][i]), *v3 = reinterpret_cast<const uint32_t*>(&f.v[3][i]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                mma_acc<T>(o[i][2 * w], p, __byte_perm(v0[w], v1[w], 0x5410), __byte_perm(v2[w], v3[w], 0x5410));
+                mma_acc<T>(o[i][2 * w + 1], p, __byte_perm(v0[w], v1[w], 0x7632), __byte_perm(v2[w], v3[w], 0x7632));
+            }
+        }
+    };
+    FewKV<DK> f0, f1;
+    int k0 = begin + 16 * warp;
+    if (k0 < end) load(f0, k0);
+    while (k0 < end) {
+        if (k0 + 16 * WK < end) load(f1, k0 + 16 * WK);
+        use(f0, k0);
+        k0 += 16 * WK;
+        if (k0 >= end) break;
+        if (k0 + 16 * WK < end) load(f0, k0 + 16 * WK);
+        use(f1, k0);
+        k0 += 16 * WK;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        l[h] = quad_sum(l[h]);
+        float* to = join + (warp * kRows + g + 8 * h) * (DK + 4);
+#pragma unroll
+        for (int i = 0; i < VI; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float4* d = reinterpret_cast<float4*>(to + 64 * i + 16 * t + 8 * e);
+                d[0] = make_float4(o[i][0][2 * h + e], o[i][1][2 * h + e], o[i][2][2 * h + e], o[i][3][2 * h + e]);
+                d[1] = make_float4(o[i][4][2 * h + e], o[i][5][2 * h + e], o[i][6][2 * h + e], o[i][7][2 * h + e]);
+            }
+        if (t == 0) {
+            to[DK] = ref[h];
+            to[DK + 1] = l[h];
+        }
+    }
+    __syncthreads();
+    join_warps<T, DK, kRows, WK, 256>(a, q, k, hk, end, first_bad, join, row0, rows);
+}
+
 // Joins the states of a row's shares in order; a warp takes a row, a lane four channels.
-template <typename T, int ROWS> __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a, int shares) {
+template <typename T> __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a, int shares) {
+    constexpr int ROWS = 16;                       // (shares are of few rows)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = a.heads / a.kv_heads, hk = blockIdx.y;
     int seq, tile;
     if (!find_slot(a.q_offsets, a.sequences, a.N, group, ROWS, blockIdx.x, &seq, &tile)) return;
@@ -383,6 +565,10 @@ template <typename T, int ROWS> __global__ void __launch_bounds__(128) attend_jo
     }
 }
 
+template <typename T> cudaError_t run_join(const AttendArgs& a, int shares, long long slots, cudaStream_t st) {
+    attend_join_kernel<T><<<dim3((unsigned)slots, a.kv_heads), 128, 0, st>>>(a, shares);
+    return cudaGetLastError();
+}
 template <typename T, int DK, int WR, int WK> cudaError_t run_rows(const AttendArgs& a, int shares, cudaStream_t st) {
     using G = RowsGeom<T, DK, WR, WK>;
     static std::atomic<unsigned long long> done{0};
@@ -390,11 +576,16 @@ template <typename T, int DK, int WR, int WK> cudaError_t run_rows(const AttendA
     const long long slots = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, G::kRows);
     attend_rows_kernel<T, DK, WR, WK><<<dim3((unsigned)slots, a.kv_heads, shares), G::kThreads, G::kSmem, st>>>(a);
     if (cudaError_t e = cudaGetLastError()) return e;
-    if (shares > 1) {
-        attend_join_kernel<T, G::kRows><<<dim3((unsigned)slots, a.kv_heads), 128, 0, st>>>(a, shares);
-        return cudaGetLastError();
-    }
-    return cudaSuccess;
+    return shares > 1 ? run_join<T>(a, shares, slots, st) : cudaSuccess;
+}
+template <typename T, int DK> cudaError_t run_few(const AttendArgs& a, int shares, cudaStream_t st) {
+    constexpr int kSmem = 8 * 16 * (DK + 4) * 4;
+    static std::atomic<unsigned long long> done{0};
+    if (cudaError_t e = allow_smem(attend_few_kernel<T, DK>, done, kSmem)) return e;
+    const long long slots = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, 16);
+    attend_few_kernel<T, DK><<<dim3((unsigned)slots, a.kv_heads, shares), 256, kSmem, st>>>(a);
+    if (cudaError_t e = cudaGetLastError()) return e;
+    return shares > 1 ? run_join<T>(a, shares, slots, st) : cudaSuccess;
 }
 
 // Few rows a sequence: sixteen of them a block, whose four warps take turns at the keys.
@@ -614,8 +805,8 @@ cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st
     const int shares = shares_of(a, sm_count, &a.chunk);
     *launches = shares > 1 ? 2 : 1;
     if (dtype != 0 && !few_rows(a)) return launch_attend_umma(dtype, a, st);
-    if (dtype == 1) return rows_of_type<__nv_bfloat16, 1, 4>(a, shares, st);
-    if (dtype == 2) return rows_of_type<__half, 1, 4>(a, shares, st);
+    if (dtype == 1) return a.d <= 64 ? run_few<__nv_bfloat16, 64>(a, shares, st) : run_few<__nv_bfloat16, 128>(a, shares, st);
+    if (dtype == 2) return a.d <= 64 ? run_few<__half, 64>(a, shares, st) : run_few<__half, 128>(a, shares, st);
     // Sixteen rows a block and four warps on the keys, too, where 64 rows would leave half of the SMs idle (196 tokens, 3 heads of 64: 26.6 -> x us); elsewhere
     // every block of keys is split into terms for four times the rows.
     const long long blocks = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, 64) * a.kv_heads;
