@@ -9,7 +9,7 @@
 // tensor core after 32 of them and join in fp32 registers, since its accumulators cut off what lies below the last bit.
 //
 // Few rows on a long axis: shares of `chunk` keys a block, whose states (maximum, sum, result) a second kernel joins in order.  Bound by HBM then.
-#include "attend.cuh"
+#include "attend_umma.cuh"
 #include "bwd_terms.cuh"
 
 #include <algorithm>
@@ -347,20 +347,29 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
     }
 }
 
-// Few queries over many keys, 16-bit types: sixteen rows a block, eight warps that take turns at sixteen keys each.  Bound by HBM, so keys and values go straight from
-// global memory into registers, a turn ahead, 16 bytes a lane and in whole lines:
-//   logits   lane (g, t) brings the channels 32 i + 8 t .. + 7 of key g: two steps of the product's sum, whose channels may come in any order if the queries' do so, too
-//   P V      lane (g, t) brings the channels 8 g .. 8 g + 7 of the keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9; byte permutes make the pairs of keys that the product wants,
+// Few queries over many keys, 16-bit types: sixteen rows a block, four warps that take turns at sixteen keys each.  Bound by HBM: every warp has a ring of its own that
+// TMA fills (100 KB in flight a SM; a turn ahead in registers was 64 KB and 4.5 TB/s), takes its keys and values from there into registers, 16 bytes a lane, and
+// hands the stage back before it computes:
+//   logits   lane (g, t) takes the channels 32 i + 8 t .. + 7 of key g: two steps of the product's sum, whose channels may come in any order if the queries' do so, too
+//   P V      lane (g, t) takes the channels 8 g .. 8 g + 7 of the keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9; byte permutes make the pairs of keys that the product wants,
 //            and column n of its tile i is channel 8 n + i
 // The exponents' reference moves only when a logit exceeds it by more than 8 (log2 units).
+constexpr int kFewWarps = 4, kFewStages = 3, kFewKeys = 16;
+struct FewArgs {
+    AttendArgs a;
+    RowMap k, v;
+};
 template <int DK> struct FewKV {
     uint4 k[2][DK / 32], v[4][DK / 64];
 };
-template <typename T, int DK> __global__ void __launch_bounds__(256) attend_few_kernel(const __grid_constant__ AttendArgs a) {
-    constexpr int WK = 8, kRows = 16, KI = DK / 32, VI = DK / 64;
-    extern __shared__ __align__(128) unsigned char smem[];
-    float* join = reinterpret_cast<float*>(smem);                       // [WK][16][DK + 4]
+template <typename T, int DK> __global__ void __launch_bounds__(32 * kFewWarps) attend_few_kernel(const __grid_constant__ FewArgs f) {
+    constexpr int WK = kFewWarps, kRows = 16, KI = DK / 32, VI = DK / 64, kBox = kFewKeys * 128, kStage = 2 * VI * kBox;
+    const AttendArgs& a = f.a;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    float* join = reinterpret_cast<float*>(smem);                       // [WK][16][DK + 4], once the rings are done with
     __shared__ int first_bad[DK];
+    __shared__ __align__(8) unsigned long long bars[WK * kFewStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int group = a.heads / a.kv_heads, hk = blockIdx.y;
     int seq, tile;
@@ -372,10 +381,27 @@ template <typename T, int DK> __global__ void __launch_bounds__(256) attend_few_
     const int begin = (int)min((long long)k_all, (long long)blockIdx.z * a.chunk), end = (int)min((long long)k_all, (long long)begin + a.chunk);
     if (blockIdx.z > 0 && begin >= k_all) return;
     const int k_whole = visible_keys(a.causal, row0 / group, q.count, k.count);          // keys that every row sees
-    const T* kp = static_cast<const T*>(a.k) + k.batch * a.lk.sb + hk * a.lk.sh + (long long)k.first * a.lk.st;
-    const T* vp = static_cast<const T*>(a.v) + k.batch * a.lv.sb + hk * a.lv.sh + (long long)k.first * a.lv.st;
-    for (int c = tid; c < DK; c += 256) first_bad[c] = INT_MAX;
+    for (int c = tid; c < DK; c += 32 * WK) first_bad[c] = INT_MAX;
+    pdl_release_next();                            // (of a launch that does not depend on this one nothing is said by it)
+    if (tid == 0) {
+        for (int i = 0; i < WK * kFewStages; ++i) mbar_init(smem_u32(bars + i), 1);
+        mbar_fence_init();
+    }
     __syncthreads();
+    const uint32_t ring = smem_u32(smem) + warp * kFewStages * kStage, bar = smem_u32(bars + warp * kFewStages);
+    const int k0 = begin + kFewKeys * warp, turns = k0 < end ? (end - k0 + WK * kFewKeys - 1) / (WK * kFewKeys) : 0;
+    auto fetch = [&](int i) {                                           // (by one lane)
+        const uint32_t to = ring + (i % kFewStages) * kStage, full = bar + 8 * (i % kFewStages);
+        const int row = k.first + k0 + i * WK * kFewKeys;
+        mbar_arrive_expect_tx(full, kStage);
+#pragma unroll
+        for (int b = 0; b < VI; ++b) {
+            load_rows(to + b * kBox, f.k, 64 * b, row, hk, k.batch, full);
+            load_rows(to + (VI + b) * kBox, f.v, 64 * b, row, hk, k.batch, full);
+        }
+    };
+    if (lane == 0)
+        for (int i = 0; i < min(turns, kFewStages); ++i) fetch(i);
 
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
     uint4 x[2][KI];                                                     // queries: rows g and g + 8, channels 32 i + 8 t
@@ -388,20 +414,17 @@ template <typename T, int DK> __global__ void __launch_bounds__(256) attend_few_
 #pragma unroll
         for (int i = 0; i < KI; ++i) x[h][i] = r < rows && 32 * i + 8 * t < a.d ? __ldg(reinterpret_cast<const uint4*>(src + 32 * i + 8 * t)) : zero;
     }
-    auto load = [&](FewKV<DK>& f, int k0) {
+    auto take = [&](FewKV<DK>& f, int i) {
+        const unsigned char* from = smem + (ring - smem_u32(smem)) + (i % kFewStages) * kStage;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int key = k0 + 8 * n + g;
-            const T* src = kp + (long long)key * a.lk.st;
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int i = 0; i < KI; ++i) f.k[n][i] = key < end && 32 * i + 8 * t < a.d ? __ldg(reinterpret_cast<const uint4*>(src + 32 * i + 8 * t)) : zero;
-        }
+            for (int c = 0; c < KI; ++c) f.k[n][c] = *reinterpret_cast<const uint4*>(from + (c >> 1) * kBox + (8 * n + g) * 128 + (((4 * (c & 1) + t) ^ g) << 4));
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-            const int key = k0 + 2 * t + (n & 1) + 8 * (n >> 1);
-            const T* src = vp + (long long)key * a.lv.st;
+            const int key = 2 * t + (n & 1) + 8 * (n >> 1);
 #pragma unroll
-            for (int i = 0; i < VI; ++i) f.v[n][i] = key < end && 64 * i + 8 * g < a.d ? __ldg(reinterpret_cast<const uint4*>(src + 64 * i + 8 * g)) : zero;
+            for (int c = 0; c < VI; ++c) f.v[n][c] = *reinterpret_cast<const uint4*>(from + (VI + c) * kBox + key * 128 + ((g ^ (key & 7)) << 4));
         }
     };
     const float c1 = a.scale * kLog2e;
@@ -433,6 +456,7 @@ template <typename T, int DK> __global__ void __launch_bounds__(256) attend_few_
             for (int n = 0; n < 4; ++n)
 #pragma unroll
                 for (int i = 0; i < VI; ++i) {
+                    if (k0 + 2 * t + (n & 1) + 8 * (n >> 1) >= end) f.v[n][i] = zero;
                     uint32_t* w = reinterpret_cast<uint32_t*>(&f.v[n][i]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -488,18 +512,29 @@ template <typename T, int DK> __global__ void __launch_bounds__(256) attend_few_
             }
         }
     };
-    FewKV<DK> f0, f1;
-    int k0 = begin + 16 * warp;
-    if (k0 < end) load(f0, k0);
-    while (k0 < end) {
-        if (k0 + 16 * WK < end) load(f1, k0 + 16 * WK);
-        use(f0, k0);
-        k0 += 16 * WK;
-        if (k0 >= end) break;
-        if (k0 + 16 * WK < end) load(f0, k0 + 16 * WK);
-        use(f1, k0);
-        k0 += 16 * WK;
+    for (int i = 0; i < turns; ++i) {
+        FewKV<DK> kv;
+        if (!mbar_wait_bounded(bar + 8 * (i % kFewStages), (i / kFewStages) & 1, 1u << 22)) {
+            if (a.status) atomicCAS(a.status, 0, kAttendTimeout);
+            for (int n = i; n < min(turns, i + kFewStages); ++n) mbar_wait_bounded(bar + 8 * (n % kFewStages), (n / kFewStages) & 1, 1u << 22);      // (copies in flight)
+            break;
+        }
+        take(kv, i);
+        // The next copy must not overtake the loads: a vote on what they brought waits until it is in registers.
+        uint32_t words = 0;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+#pragma unroll
+            for (int c = 0; c < VI; ++c) words |= kv.v[n][c].x;
+#pragma unroll
+            for (int c = 0; c < KI; ++c) words |= kv.k[n & 1][c].x;
+        }
+        words = __ballot_sync(0xffffffffu, words != 0);
+        asm volatile("" ::"r"(words) : "memory");
+        if (lane == 0 && i + kFewStages < turns) fetch(i + kFewStages);
+        use(kv, k0 + i * WK * kFewKeys);
     }
+    __syncthreads();                               // (the rings are done with)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         l[h] = quad_sum(l[h]);
@@ -518,7 +553,7 @@ template <typename T, int DK> __global__ void __launch_bounds__(256) attend_few_
         }
     }
     __syncthreads();
-    join_warps<T, DK, kRows, WK, 256>(a, q, k, hk, end, first_bad, join, row0, rows);
+    join_warps<T, DK, kRows, WK, 32 * WK>(a, q, k, hk, end, first_bad, join, row0, rows);
 }
 
 // Joins the states of a row's shares in order; a warp takes a row, a lane four channels.
@@ -533,6 +568,7 @@ template <typename T> __global__ void __launch_bounds__(128) attend_join_kernel(
     const int last = min(rows, row0 + ROWS) - 1, k_all = visible_keys(a.causal, last / group, q.count, k.count);
     const int live = max(1, (int)((k_all + (long long)a.chunk - 1) / a.chunk));
     const long long all = (long long)a.batch * a.N * a.heads * shares;
+    pdl_wait_prior();
     for (int r = row0 + warp; r <= last; r += 4) {
         const int token = r / group, head = hk * group + r % group;
         const long long at = row_index(a, q, token, head) * shares;
@@ -566,8 +602,7 @@ template <typename T> __global__ void __launch_bounds__(128) attend_join_kernel(
 }
 
 template <typename T> cudaError_t run_join(const AttendArgs& a, int shares, long long slots, cudaStream_t st) {
-    attend_join_kernel<T><<<dim3((unsigned)slots, a.kv_heads), 128, 0, st>>>(a, shares);
-    return cudaGetLastError();
+    return launch_dependent(attend_join_kernel<T>, dim3((unsigned)slots, a.kv_heads), 128, 0, st, a, shares);
 }
 template <typename T, int DK, int WR, int WK> cudaError_t run_rows(const AttendArgs& a, int shares, cudaStream_t st) {
     using G = RowsGeom<T, DK, WR, WK>;
@@ -579,11 +614,14 @@ template <typename T, int DK, int WR, int WK> cudaError_t run_rows(const AttendA
     return shares > 1 ? run_join<T>(a, shares, slots, st) : cudaSuccess;
 }
 template <typename T, int DK> cudaError_t run_few(const AttendArgs& a, int shares, cudaStream_t st) {
-    constexpr int kSmem = 8 * 16 * (DK + 4) * 4;
+    constexpr int kRing = kFewWarps * kFewStages * kFewKeys * 4 * DK, kJoin = kFewWarps * 16 * (DK + 4) * 4, kSmem = (kRing > kJoin ? kRing : kJoin) + 1024;
+    FewArgs f;
+    f.a = a;
+    if (!make_row_map(&f.k, a.k, a.lk, a.batch, a.kv_heads, a.M, a.d, kFewKeys) || !make_row_map(&f.v, a.v, a.lv, a.batch, a.kv_heads, a.M, a.d, kFewKeys)) return cudaErrorInvalidValue;
     static std::atomic<unsigned long long> done{0};
     if (cudaError_t e = allow_smem(attend_few_kernel<T, DK>, done, kSmem)) return e;
     const long long slots = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, 16);
-    attend_few_kernel<T, DK><<<dim3((unsigned)slots, a.kv_heads, shares), 256, kSmem, st>>>(a);
+    attend_few_kernel<T, DK><<<dim3((unsigned)slots, a.kv_heads, shares), 32 * kFewWarps, kSmem, st>>>(f);
     if (cudaError_t e = cudaGetLastError()) return e;
     return shares > 1 ? run_join<T>(a, shares, slots, st) : cudaSuccess;
 }
@@ -594,11 +632,13 @@ bool few_rows(const AttendArgs& a) {
     return rows <= 16 * sequences;
 }
 // Shares of the keys where blocks are too few to fill the GPU
-int shares_of(const AttendArgs& a, int sm_count, int* chunk) {
+int shares_of(const AttendArgs& a, bool few_16, int sm_count, int* chunk) {
     *chunk = std::max(1, a.M);
     if (!few_rows(a)) return 1;
     const long long blocks = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, 16) * a.kv_heads;
-    const long long want = std::max(1LL, 6LL * sm_count / blocks);
+    // One wave of blocks (two an SM; up to 64 channels of 16 bits, three): a block's start and end cost as much as some 1000 keys.  16 caches of up to 16384 keys, 4 heads
+    // of keys of 128: 2 an SM 79 us, 4 86, 6 92, 12 97; 8 heads of 64 over 8192: 2 an SM 51, 3 45, 4 48, 8 51; one cache of 65536, 8 heads of 128: 47, 50, 61, 73.
+    const long long want = std::max(1LL, (a.d <= 64 && few_16 ? 3LL : 2LL) * sm_count / blocks);
     long long c = (a.M + want - 1) / want;
     c = std::max(256LL, (c + 127) / 128 * 128);
     *chunk = (int)std::min<long long>(c, a.M);
@@ -794,7 +834,7 @@ template <typename T> cudaError_t run_dot(const AttendArgs& a, cudaStream_t st) 
 
 size_t attend_workspace(int dtype, const AttendArgs& a, int sm_count) {
     int chunk;
-    const int shares = shares_of(a, sm_count, &chunk);
+    const int shares = shares_of(a, dtype != 0, sm_count, &chunk);
     return shares > 1 ? (size_t)a.batch * a.N * a.heads * shares * (a.d + 2) * sizeof(float) + 16 : 0;
 }
 size_t attend_backward_workspace(int dtype, const AttendArgs& a, int sm_count) {
@@ -802,7 +842,7 @@ size_t attend_backward_workspace(int dtype, const AttendArgs& a, int sm_count) {
 }
 
 cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st, int* launches) {
-    const int shares = shares_of(a, sm_count, &a.chunk);
+    const int shares = shares_of(a, dtype != 0, sm_count, &a.chunk);
     *launches = shares > 1 ? 2 : 1;
     if (dtype != 0 && !few_rows(a)) return launch_attend_umma(dtype, a, st);
     if (dtype == 1) return a.d <= 64 ? run_few<__nv_bfloat16, 64>(a, shares, st) : run_few<__nv_bfloat16, 128>(a, shares, st);

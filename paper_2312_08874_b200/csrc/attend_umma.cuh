@@ -6,7 +6,7 @@
 
 namespace aa {
 
-// Map of a [batch][heads][rows][d] tensor of 16-bit elements with any strides: boxes of 64 channels x 128 rows of one head, 128-byte swizzle; channels past
+// Map of a [batch][heads][rows][d] tensor of 16-bit elements with any strides: boxes of 64 channels x `box_rows` rows of one head, 128-byte swizzle; channels past
 // d and rows past the tensor read zero.  Dimensions 1 to 3 are rows (0), head (1) and batch (2) in the order of their strides.
 struct RowMap {
     alignas(64) CUtensorMap map;
@@ -16,7 +16,7 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const RowMap& m, int cha
     auto at = [&](int i) { return m.order[i] == 0 ? row : m.order[i] == 1 ? head : batch; };
     tma_load_4d(dst, &m.map, channel, at(0), at(1), at(2), bar);
 }
-inline bool make_row_map(RowMap* out, const void* base, const TokLayout& l, int batch, int heads, int rows, int d) {
+inline bool make_row_map(RowMap* out, const void* base, const TokLayout& l, int batch, int heads, int rows, int d, int box_rows = 128) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
     const cuuint64_t n[3] = {(cuuint64_t)rows, (cuuint64_t)heads, (cuuint64_t)batch};
@@ -33,7 +33,7 @@ inline bool make_row_map(RowMap* out, const void* base, const TokLayout& l, int 
         strides[i] = n[o[i]] > 1 ? s[o[i]] : last;
         if (strides[i] % 16 || strides[i] >= (1ull << 40)) return false;
         last = strides[i];
-        if (o[i] == 0) box[i + 1] = 128;
+        if (o[i] == 0) box[i + 1] = (cuuint32_t)box_rows;
         out->order[i] = o[i];
     }
     return fn(&out->map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
