@@ -297,6 +297,7 @@ class AgentAttention:
         self._staging: Optional[torch.Tensor] = None
         self._bytes: dict = {}             # scratch sizes by call shape: they depend on nothing else
         self._rotate_bytes: Optional[int] = None
+        self._calls: dict = {}             # checked calls of `attend` by shapes and strides
         self._strides: dict = {}           # strides as the library takes them, by token count and strides
 
     def close(self):
@@ -793,6 +794,7 @@ class AgentAttention:
             raise ValueError(f"{name}: expected a contiguous {self.device} int32 tensor of {'offsets' if count is None else count}, got {tuple(t.shape)} {t.dtype} on {t.device}")
 
     def _sequences(self, q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths) -> AgentAttnSequences:
+        """Checks a call's tensors; its struct without the pointers."""
         if q.dim() != 4 or k.dim() != 4:
             raise ValueError(f"expected views [B, heads, N, d], got {tuple(q.shape)} and {tuple(k.shape)}")
         B, h, d = self.batch, self.heads, self.head_dim
@@ -811,10 +813,30 @@ class AgentAttention:
         self._numbers(k_offsets, None if q_offsets is None else q_offsets.shape[0], "k_offsets")
         self._numbers(q_lengths, B, "q_lengths")
         self._numbers(k_lengths, B, "k_lengths")
-        s = AgentAttnSequences(_ptr(q), _ptr(k), _ptr(v), self._view(q, (B, h, N, d), "q"), self._view(k, (B, kv, M, d), "k"), self._view(v, (B, kv, M, d), "v"),
-                               N, M, kv, int(bool(causal)), 0.0 if scale is None else scale, 0 if q_offsets is None else min(q_offsets.shape[0] - 1, _INT_MAX),
-                               _ptr(q_offsets), _ptr(k_offsets), _ptr(q_lengths), _ptr(k_lengths))
-        return s
+        return AgentAttnSequences(0, 0, 0, self._view(q, (B, h, N, d), "q"), self._view(k, (B, kv, M, d), "k"), self._view(v, (B, kv, M, d), "v"),
+                                  N, M, kv, int(bool(causal)), 0.0 if scale is None else scale, 0 if q_offsets is None else min(q_offsets.shape[0] - 1, _INT_MAX),
+                                  0, 0, 0, 0)
+
+    def _call(self, q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths):
+        """A struct of this call, and what is kept for calls of these shapes and strides: workspace sizes, strides of new results.
+
+        (The checks and the struct take 8 us of host time, a kernel of a small call 4; nothing here depends on an address.)
+        """
+        numbers = (q_offsets, k_offsets, q_lengths, k_lengths)
+        key = (q.shape, q.stride(), q.dtype, q.get_device(), k.shape, k.stride(), k.dtype, k.get_device(), v.shape, v.stride(), v.dtype, v.get_device(), causal, scale)
+        if q_offsets is not None or k_offsets is not None or q_lengths is not None or k_lengths is not None:
+            key += tuple(None if t is None else (t.shape, t.stride(), t.dtype, t.get_device()) for t in numbers)
+        kept = self._calls.get(key)
+        if kept is None:
+            s = self._sequences(q, k, v, causal, scale, *numbers)
+            if len(self._calls) >= 64:
+                self._calls.clear()
+            kept = self._calls[key] = {"struct": bytes(s)}
+        s = AgentAttnSequences.from_buffer_copy(kept["struct"])          # (a call's own: calls of several threads may run at once)
+        s.q, s.k, s.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
+        if len(key) > 14:
+            s.q_offsets, s.k_offsets, s.q_lengths, s.k_lengths = _ptr(q_offsets), _ptr(q_offsets if k_offsets is None else k_offsets), _ptr(q_lengths), _ptr(k_lengths)
+        return s, kept
 
     def _new_view(self, t: torch.Tensor, partial: bool, stream) -> torch.Tensor:
         """A new tensor with t's shape, token-major where t is; zeros where its rows need not all belong to a sequence."""
@@ -825,17 +847,24 @@ class AgentAttention:
         new.record_stream(torch.cuda.current_stream(self.device))
         return new
 
-    def _attend_workspace(self, s: AgentAttnSequences, backward: int, workspace, stream):
+    def _attend_workspace(self, s: AgentAttnSequences, kept: dict, backward: int, workspace, stream):
         if workspace is not None:
             self._chk_workspace(workspace)
             return workspace
-        key = ("attend", s.queries, s.keys, s.kv_heads, s.sequences, backward)
-        need = self._bytes.get(key)
+        need = kept.get(backward)
         if need is None:
-            if len(self._bytes) >= 64:
-                self._bytes.clear()
-            need = self._bytes[key] = int(self.lib.agent_attn_attend_workspace_bytes(self._h, ctypes.byref(s), backward))
+            need = kept[backward] = int(self.lib.agent_attn_attend_workspace_bytes(self._h, ctypes.byref(s), backward))
         return self._scratch(need, stream)
+
+    def _kept_strides(self, t: torch.Tensor, like: torch.Tensor, name: str, kept: dict):
+        """Strides of a given or new tensor as the library takes them."""
+        key = (name, t.shape, t.stride(), t.dtype, t.get_device())
+        got = kept.get(key)
+        if got is None:
+            got = (ctypes.c_longlong * 3)(*self._view(t, like.shape, name))
+            if len(kept) < 64:
+                kept[key] = got
+        return got
 
     def attend(self, q, k, v, causal: bool = False, scale: Optional[float] = None, q_offsets=None, k_offsets=None, q_lengths=None, k_lengths=None,
                need_lse: bool = False, out=None, workspace=None, stream=None):
@@ -850,16 +879,15 @@ class AgentAttention:
         Returns the result, [B, heads, N, d] (token-major where q is), with `need_lse` also the log-sum-exp of the logits, fp32 [B, heads, N], which
         `attend_backward` takes.  Rows of no sequence are zero in a new result and left as they are in `out`.
         """
-        s = self._sequences(q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths)
-        partial = q_offsets is not None or q_lengths is not None
+        s, kept = self._call(q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths)
         if out is None:
-            out = self._new_view(q, partial, stream)
-        sout = (ctypes.c_longlong * 3)(*self._view(out, q.shape, "out"))
+            out = self._new_view(q, q_offsets is not None or q_lengths is not None, stream)
+        sout = self._kept_strides(out, q, "out", kept)
         lse = None
         if need_lse:
             lse = _empty(q.shape[:3], torch.float32, self.device, stream) if stream is not None else q.new_empty(q.shape[:3], dtype=torch.float32)
-        ws = self._attend_workspace(s, 0, workspace, stream)
-        self._check(self.lib.agent_attn_attend(self._h, ctypes.byref(s), _ptr(out), sout, _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+        ws = self._attend_workspace(s, kept, 0, workspace, stream)
+        self._check(self.lib.agent_attn_attend(self._h, ctypes.byref(s), out.data_ptr(), sout, _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
                                                _stream_ptr(stream)))
         return (out, lse) if need_lse else out
 
@@ -870,29 +898,33 @@ class AgentAttention:
         `out` and `lse` are the forward call's results, the other arguments its own.  Returns a dict with `dq`, `dk`, `dv`, laid out as q, k and v are, or
         the three views `grads`; rows of no sequence are zero in new tensors and left as they are in given ones.
         """
-        s = self._sequences(q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths)
-        sout = (ctypes.c_longlong * 3)(*self._view(out, q.shape, "out"))
-        sdo = (ctypes.c_longlong * 3)(*self._view(d_out, q.shape, "d_out"))
+        s, kept = self._call(q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths)
+        sout, sdo = self._kept_strides(out, q, "out", kept), self._kept_strides(d_out, q, "d_out", kept)
         if lse.shape != q.shape[:3] or lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.get_device() != self._index:
             raise ValueError(f"lse: expected a contiguous {self.device} float32 tensor of shape {tuple(q.shape[:3])}, got {tuple(lse.shape)} {lse.dtype} on {lse.device}")
         if grads is None:
             packed = q_offsets is not None
             grads = tuple(self._new_view(t, packed or n is not None, stream) for t, n in ((q, q_lengths), (k, k_lengths), (v, k_lengths)))
-        g = AgentAttnAttendGrads(*(_ptr(t) for t in grads), *(self._view(t, like.shape, name) for t, like, name in zip(grads, (q, k, v), ("dq", "dk", "dv"))))
-        ws = self._attend_workspace(s, 1, workspace, stream)
+        dq, dk, dv = grads
+        g = AgentAttnAttendGrads(dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), self._kept_strides(dq, q, "dq", kept), self._kept_strides(dk, k, "dk", kept),
+                                 self._kept_strides(dv, v, "dv", kept))
+        ws = self._attend_workspace(s, kept, 1, workspace, stream)
         self._check(self.lib.agent_attn_attend_backward(self._h, ctypes.byref(s), _ptr(out), sout, _ptr(lse), _ptr(d_out), sdo, ctypes.byref(g), _ptr(ws),
                                                         0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream)))
-        return dict(zip(("dq", "dk", "dv"), grads))
+        return {"dq": dq, "dk": dk, "dv": dv}
 
     # ------------------------------------------------------------------ layer norm
     def _layer_norm(self, x, weight, bias, eps) -> AgentAttnLayerNorm:
-        if x.dim() == 0:
+        shape = x.shape
+        if len(shape) == 0:
             raise ValueError("x: expected [..., channels]")
-        C = x.shape[-1]
-        self._chk_tensor(x, x.shape, "x")
-        self._chk_tensor(weight, (C,), "weight")
-        self._chk_tensor(bias, (C,), "bias")
-        return AgentAttnLayerNorm(_ptr(x), _ptr(weight), _ptr(bias), x.numel() // C if C else 0, min(C, _INT_MAX), eps)
+        C = shape[-1]
+        self._chk_tensor(x, shape, "x")
+        if weight is not None:
+            self._chk_tensor(weight, (C,), "weight")
+        if bias is not None:
+            self._chk_tensor(bias, (C,), "bias")
+        return AgentAttnLayerNorm(x.data_ptr(), _ptr(weight), _ptr(bias), x.numel() // C if C else 0, min(C, _INT_MAX), eps)
 
     def layer_norm(self, x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=None) -> torch.Tensor:
         """`agent_attn_layer_norm`: (x - mean) / sqrt(var + eps) * weight + bias over the last dimension of x.  `out` may be x itself."""

@@ -78,6 +78,7 @@ def test_sequences_as_the_library_takes_them():
     at = OnDevice((9,), torch.int32)
     s = h._sequences(q, k, v, False, 0.5, at, None, None, None)
     assert s.sequences == 8 and s.scale == 0.5
+    assert not (s.q or s.q_offsets)                                  # (pointers are a call's own)
     one = OnDevice((1, 4, 1, 64), strides=(999, 128, 7, 1))          # strides of single entries are never used
     assert list(h._sequences(one, k, v, False, None, None, None, None, None).q_strides) == [64, 128, 64]
 
