@@ -18,33 +18,38 @@ namespace aa {
 
 namespace {
 
-template <typename T> struct Oper { using E = T; static constexpr int kTerms = 1; };
-template <> struct Oper<float> { using E = __nv_bfloat16; static constexpr int kTerms = 3; };
-
-// `count` rows of DK channels (d of them exist, the others are zero) -> planes of terms at `dst`, by THREADS threads; row(i): address or null (zeros)
-template <typename T, int DK, int THREADS, typename F> __device__ __forceinline__ void load_tile(int me, unsigned char* dst, uint32_t plane, int count, int d, const void* some, F row) {
-    constexpr int kPitch = TileGeom<DK>::kPitch, kGroups = DK / 8;
-    for (int i = me; i < count * kGroups; i += THREADS) {
-        const int r = i / kGroups, c = i % kGroups * 8;
-        const T* src = row(r);
-        unsigned char* to = dst + r * kPitch + c * 2;
-        if constexpr (sizeof(T) == 2) {
-            cp_async16(to, src && c < d ? src + c : some, src && c < d ? 16 : 0);      // (d is a multiple of 8; of no bytes nothing is read)
-        } else {
-            float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-            if (src && c < d) a = __ldg(reinterpret_cast<const float4*>(src + c));
-            if (src && c + 4 < d) b = __ldg(reinterpret_cast<const float4*>(src + c + 4));
-            const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+// `COUNT` rows of DK fp32 channels (d of them exist, the others are zero) -> three planes of bf16 terms at `dst`, by THREADS threads; row(i): address or null
+// (zeros).  Loads in batches of four: one at a time, their latencies were most of a small call (196 tokens, 3 heads of 64: 16.4 -> x us).
+template <int DK, int THREADS, int COUNT, typename F> __device__ __forceinline__ void load_tile(int me, unsigned char* dst, uint32_t plane, int d, F row) {
+    constexpr int kPitch = TileGeom<DK>::kPitch, kGroups = DK / 8, kItems = COUNT * kGroups, kBatch = 4;
+#pragma unroll 1
+    for (int base = me; base < kItems; base += kBatch * THREADS) {
+        float4 f[kBatch][2];
+#pragma unroll
+        for (int n = 0; n < kBatch; ++n) {
+            const int i = base + n * THREADS, c = i % kGroups * 8;
+            const float* src = i < kItems ? row(i / kGroups) : nullptr;
+            f[n][0] = f[n][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (src && c < d) f[n][0] = __ldg(reinterpret_cast<const float4*>(src + c));
+            if (src && c + 4 < d) f[n][1] = __ldg(reinterpret_cast<const float4*>(src + c + 4));
+        }
+#pragma unroll
+        for (int n = 0; n < kBatch; ++n) {
+            const int i = base + n * THREADS;
+            if (i >= kItems) continue;
+            const float4 a = f[n][0], b = f[n][1];
+            const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
             uint32_t w[3][4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 uint32_t t[3];
-                split_pair<__nv_bfloat16, 3>(f[2 * k], f[2 * k + 1], t);
+                split_pair<__nv_bfloat16, 3>(x[2 * k], x[2 * k + 1], t);
 #pragma unroll
-                for (int n = 0; n < 3; ++n) w[n][k] = t[n];
+                for (int m = 0; m < 3; ++m) w[m][k] = t[m];
             }
+            unsigned char* to = dst + i / kGroups * kPitch + i % kGroups * 16;
 #pragma unroll
-            for (int n = 0; n < 3; ++n) *reinterpret_cast<uint4*>(to + n * plane) = make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
+            for (int m = 0; m < 3; ++m) *reinterpret_cast<uint4*>(to + m * plane) = make_uint4(w[m][0], w[m][1], w[m][2], w[m][3]);
         }
     }
 }
@@ -141,13 +146,12 @@ template <typename E, int NT, int DK, int THREADS> __device__ void clean_values(
 }
 
 // ------------------------------------------------------------------------------------------------ forward
-template <typename T, int DK, int WR, int WK> struct RowsGeom {
-    static constexpr int NT = Oper<T>::kTerms, kRows = 16 * WR, kStep = 32 * WK, kThreads = 32 * WR * WK, kPitch = TileGeom<DK>::kPitch;
-    static constexpr int kStages = NT > 1 ? 1 : 3;
-    static constexpr uint32_t kQPlane = kRows * kPitch, kPlane = kStep * kPitch, kStage = 2 * NT * kPlane;
+template <int DK, int WR, int WK> struct RowsGeom {
+    static constexpr int NT = 3, kRows = 16 * WR, kStep = 32 * WK, kThreads = 32 * WR * WK, kPitch = TileGeom<DK>::kPitch;
+    static constexpr uint32_t kQPlane = kRows * kPitch, kPlane = kStep * kPitch;
+    static constexpr int kStage = 2 * NT * (int)kPlane;
     static constexpr int kJoin = WK > 1 ? WK * kRows * (DK + 4) * 4 : 0;                  // states of the warps that share rows
-    static constexpr int kRing = kStages * (int)kStage > kJoin ? kStages * (int)kStage : kJoin;
-    static constexpr int kSmem = NT * (int)kQPlane + kRing + DK * 4;
+    static constexpr int kRing = kStage > kJoin ? kStage : kJoin, kSmem = NT * (int)kQPlane + kRing + DK * 4;
 };
 
 // Partial state of a row and share: [row of the tensor][share]: maximum (log2 units) and sum; results behind them
@@ -195,10 +199,11 @@ __device__ __forceinline__ void join_warps(const AttendArgs& a, const Span& q, c
     }
 }
 
-template <typename T, int DK, int WR, int WK>
+template <int DK, int WR, int WK>
 __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
-    using G = RowsGeom<T, DK, WR, WK>;
-    using E = typename Oper<T>::E;
+    using T = float;
+    using E = __nv_bfloat16;
+    using G = RowsGeom<DK, WR, WK>;
     constexpr int NT = G::NT, P = G::kPitch;
     extern __shared__ __align__(128) unsigned char smem[];
     unsigned char* ring = smem + NT * G::kQPlane;
@@ -219,33 +224,20 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
 
     const T* kp = static_cast<const T*>(a.k) + k.batch * a.lk.sb + hk * a.lk.sh + (long long)k.first * a.lk.st;
     const T* vp = static_cast<const T*>(a.v) + k.batch * a.lv.sb + hk * a.lv.sh + (long long)k.first * a.lv.st;
-    load_tile<T, DK, G::kThreads>(tid, smem, G::kQPlane, G::kRows, a.d, a.q, [&](int r) -> const T* {
+    load_tile<DK, G::kThreads, G::kRows>(tid, smem, G::kQPlane, a.d, [&](int r) -> const T* {
         const int i = row0 + r;
         return i < rows ? static_cast<const T*>(a.q) + q.batch * a.lq.sb + (hk * group + i % group) * a.lq.sh + (long long)(q.first + i / group) * a.lq.st : nullptr;
     });
-    if (G::kStages > 1) cp_async_commit();
     for (int c = tid; c < DK; c += G::kThreads) first_bad[c] = INT_MAX;
     const int steps = (end - begin + G::kStep - 1) / G::kStep;
     // warps that share their keys fetch them together; one that has its own (WK > 1) waits for no other
     constexpr int LOADERS = WK > 1 ? 32 : G::kThreads, OWN = WK > 1 ? 32 : G::kStep;
     const int me = WK > 1 ? lane : tid;
+    unsigned char* mine = ring + (WK > 1 ? wk * 32 * P : 0);
     auto meet = [&] {
         if (WK > 1) __syncwarp();
         else __syncthreads();
     };
-    auto fetch = [&](int s) {
-        unsigned char* to = ring + (s % G::kStages) * G::kStage + (WK > 1 ? wk * 32 * P : 0);
-        const int k0 = begin + s * G::kStep + (WK > 1 ? wk * 32 : 0);
-        load_tile<T, DK, LOADERS>(me, to, G::kPlane, OWN, a.d, a.q, [&](int r) -> const T* { return k0 + r < end ? kp + (long long)(k0 + r) * a.lk.st : nullptr; });
-        load_tile<T, DK, LOADERS>(me, to + NT * G::kPlane, G::kPlane, OWN, a.d, a.q, [&](int r) -> const T* { return k0 + r < end ? vp + (long long)(k0 + r) * a.lv.st : nullptr; });
-    };
-    if (G::kStages > 1) {
-#pragma unroll
-        for (int s = 0; s < G::kStages - 1; ++s) {
-            if (s < steps) fetch(s);
-            cp_async_commit();
-        }
-    }
 
     int limit[2], row[2];
 #pragma unroll
@@ -259,32 +251,21 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
     for (int c = 0; c < DK / 8; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[c][e] = 0.f;
-    if (WK > 1 || G::kStages == 1) {               // (the queries, and first_bad)
-        if (G::kStages > 1) cp_async_wait<G::kStages - 1>();
-        __syncthreads();
-    }
+    __syncthreads();                               // (the queries, and first_bad)
     const uint32_t qa = smem_u32(smem) + wr * 16 * P + val_lane_offset<DK>(lane);
 
     for (int s = 0; s < steps; ++s) {
-        if (G::kStages > 1) {
-            cp_async_wait<(G::kStages > 1 ? G::kStages - 2 : 0)>();
-            meet();
-            if (s + G::kStages - 1 < steps) fetch(s + G::kStages - 1);
-            cp_async_commit();
-        } else {
-            if (s) meet();
-            fetch(s);
-            meet();
-        }
-        unsigned char* stage = ring + (s % G::kStages) * G::kStage;
-        const int block0 = begin + s * G::kStep;
-        const int k0 = block0 + wk * 32;
-        if (k0 >= end) continue;                   // (of a warp with its own keys: nothing is left to do but the barriers behind the loop)
+        const int k0 = begin + s * G::kStep + (WK > 1 ? wk * 32 : 0);
+        if (k0 >= end) break;                      // (of a warp with its own keys)
+        if (s) meet();
+        load_tile<DK, LOADERS, OWN>(me, mine, G::kPlane, a.d, [&](int r) -> const T* { return k0 + r < end ? kp + (long long)(k0 + r) * a.lk.st : nullptr; });
+        load_tile<DK, LOADERS, OWN>(me, mine + NT * G::kPlane, G::kPlane, a.d, [&](int r) -> const T* { return k0 + r < end ? vp + (long long)(k0 + r) * a.lv.st : nullptr; });
+        meet();
         if (k0 + OWN > k_whole) {
-            clean_values<E, NT, DK, LOADERS>(me, stage + NT * G::kPlane + (WK > 1 ? wk * 32 * P : 0), G::kPlane, min(OWN, end - k0), k0, first_bad);
+            clean_values<E, NT, DK, LOADERS>(me, mine + NT * G::kPlane, G::kPlane, min(OWN, end - k0), k0, first_bad);
             meet();
         }
-        const uint32_t kb = smem_u32(stage) + wk * 32 * P;
+        const uint32_t kb = smem_u32(mine);
         float x[4][4];
         block_logits<E, NT, DK>(x, qa, G::kQPlane, kb + key_lane_offset<DK>(lane), G::kPlane);
         if (k0 + 32 > min(limit[0], limit[1])) {
@@ -556,62 +537,70 @@ template <typename T, int DK> __global__ void __launch_bounds__(32 * kFewWarps) 
     join_warps<T, DK, kRows, WK, 32 * WK>(a, q, k, hk, end, first_bad, join, row0, rows);
 }
 
-// Joins the states of a row's shares in order; a warp takes a row, a lane four channels.
+// Joins the states of a row's shares: a block a row, its four warps take every fourth share, a lane four channels; the order is fixed.
 template <typename T> __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a, int shares) {
-    constexpr int ROWS = 16;                       // (shares are of few rows)
+    __shared__ float4 part[4][32];
+    __shared__ float sums[4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = a.heads / a.kv_heads, hk = blockIdx.y;
-    int seq, tile;
-    if (!find_slot(a.q_offsets, a.sequences, a.N, group, ROWS, blockIdx.x, &seq, &tile)) return;
+    int seq, r;
+    const bool found = find_slot(a.q_offsets, a.sequences, a.N, group, 1, blockIdx.x, &seq, &r);
     const Span q = span_of(a.q_offsets, a.q_lengths, a.N, seq), k = span_of(a.k_offsets, a.k_lengths, a.M, seq);
-    const int rows = q.count * group, row0 = tile * ROWS;
-    if (row0 >= rows) return;
-    const int last = min(rows, row0 + ROWS) - 1, k_all = visible_keys(a.causal, last / group, q.count, k.count);
+    if (!found || r >= q.count * group) return;
+    // (shares that a row's tile of 16 has: some may hold no key of this row, with a sum of zero)
+    const int last = min(q.count * group, r / 16 * 16 + 16) - 1, k_all = visible_keys(a.causal, last / group, q.count, k.count);
     const int live = max(1, (int)((k_all + (long long)a.chunk - 1) / a.chunk));
-    const long long all = (long long)a.batch * a.N * a.heads * shares;
+    const int token = r / group, head = hk * group + r % group;
+    const long long all = (long long)a.batch * a.N * a.heads * shares, at = row_index(a, q, token, head) * shares;
+    const float2* state = reinterpret_cast<const float2*>(a.ws) + at;
+    const float* acc = a.ws + (2 * all + 3) / 4 * 4 + at * a.d + 4 * lane;
+    const bool mine = 4 * lane < a.d;
     pdl_wait_prior();
-    for (int r = row0 + warp; r <= last; r += 4) {
-        const int token = r / group, head = hk * group + r % group;
-        const long long at = row_index(a, q, token, head) * shares;
-        const float2* state = reinterpret_cast<const float2*>(a.ws) + at;
-        float top = -INFINITY;
-        for (int s = lane; s < live; s += 32) top = fmaxf(top, state[s].x);
+    float top = -INFINITY;
+    for (int s = lane; s < live; s += 32) top = fmaxf(top, state[s].x);
 #pragma unroll
-        for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
-        const float b = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        const float* acc = a.ws + (2 * all + 3) / 4 * 4 + at * a.d + 4 * lane;
-        const bool mine = 4 * lane < a.d;
-#pragma unroll 4
-        for (int s = 0; s < live; ++s) {
-            const float2 st = state[s];
-            const float f = fast_exp2(st.x - b);
-            const float4 w = mine ? *reinterpret_cast<const float4*>(acc + (long long)s * a.d) : v;
-            sum = fmaf(f, st.y, sum);
-            v.x = fmaf(f, w.x, v.x); v.y = fmaf(f, w.y, v.y); v.z = fmaf(f, w.z, v.z); v.w = fmaf(f, w.w, v.w);
-        }
-        const bool some = visible_keys(a.causal, token, q.count, k.count) > 0;
-        const float inv = some ? 1.f / sum : 0.f;
-        if (mine) {
-            T* to = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + token) * a.lo.st + 4 * lane;
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2<T>(v.x * inv, v.y * inv), pack2<T>(v.z * inv, v.w * inv));
-            else *reinterpret_cast<float4*>(to) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-        }
-        if (lane == 0 && a.lse) a.lse[((long long)q.batch * a.heads + head) * a.N + q.first + token] = some ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
+    const float b = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int s = warp; s < live; s += 4) {
+        const float2 st = state[s];
+        const float f = fast_exp2(st.x - b);
+        const float4 w = mine ? *reinterpret_cast<const float4*>(acc + (long long)s * a.d) : make_float4(0.f, 0.f, 0.f, 0.f);
+        sum = fmaf(f, st.y, sum);
+        v.x = fmaf(f, w.x, v.x); v.y = fmaf(f, w.y, v.y); v.z = fmaf(f, w.z, v.z); v.w = fmaf(f, w.w, v.w);
     }
+    part[warp][lane] = v;
+    if (lane == 0) sums[warp] = sum;
+    __syncthreads();
+    if (warp) return;
+    sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        v.x += part[w][lane].x; v.y += part[w][lane].y; v.z += part[w][lane].z; v.w += part[w][lane].w;
+    }
+    const bool some = visible_keys(a.causal, token, q.count, k.count) > 0;
+    const float inv = some ? 1.f / sum : 0.f;
+    if (mine) {
+        T* to = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + token) * a.lo.st + 4 * lane;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to) = make_uint2(pack2<T>(v.x * inv, v.y * inv), pack2<T>(v.z * inv, v.w * inv));
+        else *reinterpret_cast<float4*>(to) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+    }
+    if (lane == 0 && a.lse) a.lse[((long long)q.batch * a.heads + head) * a.N + q.first + token] = some ? (top + log2f(sum)) * kLn2 : -INFINITY;
 }
 
-template <typename T> cudaError_t run_join(const AttendArgs& a, int shares, long long slots, cudaStream_t st) {
+template <typename T> cudaError_t run_join(const AttendArgs& a, int shares, cudaStream_t st) {
+    const long long slots = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, 1);
     return launch_dependent(attend_join_kernel<T>, dim3((unsigned)slots, a.kv_heads), 128, 0, st, a, shares);
 }
-template <typename T, int DK, int WR, int WK> cudaError_t run_rows(const AttendArgs& a, int shares, cudaStream_t st) {
-    using G = RowsGeom<T, DK, WR, WK>;
+template <int DK, int WR, int WK> cudaError_t run_rows(const AttendArgs& a, int shares, cudaStream_t st) {
+    using G = RowsGeom<DK, WR, WK>;
     static std::atomic<unsigned long long> done{0};
-    if (cudaError_t e = allow_smem(attend_rows_kernel<T, DK, WR, WK>, done, G::kSmem)) return e;
+    if (cudaError_t e = allow_smem(attend_rows_kernel<DK, WR, WK>, done, G::kSmem)) return e;
     const long long slots = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, G::kRows);
-    attend_rows_kernel<T, DK, WR, WK><<<dim3((unsigned)slots, a.kv_heads, shares), G::kThreads, G::kSmem, st>>>(a);
+    attend_rows_kernel<DK, WR, WK><<<dim3((unsigned)slots, a.kv_heads, shares), G::kThreads, G::kSmem, st>>>(a);
     if (cudaError_t e = cudaGetLastError()) return e;
-    return shares > 1 ? run_join<T>(a, shares, slots, st) : cudaSuccess;
+    return shares > 1 ? run_join<float>(a, shares, st) : cudaSuccess;
 }
 template <typename T, int DK> cudaError_t run_few(const AttendArgs& a, int shares, cudaStream_t st) {
     constexpr int kRing = kFewWarps * kFewStages * kFewKeys * 4 * DK, kJoin = kFewWarps * 16 * (DK + 4) * 4, kSmem = (kRing > kJoin ? kRing : kJoin) + 1024;
@@ -623,13 +612,13 @@ template <typename T, int DK> cudaError_t run_few(const AttendArgs& a, int share
     const long long slots = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, 16);
     attend_few_kernel<T, DK><<<dim3((unsigned)slots, a.kv_heads, shares), 32 * kFewWarps, kSmem, st>>>(f);
     if (cudaError_t e = cudaGetLastError()) return e;
-    return shares > 1 ? run_join<T>(a, shares, slots, st) : cudaSuccess;
+    return shares > 1 ? run_join<T>(a, shares, st) : cudaSuccess;
 }
 
 // Few rows a sequence: sixteen of them a block, whose four warps take turns at the keys.
 bool few_rows(const AttendArgs& a) {
     const long long rows = (long long)a.N * (a.heads / a.kv_heads), sequences = a.q_offsets ? a.sequences : 1;
-    return rows <= 16 * sequences;
+    return rows <= 16 * sequences && rows < (1LL << 28);
 }
 // Shares of the keys where blocks are too few to fill the GPU
 int shares_of(const AttendArgs& a, bool few_16, int sm_count, int* chunk) {
@@ -645,11 +634,11 @@ int shares_of(const AttendArgs& a, bool few_16, int sm_count, int* chunk) {
     return (a.M + *chunk - 1) / *chunk;
 }
 
-template <typename T, int WR, int WK> cudaError_t rows_of_type(const AttendArgs& a, int shares, cudaStream_t st) {
-    if (a.d <= 32) return run_rows<T, 32, WR, WK>(a, shares, st);
-    if (a.d <= 64) return run_rows<T, 64, WR, WK>(a, shares, st);
-    if (a.d <= 96) return run_rows<T, 96, WR, WK>(a, shares, st);
-    return run_rows<T, 128, WR, WK>(a, shares, st);
+template <int WR, int WK> cudaError_t run_rows_of(const AttendArgs& a, int shares, cudaStream_t st) {
+    if (a.d <= 32) return run_rows<32, WR, WK>(a, shares, st);
+    if (a.d <= 64) return run_rows<64, WR, WK>(a, shares, st);
+    if (a.d <= 96) return run_rows<96, WR, WK>(a, shares, st);
+    return run_rows<128, WR, WK>(a, shares, st);
 }
 
 // ------------------------------------------------------------------------------------------------ backward
@@ -731,8 +720,8 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
     auto stat = [&](int i) {
         return __ldg(reinterpret_cast<const float2*>(a.ws) + ((long long)q.batch * a.heads + hk * group + i % group) * a.N + q.first + i / group);
     };
-    load_tile<T, DK, 128>(tid, xs, G::kRowPlane, G::kRows, a.d, a.q, [&](int r) -> const T* { return row0 + r < rows ? (KEYS ? key(a.k, a.lk, row0 + r) : query(a.q, a.lq, row0 + r)) : nullptr; });
-    load_tile<T, DK, 128>(tid, ys, G::kRowPlane, G::kRows, a.d, a.q, [&](int r) -> const T* { return row0 + r < rows ? (KEYS ? key(a.v, a.lv, row0 + r) : query(a.dout, a.ldo, row0 + r)) : nullptr; });
+    load_tile<DK, 128, G::kRows>(tid, xs, G::kRowPlane, a.d, [&](int r) -> const T* { return row0 + r < rows ? (KEYS ? key(a.k, a.lk, row0 + r) : query(a.q, a.lq, row0 + r)) : nullptr; });
+    load_tile<DK, 128, G::kRows>(tid, ys, G::kRowPlane, a.d, [&](int r) -> const T* { return row0 + r < rows ? (KEYS ? key(a.v, a.lv, row0 + r) : query(a.dout, a.ldo, row0 + r)) : nullptr; });
     // columns that some row of the tile meets
     int begin = 0, end;
     if (KEYS) {
@@ -767,8 +756,8 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
     const uint32_t ut = smem_u32(us) + val_lane_offset<DK>(lane), wt = ut + (uint32_t)(ws - us);
     for (int c0 = begin; c0 < end; c0 += G::kStep) {
         if (c0 != begin) __syncthreads();
-        load_tile<T, DK, 128>(tid, us, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.q, a.lq, c0 + r) : key(a.k, a.lk, c0 + r)) : nullptr; });
-        load_tile<T, DK, 128>(tid, ws, G::kPlane, G::kStep, a.d, a.q, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.dout, a.ldo, c0 + r) : key(a.v, a.lv, c0 + r)) : nullptr; });
+        load_tile<DK, 128, G::kStep>(tid, us, G::kPlane, a.d, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.q, a.lq, c0 + r) : key(a.k, a.lk, c0 + r)) : nullptr; });
+        load_tile<DK, 128, G::kStep>(tid, ws, G::kPlane, a.d, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.dout, a.ldo, c0 + r) : key(a.v, a.lv, c0 + r)) : nullptr; });
         if (KEYS && tid < G::kStep) stats[tid] = c0 + tid < end ? stat(c0 + tid) : make_float2(0.f, 0.f);
         __syncthreads();
         float x[4][4], y[4][4];
@@ -850,7 +839,7 @@ cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st
     // Sixteen rows a block and four warps on the keys, too, where 64 rows would leave half of the SMs idle (196 tokens, 3 heads of 64: 26.6 -> x us); elsewhere
     // every block of keys is split into terms for four times the rows.
     const long long blocks = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, 64) * a.kv_heads;
-    return few_rows(a) || 2 * blocks <= sm_count ? rows_of_type<float, 1, 4>(a, shares, st) : rows_of_type<float, 4, 1>(a, shares, st);
+    return few_rows(a) || 2 * blocks <= sm_count ? run_rows_of<1, 4>(a, shares, st) : run_rows_of<4, 1>(a, shares, st);
 }
 cudaError_t launch_attend_backward(int dtype, const AttendArgs& a, int sm_count, cudaStream_t st, int* launches) {
     *launches = 3;

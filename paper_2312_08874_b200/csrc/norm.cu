@@ -12,15 +12,20 @@
 #include "kernels.h"
 
 #include <algorithm>
+#include <climits>
 
 namespace aa {
 
 namespace {
 
-// V elements of a row <-> fp32
-template <typename T, int V> __device__ __forceinline__ void read_vec(const T* p, float* f) {
-    if constexpr (V == 1) f[0] = Elem<T>::to_f32(__ldg(p));
-    else unpack16<T>(__ldg(reinterpret_cast<const uint4*>(p)), f);
+// V elements of a row as they are in memory, and as fp32
+template <typename T, int V> struct Raw { using R = uint4; };
+template <typename T> struct Raw<T, 1> { using R = T; };
+template <typename T, int V> using RawT = typename Raw<T, V>::R;
+template <typename T, int V> __device__ __forceinline__ RawT<T, V> read_raw(const T* p) { return __ldg(reinterpret_cast<const RawT<T, V>*>(p)); }
+template <typename T, int V> __device__ __forceinline__ void unpack_raw(const RawT<T, V>& r, float* f) {
+    if constexpr (V == 1) f[0] = Elem<T>::to_f32(r);
+    else unpack16<T>(r, f);
 }
 template <typename T, int V> __device__ __forceinline__ void write_vec(T* p, const float* f) {
     if constexpr (V == 1) *p = Elem<T>::from_f32(f[0]);
@@ -53,49 +58,59 @@ template <int TPR, int N> __device__ __forceinline__ void row_sums(float (&s)[N]
 // How a block's threads share rows
 template <int TPR> constexpr int kBlock = TPR > 32 ? TPR : 256;
 
+// Blocks of an SM: what registers leave (a thread holds F values of a row, backward four times that, and the next row as it is in memory)
+template <int TPR, int F, bool BACK> constexpr int kPerSm = TPR == 512 ? (F <= 8 ? 2 : 1) : (F <= 8 ? (BACK ? 4 : 6) : F <= 16 ? (BACK ? 2 : 4) : BACK ? 1 : 2) * (TPR == 128 ? 2 : 1);
 template <typename T, int TPR, int NV, int V, bool BACK>
-__global__ void __launch_bounds__(kBlock<TPR>, TPR == 512 ? 1 : BACK ? 2 : TPR > 32 ? 4 : 3) norm_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(kBlock<TPR>, kPerSm<TPR, NV * V, BACK>) norm_kernel(const __grid_constant__ NormArgs a) {
     constexpr int THREADS = kBlock<TPR>, RPB = THREADS / TPR, F = NV * V;
     extern __shared__ float sums[];                        // backward: [2][C]
     __shared__ float part[TPR > 32 ? 4 * (TPR / 32) : 1];
     const int tid = threadIdx.x, lane = tid % TPR, C = a.C;
     const float inv = 1.f / (float)C;
     int turn = 0;
-    float w[F], b[BACK ? 1 : F], dw[BACK ? F : 1], db[BACK ? F : 1];
+    float dw[BACK ? F : 1], db[BACK ? F : 1];
+    RawT<T, V> w[NV], b[BACK ? 1 : NV], x[NV], dy[BACK ? NV : 1];
+    auto fetch = [&](long long r) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * TPR + lane) * V;
+            if (r < a.rows && c < C) {
+                x[v] = read_raw<T, V>(static_cast<const T*>(a.x) + r * C + c);
+                if constexpr (BACK) dy[v] = read_raw<T, V>(static_cast<const T*>(a.dy) + r * C + c);
+            }
+        }
+    };
+    if (BACK) pdl_release_next();
+    const long long stride = (long long)gridDim.x * RPB;
+    fetch((long long)blockIdx.x * RPB + tid / TPR);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int c = (v * TPR + lane) * V;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            w[v * V + e] = 1.f;
-            if (!BACK) b[v * V + e] = 0.f;
-        }
-        if (c < C && a.w) read_vec<T, V>(static_cast<const T*>(a.w) + c, w + v * V);
-        if (!BACK && c < C && a.b) read_vec<T, V>(static_cast<const T*>(a.b) + c, b + v * V);
+        if (c < C && a.w) w[v] = read_raw<T, V>(static_cast<const T*>(a.w) + c);
+        if constexpr (!BACK)
+            if (c < C && a.b) b[v] = read_raw<T, V>(static_cast<const T*>(a.b) + c);
     }
     if (BACK)
 #pragma unroll
         for (int i = 0; i < F; ++i) dw[i] = db[i] = 0.f;
     // (every thread of a block takes the same number of turns: shuffles and barriers are met by all)
-    for (long long r0 = (long long)blockIdx.x * RPB; r0 < a.rows; r0 += (long long)gridDim.x * RPB) {
+    for (long long r0 = (long long)blockIdx.x * RPB; r0 < a.rows; r0 += stride) {
         const long long r = r0 + tid / TPR;
         const bool live = r < a.rows;
-        const T* x = static_cast<const T*>(a.x) + r * C;
         float f[F], g[BACK ? F : 1];
         float s[1] = {0.f};
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c = (v * TPR + lane) * V;
+            const bool in = live && (v * TPR + lane) * V < C;
+            unpack_raw<T, V>(x[v], f + v * V);
+            if constexpr (BACK) unpack_raw<T, V>(dy[v], g + v * V);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                f[v * V + e] = 0.f;
-                if (BACK) g[v * V + e] = 0.f;
-            }
-            if (live && c < C) {
-                read_vec<T, V>(x + c, f + v * V);
-                if constexpr (BACK) read_vec<T, V>(static_cast<const T*>(a.dy) + r * C + c, g + v * V);
+                if (!in) f[v * V + e] = 0.f;
+                if (BACK && !in) g[v * V + e] = 0.f;
             }
         }
+        fetch(r + stride);
 #pragma unroll
         for (int i = 0; i < F; ++i) s[0] += f[i];
         row_sums<TPR, 1>(s, part, turn);
@@ -117,13 +132,17 @@ __global__ void __launch_bounds__(kBlock<TPR>, TPR == 512 ? 1 : BACK ? 2 : TPR >
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int c = (v * TPR + lane) * V;
-                float y[V];
+                float y[V], gain[V], shift[V];
+                unpack_raw<T, V>(w[v], gain);
+                unpack_raw<T, V>(b[v], shift);
 #pragma unroll
-                for (int e = 0; e < V; ++e) y[e] = fmaf(f[v * V + e] * rs, w[v * V + e], b[v * V + e]);
+                for (int e = 0; e < V; ++e) y[e] = fmaf(f[v * V + e] * rs, a.w ? gain[e] : 1.f, a.b ? shift[e] : 0.f);
                 if (live && c < C) write_vec<T, V>(static_cast<T*>(a.y) + r * C + c, y);
             }
         } else {
-            float t[2] = {0.f, 0.f};
+            float t[2] = {0.f, 0.f}, gain[F];
+#pragma unroll
+            for (int v = 0; v < NV; ++v) unpack_raw<T, V>(w[v], gain + v * V);
 #pragma unroll
             for (int i = 0; i < F; ++i) {
                 f[i] *= rs;
@@ -131,7 +150,7 @@ __global__ void __launch_bounds__(kBlock<TPR>, TPR == 512 ? 1 : BACK ? 2 : TPR >
                     dw[i] = fmaf(g[i], f[i], dw[i]);
                     db[i] += g[i];
                 }
-                g[i] *= w[i];
+                if (a.w && (i / V * TPR + lane) * V < C) g[i] *= gain[i];
                 t[0] += g[i];
                 t[1] = fmaf(g[i], f[i], t[1]);
             }
@@ -242,8 +261,9 @@ template <typename T> __global__ void __launch_bounds__(256) norm_columns_kernel
     out[(long long)blockIdx.y * 2 * C + C + c] = q;
 }
 // Rows of sums [shares][2][C] -> dw, db: 32 columns a block, every warp a run of shares, joined in order
-__global__ void __launch_bounds__(1024) norm_join_kernel(const float* __restrict__ in, int shares, int C, float* dw, float* db) {
+__global__ void __launch_bounds__(1024) norm_join_kernel(const float* in, int shares, int C, float* dw, float* db) {
     __shared__ float part[32][33];
+    pdl_wait_prior();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
     float s = 0.f;
@@ -279,12 +299,17 @@ NormPlan plan_of(int dtype, int C, bool aligned) {
     if (C % vec == 0 && aligned) {
         const int n = C / vec;
         p.v = vec;
-        // the fewest lanes that hold a row in two vectors each, three where that leaves none idle
-        for (int t : {4, 8, 16}) {
-            if (n <= 2 * t) { p.tpr = t; p.nv = n <= t ? 1 : 2; return p; }
-            if (n == 3 * t) { p.tpr = t; p.nv = 3; return p; }
-        }
-        for (int t : {32, 128, 512})
+        // up to a warp a row: the fewest idle lanes, then the fewest vectors a lane
+        int idle = INT_MAX;
+        for (int v = 1; v <= 4; ++v)
+            for (int t : {4, 8, 16, 32})
+                if (n <= t * v && t * v - n < idle && (v < 4 || t == 32)) {
+                    idle = t * v - n;
+                    p.tpr = t;
+                    p.nv = v;
+                }
+        if (p.tpr) return p;
+        for (int t : {128, 512})
             if (n <= 4 * t) { p.tpr = t; p.nv = (n + t - 1) / t; return p; }
     } else {
         p.v = 1;
@@ -294,11 +319,11 @@ NormPlan plan_of(int dtype, int C, bool aligned) {
     p.tpr = 0;
     return p;
 }
-// Blocks that walk the rows: as many as run at once; with gains' gradients fewer where their rows of sums would cost more than the rows.
+// Blocks that walk the rows: as many as run at once
 long long blocks_of(const NormPlan& p, long long rows, int sm_count, bool back) {
-    const int rpb = p.tpr > 32 ? 1 : 256 / p.tpr;
-    const long long need = (rows + rpb - 1) / rpb, most = (long long)sm_count * (p.tpr == 512 ? 2 : p.tpr == 128 ? 8 : back ? 2 : 8);
-    return std::max(1LL, std::min(need, most));
+    const int rpb = p.tpr > 32 ? 1 : 256 / p.tpr, f = p.nv * p.v;
+    const int per = p.tpr == 512 ? (f <= 8 ? 2 : 1) : (f <= 8 ? (back ? 4 : 6) : f <= 16 ? (back ? 2 : 4) : back ? 1 : 2) * (p.tpr == 128 ? 2 : 1);       // kPerSm
+    return std::max(1LL, std::min((rows + rpb - 1) / rpb, (long long)sm_count * per));
 }
 
 template <typename T, int TPR, int NV, int V, bool BACK> cudaError_t run_norm(const NormArgs& a, const NormPlan& p, int sm_count, cudaStream_t st) {
@@ -354,8 +379,7 @@ cudaError_t launch_norm_backward(int dtype, const NormArgs& a, int sm_count, cud
     *launches = (p.tpr || !b.ws ? 1 : a.dx == a.dy ? 3 : 2) + (b.ws ? 1 : 0);
     if (e != cudaSuccess || !b.ws) return e;
     const int shares = p.tpr ? (int)blocks_of(p, a.rows, sm_count, true) : kColumnShares;
-    norm_join_kernel<<<(2 * a.C + 31) / 32, 1024, 0, st>>>(b.ws, shares, a.C, a.dw, a.db);
-    return cudaGetLastError();
+    return launch_dependent(norm_join_kernel, dim3((2 * a.C + 31) / 32), 1024, 0, st, b.ws, shares, a.C, a.dw, a.db);
 }
 
 }  // namespace aa
