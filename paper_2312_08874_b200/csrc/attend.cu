@@ -842,10 +842,10 @@ cudaError_t launch_attend(int dtype, AttendArgs a, int sm_count, cudaStream_t st
     return few_rows(a) || 2 * blocks <= sm_count ? run_rows_of<1, 4>(a, shares, st) : run_rows_of<4, 1>(a, shares, st);
 }
 cudaError_t launch_attend_backward(int dtype, const AttendArgs& a, int sm_count, cudaStream_t st, int* launches) {
-    *launches = 3;
-    const cudaError_t e = dtype == 0 ? run_dot<float>(a, st) : dtype == 1 ? run_dot<__nv_bfloat16>(a, st) : run_dot<__half>(a, st);
-    if (e != cudaSuccess) return e;
-    if (dtype != 0) return launch_attend_grad_umma(dtype, a, st);
+    *launches = dtype == 1 ? 2 : 3;
+    if (dtype == 1) return launch_attend_grad_umma(dtype, a, st);      // (which makes its statistics itself)
+    if (cudaError_t e = dtype == 0 ? run_dot<float>(a, st) : run_dot<__half>(a, st)) return e;
+    if (dtype == 2) return launch_attend_grad_umma(dtype, a, st);
     if (a.d <= 32) return run_grads<32>(a, st);
     if (a.d <= 64) return run_grads<64>(a, st);
     if (a.d <= 96) return run_grads<96>(a, st);

@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             const bool masked = (j < n[0] && j >= part[0]) || (j < n[1] && j >= part[1]);
             if (masked) {
                 const int left = min(kTileRows, k.count - j * kTileRows);
-                clear_rows(v, BOXES, left, lane);
+                clear_rows<kTileRows>(v, BOXES, left, lane);
                 for (int b = 0; b < BOXES; ++b)
                     for (int at = lane * 16; at < left * 128; at += 512) {
                         uint4* w = reinterpret_cast<uint4*>(smem + (v - base) + b * kTileBytes + at);
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             const int s = j % kStages;
             wait_spin(pp, G::BAR_KFULL + s, j / kStages, kAttendTimeout);
             tc_fence_after_sync();
-            mma_rows<BOXES>(elected, pp.tmem + G::TM_S + w * G::kS, base + G::OFF_Q + w * G::kOperand, base + G::OFF_K + s * G::kOperand, id_s, steps);
+            mma_rows<BOXES, kTileRows>(elected, pp.tmem + G::TM_S + w * G::kS, base + G::OFF_Q + w * G::kOperand, base + G::OFF_K + s * G::kOperand, id_s, steps);
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_S + w));
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_KFREE + s));
         };
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             wait_spin(pp, G::BAR_VREADY + s, j / kStages, kAttendTimeout);
             wait_spin(pp, G::BAR_P + w, j, kAttendTimeout);
             tc_fence_after_sync();
-            mma_sum<BOXES>(elected, pp.tmem + G::TM_O + w * G::kO, tp, tp + 32, base + G::OFF_V + s * G::kOperand, id_o, j > 0);
+            mma_sum<BOXES, kTileRows, 32>(elected, pp.tmem + G::TM_O + w * G::kO, tp, base + G::OFF_V + s * G::kOperand, id_o, j > 0);
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_O + w));
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_VFREE + s));
             if (BOXES == 2 && j + 1 < n[w]) {

@@ -79,11 +79,11 @@ __device__ __forceinline__ float2 exp2_fma(float2 x) {
     p = ffma2(p, f, c(1.0000001f));
     return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
-// Rows `from` .. 127 of a tile in shared memory (`boxes` of 64 channels) become zero: what lies behind a sequence must not meet a probability of zero.
-__device__ __forceinline__ void clear_rows(uint32_t tile, int boxes, int from, int lane) {
+// Rows from `from` on of a tile of ROWS rows in shared memory (`boxes` of 64 channels) become zero: what lies behind a sequence must not meet a probability of zero.
+template <int ROWS> __device__ __forceinline__ void clear_rows(uint32_t tile, int boxes, int from, int lane) {
     for (int b = 0; b < boxes; ++b)
-        for (uint32_t at = from * 128 + lane * 16; at < (uint32_t)kTileBytes; at += 512)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(tile + b * kTileBytes + at), "r"(0) : "memory");
+        for (uint32_t at = from * 128 + lane * 16; at < (uint32_t)ROWS * 128; at += 512)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(tile + b * ROWS * 128 + at), "r"(0) : "memory");
 }
 // Four steps of 16 of a sum with A in tensor memory (8 columns a step) and B's rows the sum's, by the elected lane
 __device__ __forceinline__ void umma_four_ts(uint32_t elected, uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
@@ -98,21 +98,21 @@ __device__ __forceinline__ void umma_four_ts(uint32_t elected, uint32_t d, uint3
         "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t}\n"
         ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate), "r"(elected) : "memory");
 }
-// D = A B with A (128 rows) and B in shared memory, both K-major: `steps` of 16 channels
-template <int BOXES> __device__ __forceinline__ void mma_rows(uint32_t elected, uint32_t d, uint32_t a, uint32_t b, uint32_t id, int steps) {
+// D = A B with A (128 rows) and B (ROWS) in shared memory, both K-major: `steps` of 16 channels
+template <int BOXES, int ROWS> __device__ __forceinline__ void mma_rows(uint32_t elected, uint32_t d, uint32_t a, uint32_t b, uint32_t id, int steps) {
 #pragma unroll
     for (int x = 0; x < BOXES; ++x) {
-        const uint64_t da = umma_desc_sw128(a + x * kTileBytes), db = umma_desc_sw128(b + x * kTileBytes);
+        const uint64_t da = umma_desc_sw128(a + x * kTileBytes), db = umma_desc_sw128(b + x * ROWS * 128);
         if (steps >= 4 * x + 4) umma_four<false, 2, 2>(elected, d, da, db, id, x);
         else
             for (int k = 0; k < steps - 4 * x; ++k) umma_step<false>(elected, d, da + 2 * k, db + 2 * k, id, x | k);
     }
 }
-// D (+)= P B: P (128 rows, 128 columns of 16 bits: 64 in `p`, 64 in `p2`) in tensor memory, B's rows are the sum's
-template <int BOXES> __device__ __forceinline__ void mma_sum(uint32_t elected, uint32_t d, uint32_t p, uint32_t p2, uint32_t b, uint32_t id, bool add) {
-    const uint64_t db = BOXES == 1 ? umma_desc_sw128(b) : desc_mn(b, kTileBytes);
-    umma_four_ts(elected, d, p, db, id, add);
-    umma_four_ts(elected, d, p2, db + 512, id, 1);
+// D (+)= P B: P (128 rows, KEYS columns of 16 bits, 64 of them every PSTEP columns) in tensor memory, B's KEYS rows are the sum's
+template <int BOXES, int KEYS, int PSTEP> __device__ __forceinline__ void mma_sum(uint32_t elected, uint32_t d, uint32_t p, uint32_t b, uint32_t id, bool add) {
+    const uint64_t db = BOXES == 1 ? umma_desc_sw128(b) : desc_mn(b, KEYS * 128);
+#pragma unroll
+    for (int k = 0; k < KEYS / 64; ++k) umma_four_ts(elected, d, p + PSTEP * k, db + 512 * k, id, add || k > 0);
 }
 
 }  // namespace aa
