@@ -5,9 +5,10 @@
 //   else   a block owns 128 queries of a head and walks their keys:  S = Q K^T, dP = dO V^T, dQ += dS K; bf16: it also makes D = rowsum(dO O) for the other one
 //   KEYS   it owns 128 keys and walks the queries, of every head of the group, that see them:  S' = K Q^T, dP' = V dO^T, dV += P' dO, dK += dS' Q
 // P = exp2(scale S - lse) and dS = P (dP - D) take the place in tensor memory of what they are made of, as A operands.  Up to 64 channels: two blocks an SM, tiles of 64
-// columns, four warps (thread = row); starts and ends of blocks overlap, and one block's exponentials run beside the other's products.  More channels: one block, tiles of
-// 128 columns of which two groups of four warps take a half each.  (Tiles of 64 columns in turns for two groups of one block, 128 channels: 335 us where this takes 251,
-// since an instruction of 64 columns costs three quarters of one of 128.)
+// columns; starts and ends of blocks overlap, and one block's exponentials run beside the other's products.  More channels: one block, tiles of 128 columns.  A thread
+// has a row and 32 columns of a tile: what a tile costs besides its arithmetic (waits, arrivals, tensor memory) is shared by sixteen warps of an SM (by eight, with 64
+// columns each: 8 heads of 4096 x 4096 x 128 257 us, 16 of 64 channels 354).
+// Tried: tiles of 64 columns in turns for two groups of one block, 128 channels: 335 us (an instruction of 64 columns costs three quarters of one of 128).
 // Roles after these warps: products; TMA (the block's own rows once, then the columns' two operands in a ring each); a warp that makes rows behind a sequence zero (they
 // meet zeros in the sums, and need not be finite) and, KEYS, fetches the queries' statistics.
 #include "attend_umma.cuh"
@@ -24,12 +25,15 @@ struct GradArgs {
 
 constexpr int OFF_DEAD = 512, OFF_TMEM = 516;
 template <int BOXES, bool KEYS> struct GradUmma {
-    static constexpr int COLS = 64 * BOXES, GROUPS = BOXES, kThreads = 128 * GROUPS + 128, kBlocks = BOXES == 1 ? 2 : 1, kColBytes = COLS * 128;
+    static constexpr int COLS = 64 * BOXES, GROUPS = 2 * BOXES, kThreads = 128 * GROUPS + 128, kBlocks = BOXES == 1 ? 2 : 1, kColBytes = COLS * 128;
     static constexpr uint32_t kTmem = 256 * BOXES;
+    // registers: of the block's threads x kStart at launch
+    static constexpr int kStart = BOXES == 1 ? 80 : 96, kRowRegs = BOXES == 1 ? 96 : 104, kRoleRegs = BOXES == 1 ? 48 : 64;
+    static_assert(128 * GROUPS * kRowRegs + 128 * kRoleRegs <= kThreads * kStart && kThreads * kStart * kBlocks <= 65536, "registers");
     // stages of the operand that the logits and the last sum read, and of the other one
-    static constexpr int kStages = BOXES == 1 ? 4 : KEYS ? 2 : 3, kStages1 = BOXES == 1 ? 4 : 2, kOwn = BOXES * kTileBytes, kOperand = BOXES * kColBytes;
-    static constexpr int OFF_X = 1024, OFF_RING = OFF_X + 2 * kOwn, OFF_RING1 = OFF_RING + kStages * kOperand, OFF_STAT = OFF_RING1 + kStages1 * kOperand,
-                         kSmem = OFF_STAT + (KEYS ? kStages * 2 * COLS * 4 : 0) + 1024;
+    static constexpr int kStages = BOXES == 1 ? 4 : KEYS ? 2 : 3, kStats = kStages, kStages1 = BOXES == 1 ? 4 : 2, kOwn = BOXES * kTileBytes, kOperand = BOXES * kColBytes;
+    static constexpr int OFF_DOT = 1024, OFF_X = 2048, OFF_RING = OFF_X + 2 * kOwn, OFF_RING1 = OFF_RING + kStages * kOperand, OFF_STAT = OFF_RING1 + kStages1 * kOperand,
+                         kSmem = OFF_STAT + (KEYS ? kStats * 2 * COLS * 4 : 0) + 1024;
     static_assert(kSmem * kBlocks <= 232448, "shared memory");
     // mbarriers                             count            waiter
     static constexpr int BAR_X = 0,               // tx               issuer
@@ -42,8 +46,8 @@ template <int BOXES, bool KEYS> struct GradUmma {
         BAR_S = BAR_FREE1 + kStages1,             // commit           rows
         BAR_T = BAR_S + 1,                        // [2] commit       rows (KEYS: one buffer)
         BAR_P = BAR_T + 2,                        // rows' warps      issuer: KEYS: P is there; else: S has been read
-        BAR_DS = BAR_P + 1,                       // rows' warps      issuer
-        BAR_V = BAR_DS + 1,                       // commit           issuer
+        BAR_DS = BAR_P + 1,                       // [2] rows' warps  issuer: in turns; without KEYS all may be a tile ahead of it, and a wait knows a phase only from its neighbours
+        BAR_V = BAR_DS + 2,                       // commit           issuer
         BAR_A = BAR_V + 1,                        // commit           issuer
         BAR_END = BAR_A + 1, kBars = BAR_END + 1;      // commit, once: everybody
     static_assert(8 * kBars <= OFF_DEAD, "mbarriers");
@@ -52,7 +56,7 @@ template <int BOXES, bool KEYS> struct GradUmma {
 template <typename T, int BOXES, bool KEYS>
 __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXES, KEYS>::kBlocks) attend_grad_umma_kernel(const __grid_constant__ GradArgs u) {
     using G = GradUmma<BOXES, KEYS>;
-    constexpr int kStages = G::kStages, kStages1 = G::kStages1, COLS = G::COLS, GROUPS = G::GROUPS, kFmt = Elem<T>::kIsBf16 ? 1 : 0;
+    constexpr int kStages = G::kStages, kStages1 = G::kStages1, COLS = G::COLS, kFmt = Elem<T>::kIsBf16 ? 1 : 0;
     // tensor memory columns.  KEYS: S, dP, dV, dK; else S, dP twice, dQ
     constexpr uint32_t TM_T = COLS, TM_V = 2 * COLS, TM_A = 3 * COLS;
     constexpr bool kDot = !KEYS && !is_f16<T>;
@@ -60,7 +64,7 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, role = warp - 4 * GROUPS;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, role = warp - 4 * G::GROUPS;
     const int group = a.heads / a.kv_heads, wide = KEYS ? a.kv_heads : a.heads, mine = blockIdx.x % wide, hk = KEYS ? mine : mine / group;
     const unsigned slot = blockIdx.x / wide;
     int seq, tile;
@@ -87,7 +91,7 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
     pp.bars = base;
     if (tid == 0) {
         *pp.dead = 0;
-        for (int i = 0; i < G::kBars; ++i) mbar_init(pp.bars + 8 * i, i >= G::BAR_P && i < G::BAR_V ? 4u * GROUPS : 1u);
+        for (int i = 0; i < G::kBars; ++i) mbar_init(pp.bars + 8 * i, i >= G::BAR_P && i < G::BAR_V ? 4u * G::GROUPS : 1u);
         mbar_fence_init();
     }
     if (role == 0) tmem_alloc<G::kTmem>(base + OFF_TMEM);
@@ -95,9 +99,11 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
     __syncthreads();
     tc_fence_after_sync();
     pp.tmem = *reinterpret_cast<const volatile uint32_t*>(smem + OFF_TMEM);
-    float* stats = reinterpret_cast<float*>(smem + G::OFF_STAT);   // [stages][lse | D][COLS]
+    float* stats = reinterpret_cast<float*>(smem + G::OFF_STAT);   // [kStats][lse | D][COLS]
     const float kappa_seq = KEYS && is_f16<T> ? grad_factor(__uint_as_float(grad_most(a, seq, hk)[0]), __uint_as_float(grad_most(a, seq, hk)[1])) : 1.f;
 
+    if (role >= 0) {
+    set_regs_dec<G::kRoleRegs>();
     if (role == 1) {
         // ------------------------------------------------------------------ producer
         if (lane == 0 && total) {
@@ -126,20 +132,27 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
     } else if (role == 2) {
         // ------------------------------------------------------------------ rows behind the sequence; statistics of the columns
         int t = 0, head = hk * group;
+        float2 next[COLS / 32];
+        auto fetch = [&](int t, int head) {                          // (a tile ahead: the loads take longer than anything else here)
+            const int c0 = (first + t) * COLS;
+            const float2* st = reinterpret_cast<const float2*>(a.ws) + ((long long)q.batch * a.heads + head) * a.N + q.first + c0;
+#pragma unroll
+            for (int i = 0; i < COLS / 32; ++i)                      // (a column that is none: a probability of zero)
+                next[i] = c0 + 32 * i + lane < q.count ? __ldg(st + 32 * i + lane) : make_float2(INFINITY, 0.f);
+        };
+        if (KEYS && total) fetch(t, head);
         for (int j = 0; j < total && !pipe_dead(pp); ++j) {
-            const int s = j % kStages, s1 = j % kStages1, c0 = (first + t) * COLS, left = y.count - c0;
+            const int s = j % kStages, s1 = j % kStages1, left = y.count - (first + t) * COLS;
+            if (++t == per) { t = 0; ++head; }
             if (KEYS) {
-                if (j >= kStages) wait_spin(pp, G::BAR_FREE + s, j / kStages - 1, kAttendTimeout);
-                const float2* st = reinterpret_cast<const float2*>(a.ws) + ((long long)q.batch * a.heads + head) * a.N + q.first + c0;
-                float* to = stats + s * 2 * COLS;
+                if (j >= G::kStats) wait_spin(pp, G::BAR_FREE + (j - G::kStats) % kStages, (j - G::kStats) / kStages, kAttendTimeout);      // (the last sum comes after all reads)
+                float* to = stats + j % G::kStats * 2 * COLS;
 #pragma unroll
                 for (int i = 0; i < COLS / 32; ++i) {
-                    const int c = 32 * i + lane;
-                    // (a column that is none: a probability of zero)
-                    const float2 v = c < left ? __ldg(st + c) : make_float2(INFINITY, 0.f);
-                    to[c] = v.x - (is_f16<T> ? kHeldP : 0.f);
-                    to[COLS + c] = v.y * kappa_seq;
+                    to[32 * i + lane] = next[i].x - (is_f16<T> ? kHeldP : 0.f);
+                    to[COLS + 32 * i + lane] = next[i].y * kappa_seq;
                 }
+                if (j + 1 < total) fetch(t, head);
             }
             wait_spin(pp, G::BAR_FULL + s, j / kStages, kAttendTimeout);
             if (left < COLS) {
@@ -157,7 +170,6 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
             __syncwarp();
             if (lane == 0) pipe_arrive(pp, G::BAR_READY1 + s1);
             __syncwarp();
-            if (++t == per) { t = 0; ++head; }
         }
         __syncwarp();
     } else if (role == 0) {
@@ -188,7 +200,7 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
             wait_spin(pp, G::BAR_P, j, kAttendTimeout);                      // (KEYS: P; else S has been read)
             tc_fence_after_sync();
             if (KEYS) {
-                mma_sum<BOXES, COLS, 64>(elected, pp.tmem + TM_V, pp.tmem, ring1(j), id_a, j > 0);
+                mma_sum<BOXES, COLS, true>(elected, pp.tmem + TM_V, pp.tmem, ring1(j), id_a, j > 0);
                 umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_FREE1 + j % kStages1));
                 umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_V));
                 if (j + 1 < total) {
@@ -200,9 +212,9 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
                 if (j > 0) wait_spin(pp, G::BAR_A, j - 1, kAttendTimeout);   // (the next slopes that of dS of two tiles ago)
                 slopes(j + 1);
             }
-            wait_spin(pp, G::BAR_DS, j, kAttendTimeout);
+            wait_spin(pp, G::BAR_DS + (j & 1), j >> 1, kAttendTimeout);
             tc_fence_after_sync();
-            mma_sum<BOXES, COLS, 64>(elected, pp.tmem + TM_A, slope_at(j), ring(j), id_a, j > 0);
+            mma_sum<BOXES, COLS, true>(elected, pp.tmem + TM_A, slope_at(j), ring(j), id_a, j > 0);
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_FREE + j % kStages));
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_A));
             if (KEYS && j + 1 < total) {
@@ -212,24 +224,25 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
         }
         umma_drain_w(pp, G::BAR_END);
         __syncwarp();
-    } else if (role < 0) {
+    }
+    } else {
         // ------------------------------------------------------------------ P and dS
+        set_regs_inc<G::kRowRegs>();
         const int w = warp >> 2, local = 32 * (warp & 3) + lane, row = r0 + local;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
         const uint32_t elected = elect_lane();
         const float c1 = a.scale * kLog2e;
         float lse = 0.f, dot = 0.f, kappa = kappa_seq;
         int limit = 0;                             // rows are queries: keys that this one sees; keys: the first query that sees it
-        if (KEYS) {
-            limit = a.causal ? row - ahead : 0;
-        } else if (row < rows) {
-            const long long at = ((long long)q.batch * a.heads + mine) * a.N + q.first + row;
-            float2 st;
-            if (kDot) {
+        float2* dots = reinterpret_cast<float2*>(smem + G::OFF_DOT);         // (one group makes the rows' statistics, all read them)
+        if (kDot) {
+            float2 st = make_float2(0.f, 0.f);
+            if (w == 0 && row < rows) {
+                const long long at = ((long long)q.batch * a.heads + mine) * a.N + q.first + row;
                 const T* o = static_cast<const T*>(a.out) + q.batch * a.lo.sb + mine * a.lo.sh + (long long)(q.first + row) * a.lo.st;
                 const T* g = static_cast<const T*>(a.dout) + q.batch * a.ldo.sb + mine * a.ldo.sh + (long long)(q.first + row) * a.ldo.st;
                 st = make_float2(a.lse[at] * kLog2e, 0.f);
-#pragma unroll 8
+#pragma unroll 4
                 for (int c = 0; c < a.d; c += 8) {
                     float f[8], h[8];
                     unpack16<T>(__ldg(reinterpret_cast<const uint4*>(o + c)), f);
@@ -237,8 +250,19 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
 #pragma unroll
                     for (int e = 0; e < 8; ++e) st.y = fmaf(f[e], h[e], st.y);
                 }
-                if (w == 0) reinterpret_cast<float2*>(a.ws)[at] = st;
+                reinterpret_cast<float2*>(a.ws)[at] = st;
+            }
+            if (w == 0) dots[local] = st;
+            asm volatile("bar.sync 1, %0;\n" ::"n"(128 * G::GROUPS) : "memory");
+        }
+        if (KEYS) {
+            limit = a.causal ? row - ahead : 0;
+        } else if (row < rows) {
+            float2 st;
+            if (kDot) {
+                st = dots[local];
             } else {
+                const long long at = ((long long)q.batch * a.heads + mine) * a.N + q.first + row;
                 st = __ldg(reinterpret_cast<const float2*>(a.ws) + at);
                 kappa = grad_factor(grad_norms(a)[at], __uint_as_float(grad_most(a, seq, hk)[1]));
             }
@@ -249,36 +273,34 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
         const int whole = KEYS ? 0 : visible_keys(a.causal, r0, q.count, k.count);         // keys that every row sees
         int t = 0;
         for (int j = 0; j < total; ++j) {
-            const int s = j % kStages, tile0 = (first + t) * COLS, c0 = tile0 + 64 * w;       // (this thread's columns)
+            const int s = j % kStages, tile0 = (first + t) * COLS, c0 = tile0 + 32 * w;       // (this thread's columns)
             if (++t == per) t = 0;
             const bool masked = KEYS ? tile0 + COLS > q.count || (a.causal && tile0 < r0 + kTileRows - 1 - ahead) : tile0 + COLS > whole;
-            const float4* st = reinterpret_cast<const float4*>(stats + s * 2 * COLS + 64 * w);
+            const float4* st = reinterpret_cast<const float4*>(stats + j % G::kStats * 2 * COLS + 32 * w);
             if (KEYS) wait_soon(pp, G::BAR_READY + s, j / kStages);
             wait_soon(pp, G::BAR_S, j);
             tc_fence_after_sync();
-            const uint32_t ts = pp.tmem + lanes + 64 * w, tt = pp.tmem + TM_T + (KEYS ? 0 : (j & 1) * COLS) + lanes + 64 * w;
-            uint32_t o[2][32];
-            tmem_ld32(ts, o[0]);
-            tmem_ld32(ts + 32, o[1]);
+            const uint32_t ts = pp.tmem + lanes + 32 * w, tt = pp.tmem + TM_T + (KEYS ? 0 : (j & 1) * COLS) + lanes + 32 * w;
+            uint32_t o[32], z[16];
+            tmem_ld32(ts, o);
             tmem_ld_wait();
             if (!KEYS) {
                 tc_fence_before_sync();
                 arrive_warp_e<false>(elected, pipe_bar(pp, G::BAR_P));
             }
-            float2 p[32];
+            float2 p[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 float4 l = make_float4(lse, lse, lse, lse);
                 if (KEYS) l = st[i];
-                const uint32_t* v = o[i >> 3] + 4 * (i & 7);
-                const float2 e0 = ffma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), make_float2(c1, c1), make_float2(-l.x, -l.y));
-                const float2 e1 = ffma2(make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])), make_float2(c1, c1), make_float2(-l.z, -l.w));
+                const float2 e0 = ffma2(make_float2(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1])), make_float2(c1, c1), make_float2(-l.x, -l.y));
+                const float2 e1 = ffma2(make_float2(__uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3])), make_float2(c1, c1), make_float2(-l.z, -l.w));
                 p[2 * i] = make_float2(fast_exp2(e0.x), fast_exp2(e0.y));
                 p[2 * i + 1] = make_float2(fast_exp2(e1.x), fast_exp2(e1.y));
             }
             if (masked) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
+                for (int i = 0; i < 16; ++i) {
                     const int c = c0 + 2 * i;
                     if (KEYS ? c < limit || c >= q.count : c >= limit) p[i].x = 0.f;
                     if (KEYS ? c + 1 < limit || c + 1 >= q.count : c + 1 >= limit) p[i].y = 0.f;
@@ -286,84 +308,71 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
             }
             if (KEYS) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t v[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = pack2<T>(p[16 * h + i].x, p[16 * h + i].y);
-                    tmem_st16(ts + 16 * h, v);
-                }
+                for (int i = 0; i < 16; ++i) z[i] = pack2<T>(p[i].x, p[i].y);
+                tmem_st16(ts, z);
                 tmem_st_wait();
                 tc_fence_before_sync();
                 arrive_warp_e<false>(elected, pipe_bar(pp, G::BAR_P));
             }
             wait_soon(pp, G::BAR_T + (KEYS ? 0 : j & 1), KEYS ? j : j >> 1);
             tc_fence_after_sync();
+            tmem_ld32(tt, o);
+            tmem_ld_wait();
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t o[32], z[16];
-                tmem_ld32(tt + 32 * h, o);
-                tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float4 d = make_float4(dot, dot, dot, dot);
-                    if (KEYS) d = st[COLS / 4 + 8 * h + i];
-                    const float2 kk = make_float2(kappa, kappa);
-                    float2 e0 = make_float2(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1])), e1 = make_float2(__uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
-                    if (is_f16<T>) {
-                        e0 = ffma2(e0, kk, make_float2(-d.x, -d.y));
-                        e1 = ffma2(e1, kk, make_float2(-d.z, -d.w));
-                    } else {
-                        e0 = fadd2(e0, make_float2(-d.x, -d.y));
-                        e1 = fadd2(e1, make_float2(-d.z, -d.w));
-                    }
-                    e0 = fmul2(e0, p[16 * h + 2 * i]);
-                    e1 = fmul2(e1, p[16 * h + 2 * i + 1]);
-                    z[2 * i] = pack2<T>(e0.x, e0.y);
-                    z[2 * i + 1] = pack2<T>(e1.x, e1.y);
+            for (int i = 0; i < 8; ++i) {
+                float4 d = make_float4(dot, dot, dot, dot);
+                if (KEYS) d = st[COLS / 4 + i];
+                const float2 kk = make_float2(kappa, kappa);
+                float2 e0 = make_float2(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1])), e1 = make_float2(__uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+                if (is_f16<T>) {
+                    e0 = ffma2(e0, kk, make_float2(-d.x, -d.y));
+                    e1 = ffma2(e1, kk, make_float2(-d.z, -d.w));
+                } else {
+                    e0 = fadd2(e0, make_float2(-d.x, -d.y));
+                    e1 = fadd2(e1, make_float2(-d.z, -d.w));
                 }
-                if (masked) {                                                // (0 * NaN)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if (p[16 * h + i].x == 0.f) z[i] &= 0xffff0000u;
-                        if (p[16 * h + i].y == 0.f) z[i] &= 0xffffu;
-                    }
-                }
-                tmem_st16(tt + 16 * h, z);
+                e0 = fmul2(e0, p[2 * i]);
+                e1 = fmul2(e1, p[2 * i + 1]);
+                z[2 * i] = pack2<T>(e0.x, e0.y);
+                z[2 * i + 1] = pack2<T>(e1.x, e1.y);
             }
+            if (masked) {                                                    // (0 * NaN)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if (p[i].x == 0.f) z[i] &= 0xffff0000u;
+                    if (p[i].y == 0.f) z[i] &= 0xffffu;
+                }
+            }
+            tmem_st16(tt, z);
             tmem_st_wait();
             tc_fence_before_sync();
-            arrive_warp_e<false>(elected, pipe_bar(pp, G::BAR_DS));
+            arrive_warp_e<false>(elected, pipe_bar(pp, G::BAR_DS + (j & 1)));
         }
         wait_soon(pp, G::BAR_END, 0);
         tc_fence_after_sync();
-        // two groups store one of the two results each, or half of the channels; one stores all
+        // every group stores its share of the results' channels, 32 at a time: dK and dV, or dQ
         const float back = is_f16<T> ? kHeldBack : 1.f;
 #pragma unroll
-        for (int r = 0; r < (KEYS ? 2 : 1); ++r) {                   // dK or dQ, dV
-            if (KEYS && GROUPS == 2 && r != w) continue;
+        for (int i = 0; i < (KEYS ? 2 : 1); ++i) {
+            const int part = KEYS ? 2 * w + i : w, r = part / (2 * BOXES), h = part % (2 * BOXES);
             const float factor = r ? back : a.scale * back / kappa;
             void* out = KEYS ? (r ? a.dv : a.dk) : a.dq;
             const TokLayout& lo = KEYS ? (r ? a.ldv : a.ldk) : a.ldq;
             T* to = static_cast<T*>(out) + x.batch * lo.sb + mine * lo.sh + (long long)(x.first + row) * lo.st;
-            const uint32_t acc = pp.tmem + (r ? TM_V : TM_A) + lanes;
+            uint32_t o[32] = {};
+            if (total) {
+                tmem_ld32(pp.tmem + (r ? TM_V : TM_A) + lanes + 32 * h, o);
+                tmem_ld_wait();
+            }
+            if (row >= rows) continue;
 #pragma unroll
-            for (int h = 0; h < 2 * BOXES; ++h) {
-                if (!KEYS && GROUPS == 2 && h / BOXES != w) continue;
-                uint32_t o[32] = {};
-                if (total) {
-                    tmem_ld32(acc + 32 * h, o);
-                    tmem_ld_wait();
-                }
-                if (row >= rows) continue;
+            for (int g = 0; g < 4; ++g) {
+                const int c = 32 * h + 8 * g;
+                if (c >= a.d) continue;
+                float f[8];
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int c = 32 * h + 8 * g;
-                    if (c >= a.d) continue;
-                    float f[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(o[8 * g + i]) * factor;
-                    *reinterpret_cast<uint4*>(to + c) = pack16<T>(f);
-                }
+                for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(o[8 * g + e]) * factor;
+                *reinterpret_cast<uint4*>(to + c) = pack16<T>(f);
             }
         }
         tc_fence_before_sync();

@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             wait_spin(pp, G::BAR_VREADY + s, j / kStages, kAttendTimeout);
             wait_spin(pp, G::BAR_P + w, j, kAttendTimeout);
             tc_fence_after_sync();
-            mma_sum<BOXES, kTileRows, 32>(elected, pp.tmem + G::TM_O + w * G::kO, tp, base + G::OFF_V + s * G::kOperand, id_o, j > 0);
+            mma_sum<BOXES, kTileRows, false>(elected, pp.tmem + G::TM_O + w * G::kO, tp, base + G::OFF_V + s * G::kOperand, id_o, j > 0);
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_O + w));
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_VFREE + s));
             if (BOXES == 2 && j + 1 < n[w]) {

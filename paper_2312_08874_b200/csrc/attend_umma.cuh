@@ -85,18 +85,18 @@ template <int ROWS> __device__ __forceinline__ void clear_rows(uint32_t tile, in
         for (uint32_t at = from * 128 + lane * 16; at < (uint32_t)ROWS * 128; at += 512)
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(tile + b * ROWS * 128 + at), "r"(0) : "memory");
 }
-// Four steps of 16 of a sum with A in tensor memory (8 columns a step) and B's rows the sum's, by the elected lane
-__device__ __forceinline__ void umma_four_ts(uint32_t elected, uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+// Four steps of 16 of a sum with A in tensor memory (8 columns a step, MID from the second to the third) and B's rows the sum's, by the elected lane
+template <int MID> __device__ __forceinline__ void umma_four_ts(uint32_t elected, uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p, q, t;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\tsetp.ne.b32 q, %5, 0;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
         "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
         "add.s32 a, %1, 8;\n\tadd.s64 b, %2, 128;\n\t"
         "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
-        "add.s32 a, a, 8;\n\tadd.s64 b, b, 128;\n\t"
+        "add.s32 a, a, %6;\n\tadd.s64 b, b, 128;\n\t"
         "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
         "add.s32 a, a, 8;\n\tadd.s64 b, b, 128;\n\t"
         "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t}\n"
-        ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate), "r"(elected) : "memory");
+        ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate), "r"(elected), "n"(MID) : "memory");
 }
 // D = A B with A (128 rows) and B (ROWS) in shared memory, both K-major: `steps` of 16 channels
 template <int BOXES, int ROWS> __device__ __forceinline__ void mma_rows(uint32_t elected, uint32_t d, uint32_t a, uint32_t b, uint32_t id, int steps) {
@@ -108,11 +108,11 @@ template <int BOXES, int ROWS> __device__ __forceinline__ void mma_rows(uint32_t
             for (int k = 0; k < steps - 4 * x; ++k) umma_step<false>(elected, d, da + 2 * k, db + 2 * k, id, x | k);
     }
 }
-// D (+)= P B: P (128 rows, KEYS columns of 16 bits, 64 of them every PSTEP columns) in tensor memory, B's KEYS rows are the sum's
-template <int BOXES, int KEYS, int PSTEP> __device__ __forceinline__ void mma_sum(uint32_t elected, uint32_t d, uint32_t p, uint32_t b, uint32_t id, bool add) {
+// D (+)= P B: P (128 rows, KEYS columns of 16 bits) in tensor memory, all together or (SPARSE) 32 of them every 32 columns; B's KEYS rows are the sum's
+template <int BOXES, int KEYS, bool SPARSE> __device__ __forceinline__ void mma_sum(uint32_t elected, uint32_t d, uint32_t p, uint32_t b, uint32_t id, bool add) {
     const uint64_t db = BOXES == 1 ? umma_desc_sw128(b) : desc_mn(b, KEYS * 128);
 #pragma unroll
-    for (int k = 0; k < KEYS / 64; ++k) umma_four_ts(elected, d, p + PSTEP * k, db + 512 * k, id, add || k > 0);
+    for (int k = 0; k < KEYS / 64; ++k) umma_four_ts<SPARSE ? 24 : 8>(elected, d, p + (SPARSE ? 64 : 32) * k, db + 512 * k, id, add || k > 0);
 }
 
 }  // namespace aa
