@@ -17,13 +17,101 @@ namespace aa {
 
 namespace {
 
+// Tiles of packed sequences in the order of their work, the most first: the tiles of few long sequences differ by as much as their number, and a long one that starts last
+// keeps one SM busy alone.  Work of tile i of a sequence, in units of 128 columns: ROWS rows from ROWS i on meet
+//   queries  the keys up to the last row's           keys  the queries from the first row's on
+// Every lane holds up to four sequences; the work of the tile of rank `slot` is found by bisection on how many tiles have at least so much, then the tile among its equals.
+// Some 600 cycles a block, so only where sequences are long (ranked_tiles).  Eight prompts of up to 4096 tokens, 16 heads of 128: 500 -> 483 us.  (The forward kernel's
+// blocks are fewer and gain nothing by it: 538 -> 544 us for prompts of up to 8192.)
+constexpr int kRanked = 128;
+inline bool ranked_tiles(const AttendArgs& a, int rows_of_all) { return a.q_offsets && a.sequences > 1 && a.sequences <= kRanked && rows_of_all / a.sequences >= 512; }
+template <int ROWS, bool KEYS> __device__ inline bool find_ranked(const AttendArgs& a, unsigned slot, int lane, int* seq, int* tile) {
+    int tiles[kRanked / 32], nq[kRanked / 32], nk[kRanked / 32];
+#pragma unroll
+    for (int i = 0; i < kRanked / 32; ++i) {
+        const int s = 32 * i + lane;
+        tiles[i] = nq[i] = nk[i] = 0;
+        if (s < a.sequences) {
+            nq[i] = span_of(a.q_offsets, nullptr, a.N, s).count;
+            nk[i] = span_of(a.k_offsets, nullptr, a.M, s).count;
+            tiles[i] = ((KEYS ? nk[i] : nq[i]) + ROWS - 1) / ROWS;
+        }
+    }
+    // tiles of sequence i with at least `units` of work: the first `n` or the last `n` of it
+    auto at_least = [&](int i, int units) {
+        if (units <= 0 || !tiles[i]) return tiles[i];
+        const int ahead = nk[i] - nq[i], need = (units - 1) * 128 + 1;           // columns
+        if (!a.causal) return (KEYS ? nq[i] : nk[i]) >= need ? tiles[i] : 0;
+        if (KEYS) {                                                              // nq - max(0, k0 - ahead) >= need
+            const int most = min(nq[i] - need, nq[i] - need + ahead);            // (k0 = 0 has nq + min(0, ahead))
+            return most < 0 ? 0 : min(tiles[i], max(0, nq[i] - need + ahead) / ROWS + 1);      // k0 <= nq - need + ahead
+        }
+        if (nk[i] < need) return 0;
+        // min(nq, (t + 1) ROWS) + ahead >= need: the last tile has all keys
+        const int t = max(0, (need - ahead + ROWS - 1) / ROWS - 1);
+        return tiles[i] - min(tiles[i] - 1, t);
+    };
+    auto count = [&](int units) {
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < kRanked / 32; ++i) c += at_least(i, units);
+        return __reduce_add_sync(0xffffffffu, c);
+    };
+    if ((unsigned)count(0) <= slot) return false;
+    int lo = 0, hi = (max(a.N, a.M) + 127) / 128 + 1;                            // count(lo) > slot >= count(hi)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((unsigned)count(mid) > slot) lo = mid;
+        else hi = mid;
+    }
+    int left = (int)slot - count(hi), found = -1, at = 0;                        // rank among the tiles with just `lo` units
+#pragma unroll
+    for (int i = 0; i < kRanked / 32; ++i) {
+        const int some = at_least(i, lo), more = at_least(i, hi), mine = some - more;
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const int before = upto - mine;
+        if (found < 0 && left >= before && left < upto) {
+            found = 32 * i + lane;
+            at = !a.causal || KEYS ? more + left - before : tiles[i] - 1 - more - (left - before);
+        }
+        left -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    const unsigned who = __ballot_sync(0xffffffffu, found >= 0);
+    if (!who) return false;
+    *seq = __shfl_sync(0xffffffffu, found, __ffs(who) - 1);
+    *tile = __shfl_sync(0xffffffffu, at, __ffs(who) - 1);
+    return true;
+}
+// A block's sequence and tile; by the first warp where tiles are ranked (`pick`: two words of shared memory)
+template <int ROWS, bool KEYS> __device__ __forceinline__ bool block_tile(const AttendArgs& a, bool ranked, unsigned slot, unsigned slots, int* pick, int* seq, int* tile) {
+    if (!ranked)       // (causal: the last queries, which see most, come first, and the first keys, which most see)
+        return find_slot(KEYS ? a.k_offsets : a.q_offsets, a.sequences, KEYS ? a.M : a.N, 1, ROWS, !KEYS && a.causal ? slots - 1 - slot : slot, seq, tile);
+    if (threadIdx.x < 32) {
+        int s = -1, t = 0;
+        if (!find_ranked<ROWS, KEYS>(a, slot, threadIdx.x, &s, &t)) s = -1;
+        if (threadIdx.x == 0) {
+            pick[0] = s;
+            pick[1] = t;
+        }
+    }
+    __syncthreads();
+    *seq = pick[0];
+    *tile = pick[1];
+    return pick[0] >= 0;
+}
 struct GradArgs {
     AttendArgs a;
     unsigned slots;
+    bool ranked;
     RowMap q, k, v, dout;
 };
 
-constexpr int OFF_DEAD = 512, OFF_TMEM = 516;
+constexpr int OFF_DEAD = 512, OFF_TMEM = 516, OFF_PICK = 520;
 template <int BOXES, bool KEYS> struct GradUmma {
     static constexpr int COLS = 64 * BOXES, GROUPS = 2 * BOXES, kThreads = 128 * GROUPS + 128, kBlocks = BOXES == 1 ? 2 : 1, kColBytes = COLS * 128;
     static constexpr uint32_t kTmem = 256 * BOXES;
@@ -68,8 +156,7 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
     const int group = a.heads / a.kv_heads, wide = KEYS ? a.kv_heads : a.heads, mine = blockIdx.x % wide, hk = KEYS ? mine : mine / group;
     const unsigned slot = blockIdx.x / wide;
     int seq, tile;
-    // (causal: the first keys, which most see, and the last queries, which see most, come first)
-    if (!find_slot(KEYS ? a.k_offsets : a.q_offsets, a.sequences, KEYS ? a.M : a.N, 1, kTileRows, !KEYS && a.causal ? u.slots - 1 - slot : slot, &seq, &tile)) return;
+    if (!block_tile<kTileRows, KEYS>(a, u.ranked, slot, u.slots, reinterpret_cast<int*>(smem + OFF_PICK), &seq, &tile)) return;
     const Span q = span_of(a.q_offsets, a.q_lengths, a.N, seq), k = span_of(a.k_offsets, a.k_lengths, a.M, seq);
     const int rows = KEYS ? k.count : q.count, r0 = tile * kTileRows;
     if (r0 >= rows) return;
@@ -89,9 +176,9 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
     pp.status = a.status;
     pp.dead = reinterpret_cast<int*>(smem + OFF_DEAD);
     pp.bars = base;
-    if (tid == 0) {
-        *pp.dead = 0;
-        for (int i = 0; i < G::kBars; ++i) mbar_init(pp.bars + 8 * i, i >= G::BAR_P && i < G::BAR_V ? 4u * G::GROUPS : 1u);
+    if (tid < 32) {
+        if (tid == 0) *pp.dead = 0;
+        for (int i = tid; i < G::kBars; i += 32) mbar_init(pp.bars + 8 * i, i >= G::BAR_P && i < G::BAR_V ? 4u * G::GROUPS : 1u);
         mbar_fence_init();
     }
     if (role == 0) tmem_alloc<G::kTmem>(base + OFF_TMEM);
@@ -200,7 +287,7 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
             wait_spin(pp, G::BAR_P, j, kAttendTimeout);                      // (KEYS: P; else S has been read)
             tc_fence_after_sync();
             if (KEYS) {
-                mma_sum<BOXES, COLS, true>(elected, pp.tmem + TM_V, pp.tmem, ring1(j), id_a, j > 0);
+                mma_sum<BOXES, COLS, 32>(elected, pp.tmem + TM_V, pp.tmem, ring1(j), id_a, j > 0);
                 umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_FREE1 + j % kStages1));
                 umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_V));
                 if (j + 1 < total) {
@@ -214,7 +301,7 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
             }
             wait_spin(pp, G::BAR_DS + (j & 1), j >> 1, kAttendTimeout);
             tc_fence_after_sync();
-            mma_sum<BOXES, COLS, true>(elected, pp.tmem + TM_A, slope_at(j), ring(j), id_a, j > 0);
+            mma_sum<BOXES, COLS, 32>(elected, pp.tmem + TM_A, slope_at(j), ring(j), id_a, j > 0);
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_FREE + j % kStages));
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_A));
             if (KEYS && j + 1 < total) {
@@ -388,6 +475,7 @@ template <typename T, int BOXES, bool KEYS> cudaError_t run(GradArgs u, cudaStre
     using G = GradUmma<BOXES, KEYS>;
     static std::atomic<unsigned long long> done{0};
     if (cudaError_t e = allow_smem(attend_grad_umma_kernel<T, BOXES, KEYS>, done, G::kSmem)) return e;
+    u.ranked = ranked_tiles(u.a, KEYS ? u.a.M : u.a.N);
     u.slots = (unsigned)(KEYS ? slots_of(u.a.k_offsets != nullptr, u.a.sequences, u.a.M, 1, kTileRows) : slots_of(u.a.q_offsets != nullptr, u.a.sequences, u.a.N, 1, kTileRows));
     attend_grad_umma_kernel<T, BOXES, KEYS><<<(unsigned)((long long)u.slots * (KEYS ? u.a.kv_heads : u.a.heads)), G::kThreads, G::kSmem, st>>>(u);
     return cudaGetLastError();

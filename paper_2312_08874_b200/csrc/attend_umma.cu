@@ -43,8 +43,8 @@ constexpr int kThreads = 384;
 constexpr int kRowRegs = 208, kRoleRegs = 80;       // 256 x 208 + 128 x 80 of the 384 x 168 that the block starts with
 static_assert(256 * kRowRegs + 128 * kRoleRegs <= kThreads * 168, "registers");
 
-// Turns of two warps, one of each tile, that share a scheduler (more than 64 channels): the exponentials of one run beside the products of the other.  In step with
-// each other both would wait for the tensor cores, and then both for the special-function unit (8 heads of 8192 x 8192 x 128: 323 -> 287 us).
+// Turns of two warps, one of each tile, that share a scheduler: the exponentials of one run beside the products and maxima of the other.  In step with each other both
+// would wait for the tensor cores, and then both for the special-function unit (8 heads of 8192 x 8192 x 128: 325 -> 283 us, 16 of 64 channels 476 -> 421).
 __device__ __forceinline__ void bar_sync_pair(int id) { asm volatile("bar.sync %0, 64;\n" ::"r"(id) : "memory"); }
 __device__ __forceinline__ void bar_arrive_pair(int id) { asm volatile("bar.arrive %0, 64;\n" ::"r"(id) : "memory"); }
 
@@ -52,7 +52,6 @@ template <typename T, int BOXES>
 __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_constant__ UmmaArgs u) {
     using G = FwdGeom<BOXES>;
     constexpr int kStages = G::kStages, kFmt = Elem<T>::kIsBf16 ? 1 : 0;
-    constexpr bool TURNS = BOXES == 2;
     const AttendArgs& a = u.a;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -81,9 +80,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
     pp.dead = reinterpret_cast<int*>(smem + OFF_DEAD);
     pp.bars = base;
     int* first_bad = reinterpret_cast<int*>(smem + G::OFF_BAD);
-    if (tid == 0) {
-        *pp.dead = 0;
-        for (int i = 0; i < G::kBars; ++i) mbar_init(pp.bars + 8 * i, i >= G::BAR_READ && i < G::BAR_O ? 4u : (i >= G::BAR_KFREE && i < G::BAR_VFULL) || (i >= G::BAR_VFREE && i < G::BAR_S) ? 2u : 1u);
+    if (tid < 32) {
+        if (tid == 0) *pp.dead = 0;
+        for (int i = tid; i < G::kBars; i += 32) mbar_init(pp.bars + 8 * i, i >= G::BAR_READ && i < G::BAR_O ? 4u : (i >= G::BAR_KFREE && i < G::BAR_VFULL) || (i >= G::BAR_VFREE && i < G::BAR_S) ? 2u : 1u);
         mbar_fence_init();
     }
     if (tid < 64 * BOXES) first_bad[tid] = INT_MAX;
@@ -124,26 +123,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             if (masked) {
                 const int left = min(kTileRows, k.count - j * kTileRows);
                 clear_rows<kTileRows>(v, BOXES, left, lane);
-                for (int b = 0; b < BOXES; ++b)
-                    for (int at = lane * 16; at < left * 128; at += 512) {
-                        uint4* w = reinterpret_cast<uint4*>(smem + (v - base) + b * kTileBytes + at);
-                        const uint4 x = *w;
-                        // an exponent of ones: infinity or NaN
-                        constexpr uint32_t kExp = Elem<T>::kIsBf16 ? 0x7f807f80u : 0x7c007c00u;
-                        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-                        bool bad = false;
+                __syncwarp();
+                // an exponent of ones, infinity or NaN, carries into the sign bit; eight loads at a time (one by one they took longer than a tile)
+                constexpr uint32_t kExp = Elem<T>::kIsBf16 ? 0x7f807f80u : 0x7c007c00u, kOne = Elem<T>::kIsBf16 ? 0x00800080u : 0x04000400u;
+                for (int at = lane * 16; at < BOXES * kTileBytes; at += 8 * 512) {
+                    uint4 x[8];
+                    uint32_t bad = 0;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) bad |= (y[i] & kExp & 0xffffu) == (kExp & 0xffffu) || (y[i] & kExp) >> 16 == kExp >> 16;
-                        if (bad) {
-                            const int row = at / 128, c0 = 64 * b + (((at >> 4) & 7) ^ (row & 7)) * 8;
-                            unsigned short* e = reinterpret_cast<unsigned short*>(w);
-                            for (int i = 0; i < 8; ++i)
-                                if ((e[i] & (kExp & 0xffffu)) == (kExp & 0xffffu)) {
-                                    e[i] = 0;
-                                    atomicMin(first_bad + c0 + i, j * kTileRows + row);
-                                }
-                        }
+                    for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const uint4*>(smem + (v - base) + at + 512 * i);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) bad |= ((x[i].x & kExp) + kOne) | ((x[i].y & kExp) + kOne) | ((x[i].z & kExp) + kOne) | ((x[i].w & kExp) + kOne);
+                    if (!(bad & 0x80008000u)) continue;
+                    for (int i = 0; i < 8; ++i) {
+                        const int here = at + 512 * i, row = here % kTileBytes / 128, c0 = 64 * (here / kTileBytes) + (((here >> 4) & 7) ^ (row & 7)) * 8;
+                        unsigned short* e = reinterpret_cast<unsigned short*>(smem + (v - base) + here);
+                        for (int n = 0; n < 8; ++n)
+                            if ((e[n] & (kExp & 0xffffu)) == (kExp & 0xffffu)) {
+                                e[n] = 0;
+                                atomicMin(first_bad + c0 + n, j * kTileRows + row);
+                            }
                     }
+                }
                 fence_proxy_async();
             }
             __syncwarp();
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             wait_spin(pp, G::BAR_VREADY + s, j / kStages, kAttendTimeout);
             wait_spin(pp, G::BAR_P + w, j, kAttendTimeout);
             tc_fence_after_sync();
-            mma_sum<BOXES, kTileRows, false>(elected, pp.tmem + G::TM_O + w * G::kO, tp, base + G::OFF_V + s * G::kOperand, id_o, j > 0);
+            mma_sum<BOXES, kTileRows, kTileRows>(elected, pp.tmem + G::TM_O + w * G::kO, tp, base + G::OFF_V + s * G::kOperand, id_o, j > 0);
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_O + w));
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_VFREE + s));
             if (BOXES == 2 && j + 1 < n[w]) {
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
         set_regs_inc<kRowRegs>();
         const int w = warp >> 2, row = 32 * (warp & 3) + lane, token = q0 + w * kTileRows + row;
         const int limit = visible_keys(a.causal, min(token, q.count - 1), q.count, k.count);
-        const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+        const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, elected = elect_lane();
         const uint32_t ts = pp.tmem + G::TM_S + w * G::kS + lanes, tp = pp.tmem + G::TM_P + w * G::kP + lanes, to = pp.tmem + G::TM_O + w * G::kO + lanes;
         const float c1 = a.scale * kLog2e;
         float ref = -INFINITY;
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             for (int i = 0; i < 64; ++i) x[i] = make_float2(__uint_as_float(o[i >> 4][2 * (i & 15)]), __uint_as_float(o[i >> 4][2 * (i & 15) + 1]));
             if (BOXES == 1) {
                 tc_fence_before_sync();
-                pipe_arrive_warp(pp, G::BAR_READ + w, lane);
+                arrive_warp_e<false>(elected, pipe_bar(pp, G::BAR_READ + w));
             }
             if (j >= part[w]) {
                 const int left = limit - j * kTileRows;
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             }
             const float nr = ref == -INFINITY ? 0.f : -ref;
             uint32_t p[4][16];
-            if (TURNS && (w == 0 ? j > 0 && j <= n[1] : j < n[0])) bar_sync_pair(1 + (warp & 3) + 4 * w);
+            if ((w == 0 ? j > 0 && j <= n[1] : j < n[0])) bar_sync_pair(1 + (warp & 3) + 4 * w);
             // groups of eight pairs: exponentials of one, sums and roundings of the one before
             float2 v[2][8];
 #pragma unroll
@@ -270,8 +270,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
 #pragma unroll
                     for (int i = 0; i < 8; ++i) e[i] = ffma2(x[8 * g + i], make_float2(c1, c1), make_float2(nr, nr));
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[g & 1][i] = false ? exp2_fma(e[i]) : make_float2(fast_exp2(e[i].x), fast_exp2(e[i].y));
+                    for (int i = 0; i < 8; ++i) v[g & 1][i] = make_float2(fast_exp2(e[i].x), fast_exp2(e[i].y));
                 }
+                if (g == 8 && (w == 0 ? j < n[1] : j + 1 < n[0])) bar_arrive_pair(5 + (warp & 3) - 4 * w);
                 if (g > 0) {
                     const int k = g - 1;
 #pragma unroll
@@ -279,23 +280,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
                         sum[i & 1] = fadd2(sum[i & 1], v[k & 1][i]);
                         p[k >> 1][8 * (k & 1) + i] = pack2<T>(v[k & 1][i].x, v[k & 1][i].y);
                     }
-                    if (BOXES == 1 && k == 5 && j > 0) {                         // P V of the keys before has read its probabilities
-                        wait_soon(pp, G::BAR_O + w, j - 1);
-                        tc_fence_after_sync();
-                    }
-                    if (k & 1) {
-                        if (BOXES == 2 || k >= 5) tmem_st16(tp + 8 * (k - 1), p[k >> 1]);
-                        if (BOXES == 1 && k == 5) {
-                            tmem_st16(tp, p[0]);
-                            tmem_st16(tp + 16, p[1]);
-                        }
-                    }
+                    if (BOXES == 2 && (k & 1)) tmem_st16(tp + 8 * (k - 1), p[k >> 1]);
                 }
             }
-            if (TURNS && (w == 0 ? j < n[1] : j + 1 < n[0])) bar_arrive_pair(5 + (warp & 3) - 4 * w);
+            if (BOXES == 1) {
+                if (j > 0) {                                                     // P V of the keys before has read its probabilities
+                    wait_soon(pp, G::BAR_O + w, j - 1);
+                    tc_fence_after_sync();
+                }
+#pragma unroll
+                for (int h = 0; h < 4; ++h) tmem_st16(tp + 16 * h, p[h]);
+            }
             tmem_st_wait();
             tc_fence_before_sync();
-            pipe_arrive_warp(pp, G::BAR_P + w, lane);
+            arrive_warp_e<false>(elected, pipe_bar(pp, G::BAR_P + w));
         }
         const bool live = token < q.count;
         if (n[w]) {

@@ -53,9 +53,7 @@ __device__ __forceinline__ void wait_soon(Pipe& pp, int i, uint32_t parity) {
     *reinterpret_cast<volatile int*>(pp.dead) = 1;
     if (pp.status) atomicCAS(pp.status, 0, kAttendTimeout);
 }
-// 2^x of a pair on the FMA pipe: the special-function unit makes 16 exponentials a cycle and SM and bounds these kernels, so that a share of them is made here.
-// x = n + f, |f| <= 1/2, n by adding 1.5 2^23; 2^f as a polynomial of degree 5 fitted here for the least relative error (2.4e-7 in fp32).  Below -126: 2^-126;
-// what is masked does not come here.
+// Maxima that keep a NaN
 __device__ __forceinline__ float max_nan(float a, float b) {
     float d;
     asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(d) : "f"(a), "f"(b));
@@ -65,19 +63,6 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
     float d;
     asm("max.NaN.f32 %0, %1, %2, %3;\n" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
-}
-__device__ __forceinline__ float2 exp2_fma(float2 x) {
-    x.x = max_nan(x.x, -126.f);
-    x.y = max_nan(x.y, -126.f);
-    const float2 t = fadd2(x, make_float2(12582912.f, 12582912.f));
-    const float2 f = fadd2(x, fadd2(make_float2(12582912.f, 12582912.f), make_float2(-t.x, -t.y)));
-    auto c = [](float v) { return make_float2(v, v); };
-    float2 p = ffma2(f, c(0.0013276472f), c(0.0096755419f));
-    p = ffma2(p, f, c(0.055507131f));
-    p = ffma2(p, f, c(0.2402212f));
-    p = ffma2(p, f, c(0.69314694f));
-    p = ffma2(p, f, c(1.0000001f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 // Rows from `from` on of a tile of ROWS rows in shared memory (`boxes` of 64 channels) become zero: what lies behind a sequence must not meet a probability of zero.
 template <int ROWS> __device__ __forceinline__ void clear_rows(uint32_t tile, int boxes, int from, int lane) {
@@ -108,11 +93,11 @@ template <int BOXES, int ROWS> __device__ __forceinline__ void mma_rows(uint32_t
             for (int k = 0; k < steps - 4 * x; ++k) umma_step<false>(elected, d, da + 2 * k, db + 2 * k, id, x | k);
     }
 }
-// D (+)= P B: P (128 rows, KEYS columns of 16 bits) in tensor memory, all together or (SPARSE) 32 of them every 32 columns; B's KEYS rows are the sum's
-template <int BOXES, int KEYS, bool SPARSE> __device__ __forceinline__ void mma_sum(uint32_t elected, uint32_t d, uint32_t p, uint32_t b, uint32_t id, bool add) {
+// D (+)= P B: P (128 rows, KEYS columns of 16 bits) in tensor memory, EACH of them together every EACH columns; B's KEYS rows are the sum's
+template <int BOXES, int KEYS, int EACH> __device__ __forceinline__ void mma_sum(uint32_t elected, uint32_t d, uint32_t p, uint32_t b, uint32_t id, bool add) {
     const uint64_t db = BOXES == 1 ? umma_desc_sw128(b) : desc_mn(b, KEYS * 128);
 #pragma unroll
-    for (int k = 0; k < KEYS / 64; ++k) umma_four_ts<SPARSE ? 24 : 8>(elected, d, p + (SPARSE ? 64 : 32) * k, db + 512 * k, id, add || k > 0);
+    for (int k = 0; k < KEYS / 64; ++k) umma_four_ts<EACH == 32 ? 24 : 8>(elected, d, p + (EACH == 32 || EACH == 64 ? 64 : 32) * k, db + 512 * k, id, add || k > 0);
 }
 
 }  // namespace aa
