@@ -176,10 +176,30 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
     pp.status = a.status;
     pp.dead = reinterpret_cast<int*>(smem + OFF_DEAD);
     pp.bars = base;
-    if (tid < 32) {
-        if (tid == 0) *pp.dead = 0;
-        for (int i = tid; i < G::kBars; i += 32) mbar_init(pp.bars + 8 * i, i >= G::BAR_P && i < G::BAR_V ? 4u * G::GROUPS : 1u);
+    auto load = [&](int j, int which, int row, int head) {          // one operand of a tile of columns (by one lane)
+        const int s = j % (which ? kStages1 : kStages);
+        const uint32_t bar = pipe_bar(pp, (which ? G::BAR_FULL1 : G::BAR_FULL) + s), dst = base + (which ? G::OFF_RING1 : G::OFF_RING) + s * G::kOperand;
+        mbar_arrive_expect_tx(bar, G::kOperand);
+        for (int b = 0; b < BOXES; ++b)
+            load_rows(dst + b * G::kColBytes, which ? (KEYS ? u.dout : u.v) : (KEYS ? u.q : u.k), 64 * b, row, KEYS ? head : hk, y.batch, bar);
+    };
+    if (role == 1) {                                                // the first loads are on their way while the block is set up
+        if (lane == 0) *pp.dead = 0;
+        for (int i = lane; i < G::kBars; i += 32) mbar_init(pp.bars + 8 * i, i >= G::BAR_P && i < G::BAR_V ? 4u * G::GROUPS : 1u);
         mbar_fence_init();
+        __syncwarp();
+        if (lane == 0 && total) {
+            constexpr int kParts = kTileRows / COLS;               // (boxes of COLS rows)
+            mbar_arrive_expect_tx(pipe_bar(pp, G::BAR_X), 2 * G::kOwn);
+            for (int b = 0; b < kParts * BOXES; ++b) {
+                const int ch = 64 * (b / kParts), row = x.first + r0 + COLS * (b % kParts);
+                load_rows(base + G::OFF_X + b * G::kColBytes, KEYS ? u.k : u.q, ch, row, mine, x.batch, pipe_bar(pp, G::BAR_X));
+                load_rows(base + G::OFF_X + G::kOwn + b * G::kColBytes, KEYS ? u.v : u.dout, ch, row, mine, x.batch, pipe_bar(pp, G::BAR_X));
+            }
+            load(0, 0, y.first + first * COLS, hk * group);
+            load(0, 1, y.first + first * COLS, hk * group);
+        }
+        __syncwarp();
     }
     if (role == 0) tmem_alloc<G::kTmem>(base + OFF_TMEM);
     tc_fence_before_sync();
@@ -193,26 +213,15 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
     set_regs_dec<G::kRoleRegs>();
     if (role == 1) {
         // ------------------------------------------------------------------ producer
-        if (lane == 0 && total) {
-            constexpr int kBoxBytes = COLS * 128, kParts = kTileRows / COLS;           // (boxes of COLS rows)
-            mbar_arrive_expect_tx(pipe_bar(pp, G::BAR_X), 2 * G::kOwn);
-            for (int b = 0; b < kParts * BOXES; ++b) {
-                const int ch = 64 * (b / kParts), row = x.first + r0 + COLS * (b % kParts);
-                load_rows(base + G::OFF_X + b * kBoxBytes, KEYS ? u.k : u.q, ch, row, mine, x.batch, pipe_bar(pp, G::BAR_X));
-                load_rows(base + G::OFF_X + G::kOwn + b * kBoxBytes, KEYS ? u.v : u.dout, ch, row, mine, x.batch, pipe_bar(pp, G::BAR_X));
-            }
+        if (lane == 0) {
             int t = 0, head = hk * group;
-            for (int j = 0; j < total && !pipe_dead(pp); ++j) {
-                const int row = y.first + (first + t) * COLS;
-                for (int which = 0; which < 2; ++which) {
-                    const int stages = which ? kStages1 : kStages, s = j % stages;
-                    if (j >= stages) wait_spin(pp, (which ? G::BAR_FREE1 : G::BAR_FREE) + s, j / stages - 1, kAttendTimeout);
-                    const uint32_t bar = pipe_bar(pp, (which ? G::BAR_FULL1 : G::BAR_FULL) + s), dst = base + (which ? G::OFF_RING1 : G::OFF_RING) + s * G::kOperand;
-                    mbar_arrive_expect_tx(bar, G::kOperand);
-                    for (int b = 0; b < BOXES; ++b)
-                        load_rows(dst + b * kBoxBytes, which ? (KEYS ? u.dout : u.v) : (KEYS ? u.q : u.k), 64 * b, row, KEYS ? head : hk, y.batch, bar);
-                }
+            for (int j = 1; j < total && !pipe_dead(pp); ++j) {
                 if (++t == per) { t = 0; ++head; }
+                for (int which = 0; which < 2; ++which) {
+                    const int stages = which ? kStages1 : kStages;
+                    if (j >= stages) wait_spin(pp, (which ? G::BAR_FREE1 : G::BAR_FREE) + j % stages, j / stages - 1, kAttendTimeout);
+                    load(j, which, y.first + (first + t) * COLS, head);
+                }
             }
         }
         __syncwarp();
@@ -445,21 +454,28 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
             const float factor = r ? back : a.scale * back / kappa;
             void* out = KEYS ? (r ? a.dv : a.dk) : a.dq;
             const TokLayout& lo = KEYS ? (r ? a.ldv : a.ldk) : a.ldq;
-            T* to = static_cast<T*>(out) + x.batch * lo.sb + mine * lo.sh + (long long)(x.first + row) * lo.st;
+            T* to = static_cast<T*>(out) + x.batch * lo.sb + mine * lo.sh + (long long)(x.first + r0 + 32 * (warp & 3)) * lo.st + 32 * h;       // the warp's first row
             uint32_t o[32] = {};
             if (total) {
                 tmem_ld32(pp.tmem + (r ? TM_V : TM_A) + lanes + 32 * h, o);
                 tmem_ld_wait();
             }
-            if (row >= rows) continue;
+            // through a place of the warp's own among the block's rows, which nothing reads any more (nor, without columns, has loaded): 64 bytes a row
+            unsigned char* stage = smem + G::OFF_X + (i * 4 * G::GROUPS + warp) * 2048;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int c = 32 * h + 8 * g;
-                if (c >= a.d) continue;
                 float f[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(o[8 * g + e]) * factor;
-                *reinterpret_cast<uint4*>(to + c) = pack16<T>(f);
+                *reinterpret_cast<uint4*>(stage + lane * 64 + ((g ^ ((lane >> 1) & 3)) << 4)) = pack16<T>(f);
+            }
+            __syncwarp();
+            const int chunk = lane & 3;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const int line = 8 * n + (lane >> 2);
+                if (r0 + 32 * (warp & 3) + line < rows && 32 * h + 8 * chunk < a.d)
+                    *reinterpret_cast<uint4*>(to + (long long)line * lo.st + 8 * chunk) = *reinterpret_cast<const uint4*>(stage + line * 64 + ((chunk ^ ((line >> 1) & 3)) << 4));
             }
         }
         tc_fence_before_sync();

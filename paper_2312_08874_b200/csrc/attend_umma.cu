@@ -80,10 +80,28 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
     pp.dead = reinterpret_cast<int*>(smem + OFF_DEAD);
     pp.bars = base;
     int* first_bad = reinterpret_cast<int*>(smem + G::OFF_BAD);
-    if (tid < 32) {
-        if (tid == 0) *pp.dead = 0;
-        for (int i = tid; i < G::kBars; i += 32) mbar_init(pp.bars + 8 * i, i >= G::BAR_READ && i < G::BAR_O ? 4u : (i >= G::BAR_KFREE && i < G::BAR_VFULL) || (i >= G::BAR_VFREE && i < G::BAR_S) ? 2u : 1u);
+    auto fetch = [&](int j, int kind) {                             // keys or values of a tile (by one lane)
+        const int s = j % kStages;
+        const uint32_t bar = pipe_bar(pp, (kind ? G::BAR_VFULL : G::BAR_KFULL) + s), dst = base + (kind ? G::OFF_V : G::OFF_K) + s * G::kOperand;
+        mbar_arrive_expect_tx(bar, G::kOperand);
+        for (int b = 0; b < BOXES; ++b) load_rows(dst + b * kTileBytes, kind ? u.v : u.k, 64 * b, k.first + j * kTileRows, hk, k.batch, bar);
+    };
+    if (warp == 9) {                                                // the first loads are on their way while the block is set up
+        if (lane == 0) *pp.dead = 0;
+        for (int i = lane; i < G::kBars; i += 32)
+            mbar_init(pp.bars + 8 * i, i >= G::BAR_READ && i < G::BAR_O ? 4u : (i >= G::BAR_KFREE && i < G::BAR_VFULL) || (i >= G::BAR_VFREE && i < G::BAR_S) ? 2u : 1u);
         mbar_fence_init();
+        __syncwarp();
+        if (lane == 0 && tiles) {
+            const int both = n[1] ? 2 : 1;
+            mbar_arrive_expect_tx(pipe_bar(pp, G::BAR_Q), both * G::kOperand);
+            for (int w = 0; w < both; ++w)
+                for (int b = 0; b < BOXES; ++b)
+                    load_rows(base + G::OFF_Q + w * G::kOperand + b * kTileBytes, u.q, 64 * b, q.first + q0 + w * kTileRows, head, q.batch, pipe_bar(pp, G::BAR_Q));
+            for (int j = 0; j < min(tiles, kStages); ++j)
+                for (int kind = 0; kind < 2; ++kind) fetch(j, kind);
+        }
+        __syncwarp();
     }
     if (tid < 64 * BOXES) first_bad[tid] = INT_MAX;
     if (warp == 8) tmem_alloc<512>(base + OFF_TMEM);
@@ -96,22 +114,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
     set_regs_dec<kRoleRegs>();
     if (warp == 9) {
         // ------------------------------------------------------------------ producer
-        if (lane == 0 && tiles) {
-            const int both = n[1] ? 2 : 1;
-            mbar_arrive_expect_tx(pipe_bar(pp, G::BAR_Q), both * G::kOperand);
-            for (int w = 0; w < both; ++w)
-                for (int b = 0; b < BOXES; ++b)
-                    load_rows(base + G::OFF_Q + w * G::kOperand + b * kTileBytes, u.q, 64 * b, q.first + q0 + w * kTileRows, head, q.batch, pipe_bar(pp, G::BAR_Q));
-            for (int j = 0; j < tiles && !pipe_dead(pp); ++j) {
-                const int s = j % kStages;
+        if (lane == 0)
+            for (int j = kStages; j < tiles && !pipe_dead(pp); ++j)
                 for (int kind = 0; kind < 2; ++kind) {
-                    if (j >= kStages) wait_spin(pp, (kind ? G::BAR_VFREE : G::BAR_KFREE) + s, j / kStages - 1, kAttendTimeout);
-                    const uint32_t bar = pipe_bar(pp, (kind ? G::BAR_VFULL : G::BAR_KFULL) + s), dst = base + (kind ? G::OFF_V : G::OFF_K) + s * G::kOperand;
-                    mbar_arrive_expect_tx(bar, G::kOperand);
-                    for (int b = 0; b < BOXES; ++b) load_rows(dst + b * kTileBytes, kind ? u.v : u.k, 64 * b, k.first + j * kTileRows, hk, k.batch, bar);
+                    wait_spin(pp, (kind ? G::BAR_VFREE : G::BAR_KFREE) + j % kStages, j / kStages - 1, kAttendTimeout);
+                    fetch(j, kind);
                 }
-            }
-        }
         __syncwarp();
     } else if (warp == 10) {
         // ------------------------------------------------------------------ values that not every query sees
@@ -302,27 +310,39 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             tc_fence_after_sync();
         }
         const float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y), inv = limit > 0 ? 1.f / total : 0.f;
-        T* out = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + token) * a.lo.st;
+        T* out = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + q0 + w * kTileRows + 32 * (warp & 3)) * a.lo.st;      // the warp's first row
+        // Through the queries' place in shared memory, which nothing reads any more (rows 16 bytes a lane took 2900 cycles for 64 channels), a box at a time; a tile without
+        // keys has loads of its queries in flight, maybe, but only zeros to store.
 #pragma unroll
-        for (int h = 0; h < 2 * BOXES; ++h) {
-            uint32_t o[32] = {};
+        for (int b = 0; b < BOXES; ++b) {
+            unsigned char* stage = smem + G::OFF_Q + w * G::kOperand + b * kTileBytes + 32 * (warp & 3) * 128;
             if (n[w]) {
-                tmem_ld32(to + 32 * h, o);
-                tmem_ld_wait();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t o[32];
+                    tmem_ld32(to + 64 * b + 32 * h, o);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        float f[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[i] = limit > 0 ? __uint_as_float(o[8 * g + i]) * inv : 0.f;
+                        if (part[0] < n[0] || part[1] < n[1])
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                if (first_bad[64 * b + 32 * h + 8 * g + i] < limit) f[i] = NAN;
+                        *reinterpret_cast<uint4*>(stage + lane * 128 + (((4 * h + g) ^ (lane & 7)) << 4)) = pack16<T>(f);
+                    }
+                }
+                __syncwarp();
             }
-            if (!live) continue;
+            const int chunk = lane & 7, rows = q.count - (q0 + w * kTileRows + 32 * (warp & 3));
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int c = 32 * h + 8 * g;
-                if (c >= a.d) continue;
-                float f[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = limit > 0 ? __uint_as_float(o[8 * g + i]) * inv : 0.f;
-                if (part[0] < n[0] || part[1] < n[1])
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (first_bad[c + i] < limit) f[i] = NAN;
-                *reinterpret_cast<uint4*>(out + c) = pack16<T>(f);
+            for (int i = 0; i < 8; ++i) {
+                const int r = 4 * i + (lane >> 3);
+                if (r < rows && 64 * b + 8 * chunk < a.d)
+                    *reinterpret_cast<uint4*>(out + (long long)r * a.lo.st + 64 * b + 8 * chunk) =
+                        n[w] ? *reinterpret_cast<const uint4*>(stage + r * 128 + ((chunk ^ (r & 7)) << 4)) : make_uint4(0u, 0u, 0u, 0u);
             }
         }
         if (live && a.lse) a.lse[((long long)q.batch * a.heads + head) * a.N + q.first + token] = limit > 0 ? (ref + log2f(total)) * kLn2 : -INFINITY;
