@@ -60,148 +60,158 @@ template <int TPR> constexpr int kBlock = TPR > 32 ? TPR : 256;
 
 // Blocks of an SM: what registers leave (a thread holds F values of a row, backward four times that, and the next row as it is in memory)
 template <int TPR, int F, bool BACK> constexpr int kPerSm = TPR == 512 ? (F <= 8 ? 2 : 1) : (F <= 8 ? (BACK ? 4 : 6) : F <= 16 ? (BACK ? 2 : 4) : BACK ? 1 : 2) * (TPR == 128 ? 2 : 1);
-template <typename T, int TPR, int NV, int V, bool BACK>
+// FULL: the threads' vectors are just the row's
+template <typename T, int TPR, int NV, int V, bool BACK, bool FULL>
 __global__ void __launch_bounds__(kBlock<TPR>, kPerSm<TPR, NV * V, BACK>) norm_kernel(const __grid_constant__ NormArgs a) {
-    constexpr int THREADS = kBlock<TPR>, RPB = THREADS / TPR, F = NV * V;
-    extern __shared__ float sums[];                        // backward: [2][C]
+    constexpr int THREADS = kBlock<TPR>, RPB = THREADS / TPR, F = NV * V, P = F / 2;
+    extern __shared__ float sums[];                        // backward: [warps][C]
     __shared__ float part[TPR > 32 ? 4 * (TPR / 32) : 1];
     const int tid = threadIdx.x, lane = tid % TPR, C = a.C;
     const float inv = 1.f / (float)C;
     int turn = 0;
-    float dw[BACK ? F : 1], db[BACK ? F : 1];
-    RawT<T, V> w[NV], b[BACK ? 1 : NV], x[NV], dy[BACK ? NV : 1];
-    auto fetch = [&](long long r) {
+    float2 dw[BACK ? P : 1], db[BACK ? P : 1], w[P], b[BACK ? 1 : P];      // pairs of neighbouring values: half the instructions, which bound these kernels
+    RawT<T, V> x[NV], dy[BACK ? NV : 1];
+    auto in = [&](int v) { return FULL || (v * TPR + lane) * V < C; };
+    auto fetch = [&](bool some, long long at) {            // (this lane's first element of the row)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c = (v * TPR + lane) * V;
-            if (r < a.rows && c < C) {
-                x[v] = read_raw<T, V>(static_cast<const T*>(a.x) + r * C + c);
-                if constexpr (BACK) dy[v] = read_raw<T, V>(static_cast<const T*>(a.dy) + r * C + c);
+            x[v] = RawT<T, V>{};                           // (what is none counts as zero)
+            if constexpr (BACK) dy[v] = RawT<T, V>{};
+            if (some && in(v)) {
+                x[v] = read_raw<T, V>(static_cast<const T*>(a.x) + at + v * TPR * V);
+                if constexpr (BACK) dy[v] = read_raw<T, V>(static_cast<const T*>(a.dy) + at + v * TPR * V);
             }
         }
     };
+    auto unpack = [&](const RawT<T, V>* raw, float2* f) {
+        float t[F];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) unpack_raw<T, V>(raw[v], t + v * V);
+#pragma unroll
+        for (int i = 0; i < P; ++i) f[i] = make_float2(t[2 * i], t[2 * i + 1]);
+    };
+    auto both = [](float v) { return make_float2(v, v); };
     if (BACK) pdl_release_next();
-    const long long stride = (long long)gridDim.x * RPB;
-    fetch((long long)blockIdx.x * RPB + tid / TPR);
+    const unsigned rows = (unsigned)a.rows, stride = gridDim.x * RPB, own = tid / TPR;
+    const long long step = (long long)stride * C;
+    long long at = (long long)(blockIdx.x * RPB + own) * C + lane * V;
+    fetch(blockIdx.x * RPB + own < rows, at);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int c = (v * TPR + lane) * V;
-        if (c < C && a.w) w[v] = read_raw<T, V>(static_cast<const T*>(a.w) + c);
-        if constexpr (!BACK)
-            if (c < C && a.b) b[v] = read_raw<T, V>(static_cast<const T*>(a.b) + c);
+    for (int i = 0; i < P; ++i) {
+        w[i] = both(1.f);
+        if (!BACK) b[i] = both(0.f);
+        if (BACK) dw[i] = db[i] = both(0.f);
     }
-    if (BACK)
+    {
+        RawT<T, V> t[NV];
+        if (a.w) {
 #pragma unroll
-        for (int i = 0; i < F; ++i) dw[i] = db[i] = 0.f;
-    // (every thread of a block takes the same number of turns: shuffles and barriers are met by all)
-    for (long long r0 = (long long)blockIdx.x * RPB; r0 < a.rows; r0 += stride) {
-        const long long r = r0 + tid / TPR;
-        const bool live = r < a.rows;
-        float f[F], g[BACK ? F : 1];
-        float s[1] = {0.f};
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const bool in = live && (v * TPR + lane) * V < C;
-            unpack_raw<T, V>(x[v], f + v * V);
-            if constexpr (BACK) unpack_raw<T, V>(dy[v], g + v * V);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                if (!in) f[v * V + e] = 0.f;
-                if (BACK && !in) g[v * V + e] = 0.f;
-            }
+            for (int v = 0; v < NV; ++v) t[v] = in(v) ? read_raw<T, V>(static_cast<const T*>(a.w) + (v * TPR + lane) * V) : RawT<T, V>{};
+            unpack(t, w);
         }
-        fetch(r + stride);
+        if constexpr (!BACK)
+            if (a.b) {
 #pragma unroll
-        for (int i = 0; i < F; ++i) s[0] += f[i];
+                for (int v = 0; v < NV; ++v) t[v] = in(v) ? read_raw<T, V>(static_cast<const T*>(a.b) + (v * TPR + lane) * V) : RawT<T, V>{};
+                unpack(t, b);
+            }
+    }
+    // (every thread of a block takes the same number of turns: shuffles and barriers are met by all)
+    for (unsigned r0 = blockIdx.x * RPB; r0 < rows; r0 += stride, at += step) {
+        const bool live = r0 + own < rows;
+        float2 f[P], g[BACK ? P : 1];
+        unpack(x, f);
+        if constexpr (BACK) unpack(dy, g);
+        fetch(r0 + own + stride < rows, at + step);
+        float2 q = f[0];
+#pragma unroll
+        for (int i = 1; i < P; ++i) q = fadd2(q, f[i]);
+        float s[1] = {q.x + q.y};
         row_sums<TPR, 1>(s, part, turn);
         const float mean = s[0] * inv;
-        s[0] = 0.f;
+        q = both(0.f);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const bool in = (v * TPR + lane) * V < C;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                float& z = f[v * V + e];
-                z = in ? z - mean : 0.f;
-                s[0] = fmaf(z, z, s[0]);
+        for (int i = 0; i < P; ++i) {
+            f[i] = fadd2(f[i], both(-mean));
+            if (!FULL) {
+                if (!in(2 * i / V)) f[i].x = 0.f;
+                if (!in((2 * i + 1) / V)) f[i].y = 0.f;
             }
+            q = ffma2(f[i], f[i], q);
         }
+        s[0] = q.x + q.y;
         row_sums<TPR, 1>(s, part, turn);
-        const float rs = 1.f / sqrtf(s[0] * inv + a.eps);
+        const float root = rsqrtf(s[0] * inv + a.eps), rs = live ? root : 0.f;      // (of a row that is none it may be infinite)
         if constexpr (!BACK) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c = (v * TPR + lane) * V;
-                float y[V], gain[V], shift[V];
-                unpack_raw<T, V>(w[v], gain);
-                unpack_raw<T, V>(b[v], shift);
+            for (int i = 0; i < P; ++i) f[i] = ffma2(fmul2(f[i], both(rs)), w[i], b[i]);
 #pragma unroll
-                for (int e = 0; e < V; ++e) y[e] = fmaf(f[v * V + e] * rs, a.w ? gain[e] : 1.f, a.b ? shift[e] : 0.f);
-                if (live && c < C) write_vec<T, V>(static_cast<T*>(a.y) + r * C + c, y);
+            for (int v = 0; v < NV; ++v) {
+                float y[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = (v * V + e) & 1 ? f[(v * V + e) / 2].y : f[(v * V + e) / 2].x;
+                if (live && in(v)) write_vec<T, V>(static_cast<T*>(a.y) + at + v * TPR * V, y);
             }
         } else {
-            float t[2] = {0.f, 0.f}, gain[F];
+            float2 t0 = both(0.f), t1 = t0;
 #pragma unroll
-            for (int v = 0; v < NV; ++v) unpack_raw<T, V>(w[v], gain + v * V);
-#pragma unroll
-            for (int i = 0; i < F; ++i) {
-                f[i] *= rs;
-                if (live) {                                // (a row that is none has r = 1 / sqrt(eps), which may be infinite)
-                    dw[i] = fmaf(g[i], f[i], dw[i]);
-                    db[i] += g[i];
-                }
-                if (a.w && (i / V * TPR + lane) * V < C) g[i] *= gain[i];
-                t[0] += g[i];
-                t[1] = fmaf(g[i], f[i], t[1]);
+            for (int i = 0; i < P; ++i) {
+                f[i] = fmul2(f[i], both(rs));
+                dw[i] = ffma2(g[i], f[i], dw[i]);
+                db[i] = fadd2(db[i], g[i]);
+                g[i] = fmul2(g[i], w[i]);
+                t0 = fadd2(t0, g[i]);
+                t1 = ffma2(g[i], f[i], t1);
             }
             if (a.dx) {
+                float t[2] = {t0.x + t0.y, t1.x + t1.y};
                 row_sums<TPR, 2>(t, part, turn);
-                t[0] *= inv;
-                t[1] *= inv;
+                const float2 m0 = both(-t[0] * inv), m1 = both(-t[1] * inv);
+#pragma unroll
+                for (int i = 0; i < P; ++i) g[i] = fmul2(fadd2(ffma2(f[i], m1, g[i]), m0), both(rs));
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
-                    const int c = (v * TPR + lane) * V;
                     float y[V];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) y[e] = rs * (g[v * V + e] - t[0] - f[v * V + e] * t[1]);
-                    if (live && c < C) write_vec<T, V>(static_cast<T*>(a.dx) + r * C + c, y);
+                    for (int e = 0; e < V; ++e) y[e] = (v * V + e) & 1 ? g[(v * V + e) / 2].y : g[(v * V + e) / 2].x;
+                    if (live && in(v)) write_vec<T, V>(static_cast<T*>(a.dx) + at + v * TPR * V, y);
                 }
             }
         }
     }
     if constexpr (BACK) {
         if (!a.ws) return;
-        // one row of sums a block: warps add theirs in turn
+        // one row of sums a block
         if constexpr (TPR < 32) {
 #pragma unroll
             for (int o = TPR; o < 32; o <<= 1)
 #pragma unroll
-                for (int i = 0; i < F; ++i) {
-                    dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
-                    db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
+                for (int i = 0; i < P; ++i) {
+                    dw[i] = fadd2(dw[i], make_float2(__shfl_xor_sync(0xffffffffu, dw[i].x, o), __shfl_xor_sync(0xffffffffu, dw[i].y, o)));
+                    db[i] = fadd2(db[i], make_float2(__shfl_xor_sync(0xffffffffu, db[i].x, o), __shfl_xor_sync(0xffffffffu, db[i].y, o)));
                 }
         }
         float* out = a.ws + (long long)blockIdx.x * 2 * C;
-        constexpr int TURNS = TPR > 32 ? 1 : THREADS / 32;
-        for (int k = 0; k < TURNS; ++k) {
-            if (TURNS == 1 || (tid >> 5) == k) {
+        constexpr int WARPS = TPR > 32 ? 1 : THREADS / 32;         // whose sums of the same columns meet in shared memory, in order
+        const bool first = TPR >= 32 || (tid & 31) < TPR;
 #pragma unroll
-                for (int v = 0; v < NV; ++v)
+        for (int side = 0; side < 2; ++side) {
+            if (WARPS > 1 && side) __syncthreads();
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const int c = (v * TPR + lane) * V + e, i = v * V + e;
-                        if (c >= C || (TPR < 32 && (tid & 31) >= TPR)) continue;
-                        const float p = k ? sums[c] + dw[i] : dw[i], q = k ? sums[C + c] + db[i] : db[i];
-                        if (k + 1 < TURNS) {
-                            sums[c] = p;
-                            sums[C + c] = q;
-                        } else {
-                            out[c] = p;
-                            out[C + c] = q;
-                        }
-                    }
+            for (int i = 0; i < F; ++i) {
+                const int c = (i / V * TPR + lane) * V + i % V;
+                const float2 t = side ? db[i / 2] : dw[i / 2];
+                if (first && in(i / V)) (WARPS > 1 ? sums + (tid >> 5) * C : out + side * C)[c] = i & 1 ? t.y : t.x;
             }
-            if (TURNS > 1) __syncthreads();
+            if (WARPS > 1) {
+                __syncthreads();
+                for (int c = tid; c < C; c += THREADS) {
+                    float t = sums[c];
+#pragma unroll
+                    for (int k = 1; k < WARPS; ++k) t += sums[k * C + c];
+                    out[side * C + c] = t;
+                }
+            }
         }
     }
 }
@@ -268,7 +278,7 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const float* in, int sh
     const int c = blockIdx.x * 32 + lane;
     float s = 0.f;
     if (c < 2 * C)
-#pragma unroll 8
+#pragma unroll 16
         for (int k = shares * warp / 32; k < shares * (warp + 1) / 32; ++k) s += in[(long long)k * 2 * C + c];
     part[warp][lane] = s;
     __syncthreads();
@@ -293,18 +303,19 @@ bool aligned16(const NormArgs& a) {
 struct NormPlan {
     int tpr, nv, v;
 };
-NormPlan plan_of(int dtype, int C, bool aligned) {
+NormPlan plan_of(int dtype, int C, bool aligned, bool back) {
     const int vec = dtype == 0 ? 4 : 8;
     NormPlan p{0, 0, 0};
     if (C % vec == 0 && aligned) {
         const int n = C / vec;
         p.v = vec;
-        // up to a warp a row: the fewest idle lanes, then the fewest vectors a lane
-        int idle = INT_MAX;
+        // up to a warp a row: the fewest idle lanes, then the fewest vectors a lane; backward, where a thread holds four times as much, three vectors only for a third less
+        // (8192 x 320 f16: three vectors in 16 lanes 19.7 us, two in 32 x us)
+        int least = INT_MAX;
         for (int v = 1; v <= 4; ++v)
             for (int t : {4, 8, 16, 32})
-                if (n <= t * v && t * v - n < idle && (v < 4 || t == 32)) {
-                    idle = t * v - n;
+                if (const int cost = t * v * (back && v > 2 ? 3 : 2); n <= t * v && cost < least && (v < 4 || t == 32)) {
+                    least = cost;
                     p.tpr = t;
                     p.nv = v;
                 }
@@ -327,13 +338,15 @@ long long blocks_of(const NormPlan& p, long long rows, int sm_count, bool back) 
 }
 
 template <typename T, int TPR, int NV, int V, bool BACK> cudaError_t run_norm(const NormArgs& a, const NormPlan& p, int sm_count, cudaStream_t st) {
-    const int smem = BACK && a.ws && TPR <= 32 ? 2 * a.C * 4 : 0;
-    norm_kernel<T, TPR, NV, V, BACK><<<(unsigned)blocks_of(p, a.rows, sm_count, BACK), kBlock<TPR>, smem, st>>>(a);
+    const int smem = BACK && a.ws && TPR <= 32 ? kBlock<TPR> / 32 * a.C * 4 : 0;       // (32 KB at most: 1024 channels)
+    const unsigned blocks = (unsigned)blocks_of(p, a.rows, sm_count, BACK);
+    if (V > 1 && a.C == TPR * NV * V) norm_kernel<T, TPR, NV, V, BACK, true><<<blocks, kBlock<TPR>, smem, st>>>(a);
+    else norm_kernel<T, TPR, NV, V, BACK, false><<<blocks, kBlock<TPR>, smem, st>>>(a);
     return cudaGetLastError();
 }
 template <typename T, bool BACK> cudaError_t norm_of(const NormArgs& a, int sm_count, cudaStream_t st) {
     constexpr int V = Elem<T>::kVec;
-    const NormPlan p = plan_of(sizeof(T) == 4 ? 0 : 1, a.C, aligned16(a));
+    const NormPlan p = plan_of(sizeof(T) == 4 ? 0 : 1, a.C, aligned16(a), BACK);
 #define AA_NORM(TPR, NV, VEC) if (p.tpr == TPR && p.nv == NV && p.v == VEC) return run_norm<T, TPR, NV, VEC, BACK>(a, p, sm_count, st);
     AA_NORM(4, 1, V) AA_NORM(4, 2, V) AA_NORM(4, 3, V)
     AA_NORM(8, 1, V) AA_NORM(8, 2, V) AA_NORM(8, 3, V)
@@ -362,7 +375,7 @@ template <typename T, bool BACK> cudaError_t norm_of(const NormArgs& a, int sm_c
 size_t norm_backward_bytes(int dtype, long long rows, int C, int sm_count) {
     size_t most = 0;                               // (the size does not depend on the pointers)
     for (bool aligned : {false, true}) {
-        const NormPlan p = plan_of(dtype, C, aligned);
+        const NormPlan p = plan_of(dtype, C, aligned, true);
         const size_t shares = p.tpr ? (size_t)blocks_of(p, rows, sm_count, true) : (size_t)kColumnShares;
         most = std::max(most, shares * 2 * C * sizeof(float) + (p.tpr ? 0 : (size_t)rows * sizeof(float2)));
     }
@@ -375,7 +388,7 @@ cudaError_t launch_norm_backward(int dtype, const NormArgs& a, int sm_count, cud
     NormArgs b = a;
     if (!a.dw && !a.db) b.ws = nullptr;
     const cudaError_t e = dtype == 0 ? norm_of<float, true>(b, sm_count, st) : dtype == 1 ? norm_of<__nv_bfloat16, true>(b, sm_count, st) : norm_of<__half, true>(b, sm_count, st);
-    const NormPlan p = plan_of(dtype, a.C, aligned16(a));
+    const NormPlan p = plan_of(dtype, a.C, aligned16(a), true);
     *launches = (p.tpr || !b.ws ? 1 : a.dx == a.dy ? 3 : 2) + (b.ws ? 1 : 0);
     if (e != cudaSuccess || !b.ws) return e;
     const int shares = p.tpr ? (int)blocks_of(p, a.rows, sm_count, true) : kColumnShares;
