@@ -945,26 +945,32 @@ class AgentAttention:
         """
         a = self._layer_norm(x, weight, bias, eps)
         self._chk_tensor(d_out, x.shape, "d_out")
-        g = {}
+        g, dx, dw, db, size = {}, None, None, None, 0
         if need_input_grad:
-            g["dx"] = _dense_like(x, stream) if out is None else out
-            self._chk_tensor(g["dx"], x.shape, "out")
-        if need_weight_grads:
-            for name, t in (("dw", weight), ("db", bias)):
-                if t is not None:
-                    g[name] = t.new_empty(t.shape, dtype=torch.float32) if stream is None else _empty(t.shape, torch.float32, self.device, stream)
-        if not ("dw" in g or "db" in g):
+            if out is None:
+                dx = _dense_like(x, stream)
+            else:
+                self._chk_tensor(out, x.shape, "out")
+                dx = out
+            g["dx"] = dx
+        if need_weight_grads and weight is not None:
+            g["dw"] = dw = weight.new_empty(weight.shape, dtype=torch.float32) if stream is None else _empty(weight.shape, torch.float32, self.device, stream)
+        if need_weight_grads and bias is not None:
+            g["db"] = db = bias.new_empty(bias.shape, dtype=torch.float32) if stream is None else _empty(bias.shape, torch.float32, self.device, stream)
+        if dw is None and db is None:
             workspace = None               # (not read)
-        elif workspace is not None:
-            self._chk_workspace(workspace)
         else:
-            key = ("norm", a.rows, a.channels)
-            need = self._bytes.get(key)
-            if need is None:
-                if len(self._bytes) >= 64:
-                    self._bytes.clear()
-                need = self._bytes[key] = int(self.lib.agent_attn_layer_norm_workspace_bytes(self._h, a.rows, a.channels))
-            workspace = self._scratch(need, stream)
-        self._check(self.lib.agent_attn_layer_norm_backward(self._h, ctypes.byref(a), _ptr(d_out), _ptr(g.get("dx")), _ptr(g.get("dw")), _ptr(g.get("db")), _ptr(workspace),
-                                                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+            if workspace is not None:
+                self._chk_workspace(workspace)
+            else:
+                key = ("norm", a.rows, a.channels)
+                need = self._bytes.get(key)
+                if need is None:
+                    if len(self._bytes) >= 64:
+                        self._bytes.clear()
+                    need = self._bytes[key] = int(self.lib.agent_attn_layer_norm_workspace_bytes(self._h, a.rows, a.channels))
+                # (of x's type: half of the host time that another one takes)
+                workspace = x.new_empty(-(-need // x.element_size())) if stream is None else _empty(need, torch.uint8, self.device, stream)
+            size = workspace.numel() * workspace.element_size()
+        self._check(self.lib.agent_attn_layer_norm_backward(self._h, ctypes.byref(a), d_out.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db), _ptr(workspace), size, _stream_ptr(stream)))
         return g
