@@ -772,7 +772,8 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
                 const bool seen = KEYS ? c0 + c < end && c0 + c >= limit[h] : c0 + c < limit[h];
                 const float p = seen ? fast_exp2(fmaf(x[j][e], c1, -s.x)) : 0.f;
                 x[j][e] = p;
-                y[j][e] = seen ? p * (y[j][e] - s.y) : 0.f;
+                // (a query that sees one key has P = 1, whatever its logit: no gradient but that of the value)
+                y[j][e] = seen && (KEYS ? k.count : limit[h]) != 1 ? p * (y[j][e] - s.y) : 0.f;
             }
         uint32_t w[NT][2][4];
         block_operand<E, NT>(y, w);

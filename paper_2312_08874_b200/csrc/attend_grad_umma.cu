@@ -414,6 +414,23 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
             tc_fence_after_sync();
             tmem_ld32(tt, o);
             tmem_ld_wait();
+            if (!KEYS && total == 1) {
+                // All keys of these rows are here: D = sum P dP.  Out of the result, which is rounded, it would be off by as much as the slopes of two or three keys
+                // differ (sequences of two: error of dQ and dK 2.4 of a rounding, so 1.4).  (The ring's second stage is free.)
+                float2 sum2 = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    sum2 = make_float2(p[i].x != 0.f ? fmaf(p[i].x, __uint_as_float(o[2 * i]), sum2.x) : sum2.x, p[i].y != 0.f ? fmaf(p[i].y, __uint_as_float(o[2 * i + 1]), sum2.y) : sum2.y);
+                float* share = reinterpret_cast<float*>(smem + G::OFF_RING + G::kOperand);
+                share[128 * w + local] = sum2.x + sum2.y;
+                asm volatile("bar.sync 1, %0;\n" ::"n"(128 * G::GROUPS) : "memory");
+                dot = 0.f;
+#pragma unroll
+                for (int i = 0; i < G::GROUPS; ++i) dot += share[128 * i + local];
+                dot *= is_f16<T> ? kHeldBack : 1.f;
+                if (w == 0 && row < rows) a.ws[2 * (((long long)q.batch * a.heads + mine) * a.N + q.first + row) + 1] = dot;
+                dot *= kappa;
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 float4 d = make_float4(dot, dot, dot, dot);
@@ -451,7 +468,8 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
 #pragma unroll
         for (int i = 0; i < (KEYS ? 2 : 1); ++i) {
             const int part = KEYS ? 2 * w + i : w, r = part / (2 * BOXES), h = part % (2 * BOXES);
-            const float factor = r ? back : a.scale * back / kappa;
+            // (a query that sees one key has P = 1, whatever its logit: no gradient but that of the value)
+            const float factor = r ? back : (KEYS ? k.count : limit) == 1 ? 0.f : a.scale * back / kappa;
             void* out = KEYS ? (r ? a.dv : a.dk) : a.dq;
             const TokLayout& lo = KEYS ? (r ? a.ldv : a.ldk) : a.ldq;
             T* to = static_cast<T*>(out) + x.batch * lo.sb + mine * lo.sh + (long long)(x.first + r0 + 32 * (warp & 3)) * lo.st + 32 * h;       // the warp's first row
