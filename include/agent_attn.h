@@ -473,7 +473,7 @@ size_t agent_attn_attend_workspace_bytes(const agent_attn_handle* h, const agent
 /* out  device, element type, strides out_strides;  lse  device fp32 [B][heads][queries], or NULL: natural
  * log-sum-exp of the logits, which the gradient takes.  No overlap of results with inputs.
  * Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED (tokens past max_tokens; queries x heads, or keys, past
- * 2^31 - 2^16 - 1), AA_ERR_WORKSPACE, AA_ERR_CUDA.  No host synchronisation, no allocation. */
+ * 2^31 - 2^16 - 1, sequences x heads past 2^27 - 2^12), AA_ERR_WORKSPACE, AA_ERR_CUDA.  No host synchronisation, no allocation. */
 int agent_attn_attend(agent_attn_handle* h, const agent_attn_sequences* s, void* out, const long long out_strides[3],
                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -906,7 +906,7 @@ static int attend_args(agent_attn_handle* h, const agent_attn_sequences* s, Atte
     a->sequences = s->q_offsets ? s->sequences : h->cfg.batch;
     // rows of queries x heads and of keys, and tiles of them, are numbers of 31 bits
     const long long most = INT_MAX - 65536LL, rows = (long long)a->N * a->heads;
-    if (rows > most || (long long)a->sequences > most / 16 || rows / 16 + a->sequences > most || a->M > most ||
+    if (rows > most || (long long)a->sequences * a->heads > most / 16 || rows / 16 + a->sequences > most || a->M > most ||
         (!s->q_offsets && ((rows + 15) / 16 * a->batch > most || ((long long)a->M + 63) / 64 * a->batch > most)))
         return fail(h, AA_ERR_UNSUPPORTED, "%d queries of %d heads over %d keys: rows must fit in 31 bits", a->N, a->heads, a->M);
     a->q_offsets = s->q_offsets; a->k_offsets = s->k_offsets; a->q_lengths = s->q_lengths; a->k_lengths = s->k_lengths;

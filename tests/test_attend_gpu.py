@@ -304,6 +304,46 @@ def test_small_gradients_in_f16():
     check(q, k, v, do=do)
 
 
+@pytest.mark.parametrize("dt,d", [(F32, 12), (F32, 100), (BF, 24), (FH, 104), (BF, 56), (FH, 72)])
+def test_head_sizes(dt, d):
+    q, k, v = make(1, 4, 2, 150, 270, d, dt)
+    check(q, k, v, causal=True)
+    check(q[:, :, :2].contiguous(), k, v, grad=False)
+
+
+@pytest.mark.parametrize("dt", [F32, BF, FH])
+@pytest.mark.parametrize("d", [64, 128])
+def test_sequences_of_one_to_a_few_keys(dt, d):
+    """One key: a weight of one, whatever its logit, so exactly no gradient of queries and keys.  A few keys: slopes are differences of a few numbers, which keep the
+    accuracy of theirs: two roundings (of dS and the result), each 0.44 u in the 2-norm, so 0.62 u, with room for chance 0.8 u."""
+    lengths = [1, 1, 2, 2, 3, 1, 4, 2, 3, 5] * 20
+    at = [0]
+    for n in lengths:
+        at.append(at[-1] + n)
+    q, k, v = make(1, 4, 2, at[-1], at[-1], d, dt, fused=True)
+    mod = AgentAttention(1, 4, d, at[-1], 1, dt)
+    o = torch.tensor(at, dtype=torch.int32, device="cuda")
+    do = torch.randn(q.shape, device="cuda").to(dt)
+    out, lse = mod.attend(q, k, v, q_offsets=o, need_lse=True)
+    g = mod.attend_backward(q, k, v, out, lse, do, q_offsets=o)
+    want = {n: torch.zeros(t.shape, dtype=torch.float64, device="cuda") for n, t in (("dq", q), ("dk", k), ("dv", v))}
+    for a, b in zip(at, at[1:]):
+        for h in range(4):
+            r = reference(q[0, h, a:b], k[0, h // 2, a:b], v[0, h // 2, a:b], False, d ** -0.5, do[0, h, a:b])
+            want["dq"][0, h, a:b] = r["dq"]
+            want["dk"][0, h // 2, a:b] += r["dk"]
+            want["dv"][0, h // 2, a:b] += r["dv"]
+        if b - a == 1:
+            assert (g["dq"][:, :, a] == 0).all() and (g["dk"][:, :, a] == 0).all()
+            # p = 1 within 2^-23, the same in the result's sum and its weights'; what is left are the roundings of p v, 1 / sum and their product, 2^-24 each and below half a
+            # step of a 16-bit type
+            value = v[0, :, a].repeat_interleave(2, 0)
+            assert torch.equal(out[0, :, a], value) if dt is not F32 else ((out[0, :, a] - value).abs() <= 2.0 ** -22 * value.abs()).all()
+    for n in g:
+        rel = (g[n].double() - want[n]).norm() / want[n].norm()
+        assert rel <= (0.8 * u_of(dt) if dt is not F32 else 4e-7), (n, float(rel))
+
+
 def test_long_axis():
     """Offsets of a fused projection past 2^31 bytes and 2^31 elements (in halves), one query at the far end and keys all over."""
     d, M = 64, (1 << 25) + 17
