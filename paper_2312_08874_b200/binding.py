@@ -882,7 +882,11 @@ class AgentAttention:
         s, kept = self._call(q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths)
         if out is None:
             out = self._new_view(q, q_offsets is not None or q_lengths is not None, stream)
-        sout = self._kept_strides(out, q, "out", kept)
+            sout = kept.get("new")         # (follow from q's)
+            if sout is None:
+                sout = kept["new"] = self._kept_strides(out, q, "out", kept)
+        else:
+            sout = self._kept_strides(out, q, "out", kept)
         lse = None
         if need_lse:
             lse = _empty(q.shape[:3], torch.float32, self.device, stream) if stream is not None else q.new_empty(q.shape[:3], dtype=torch.float32)
@@ -904,10 +908,14 @@ class AgentAttention:
             raise ValueError(f"lse: expected a contiguous {self.device} float32 tensor of shape {tuple(q.shape[:3])}, got {tuple(lse.shape)} {lse.dtype} on {lse.device}")
         if grads is None:
             packed = q_offsets is not None
-            grads = tuple(self._new_view(t, packed or n is not None, stream) for t, n in ((q, q_lengths), (k, k_lengths), (v, k_lengths)))
-        dq, dk, dv = grads
-        g = AgentAttnAttendGrads(dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), self._kept_strides(dq, q, "dq", kept), self._kept_strides(dk, k, "dk", kept),
-                                 self._kept_strides(dv, v, "dv", kept))
+            dq, dk, dv = (self._new_view(t, packed or n is not None, stream) for t, n in ((q, q_lengths), (k, k_lengths), (v, k_lengths)))
+            strides = kept.get("new grads")
+            if strides is None:
+                strides = kept["new grads"] = tuple(self._kept_strides(t, like, name, kept) for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")))
+        else:
+            dq, dk, dv = grads
+            strides = tuple(self._kept_strides(t, like, name, kept) for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")))
+        g = AgentAttnAttendGrads(dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), *strides)
         ws = self._attend_workspace(s, kept, 1, workspace, stream)
         self._check(self.lib.agent_attn_attend_backward(self._h, ctypes.byref(s), _ptr(out), sout, _ptr(lse), _ptr(d_out), sdo, ctypes.byref(g), _ptr(ws),
                                                         0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream)))
