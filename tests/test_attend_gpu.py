@@ -156,6 +156,24 @@ def test_packed(dt, causal, h, kv, d):
     check(q, k, v, causal=causal, q_offsets=at, k_offsets=ak)
 
 
+@pytest.mark.parametrize("dt", [BF, FH])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("h,kv,d", [(2, 1, 64), (2, 2, 128)])
+def test_long_packed_sequences(dt, causal, h, kv, d):
+    """At least 512 rows a sequence on average, where the gradient's blocks take tiles by their work; empty and very short ones among them, more and fewer keys than queries."""
+    def offsets(lengths):
+        at = [2]
+        for n in lengths:
+            at.append(at[-1] + n)
+        return at
+    at = offsets([700, 0, 1500, 3, 900, 1, 640])
+    q, k, v = make(1, h, kv, at[-1] + 9, at[-1] + 9, d, dt, fused=True)
+    check(q, k, v, causal=causal, q_offsets=at)
+    ak = offsets([1300, 40, 600, 0, 901, 1, 1024])
+    q, k, v = make(1, h, kv, at[-1] + 9, ak[-1] + 9, d, dt, seed=1)
+    check(q, k, v, causal=causal, q_offsets=at, k_offsets=ak)
+
+
 @pytest.mark.parametrize("dt", [F32, BF, FH])
 @pytest.mark.parametrize("h,kv,d,N", [(8, 2, 128, 1), (4, 4, 64, 1), (2, 1, 40, 3), (24, 1, 64, 1), (4, 1, 128, 5), (2, 2, 64, 16), (1, 1, 32, 40)])
 def test_few_queries_over_caches(dt, h, kv, d, N):
