@@ -1,14 +1,16 @@
-// Softmax attention over whole sequences on mma.sync: fp32 tensors as sums of three bf16 terms, and few queries over many keys in any type.
+// Softmax attention over whole sequences on mma.sync: fp32 tensors as sums of three bf16 terms, and few queries over many keys in any type; statistics for the gradients.
 //
 // A row is a query of one head; the heads that share keys stand side by side (row = query * group + head), so that single tokens fill a tile's rows
-// with their heads.  Forward: WR warps own 16 rows each, WK of them share the rows and take turns at blocks of 32 keys; logits, probabilities and
+// with their heads.  fp32, forward: WR warps own 16 rows each, WK of them share the rows and take turns at blocks of 32 keys; logits, probabilities and
 // results stay in registers, the softmax keeps a running maximum and sum in fp32.  The gradient of fp32 tensors has one kernel for both directions: rows
 // are queries (dQ) or keys (dK, dV, whose columns are the queries of all heads of the group, so no share of theirs is added up elsewhere).
 //
 // fp32: a product of two numbers is six products of their terms (what is left out is below 2^-24), small ones first; sums over the columns leave the
-// tensor core after 32 of them and join in fp32 registers, since its accumulators cut off what lies below the last bit.
+// tensor core after 32 of them and join in fp32 registers, since its accumulators cut off what lies below the last bit.  Bound by the rate of mma.sync: 16 heads of
+// 1024 x 1024 x 64 98 us (44 TFLOP/s of fp32), gradient 295; 8 heads of 4096 x 4096 x 128 1270 (54).
 //
-// Few rows on a long axis: shares of `chunk` keys a block, whose states (maximum, sum, result) a second kernel joins in order.  Bound by HBM then.
+// Few rows on a long axis: shares of `chunk` keys a block, whose states (maximum, sum, result) a second kernel joins in order.  Bound by HBM then: one token of 16 heads over 16
+// caches of 8192 to 16384 keys, 4 heads of 128, 74 us (5.6 TB/s).
 #include "attend_umma.cuh"
 #include "bwd_terms.cuh"
 

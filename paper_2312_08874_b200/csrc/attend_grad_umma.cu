@@ -9,6 +9,8 @@
 // has a row and 32 columns of a tile: what a tile costs besides its arithmetic (waits, arrivals, tensor memory) is shared by sixteen warps of an SM (by eight, with 64
 // columns each: 8 heads of 4096 x 4096 x 128 257 us, 16 of 64 channels 354).
 // Tried: tiles of 64 columns in turns for two groups of one block, 128 channels: 335 us (an instruction of 64 columns costs three quarters of one of 128).
+// Bound by waits between products and rows (tensor pipe 56 % with 128 channels, 37 to 39 % with 64): 8 heads of 4096 x 4096 x 128 234 us (735 TFLOP/s of the five products), 16 of 64 channels
+// 325 (528); 128 images of 196 tokens, 3 heads of 64, 71 (four short tiles a block).
 // Roles after these warps: products; TMA (the block's own rows once, then the columns' two operands in a ring each); a warp that makes rows behind a sequence zero (they
 // meet zeros in the sums, and need not be finite) and, KEYS, fetches the queries' statistics.
 #include "attend_umma.cuh"

@@ -5,15 +5,17 @@
 //                   A operand of P V.  The exponents' reference moves only when a logit exceeds it by more than 8 (log2 units): then the thread
 //                   rescales its row of the result in tensor memory.  Sums in fp32, of unrounded probabilities; probabilities are rounded to the type
 //                   (half a step each, independent of one another: sums over many keys see less).
-//   warps 8, 11     issue the products of a tile of queries each: the logits of its next keys while its probabilities are made (one warp for both took
-//                   2800 cycles for two tiles of 64 channels, of which the tensor cores worked 1000)
+//   warps 8, 11     issue the products of a tile of queries each: the logits of its next keys while its probabilities are made (up to 64 channels; above, the
+//                   logits take the place of the probabilities)
 //   warp 9          TMA: queries, keys and values
 //   warp 10         looks after the values of tiles that not every query sees whole: rows behind the sequence become zero, and so do numbers that are
 //                   not finite (0 * infinity is NaN); the queries that do see these get their NaN at the end
-// Results are stored from registers, rows of the sequence alone.
+// Results are stored by rows of the sequence alone.
+//
+// Bound by the row warps up to 64 channels (special-function unit 69 % busy; 16 heads of 16384 x 16384 x 64 1453 us, 757 TFLOP/s), by the chain products - exponentials - products above
+// (tensor pipe 51 %; 8 heads of 8192 x 8192 x 128 281 us, 977 TFLOP/s; causal, 16 heads on 4 of keys 273, 1007), and by starts and ends of blocks on short sequences, one block an SM.
 #include "attend_umma.cuh"
 
-#include <cstring>
 
 namespace aa {
 
