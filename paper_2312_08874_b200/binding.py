@@ -822,6 +822,7 @@ class AgentAttention:
 
         (The checks and the struct take 8 us of host time, a kernel of a small call 4; nothing here depends on an address.)
         """
+        causal, scale = bool(causal), None if scale is None else float(scale)          # (values: a tensor would be known by its identity)
         numbers = (q_offsets, k_offsets, q_lengths, k_lengths)
         key = (q.shape, q.stride(), q.dtype, q.get_device(), k.shape, k.stride(), k.dtype, k.get_device(), v.shape, v.stride(), v.dtype, v.get_device(), causal, scale)
         if q_offsets is not None or k_offsets is not None or q_lengths is not None or k_lengths is not None:

@@ -110,6 +110,21 @@ def test_refusals():
     assert a.rows == 1 << 33 and a.channels == 8                     # (which the library refuses)
 
 
+
+def test_numbers_of_a_kept_call_are_its_own():
+    """What is kept for a call's shapes follows the scale's value and not the object that holds it."""
+    h = handle()
+    h._calls = {}
+    q, k = OnDevice((1, 4, 32, 64)), OnDevice((1, 2, 32, 64))
+    h._call = pkg.AgentAttention._call.__get__(h)
+    scale, causal = torch.tensor(0.5), torch.tensor(True)
+    for value, below in ((0.5, True), (0.25, False), (0.125, True)):
+        scale.fill_(value)
+        causal.fill_(below)
+        s, _ = h._call(q, k, k, causal, scale, None, None, None, None)
+        assert s.scale == value and s.causal == int(below)
+
+
 def slots(offsets, unit, rows, most):
     """The kernels' search: which sequence and tile a slot has."""
     S = len(offsets) - 1
