@@ -801,8 +801,8 @@ class AgentAttention:
         N, M, kv = self._tokens(q), self._tokens(k), k.shape[1]
         if kv < 1 or h % kv:
             raise ValueError(f"k: expected a number of heads that divides {h}, got {kv}")
-        if scale is not None and not scale > 0:
-            raise ValueError(f"scale: expected a positive number or None, got {scale}")
+        if scale is not None and not ctypes.c_float(scale).value > 0:          # (as the library gets it, where 0 is the default)
+            raise ValueError(f"scale: expected a number that is positive in fp32, or None, got {scale}")
         if q_offsets is None and k_offsets is not None:
             raise ValueError("k_offsets belong to q_offsets")
         if q_offsets is not None and k_offsets is None:

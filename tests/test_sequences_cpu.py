@@ -125,6 +125,15 @@ def test_numbers_of_a_kept_call_are_its_own():
         assert s.scale == value and s.causal == int(below)
 
 
+def test_a_scale_that_is_zero_in_fp32_is_refused():
+    h = handle()
+    q, k = OnDevice((1, 4, 32, 64)), OnDevice((1, 2, 32, 64))
+    with pytest.raises(ValueError):
+        h._sequences(q, k, k, False, 1e-50, None, None, None, None)              # (0 means the default to the library)
+    assert h._sequences(q, k, k, False, 1e39, None, None, None, None).scale == float("inf")      # (which the library refuses)
+    assert h._sequences(q, k, k, False, 1e-30, None, None, None, None).scale > 0
+
+
 def slots(offsets, unit, rows, most):
     """The kernels' search: which sequence and tile a slot has."""
     S = len(offsets) - 1
