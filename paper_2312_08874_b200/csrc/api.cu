@@ -1043,6 +1043,7 @@ int agent_attn_layer_norm_backward(agent_attn_handle* h, const agent_attn_layer_
     if (off_elements(h, a.x) || off_elements(h, a.w) || off_elements(h, d_y) || off_elements(h, dx) || ((reinterpret_cast<uintptr_t>(d_weight) | reinterpret_cast<uintptr_t>(d_bias)) & 3u))
         return fail(h, AA_ERR_INVALID_ARG, "pointers must be aligned to their elements");
     if (dx == a.x || (dx && dx == a.w)) return fail(h, AA_ERR_INVALID_ARG, "a gradient buffer aliases an input");
+    if (d_weight && d_weight == d_bias) return fail(h, AA_ERR_INVALID_ARG, "two gradient buffers alias");
     if (d_weight || d_bias) {
         const size_t need = norm_backward_bytes(h->cfg.dtype, a.rows, a.C, h->sm_count);
         if (!workspace || need > workspace_bytes) return fail(h, AA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, need);

@@ -3,6 +3,8 @@
 Bounds, u = half a step of the type: x^ = (x - m) r carries some 8 roundings of fp32 and what cancels in x - m, 2^-22 (|x| + |m|) r; y one rounding more.
 dx: 2^-20 of r (|g| + mean |g| + |x^| mean |g x^|), the errors of x^, one rounding.  dw, db: 2^-21 of the summands' magnitudes (sums of runs).
 """
+import ctypes
+
 import pytest
 import torch
 
@@ -175,3 +177,15 @@ def test_refusals():
     for change in (dict(d_out=dy[:4]), dict(d_out=dy.float()), dict(out=x), dict(need_input_grad=False, need_weight_grads=False), dict(workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))):
         with pytest.raises((ValueError, AgentAttnError)):
             mod.layer_norm_backward(**{**dict(x=x, d_out=dy, weight=w, bias=b), **change})
+
+
+def test_gradient_buffers_that_alias_are_refused():
+    x, w, b, dy = make(8, 64, BF)
+    mod = handle(BF)
+    a, g = mod._layer_norm(x, w, b, 1e-5), torch.zeros(64, device="cuda")
+    ws = torch.empty(mod.lib.agent_attn_layer_norm_workspace_bytes(mod._h, 8, 64), dtype=torch.uint8, device="cuda")
+    args = (mod._h, ctypes.byref(a), dy.data_ptr())
+    assert mod.lib.agent_attn_layer_norm_backward(*args, None, g.data_ptr(), g.data_ptr(), ws.data_ptr(), ws.numel(), None) == 1
+    assert mod.lib.agent_attn_layer_norm_backward(*args, x.data_ptr(), g.data_ptr(), None, ws.data_ptr(), ws.numel(), None) == 1
+    torch.cuda.synchronize()
+    assert (g == 0).all()
