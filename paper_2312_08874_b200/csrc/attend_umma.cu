@@ -12,7 +12,7 @@
 //                   not finite (0 * infinity is NaN); the queries that do see these get their NaN at the end
 // Results are stored by rows of the sequence alone.
 //
-// Bound by the row warps up to 64 channels (special-function unit 69 % busy; 16 heads of 16384 x 16384 x 64 1453 us, 757 TFLOP/s), by the chain products - exponentials - products above
+// Bound by the row warps up to 64 channels (special-function unit 69 % busy; 16 heads of 16384 x 16384 x 64 1452 to 1481 us, 742 to 757 TFLOP/s), by the chain products - exponentials - products above
 // (tensor pipe 51 %; 8 heads of 8192 x 8192 x 128 281 us, 977 TFLOP/s; causal, 16 heads on 4 of keys 273, 1007), and by starts and ends of blocks on short sequences, one block an SM.
 #include "attend_umma.cuh"
 
