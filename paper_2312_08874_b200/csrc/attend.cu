@@ -479,10 +479,9 @@ template <typename T, int DK> __global__ void __launch_bounds__(32 * kFewWarps) 
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[n][e] = fast_exp2(fmaf(s[n][e], c1, -base[e >> 1]));
-                l[e >> 1] += s[n][e];
-            }
+            for (int e = 0; e < 4; ++e) s[n][e] = fast_exp2(fmaf(s[n][e], c1, -base[e >> 1]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) l[h] += (s[0][2 * h] + s[0][2 * h + 1]) + (s[1][2 * h] + s[1][2 * h + 1]);
         const uint32_t p[4] = {pack2<T>(s[0][0], s[0][1]), pack2<T>(s[0][2], s[0][3]), pack2<T>(s[1][0], s[1][1]), pack2<T>(s[1][2], s[1][3])};
 #pragma unroll
         for (int i = 0; i < VI; ++i) {
@@ -631,7 +630,7 @@ int shares_of(const AttendArgs& a, bool few_16, int sm_count, int* chunk) {
     // of keys of 128: 2 an SM 79 us, 4 86, 6 92, 12 97; 8 heads of 64 over 8192: 2 an SM 51, 3 45, 4 48, 8 51; one cache of 65536, 8 heads of 128: 47, 50, 61, 73.
     const long long want = std::max(1LL, (a.d <= 64 && few_16 ? 3LL : 2LL) * sm_count / blocks);
     long long c = (a.M + want - 1) / want;
-    c = std::max(256LL, (c + 127) / 128 * 128);
+    c = std::min(std::max(256LL, (c + 127) / 128 * 128), 4LL * kPieceKeys);      // (four warps take a piece each, see kPieceKeys)
     *chunk = (int)std::min<long long>(c, a.M);
     return (a.M + *chunk - 1) / *chunk;
 }

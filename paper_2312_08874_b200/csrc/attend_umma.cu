@@ -3,7 +3,7 @@
 // A block takes two tiles of 128 queries of a head and walks the keys in tiles of 128 that both share.  Roles:
 //   warps 0-3, 4-7  a tile each: thread = query.  Logits come out of tensor memory into registers, 128 at a time; probabilities go back to tensor memory as the
 //                   A operand of P V.  The exponents' reference moves only when a logit exceeds it by more than 8 (log2 units): then the thread
-//                   rescales its row of the result in tensor memory.  Sums in fp32, of unrounded probabilities; probabilities are rounded to the type
+//                   rescales its row of the result in tensor memory.  Sums over long axes come in pieces (kPieceKeys).  Sums in fp32, of unrounded probabilities; probabilities are rounded to the type
 //                   (half a step each, independent of one another: sums over many keys see less).
 //   warps 8, 11     issue the products of a tile of queries each: the logits of its next keys while its probabilities are made (up to 64 channels; above, the
 //                   logits take the place of the probabilities)
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             wait_spin(pp, G::BAR_VREADY + s, j / kStages, kAttendTimeout);
             wait_spin(pp, G::BAR_P + w, j, kAttendTimeout);
             tc_fence_after_sync();
-            mma_sum<BOXES, kTileRows, kTileRows>(elected, pp.tmem + G::TM_O + w * G::kO, tp, base + G::OFF_V + s * G::kOperand, id_o, j > 0);
+            mma_sum<BOXES, kTileRows, kTileRows>(elected, pp.tmem + G::TM_O + w * G::kO, tp, base + G::OFF_V + s * G::kOperand, id_o, j % (kPieceKeys / kTileRows) != 0);
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_O + w));
             umma_commit_e<false>(elected, pipe_bar(pp, G::BAR_VFREE + s));
             if (BOXES == 2 && j + 1 < n[w]) {
@@ -220,7 +220,26 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
         const float c1 = a.scale * kLog2e;
         float ref = -INFINITY;
         float2 sum[2] = {};
+        // a long axis: sums of the pieces so far, relative to `kept_ref` (in local memory: 512 bytes at most, touched once a piece)
+        volatile float kept[64 * BOXES];
+        float kept_sum = 0.f, kept_ref = -INFINITY;
         for (int j = 0; j < n[w]; ++j) {
+            if (j > 0 && j % (kPieceKeys / kTileRows) == 0) {
+                wait_soon(pp, G::BAR_O + w, j - 1);
+                tc_fence_after_sync();
+                const float f = kept_ref == ref ? 1.f : fast_exp2(kept_ref - ref);       // (no visible key so far: -inf both)
+                kept_ref = ref;
+                kept_sum = fmaf(kept_sum, f, (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
+                sum[0] = sum[1] = make_float2(0.f, 0.f);
+#pragma unroll 1
+                for (int h = 0; h < 2 * BOXES; ++h) {
+                    uint32_t o[32];
+                    tmem_ld32(to + 32 * h, o);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) kept[32 * h + i] = j == kPieceKeys / kTileRows ? __uint_as_float(o[i]) : fmaf(kept[32 * h + i], f, __uint_as_float(o[i]));
+                }
+            }
             wait_soon(pp, G::BAR_S + w, j);
             tc_fence_after_sync();
             uint32_t o[4][32];
@@ -272,7 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             uint32_t p[4][16];
             if ((w == 0 ? j > 0 && j <= n[1] : j < n[0])) bar_sync_pair(1 + (warp & 3) + 4 * w);
             // groups of eight pairs: exponentials of one, sums and roundings of the one before
-            float2 v[2][8];
+            float2 v[2][8], part_sum[2];                                         // (a tile's own sum: 128 keys more on a long one would lose their last bits)
 #pragma unroll
             for (int g = 0; g <= 8; ++g) {
                 if (g < 8) {
@@ -287,12 +306,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
                     const int k = g - 1;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        sum[i & 1] = fadd2(sum[i & 1], v[k & 1][i]);
+                        part_sum[i & 1] = k == 0 && i < 2 ? v[0][i] : fadd2(part_sum[i & 1], v[k & 1][i]);
                         p[k >> 1][8 * (k & 1) + i] = pack2<T>(v[k & 1][i].x, v[k & 1][i].y);
                     }
                     if (BOXES == 2 && (k & 1)) tmem_st16(tp + 8 * (k - 1), p[k >> 1]);
                 }
             }
+            sum[0] = fadd2(sum[0], part_sum[0]);
+            sum[1] = fadd2(sum[1], part_sum[1]);
             if (BOXES == 1) {
                 if (j > 0) {                                                     // P V of the keys before has read its probabilities
                     wait_soon(pp, G::BAR_O + w, j - 1);
@@ -311,7 +332,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
             wait_soon(pp, G::BAR_MENDED, 0);
             tc_fence_after_sync();
         }
-        const float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y), inv = limit > 0 ? 1.f / total : 0.f;
+        const bool pieces = n[w] > kPieceKeys / kTileRows;
+        const float before = kept_ref == ref ? 1.f : fast_exp2(kept_ref - ref);
+        const float total = fmaf(kept_sum, pieces ? before : 0.f, (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y)), inv = limit > 0 ? 1.f / total : 0.f;
         T* out = static_cast<T*>(a.out) + q.batch * a.lo.sb + head * a.lo.sh + (long long)(q.first + q0 + w * kTileRows + 32 * (warp & 3)) * a.lo.st;      // the warp's first row
         // Through the queries' place in shared memory, which nothing reads any more (rows 16 bytes a lane took 2900 cycles for 64 channels), a box at a time; a tile without
         // keys has loads of its queries in flight, maybe, but only zeros to store.
@@ -324,6 +347,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
                     uint32_t o[32];
                     tmem_ld32(to + 64 * b + 32 * h, o);
                     tmem_ld_wait();
+                    if (pieces)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(fmaf(kept[64 * b + 32 * h + i], before, __uint_as_float(o[i])));
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         float f[8];

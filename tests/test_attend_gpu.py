@@ -465,3 +465,44 @@ def test_refusals():
     with pytest.raises(AgentAttnError) as e:
         few.attend(q[:, :, :1].contiguous(), k2, k2.clone(), workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 3
+
+
+@pytest.mark.parametrize("dt", [BF, FH])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("N,M,d", [(64, (1 << 20) + 77, 64), (300, (1 << 20) + 77, 128), (300, (1 << 23) + 1, 64), (129, 16384 + 129, 64), (257, 32768, 128)])
+def test_sums_over_long_axes(dt, causal, N, M, d):
+    """Values of one and probabilities of all sizes: the result is one.  u of it and of the probabilities, 2^-14 of the tensor cores' sums (1024 steps of 2^-24), and of
+    the sums in fp32 (32 of a tile, 128 tiles of a piece, the pieces) 2^-24 each, which the log-sum-exp has, too, with 2^-21 of exponentials and logarithm."""
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    q, k, v = torch.zeros((1, 1, N, d), device="cuda"), torch.zeros((1, 1, M, d), device="cuda"), torch.ones((1, 1, M, d), device="cuda")
+    q[..., 0] = 1.0
+    k[..., 0] = torch.randn(M, generator=gen, device="cuda") + torch.linspace(-3, 3, M, device="cuda")       # (the largest logit moves from piece to piece)
+    q, k, v = q.to(dt), k.to(dt), v.to(dt)
+    mod = AgentAttention(1, 1, d, M, 1, dt)
+    out, lse = mod.attend(q, k, v, causal=causal, scale=1.0, need_lse=True)
+    s = k[0, 0, :, 0].double()
+    want = torch.stack([torch.logsumexp(s[:M - N + i + 1] if causal else s, 0) for i in range(N)]) if causal else torch.logsumexp(s, 0).expand(N)
+    sums = 2.0 ** -24 * (32 + 128 + M / 16384)
+    assert (out.double() - 1).abs().max() <= 2 * u_of(dt) + 2.0 ** -14 + sums, float((out.double() - 1).abs().max())
+    assert ((lse[0, 0].double() - want).abs() <= sums + 2.0 ** -21 + 2.0 ** -23 * want.abs()).all(), float((lse[0, 0].double() - want).abs().max())
+    assert mod.query_status() == 0
+
+
+@pytest.mark.parametrize("dt", [BF, FH])
+def test_single_queries_over_many_long_caches(dt):
+    """Caches that fill the GPU without shares of their keys (windows of one buffer): sums of 2^22 keys come in pieces all the same.  Bounds as above."""
+    B, kv, M, d = 150, 2, (1 << 22) + 5, 64
+    rows = torch.ones((M + 3 * B, d), device="cuda")
+    rows[:, 0] = torch.randn(M + 3 * B, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    k = rows.to(dt).as_strided((B, kv, M, d), (2 * d, d, d, 1))
+    v = torch.ones((M + 3 * B, d), dtype=dt, device="cuda").as_strided((B, kv, M, d), (2 * d, d, d, 1))
+    q = torch.zeros((B, 2, 1, d), dtype=dt, device="cuda")
+    q[..., 0] = 1.0
+    mod = AgentAttention(B, 2, d, M, 1, dt)
+    out, lse = mod.attend(q, k, v, scale=1.0, need_lse=True)
+    sums = 2.0 ** -24 * (1024 + 64 + M / 65536)
+    assert (out.double() - 1).abs().max() <= 2 * u_of(dt) + 2.0 ** -14 + sums, float((out.double() - 1).abs().max())
+    for b in (0, 77, 149):
+        want = torch.stack([torch.logsumexp(k[b, h, :, 0].double(), 0) for h in range(2)])
+        assert ((lse[b, :, 0].double() - want).abs() <= sums + 2.0 ** -21 + 2.0 ** -23 * want.abs()).all()
+    assert mod.query_status() == 0
