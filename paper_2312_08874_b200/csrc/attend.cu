@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
 //   logits   lane (g, t) takes the channels 32 i + 8 t .. + 7 of key g: two steps of the product's sum, whose channels may come in any order if the queries' do so, too
 //   P V      lane (g, t) takes the channels 8 g .. 8 g + 7 of the keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9; byte permutes make the pairs of keys that the product wants,
 //            and column n of its tile i is channel 8 n + i
-// The exponents' reference moves only when a logit exceeds it by more than 8 (log2 units).
+// The exponents' reference moves only when a logit exceeds it by more than kSlack.
 constexpr int kFewWarps = 4, kFewStages = 3, kFewKeys = 16;
 struct FewArgs {
     AttendArgs a;
@@ -456,13 +456,13 @@ template <typename T, int DK> __global__ void __launch_bounds__(32 * kFewWarps) 
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             m[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1])) * c1;
-            grow |= m[h] > ref[h] + 8.f;
+            grow |= m[h] > ref[h] + kSlack<T>;
         }
         if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float top = quad_max(m[h]);
-                if (!(top > ref[h] + 8.f)) continue;                    // (the same of a row's four lanes; no shuffles below)
+                if (!(top > ref[h] + kSlack<T>)) continue;                 // (the same of a row's four lanes; no shuffles below)
                 const float f = fast_exp2(ref[h] - top);                // (0 of a row without a key so far)
                 ref[h] = top;
                 l[h] *= f;
@@ -475,7 +475,7 @@ template <typename T, int DK> __global__ void __launch_bounds__(32 * kFewWarps) 
                     }
             }
         }
-        const float base[2] = {ref[0] == -INFINITY ? 0.f : ref[0], ref[1] == -INFINITY ? 0.f : ref[1]};
+        const float base[2] = {ref[0] == -INFINITY ? 0.f : ref[0] - kHeld<T>, ref[1] == -INFINITY ? 0.f : ref[1] - kHeld<T>};
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -530,7 +530,7 @@ template <typename T, int DK> __global__ void __launch_bounds__(32 * kFewWarps) 
                 d[1] = make_float4(o[i][4][2 * h + e], o[i][5][2 * h + e], o[i][6][2 * h + e], o[i][7][2 * h + e]);
             }
         if (t == 0) {
-            to[DK] = ref[h];
+            to[DK] = ref[h] - kHeld<T>;            // (what the exponents are relative to)
             to[DK + 1] = l[h];
         }
     }

@@ -64,10 +64,16 @@ constexpr int kPieceKeys = 16384;
 
 constexpr float kLn2 = 0.6931471805599453f;
 
+// The exponents' reference of a row moves only when a logit exceeds it by more than kSlack (log2 units), so P is at most 2^kSlack.  f16, whose normal numbers end at
+// 2^-14 and whose last one is 2^-24, holds P times 2^kHeld, as much as its range leaves: keys far below a row's largest lose nothing before 2^-25 of it, and half a
+// step of the last number is 2^-36 (the sum counts what P V would lose: 65536 keys 17.5 below one, 1.6e-3 of the result).  The factor leaves with the row's sum.
+template <typename T> constexpr bool is_f16 = sizeof(T) == 2 && !Elem<T>::kIsBf16;
+template <typename T> constexpr float kSlack = is_f16<T> ? 4.f : 8.f;
+template <typename T> constexpr float kHeld = is_f16<T> ? 11.f : 0.f;
+
 // f16 gradients.  P and dS are operands of products and have to be f16, whose normal numbers end at 2^-14: P is held times 2^15 (it is at most one), dS times the
 // power of two that brings the bound 2 |dO_i| max |v_j| of |dP - D| into [2^14, 2^15): of the row where rows are queries, of the sequence's largest row
 // where the sum goes over them.  The results are brought back in fp32.
-template <typename T> constexpr bool is_f16 = sizeof(T) == 2 && !Elem<T>::kIsBf16;
 constexpr float kHeldP = 15.f, kHeldBack = 1.f / 32768.f;
 constexpr int kDotRows = 64;
 __host__ __device__ inline float* grad_norms(const AttendArgs& a) { return a.ws + 2 * (long long)a.batch * a.heads * a.N; }

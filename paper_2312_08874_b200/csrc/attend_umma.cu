@@ -2,7 +2,7 @@
 //
 // A block takes two tiles of 128 queries of a head and walks the keys in tiles of 128 that both share.  Roles:
 //   warps 0-3, 4-7  a tile each: thread = query.  Logits come out of tensor memory into registers, 128 at a time; probabilities go back to tensor memory as the
-//                   A operand of P V.  The exponents' reference moves only when a logit exceeds it by more than 8 (log2 units): then the thread
+//                   A operand of P V.  The exponents' reference moves only when a logit exceeds it by more than kSlack: then the thread
 //                   rescales its row of the result in tensor memory.  Sums over long axes come in pieces (kPieceKeys).  Sums in fp32, of unrounded probabilities; probabilities are rounded to the type
 //                   (half a step each, independent of one another: sums over many keys see less).
 //   warps 8, 11     issue the products of a tile of queries each: the logits of its next keys while its probabilities are made (up to 64 channels; above, the
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
 #pragma unroll
             for (int i = 4; i < 64; ++i) top[i & 3] = max3_nan(top[i & 3], x[i].x, x[i].y);
             const float m = max_nan(max3_nan(top[0], top[1], top[2]), top[3]) * c1;
-            const bool grow = !(m <= ref + 8.f);                                 // (a NaN makes its row NaN)
+            const bool grow = !(m <= ref + kSlack<T>);                                // (a NaN makes its row NaN)
             if (__any_sync(0xffffffffu, grow)) {
                 const float next = grow ? m : ref, f = grow ? fast_exp2(ref - next) : 1.f;      // (exp2(-inf) = 0)
                 ref = next;
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
                     }
                 }
             }
-            const float nr = ref == -INFINITY ? 0.f : -ref;
+            const float nr = ref == -INFINITY ? 0.f : kHeld<T> - ref;
             uint32_t p[4][16];
             if ((w == 0 ? j > 0 && j <= n[1] : j < n[0])) bar_sync_pair(1 + (warp & 3) + 4 * w);
             // groups of eight pairs: exponentials of one, sums and roundings of the one before
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_umma_kernel(const __grid_c
                         n[w] ? *reinterpret_cast<const uint4*>(stage + r * 128 + ((chunk ^ (r & 7)) << 4)) : make_uint4(0u, 0u, 0u, 0u);
             }
         }
-        if (live && a.lse) a.lse[((long long)q.batch * a.heads + head) * a.N + q.first + token] = limit > 0 ? (ref + log2f(total)) * kLn2 : -INFINITY;
+        if (live && a.lse) a.lse[((long long)q.batch * a.heads + head) * a.N + q.first + token] = limit > 0 ? (ref - kHeld<T> + log2f(total)) * kLn2 : -INFINITY;
         tc_fence_before_sync();
     }
     __syncthreads();

@@ -506,3 +506,27 @@ def test_single_queries_over_many_long_caches(dt):
         want = torch.stack([torch.logsumexp(k[b, h, :, 0].double(), 0) for h in range(2)])
         assert ((lse[b, :, 0].double() - want).abs() <= sums + 2.0 ** -21 + 2.0 ** -23 * want.abs()).all()
     assert mod.query_status() == 0
+
+
+def rows_over_one_strong_key(N, M, below, dt, d=64, first=0):
+    """Queries whose logit is 0 at one key and -below at the others; constant values (the result is 1), and a channel of the strong key alone."""
+    q, k, v = torch.zeros((1, 1, N, d)), torch.zeros((1, 1, M, d)), torch.ones((1, 1, M, d))
+    q[..., 0], k[..., 0] = 1.0, -below
+    k[..., first, 0] = 0.0
+    v[..., 1] = 0.0
+    v[..., first, 1] = 1.0
+    return tuple(t.to("cuda", dt) for t in (q, k, v))
+
+
+@pytest.mark.parametrize("dt", [FH, BF])
+@pytest.mark.parametrize("N,d", [(1, 64), (32, 64), (300, 64), (300, 128)])
+def test_many_keys_far_below_one(dt, N, d):
+    """65535 keys 16 to 18 below one: 2e-3 of the result, each of them below f16's normal numbers, or its last one; and 2^20 keys 19 to 21 below one.  Bound as above: u of
+    the result, u of the probabilities, 2^-14 of the tensor cores' sums."""
+    for below in (16.0, 17.0, 17.5, 18.0):
+        check(*rows_over_one_strong_key(N, 65536, below, dt, d), scale=1.0, grad=False, what=below)
+    for below in (19.0, 20.0, 21.0):
+        q, k, v = rows_over_one_strong_key(N, 1 << 20, below, dt, d)
+        got = AgentAttention(1, 1, d, 1 << 20, 1, dt).attend(q, k, v, scale=1.0).double()
+        want = torch.softmax(k[0, 0, :, 0].double(), 0) @ v[0, 0].double()
+        assert ((got - want).abs() <= (2 * u_of(dt) + 2.0 ** -14) * want).all(), (below, float((got / want - 1).abs().max()))
