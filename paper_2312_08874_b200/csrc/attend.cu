@@ -6,8 +6,9 @@
 // are queries (dQ) or keys (dK, dV, whose columns are the queries of all heads of the group, so no share of theirs is added up elsewhere).
 //
 // fp32: a product of two numbers is six products of their terms (what is left out is below 2^-24), small ones first; sums over the columns leave the
-// tensor core after 32 of them and join in fp32 registers, since its accumulators cut off what lies below the last bit.  Bound by the rate of mma.sync: 16 heads of
-// 1024 x 1024 x 64 98 us (44 TFLOP/s of fp32), gradient 295; 8 heads of 4096 x 4096 x 128 1270 (54).
+// tensor core after 32 of them and join in fp32 registers, since its accumulators cut off what lies below the last bit, and in pieces of kPieceBlocks such blocks, since a
+// sum of thousands loses bits in fp32, too.  Bound by the rate of mma.sync: 16 heads of
+// 1024 x 1024 x 64 100 us (43 TFLOP/s of fp32), gradient 295; 8 heads of 4096 x 4096 x 128 1278 (54).
 //
 // Few rows on a long axis: shares of `chunk` keys a block, whose states (maximum, sum, result) a second kernel joins in order.  Bound by HBM then: one token of 16 heads over 16
 // caches of 8192 to 16384 keys, 4 heads of 128, 74 us (5.6 TB/s).
@@ -147,6 +148,10 @@ template <typename E, int NT, int DK, int THREADS> __device__ void clean_values(
     }
 }
 
+// Blocks of 32 columns that a sum in fp32 takes before it joins the others: equal numbers on a growing sum are rounded the same way each time, up to 2^-25 of it (65536 keys of
+// 2^-35 of one: result and log-sum-exp off by 1.4e-4 without pieces, 2^20 by 2e-3).
+constexpr int kPieceBlocks = 128;
+
 // ------------------------------------------------------------------------------------------------ forward
 template <int DK, int WR, int WK> struct RowsGeom {
     static constexpr int NT = 3, kRows = 16 * WR, kStep = 32 * WK, kThreads = 32 * WR * WK, kPitch = TileGeom<DK>::kPitch;
@@ -256,9 +261,31 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
     __syncthreads();                               // (the queries, and first_bad)
     const uint32_t qa = smem_u32(smem) + wr * 16 * P + val_lane_offset<DK>(lane);
 
+    // a long axis: sums of the pieces so far, relative to kept_m (in local memory, touched once a piece)
+    volatile float kept[DK / 8][4];
+    float kept_m[2] = {-INFINITY, -INFINITY}, kept_l[2] = {0.f, 0.f};
+    int pieces = 0;
     for (int s = 0; s < steps; ++s) {
         const int k0 = begin + s * G::kStep + (WK > 1 ? wk * 32 : 0);
         if (k0 >= end) break;                      // (of a warp with its own keys)
+        if (s && s % kPieceBlocks == 0) {
+            float f[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f[h] = kept_m[h] == m[h] ? 1.f : fast_exp2(kept_m[h] - m[h]);          // (no visible key so far: -inf both)
+                kept_m[h] = m[h];
+                kept_l[h] = fmaf(kept_l[h], f[h], l[h]);
+                l[h] = 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < DK / 8; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    kept[c][e] = pieces ? fmaf(kept[c][e], f[e >> 1], o[c][e]) : o[c][e];
+                    o[c][e] = 0.f;
+                }
+            ++pieces;
+        }
         if (s) meet();
         load_tile<DK, LOADERS, OWN>(me, mine, G::kPlane, a.d, [&](int r) -> const T* { return k0 + r < end ? kp + (long long)(k0 + r) * a.lk.st : nullptr; });
         load_tile<DK, LOADERS, OWN>(me, mine + NT * G::kPlane, G::kPlane, a.d, [&](int r) -> const T* { return k0 + r < end ? vp + (long long)(k0 + r) * a.lv.st : nullptr; });
@@ -287,15 +314,18 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
             base[h] = n == -INFINITY ? 0.f : n;                          // (no visible key so far)
             f[h] = m[h] == -INFINITY ? 0.f : fast_exp2(m[h] - base[h]);
             m[h] = n;
-            l[h] *= f[h];
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[j][e] = fast_exp2(fmaf(x[j][e], c1, -base[e >> 1]));
-                l[e >> 1] += x[j][e];
-            }
+            for (int e = 0; e < 4; ++e) x[j][e] = fast_exp2(fmaf(x[j][e], c1, -base[e >> 1]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {              // (the block's own sum first: eight small numbers on a long one would lose their last bits)
+            float t = x[0][2 * h] + x[0][2 * h + 1];
+#pragma unroll
+            for (int j = 1; j < 4; ++j) t += x[j][2 * h] + x[j][2 * h + 1];
+            l[h] = fmaf(l[h], f[h], t);
+        }
 #pragma unroll
         for (int c = 0; c < DK / 8; ++c)
 #pragma unroll
@@ -303,6 +333,18 @@ __global__ void __launch_bounds__(32 * WR * WK) attend_rows_kernel(const __grid_
         uint32_t p[NT][2][4];
         block_operand<E, NT>(x, p);
         block_product<E, NT, DK>(o, p, kb + NT * G::kPlane + val_lane_offset<DK>(lane), G::kPlane);
+    }
+    if (pieces) {
+        float f[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f[h] = kept_m[h] == m[h] ? 1.f : fast_exp2(kept_m[h] - m[h]);
+            l[h] = fmaf(kept_l[h], f[h], l[h]);
+        }
+#pragma unroll
+        for (int c = 0; c < DK / 8; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][e] = fmaf(kept[c][e], f[e >> 1], o[c][e]);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) l[h] = quad_sum(l[h]);

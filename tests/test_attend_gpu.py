@@ -530,3 +530,17 @@ def test_many_keys_far_below_one(dt, N, d):
         got = AgentAttention(1, 1, d, 1 << 20, 1, dt).attend(q, k, v, scale=1.0).double()
         want = torch.softmax(k[0, 0, :, 0].double(), 0) @ v[0, 0].double()
         assert ((got - want).abs() <= (2 * u_of(dt) + 2.0 ** -14) * want).all(), (below, float((got / want - 1).abs().max()))
+
+
+@pytest.mark.parametrize("N,M,below", [(1, 65536, 17.0), (64, 65536, 17.0), (300, 65536, 24.0), (2000, 20000, 12.0), (64, 1 << 20, 17.0), (300, (1 << 20) + 77, 20.0), (1, 1 << 23, 17.0)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_sums_in_fp32(N, M, below, d):
+    """Equal probabilities beside a large one: their sums are rounded the same way at every step.  2^-24 for each of a piece's 128 steps and of the pieces, twice (the
+    result's sum and the probabilities'), 2^-21 of exponentials."""
+    q, k, v = rows_over_one_strong_key(N, M, below, F32, d)
+    mod = AgentAttention(1, 1, d, M, 1, F32)
+    out, lse = mod.attend(q, k, v, scale=1.0, need_lse=True)
+    s = k[0, 0, :, 0].double()
+    want, sums = torch.softmax(s, 0) @ v[0, 0].double(), 2.0 ** -24 * (8 + 128 + M / 4096)
+    assert ((out.double() - want).abs() <= (2 * sums + 2.0 ** -21) * want).all(), float((out.double() / want - 1).abs().max())
+    assert (lse.double() - torch.logsumexp(s, 0)).abs().max() <= sums + 2.0 ** -21
