@@ -544,3 +544,58 @@ def test_long_sums_in_fp32(N, M, below, d):
     want, sums = torch.softmax(s, 0) @ v[0, 0].double(), 2.0 ** -24 * (8 + 128 + M / 4096)
     assert ((out.double() - want).abs() <= (2 * sums + 2.0 ** -21) * want).all(), float((out.double() / want - 1).abs().max())
     assert (lse.double() - torch.logsumexp(s, 0)).abs().max() <= sums + 2.0 ** -21
+
+
+@pytest.mark.parametrize("dt", [FH, BF])
+@pytest.mark.parametrize("h,N,M,d", [(1, (1 << 20) + 77, 130, 64), (2, 1 << 19, 70, 128), (4, 16384 + 5, 130, 64)])
+def test_gradient_sums_over_many_queries(dt, h, N, M, d):
+    """Gradients of keys and values that all queries add to with one sign.  Bound: u of the result, of P and of dS, u of a rounded result in D, 2^-14 of the tensor cores'
+    sums and 2^-20 of a probability."""
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    q, k, v, do = torch.zeros((1, h, N, d), device="cuda"), torch.zeros((1, 1, M, d), device="cuda"), torch.zeros((1, 1, M, d), device="cuda"), torch.zeros((1, h, N, d), device="cuda")
+    q[..., 0], k[..., 0] = rand(h, N), rand(M)
+    q[..., 1] = do[..., 1] = torch.where(rand(h, N) > 0, 1.0, -1.0)
+    v[..., 1], do[..., 2] = rand(M), 1.0
+    q, k, v, do = (t.to(dt) for t in (q, k, v, do))
+    mod = AgentAttention(1, h, d, N, 1, dt)
+    out, lse = mod.attend(q, k, v, scale=1.0, need_lse=True)
+    g = mod.attend_backward(q, k, v, out, lse, do, scale=1.0)
+    want = torch.zeros((4, M), dtype=torch.float64, device="cuda")         # dV, dK and what dK's errors are made of
+    for i in range(h):
+        for r in range(0, N, 1 << 17):
+            p = torch.softmax(q[0, i, r:r + (1 << 17), :1].double() * k[0, 0, :, 0].double(), -1)
+            mean = p @ v[0, 0, :, 1].double()
+            slope = p * (v[0, 0, :, 1].double() - mean[:, None])
+            want += torch.stack([p.sum(0), slope.sum(0), slope.abs().sum(0), (p * mean[:, None].abs()).sum(0)])
+    u, e = u_of(dt), 2.0 ** -14 + 2.0 ** -20
+    rel = (g["dv"][0, 0, :, 2].double() - want[0]).abs() / want[0]
+    assert rel.max() <= 2 * u + e, float(rel.max())
+    rel = (g["dk"][0, 0, :, 1].double() - want[1]).abs() / (want[1].abs() * u + want[2] * (u + e) + want[3] * (u + e))
+    assert rel.max() <= 1, float(rel.max())
+    assert mod.query_status() == 0
+
+
+@pytest.mark.parametrize("dt", [FH, BF])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("N,M,d", [(130, (1 << 20) + 77, 64), (70, (1 << 19) + 1, 128), (200, 16384 + 1, 64), (1, 1 << 20, 128)])
+def test_gradient_sums_over_many_keys(dt, causal, N, M, d):
+    """Gradients of queries that all keys add to with one sign: dQ = sum P (1 - D k).  Bounds as above."""
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    q, k, v, do = torch.zeros((1, 1, N, d), device="cuda"), torch.zeros((1, 1, M, d), device="cuda"), torch.zeros((1, 1, M, d), device="cuda"), torch.zeros((1, 1, N, d), device="cuda")
+    q[..., 0], k[..., 0] = 1.0, torch.randn(M, generator=gen, device="cuda")
+    k[..., 1] = v[..., 1] = torch.where(torch.randn(M, generator=gen, device="cuda") > 0, 1.0, -1.0)
+    do[..., 1] = 1.0
+    q, k, v, do = (t.to(dt) for t in (q, k, v, do))
+    mod = AgentAttention(1, 1, d, M, 1, dt)
+    out, lse = mod.attend(q, k, v, causal=causal, scale=1.0, need_lse=True)
+    g = mod.attend_backward(q, k, v, out, lse, do, causal=causal, scale=1.0)
+    s, sign = k[0, 0, :, 0].double(), k[0, 0, :, 1].double()
+    for i in {0, N // 2, N - 1}:
+        m = M - N + i + 1 if causal else M
+        p = torch.softmax(s[:m], 0)
+        mean = p @ sign[:m]
+        want = p @ (sign[:m] * (sign[:m] - mean))
+        err = float((g["dq"][0, 0, i, 1].double() - want).abs())
+        assert err <= u_of(dt) * (want.abs() + 1 + 2 * mean.abs()) + (2.0 ** -14 + 2.0 ** -20) * (1 + mean.abs()), (i, err)
+    assert mod.query_status() == 0
