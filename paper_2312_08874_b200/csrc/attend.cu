@@ -740,7 +740,8 @@ template <int DK> struct GradGeom {
 };
 
 // KEYS: rows are keys (x = K, y = V), columns queries (u = Q, w = dO); else rows are queries (x = Q, y = dO), columns keys (u = K, w = V).
-template <int DK, bool KEYS>
+// LONG: sums may be longer than a piece (the others do without its registers: 8 heads of 4096 x 4096 x 128 6.04 ms with them, 5.74 without).
+template <int DK, bool KEYS, bool LONG>
 __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant__ AttendArgs a) {
     using T = float;
     using G = GradGeom<DK>;
@@ -797,8 +798,27 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
     const uint32_t xa = smem_u32(xs) + warp * 16 * P + val_lane_offset<DK>(lane), ya = xa + (uint32_t)(ys - xs);
     const uint32_t ub = smem_u32(us) + key_lane_offset<DK>(lane), wb = ub + (uint32_t)(ws - us);
     const uint32_t ut = smem_u32(us) + val_lane_offset<DK>(lane), wt = ut + (uint32_t)(ws - us);
+    volatile float kept[LONG ? (KEYS ? 2 : 1) * DK / 8 : 1][4];    // of a long sum the pieces so far (in local memory, touched once a piece)
+    int pieces = 0, blocks = 0;
     for (int c0 = begin; c0 < end; c0 += G::kStep) {
         if (c0 != begin) __syncthreads();
+        if constexpr (LONG) {
+            if (blocks++ == kPieceBlocks) {
+                blocks = 1;
+#pragma unroll
+                for (int c = 0; c < DK / 8; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        kept[c][e] = pieces ? kept[c][e] + acc[c][e] : acc[c][e];
+                        acc[c][e] = 0.f;
+                        if constexpr (KEYS) {
+                            kept[DK / 8 + c][e] = pieces ? kept[DK / 8 + c][e] + acc2[c][e] : acc2[c][e];
+                            acc2[c][e] = 0.f;
+                        }
+                    }
+                ++pieces;
+            }
+        }
         load_tile<DK, 128, G::kStep>(tid, us, G::kPlane, a.d, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.q, a.lq, c0 + r) : key(a.k, a.lk, c0 + r)) : nullptr; });
         load_tile<DK, 128, G::kStep>(tid, ws, G::kPlane, a.d, [&](int r) -> const T* { return c0 + r < end ? (KEYS ? query(a.dout, a.ldo, c0 + r) : key(a.v, a.lv, c0 + r)) : nullptr; });
         if (KEYS && tid < G::kStep) stats[tid] = c0 + tid < end ? stat(c0 + tid) : make_float2(0.f, 0.f);
@@ -826,6 +846,17 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
             block_product<E, NT, DK>(acc2, w, wt, G::kPlane);
         }
     }
+    if constexpr (LONG) {
+        if (pieces) {
+#pragma unroll
+            for (int c = 0; c < DK / 8; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    acc[c][e] += kept[c][e];
+                    if constexpr (KEYS) acc2[c][e] += kept[DK / 8 + c][e];
+                }
+        }
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         if (row[h] >= rows) continue;
@@ -842,13 +873,17 @@ __global__ void __launch_bounds__(128) attend_grad_kernel(const __grid_constant_
     }
 }
 
-template <int DK, bool KEYS> cudaError_t run_grad(const AttendArgs& a, cudaStream_t st) {
+template <int DK, bool KEYS, bool LONG> cudaError_t run_grad_form(const AttendArgs& a, cudaStream_t st) {
     using G = GradGeom<DK>;
     static std::atomic<unsigned long long> done{0};
-    if (cudaError_t e = allow_smem(attend_grad_kernel<DK, KEYS>, done, G::kSmem)) return e;
+    if (cudaError_t e = allow_smem(attend_grad_kernel<DK, KEYS, LONG>, done, G::kSmem)) return e;
     const long long slots = KEYS ? slots_of(a.k_offsets != nullptr, a.sequences, a.M, 1, G::kRows) : slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, G::kRows);
-    attend_grad_kernel<DK, KEYS><<<dim3((unsigned)slots, a.kv_heads), 128, G::kSmem, st>>>(a);
+    attend_grad_kernel<DK, KEYS, LONG><<<dim3((unsigned)slots, a.kv_heads), 128, G::kSmem, st>>>(a);
     return cudaGetLastError();
+}
+template <int DK, bool KEYS> cudaError_t run_grad(const AttendArgs& a, cudaStream_t st) {
+    const long long columns = KEYS ? (long long)a.N * (a.heads / a.kv_heads) : a.M;        // (of packed sequences the longest may have all rows)
+    return columns > 32LL * kPieceBlocks ? run_grad_form<DK, KEYS, true>(a, st) : run_grad_form<DK, KEYS, false>(a, st);
 }
 template <int DK> cudaError_t run_grads(const AttendArgs& a, cudaStream_t st) {
     if (cudaError_t e = run_grad<DK, true>(a, st)) return e;

@@ -599,3 +599,25 @@ def test_gradient_sums_over_many_keys(dt, causal, N, M, d):
         err = float((g["dq"][0, 0, i, 1].double() - want).abs())
         assert err <= u_of(dt) * (want.abs() + 1 + 2 * mean.abs()) + (2.0 ** -14 + 2.0 ** -20) * (1 + mean.abs()), (i, err)
     assert mod.query_status() == 0
+
+
+@pytest.mark.parametrize("h,N,M,d", [(1, 1 << 18, 70, 64), (2, 1 << 17, 33, 128), (4, 16384, 64, 32), (1, 70, 1 << 18, 64), (2, 33, 1 << 17, 128), (1, 1 << 16, 64, 96)])
+def test_gradient_long_sums_in_fp32(h, N, M, d):
+    """Equal summands, which are rounded the same way at every step: P = 1 / M, dO = 0.7, so dV = 0.7 N h / M; dK and dQ of slopes that are one number.  2^-24 for each of a
+    piece's 128 steps of 32 columns and of the pieces, 2^-20 of probabilities, slopes and products."""
+    q, k = torch.zeros((1, h, N, d), device="cuda"), torch.zeros((1, 1, M, d), device="cuda")
+    v, do = torch.zeros((1, 1, M, d), device="cuda"), torch.zeros((1, h, N, d), device="cuda")
+    q[..., 1], do[..., 1], do[..., 2] = 0.3, 0.9, 0.7
+    sign = torch.where(torch.arange(M, device="cuda") % 3 == 0, 1.0, -1.0)
+    v[..., 1] = sign
+    mod = AgentAttention(1, h, d, max(N, M), 1, F32)
+    k[..., 3] = sign                                                      # (q has nothing there: all logits are 0)
+    out, lse = mod.attend(q, k, v, scale=1.0, need_lse=True)
+    g = mod.attend_backward(q, k, v, out, lse, do, scale=1.0)
+    f = lambda x: float(torch.tensor(x))  # noqa: E731  (as it is in fp32)
+    mean = float(sign.double().mean())
+    slope = f(0.9) / M * (sign.double() - mean)
+    sums = lambda columns: 2.0 ** -24 * (128 + columns / 4096) + 2.0 ** -20  # noqa: E731
+    assert (g["dv"][0, 0, :, 2].double() * M / (f(0.7) * N * h) - 1).abs().max() <= sums(N * h)
+    assert (g["dk"][0, 0, :, 1].double() / (slope * N * h * f(0.3)) - 1).abs().max() <= 4 * sums(N * h)       # (a slope: 2 / 3 or more of P, out of D with an error of P's)
+    assert (g["dq"][0, :, :, 3].double() / (slope * sign.double()).sum() - 1).abs().max() <= 4 * sums(M)
