@@ -56,6 +56,10 @@ template <int TPR, int N> __device__ __forceinline__ void row_sums(float (&s)[N]
     }
 }
 
+// Rows that a thread adds up before the sum joins others: equal numbers on a growing sum are rounded the same way each time, up to 2^-25 of it (2^21 rows of 2048 channels in
+// 592 blocks: 5e-5).
+constexpr int kMostRows = 256;
+
 // How a block's threads share rows
 template <int TPR> constexpr int kBlock = TPR > 32 ? TPR : 256;
 
@@ -262,11 +266,16 @@ template <typename T> __global__ void __launch_bounds__(256) norm_columns_kernel
     const long long first = a.rows * blockIdx.y / gridDim.y, last = a.rows * (blockIdx.y + 1) / gridDim.y;
     if (c >= C) return;
     float p = 0.f, q = 0.f;
-    for (long long r = first; r < last; ++r) {
-        const float2 s = __ldg(stats + r);
-        const float g = Elem<T>::to_f32(static_cast<const T*>(a.dy)[r * C + c]);
-        p = fmaf(g, (Elem<T>::to_f32(static_cast<const T*>(a.x)[r * C + c]) - s.x) * s.y, p);
-        q += g;
+    for (long long r0 = first; r0 < last; r0 += kMostRows) {
+        float u = 0.f, v = 0.f;
+        for (long long r = r0; r < min(last, r0 + kMostRows); ++r) {
+            const float2 s = __ldg(stats + r);
+            const float g = Elem<T>::to_f32(static_cast<const T*>(a.dy)[r * C + c]);
+            u = fmaf(g, (Elem<T>::to_f32(static_cast<const T*>(a.x)[r * C + c]) - s.x) * s.y, u);
+            v += g;
+        }
+        p += u;
+        q += v;
     }
     out[(long long)blockIdx.y * 2 * C + c] = p;
     out[(long long)blockIdx.y * 2 * C + C + c] = q;
@@ -278,9 +287,17 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const float* in, int sh
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
     float s = 0.f;
-    if (c < 2 * C)
+    const int first = (int)((long long)shares * warp / 32), last = (int)((long long)shares * (warp + 1) / 32);
+    if (c < 2 * C) {
+        const int most = min(last, first + kMostRows);
 #pragma unroll 16
-        for (int k = shares * warp / 32; k < shares * (warp + 1) / 32; ++k) s += in[(long long)k * 2 * C + c];
+        for (int k = first; k < most; ++k) s += in[(long long)k * 2 * C + c];
+        for (int k0 = most; k0 < last; k0 += kMostRows) {
+            float t = 0.f;
+            for (int k = k0; k < min(last, k0 + kMostRows); ++k) t += in[(long long)k * 2 * C + c];
+            s += t;
+        }
+    }
     part[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && c < 2 * C) {
@@ -331,11 +348,12 @@ NormPlan plan_of(int dtype, int C, bool aligned, bool back) {
     p.tpr = 0;
     return p;
 }
-// Blocks that walk the rows: as many as run at once
+// Blocks that walk the rows: as many as run at once; where the gains' gradients are sums of too many rows (kMostRows), a multiple of that
 long long blocks_of(const NormPlan& p, long long rows, int sm_count, bool back) {
     const int rpb = p.tpr > 32 ? 1 : 256 / p.tpr, f = p.nv * p.v;
     const int per = p.tpr == 512 ? (f <= 8 ? 2 : 1) : (f <= 8 ? (back ? 4 : 6) : f <= 16 ? (back ? 2 : 4) : back ? 1 : 2) * (p.tpr == 128 ? 2 : 1);       // kPerSm
-    return std::max(1LL, std::min((rows + rpb - 1) / rpb, (long long)sm_count * per));
+    const long long turns = (rows + rpb - 1) / rpb, wave = (long long)sm_count * per;
+    return turns <= wave ? turns : back ? wave * ((turns + wave * kMostRows - 1) / (wave * kMostRows)) : wave;
 }
 
 template <typename T, int TPR, int NV, int V, bool BACK> cudaError_t run_norm(const NormArgs& a, const NormPlan& p, int sm_count, cudaStream_t st) {

@@ -189,3 +189,20 @@ def test_gradient_buffers_that_alias_are_refused():
     assert mod.lib.agent_attn_layer_norm_backward(*args, x.data_ptr(), g.data_ptr(), None, ws.data_ptr(), ws.numel(), None) == 1
     torch.cuda.synchronize()
     assert (g == 0).all()
+
+
+@pytest.mark.parametrize("dt,rows,C", [(BF, 1 << 21, 2048), (F32, 1 << 17, 8192), (FH, 1 << 18, 1023), (BF, 1 << 16, 20001), (FH, (1 << 22) + 3, 8), (F32, 200704, 64)])
+def test_gain_gradients_of_equal_rows(dt, rows, C):
+    """Equal summands, which are rounded the same way at every step.  A sum of n of them is off by n 2^-25 at most: 256 rows of a thread, up to 256 shares of a warp in the join and
+    the warps' 32; x^ itself, the same in every row, by 2^-21."""
+    x = make(1, C, dt)[0].expand(rows, C).contiguous()
+    dy = torch.full((rows, C), 0.7, dtype=dt, device="cuda")
+    w, b = torch.ones(C, dtype=dt, device="cuda"), torch.zeros(C, dtype=dt, device="cuda")
+    g = handle(dt).layer_norm_backward(x, dy, w, b, need_input_grad=False)
+    X, d = x[0].double(), dy[0, 0].double()
+    m = X.mean()
+    r = 1 / ((X - m).square().mean() + 1e-5).sqrt()
+    xh, few = (X - m) * r, 2.0 ** -25 * (256 + min(256, rows / 256) + 64)
+    assert (g["db"].double() / (d * rows) - 1).abs().max() <= few
+    exh = 2.0 ** -21 * xh.abs() + 2.0 ** -22 * (X.abs() + X.abs().mean()) * r * (1 + xh.abs() / 4)
+    assert ((g["dw"].double() - d * rows * xh).abs() <= d * rows * (few * xh.abs() + exh)).all()
