@@ -448,8 +448,10 @@ int agent_attn_gated_backward_two_terms(agent_attn_handle* h, const agent_attn_g
  * change between replays of a captured call, and the kernels hold them to the tensors (offsets that
  * do not rise make results meaningless, but no access outside).
  * Logits, softmax and sums are fp32 (fp32 tensors: products as sums of bf16 terms, fp32 accuracy); 16-bit types round the
- * probabilities, and in the gradient dS, once to the element type.  A row whose logits have an infinity or a
- * NaN is NaN; an infinite or NaN value makes its channel non-finite in the rows that see it, and in no other.
+ * probabilities, and in the gradient dS, once to the element type.  A row whose logits have +infinity or a NaN is
+ * NaN.  A key whose logit is -infinity has weight 0 in the 16-bit types (a row of nothing else is NaN); in fp32 it makes the
+ * row NaN (elements from 3.39e38 on, which bf16 terms do not hold, count as infinite there).  An infinite or NaN value makes
+ * its channel non-finite in the rows that see it, and in no other.
  * In a gradient a number that is not finite may also reach rows of the sequence that do not see it. */
 typedef struct {
     const void *q;            /* device; element (b, head, token, c) at base + b * strides[0] + head * strides[1]

@@ -621,3 +621,33 @@ def test_gradient_long_sums_in_fp32(h, N, M, d):
     assert (g["dv"][0, 0, :, 2].double() * M / (f(0.7) * N * h) - 1).abs().max() <= sums(N * h)
     assert (g["dk"][0, 0, :, 1].double() / (slope * N * h * f(0.3)) - 1).abs().max() <= 4 * sums(N * h)       # (a slope: 2 / 3 or more of P, out of D with an error of P's)
     assert (g["dq"][0, :, :, 3].double() / (slope * sign.double()).sum() - 1).abs().max() <= 4 * sums(M)
+
+
+@pytest.mark.parametrize("dt", [BF, FH, F32])
+@pytest.mark.parametrize("N,M,d", [(1, 700, 64), (5, 700, 128), (200, 300, 64), (300, 200, 128)])
+def test_infinite_logits(dt, N, M, d):
+    """+infinity: a NaN row.  -infinity: weight 0 in 16 bits, what the formulas give; NaN in fp32.  A row of nothing but -infinity: NaN.  Other heads do not notice."""
+    q, k, v = make(1, 2, 2, N, M, d, dt)
+    q[..., 0] = q[..., 0].abs() + 1
+    mod = AgentAttention(1, 2, d, max(N, M), 1, dt)
+    plain, _ = mod.attend(q, k, v, need_lse=True)
+    up, down = k.clone(), k.clone()
+    up[0, 0, M // 2, 0] = float("inf")
+    down[0, 0, [3, M // 2, M - 1], 0] = -float("inf")
+    got = mod.attend(q, up, v)
+    assert got[0, 0].isnan().all() and torch.equal(got[0, 1], plain[0, 1])
+    got, lse = mod.attend(q, down, v, need_lse=True)
+    assert torch.equal(got[0, 1], plain[0, 1])
+    if dt is F32:
+        assert got[0, 0].isnan().all()
+    else:
+        keep = torch.ones(M, dtype=torch.bool, device="cuda")
+        keep[[3, M // 2, M - 1]] = False
+        for i in {0, N - 1}:
+            s = k[0, 0, keep].double() @ q[0, 0, i].double() * d ** -0.5
+            p, w = torch.softmax(s, 0), v[0, 0, keep].double()
+            assert ((got[0, 0, i].double() - p @ w).abs() <= 2 * u_of(dt) * (p @ w.abs()) + 1e-5).all()
+            assert abs(float(lse[0, 0, i].double() - torch.logsumexp(s, 0))) <= 1e-5
+    down[0, 0, :, 0] = -float("inf")
+    assert mod.attend(q, down, v)[0, 0].isnan().all()
+    assert mod.query_status() == 0
