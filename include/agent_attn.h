@@ -462,7 +462,7 @@ typedef struct {
     int queries, keys;        /* rows of a batch entry: 1 .. max_tokens                            */
     int kv_heads;             /* divides the handle's heads                                        */
     int causal;
-    float scale;              /* of the logits; 0: 1 / sqrt(head_dim)                              */
+    float scale;              /* of the logits, below 2^127; 0: 1 / sqrt(head_dim)                 */
     int sequences;            /* packed: their number; else 0                                      */
     const int *q_offsets, *k_offsets;   /* device [sequences + 1], rising, or both NULL            */
     const int *q_lengths, *k_lengths;   /* device [batch], or NULL (all); not with offsets         */

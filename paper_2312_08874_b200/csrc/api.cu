@@ -890,7 +890,8 @@ static int attend_args(agent_attn_handle* h, const agent_attn_sequences* s, Atte
     if (s->queries > h->cfg.max_tokens || s->keys > h->cfg.max_tokens)
         return fail(h, AA_ERR_UNSUPPORTED, "N=%d exceeds the handle's max_tokens=%d", std::max(s->queries, s->keys), h->cfg.max_tokens);
     if (s->kv_heads <= 0 || h->cfg.heads % s->kv_heads) return fail(h, AA_ERR_INVALID_ARG, "%d heads of keys do not divide %d heads", s->kv_heads, h->cfg.heads);
-    if (!(s->scale >= 0.f) || std::isinf(s->scale)) return fail(h, AA_ERR_INVALID_ARG, "scale must be finite and not negative");
+    // (the kernels take logits in units of log2, where a logit of zero times an infinite scale would be NaN)
+    if (!(s->scale >= 0.f) || std::isinf(s->scale * 1.4426950408889634f)) return fail(h, AA_ERR_INVALID_ARG, "scale must be not negative and finite times log2(e)");
     if (!s->q_offsets != !s->k_offsets) return fail(h, AA_ERR_INVALID_ARG, "offsets of queries and keys belong together");
     if (s->q_offsets) {
         if (h->cfg.batch != 1) return fail(h, AA_ERR_INVALID_ARG, "packed sequences need a handle of one batch entry, not %d", h->cfg.batch);

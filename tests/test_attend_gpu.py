@@ -651,3 +651,14 @@ def test_infinite_logits(dt, N, M, d):
     down[0, 0, :, 0] = -float("inf")
     assert mod.attend(q, down, v)[0, 0].isnan().all()
     assert mod.query_status() == 0
+
+
+def test_a_scale_whose_units_of_log2_are_infinite_is_refused():
+    q, k, v = make(1, 2, 2, 40, 40, 64, BF)
+    mod = AgentAttention(1, 2, 64, 40, 1, BF)
+    for scale in (2.5e38, 3.4e38):
+        with pytest.raises(AgentAttnError) as e:
+            mod.attend(torch.zeros_like(q), k, v, scale=scale)
+        assert e.value.status == 1
+    out = mod.attend(torch.zeros_like(q), k, v, scale=2.0 ** 126)                # (logits of zero: the mean)
+    assert ((out.double() - v.double().mean(2, keepdim=True)).abs() <= 2 * u_of(BF) * v.double().abs().mean(2, keepdim=True)).all()
