@@ -662,3 +662,34 @@ def test_a_scale_whose_units_of_log2_are_infinite_is_refused():
         assert e.value.status == 1
     out = mod.attend(torch.zeros_like(q), k, v, scale=2.0 ** 126)                # (logits of zero: the mean)
     assert ((out.double() - v.double().mean(2, keepdim=True)).abs() <= 2 * u_of(BF) * v.double().abs().mean(2, keepdim=True)).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF, FH])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("h,kv,d", [(2, 2, 64), (8, 1, 128), (3, 1, 40)])
+def test_few_queries_over_packed_keys(dt, causal, h, kv, d):
+    """Up to three queries each of packed sequences of 0 to 9000 keys: several shares of the keys, some of them without a key of a sequence."""
+    lengths, keys = [1, 2, 0, 1, 3, 1], [9000, 700, 30, 0, 2, 4001]
+    at, ak = [1], [5]
+    for n, m in zip(lengths, keys):
+        at.append(at[-1] + n)
+        ak.append(ak[-1] + m)
+    q, k, v = make(1, h, kv, at[-1] + 2, ak[-1] + 3, d, dt)
+    k[:, :, :5], v[:, :, ak[-1]:] = float("nan"), float("inf")
+    check(q, k, v, causal=causal, q_offsets=at, k_offsets=ak, grad=False)
+
+
+@pytest.mark.parametrize("dt", [BF, FH])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("S", [40, 128, 129])
+def test_gradient_of_many_long_packed_sequences(dt, causal, S):
+    """More sequences than a lane's first place holds, as many as take tiles by work, and one more."""
+    gen = torch.Generator().manual_seed(S)
+    lengths = [int(x) for x in torch.randint(1, 1200, (S,), generator=gen)]
+    lengths[3] = lengths[S - 2] = 0
+    at = [2]
+    for n in lengths:
+        at.append(at[-1] + n)
+    assert at[-1] / S >= 512
+    q, k, v = make(1, 2, 1, at[-1] + 9, at[-1] + 9, 64, dt, fused=True)
+    check(q, k, v, causal=causal, q_offsets=at)

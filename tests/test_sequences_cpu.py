@@ -176,3 +176,71 @@ def test_offsets_that_do_not_rise_stay_inside():
     for at in ([0, 100, 1 << 30], [-5, 100, 300], [0, 200, 100, 256], [1 << 30, 1 << 30], [256, 0, 256, 0, 256], [-(1 << 31), (1 << 31) - 1]):
         for unit, rows in ((1, 256), (3, 16), (1, 64)):
             slots(at, unit, rows, 256)
+
+
+def ranked(q_at, k_at, causal, keys, rows=128):
+    """The gradient's order of a packed call's tiles, restated: (sequence, tile) of every slot.  A lane holds the sequences lane, lane + 32, ..."""
+    nq, nk = [b - a for a, b in zip(q_at, q_at[1:])], [b - a for a, b in zip(k_at, k_at[1:])]
+    S = len(nq)
+    tiles = [((nk if keys else nq)[s] + rows - 1) // rows for s in range(S)]
+    div = lambda a, b: int(a / b)  # noqa: E731  (towards zero, as in C)
+
+    def at_least(s, units):
+        if units <= 0 or not tiles[s]:
+            return tiles[s]
+        ahead, need = nk[s] - nq[s], (units - 1) * 128 + 1
+        if not causal:
+            return tiles[s] if (nq if keys else nk)[s] >= need else 0
+        if keys:
+            most = min(nq[s] - need, nq[s] - need + ahead)
+            return 0 if most < 0 else min(tiles[s], div(max(0, nq[s] - need + ahead), rows) + 1)
+        if nk[s] < need:
+            return 0
+        return tiles[s] - min(tiles[s] - 1, max(0, div(need - ahead + rows - 1, rows) - 1))
+    count = lambda units: sum(at_least(s, units) for s in range(S))  # noqa: E731
+    found, slot = [], 0
+    while count(0) > slot:
+        lo, hi = 0, (max(q_at[-1], k_at[-1]) + 127) // 128 + 1
+        while hi - lo > 1:
+            mid = (lo + hi) >> 1
+            lo, hi = (mid, hi) if count(mid) > slot else (lo, mid)
+        left, hit = slot - count(hi), None
+        for i in range(4):                                               # (groups of 32 sequences, a lane's places)
+            mine = [(s, at_least(s, lo) - at_least(s, hi), at_least(s, hi)) for s in range(32 * i, min(S, 32 * i + 32))]
+            for s, some, more in mine:
+                if hit is None and 0 <= left < some:
+                    hit = (s, more + left if not causal or keys else tiles[s] - 1 - more - left)
+                left -= some
+        found.append(hit)
+        slot += 1
+    return found, [(s, t) for s in range(S) for t in range(tiles[s])]
+
+
+@pytest.mark.parametrize("keys", [False, True])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("most", [1, 7, 33, 70, 128])
+def test_ranked_tiles_are_found_once_each_and_fall_in_work(keys, causal, most):
+    gen = torch.Generator().manual_seed(most * 4 + 2 * causal + keys)
+    for trial in range(6):
+        S = most if trial < 2 else int(torch.randint(1, most + 1, (1,), generator=gen))
+        draw = lambda: [int(x) for x in torch.randint(0, 1500, (S,), generator=gen) * (torch.rand(S, generator=gen) < 0.8)]  # noqa: E731
+        nq = draw()
+        nk = nq if trial % 3 == 0 else draw() if trial % 3 == 1 else [a + b for a, b in zip(nq, draw())]
+        q_at, k_at = [0], [0]
+        for a, b in zip(nq, nk):
+            q_at.append(q_at[-1] + a)
+            k_at.append(k_at[-1] + b)
+        if q_at[-1] == 0 or k_at[-1] == 0:
+            continue
+        found, want = ranked(q_at, k_at, causal, keys)
+        assert sorted(found) == want
+
+        def work(s, t):                                                  # columns in units of 128
+            ahead = nk[s] - nq[s]
+            if keys:
+                n = nq[s] - (max(0, 128 * t - ahead) if causal else 0)
+            else:
+                n = min(nk[s], min(nq[s], 128 * t + 128) + ahead) if causal else nk[s]
+            return max(0, n + 127) // 128 if n > 0 else 0
+        works = [work(*x) for x in found]
+        assert all(a >= b for a, b in zip(works, works[1:])), (q_at, k_at)
