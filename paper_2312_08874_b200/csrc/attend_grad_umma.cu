@@ -440,22 +440,30 @@ __global__ void __launch_bounds__(GradUmma<BOXES, KEYS>::kThreads, GradUmma<BOXE
             tc_fence_after_sync();
             tmem_ld32(tt, o);
             tmem_ld_wait();
-            if (!KEYS && total == 1) {
-                // All keys of these rows are here: D = sum P dP.  Out of the result, which is rounded, it would be off by as much as the slopes of two or three keys
-                // differ (sequences of two: error of dQ and dK 2.4 of a rounding, so 1.4).  (The ring's second stage is free.)
+            if (!KEYS && j == 0 && whole <= COLS) {
+                // Rows whose keys are all in this tile (short sequences, the first rows of a causal one): D = sum P dP.  Out of the result, which is rounded, it would be off
+                // by as much as the slopes of two or three keys differ (sequences of two: error of dQ and dK 2.4 of a rounding, so 1.5).
                 float2 sum2 = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     sum2 = make_float2(p[i].x != 0.f ? fmaf(p[i].x, __uint_as_float(o[2 * i]), sum2.x) : sum2.x, p[i].y != 0.f ? fmaf(p[i].y, __uint_as_float(o[2 * i + 1]), sum2.y) : sum2.y);
-                float* share = reinterpret_cast<float*>(smem + G::OFF_RING + G::kOperand);
-                share[128 * w + local] = sum2.x + sum2.y;
-                asm volatile("bar.sync 1, %0;\n" ::"n"(128 * G::GROUPS) : "memory");
-                dot = 0.f;
-#pragma unroll
-                for (int i = 0; i < G::GROUPS; ++i) dot += share[128 * i + local];
-                dot *= is_f16<T> ? kHeldBack : 1.f;
-                if (w == 0 && row < rows) a.ws[2 * (((long long)q.batch * a.heads + mine) * a.N + q.first + row) + 1] = dot;
-                dot *= kappa;
+                float* share = reinterpret_cast<float*>(smem + G::OFF_DOT);          // two groups' shares of 128 rows, in place of the statistics, which all have read
+                float own = sum2.x + sum2.y;
+                auto meet = [] { asm volatile("bar.sync 1, %0;\n" ::"n"(128 * G::GROUPS) : "memory"); };
+                if (kDot) meet();
+                if (G::GROUPS > 2) {
+                    if (w >= 2) share[128 * (w - 2) + local] = own;
+                    meet();
+                    if (w < 2) own += share[128 * w + local];
+                    meet();
+                }
+                if (w < 2) share[128 * w + local] = own;
+                meet();
+                if (limit <= COLS) {
+                    dot = (share[local] + share[128 + local]) * (is_f16<T> ? kHeldBack : 1.f);
+                    if (w == 0 && row < rows) a.ws[2 * (((long long)q.batch * a.heads + mine) * a.N + q.first + row) + 1] = dot;
+                    dot *= kappa;
+                }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
