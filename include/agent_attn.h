@@ -474,7 +474,7 @@ typedef struct {
 size_t agent_attn_attend_workspace_bytes(const agent_attn_handle* h, const agent_attn_sequences* s, int backward);
 
 /* out  device, element type, strides out_strides;  lse  device fp32 [B][heads][queries], or NULL: natural
- * log-sum-exp of the logits, which the gradient takes.  No overlap of results with inputs.
+ * log-sum-exp of the logits, which the gradient takes (rows of no sequence as they were).  No overlap of results with inputs.
  * Errors: AA_ERR_INVALID_ARG, AA_ERR_UNSUPPORTED (tokens past max_tokens; queries x heads, or keys, past
  * 2^31 - 2^16 - 1, sequences x heads past 2^27 - 2^12), AA_ERR_WORKSPACE, AA_ERR_CUDA.  No host synchronisation, no allocation. */
 int agent_attn_attend(agent_attn_handle* h, const agent_attn_sequences* s, void* out, const long long out_strides[3],
@@ -496,7 +496,8 @@ int agent_attn_attend_backward(agent_attn_handle* h, const agent_attn_sequences*
 /* ------------------------------------------------------------------------------------------------
  * Layer norm of every row x of `channels` elements:
  *     y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * weight + bias
- * Of the handle it uses device and element type.  Sums are fp32, taken about the mean; y is rounded once. */
+ * Of the handle it uses device and element type.  Sums are fp32, taken about the mean (a row whose sum of squares leaves
+ * fp32, values past some 1e19, is not normalised); y is rounded once. */
 typedef struct {
     const void* x;            /* device [rows][channels], element type                             */
     const void* weight;       /* device [channels], or NULL (1)                                    */

@@ -878,7 +878,7 @@ class AgentAttention:
         on the device.  `causal`: the last query sees every key of its sequence, each one before it a key less.  A query without a key has the result 0.
 
         Returns the result, [B, heads, N, d] (token-major where q is), with `need_lse` also the log-sum-exp of the logits, fp32 [B, heads, N], which
-        `attend_backward` takes.  Rows of no sequence are zero in a new result and left as they are in `out`.
+        `attend_backward` takes.  Rows of no sequence are zero in a new result and left as they are in `out`; the log-sum-exp has no value there.
         """
         s, kept = self._call(q, k, v, causal, scale, q_offsets, k_offsets, q_lengths, k_lengths)
         if out is None:

@@ -669,7 +669,8 @@ int shares_of(const AttendArgs& a, bool few_16, int sm_count, int* chunk) {
     if (!few_rows(a)) return 1;
     const long long blocks = slots_of(a.q_offsets != nullptr, a.sequences, a.N, a.heads / a.kv_heads, 16) * a.kv_heads;
     // One wave of blocks (two an SM; up to 64 channels of 16 bits, three): a block's start and end cost as much as some 1000 keys.  16 caches of up to 16384 keys, 4 heads
-    // of keys of 128: 2 an SM 79 us, 4 86, 6 92, 12 97; 8 heads of 64 over 8192: 2 an SM 51, 3 45, 4 48, 8 51; one cache of 65536, 8 heads of 128: 47, 50, 61, 73.
+    // of keys of 128: one an SM 114 us, 2 75, 3 84, 4 83, 12 85; 8 heads of 64 over 8192: 70, 49, 49, 51, 51; one cache of 65536, 8 heads of 128: 56, 54, 64, 60, 74.
+    // fp32, bound by its loads (with 128 channels one block fits an SM): 567, 574, 473, 418, 441 (lengths even out); 291, 296, 297, 300, 293; 265, 263, 283, 272, 312.
     const long long want = std::max(1LL, (a.d <= 64 && few_16 ? 3LL : 2LL) * sm_count / blocks);
     long long c = (a.M + want - 1) / want;
     c = std::min(std::max(256LL, (c + 127) / 128 * 128), 4LL * kPieceKeys);      // (four warps take a piece each, see kPieceKeys)

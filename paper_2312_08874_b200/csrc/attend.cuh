@@ -65,8 +65,9 @@ constexpr int kPieceKeys = 16384;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // The exponents' reference of a row moves only when a logit exceeds it by more than kSlack (log2 units), so P is at most 2^kSlack.  f16, whose normal numbers end at
-// 2^-14 and whose last one is 2^-24, holds P times 2^kHeld, as much as its range leaves: keys far below a row's largest lose nothing before 2^-25 of it, and half a
+// 2^-14 and whose last one is 2^-24, holds P times 2^kHeld, as much as its range leaves: keys far below a row's largest lose no bits before 2^-25 of it, and half a
 // step of the last number is 2^-36 (the sum counts what P V would lose: 65536 keys 17.5 below one, 1.6e-3 of the result).  The factor leaves with the row's sum.
+// (The smaller slack: 8 heads of 8192 x 8192 x 128 281 us with logits that vary by 1, bf16 280; 313 where they vary by 3, bf16 291; 324 by 10, bf16 318.)
 template <typename T> constexpr bool is_f16 = sizeof(T) == 2 && !Elem<T>::kIsBf16;
 template <typename T> constexpr float kSlack = is_f16<T> ? 4.f : 8.f;
 template <typename T> constexpr float kHeld = is_f16<T> ? 11.f : 0.f;

@@ -3,8 +3,8 @@
 // A block takes two tiles of 128 queries of a head and walks the keys in tiles of 128 that both share.  Roles:
 //   warps 0-3, 4-7  a tile each: thread = query.  Logits come out of tensor memory into registers, 128 at a time; probabilities go back to tensor memory as the
 //                   A operand of P V.  The exponents' reference moves only when a logit exceeds it by more than kSlack: then the thread
-//                   rescales its row of the result in tensor memory.  Sums over long axes come in pieces (kPieceKeys).  Sums in fp32, of unrounded probabilities; probabilities are rounded to the type
-//                   (half a step each, independent of one another: sums over many keys see less).
+//                   rescales its row of the result in tensor memory.  Sums over long axes come in pieces (kPieceKeys).  Sums in fp32, of unrounded probabilities;
+//                   probabilities are rounded to the type (half a step each; sums over many keys see less, unless the keys are equal, which are rounded alike).
 //   warps 8, 11     issue the products of a tile of queries each: the logits of its next keys while its probabilities are made (up to 64 channels; above, the
 //                   logits take the place of the probabilities)
 //   warp 9          TMA: queries, keys and values
@@ -12,7 +12,7 @@
 //                   not finite (0 * infinity is NaN); the queries that do see these get their NaN at the end
 // Results are stored by rows of the sequence alone.
 //
-// Bound by the row warps up to 64 channels (special-function unit 69 % busy; 16 heads of 16384 x 16384 x 64 1452 to 1481 us, 742 to 757 TFLOP/s), by the chain products - exponentials - products above
+// Bound by the row warps up to 64 channels (special-function unit 69 % busy; 16 heads of 16384 x 16384 x 64 1451 to 1473 us, 746 to 758 TFLOP/s), by the chain products - exponentials - products above
 // (tensor pipe 51 %; 8 heads of 8192 x 8192 x 128 281 us, 977 TFLOP/s; causal, 16 heads on 4 of keys 273, 1007), and by starts and ends of blocks on short sequences, one block an SM.
 #include "attend_umma.cuh"
 
